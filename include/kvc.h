@@ -116,6 +116,9 @@ kvc_status kvc_book_append_free_closed(kvc_book* book, const int32_t* n_new, con
 kvc_status kvc_book_compress(kvc_book* book, const int32_t* seq, const int64_t* cl, const int64_t* cr,
                              int n_spans);
 
+/* The bookkeeping of kvc_evict (same arguments, checks and errors). */
+kvc_status kvc_book_evict(kvc_book* book, const int64_t* keep, const int64_t* recent);
+
 /* Closed spans of `seq` that are not yet freed: up to `max` (cl, cr) pairs; *n gets the count. */
 kvc_status kvc_book_pending_spans(const kvc_book* book, int seq, int64_t* cl, int64_t* cr, int64_t max,
                                   int64_t* n);
@@ -136,7 +139,9 @@ kvc_status kvc_book_lengths(const kvc_book* book, int64_t* len_out, int64_t* att
 
 /* The full history of `seq` (kinds, positions, n_full = tokens so far), which history tokens the
  * query at the last token attends to under the mask (visible_full), and the stored rows in order
- * as history indices and positions (n_stored).  Buffers hold `cap` entries each (host). */
+ * as history indices and positions (n_stored).  Buffers hold `cap` entries each (host).  After an
+ * eviction the rows below the recent ones differ between heads: they are listed as -1, and the
+ * tokens they stand for are not marked visible. */
 kvc_status kvc_book_layout(const kvc_book* book, int seq, int64_t cap, uint8_t* kind_full, int32_t* pos_full,
                            uint8_t* visible_full, int64_t* n_full, int32_t* stored_orig_idx, int32_t* stored_pos,
                            int64_t* n_stored);
@@ -268,6 +273,68 @@ kvc_status kvc_decode_attention_layers(kvc_cache* cache, int first, int n_layers
  *     counters it relies on before its kernel runs, on `stream`. */
 kvc_status kvc_decode_attention_static_scratch(kvc_cache* cache, int layer, const void* q, float scale, float* out,
                                                void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Accumulated attention weights, and eviction by them.                       */
+/* ------------------------------------------------------------------------ */
+
+/* Attaches a score per stored row and (layer, head): device fp32 [M][H * C] in the rows' layout,
+ * 16-byte aligned, the caller's, to live until it is replaced or the cache is destroyed; NULL detaches.
+ * Slots without a row hold 0 on attaching and are kept so: appended rows start at 0, and rows that are
+ * freed or evicted leave 0 behind.  kvc_compress_spans and kvc_evict move the scores with their rows
+ * (kvc_compress_spans in one more kernel).  Between calls the caller may change the scores of stored
+ * rows, on the stream of the calls.  KVC_ERR_UNSUPPORTED under KVC_POLICY_LOCAL. */
+kvc_status kvc_set_scores(kvc_cache* cache, float* scores);
+
+/* kvc_decode_attention_layers that also adds to the score of every row its attention weight,
+ *   score_j += softmax_j(scale * <q, k_j>),
+ * of each (layer, sequence, head).  Hidden rows get nothing.  One launch over all layers, whatever the
+ * lengths; one addition per row, so the scores do not depend on the order of the work. */
+kvc_status kvc_decode_attention_scored(kvc_cache* cache, int first, int n_layers, const void* q, int64_t q_layer_stride,
+                                       float scale, float* out, int64_t out_layer_stride, void* stream);
+
+/* Evicts rows of the sequences s with keep[s] >= 0 that store more than keep[s] rows: every (layer, head)
+ * stream keeps its last recent[s] rows and the keep[s] - recent[s] others with the largest scores (equal
+ * ones: the lower rows; a NaN counts below every number, and a score of +infinity pins its row).
+ *   keep, recent: host [b], 1 <= recent[s] <= keep[s] where keep[s] >= 0.
+ *   kept: device int32 [M][H * C] in the rows' layout, or NULL: for each row that is left the number that
+ *     it had before the call (written for the evicted sequences only).
+ * The streams of a sequence go on with rows of different tokens.  Of the rows below the recent ones, those
+ * that stay below row keep - recent keep their places, and the holes are filled, in order, by those that
+ * stay beyond it; the recent rows follow in their order.  pos and orig of the rows below the recent ones
+ * become -1.  Attention, appends, spans among the recent and later tokens, compaction and prefills of later
+ * tokens work on as before.
+ * Errors: KVC_ERR_STATE without scores, with layers of the last tokens not written, or where an open span
+ * or one that is closed and not freed reaches before the recent rows; KVC_ERR_UNSUPPORTED under
+ * KVC_POLICY_LOCAL. */
+kvc_status kvc_evict(kvc_cache* cache, const int64_t* keep, const int64_t* recent, int32_t* kept, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Sequences that share a prefix.                                             */
+/* ------------------------------------------------------------------------ */
+
+/* Makes the sequences of `prefix` prefixes of this cache's: the rows of sequence parent[s] of `prefix`
+ * come before the own rows of sequence s (parent[s] = -1: none), as for the samples of one prompt, whose
+ * rows are then stored, and read by a step, once for all of them.  The caches agree in M, H, d_head, dtype
+ * and rotation and share a stream; capacities and batch differ as they like.
+ *   parent: host [b], copied.
+ *   scratch: device, 256-byte aligned, kvc_prefix_scratch_bytes(cache) bytes, the cache's until another
+ *     prefix is set or the cache is destroyed.
+ * The prefix may grow, be compacted or evicted between calls, and outlives its use here; NULL for `prefix`
+ * ends it (parent and scratch are then ignored).  Positions are the caller's: append the own tokens at the
+ * positions that continue the prefix's. */
+size_t kvc_prefix_scratch_bytes(const kvc_cache* cache);
+kvc_status kvc_set_prefix(kvc_cache* cache, kvc_cache* prefix, const int32_t* parent, void* scratch,
+                          size_t scratch_bytes);
+
+/* kvc_decode_attention_layers over the rows of each sequence's prefix and its own: the query of sequence s,
+ * its last own token, sees every stored row of its prefix (a <CL> query none: it sees itself) and of its own
+ * rows those that the decode shows it.  Sequences without own tokens are skipped.  q and each layer's part of
+ * it are 16-byte aligned.
+ * Errors, besides the decode's: KVC_ERR_STATE without a prefix, where a prefix has a span that is open or
+ * closed and not freed, or where its layers are not written. */
+kvc_status kvc_decode_attention_shared(kvc_cache* cache, int first, int n_layers, const void* q, int64_t q_layer_stride,
+                                       float scale, float* out, int64_t out_layer_stride, void* stream);
 
 /* Masked prefill attention of layer `layer` on the tensor cores (Sec. 3.1: the modified causal
  * mask holds for every token of a prompt; Manipulating Key-Value Memory: a long prefix may be run

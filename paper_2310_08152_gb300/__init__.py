@@ -72,6 +72,16 @@ def stream_handle(stream=None) -> int:
     return _stream_handle(stream)
 
 
+def _per_seq(a, b: int, name: str):
+    """One int64 for each of b sequences; a single number stands for all of them."""
+    a = np.asarray(a, dtype=np.int64)
+    if a.ndim == 0:
+        return np.full(b, a, np.int64)
+    if a.shape != (b,):
+        raise ValueError(f"{name} must be a number or have {b} elements, got shape {a.shape}")
+    return np.ascontiguousarray(a)
+
+
 def _dev(t, name, dtype=None, numel=None):
     if not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous CUDA tensor")
@@ -121,6 +131,11 @@ def kvc_book_append_free_closed(book: int, n_new, kinds, pos):
 def kvc_book_compress(book: int, seq, cl, cr):
     seq, cl, cr = _np(seq, np.int32), _np(cl, np.int64), _np(cr, np.int64)
     _check(lib().kvc_book_compress(book, seq.ctypes.data, cl.ctypes.data, cr.ctypes.data, seq.size))
+
+
+def kvc_book_evict(book: int, keep, recent):
+    keep, recent = _np(keep, np.int64), _np(recent, np.int64)
+    _check(lib().kvc_book_evict(book, keep.ctypes.data, recent.ctypes.data))
 
 
 def kvc_book_pending_spans(book: int, seq: int):
@@ -204,6 +219,11 @@ class Book:
         if self.readonly:
             raise KvcError(5, "a cache's book is read-only; compress through the cache")
         kvc_book_compress(self.handle, seq, cl, cr)
+
+    def evict(self, keep, recent):
+        if self.readonly:
+            raise KvcError(5, "a cache's book is read-only; evict through the cache")
+        kvc_book_evict(self.handle, _per_seq(keep, self.b, "keep"), _per_seq(recent, self.b, "recent"))
 
     def pending_spans(self, seq: int):
         return kvc_book_pending_spans(self.handle, seq)
@@ -315,6 +335,39 @@ def kvc_decode_attention_static_scratch(cache: int, layer: int, q, scale: float,
                                                      _stream_handle(stream)))
 
 
+def kvc_set_scores(cache: int, scores):
+    _check(lib().kvc_set_scores(cache, _ptr(scores)))
+
+
+def kvc_decode_attention_scored(cache: int, first: int, n_layers: int, q, q_layer_stride: int, scale: float, out,
+                                out_layer_stride: int, stream=None):
+    """kvc_decode_attention_layers that adds each row's attention weight to its score."""
+    _check(lib().kvc_decode_attention_scored(cache, first, n_layers, _ptr(q), int(q_layer_stride), float(scale), _ptr(out),
+                                             int(out_layer_stride), _stream_handle(stream)))
+
+
+def kvc_prefix_scratch_bytes(cache: int) -> int:
+    return lib().kvc_prefix_scratch_bytes(cache)
+
+
+def kvc_set_prefix(cache: int, prefix, parent, scratch):
+    parent = _np(parent, np.int32) if parent is not None else None
+    n = 0 if scratch is None else scratch.numel() * scratch.element_size()
+    _check(lib().kvc_set_prefix(cache, prefix, _ptr(parent), _ptr(scratch), n))
+
+
+def kvc_decode_attention_shared(cache: int, first: int, n_layers: int, q, q_layer_stride: int, scale: float, out,
+                                out_layer_stride: int, stream=None):
+    """kvc_decode_attention_layers over each sequence's prefix (kvc_set_prefix) and its own rows."""
+    _check(lib().kvc_decode_attention_shared(cache, first, n_layers, _ptr(q), int(q_layer_stride), float(scale), _ptr(out),
+                                             int(out_layer_stride), _stream_handle(stream)))
+
+
+def kvc_evict(cache: int, keep, recent, kept=None, stream=None):
+    keep, recent = _np(keep, np.int64), _np(recent, np.int64)
+    _check(lib().kvc_evict(cache, keep.ctypes.data, recent.ctypes.data, _ptr(kept), _stream_handle(stream)))
+
+
 def kvc_prefill_attention(cache: int, layer: int, q, n_q, scale: float, out, stream=None):
     n_q = _np(n_q, np.int32)
     _check(lib().kvc_prefill_attention(cache, layer, _ptr(q), n_q.ctypes.data, float(scale), _ptr(out),
@@ -414,6 +467,8 @@ class KVCache:
                 lib().kvc_thread_capture_mode(mode)
             kvc_set_staging(self.handle, self.staging)
         self.book = Book(self.b, cap, policy, _handle=lib().kvc_get_book(self.handle))
+        self.scores = None
+        self.prefix = None
 
     # views of the device layout (rows of d_head elements)
     def k_plane(self, layer: int):
@@ -488,6 +543,81 @@ class KVCache:
         _dev(out, "out", torch.float32, self.M * self.b * self.H * self.d)
         n = self.b * self.H * self.d
         kvc_decode_attention_layers(self.handle, 0, self.M, q, n, scale, out, n, stream)
+        return out
+
+    def _layers(self, q, out, first: int, n_layers):
+        """The number of layers of a call over layers from `first` on (all that follow unless given), and its output."""
+        import torch
+
+        n_layers = self.M - first if n_layers is None else n_layers
+        n = n_layers * self.b * self.H * self.d
+        _dev(q, "q", self.torch_dtype, n)
+        if out is None:
+            out = torch.empty(n_layers, self.b, self.H, self.d, dtype=torch.float32, device=q.device)
+        return n_layers, _dev(out, "out", torch.float32, n)
+
+    # eviction by accumulated attention weight
+    def attach_scores(self, scores=None):
+        """Gives every stored row of every (layer, head) a score: `scores`, fp32 and zero where no row is stored, in the
+        layout of the rows ([M, H * C]), or a new zeroed tensor.  The cache keeps and returns it."""
+        import torch
+
+        if scores is None:
+            scores = torch.zeros(self.M, self.H * self.C, dtype=torch.float32, device=self.k.device)
+        _dev(scores, "scores", torch.float32, self.M * self.H * self.C)
+        kvc_set_scores(self.handle, scores)
+        self.scores = scores
+        return scores
+
+    def detach_scores(self):
+        kvc_set_scores(self.handle, None)
+        self.scores = None
+
+    def score_rows(self, layer: int, s: int, h: int, n: int):
+        """The scores of rows [0, n) of sequence s, head h in a layer."""
+        return self.stream_rows(self.scores.view(self.M, self.H * self.C)[layer], s, h, n)
+
+    def decode_attention_scored(self, q, scale: float, out=None, stream=None, first: int = 0, n_layers=None):
+        """Decode attention of layers [first, first + n_layers) that adds each row's weight to its score: q and out
+        [n_layers][b][H][d_head]; every layer from `first` on unless n_layers is given."""
+        n_layers, out = self._layers(q, out, first, n_layers)
+        n = self.b * self.H * self.d
+        kvc_decode_attention_scored(self.handle, first, n_layers, q, n, scale, out, n, stream)
+        return out
+
+    def evict(self, keep, recent, kept=None, stream=None):
+        """Brings every (layer, head) stream of the sequences with keep >= 0 down to `keep` rows: its last `recent` ones
+        and those with the largest scores.  keep, recent: a number, or one per sequence; kept: int32 [M, H * C] for the
+        earlier number of each row that is left."""
+        if kept is not None:
+            import torch
+
+            _dev(kept, "kept", torch.int32, self.M * self.H * self.C)
+        kvc_evict(self.handle, _per_seq(keep, self.b, "keep"), _per_seq(recent, self.b, "recent"), kept, stream)
+
+    # sequences that share a prefix
+    def set_prefix(self, prefix: Optional["KVCache"], parent=None):
+        """The rows of sequence parent[s] of the cache `prefix` come before the own rows of sequence s (-1: none do): the
+        samples of one prompt, whose rows are stored and read once.  None ends it.  The cache keeps `prefix` alive."""
+        import torch
+
+        if prefix is None:
+            kvc_set_prefix(self.handle, None, None, None)
+            self.prefix = self._prefix_scratch = None
+            return
+        parent = np.asarray(parent, np.int32)
+        if parent.shape != (self.b,):
+            raise ValueError(f"parent must have {self.b} elements, got shape {parent.shape}")
+        scratch = torch.empty(kvc_prefix_scratch_bytes(self.handle), dtype=torch.uint8, device=self.k.device)
+        kvc_set_prefix(self.handle, prefix.handle, parent, scratch)
+        self.prefix, self._prefix_scratch = prefix, scratch
+
+    def decode_attention_shared(self, q, scale: float, out=None, stream=None, first: int = 0, n_layers=None):
+        """Decode attention of layers [first, first + n_layers) over each sequence's prefix and its own rows: q and out
+        [n_layers][b][H][d_head]; every layer from `first` on unless n_layers is given."""
+        n_layers, out = self._layers(q, out, first, n_layers)
+        n = self.b * self.H * self.d
+        kvc_decode_attention_shared(self.handle, first, n_layers, q, n, scale, out, n, stream)
         return out
 
     def masked_reference_layout(self, seq: int, stream=None):

@@ -44,6 +44,7 @@ SIGNATURES = [
     ("kvc_book_append", c_int, [P, P, P, P]),
     ("kvc_book_append_free_closed", c_int, [P, P, P, P]),
     ("kvc_book_compress", c_int, [P, P, P, P, c_int]),
+    ("kvc_book_evict", c_int, [P, P, P]),
     ("kvc_book_pending_spans", c_int, [P, c_int, P, P, c_int64, P]),
     ("kvc_book_lengths", c_int, [P, P, P]),
     ("kvc_book_prefill_keys", c_int, [P, c_int, c_int64, P, c_int64, P]),
@@ -62,6 +63,12 @@ SIGNATURES = [
     ("kvc_decode_attention", c_int, [P, c_int, P, c_float, P, P]),
     ("kvc_decode_attention_static_scratch", c_int, [P, c_int, P, c_float, P, P]),
     ("kvc_decode_attention_layers", c_int, [P, c_int, c_int, P, c_int64, c_float, P, c_int64, P]),
+    ("kvc_set_scores", c_int, [P, P]),
+    ("kvc_decode_attention_scored", c_int, [P, c_int, c_int, P, c_int64, c_float, P, c_int64, P]),
+    ("kvc_prefix_scratch_bytes", c_size_t, [P]),
+    ("kvc_set_prefix", c_int, [P, P, P, P, c_size_t]),
+    ("kvc_decode_attention_shared", c_int, [P, c_int, c_int, P, c_int64, c_float, P, c_int64, P]),
+    ("kvc_evict", c_int, [P, P, P, P, P]),
     ("kvc_prefill_attention", c_int, [P, c_int, P, P, c_float, P, P]),
     ("kvc_masked_reference_layout", c_int, [P, c_int, c_int64, P, P, P, P, P, P, P, P]),
     ("kvc_device_status", c_int, [P, P, P]),

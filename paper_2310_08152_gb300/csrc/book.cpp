@@ -214,11 +214,88 @@ int Book::find_span(const Seq& q, int64_t cl) const {
 
 int64_t Book::stored_index(int s, int64_t j) const {
   const Seq& q = seqs_[s];
+  if (j < q.first_named) return -1;
   // freed ranges are sorted and disjoint: count freed rows before j
   auto it = std::upper_bound(q.freed.begin(), q.freed.end(), std::make_pair(j, INT64_MAX));
   size_t k = (size_t)(it - q.freed.begin());  // ranges with lo <= j
   if (k > 0 && j < q.freed[k - 1].second) return -1;
-  return j - q.freed_before[k];
+  return q.unnamed + (j - q.first_named) - q.freed_before[k];
+}
+
+int64_t Book::named_token(int s, int64_t row) const {
+  const Seq& q = seqs_[s];
+  int64_t a = q.first_named, z = (int64_t)q.kind.size();
+  while (a < z) {  // the first token whose row, or the row after it where it was freed, is `row` or a later one
+    const int64_t mid = a + (z - a) / 2;
+    auto it = std::upper_bound(q.freed.begin(), q.freed.end(), std::make_pair(mid, INT64_MAX));
+    const size_t k = (size_t)(it - q.freed.begin());
+    int64_t gone = q.freed_before[k];
+    if (k > 0 && mid < q.freed[k - 1].second) gone -= q.freed[k - 1].second - mid;
+    if (q.unnamed + (mid - q.first_named) - gone < row)
+      a = mid + 1;
+    else
+      z = mid;
+  }
+  auto it = std::upper_bound(q.freed.begin(), q.freed.end(), std::make_pair(a, INT64_MAX));
+  if (it != q.freed.begin() && a < (it - 1)->second) a = (it - 1)->second;
+  return a;
+}
+
+bool Book::plan_evict(const int64_t* keep, const int64_t* recent, std::vector<EvictSeq>& plan, std::string& err,
+                      int& code) const {
+  char buf[256];
+  plan.clear();
+  for (int s = 0; s < b_; ++s) {
+    if (keep[s] < 0) continue;
+    const Seq& q = seqs_[s];
+    if (recent[s] < 1 || recent[s] > keep[s]) {
+      std::snprintf(buf, sizeof buf, "sequence %d: recent = %lld outside [1, keep = %lld]", s, (long long)recent[s],
+                    (long long)keep[s]);
+      err = buf;
+      code = 1;
+      return false;
+    }
+    if (q.stored <= keep[s]) continue;
+    const int64_t row0 = std::max(q.stored - recent[s], q.unnamed);
+    const int64_t first = named_token(s, row0);
+    for (const Span& sp : q.spans) {
+      if (sp.freed || sp.cl >= first) continue;
+      std::snprintf(buf, sizeof buf,
+                    "sequence %d: the span opened at token %lld reaches before the %lld recent rows (free it, or keep "
+                    "more recent rows)",
+                    s, (long long)sp.cl, (long long)recent[s]);
+      err = buf;
+      code = 5;
+      return false;
+    }
+    EvictSeq e;
+    e.s = s;
+    e.len_old = q.stored;
+    e.keep = keep[s];
+    e.recent = recent[s];
+    plan.push_back(e);
+  }
+  return true;
+}
+
+void Book::apply_evict(const std::vector<EvictSeq>& plan) {
+  for (const EvictSeq& e : plan) {
+    Seq& q = seqs_[e.s];
+    const int64_t row0 = std::max(q.stored - e.recent, q.unnamed);
+    const int64_t first = named_token(e.s, row0);
+    const int64_t named = q.stored - row0;
+    q.freed.erase(q.freed.begin(), std::lower_bound(q.freed.begin(), q.freed.end(), std::make_pair(first, (int64_t)0)));
+    q.first_named = first;
+    q.unnamed = e.keep - named;
+    q.stored = e.keep;
+    rebuild_prefix(q);
+  }
+}
+
+bool Book::all_visible(int s) const {
+  for (const Span& sp : seqs_[s].spans)
+    if (!sp.freed) return false;
+  return true;
 }
 
 void Book::rebuild_prefix(Seq& q) {
@@ -321,7 +398,8 @@ bool Book::decode_view(int s, DecodeView& v, std::string& err) const {
     v.wrap = q.cap - v.begin;
     return true;
   }
-  if (q.kind[tq] == CL) {  // a <CL> attends only to itself (Sec. 3.1)
+  v.is_cl = q.kind[tq] == CL;
+  if (v.is_cl) {  // a <CL> attends only to itself (Sec. 3.1)
     v.begin = q.stored - 1;
     return true;
   }
@@ -428,7 +506,8 @@ void Book::visible(int s, uint8_t* vis) const {
     for (int64_t j = 0; j < T; ++j) vis[j] = (uint8_t)(j == tq);
     return;
   }
-  for (int64_t j = 0; j < T; ++j) vis[j] = (uint8_t)!(policy_ == POLICY_PAPER && q.kind[j] == CL);
+  for (int64_t j = 0; j < T; ++j)
+    vis[j] = (uint8_t)(j >= q.first_named && !(policy_ == POLICY_PAPER && q.kind[j] == CL));
   for (const Span& sp : q.spans)
     if (sp.cr >= 0 && sp.cr < tq)
       for (int64_t j = sp.cl + 1; j < sp.cr; ++j) vis[j] = 0;
@@ -446,7 +525,9 @@ void Book::stored_rows(int s, std::vector<int32_t>& orig, std::vector<int32_t>& 
     }
     return;
   }
-  for (int64_t j = 0; j < (int64_t)q.kind.size(); ++j) {
+  orig.assign((size_t)q.unnamed, -1);
+  pos.assign((size_t)q.unnamed, -1);
+  for (int64_t j = q.first_named; j < (int64_t)q.kind.size(); ++j) {
     if (stored_index(s, j) >= 0) {
       orig.push_back((int32_t)j);
       pos.push_back(q.pos[j]);

@@ -33,7 +33,17 @@ struct DecodeView {
   int64_t mask_hi = 0;
   int64_t wrap = INT64_MAX;
   int32_t qpos = 0;
+  bool is_cl = false;  // a <CL> query: it sees its own row only
   int64_t attended() const { return len - begin - (mask_hi - mask_lo); }
+};
+
+// One sequence's part of an eviction: of its len_old stored rows, every (layer, head) stream keeps the last `recent`
+// and the keep - recent others with the largest scores.
+struct EvictSeq {
+  int s = 0;
+  int64_t len_old = 0;
+  int64_t keep = 0;
+  int64_t recent = 0;
 };
 
 // One sequence's part of a compaction: drop ranges in history-index space (sorted, disjoint).
@@ -75,6 +85,14 @@ class Book {
                      std::string& err) const;
   void apply_compress(const std::vector<CompactSeq>& plan, const int32_t* seq, const int64_t* cl, int n);
 
+  // Eviction to keep[s] rows, the last recent[s] of them untouched, of the sequences with keep[s] >= 0 that store
+  // more.  The rows below the recent ones differ between streams from then on: they are counted, no longer told
+  // apart ("unnamed"), and the tokens before the first recent row have no stored row of their own.
+  bool plan_evict(const int64_t* keep, const int64_t* recent, std::vector<EvictSeq>& plan, std::string& err, int& code) const;
+  void apply_evict(const std::vector<EvictSeq>& plan);
+  // Rows of sequence s that evictions have left unnamed (its first ones).
+  int64_t unnamed(int s) const { return seqs_[s].unnamed; }
+
   // The decode query of sequence s (its last token).  False (with `err`) if the rows hidden from it
   // are not one contiguous run of stored rows.
   bool decode_view(int s, DecodeView& v, std::string& err) const;
@@ -88,8 +106,11 @@ class Book {
   static constexpr int32_t kPrefillNever = 0x3FFFFFFF;
   bool prefill_keys(int s, int64_t n_q, std::vector<int32_t>& meta, std::string& err) const;
 
+  // Whether the next normal token of sequence s sees every stored row (no span is open or closed and not freed).
+  bool all_visible(int s) const;
+
   void pending_spans(int s, std::vector<std::pair<int64_t, int64_t>>& out) const;
-  // history index -> stored row (or -1 when freed)
+  // history index -> stored row (or -1 when freed, or before the first named row of an evicted sequence)
   int64_t stored_index(int s, int64_t j) const;
   // visibility of every history token to the query at the last token
   void visible(int s, uint8_t* vis) const;
@@ -106,10 +127,14 @@ class Book {
     bool open = false;
     int64_t stored = 0;
     int64_t cap = 0;
-    std::vector<std::pair<int64_t, int64_t>> freed;  // sorted freed history ranges
+    int64_t unnamed = 0;       // stored rows [0, unnamed) stand for some tokens of history [0, first_named)
+    int64_t first_named = 0;
+    std::vector<std::pair<int64_t, int64_t>> freed;  // sorted freed history ranges, from first_named on
     std::vector<int64_t> freed_before;               // prefix sums of freed lengths
   };
   void rebuild_prefix(Seq& q);
+  // history index of the token at stored row `row` (unnamed <= row < stored)
+  int64_t named_token(int s, int64_t row) const;
   int find_span(const Seq& q, int64_t cl) const;
 
   int b_;

@@ -37,12 +37,20 @@ struct BF16T {
 // [-pi, pi], come from the hardware approximation, whose absolute error there (about 2^-21) is
 // far below the 16-bit rounding of the rotated values (2^-11 relative for fp16).
 // ---------------------------------------------------------------------------------------------
-__device__ __forceinline__ void rope_sincos(int32_t pos, float2 g, float* s, float* c) {
+__device__ __forceinline__ float rope_turns(int32_t pos, float2 g) {
   const float p = (float)pos;
   const float a = __fmul_rn(p, g.x);
   const float e = __fmaf_rn(p, g.x, -a);
-  const float f = __fadd_rn(__fsub_rn(a, rintf(a)), __fmaf_rn(p, g.y, e));
-  __sincosf(6.28318530717958647692f * f, s, c);
+  return __fadd_rn(__fsub_rn(a, rintf(a)), __fmaf_rn(p, g.y, e));
+}
+__device__ __forceinline__ void rope_sincos(int32_t pos, float2 g, float* s, float* c) {
+  __sincosf(6.28318530717958647692f * rope_turns(pos, g), s, c);
+}
+// The same to the last bits of binary32, where the rotated query is not rounded to 16 bits and the outputs are held to
+// more than that: the approximation's 2^-21 was half of the output's error (1.4e-6 against 64 bits, 8 samples of a prefix
+// of 800 rows).
+__device__ __forceinline__ void rope_sincos_full(int32_t pos, float2 g, float* s, float* c) {
+  sincospif(2.f * rope_turns(pos, g), s, c);
 }
 
 // ---------------------------------------------------------------------------------------------

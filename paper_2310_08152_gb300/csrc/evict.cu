@@ -1,0 +1,379 @@
+// Eviction by accumulated attention weight: every (layer, head) stream of a sequence keeps its recent rows and, of the
+// others, those whose scores are largest.
+//
+// A stream of n rows keeps `keep`, the last `recent` of them whatever their scores.  Of its n - recent candidates the
+// A = keep - recent with the largest scores stay (ties: the lower row; a NaN counts below every number).  Attention does
+// not depend on the order of the rows, so as few as possible move: the candidates that stay and lie below row A stay
+// where they are, the j-th row below A that goes is replaced by the j-th candidate beyond it that stays, and the recent
+// rows, whose order the span bookkeeping relies on, move down behind them.
+//
+// One CTA, or a cluster where there are few streams, per stream:
+//   1. the A-th largest score by radix selection (11 + 11 + 10 bits of the scores' ordered bit patterns, kept in shared
+//      memory), stopping at the first digit whose bin stays whole;
+//   2. two scans in row order, over the rows below A and over those beyond, list the holes and the rows that fill them;
+//      the copies of one list's rows are disjoint from each other, so they need no barrier between them;
+//   3. the recent rows move down in ascending chunks, a barrier between each chunk's loads and its stores.
+// What bounds it: HBM, for the rows that move, and for evictions of few rows the selection, some barriers per stream.
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <atomic>
+#include <cstdint>
+
+#include "device_common.cuh"
+#include "kernels.hpp"
+
+namespace kvc {
+namespace {
+
+constexpr unsigned kFull = 0xFFFFFFFFu;
+constexpr int kThreads = 256;
+constexpr int kWarps = kThreads / 32;
+constexpr int kScan = 4 * kThreads;  // candidates of one scan step
+constexpr int kBins = 2048;
+constexpr int kMaxHeldKeys = 40 * 1024;  // candidates whose keys stay in shared memory (160 KB); else they are read again
+constexpr int kMaxCluster = 8;
+
+// A score's order as an unsigned number: a NaN below everything, -0 and +0 equal.
+__device__ __forceinline__ uint32_t order_key(float x) {
+  if (x != x) return 0u;
+  const uint32_t u = __float_as_uint(x == 0.f ? 0.f : x);
+  return (u >> 31) ? ~u : u | 0x80000000u;
+}
+
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+struct EvictShared {
+  union {
+    uint32_t hist[kBins];
+    struct {
+      int32_t holes[kScan];
+    } l;
+  };
+  int32_t srcs[2 * kScan];
+  uint32_t wsum[kWarps];
+  uint32_t bin, above, in_bin;
+};
+
+// Exclusive prefix of one value per thread over the block, and the block's sum (two barriers).
+__device__ __forceinline__ uint32_t block_scan(uint32_t v, EvictShared& sh, uint32_t* sum) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint32_t incl = v;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const uint32_t u = __shfl_up_sync(kFull, incl, d);
+    if (lane >= d) incl += u;
+  }
+  if (lane == 31) sh.wsum[warp] = incl;
+  __syncthreads();
+  uint32_t before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    const uint32_t x = sh.wsum[w];
+    before += w < warp ? x : 0u;
+    all += x;
+  }
+  __syncthreads();
+  *sum = all;
+  return before + incl - v;
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads) evict_kernel(Geometry g, Static st, Buffers buf, float* __restrict__ scores,
+                                                         const AffSeq* __restrict__ aff, int32_t* __restrict__ kept,
+                                                         int held, int CN) {
+  constexpr int VPR = D / 8;  // 16-byte vectors per row
+  extern __shared__ __align__(16) uint32_t keys[];
+  __shared__ EvictShared sh;
+  const int tid = threadIdx.x;
+  const int rank = CN > 1 ? (int)(blockIdx.x % (unsigned)CN) : 0;
+  const int unit = CN > 1 ? (int)(blockIdx.x / (unsigned)CN) : (int)blockIdx.x;
+  const int streams = g.M * g.H;
+  const AffSeq a = aff[unit / streams];
+  const int sidx = unit % streams, m = sidx / g.H, h = sidx % g.H;
+  const int n = a.len_old, keep = a.len_new, recent = a.first_row;
+  const int A = keep - recent, cand = n - recent;
+  const int64_t row0 = (int64_t)m * g.H * g.C + st.seq_row0[a.s] + (int64_t)h * st.cap[a.s];
+  float* sc = scores + row0;
+  int32_t* kp = kept ? kept + row0 : nullptr;
+  uint4* K = reinterpret_cast<uint4*>(buf.k + row0 * D);
+  uint4* V = reinterpret_cast<uint4*>(buf.v + row0 * D);
+  const bool in_smem = cand <= held;
+  auto key = [&](int i) { return in_smem ? keys[i] : order_key(sc[i]); };
+
+  // ------------------------------ the A-th largest score ---------------------------------------
+  uint32_t T = 0;              // stays: key > T, and the first `need` (in row order) with key == T
+  int need = 0x7FFFFFFF;
+  bool ties = false;           // fewer of the equal ones stay than there are
+  if (A > 0) {
+    if (in_smem)
+      for (int i = tid; i < cand; i += kThreads) keys[i] = order_key(sc[i]);
+    uint32_t prefix = 0, want = (uint32_t)A;
+    int shift = 21;
+    for (int pass = 0; pass < 3; ++pass) {
+      const int width = pass == 2 ? 10 : 11;
+      const int hi = shift + width;  // the digits above are `prefix`
+#pragma unroll
+      for (int b = 0; b < kBins / kThreads; ++b) sh.hist[b * kThreads + tid] = 0;
+      __syncthreads();
+      const uint32_t mask = (1u << width) - 1u;
+      for (int i = tid; i < cand; i += kThreads) {
+        const uint32_t k = key(i);
+        if (pass == 0 || k >> hi == prefix) atomicAdd(&sh.hist[(k >> shift) & mask], 1u);
+      }
+      __syncthreads();
+      // thread t holds the eight bins from the (t + 1)-th eight from the top down
+      const int per = kBins / kThreads, top = kBins - 1 - tid * per;
+      uint32_t c[kBins / kThreads], mine = 0;
+#pragma unroll
+      for (int b = 0; b < per; ++b) {
+        c[b] = sh.hist[top - b];
+        mine += c[b];
+      }
+      uint32_t all;
+      uint32_t above = block_scan(mine, sh, &all);
+      if (above < want && want <= above + mine) {
+#pragma unroll
+        for (int b = 0; b < per; ++b) {
+          if (above < want && want <= above + c[b]) {
+            sh.bin = (uint32_t)(top - b);
+            sh.above = above;
+            sh.in_bin = c[b];
+          }
+          above += c[b];
+        }
+      }
+      __syncthreads();
+      prefix = prefix << width | sh.bin;
+      want -= sh.above;
+      T = prefix << shift;
+      if (want == sh.in_bin) break;  // the whole bin stays: every key from its lowest on
+      if (pass == 2) {
+        need = (int)want;
+        ties = true;
+      }
+      shift -= pass == 1 ? 10 : 11;
+      __syncthreads();
+    }
+    // no key of the bin's range lies at or below T but T itself, so "key >= T" is "key > T or the equal ones"
+  }
+
+  // ------------------------------ holes, and the rows that fill them ---------------------------
+  const uint32_t uneed = (uint32_t)need;
+  uint32_t eq_hole = 0, eq_src = 0;  // equal ones before each scan's next candidate
+  if (ties) {                        // those below row A
+    uint32_t c = 0;
+    for (int i = tid; i < A; i += kThreads) c += key(i) == T;
+    block_scan(c, sh, &eq_src);
+  }
+  __syncthreads();
+  if (CN > 1) cluster_sync();  // every CTA of the cluster has read the scores
+  // One step of a scan: the candidates [base, min(base + kScan, end)) that stay (or go) are appended to list at *count.
+  auto scan = [&](int base, int end, uint32_t& eq_before, bool stay, int32_t* list, int count) {
+    uint32_t gt = 0, eq = 0;
+    const int i0 = base + 4 * tid;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (i0 + u < end) {
+        const uint32_t k = key(i0 + u);
+        gt |= (uint32_t)(k > T) << u;
+        eq |= (uint32_t)(k == T) << u;
+      }
+    }
+    uint32_t sum;
+    const uint32_t pre = block_scan(__popc(gt) | __popc(eq) << 16, sh, &sum);
+    uint32_t e = eq_before + (pre >> 16);
+    uint32_t stayed = (pre & 0xFFFFu) + (min(e, uneed) - min(eq_before, uneed));
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = i0 + u;
+      if (i < end) {
+        const bool s = (gt >> u & 1u) || ((eq >> u & 1u) && e < uneed);
+        e += eq >> u & 1u;
+        if (stay && s) list[count + stayed] = i;
+        if (!stay && !s) list[count + (uint32_t)(i - base) - stayed] = i;
+        if (!stay && s && kp != nullptr && rank == 0) kp[i] = i;
+        stayed += s;
+      }
+    }
+    const int total = (int)((sum & 0xFFFFu) + (min(eq_before + (sum >> 16), uneed) - min(eq_before, uneed)));
+    eq_before += sum >> 16;
+    __syncthreads();
+    return stay ? total : min(end - base, kScan) - total;
+  };
+  int at_src = A, n_src = 0;
+  for (int at_hole = 0; at_hole < A; at_hole += kScan) {
+    const int n_hole = scan(at_hole, A, eq_hole, false, sh.l.holes, 0);
+    while (n_src < n_hole && at_src < cand) {
+      n_src += scan(at_src, cand, eq_src, true, sh.srcs, n_src);
+      at_src += kScan;
+    }
+    if (n_hole > n_src) {  // cannot be: as many stay beyond row A as go below it
+      if (tid == 0) atomicOr(buf.status, STATUS_CHECK);
+      break;
+    }
+    constexpr int U = 4;
+    const int step = CN * kThreads, total = n_hole * VPR;
+    for (int v0 = rank * kThreads + tid; v0 < total; v0 += U * step) {
+      uint4 k[U], v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int x = v0 + u * step;
+        if (x < total) {
+          const int64_t at = (int64_t)sh.srcs[x / VPR] * VPR + x % VPR;
+          k[u] = K[at];
+          v[u] = V[at];
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int x = v0 + u * step;
+        if (x < total) {
+          const int64_t at = (int64_t)sh.l.holes[x / VPR] * VPR + x % VPR;
+          K[at] = k[u];
+          V[at] = v[u];
+        }
+      }
+    }
+    if (rank == 0)
+      for (int j = tid; j < n_hole; j += kThreads) {
+        const int to = sh.l.holes[j], from = sh.srcs[j];
+        sc[to] = sc[from];
+        if (kp != nullptr) kp[to] = from;
+      }
+    __syncthreads();
+    // the rows not used yet go to the front of their list
+    const int left = n_src - n_hole;
+    int32_t keep_src[kScan / kThreads];
+#pragma unroll
+    for (int u = 0; u < kScan / kThreads; ++u) {
+      const int j = u * kThreads + tid;
+      if (j < left) keep_src[u] = sh.srcs[n_hole + j];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kScan / kThreads; ++u) {
+      const int j = u * kThreads + tid;
+      if (j < left) sh.srcs[j] = keep_src[u];
+    }
+    n_src = left;
+    __syncthreads();
+  }
+  if (CN > 1)
+    cluster_sync();
+  else
+    __syncthreads();
+
+  // ------------------------------ the recent rows move down ------------------------------------
+  // A cluster's CTAs take one of K and V each, and parts of the rows' columns.
+  {
+    const bool do_k = CN == 1 || (rank & 1) == 0, do_v = CN == 1 || (rank & 1) == 1;
+    const int parts = CN > 1 ? CN / 2 : 1, part = CN > 1 ? rank / 2 : 0;
+    const int c0 = part * VPR / parts, W = (part + 1) * VPR / parts - c0;
+    constexpr int U = 4;
+    const int total = recent * W;
+    const int64_t from = (int64_t)cand * VPR + c0, to = (int64_t)A * VPR + c0;
+    for (int v0 = 0; v0 < total; v0 += U * kThreads) {
+      uint4 k[U], v[U];
+      int at[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int x = v0 + u * kThreads + tid;
+        at[u] = x / W * VPR + x % W;
+        if (x < total) {
+          if (do_k) k[u] = K[from + at[u]];
+          if (do_v) v[u] = V[from + at[u]];
+        }
+      }
+      __syncthreads();  // rows move down: this chunk's destinations lie below every later chunk's sources
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (v0 + u * kThreads + tid < total) {
+          if (do_k) K[to + at[u]] = k[u];
+          if (do_v) V[to + at[u]] = v[u];
+        }
+      }
+    }
+  }
+  if (rank == 0) {
+    const bool meta = m == 0 && h == 0;  // the sequence's positions and history indices
+    int32_t* pos = buf.pos + st.off[a.s];
+    int32_t* orig = buf.orig + st.off[a.s];
+    for (int i0 = 0; i0 < recent; i0 += kThreads) {
+      const int i = i0 + tid;
+      const bool in = i < recent;
+      const float s = in ? sc[cand + i] : 0.f;
+      const int32_t po = in && meta ? pos[cand + i] : 0, oo = in && meta ? orig[cand + i] : 0;
+      __syncthreads();
+      if (in) {
+        sc[A + i] = s;
+        if (kp != nullptr) kp[A + i] = cand + i;
+        if (meta) {
+          pos[A + i] = po;
+          orig[A + i] = oo;
+        }
+      }
+    }
+    __syncthreads();
+    for (int i = keep + tid; i < n; i += kThreads) sc[i] = 0.f;
+    if (meta)
+      for (int i = tid; i < A; i += kThreads) pos[i] = orig[i] = -1;  // they differ between streams now
+  }
+}
+
+template <int D>
+cudaError_t launch_evict_t(const Geometry& g, const Static& st, const Buffers& buf, float* scores, const AffSeq* aff,
+                           int n_aff, int64_t max_len, int32_t* kept, int num_sms, cudaStream_t stream) {
+  static std::atomic<bool> done[64];
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  if (!done[dev].load(std::memory_order_acquire)) {
+    e = cudaFuncSetAttribute(evict_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, 4 * kMaxHeldKeys);
+    if (e != cudaSuccess) return e;
+    done[dev].store(true, std::memory_order_release);
+  }
+  const int64_t units = (int64_t)n_aff * g.M * g.H;
+  // keys that do not fit are read again from the scores, which the CTAs of a cluster would change under each other
+  const int held = (int)std::min<int64_t>(max_len, kMaxHeldKeys);
+  int cn = 1;
+  if (max_len <= kMaxHeldKeys)
+    while (2 * cn <= kMaxCluster && 2 * cn * units <= 2 * num_sms) cn *= 2;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(units * cn));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = 4 * (size_t)held;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = cn;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cn > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, evict_kernel<D>, g, st, buf, scores, aff, kept, held, cn);
+}
+
+}  // namespace
+
+cudaError_t launch_evict(const Geometry& g, const Static& st, const Buffers& buf, float* scores, const AffSeq* aff,
+                         int n_aff, int64_t max_len, int32_t* kept, int num_sms, cudaStream_t stream) {
+  if (n_aff <= 0) return cudaSuccess;
+  switch (g.D) {
+    case 64:
+      return launch_evict_t<64>(g, st, buf, scores, aff, n_aff, max_len, kept, num_sms, stream);
+    case 80:
+      return launch_evict_t<80>(g, st, buf, scores, aff, n_aff, max_len, kept, num_sms, stream);
+    case 96:
+      return launch_evict_t<96>(g, st, buf, scores, aff, n_aff, max_len, kept, num_sms, stream);
+    case 128:
+      return launch_evict_t<128>(g, st, buf, scores, aff, n_aff, max_len, kept, num_sms, stream);
+    default:
+      return cudaErrorInvalidValue;
+  }
+}
+
+}  // namespace kvc

@@ -542,6 +542,11 @@ struct DecodeDev {
   // k > 0: worker w owns segments [w k, w k + k) whole; -1: worker w owns the whole segments whose
   // first row lies in its even share of the rows; 0: stream-K split of the rows
   int seg_per_worker;
+  // the scored decode (the CTA kernel): scores of the launch's first layer, floats between layers' scores, and the
+  // logits that a CTA holds
+  float* scores;
+  int64_t score_plane;
+  int held;
 };
 
 // The tiles of a worker: its flat row range [x, hi) of the concatenation over (layer, sequence,
@@ -1071,8 +1076,12 @@ struct Piece {
 
 // CTAs [u CN, (u + 1) CN) -- a cluster when CN > 1 -- take segments [u k_segs, (u + 1) k_segs) of the
 // launch's (layer, sequence, head) segments whole; CN > 1 goes with k_segs = 1.
-template <typename T, int D, int W, int KPT, int S>
-__global__ void __launch_bounds__((W + 1) * 32, CtaCfg<D, W, KPT, S>::CPS)
+// SCORED adds each row's weight to its score: the logits of the CTA's rows (the first p.held of them) stay in shared
+// memory until the segment's maximum and sum are known; a warp then takes the rows that it did the logits of, so no
+// barrier is needed, and its additions go out as reductions, one per row and launch, without waiting for the old
+// score.  Rows past p.held have their logits computed again from K.
+template <typename T, int D, int W, int KPT, int S, bool SCORED = false>
+__global__ void __launch_bounds__((W + 1) * 32, SCORED && W == 4 ? 2 : CtaCfg<D, W, KPT, S>::CPS)
     decode_cta_kernel(Geometry g, Static st, DecodeDev p, int CN, int k_segs) {
   using C = CtaCfg<D, W, KPT, S>;
   using L = Lanes<D>;
@@ -1209,11 +1218,13 @@ __global__ void __launch_bounds__((W + 1) * 32, CtaCfg<D, W, KPT, S>::CPS)
   bool dead = false;
   int piece = 0;
   const int jw = warp * C::WR;  // the warp's first row of every tile
+  [[maybe_unused]] float* logits = reinterpret_cast<float*>(smem + C::SMEM);  // SCORED: p.held of them
   pdl_wait();
   fetch_q();
   for (; sg < sg1;) {
     set_rows();
     const int s = pc.s, h = pc.h, layer = pc.layer, r1 = pc.r1;
+    [[maybe_unused]] const int pc_r0 = pc.r0;
     if (Lc == 0) {  // a sequence without rows
       next();
       if (sg < sg1) fetch_q();
@@ -1237,7 +1248,10 @@ __global__ void __launch_bounds__((W + 1) * 32, CtaCfg<D, W, KPT, S>::CPS)
           if (c < g.rot) {
             const bool lo_half = c < half;
             float sn, cs;
-            rope_sincos(qpos, st.rope_g[lo_half ? c : c - half], &sn, &cs);
+            if constexpr (SCORED)
+              rope_sincos_full(qpos, st.rope_g[lo_half ? c : c - half], &sn, &cs);
+            else
+              rope_sincos(qpos, st.rope_g[lo_half ? c : c - half], &sn, &cs);
             const float y = T::f1((uint16_t)(qraw[j] >> 16));
             x = lo_half ? x * cs - y * sn : x * cs + y * sn;
           }
@@ -1303,6 +1317,13 @@ __global__ void __launch_bounds__((W + 1) * 32, CtaCfg<D, W, KPT, S>::CPS)
         for (int k = 0; k < KPT; ++k) {
           if (!valid[k]) z[k] = -INFINITY;
           mn = fmaxf(mn, z[k]);
+        }
+        if constexpr (SCORED) {
+#pragma unroll
+          for (int k = 0; k < KPT; ++k) {
+            const int x = r - pc_r0 + jw + k * L::RPI + grp;
+            if (tl == 0 && x < p.held) logits[x] = z[k];
+          }
         }
         const float mu = (mn == -INFINITY) ? 0.f : mn;
         const float alpha = exp2f(m - mu);
@@ -1439,12 +1460,72 @@ __global__ void __launch_bounds__((W + 1) * 32, CtaCfg<D, W, KPT, S>::CPS)
           st_cluster_f32(dst + 1, 0, Lx);
           st_cluster_f32(dst + 2, 0, bad);
         }
+        if constexpr (SCORED) {  // every CTA needs the segment's maximum and sum
+          if (lane > 0 && lane < CN) {
+            st_cluster_f32(dst, lane, Mx);
+            st_cluster_f32(dst + 1, lane, Lx);
+            st_cluster_f32(dst + 2, lane, bad);
+          }
+        }
+      }
+    };
+    // SCORED: the weights of the rows that this warp did the logits of, from the n results of the segment
+    [[maybe_unused]] auto add_weights = [&](const float* sp, int n) {
+      float Mx = -INFINITY, bad = 0.f;
+      for (int w = 0; w < n; ++w) {
+        Mx = fmaxf(Mx, sp[w * C::PO]);
+        bad = fmaxf(bad, sp[w * C::PO + 2]);
+      }
+      if (bad != 0.f) return;
+      const float Mxu = (Mx == -INFINITY) ? 0.f : Mx;
+      float Lx = 0.f;
+      for (int w = 0; w < n; ++w) Lx += sp[w * C::PO + 1] * exp2f(sp[w * C::PO] - Mxu);
+      const float inv = 1.f / Lx;
+      const int64_t row0 = st.seq_row0[s] + (int64_t)h * st.cap[s] + p.ds[s].begin + pc_r0;
+      float* sc = p.scores + (int64_t)layer * p.score_plane + row0;
+      const int rows = r1 - pc_r0, in_smem = min(rows, p.held);
+      for (int e = lane;; e += 32) {
+        const int x = e / C::WR * C::TR + jw + e % C::WR;
+        if (e / C::WR * C::TR >= in_smem) break;
+        if (x >= in_smem) continue;
+        const float w = exp2f(logits[x] - Mxu) * inv;
+        if (w != 0.f) atomicAdd(sc + x, w);
+      }
+      // rows past those: a warp step at a time, from global memory
+      const uint16_t* krow = p.k + (int64_t)layer * p.plane + row0 * D;
+      for (int x0 = p.held + warp * L::RPI; x0 < rows; x0 += W * L::RPI) {
+        const int x = x0 + grp, row = pc_r0 + x;
+        const bool seen = x < rows && (row < mlo || row >= mhi);
+        float z = 0.f;
+        if (seen) {
+          float2 acc0 = make_float2(0.f, 0.f), acc1 = make_float2(0.f, 0.f);
+#pragma unroll
+          for (int i = 0; i < L::NV; ++i) {
+            const int c = tl * L::NV + (i + rot) % L::NV;
+            const uint4 u = __ldg(reinterpret_cast<const uint4*>(krow + (int64_t)x * D) + c);
+            acc0 = ffma2(qv[i * 4 + 0], T::f2(u.x), acc0);
+            acc1 = ffma2(qv[i * 4 + 1], T::f2(u.y), acc1);
+            acc0 = ffma2(qv[i * 4 + 2], T::f2(u.z), acc0);
+            acc1 = ffma2(qv[i * 4 + 3], T::f2(u.w), acc1);
+          }
+          z = (acc0.x + acc1.x) + (acc0.y + acc1.y);
+        }
+#pragma unroll
+        for (int off = L::LPR / 2; off >= 1; off >>= 1) z += __shfl_xor_sync(kFull, z, off);
+        if (seen && tl == 0) atomicAdd(sc + x, exp2f(z - Mxu) * inv);
       }
     };
     if (CN > 1) {
       cluster_wait();  // every CTA of the cluster has started
       if (mine_to_merge) merge(sO + (piece & 1) * W * C::PO, W, false);
       cluster_arrive();
+      if constexpr (SCORED) {
+        cluster_wait();
+        const float* all = reinterpret_cast<const float*>(smem + C::OFF_C);
+        if (rank == 0 && mine_to_merge) merge(all, CN, true);
+        add_weights(all, CN);
+        return;
+      }
       if (rank == 0) {
         cluster_wait();
         if (mine_to_merge) merge(reinterpret_cast<const float*>(smem + C::OFF_C), CN, true);
@@ -1452,6 +1533,7 @@ __global__ void __launch_bounds__((W + 1) * 32, CtaCfg<D, W, KPT, S>::CPS)
       return;  // one segment per cluster
     }
     if (mine_to_merge) merge(sO + (piece & 1) * W * C::PO, W, true);
+    if constexpr (SCORED) add_weights(sO + (piece & 1) * W * C::PO, W);
     ++piece;
   }
 }
@@ -1494,6 +1576,9 @@ inline DecodeDev decode_dev(const Geometry& g, const Buffers& buf, const DecodeA
   p.limit_ns = a.wait_limit_ns;
   p.kv_before_wait = a.kv_before_wait;
   p.seg_per_worker = seg_per_worker;
+  p.scores = nullptr;
+  p.score_plane = 0;
+  p.held = 0;
   return p;
 }
 
@@ -1517,17 +1602,23 @@ cudaError_t launch_decode_cfg(const Geometry& g, const Static& st, const Buffers
   return cudaLaunchKernelEx(&cfg, decode_kernel<T, D, KPT, S>, g, st, p);
 }
 
-template <typename T, int D, int W, int KPT, int S>
+template <typename T, int D, int W, int KPT, int S, bool SCORED = false>
 cudaError_t launch_decode_cta(const Geometry& g, const Static& st, const Buffers& buf, const DecodeArgs& a, int CN,
-                              int64_t k_segs, int mode, cudaStream_t stream, int* grid, DecodePlan* plan) {
+                              int64_t k_segs, int mode, cudaStream_t stream, int* grid, DecodePlan* plan,
+                              float* scores = nullptr, int held = 0) {
   using C = CtaCfg<D, W, KPT, S>;
-  const DecodeDev p = decode_dev(g, buf, a, D, 0, 0);
+  DecodeDev p = decode_dev(g, buf, a, D, 0, 0);
+  if constexpr (SCORED) {
+    p.held = held;
+    p.score_plane = (int64_t)g.H * g.C;
+    p.scores = scores + a.layer * p.score_plane;
+  }
   const int64_t nseg = (int64_t)p.n_layers * g.b * g.H;
   const int64_t ctas = (nseg + k_segs - 1) / k_segs * CN;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)ctas);
   cfg.blockDim = dim3(C::THREADS);
-  cfg.dynamicSmemBytes = C::SMEM;
+  cfg.dynamicSmemBytes = C::SMEM + 4 * held;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -1540,7 +1631,7 @@ cudaError_t launch_decode_cta(const Geometry& g, const Static& st, const Buffers
   cfg.numAttrs = CN > 1 ? 2 : 1;
   *plan = {mode, (int)(ctas * W), C::TR, S};
   *grid = (int)ctas;
-  return cudaLaunchKernelEx(&cfg, decode_cta_kernel<T, D, W, KPT, S>, g, st, p, CN, (int)k_segs);
+  return cudaLaunchKernelEx(&cfg, decode_cta_kernel<T, D, W, KPT, S, SCORED>, g, st, p, CN, (int)k_segs);
 }
 
 // k whole segments per warp, k as small as one wave of `occ` warps per SM allows; `busiest`: the segments on the
@@ -1764,6 +1855,59 @@ cudaError_t launch_append_t(const Geometry& g, const Static& st, const Buffers& 
   return cudaGetLastError();
 }
 
+// The shapes of the scored decode: two CTAs per SM of four consumer warps and two stages, and the small shape of two
+// consumer warps, three or four CTAs per SM; what two (four) CTAs leave of the shared memory holds logits.
+template <int D>
+struct ScoredShape {
+  using Main = CtaCfg<D, 4, 2, 2>;
+  using Small = CtaCfg<D, 2, 2, 2>;
+  static constexpr int kHeldMain = (113 * 1024 - Main::SMEM) / 4 / 32 * 32;
+  static constexpr int kHeldSmall = (56 * 1024 - Small::SMEM) / 4 / 32 * 32;
+  static_assert(kHeldMain >= 1024 && kHeldSmall >= 512, "room for logits");
+};
+
+template <typename T, int D>
+cudaError_t scored_setup(int dev) {
+  static std::atomic<bool> done[64];
+  if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  if (done[dev].load(std::memory_order_acquire)) return cudaSuccess;
+  using E = ScoredShape<D>;
+  cudaError_t e = cudaFuncSetAttribute(decode_cta_kernel<T, D, 4, 2, 2, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       E::Main::SMEM + 4 * E::kHeldMain);
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(decode_cta_kernel<T, D, 2, 2, 2, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             E::Small::SMEM + 4 * E::kHeldSmall);
+  if (e == cudaSuccess) done[dev].store(true, std::memory_order_release);
+  return e;
+}
+
+template <typename T, int D>
+cudaError_t launch_scored_t(const Geometry& g, const Static& st, const Buffers& buf, const DecodeArgs& a, float* scores,
+                            int num_sms, cudaStream_t stream, int* grid, DecodePlan* plan) {
+  using E = ScoredShape<D>;
+  const cudaError_t e = scored_setup<T, D>(a.device);
+  if (e != cudaSuccess) return e;
+  const int n_layers = a.n_layers < 1 ? 1 : a.n_layers;
+  const int64_t nseg = (int64_t)n_layers * g.b * g.H;
+  const int64_t mean = a.R / (a.n_segments < 1 ? 1 : a.n_segments);
+  const bool balanced = decode_balanced(a);
+  const int mode = balanced ? 1 : n_layers > 1 ? 4 : 0;
+  const int64_t slots = 2 * (int64_t)num_sms;
+  // Clusters as the plain decode takes them, and wherever a CTA's rows would pass the logits that it holds.
+  int cn = 1;
+  while (2 * cn <= kMaxClusterCtas && ((2 * cn * nseg <= slots && a.max_segment >= 2 * cn * 192) ||
+                                       a.max_segment > (int64_t)cn * E::kHeldMain))
+    cn *= 2;
+  if (cn == 1 && mean < 384 && a.max_segment <= 6 * mean + 256 && nseg > slots) {
+    const int64_t k = balanced ? std::max<int64_t>(1, std::min<int64_t>(8, nseg / (8 * slots))) : 1;
+    const int held = (int)std::min<int64_t>(E::kHeldSmall, (a.max_segment + 31) / 32 * 32);
+    return launch_decode_cta<T, D, 2, 2, 2, true>(g, st, buf, a, 1, k, mode, stream, grid, plan, scores, held);
+  }
+  const int64_t rows = (a.max_segment + cn - 1) / cn;
+  const int held = (int)std::min<int64_t>(E::kHeldMain, (rows + 31) / 32 * 32);
+  return launch_decode_cta<T, D, 4, 2, 2, true>(g, st, buf, a, cn, 1, mode, stream, grid, plan, scores, held);
+}
+
 template <typename F>
 cudaError_t by_dhead(int D, F&& f) {
   switch (D) {
@@ -1853,6 +1997,52 @@ cudaError_t launch_decode(const Geometry& g, const Static& st, const Buffers& bu
     if (g.dtype == 1) return launch_decode_t<BF16T, D>(g, st, buf, a, num_sms, stream, grid, plan);
     return launch_decode_t<F16T, D>(g, st, buf, a, num_sms, stream, grid, plan);
   });
+}
+
+cudaError_t launch_decode_scored(const Geometry& g, const Static& st, const Buffers& buf, const DecodeArgs& a,
+                                 float* scores, int num_sms, cudaStream_t stream, int* grid, DecodePlan* plan) {
+  *grid = 0;
+  *plan = {-1, 0, 0, 0};
+  if (a.R <= 0) return cudaSuccess;
+  return by_dhead(g.D, [&](auto dc) {
+    constexpr int D = decltype(dc)::value;
+    return g.dtype == 1 ? launch_scored_t<BF16T, D>(g, st, buf, a, scores, num_sms, stream, grid, plan)
+                        : launch_scored_t<F16T, D>(g, st, buf, a, scores, num_sms, stream, grid, plan);
+  });
+}
+
+// Scores through a compaction, as the row moves do it: a CTA per (sequence, layer, head) stream walks its destination
+// rows upward, each chunk's loads ahead of its stores; then the slots that lost their row are zeroed.
+__global__ void __launch_bounds__(256) compact_scores_kernel(Geometry g, Static st, float* __restrict__ scores,
+                                                             const AffSeq* __restrict__ aff,
+                                                             const int32_t* __restrict__ src_map) {
+  const int streams = g.M * g.H;
+  const AffSeq a = aff[blockIdx.x / streams];
+  const int sidx = blockIdx.x % streams;
+  float* sc = scores + (int64_t)(sidx / g.H) * g.H * g.C + st.seq_row0[a.s] + (int64_t)(sidx % g.H) * st.cap[a.s];
+  const int32_t* smap = src_map + st.off[a.s];
+  for (int d0 = a.first_row; d0 < a.len_new; d0 += 1024) {
+    float v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int d = d0 + u * 256 + threadIdx.x;
+      v[u] = d < a.len_new ? sc[__ldg(smap + d)] : 0.f;
+    }
+    __syncthreads();  // a kept row only moves down: later chunks' sources lie above this chunk's destinations
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int d = d0 + u * 256 + threadIdx.x;
+      if (d < a.len_new) sc[d] = v[u];
+    }
+  }
+  __syncthreads();
+  for (int d = a.len_new + threadIdx.x; d < a.len_old; d += 256) sc[d] = 0.f;
+}
+
+cudaError_t launch_compact_scores(const Geometry& g, const Static& st, float* scores, const AffSeq* aff, int n_aff,
+                                  const int32_t* src_map, cudaStream_t stream) {
+  compact_scores_kernel<<<(unsigned)((int64_t)n_aff * g.M * g.H), 256, 0, stream>>>(g, st, scores, aff, src_map);
+  return cudaGetLastError();
 }
 
 // ---------------------------------------------------------------------------------------------

@@ -12,7 +12,9 @@ namespace kvc {
 // begin + r lives in slot begin + r while r < wrap and in slot r - wrap after it (a ring, for the
 // local-attention cache; wrap is INT32_MAX otherwise).
 struct DState {
-  int32_t len, begin, mask_lo, mask_hi, qpos, wrap, pad1, pad2;
+  int32_t len, begin, mask_lo, mask_hi, qpos, wrap;
+  int32_t is_cl;  // a <CL> query: it sees its own row only, and none of a prefix
+  int32_t pad;
 };
 
 // One stored token: its sequence, destination row, position, history index, and its index among
@@ -21,7 +23,7 @@ struct TokPlan {
   int32_t s, row, pos, orig, in_tok, pad0, pad1, pad2;
 };
 
-// One sequence of a compaction; its drop ranges (history indices, [lo, hi)) are
+// One sequence of a compaction, or of an eviction (see launch_evict); its drop ranges (history indices, [lo, hi)) are
 // ranges[range_off .. range_off + n_ranges).
 struct AffSeq {
   int32_t s, len_old, len_new, first_row, range_off, n_ranges, pad0, pad1;
@@ -124,6 +126,64 @@ struct DecodePlan {
 // cudaErrorNotSupported, and the caller goes layer by layer.
 cudaError_t launch_decode(const Geometry& g, const Static& st, const Buffers& buf, const DecodeArgs& a,
                           int num_sms, cudaStream_t stream, int* grid, DecodePlan* plan);
+
+// The decode with each row's attention weight added to its score (scores: [M][H * C], in the rows' layout): a CTA or a
+// cluster per segment, or several segments per CTA, whatever the segments.
+cudaError_t launch_decode_scored(const Geometry& g, const Static& st, const Buffers& buf, const DecodeArgs& a,
+                                 float* scores, int num_sms, cudaStream_t stream, int* grid, DecodePlan* plan);
+
+// The prefix part of a shared-prefix decode (prefix.cu).  A unit is a run of a prefix's rows for some of its members.
+struct PrefixUnit {
+  int32_t s;           // sequence of the prefix's cache
+  int32_t key0, key1;  // its stored rows
+  int32_t mem0, n_mem; // members[mem0 ..], at most prefix_rows' answer of them
+  int32_t split;       // the run's number among the prefix's
+  int32_t pad0, pad1;
+};
+struct PrefixArgs {
+  int layer, n_layers, H, rot;
+  int64_t C;                // of the prefix's cache, as st, k and v
+  Static st;
+  const uint16_t* k;
+  const uint16_t* v;
+  const PrefixUnit* units;  // [n_units], for each (layer, head)
+  int n_units;
+  const int32_t* members;   // sequences of the own rows' cache
+  const DState* ds;         // theirs
+  // sequence s has n_split[s] parts, from entry split0[s] on; entry e of head h in the launch's layer i starts at
+  // parts + ((i * n_parts + e) * H + h) * (D + 4) floats: maximum and sum (exp2 domain), two unused, then D columns
+  const int32_t* split0;
+  const int32_t* n_split;
+  int64_t n_parts;
+  float* parts;
+  const uint16_t* q;        // [b][H][D] per layer, 16-byte aligned
+  int64_t q_stride;
+  float c2;                 // scale * log2(e)
+};
+// The own rows' part, joined with the prefix's.
+struct OwnArgs {
+  PrefixArgs px;            // st, k, v, C of the own rows' cache here
+  int b;
+  float* out;               // [b][H][D] per layer
+  int64_t out_stride;
+  int after_prefix;         // the kernel before this one is the prefix kernel
+};
+// Queries of one CTA where the largest group has `group` members; CTAs per SM of that kernel.
+int prefix_rows(int group);
+cudaError_t prefix_ctas_per_sm(const Geometry& g, int device, int rows, int* occ);
+cudaError_t launch_prefix(const Geometry& g, const PrefixArgs& a, int device, int rows, cudaStream_t stream);
+cudaError_t launch_own(const Geometry& g, const OwnArgs& a, int64_t max_segment, int num_sms, cudaStream_t stream);
+
+// Scores follow their rows through a compaction (after launch_compact, from the same source map): in place, zero in
+// the slots that lost their row.
+cudaError_t launch_compact_scores(const Geometry& g, const Static& st, float* scores, const AffSeq* aff, int n_aff,
+                                  const int32_t* src_map, cudaStream_t stream);
+
+// Eviction (evict.cu): in every (layer, head) stream of the n_aff sequences, len_new of len_old rows stay, the last
+// `first_row` of them (the recent ones) and those with the largest scores.  max_len: the longest len_old; kept: [M][H * C]
+// or NULL, the earlier row number of each kept row.
+cudaError_t launch_evict(const Geometry& g, const Static& st, const Buffers& buf, float* scores, const AffSeq* aff,
+                         int n_aff, int64_t max_len, int32_t* kept, int num_sms, cudaStream_t stream);
 
 // ---------------------------------------------------------------------------------------------
 // Masked prefill attention (prefill.cu)

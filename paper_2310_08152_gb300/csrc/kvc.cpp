@@ -266,6 +266,16 @@ struct kvc_cache {
   size_t pre_items = 0, pre_meta = 0, pre_klist = 0;  // offsets inside the plan
   int pre_ctas = 0;
   kvc::PrefillMaps maps;
+  float* scores = nullptr;  // kvc_set_scores
+  // kvc_set_prefix: the prefix's cache, each sequence's prefix in it (or -1) and the scratch; then the plan in the
+  // scratch, as long as the prefix's rows and the number of layers stay
+  kvc_cache* prefix = nullptr;
+  std::vector<int32_t> parent;
+  unsigned char* px = nullptr;
+  uint64_t px_version = UINT64_MAX;
+  int px_layers = 0, px_rows = 0, px_units = 0;
+  int64_t px_parts = 0;
+  size_t px_members = 0, px_split0 = 0, px_nsplit = 0;  // offsets behind the units
   bool amaps_ok = false;  // the append kernel's TMA descriptors are in the workspace
   // compaction timing (kvc_set_compaction_timing): events before the scan, between the kernels, after
   bool time_compaction = false;
@@ -409,6 +419,7 @@ struct kvc_cache {
         ds[s].mask_hi = (int32_t)v.mask_hi;
         ds[s].qpos = v.qpos;
         ds[s].wrap = (int32_t)std::min<int64_t>(v.wrap, INT32_MAX);
+        ds[s].is_cl = v.is_cl;
         Lc = v.len - v.begin;
       } else {
         if (decode_ok) decode_err = err;
@@ -541,6 +552,19 @@ kvc_status kvc_book_compress(kvc_book* book, const int32_t* seq, const int64_t* 
   std::string err;
   if (!book->book.plan_compress(seq, cl, cr, n_spans, plan, err)) return fail(KVC_ERR_SPAN, "%s", err.c_str());
   book->book.apply_compress(plan, seq, cl, n_spans);
+  return ok();
+}
+
+kvc_status kvc_book_evict(kvc_book* book, const int64_t* keep, const int64_t* recent) {
+  if (!book) return fail(KVC_ERR_INVALID_ARG, "book is NULL");
+  if (!keep || !recent) return fail(KVC_ERR_INVALID_ARG, "keep/recent are NULL");
+  if (book->book.policy() == kvc::POLICY_LOCAL)
+    return fail(KVC_ERR_UNSUPPORTED, "the local-attention cache keeps a window; nothing is evicted from it");
+  std::vector<kvc::EvictSeq> plan;
+  std::string err;
+  int code = 0;
+  if (!book->book.plan_evict(keep, recent, plan, err, code)) return fail((kvc_status)code, "%s", err.c_str());
+  book->book.apply_evict(plan);
   return ok();
 }
 
@@ -867,6 +891,13 @@ kvc_status kvc_compress_spans(kvc_cache* c, const int32_t* seq, const int64_t* c
   c->launches += launched;
   c->last_was_decode = false;
   if (e != cudaSuccess) return cuda_fail(e, "compaction kernels");
+  if (c->scores && n_aff > 0) {
+    e = kvc::launch_compact_scores(c->geom(), c->stat(), c->scores,
+                                   reinterpret_cast<const kvc::AffSeq*>(c->wsp(c->ws.dyn + c->ws.dyn_payload)), n_aff,
+                                   reinterpret_cast<const int32_t*>(c->wsp(c->ws.src_map)), stream);
+    if (e != cudaSuccess) return cuda_fail(e, "score compaction kernel");
+    c->launches += 1;
+  }
   if (timed) {
     if ((e = cudaEventRecord(c->cev[2], stream)) != cudaSuccess) return cuda_fail(e, "cudaEventRecord");
     c->timed_compaction = true;
@@ -1007,6 +1038,294 @@ kvc_status kvc_decode_attention_static_scratch(kvc_cache* c, int layer, const vo
   if (e != cudaSuccess) return cuda_fail(e, "decode kernel (static scratch)");
   c->launches += grid > 0 ? 1 : 0;
   c->last_was_decode = true;
+  return ok();
+}
+
+kvc_status kvc_set_scores(kvc_cache* c, float* scores) {
+  if (!c) return fail(KVC_ERR_INVALID_ARG, "cache is NULL");
+  if (reinterpret_cast<uintptr_t>(scores) & 15) return fail(KVC_ERR_INVALID_ARG, "scores must be 16-byte aligned");
+  if (scores && c->cfg.policy == KVC_POLICY_LOCAL)
+    return fail(KVC_ERR_UNSUPPORTED, "the local-attention cache keeps a window and has no scores");
+  c->scores = scores;
+  return ok();
+}
+
+// Checks the arguments of the decodes over several layers.
+static kvc_status layers_check(kvc_cache* c, int first, int n_layers, const void* q, int64_t q_layer_stride, float scale,
+                               float* out, int64_t out_layer_stride) {
+  if (!c) return fail(KVC_ERR_INVALID_ARG, "cache is NULL");
+  const int64_t need = (int64_t)c->cfg.b * c->cfg.H * c->cfg.d_head;
+  if (n_layers > 1 && (q_layer_stride < need || out_layer_stride < need))
+    return fail(KVC_ERR_INVALID_ARG, "layer strides (%lld, %lld) below one layer's %lld elements",
+                (long long)q_layer_stride, (long long)out_layer_stride, (long long)need);
+  return decode_check(c, first, n_layers, q, scale, out);
+}
+
+kvc_status kvc_decode_attention_scored(kvc_cache* c, int first, int n_layers, const void* q, int64_t q_layer_stride,
+                                       float scale, float* out, int64_t out_layer_stride, void* stream_) {
+  kvc_status st = layers_check(c, first, n_layers, q, q_layer_stride, scale, out, out_layer_stride);
+  if (st != KVC_OK) return st;
+  if (!c->scores) return fail(KVC_ERR_STATE, "the cache has no scores (kvc_set_scores)");
+  cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+  st = c->ensure_cuda(stream);
+  if (st != KVC_OK) return st;
+  kvc::DecodeArgs a = decode_args(c, first, q, scale, out);
+  a.n_layers = n_layers;
+  a.q_layer_stride = q_layer_stride;
+  a.out_layer_stride = out_layer_stride;
+  int grid = 0;
+  const cudaError_t e =
+      kvc::launch_decode_scored(c->geom(), c->stat(), c->bufs(), a, c->scores, c->num_sms, stream, &grid, &c->last_plan);
+  if (e != cudaSuccess) return cuda_fail(e, "scored decode kernel");
+  c->launches += grid > 0 ? 1 : 0;
+  c->last_was_decode = true;
+  return ok();
+}
+
+// The scratch of a shared-prefix decode: [units][members b][split0 b][n_split b], then the parts.  Units of one (layer,
+// head): at most one run per group of prefix_rows sequences, and kPrefixUnits more that splitting adds over all (layer,
+// head) pairs; parts: as many as sequences, layers and heads, and 64 for each run that splitting adds.
+static constexpr int64_t kPrefixUnits = 1280;
+static size_t prefix_tables(int b) { return align_up(sizeof(kvc::PrefixUnit) * (size_t)(kPrefixUnits + b), 16) + 3 * align_up(4 * (size_t)b, 16); }
+
+size_t kvc_prefix_scratch_bytes(const kvc_cache* c) {
+  if (!c) return 0;
+  const int64_t rows = (int64_t)c->cfg.M * c->cfg.H * c->cfg.b + 64 * kPrefixUnits;
+  return align_up(prefix_tables(c->cfg.b), 256) + 4 * (size_t)rows * (size_t)(c->cfg.d_head + 4);
+}
+
+kvc_status kvc_set_prefix(kvc_cache* c, kvc_cache* prefix, const int32_t* parent, void* scratch, size_t scratch_bytes) {
+  if (!c) return fail(KVC_ERR_INVALID_ARG, "cache is NULL");
+  if (!prefix) {
+    c->prefix = nullptr;
+    c->px = nullptr;
+    return ok();
+  }
+  if (prefix == c) return fail(KVC_ERR_INVALID_ARG, "a cache cannot be its own prefix");
+  if (!parent || !scratch) return fail(KVC_ERR_INVALID_ARG, "parent/scratch are NULL");
+  const kvc_config &a = c->cfg, &p = prefix->cfg;
+  if (a.policy == KVC_POLICY_LOCAL || p.policy == KVC_POLICY_LOCAL)
+    return fail(KVC_ERR_UNSUPPORTED, "the local-attention cache keeps a window and has no shared prefix");
+  if (a.M != p.M || a.H != p.H || a.d_head != p.d_head || a.dtype != p.dtype || a.rotary_dim != p.rotary_dim ||
+      (a.rotary_dim > 0 && a.rope_base != p.rope_base))
+    return fail(KVC_ERR_INVALID_ARG, "the caches differ in layers, heads, d_head, type or rotation");
+  for (int s = 0; s < a.b; ++s)
+    if (parent[s] < -1 || parent[s] >= p.b)
+      return fail(KVC_ERR_INVALID_ARG, "parent[%d] = %d outside [-1, %d)", s, parent[s], p.b);
+  if (reinterpret_cast<uintptr_t>(scratch) & 255) return fail(KVC_ERR_INVALID_ARG, "scratch must be 256-byte aligned");
+  if (scratch_bytes < kvc_prefix_scratch_bytes(c))
+    return fail(KVC_ERR_INVALID_ARG, "%zu bytes of scratch, %zu needed", scratch_bytes, kvc_prefix_scratch_bytes(c));
+  c->prefix = prefix;
+  c->parent.assign(parent, parent + a.b);
+  c->px = static_cast<unsigned char*>(scratch);
+  c->px_version = UINT64_MAX;
+  return ok();
+}
+
+// Cuts the prefixes' rows into runs and uploads the plan (units, members, each sequence's parts).
+static kvc_status plan_prefix(kvc_cache* c, int n_layers, cudaStream_t stream) {
+  const int b = c->cfg.b, P = c->prefix->cfg.b;
+  std::vector<std::vector<int32_t>> group(P);
+  for (int s = 0; s < b; ++s)
+    if (c->parent[s] >= 0 && c->prefix->bk.book.stored(c->parent[s]) > 0) group[c->parent[s]].push_back(s);
+  int largest = 0;
+  int64_t longest = 0, units1 = 0;  // units without splits
+  for (int g = 0; g < P; ++g) {
+    largest = std::max(largest, (int)group[g].size());
+    if (!group[g].empty()) longest = std::max(longest, c->prefix->bk.book.stored(g));
+  }
+  const int rows = kvc::prefix_rows(largest);
+  int occ = 1;
+  cudaError_t e = kvc::prefix_ctas_per_sm(c->geom(), c->device, rows, &occ);
+  if (e != cudaSuccess) return cuda_fail(e, "prefix kernel");
+  const int64_t pairs = (int64_t)n_layers * c->cfg.H, slots = (int64_t)occ * c->num_sms;
+  for (int g = 0; g < P; ++g) units1 += pairs * (int64_t)((group[g].size() + rows - 1) / rows);
+  // Rows of a run: at least 32 per member, so that a part's 8 (d_head + 4) bytes a member, written and read, stay small
+  // beside the run's rows, and 256.
+  auto run_of = [&](int g, int64_t run) {
+    const int64_t least = std::max<int64_t>(256, 32 * std::min<int64_t>((int64_t)group[g].size(), rows));
+    return std::max(run, least);
+  };
+  auto runs_of = [&](int g, int64_t run) {
+    const int64_t len = c->prefix->bk.book.stored(g), r = run_of(g, run);
+    return (len + r - 1) / r;
+  };
+  // The run length whose last wave ends first, a CTA's start and end counted as 160 rows; one run each where that is
+  // more than kPrefixUnits runs beyond one each.
+  int64_t best_run = longest;
+  double best = -1;
+  for (int64_t run = longest; run >= 64 && longest > 0; run = run * 15 / 16) {
+    const int64_t r = (run + 63) / 64 * 64;
+    int64_t units = 0, most = 0;
+    for (int g = 0; g < P; ++g) {
+      if (group[g].empty()) continue;
+      const int64_t n = runs_of(g, r);
+      units += pairs * n * (int64_t)((group[g].size() + rows - 1) / rows);
+      most = std::max(most, std::min(c->prefix->bk.book.stored(g), run_of(g, r)));
+    }
+    if (units > units1 + kPrefixUnits) break;
+    double rows_all = 0;
+    for (int g = 0; g < P; ++g)
+      rows_all += (double)pairs * (double)((group[g].size() + rows - 1) / rows) * (double)c->prefix->bk.book.stored(g);
+    const double even = (rows_all + 160.0 * (double)units) / (double)slots;
+    // balanced units finish in whole waves; ragged ones fill the gaps, but no earlier than an even share and a unit
+    const double waves = (double)((units + slots - 1) / slots) * (double)(most + 160);
+    const double cost = std::max((double)(most + 160), std::min(waves, even + 0.5 * (double)most));
+    if (best < 0 || cost < best) {
+      best = cost;
+      best_run = r;
+    }
+  }
+  std::vector<kvc::PrefixUnit> units;
+  std::vector<int32_t> members, split0(b, 0), n_split(b, 0);
+  int64_t parts = 0;
+  for (int g = 0; g < P; ++g) {
+    if (group[g].empty()) continue;
+    const int64_t len = c->prefix->bk.book.stored(g), n = runs_of(g, best_run);
+    const int64_t step = ((len + n - 1) / n + 63) / 64 * 64;  // whole tiles
+    const int64_t n_runs = (len + step - 1) / step;
+    const int32_t mem0 = (int32_t)members.size(), n_mem = (int32_t)group[g].size();
+    for (int64_t k = 0; k < n_runs; ++k)
+      for (int32_t m = 0; m < n_mem; m += rows)
+        units.push_back({g, (int32_t)(k * step), (int32_t)std::min(len, (k + 1) * step), mem0 + m, std::min(rows, n_mem - m),
+                         (int32_t)k, 0, 0});
+    for (int32_t s : group[g]) {
+      members.push_back(s);
+      split0[s] = (int32_t)parts;
+      n_split[s] = (int32_t)n_runs;
+      parts += n_runs;
+    }
+  }
+  const size_t ub = align_up(sizeof(kvc::PrefixUnit) * units.size(), 16), ib = align_up(4 * (size_t)b, 16);
+  const size_t part_bytes = 4 * (size_t)(parts * pairs) * (size_t)(c->cfg.d_head + 4);
+  if (ub + 3 * ib > prefix_tables(b) || align_up(prefix_tables(b), 256) + part_bytes > kvc_prefix_scratch_bytes(c))
+    return fail(KVC_ERR_STATE, "the prefix plan exceeds its scratch");
+  unsigned char* img = c->ring.reserve(ub + 3 * ib, &e);
+  if (!img) return e != cudaSuccess ? cuda_fail(e, "staging") : fail(KVC_ERR_INVALID_ARG, "prefix plan exceeds ring");
+  std::memset(img, 0, ub + 3 * ib);
+  if (!units.empty()) std::memcpy(img, units.data(), sizeof(kvc::PrefixUnit) * units.size());
+  if (!members.empty()) std::memcpy(img + ub, members.data(), 4 * members.size());
+  std::memcpy(img + ub + ib, split0.data(), 4 * (size_t)b);
+  std::memcpy(img + ub + 2 * ib, n_split.data(), 4 * (size_t)b);
+  c->px_version = UINT64_MAX;
+  e = c->ring.commit(c->px, ub + 3 * ib, stream);
+  if (e != cudaSuccess) return cuda_fail(e, "upload prefix plan");
+  c->px_version = c->prefix->version;
+  c->px_layers = n_layers;
+  c->px_rows = rows;
+  c->px_units = (int)units.size();
+  c->px_parts = parts;
+  c->px_members = ub;
+  c->px_split0 = ub + ib;
+  c->px_nsplit = ub + 2 * ib;
+  return KVC_OK;
+}
+
+kvc_status kvc_decode_attention_shared(kvc_cache* c, int first, int n_layers, const void* q, int64_t q_layer_stride,
+                                       float scale, float* out, int64_t out_layer_stride, void* stream_) {
+  kvc_status st = layers_check(c, first, n_layers, q, q_layer_stride, scale, out, out_layer_stride);
+  if (st != KVC_OK) return st;
+  if (!c->prefix) return fail(KVC_ERR_STATE, "the cache has no prefix (kvc_set_prefix)");
+  if ((reinterpret_cast<uintptr_t>(q) & 15) || (n_layers > 1 && q_layer_stride % 8 != 0))
+    return fail(KVC_ERR_INVALID_ARG, "q must be 16-byte aligned, and so each layer's");
+  const kvc_cache* p = c->prefix;
+  if (first + n_layers > p->layers_done)
+    return fail(KVC_ERR_STATE, "layer %d of the prefix's last tokens is not written yet", std::max(first, p->layers_done));
+  for (int s = 0; s < c->cfg.b; ++s)
+    if (c->parent[s] >= 0 && !p->bk.book.all_visible(c->parent[s]))
+      return fail(KVC_ERR_STATE, "prefix %d has a span that is open or closed and not freed", c->parent[s]);
+  cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+  st = c->ensure_cuda(stream);
+  if (st != KVC_OK) return st;
+  if (p->cuda_ready && p->device != c->device) return fail(KVC_ERR_STATE, "the prefix is on another device");
+  if (c->px_version != p->version || c->px_layers != n_layers) {
+    st = plan_prefix(c, n_layers, stream);
+    if (st != KVC_OK) return st;
+  }
+  kvc::PrefixArgs pa;
+  pa.layer = first;
+  pa.n_layers = n_layers;
+  pa.H = c->cfg.H;
+  pa.rot = c->cfg.rotary_dim;
+  pa.C = p->C;
+  pa.st = p->stat();
+  pa.k = p->bufs().k;
+  pa.v = p->bufs().v;
+  pa.units = reinterpret_cast<const kvc::PrefixUnit*>(c->px);
+  pa.n_units = c->px_units;
+  pa.members = reinterpret_cast<const int32_t*>(c->px + c->px_members);
+  pa.ds = reinterpret_cast<const kvc::DState*>(c->wsp(c->ws.dyn));
+  pa.split0 = reinterpret_cast<const int32_t*>(c->px + c->px_split0);
+  pa.n_split = reinterpret_cast<const int32_t*>(c->px + c->px_nsplit);
+  pa.n_parts = c->px_parts;
+  pa.parts = reinterpret_cast<float*>(c->px + align_up(prefix_tables(c->cfg.b), 256));
+  pa.q = static_cast<const uint16_t*>(q);
+  pa.q_stride = q_layer_stride;
+  pa.c2 = scale * 1.4426950408889634f;
+  cudaError_t e;
+  if (c->px_units > 0) {
+    e = kvc::launch_prefix(c->geom(), pa, c->device, c->px_rows, stream);
+    if (e != cudaSuccess) return cuda_fail(e, "prefix kernel");
+    c->launches += 1;
+    c->last_was_decode = false;  // until the launch below
+  }
+  kvc::OwnArgs oa;
+  oa.px = pa;
+  oa.px.C = c->C;
+  oa.px.st = c->stat();
+  oa.px.k = c->bufs().k;
+  oa.px.v = c->bufs().v;
+  oa.b = c->cfg.b;
+  oa.out = out;
+  oa.out_stride = out_layer_stride;
+  oa.after_prefix = c->px_units > 0;
+  e = kvc::launch_own(c->geom(), oa, c->max_segment, c->num_sms, stream);
+  if (e != cudaSuccess) return cuda_fail(e, "own rows' kernel");
+  c->launches += 1;
+  c->last_was_decode = true;
+  return ok();
+}
+
+kvc_status kvc_evict(kvc_cache* c, const int64_t* keep, const int64_t* recent, int32_t* kept, void* stream_) {
+  if (!c) return fail(KVC_ERR_INVALID_ARG, "cache is NULL");
+  if (!keep || !recent) return fail(KVC_ERR_INVALID_ARG, "keep/recent are NULL");
+  if (c->cfg.policy == KVC_POLICY_LOCAL)
+    return fail(KVC_ERR_UNSUPPORTED, "the local-attention cache keeps a window; nothing is evicted from it");
+  if (c->layers_done != c->cfg.M)
+    return fail(KVC_ERR_STATE, "layers %d..%d of the last tokens are not written yet", c->layers_done, c->cfg.M - 1);
+  if (!c->scores) return fail(KVC_ERR_STATE, "the cache has no scores (kvc_set_scores)");
+  std::vector<kvc::EvictSeq> plan;
+  std::string err;
+  int code = 0;
+  if (!c->bk.book.plan_evict(keep, recent, plan, err, code)) return fail((kvc_status)code, "%s", err.c_str());
+  if (plan.empty()) return ok();
+  cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+  kvc_status st = c->ensure_cuda(stream);
+  if (st != KVC_OK) return st;
+  const size_t bytes = c->ws.dyn_payload + sizeof(kvc::AffSeq) * plan.size();
+  cudaError_t e;
+  unsigned char* img = c->ring.reserve(bytes, &e);
+  if (!img) return cuda_fail(e, "staging");
+  c->bk.book.apply_evict(plan);
+  c->fill_state(img);
+  kvc::AffSeq* aff = reinterpret_cast<kvc::AffSeq*>(img + c->ws.dyn_payload);
+  int64_t max_len = 0;
+  for (size_t i = 0; i < plan.size(); ++i) {
+    std::memset(&aff[i], 0, sizeof(kvc::AffSeq));
+    aff[i].s = plan[i].s;
+    aff[i].len_old = (int32_t)plan[i].len_old;
+    aff[i].len_new = (int32_t)plan[i].keep;
+    aff[i].first_row = (int32_t)plan[i].recent;
+    max_len = std::max(max_len, plan[i].len_old);
+  }
+  e = c->ring.commit(c->wsp(c->ws.dyn), bytes, stream);
+  if (e != cudaSuccess) return cuda_fail(e, "upload eviction plan");
+  e = kvc::launch_evict(c->geom(), c->stat(), c->bufs(), c->scores,
+                        reinterpret_cast<const kvc::AffSeq*>(c->wsp(c->ws.dyn + c->ws.dyn_payload)), (int)plan.size(),
+                        max_len, kept, c->num_sms, stream);
+  if (e != cudaSuccess) return cuda_fail(e, "eviction kernel");
+  c->launches += 1;
+  c->last_was_decode = false;
   return ok();
 }
 
