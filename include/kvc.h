@@ -293,6 +293,18 @@ kvc_status kvc_set_scores(kvc_cache* cache, float* scores);
 kvc_status kvc_decode_attention_scored(kvc_cache* cache, int first, int n_layers, const void* q, int64_t q_layer_stride,
                                        float scale, float* out, int64_t out_layer_stride, void* stream);
 
+/* Adds the attention weights of a prompt's queries to the scores of layer `layer`, on the tensor cores:
+ * for each of the last n_q[s] tokens of every sequence s,
+ *   score_j += softmax_j(scale * <q, k_j>)  over the stored rows j that the token sees,
+ * q, n_q, scale, the mask and the rows that have to be stored as for kvc_prefill_attention (all of a prompt's
+ * tokens, block by block, for the weights that its rows got in it; its last few for an observation window).
+ *   scratch: device, 256-byte aligned, the bytes that kvc_score_scratch_bytes gives for these n_q at this
+ *     time, the call's until it is complete on `stream`.
+ * Every sum is made in one order.  Errors as kvc_prefill_attention's, and KVC_ERR_STATE without scores. */
+kvc_status kvc_score_scratch_bytes(kvc_cache* cache, const int32_t* n_q, size_t* bytes);
+kvc_status kvc_score_prompt(kvc_cache* cache, int layer, const void* q, const int32_t* n_q, float scale, void* scratch,
+                            size_t scratch_bytes, void* stream);
+
 /* Evicts rows of the sequences s with keep[s] >= 0 that store more than keep[s] rows: every (layer, head)
  * stream keeps its last recent[s] rows and the keep[s] - recent[s] others with the largest scores (equal
  * ones: the lower rows; a NaN counts below every number, and a score of +infinity pins its row).

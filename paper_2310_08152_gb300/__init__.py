@@ -346,6 +346,19 @@ def kvc_decode_attention_scored(cache: int, first: int, n_layers: int, q, q_laye
                                              int(out_layer_stride), _stream_handle(stream)))
 
 
+def kvc_score_scratch_bytes(cache: int, n_q) -> int:
+    n_q = _np(n_q, np.int32)
+    n = ctypes.c_size_t()
+    _check(lib().kvc_score_scratch_bytes(cache, n_q.ctypes.data, ctypes.byref(n)))
+    return n.value
+
+
+def kvc_score_prompt(cache: int, layer: int, q, n_q, scale: float, scratch, stream=None):
+    n_q = _np(n_q, np.int32)
+    _check(lib().kvc_score_prompt(cache, layer, _ptr(q), n_q.ctypes.data, float(scale), _ptr(scratch),
+                                  scratch.numel() * scratch.element_size(), _stream_handle(stream)))
+
+
 def kvc_prefix_scratch_bytes(cache: int) -> int:
     return lib().kvc_prefix_scratch_bytes(cache)
 
@@ -469,6 +482,7 @@ class KVCache:
         self.book = Book(self.b, cap, policy, _handle=lib().kvc_get_book(self.handle))
         self.scores = None
         self.prefix = None
+        self._score_scratch = None
 
     # views of the device layout (rows of d_head elements)
     def k_plane(self, layer: int):
@@ -584,6 +598,22 @@ class KVCache:
         n = self.b * self.H * self.d
         kvc_decode_attention_scored(self.handle, first, n_layers, q, n, scale, out, n, stream)
         return out
+
+    def score_prompt(self, layer: int, q, n_q, scale: float, stream=None):
+        """Adds the attention weights of the last n_q[s] tokens of every sequence s to the scores of a layer (q:
+        [sum n_q, H, d_head], as for prefill_attention)."""
+        import torch
+
+        n_q = _np(n_q, np.int32)
+        if n_q.shape != (self.b,):
+            raise ValueError(f"n_q must have {self.b} elements, got shape {n_q.shape}")
+        _dev(q, "q", self.torch_dtype, int(np.add.reduce(n_q)) * self.H * self.d)
+        need = kvc_score_scratch_bytes(self.handle, n_q)
+        if self._score_scratch is None or self._score_scratch.numel() < need:
+            if self._score_scratch is not None and stream is not None:
+                torch.cuda.synchronize(self.k.device)  # the old one may be in use on that stream
+            self._score_scratch = torch.empty(max(need, 256), dtype=torch.uint8, device=self.k.device)
+        kvc_score_prompt(self.handle, layer, q, n_q, scale, self._score_scratch, stream)
 
     def evict(self, keep, recent, kept=None, stream=None):
         """Brings every (layer, head) stream of the sequences with keep >= 0 down to `keep` rows: its last `recent` ones

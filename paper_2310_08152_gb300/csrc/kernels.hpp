@@ -238,6 +238,10 @@ struct alignas(64) PrefillMaps {
 };
 
 cudaError_t encode_prefill_maps(const Geometry& g, const Buffers& buf, PrefillMaps* maps);
+// A 2-D map of the K planes as above in boxes of 128 rows; a 3-D map of queries [n_tok][H][D] in boxes of one column
+// subtile x one head x 128 tokens.  out: 128 bytes.
+cudaError_t encode_key_map(const Geometry& g, const Buffers& buf, unsigned char* out);
+cudaError_t encode_query_map(const Geometry& g, const void* q, int64_t n_tok, unsigned char* out);
 // Most CTAs of the persistent prefill grid.
 constexpr int kMaxPrefillCtas = 1024;
 // Keys of one key tile for head dimension D and the cache type, and where a tile's own rows start among
@@ -248,6 +252,51 @@ inline int prefill_own_start(int n_before, int kt) { return 128 % kt == 0 ? (n_b
 int prefill_ctas_per_sm(int D);
 // A persistent grid of a.n_ctas CTAs walks the a.n_items work items.
 cudaError_t launch_prefill(const Geometry& g, const PrefillMaps& maps, const PrefillArgs& a, cudaStream_t stream);
+
+// ---------------------------------------------------------------------------------------------
+// Scores of a prompt (score.cu)
+// ---------------------------------------------------------------------------------------------
+// A sequence with queries: they are stored rows [q0, len), tokens tok0 .. of q; row0 = seq_row0[s]; its rows' mask bounds
+// (as the prefill's) start at meta[moff], a multiple of 128, the least `hid` of each 128 rows at least[moff / 128].
+struct ScoreSeq {
+  int32_t tok0, q0, len, moff, row0, cap, s, pad;
+};
+// A unit of the first pass: key tiles [kt0, kt1) for query tile qt; of the second: key tiles [kt0, kt1).
+struct ScoreUnit {
+  int32_t seq, qt, kt0, kt1, split, pad0, pad1, pad2;
+};
+struct ScoreArgs {
+  int layer, H, rot;
+  int64_t C, n_tok;         // tokens of q
+  const ScoreSeq* seqs;
+  const ScoreUnit* units;   // of the pass
+  int n_units;              // each for H heads
+  const int32_t* meta;
+  const int32_t* least;
+  float2* lse;              // [n_split][H][n_tok]: (maximum, sum) of each query over a split's keys, exp2 domain
+  int n_split;
+  float* scores;            // [M][H * C]
+  float c2;
+  int* status;
+  unsigned long long wait_limit_ns;
+  // rotated queries: their high and low parts
+  const uint16_t* q;
+  uint16_t* q_hi;
+  uint16_t* q_lo;
+  const int32_t* pos;
+  const int64_t* off;
+  const float2* rope_g;
+};
+struct alignas(64) ScoreMaps {
+  unsigned char k[128], q[128], q_lo[128];
+};
+// Resident CTAs per SM of the passes' kernels (sizes the units).
+int score_ctas_per_sm(int D, bool rot);
+// Rotates a.q into a.q_hi and a.q_lo (n_qt 128-query tiles: the first pass's units with split 0).
+cudaError_t launch_score_rotate(const Geometry& g, const ScoreArgs& a, cudaStream_t stream);
+// The first pass, and the second, where no sequence has more than 128 queries (few) or some do.
+cudaError_t launch_score_lse(const Geometry& g, const ScoreMaps& maps, const ScoreArgs& a, cudaStream_t stream);
+cudaError_t launch_score_sum(const Geometry& g, const ScoreMaps& maps, const ScoreArgs& a, bool few, cudaStream_t stream);
 
 // One warp waits on an mbarrier phase that never completes, with the limit given; the bounded wait
 // gives up and sets STATUS_TIMEOUT in *status.  Exercises the kernels' timeout reporting.

@@ -65,8 +65,17 @@ struct WsLayout {
   size_t pre = 0;        // prefill plan: [PfTileRec tiles][PfItemRec items][int32 meta rows][int32 klist rows]
   int64_t pre_max_tiles = 0;
   size_t pre_bytes = 0;
+  size_t sp = 0;         // plan of a prompt's scores: [ScoreSeq][ScoreUnit first pass][second pass][int32 least][int32 meta]
+  size_t sp_bytes = 0;
   size_t total = 0;
 };
+
+// Units that splitting the keys adds to the first pass of a prompt's scores, at most.
+constexpr int64_t kScoreUnits = 1280;
+size_t score_plan_bytes(int64_t n_seq, int64_t units0, int64_t units1, int64_t n_least, int64_t n_meta) {
+  return sizeof(kvc::ScoreSeq) * (size_t)n_seq + sizeof(kvc::ScoreUnit) * (size_t)(units0 + units1) +
+         align_up(4 * (size_t)n_least, 16) + 4 * (size_t)n_meta;
+}
 
 WsLayout ws_layout(int b, int H, int D, int rot, int64_t C) {
   WsLayout L;
@@ -98,6 +107,8 @@ WsLayout ws_layout(int b, int H, int D, int rot, int64_t C) {
   L.pre_max_tiles = (C + 127) / 128 + b;
   L.pre_bytes = (sizeof(kvc::PfTileRec) + sizeof(kvc::PfItemRec) * (size_t)H) * (size_t)L.pre_max_tiles + 8 * (size_t)C;
   L.pre = take(L.pre_bytes);
+  L.sp_bytes = score_plan_bytes(b, L.pre_max_tiles, L.pre_max_tiles + kScoreUnits, L.pre_max_tiles, C + 128 * (int64_t)b);
+  L.sp = take(L.sp_bytes);
   L.total = o;
   return L;
 }
@@ -267,6 +278,14 @@ struct kvc_cache {
   int pre_ctas = 0;
   kvc::PrefillMaps maps;
   float* scores = nullptr;  // kvc_set_scores
+  // plan of kvc_score_prompt in the workspace
+  uint64_t sp_version = UINT64_MAX;
+  std::vector<int32_t> sp_nq;
+  int sp_units0 = 0, sp_units1 = 0;
+  bool sp_few = true;
+  size_t sp_unit0 = 0, sp_unit1 = 0, sp_least = 0, sp_meta = 0;  // offsets inside the plan
+  kvc::ScoreMaps sp_maps;
+  bool sp_maps_ready = false;
   // kvc_set_prefix: the prefix's cache, each sequence's prefix in it (or -1) and the scratch; then the plan in the
   // scratch, as long as the prefix's rows and the number of layers stay
   kvc_cache* prefix = nullptr;
@@ -332,7 +351,8 @@ struct kvc_cache {
   }
 
   size_t staging_bytes() const {
-    return 2 * ws.dyn_bytes + ws.pre_bytes + 2 * ws.st_rope + kvc::append_maps_bytes(cfg.b) + 65536;
+    return std::max(2 * ws.dyn_bytes + ws.pre_bytes + 2 * ws.st_rope + kvc::append_maps_bytes(cfg.b) + 65536,
+                    ws.sp_bytes + 256);
   }
 
   kvc_status ensure_cuda(cudaStream_t stream) {
@@ -1079,6 +1099,199 @@ kvc_status kvc_decode_attention_scored(kvc_cache* c, int first, int n_layers, co
   if (e != cudaSuccess) return cuda_fail(e, "scored decode kernel");
   c->launches += grid > 0 ? 1 : 0;
   c->last_was_decode = true;
+  return ok();
+}
+
+// Parts that the keys of each query tile are cut into in the first pass of a prompt's scores: enough for two waves.
+static int score_splits(const kvc_cache* c, const int32_t* n_q) {
+  int64_t tiles = 0, longest = 0;
+  for (int s = 0; s < c->cfg.b; ++s) {
+    if (n_q[s] <= 0) continue;
+    tiles += (n_q[s] + 127) / 128;
+    longest = std::max(longest, (c->bk.book.stored(s) + 127) / 128);
+  }
+  if (tiles == 0) return 1;
+  const int64_t slots = (int64_t)kvc::score_ctas_per_sm(c->cfg.d_head, c->cfg.rotary_dim > 0) * c->num_sms;
+  const int64_t want = 2 * slots / std::max<int64_t>(1, tiles * c->cfg.H);
+  return (int)std::max<int64_t>(1, std::min<int64_t>({want, longest / 2, kScoreUnits / tiles, 32}));
+}
+
+static kvc_status score_check(kvc_cache* c, const int32_t* n_q) {
+  if (!c) return fail(KVC_ERR_INVALID_ARG, "cache is NULL");
+  if (!n_q) return fail(KVC_ERR_INVALID_ARG, "n_q is NULL");
+  if (c->cfg.policy == KVC_POLICY_LOCAL)
+    return fail(KVC_ERR_UNSUPPORTED, "the local-attention cache keeps a window and has no scores");
+  if ((int64_t)c->cfg.M * c->cfg.H * c->C >= ((int64_t)1 << 31))
+    return fail(KVC_ERR_UNSUPPORTED, "M*H*sum(capacity) rows exceed the 2^31 rows a tensor-map coordinate reaches");
+  for (int s = 0; s < c->cfg.b; ++s)
+    if (n_q[s] < 0 || n_q[s] > c->bk.book.history(s))
+      return fail(KVC_ERR_INVALID_ARG, "n_q[%d] = %d outside [0, %lld]", s, n_q[s], (long long)c->bk.book.history(s));
+  if (!c->cuda_ready) return fail(KVC_ERR_STATE, "nothing appended yet");
+  return KVC_OK;
+}
+
+kvc_status kvc_score_scratch_bytes(kvc_cache* c, const int32_t* n_q, size_t* bytes) {
+  const kvc_status st = score_check(c, n_q);
+  if (st != KVC_OK) return st;
+  if (!bytes) return fail(KVC_ERR_INVALID_ARG, "bytes is NULL");
+  int64_t n = 0;
+  for (int s = 0; s < c->cfg.b; ++s) n += n_q[s];
+  *bytes = align_up(8 * (size_t)score_splits(c, n_q) * c->cfg.H * (size_t)n, 256);
+  if (c->cfg.rotary_dim > 0) *bytes += 2 * align_up(2 * (size_t)n * c->cfg.H * c->cfg.d_head, 256);
+  return ok();
+}
+
+// Builds and uploads the plan of a prompt's scores.
+static kvc_status plan_score(kvc_cache* c, const int32_t* n_q, int n_split, cudaStream_t stream) {
+  const int b = c->cfg.b, H = c->cfg.H;
+  std::vector<kvc::ScoreSeq> seqs;
+  std::vector<kvc::ScoreUnit> u0, u1;
+  std::vector<int32_t> meta, least, rows;
+  int32_t tok = 0;
+  bool few = true;
+  int64_t key_tiles = 0;
+  for (int s = 0; s < b; ++s) {
+    if (n_q[s] == 0) continue;
+    std::string err;
+    if (!c->bk.book.prefill_keys(s, n_q[s], rows, err)) return fail(KVC_ERR_STATE, "%s", err.c_str());
+    const int32_t len = (int32_t)rows.size();
+    seqs.push_back({tok, len - n_q[s], len, (int32_t)meta.size(), (int32_t)((int64_t)H * c->off[s]), (int32_t)c->cap[s], s, 0});
+    rows.resize(align_up(rows.size(), 128), kvc::Book::kPrefillNever << 1);
+    for (size_t i = 0; i < rows.size(); i += 128) {
+      int32_t lo = kvc::Book::kPrefillNever;
+      for (size_t j = i; j < i + 128; ++j) lo = std::min(lo, rows[j] >> 1);
+      least.push_back(lo);
+    }
+    meta.insert(meta.end(), rows.begin(), rows.end());
+    tok += n_q[s];
+    few = few && n_q[s] <= 128;
+    key_tiles += (len + 127) / 128;
+  }
+  // key tiles of a unit of the second pass where its query tile stays: two waves of units, sixteen tiles at most
+  const int64_t slots = (int64_t)kvc::score_ctas_per_sm(c->cfg.d_head, c->cfg.rotary_dim > 0) * c->num_sms;
+  const int64_t per = few ? std::max<int64_t>(1, std::min<int64_t>(16, key_tiles * H / (2 * slots))) : 1;
+  for (size_t i = 0; i < seqs.size(); ++i) {
+    const kvc::ScoreSeq& q = seqs[i];
+    for (int32_t r = q.q0, qt = 0; r < q.len; r += 128, ++qt) {
+      const int32_t nk = (std::min(r + 128, q.len) + 127) / 128;
+      for (int32_t k = 0; k < n_split; ++k)
+        u0.push_back({(int32_t)i, qt, (int32_t)((int64_t)nk * k / n_split), (int32_t)((int64_t)nk * (k + 1) / n_split), k, 0, 0, 0});
+    }
+    const int32_t nkt = (q.len + 127) / 128;
+    for (int32_t k = 0; k < nkt; k += (int32_t)per)
+      u1.push_back({(int32_t)i, 0, k, std::min(nkt, k + (int32_t)per), 0, 0, 0, 0});
+  }
+  // the longest first: the first pass's by their key tiles, the second's by the query tiles that see them
+  std::stable_sort(u0.begin(), u0.end(), [](const kvc::ScoreUnit& x, const kvc::ScoreUnit& y) { return x.kt1 - x.kt0 > y.kt1 - y.kt0; });
+  auto q_tiles = [&](const kvc::ScoreUnit& u) { return seqs[u.seq].len - std::max(seqs[u.seq].q0, u.kt0 * 128); };
+  if (!few) std::stable_sort(u1.begin(), u1.end(), [&](const kvc::ScoreUnit& x, const kvc::ScoreUnit& y) { return q_tiles(x) > q_tiles(y); });
+  const size_t bytes = score_plan_bytes((int64_t)seqs.size(), (int64_t)u0.size(), (int64_t)u1.size(), (int64_t)least.size(), (int64_t)meta.size());
+  if (bytes > c->ws.sp_bytes) return fail(KVC_ERR_STATE, "the plan of a prompt's scores exceeds the workspace");
+  cudaError_t e;
+  unsigned char* img = c->ring.reserve(bytes, &e);
+  if (!img) return e != cudaSuccess ? cuda_fail(e, "staging") : fail(KVC_ERR_INVALID_ARG, "score plan exceeds ring");
+  c->sp_unit0 = sizeof(kvc::ScoreSeq) * seqs.size();
+  c->sp_unit1 = c->sp_unit0 + sizeof(kvc::ScoreUnit) * u0.size();
+  c->sp_least = c->sp_unit1 + sizeof(kvc::ScoreUnit) * u1.size();
+  c->sp_meta = c->sp_least + align_up(4 * least.size(), 16);
+  if (!seqs.empty()) {
+    std::memcpy(img, seqs.data(), sizeof(kvc::ScoreSeq) * seqs.size());
+    std::memcpy(img + c->sp_unit0, u0.data(), sizeof(kvc::ScoreUnit) * u0.size());
+    std::memcpy(img + c->sp_unit1, u1.data(), sizeof(kvc::ScoreUnit) * u1.size());
+    std::memcpy(img + c->sp_least, least.data(), 4 * least.size());
+    std::memcpy(img + c->sp_meta, meta.data(), 4 * meta.size());
+  }
+  c->sp_version = UINT64_MAX;  // until the plan is uploaded
+  e = c->ring.commit(c->wsp(c->ws.sp), bytes, stream);
+  if (e != cudaSuccess) return cuda_fail(e, "upload score plan");
+  c->sp_version = c->version;
+  c->sp_nq.assign(n_q, n_q + b);
+  c->sp_units0 = (int)u0.size();
+  c->sp_units1 = (int)u1.size();
+  c->sp_few = few;
+  return KVC_OK;
+}
+
+kvc_status kvc_score_prompt(kvc_cache* c, int layer, const void* q, const int32_t* n_q, float scale, void* scratch,
+                            size_t scratch_bytes, void* stream_) {
+  kvc_status st = score_check(c, n_q);
+  if (st != KVC_OK) return st;
+  if (layer < 0 || layer >= c->cfg.M) return fail(KVC_ERR_INVALID_ARG, "layer %d out of range", layer);
+  if (std::all_of(n_q, n_q + c->cfg.b, [](int32_t n) { return n == 0; })) return ok();
+  if (!q || !scratch) return fail(KVC_ERR_INVALID_ARG, "q/scratch are NULL");
+  if (reinterpret_cast<uintptr_t>(q) & 15) return fail(KVC_ERR_INVALID_ARG, "q must be 16-byte aligned");
+  if (reinterpret_cast<uintptr_t>(scratch) & 255) return fail(KVC_ERR_INVALID_ARG, "scratch must be 256-byte aligned");
+  if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(KVC_ERR_INVALID_ARG, "scale must be positive and finite");
+  if (layer >= c->layers_done) return fail(KVC_ERR_STATE, "layer %d of the last tokens is not written yet", layer);
+  if (!c->scores) return fail(KVC_ERR_STATE, "the cache has no scores (kvc_set_scores)");
+  size_t need = 0;
+  st = kvc_score_scratch_bytes(c, n_q, &need);
+  if (st != KVC_OK) return st;
+  if (scratch_bytes < need) return fail(KVC_ERR_INVALID_ARG, "%zu bytes of scratch, %zu needed", scratch_bytes, need);
+  cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+  st = c->ensure_cuda(stream);
+  if (st != KVC_OK) return st;
+  const int n_split = score_splits(c, n_q);
+  if (c->sp_version != c->version || !std::equal(c->sp_nq.begin(), c->sp_nq.end(), n_q)) {
+    st = plan_score(c, n_q, n_split, stream);
+    if (st != KVC_OK) return st;
+  }
+  if (c->sp_units0 == 0) return ok();
+  cudaError_t e = cudaSuccess;
+  if (!c->sp_maps_ready) {
+    e = kvc::encode_key_map(c->geom(), c->bufs(), c->sp_maps.k);
+    if (e != cudaSuccess) return cuda_fail(e, "cuTensorMapEncodeTiled (K planes)");
+    c->sp_maps_ready = true;
+  }
+  const unsigned char* plan = c->wsp(c->ws.sp);
+  kvc::ScoreArgs a;
+  std::memset(&a, 0, sizeof a);
+  a.layer = layer;
+  a.H = c->cfg.H;
+  a.rot = c->cfg.rotary_dim;
+  a.C = c->C;
+  for (int s = 0; s < c->cfg.b; ++s) a.n_tok += n_q[s];
+  a.seqs = reinterpret_cast<const kvc::ScoreSeq*>(plan);
+  a.units = reinterpret_cast<const kvc::ScoreUnit*>(plan + c->sp_unit0);
+  a.n_units = c->sp_units0;
+  a.meta = reinterpret_cast<const int32_t*>(plan + c->sp_meta);
+  a.least = reinterpret_cast<const int32_t*>(plan + c->sp_least);
+  a.lse = static_cast<float2*>(scratch);
+  a.n_split = n_split;
+  a.scores = c->scores;
+  a.c2 = (float)((double)scale * 1.4426950408889634);
+  a.status = c->bufs().status;
+  a.wait_limit_ns = 2000000000ull;
+  a.q = static_cast<const uint16_t*>(q);
+  a.pos = c->cfg.pos_base;
+  const kvc::Static sta = c->stat();
+  a.off = sta.off;
+  a.rope_g = sta.rope_g;
+  kvc::ScoreMaps maps = c->sp_maps;
+  const void* q_hi = q;
+  const void* q_lo = q;
+  if (a.rot > 0) {
+    unsigned char* at = static_cast<unsigned char*>(scratch) + align_up(8 * (size_t)n_split * a.H * (size_t)a.n_tok, 256);
+    a.q_hi = reinterpret_cast<uint16_t*>(at);
+    a.q_lo = reinterpret_cast<uint16_t*>(at + align_up(2 * (size_t)a.n_tok * a.H * c->cfg.d_head, 256));
+    q_hi = a.q_hi;
+    q_lo = a.q_lo;
+    e = kvc::launch_score_rotate(c->geom(), a, stream);
+    if (e != cudaSuccess) return cuda_fail(e, "query rotation kernel");
+    c->launches += 1;
+  }
+  e = kvc::encode_query_map(c->geom(), q_hi, a.n_tok, maps.q);
+  if (e == cudaSuccess) e = kvc::encode_query_map(c->geom(), q_lo, a.n_tok, maps.q_lo);
+  if (e != cudaSuccess) return cuda_fail(e, "cuTensorMapEncodeTiled (queries)");
+  e = kvc::launch_score_lse(c->geom(), maps, a, stream);
+  if (e != cudaSuccess) return cuda_fail(e, "score kernel (first pass)");
+  c->launches += 1;
+  a.units = reinterpret_cast<const kvc::ScoreUnit*>(plan + c->sp_unit1);
+  a.n_units = c->sp_units1;
+  e = kvc::launch_score_sum(c->geom(), maps, a, c->sp_few, stream);
+  c->last_was_decode = false;
+  if (e != cudaSuccess) return cuda_fail(e, "score kernel (second pass)");
+  c->launches += 1;
   return ok();
 }
 

@@ -1,0 +1,461 @@
+// Attention weights of a prompt's queries, summed for each key: what the scores of a prompt's rows are made of.
+//
+//   score_i += sum over the queries t that see row i of  2^(z_ti - L_t),   z_ti = scale log2(e) <q_t, k_i>,
+//   L_t = log2 sum over the rows that t sees of 2^z_ti
+//
+// in two passes over the products of queries and keys on the tensor cores (tcgen05, accumulators in TMEM, operands by
+// TMA): keeping z between them would write and read 4 bytes a pair where the product costs d_head multiply-adds.
+//
+//   pass 0   S = Q K^T, a query per thread and a key per column: the running maximum and sum of each query.  A unit is
+//            128 queries of one head against some key tiles (all, or a part where the units are few).
+//   pass 1   S^T = K Q^T, a key per thread and a query per column, so that a key's sum over the queries stays in one
+//            thread's register: no shuffles, no atomics, one addition to the score at the end.  A unit is some key tiles
+//            of one head against every query tile that sees them; where there is one query tile, it stays and the key
+//            tiles stream by (few), else the key tile stays and the query tiles stream by.
+//
+// Mask: row i is visible to the query at stored row t exactly when i <= t <= hid(i), except that a <CL> query sees only
+// itself.  Tiles wholly visible skip the test.
+//
+// Warps 0 to 3 take S from TMEM (two buffers of 128 columns), warp 4 loads the tiles, warp 5 issues the products.
+// Rotated queries come from a kernel of their own as a high and a low 16-bit part, each a product of its own.
+// What bounds it: the exponentials, two a visible pair, and the instructions around them.
+#include <cuda.h>
+
+#include <atomic>
+#include <cstring>
+
+#include "device_common.cuh"
+#include "kernels.hpp"
+#include "tensor_core.cuh"
+
+namespace kvc {
+namespace {
+
+constexpr int kScThreads = 192;
+constexpr int kRows = 128;  // queries, and keys, of a tile
+enum Pass { kLse = 0, kSumFew = 1, kSumMany = 2 };
+
+template <int D, bool LO, int PASS>
+struct ScCfg {
+  static constexpr int SW = (2 * D) % 128 == 0 ? 128 : (2 * D) % 64 == 0 ? 64 : 32;
+  static constexpr int SUB = SW / 2;
+  static constexpr int NSUB = D / SUB;
+  static constexpr uint32_t SUBB = kRows * SW;
+  static constexpr uint32_t TILE = kRows * D * 2;
+  static constexpr uint32_t QT = TILE * (LO ? 2 : 1);
+  // Stages: what two CTAs per SM leave room for, up to three; with two parts of the queries at 128 columns one CTA.
+  static constexpr uint32_t ROOM = 110 * 1024;
+  static constexpr int fit(uint32_t fixed, uint32_t each) {
+    return fixed + 3 * each <= ROOM ? 3 : 2;
+  }
+  static constexpr int KS = PASS == kSumMany ? 1 : fit(QT, TILE);
+  static constexpr int QS = PASS == kSumMany ? fit(TILE, QT) : 1;
+  static constexpr uint32_t Q_OFF = KS * TILE;
+  static constexpr uint32_t NEED = Q_OFF + QS * QT + 1024;  // + aligning the base
+  // no third CTA on an SM, which would wait for columns of TMEM
+  static constexpr uint32_t SMEM = NEED < 80 * 1024 ? 80 * 1024 : NEED;
+  static constexpr int CPS = SMEM <= ROOM + 1024 ? 2 : 1;
+  static_assert(SMEM <= 227 * 1024, "shared memory");
+};
+
+template <typename T, int D, bool LO, int PASS>
+__global__ void __launch_bounds__(kScThreads, ScCfg<D, LO, PASS>::CPS)
+    score_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mq,
+                 const __grid_constant__ CUtensorMap mql, const ScoreArgs a) {
+  using Cf = ScCfg<D, LO, PASS>;
+  constexpr int KS = Cf::KS, QS = Cf::QS;
+  extern __shared__ unsigned char raw[];
+  __shared__ __align__(8) uint64_t k_full[KS], k_empty[KS], q_full[QS], q_empty[QS], s_full[2], s_empty[2];
+  __shared__ uint32_t tmem_slot;
+  __shared__ __align__(16) float s_neg[2][kRows];  // pass 1: -L of a tile's queries
+  const uint32_t sm = (smem_addr(raw) + 1023u) & ~1023u;
+  const int warp = uniform((int)(threadIdx.x >> 5)), lane = threadIdx.x & 31, tid = threadIdx.x;
+  const uint32_t limit_ns = (uint32_t)a.wait_limit_ns;
+  if (warp == 0) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_slot)), "r"(256u)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  if (tid == 32) {
+    for (int i = 0; i < KS; ++i) {
+      mbar_init(&k_full[i], 1);
+      mbar_init(&k_empty[i], 1);
+    }
+    for (int i = 0; i < QS; ++i) {
+      mbar_init(&q_full[i], 1);
+      mbar_init(&q_empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&s_full[i], 1);
+      mbar_init(&s_empty[i], 128);
+    }
+    fence_mbar_init();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  // Not before this CTA has its columns of TMEM: a CTA of the second pass that took them would wait for this one.
+  pdl_launch_dependents();
+  const uint32_t tmem = tmem_slot;
+  const int item = (int)(blockIdx.x / (unsigned)a.H), h = (int)(blockIdx.x - (unsigned)item * a.H);
+  const ScoreUnit un = a.units[item];
+  const ScoreSeq sq = a.seqs[un.seq];
+  const int nqt = (sq.len - sq.q0 + kRows - 1) / kRows;
+  // the query tiles of key tile kt: those that end at or after its first row
+  auto first_qt = [&](int kt) { return PASS == kLse ? un.qt : kt * kRows <= sq.q0 ? 0 : (kt * kRows - sq.q0) / kRows; };
+  auto end_qt = [&]() { return PASS == kLse ? un.qt + 1 : nqt; };
+  bool ok = true;
+
+  if (warp == 4) {
+    // ---------------- loads ----------------
+    if (lane == 0) {
+      const int row0 = (int)((int64_t)a.layer * a.H * a.C) + sq.row0 + h * sq.cap;
+      uint32_t nk = 0, nq = 0;
+      for (int kt = un.kt0; ok && kt < un.kt1; ++kt, ++nk) {
+        const int st = nk % KS;
+        if (nk >= KS && !(ok = pf_wait(&k_empty[st], (nk / KS & 1) ^ 1, limit_ns))) break;
+        mbar_arrive_expect_tx(&k_full[st], Cf::TILE);
+#pragma unroll
+        for (int i = 0; i < Cf::NSUB; ++i)
+          tma_load_2d(sm + st * Cf::TILE + i * Cf::SUBB, &mk, i * Cf::SUB, row0 + kt * kRows, &k_full[st]);
+        for (int qt = first_qt(kt); qt < end_qt(); ++qt) {
+          if (PASS != kSumMany && nq > 0) break;  // one query tile, which stays
+          const int qs = nq % QS;
+          if (nq >= QS && !(ok = pf_wait(&q_empty[qs], (nq / QS & 1) ^ 1, limit_ns))) break;
+          mbar_arrive_expect_tx(&q_full[qs], Cf::QT);
+          const uint32_t dst = sm + Cf::Q_OFF + qs * Cf::QT;
+#pragma unroll
+          for (int i = 0; i < Cf::NSUB; ++i) {
+            tma_load_3d(dst + i * Cf::SUBB, &mq, i * Cf::SUB, h, sq.tok0 + qt * kRows, &q_full[qs]);
+            if constexpr (LO) tma_load_3d(dst + Cf::TILE + i * Cf::SUBB, &mql, i * Cf::SUB, h, sq.tok0 + qt * kRows, &q_full[qs]);
+          }
+          ++nq;
+        }
+      }
+      // never leave with copies in flight (every full barrier's last phase)
+      for (int i = 0; i < KS; ++i)
+        if ((uint32_t)i < nk) (void)pf_wait(&k_full[i], ((nk - 1 - i) / KS) & 1, limit_ns);
+      for (int i = 0; i < QS; ++i)
+        if ((uint32_t)i < nq) (void)pf_wait(&q_full[i], ((nq - 1 - i) / QS) & 1, limit_ns);
+    }
+    __syncwarp();
+  } else if (warp == 5) {
+    // ---------------- products ----------------
+    constexpr uint32_t id = mma_idesc(Pack16<T>::kType, 0, kRows, kRows);
+    constexpr uint32_t SBO = 8 * Cf::SW;
+    auto uni_wait = [&](uint64_t* bar, uint32_t parity) -> bool { return __all_sync(0xFFFFFFFFu, pf_wait(bar, parity, limit_ns)); };
+    uint32_t nk = 0, nq = 0, step = 0;
+    for (int kt = un.kt0; ok && kt < un.kt1; ++kt, ++nk) {
+      const int st = nk % KS;
+      if (!(ok = uni_wait(&k_full[st], nk / KS & 1))) break;
+      const uint32_t k_d = desc_lo(sm + st * Cf::TILE, 16);
+      const int qe = end_qt();
+      for (int qt = first_qt(kt); qt < qe; ++qt, ++step) {
+        const int qs = PASS == kSumMany ? nq % QS : 0, sb = step & 1;
+        if ((PASS == kSumMany || nq == 0) && !(ok = uni_wait(&q_full[qs], nq / QS & 1))) break;
+        if (step >= 2 && !(ok = uni_wait(&s_empty[sb], (step / 2 & 1) ^ 1))) break;
+        tc_fence_after();
+        const uint32_t q_d = desc_lo(sm + Cf::Q_OFF + qs * Cf::QT, 16);
+        if (elect_one()) {
+#pragma unroll
+          for (int part = 0; part < (LO ? 2 : 1); ++part) {
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk) {
+              const uint32_t off = ((kk * 16) / Cf::SUB * Cf::SUBB + (kk * 16) % Cf::SUB * 2) >> 4;
+              const uint64_t dk = desc(k_d + off, SBO, Cf::SW), dq = desc(q_d + part * (Cf::TILE >> 4) + off, SBO, Cf::SW);
+              tc_mma(tmem + sb * kRows, PASS == kLse ? dq : dk, PASS == kLse ? dk : dq, id, part + kk > 0);
+            }
+          }
+          tc_commit(&s_full[sb]);
+          if (PASS == kSumMany) tc_commit(&q_empty[qs]);
+          if (qt + 1 == qe) tc_commit(&k_empty[st]);
+        }
+        __syncwarp();
+        ++nq;
+      }
+    }
+  } else {
+    // ---------------- S ----------------
+    const uint32_t my = tmem + ((uint32_t)(warp * 32) << 16);
+    const float c2 = a.c2;
+    uint32_t step = 0;
+    auto s_wait = [&]() -> bool {
+      const bool got = __all_sync(0xFFFFFFFFu, pf_wait(&s_full[step & 1], step / 2 & 1, limit_ns));
+      tc_fence_after();
+      return got;
+    };
+    auto s_done = [&]() {
+      tc_fence_before();
+      mbar_arrive(&s_empty[step & 1]);
+      ++step;
+    };
+    if constexpr (PASS == kLse) {
+      const int t = sq.q0 + un.qt * kRows + tid;  // the query's stored row
+      const int t0 = sq.q0 + un.qt * kRows, t1 = min(t0 + kRows, sq.len);
+      const bool mine = t < sq.len;
+      const bool is_cl = mine && (a.meta[sq.moff + t] & 1);
+      float m = -INFINITY, l = 0.f;
+      for (int kt = un.kt0; kt < un.kt1; ++kt) {
+        const int i0 = kt * kRows;
+        const bool spans = a.least[sq.moff / kRows + kt] < t1 - 1;  // a row of the tile is hidden from some of the queries
+        const bool test = spans || i0 + kRows - 1 > t0;
+        if (!(ok = s_wait())) break;
+#pragma unroll 1
+        for (int c = 0; c < kRows; c += 32) {
+          float s[32];
+          tmem_ld32(my + (step & 1) * kRows + c, s);
+          tmem_wait_ld();
+          if (test) {
+            const int last = t - i0 - c;  // columns past it are later rows
+            if (spans) {
+              const int4* hid = reinterpret_cast<const int4*>(a.meta + sq.moff + i0 + c);
+#pragma unroll
+              for (int x = 0; x < 8; ++x) {
+                const int4 v = __ldg(hid + x);
+                if (t > v.x >> 1) s[4 * x] = -INFINITY;
+                if (t > v.y >> 1) s[4 * x + 1] = -INFINITY;
+                if (t > v.z >> 1) s[4 * x + 2] = -INFINITY;
+                if (t > v.w >> 1) s[4 * x + 3] = -INFINITY;
+              }
+            }
+#pragma unroll
+            for (int x = 0; x < 32; ++x)
+              if (x > last) s[x] = -INFINITY;
+          }
+          float mx = fmaxf(s[0], s[1]);
+#pragma unroll
+          for (int x = 2; x < 32; x += 2) mx = fmaxf(mx, fmaxf(s[x], s[x + 1]));
+          const float mn = fmaxf(m, mx * c2), mu = mn == -INFINITY ? 0.f : mn;
+          float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
+          const float2 cc = make_float2(c2, c2), mm = make_float2(-mu, -mu);
+#pragma unroll
+          for (int x = 0; x < 32; x += 4) {
+            const float2 z0 = __ffma2_rn(make_float2(s[x], s[x + 1]), cc, mm);
+            const float2 z1 = __ffma2_rn(make_float2(s[x + 2], s[x + 3]), cc, mm);
+            sum0 = __fadd2_rn(sum0, make_float2(ex2(z0.x), ex2(z0.y)));
+            sum1 = __fadd2_rn(sum1, make_float2(ex2(z1.x), ex2(z1.y)));
+          }
+          l = l * ex2(m - mu) + ((sum0.x + sum0.y) + (sum1.x + sum1.y));
+          m = mn;
+        }
+        s_done();
+      }
+      if (ok && mine)
+        a.lse[((int64_t)un.split * a.H + h) * a.n_tok + sq.tok0 + un.qt * kRows + tid] =
+            is_cl ? make_float2(INFINITY, 1.f) : make_float2(m, l);
+    } else {
+      // -L of query tile qt's tid-th query; a <CL> query's is -infinity
+      auto neg_lse = [&](int qt) -> float {
+        const int x = qt * kRows + tid;
+        if (sq.q0 + x >= sq.len) return -INFINITY;
+        const float2* p = a.lse + (int64_t)h * a.n_tok + sq.tok0 + x;
+        const int64_t step_s = (int64_t)a.H * a.n_tok;
+        float M = -INFINITY, L = 0.f;
+        for (int s = 0; s < a.n_split; ++s) {
+          const float2 v = __ldcg(p + s * step_s);
+          if (v.x == INFINITY) return -INFINITY;  // a <CL> query, in every split
+          const float Mn = fmaxf(M, v.x), Mu = Mn == -INFINITY ? 0.f : Mn;
+          L = L * ex2(M - Mu) + v.y * ex2(v.x - Mu);
+          M = Mn;
+        }
+        return -(M + log2f(L));
+      };
+      pdl_wait();  // the queries' sums
+      float next = neg_lse(first_qt(un.kt0));
+      for (int kt = un.kt0; kt < un.kt1; ++kt) {
+        const int i = kt * kRows + tid;
+        const bool row = i < sq.len;
+        const int meta = row ? a.meta[sq.moff + i] : 0, hid = meta >> 1;
+        float total = 0.f;
+        const int qe = end_qt();
+        for (int qt = first_qt(kt); qt < qe; ++qt) {
+          const int t0 = sq.q0 + qt * kRows, t1 = min(t0 + kRows, sq.len);
+          const float mine = next;
+          s_neg[step & 1][tid] = mine;
+          // also whether a query of the tile is a <CL> or none
+          uint32_t odd = mine == -INFINITY;
+          asm volatile(
+              "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %0, 0;\n\tbarrier.cta.red.or.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+              : "+r"(odd)
+              :
+              : "memory");
+          {  // the next step's
+            const bool more = qt + 1 < qe;
+            if (more || kt + 1 < un.kt1) {
+              const int nx = more ? qt + 1 : first_qt(kt + 1);
+              if (PASS == kSumMany) next = neg_lse(nx);
+            }
+          }
+          const int lo = max(i - t0, 0), hi = row ? min(hid, t1 - 1) - t0 : -1;  // the columns that see row i
+          const bool whole = __all_sync(0xFFFFFFFFu, lo == 0 && hi == kRows - 1) && !odd;
+          const float4* neg = reinterpret_cast<const float4*>(s_neg[step & 1]);
+          // after a wait that ran out the warp only keeps up with the others' barriers
+          if (!ok || !(ok = s_wait())) {
+            ++step;
+            continue;
+          }
+          float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
+          const float2 cc = make_float2(c2, c2);
+#pragma unroll 1
+          for (int c = 0; c < kRows; c += 32) {
+            float s[32];
+            tmem_ld32(my + (step & 1) * kRows + c, s);
+            tmem_wait_ld();
+#pragma unroll
+            for (int x = 0; x < 32; x += 4) {
+              const float4 n = neg[(c + x) / 4];
+              float2 z0 = __ffma2_rn(make_float2(s[x], s[x + 1]), cc, make_float2(n.x, n.y));
+              float2 z1 = __ffma2_rn(make_float2(s[x + 2], s[x + 3]), cc, make_float2(n.z, n.w));
+              if (!whole) {
+                const unsigned span = (unsigned)(hi - lo);
+                const int at = c + x - lo;
+                const bool any = hi >= lo;
+                if (!any || (unsigned)at > span || n.x == -INFINITY) z0.x = -INFINITY;
+                if (!any || (unsigned)(at + 1) > span || n.y == -INFINITY) z0.y = -INFINITY;
+                if (!any || (unsigned)(at + 2) > span || n.z == -INFINITY) z1.x = -INFINITY;
+                if (!any || (unsigned)(at + 3) > span || n.w == -INFINITY) z1.y = -INFINITY;
+              }
+              sum0 = __fadd2_rn(sum0, make_float2(ex2(z0.x), ex2(z0.y)));
+              sum1 = __fadd2_rn(sum1, make_float2(ex2(z1.x), ex2(z1.y)));
+            }
+          }
+          total += (sum0.x + sum0.y) + (sum1.x + sum1.y);
+          s_done();
+        }
+        if (ok && row) {
+          if ((meta & 1) && i >= sq.q0) total += 1.f;  // a <CL> query's weight is its own row's
+          float* sc = a.scores + ((int64_t)a.layer * a.H * a.C + sq.row0 + (int64_t)h * sq.cap + i);
+          *sc += total;
+        }
+      }
+    }
+  }
+  if (!ok) atomicOr(a.status, STATUS_TIMEOUT);
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 0) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(256u) : "memory");
+  }
+}
+
+// The queries of a 128-query tile (blockIdx.x), rotated at their positions, as high and low parts.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) score_rotate_kernel(const ScoreArgs a) {
+  constexpr int CH = D / 8;
+  const ScoreUnit un = a.units[blockIdx.x];
+  if (un.split != 0) return;
+  const ScoreSeq sq = a.seqs[un.seq];
+  const int n = min(kRows, sq.len - sq.q0 - un.qt * kRows);
+  const int half = a.rot / 2;
+  for (int x = blockIdx.y * 256 + threadIdx.x; x < n * a.H * CH; x += gridDim.y * 256) {
+    const int r = x / (a.H * CH), w = x - r * (a.H * CH), c = w % CH;
+    const int64_t at = ((int64_t)(sq.tok0 + un.qt * kRows + r) * a.H * D) + w * 8;
+    uint4 hi = *reinterpret_cast<const uint4*>(a.q + at), lo = make_uint4(0, 0, 0, 0);
+    if (c * 8 < a.rot) {
+      const bool first = c * 8 < half;  // half is a multiple of eight
+      const uint4 other = *reinterpret_cast<const uint4*>(a.q + at + (first ? half : -half));
+      const int32_t pos = a.pos[a.off[sq.s] + sq.q0 + un.qt * kRows + r];
+      const uint32_t p[4] = {hi.x, hi.y, hi.z, hi.w}, o[4] = {other.x, other.y, other.z, other.w};
+      uint32_t vh[4], vl[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float2 x2 = T::f2(p[e]), y2 = T::f2(o[e]);
+        const int i = (first ? c * 8 : c * 8 - half) + 2 * e;
+        float sn0, cs0, sn1, cs1;
+        rope_sincos_full(pos, a.rope_g[i], &sn0, &cs0);
+        rope_sincos_full(pos, a.rope_g[i + 1], &sn1, &cs1);
+        const float z0 = first ? x2.x * cs0 - y2.x * sn0 : x2.x * cs0 + y2.x * sn0;
+        const float z1 = first ? x2.y * cs1 - y2.y * sn1 : x2.y * cs1 + y2.y * sn1;
+        vh[e] = Pack16<T>::two(z0, z1);
+        const float2 back = T::f2(vh[e]);
+        vl[e] = Pack16<T>::two(z0 - back.x, z1 - back.y);
+      }
+      hi = make_uint4(vh[0], vh[1], vh[2], vh[3]);
+      lo = make_uint4(vl[0], vl[1], vl[2], vl[3]);
+    }
+    *reinterpret_cast<uint4*>(a.q_hi + at) = hi;
+    *reinterpret_cast<uint4*>(a.q_lo + at) = lo;
+  }
+}
+
+template <typename T, int D, bool LO, int PASS>
+cudaError_t launch_score_t(const ScoreMaps& maps, const ScoreArgs& a, cudaStream_t stream) {
+  using Cf = ScCfg<D, LO, PASS>;
+  static std::atomic<bool> done[64];
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  if (!done[dev].load(std::memory_order_acquire)) {
+    e = cudaFuncSetAttribute(score_kernel<T, D, LO, PASS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cf::SMEM);
+    if (e != cudaSuccess) return e;
+    done[dev].store(true, std::memory_order_release);
+  }
+  CUtensorMap mk, mq, ml;
+  std::memcpy(&mk, maps.k, sizeof mk);
+  std::memcpy(&mq, maps.q, sizeof mq);
+  std::memcpy(&ml, maps.q_lo, sizeof ml);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((int64_t)a.n_units * a.H));
+  cfg.blockDim = dim3(kScThreads);
+  cfg.dynamicSmemBytes = Cf::SMEM;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = PASS == kLse ? 0 : 1;  // the first pass starts when all before it is complete
+  return cudaLaunchKernelEx(&cfg, score_kernel<T, D, LO, PASS>, mk, mq, ml, a);
+}
+
+template <typename F>
+cudaError_t by_type(const Geometry& g, F&& f) {
+  auto dt = [&](auto dc) { return g.dtype == 1 ? f(BF16T{}, dc) : f(F16T{}, dc); };
+  switch (g.D) {
+    case 64:
+      return dt(std::integral_constant<int, 64>{});
+    case 80:
+      return dt(std::integral_constant<int, 80>{});
+    case 96:
+      return dt(std::integral_constant<int, 96>{});
+    case 128:
+      return dt(std::integral_constant<int, 128>{});
+    default:
+      return cudaErrorInvalidValue;
+  }
+}
+
+template <int PASS>
+cudaError_t launch_pass(const Geometry& g, const ScoreMaps& maps, const ScoreArgs& a, cudaStream_t stream) {
+  if (a.n_units <= 0) return cudaSuccess;
+  return by_type(g, [&](auto t, auto d) {
+    using T = decltype(t);
+    constexpr int D = decltype(d)::value;
+    return g.rot > 0 ? launch_score_t<T, D, true, PASS>(maps, a, stream) : launch_score_t<T, D, false, PASS>(maps, a, stream);
+  });
+}
+
+}  // namespace
+
+int score_ctas_per_sm(int D, bool rot) { return rot && D == 128 ? 1 : 2; }
+
+cudaError_t launch_score_rotate(const Geometry& g, const ScoreArgs& a, cudaStream_t stream) {
+  if (a.n_units <= 0) return cudaSuccess;
+  return by_type(g, [&](auto t, auto d) {
+    using T = decltype(t);
+    constexpr int D = decltype(d)::value;
+    score_rotate_kernel<T, D><<<dim3((unsigned)a.n_units, 16), 256, 0, stream>>>(a);
+    return cudaGetLastError();
+  });
+}
+
+cudaError_t launch_score_lse(const Geometry& g, const ScoreMaps& maps, const ScoreArgs& a, cudaStream_t stream) {
+  return launch_pass<kLse>(g, maps, a, stream);
+}
+
+cudaError_t launch_score_sum(const Geometry& g, const ScoreMaps& maps, const ScoreArgs& a, bool few, cudaStream_t stream) {
+  return few ? launch_pass<kSumFew>(g, maps, a, stream) : launch_pass<kSumMany>(g, maps, a, stream);
+}
+
+}  // namespace kvc
