@@ -12,7 +12,9 @@
 //      memory), stopping at the first digit whose bin stays whole;
 //   2. two scans in row order, over the rows below A and over those beyond, list the holes and the rows that fill them;
 //      the copies of one list's rows are disjoint from each other, so they need no barrier between them;
-//   3. the recent rows move down in ascending chunks, a barrier between each chunk's loads and its stores.
+//   3. the recent rows move down through shared memory with 1-D bulk copies: the first chunk is under way from the
+//      kernel's start, while the scores are sorted (moved by registers after that, the step of 12,288 streams that drop
+//      one of 1,025 rows took 231 us), and goes back once the holes are filled; the rest follow chunk by chunk.
 // What bounds it: HBM, for the rows that move, and for evictions of few rows the selection, some barriers per stream.
 #include <cuda_runtime.h>
 
@@ -45,14 +47,19 @@ __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
+__device__ __forceinline__ void bulk_s2g(void* dst, const void* src, uint32_t bytes) {
+  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(smem_addr(src)), "r"(bytes)
+               : "memory");
+}
+
 struct EvictShared {
   union {
     uint32_t hist[kBins];
     struct {
-      int32_t holes[kScan];
+      int32_t holes[kScan], srcs[2 * kScan];
     } l;
   };
-  int32_t srcs[2 * kScan];
+  uint64_t full;
   uint32_t wsum[kWarps];
   uint32_t bin, above, in_bin;
 };
@@ -83,9 +90,11 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, EvictShared& sh, uint
 template <int D>
 __global__ void __launch_bounds__(kThreads) evict_kernel(Geometry g, Static st, Buffers buf, float* __restrict__ scores,
                                                          const AffSeq* __restrict__ aff, int32_t* __restrict__ kept,
-                                                         int held, int CN) {
+                                                         int held, int chunk, int CN) {
   constexpr int VPR = D / 8;  // 16-byte vectors per row
-  extern __shared__ __align__(16) uint32_t keys[];
+  extern __shared__ __align__(128) unsigned char dyn[];
+  // `chunk` recent rows of K and then of V (of one of them in a cluster), then the keys
+  uint32_t* keys = reinterpret_cast<uint32_t*>(dyn + (size_t)chunk * (CN > 1 ? 1 : 2) * D * 2);
   __shared__ EvictShared sh;
   const int tid = threadIdx.x;
   const int rank = CN > 1 ? (int)(blockIdx.x % (unsigned)CN) : 0;
@@ -101,6 +110,19 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(Geometry g, Static st, 
   uint4* K = reinterpret_cast<uint4*>(buf.k + row0 * D);
   uint4* V = reinterpret_cast<uint4*>(buf.v + row0 * D);
   const bool in_smem = cand <= held;
+  // Recent rows [r, min(r + chunk, recent)) into shared memory; the first two of a cluster's CTAs take K and V.
+  const bool do_k = CN == 1 || (rank & 1) == 0, do_v = CN == 1 || (rank & 1) == 1;
+  auto load_recent = [&](int r) {
+    const uint32_t bytes = (uint32_t)min(chunk, recent - r) * D * 2;
+    mbar_arrive_expect_tx(&sh.full, bytes * (CN > 1 ? 1 : 2));
+    if (do_k) bulk_g2s(dyn, K + (int64_t)(cand + r) * VPR, bytes, &sh.full);
+    if (do_v) bulk_g2s(dyn + (CN > 1 ? 0 : (size_t)chunk * D * 2), V + (int64_t)(cand + r) * VPR, bytes, &sh.full);
+  };
+  if (tid == 0) {
+    mbar_init(&sh.full, 1);
+    fence_mbar_init();
+    if (rank < 2) load_recent(0);
+  }
   auto key = [&](int i) { return in_smem ? keys[i] : order_key(sc[i]); };
 
   // ------------------------------ the A-th largest score ---------------------------------------
@@ -207,7 +229,7 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(Geometry g, Static st, 
   for (int at_hole = 0; at_hole < A; at_hole += kScan) {
     const int n_hole = scan(at_hole, A, eq_hole, false, sh.l.holes, 0);
     while (n_src < n_hole && at_src < cand) {
-      n_src += scan(at_src, cand, eq_src, true, sh.srcs, n_src);
+      n_src += scan(at_src, cand, eq_src, true, sh.l.srcs, n_src);
       at_src += kScan;
     }
     if (n_hole > n_src) {  // cannot be: as many stay beyond row A as go below it
@@ -222,7 +244,7 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(Geometry g, Static st, 
       for (int u = 0; u < U; ++u) {
         const int x = v0 + u * step;
         if (x < total) {
-          const int64_t at = (int64_t)sh.srcs[x / VPR] * VPR + x % VPR;
+          const int64_t at = (int64_t)sh.l.srcs[x / VPR] * VPR + x % VPR;
           k[u] = K[at];
           v[u] = V[at];
         }
@@ -239,7 +261,7 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(Geometry g, Static st, 
     }
     if (rank == 0)
       for (int j = tid; j < n_hole; j += kThreads) {
-        const int to = sh.l.holes[j], from = sh.srcs[j];
+        const int to = sh.l.holes[j], from = sh.l.srcs[j];
         sc[to] = sc[from];
         if (kp != nullptr) kp[to] = from;
       }
@@ -250,13 +272,13 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(Geometry g, Static st, 
 #pragma unroll
     for (int u = 0; u < kScan / kThreads; ++u) {
       const int j = u * kThreads + tid;
-      if (j < left) keep_src[u] = sh.srcs[n_hole + j];
+      if (j < left) keep_src[u] = sh.l.srcs[n_hole + j];
     }
     __syncthreads();
 #pragma unroll
     for (int u = 0; u < kScan / kThreads; ++u) {
       const int j = u * kThreads + tid;
-      if (j < left) sh.srcs[j] = keep_src[u];
+      if (j < left) sh.l.srcs[j] = keep_src[u];
     }
     n_src = left;
     __syncthreads();
@@ -267,35 +289,23 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(Geometry g, Static st, 
     __syncthreads();
 
   // ------------------------------ the recent rows move down ------------------------------------
-  // A cluster's CTAs take one of K and V each, and parts of the rows' columns.
-  {
-    const bool do_k = CN == 1 || (rank & 1) == 0, do_v = CN == 1 || (rank & 1) == 1;
-    const int parts = CN > 1 ? CN / 2 : 1, part = CN > 1 ? rank / 2 : 0;
-    const int c0 = part * VPR / parts, W = (part + 1) * VPR / parts - c0;
-    constexpr int U = 4;
-    const int total = recent * W;
-    const int64_t from = (int64_t)cand * VPR + c0, to = (int64_t)A * VPR + c0;
-    for (int v0 = 0; v0 < total; v0 += U * kThreads) {
-      uint4 k[U], v[U];
-      int at[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int x = v0 + u * kThreads + tid;
-        at[u] = x / W * VPR + x % W;
-        if (x < total) {
-          if (do_k) k[u] = K[from + at[u]];
-          if (do_v) v[u] = V[from + at[u]];
-        }
+  // Rows move down, so a chunk's places lie below every later chunk's rows.
+  if (tid == 0 && rank < 2) {
+    bool ok = true;
+    int phase = 0;
+    for (int r = 0; r < recent; r += chunk, phase ^= 1) {
+      if (r > 0) {
+        asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // the last chunk is read
+        load_recent(r);
       }
-      __syncthreads();  // rows move down: this chunk's destinations lie below every later chunk's sources
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (v0 + u * kThreads + tid < total) {
-          if (do_k) K[to + at[u]] = k[u];
-          if (do_v) V[to + at[u]] = v[u];
-        }
-      }
+      if (!(ok = mbar_wait_bounded(&sh.full, phase, 2000000000ull))) break;
+      const uint32_t bytes = (uint32_t)min(chunk, recent - r) * D * 2;
+      if (do_k) bulk_s2g(K + (int64_t)(A + r) * VPR, dyn, bytes);
+      if (do_v) bulk_s2g(V + (int64_t)(A + r) * VPR, dyn + (CN > 1 ? 0 : (size_t)chunk * D * 2), bytes);
+      asm volatile("cp.async.bulk.commit_group;" ::: "memory");
     }
+    if (!ok) atomicOr(buf.status, STATUS_TIMEOUT);
+    asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   }
   if (rank == 0) {
     const bool meta = m == 0 && h == 0;  // the sequence's positions and history indices
@@ -325,27 +335,32 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(Geometry g, Static st, 
 
 template <int D>
 cudaError_t launch_evict_t(const Geometry& g, const Static& st, const Buffers& buf, float* scores, const AffSeq* aff,
-                           int n_aff, int64_t max_len, int32_t* kept, int num_sms, cudaStream_t stream) {
+                           int n_aff, int64_t max_cand, int64_t max_recent, int32_t* kept, int num_sms, cudaStream_t stream) {
   static std::atomic<bool> done[64];
+  constexpr int kMost = 200 * 1024;  // of dynamic shared memory
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
   if (!done[dev].load(std::memory_order_acquire)) {
-    e = cudaFuncSetAttribute(evict_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, 4 * kMaxHeldKeys);
+    e = cudaFuncSetAttribute(evict_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
     if (e != cudaSuccess) return e;
     done[dev].store(true, std::memory_order_release);
   }
   const int64_t units = (int64_t)n_aff * g.M * g.H;
   // keys that do not fit are read again from the scores, which the CTAs of a cluster would change under each other
-  const int held = (int)std::min<int64_t>(max_len, kMaxHeldKeys);
+  const int held = (int)std::min<int64_t>(max_cand, kMaxHeldKeys);
   int cn = 1;
-  if (max_len <= kMaxHeldKeys)
+  if (max_cand <= kMaxHeldKeys)
     while (2 * cn <= kMaxCluster && 2 * cn * units <= 2 * num_sms) cn *= 2;
+  // recent rows of a chunk: 32 KB of K and V
+  const int chunk = (int)std::min<int64_t>(max_recent, (cn > 1 ? 32 : 16) * 1024 / (D * 2));
+  const size_t smem = (size_t)chunk * (cn > 1 ? 1 : 2) * D * 2 + 4 * (size_t)held;
+  static_assert(32 * 1024 + 4 * kMaxHeldKeys <= kMost, "shared memory");
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(units * cn));
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = 4 * (size_t)held;
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -354,23 +369,23 @@ cudaError_t launch_evict_t(const Geometry& g, const Static& st, const Buffers& b
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = cn > 1 ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, evict_kernel<D>, g, st, buf, scores, aff, kept, held, cn);
+  return cudaLaunchKernelEx(&cfg, evict_kernel<D>, g, st, buf, scores, aff, kept, held, chunk, cn);
 }
 
 }  // namespace
 
 cudaError_t launch_evict(const Geometry& g, const Static& st, const Buffers& buf, float* scores, const AffSeq* aff,
-                         int n_aff, int64_t max_len, int32_t* kept, int num_sms, cudaStream_t stream) {
+                         int n_aff, int64_t max_cand, int64_t max_recent, int32_t* kept, int num_sms, cudaStream_t stream) {
   if (n_aff <= 0) return cudaSuccess;
   switch (g.D) {
     case 64:
-      return launch_evict_t<64>(g, st, buf, scores, aff, n_aff, max_len, kept, num_sms, stream);
+      return launch_evict_t<64>(g, st, buf, scores, aff, n_aff, max_cand, max_recent, kept, num_sms, stream);
     case 80:
-      return launch_evict_t<80>(g, st, buf, scores, aff, n_aff, max_len, kept, num_sms, stream);
+      return launch_evict_t<80>(g, st, buf, scores, aff, n_aff, max_cand, max_recent, kept, num_sms, stream);
     case 96:
-      return launch_evict_t<96>(g, st, buf, scores, aff, n_aff, max_len, kept, num_sms, stream);
+      return launch_evict_t<96>(g, st, buf, scores, aff, n_aff, max_cand, max_recent, kept, num_sms, stream);
     case 128:
-      return launch_evict_t<128>(g, st, buf, scores, aff, n_aff, max_len, kept, num_sms, stream);
+      return launch_evict_t<128>(g, st, buf, scores, aff, n_aff, max_cand, max_recent, kept, num_sms, stream);
     default:
       return cudaErrorInvalidValue;
   }

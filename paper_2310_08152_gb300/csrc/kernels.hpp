@@ -180,10 +180,10 @@ cudaError_t launch_compact_scores(const Geometry& g, const Static& st, float* sc
                                   const int32_t* src_map, cudaStream_t stream);
 
 // Eviction (evict.cu): in every (layer, head) stream of the n_aff sequences, len_new of len_old rows stay, the last
-// `first_row` of them (the recent ones) and those with the largest scores.  max_len: the longest len_old; kept: [M][H * C]
-// or NULL, the earlier row number of each kept row.
+// `first_row` of them (the recent ones) and those with the largest scores.  max_cand, max_recent: the most candidates and
+// recent rows of a stream; kept: [M][H * C] or NULL, the earlier row number of each kept row.
 cudaError_t launch_evict(const Geometry& g, const Static& st, const Buffers& buf, float* scores, const AffSeq* aff,
-                         int n_aff, int64_t max_len, int32_t* kept, int num_sms, cudaStream_t stream);
+                         int n_aff, int64_t max_cand, int64_t max_recent, int32_t* kept, int num_sms, cudaStream_t stream);
 
 // ---------------------------------------------------------------------------------------------
 // Masked prefill attention (prefill.cu)

@@ -1181,8 +1181,10 @@ static kvc_status plan_score(kvc_cache* c, const int32_t* n_q, int n_split, cuda
     for (int32_t k = 0; k < nkt; k += (int32_t)per)
       u1.push_back({(int32_t)i, 0, k, std::min(nkt, k + (int32_t)per), 0, 0, 0, 0});
   }
-  // the longest first: the first pass's by their key tiles, the second's by the query tiles that see them
-  std::stable_sort(u0.begin(), u0.end(), [](const kvc::ScoreUnit& x, const kvc::ScoreUnit& y) { return x.kt1 - x.kt0 > y.kt1 - y.kt0; });
+  // the second pass begins with the keys that the first read last, which are in L2; or the longest first: the first pass's
+  // by their key tiles, the second's by the query tiles that see them
+  if (few) std::reverse(u1.begin(), u1.end());
+  if (!few) std::stable_sort(u0.begin(), u0.end(), [](const kvc::ScoreUnit& x, const kvc::ScoreUnit& y) { return x.kt1 - x.kt0 > y.kt1 - y.kt0; });
   auto q_tiles = [&](const kvc::ScoreUnit& u) { return seqs[u.seq].len - std::max(seqs[u.seq].q0, u.kt0 * 128); };
   if (!few) std::stable_sort(u1.begin(), u1.end(), [&](const kvc::ScoreUnit& x, const kvc::ScoreUnit& y) { return q_tiles(x) > q_tiles(y); });
   const size_t bytes = score_plan_bytes((int64_t)seqs.size(), (int64_t)u0.size(), (int64_t)u1.size(), (int64_t)least.size(), (int64_t)meta.size());
@@ -1522,20 +1524,21 @@ kvc_status kvc_evict(kvc_cache* c, const int64_t* keep, const int64_t* recent, i
   c->bk.book.apply_evict(plan);
   c->fill_state(img);
   kvc::AffSeq* aff = reinterpret_cast<kvc::AffSeq*>(img + c->ws.dyn_payload);
-  int64_t max_len = 0;
+  int64_t max_cand = 0, max_recent = 0;
   for (size_t i = 0; i < plan.size(); ++i) {
     std::memset(&aff[i], 0, sizeof(kvc::AffSeq));
     aff[i].s = plan[i].s;
     aff[i].len_old = (int32_t)plan[i].len_old;
     aff[i].len_new = (int32_t)plan[i].keep;
     aff[i].first_row = (int32_t)plan[i].recent;
-    max_len = std::max(max_len, plan[i].len_old);
+    max_cand = std::max(max_cand, plan[i].len_old - plan[i].recent);
+    max_recent = std::max(max_recent, plan[i].recent);
   }
   e = c->ring.commit(c->wsp(c->ws.dyn), bytes, stream);
   if (e != cudaSuccess) return cuda_fail(e, "upload eviction plan");
   e = kvc::launch_evict(c->geom(), c->stat(), c->bufs(), c->scores,
                         reinterpret_cast<const kvc::AffSeq*>(c->wsp(c->ws.dyn + c->ws.dyn_payload)), (int)plan.size(),
-                        max_len, kept, c->num_sms, stream);
+                        max_cand, max_recent, kept, c->num_sms, stream);
   if (e != cudaSuccess) return cuda_fail(e, "eviction kernel");
   c->launches += 1;
   c->last_was_decode = false;

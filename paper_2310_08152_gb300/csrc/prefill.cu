@@ -174,12 +174,6 @@ __device__ __forceinline__ uint4 ld_shared_v4(uint32_t addr) {
 }
 
 
-// Bits [0, n) of a 32-bit word, n clamped to [0, 32].
-__device__ __forceinline__ uint32_t low_bits(int n) {
-  uint32_t r;
-  asm("bmsk.clamp.b32 %0, 0, %1;" : "=r"(r) : "r"(max(n, 0)));
-  return r;
-}
 // The maximum, NaN if one of them is.
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float r;

@@ -14,9 +14,11 @@
 //            tiles stream by (few), else the key tile stays and the query tiles stream by.
 //
 // Mask: row i is visible to the query at stored row t exactly when i <= t <= hid(i), except that a <CL> query sees only
-// itself.  Tiles wholly visible skip the test.
+// itself.
 //
-// Warps 0 to 3 take S from TMEM (two buffers of 128 columns), warp 4 loads the tiles, warp 5 issues the products.
+// Eight warps take S from TMEM (two buffers of 128 columns), 64 columns each, so that four warps per scheduler hide each
+// other's latencies (four warps a CTA, two per scheduler: 325 us on OPT-1.3B-shaped prompts); one loads the tiles and one
+// issues the products.  A mask is a bit per column, looked at where a bit is missing.
 // Rotated queries come from a kernel of their own as a high and a low 16-bit part, each a product of its own.
 // What bounds it: the exponentials, two a visible pair, and the instructions around them.
 #include <cuda.h>
@@ -31,8 +33,12 @@
 namespace kvc {
 namespace {
 
-constexpr int kScThreads = 192;
+constexpr int kSWarps = 8;  // warps that take S
+constexpr int kSThreads = kSWarps * 32;
+constexpr int kScThreads = kSThreads + 64;
 constexpr int kRows = 128;  // queries, and keys, of a tile
+__device__ __forceinline__ void bar_sync(int id, int n) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n) : "memory"); }
+
 enum Pass { kLse = 0, kSumFew = 1, kSumMany = 2 };
 
 template <int D, bool LO, int PASS>
@@ -68,6 +74,8 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, LO, PASS>::CPS)
   __shared__ __align__(8) uint64_t k_full[KS], k_empty[KS], q_full[QS], q_empty[QS], s_full[2], s_empty[2];
   __shared__ uint32_t tmem_slot;
   __shared__ __align__(16) float s_neg[2][kRows];  // pass 1: -L of a tile's queries
+  __shared__ uint32_t s_none[2][4];                // and which of them are <CL> or none
+  __shared__ float2 s_half[kRows];                 // results of the upper columns
   const uint32_t sm = (smem_addr(raw) + 1023u) & ~1023u;
   const int warp = uniform((int)(threadIdx.x >> 5)), lane = threadIdx.x & 31, tid = threadIdx.x;
   const uint32_t limit_ns = (uint32_t)a.wait_limit_ns;
@@ -87,7 +95,7 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, LO, PASS>::CPS)
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&s_full[i], 1);
-      mbar_init(&s_empty[i], 128);
+      mbar_init(&s_empty[i], kSThreads);
     }
     fence_mbar_init();
   }
@@ -106,7 +114,7 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, LO, PASS>::CPS)
   auto end_qt = [&]() { return PASS == kLse ? un.qt + 1 : nqt; };
   bool ok = true;
 
-  if (warp == 4) {
+  if (warp == kSWarps) {
     // ---------------- loads ----------------
     if (lane == 0) {
       const int row0 = (int)((int64_t)a.layer * a.H * a.C) + sq.row0 + h * sq.cap;
@@ -139,7 +147,7 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, LO, PASS>::CPS)
         if ((uint32_t)i < nq) (void)pf_wait(&q_full[i], ((nq - 1 - i) / QS) & 1, limit_ns);
     }
     __syncwarp();
-  } else if (warp == 5) {
+  } else if (warp == kSWarps + 1) {
     // ---------------- products ----------------
     constexpr uint32_t id = mma_idesc(Pack16<T>::kType, 0, kRows, kRows);
     constexpr uint32_t SBO = 8 * Cf::SW;
@@ -176,83 +184,101 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, LO, PASS>::CPS)
     }
   } else {
     // ---------------- S ----------------
-    const uint32_t my = tmem + ((uint32_t)(warp * 32) << 16);
-    const float c2 = a.c2;
+    const int half = warp >> 2;                      // columns [64 half, 64 half + 64)
+    const int r = (warp & 3) * 32 + lane;            // the thread's row of S (its TMEM lane)
+    const uint32_t my = tmem + ((uint32_t)((warp & 3) * 32) << 16) + half * 64;
+    const float2 cc = make_float2(a.c2, a.c2);
     uint32_t step = 0;
-    auto s_wait = [&]() -> bool {
+    float s[64];
+    // S of the next step into registers, its columns of TMEM free again
+    auto take = [&]() -> bool {
       const bool got = __all_sync(0xFFFFFFFFu, pf_wait(&s_full[step & 1], step / 2 & 1, limit_ns));
       tc_fence_after();
-      return got;
-    };
-    auto s_done = [&]() {
+      if (got) {
+        tmem_ld32(my + (step & 1) * kRows, s);
+        tmem_ld32(my + (step & 1) * kRows + 32, s + 32);
+        tmem_wait_ld();
+      }
       tc_fence_before();
       mbar_arrive(&s_empty[step & 1]);
       ++step;
+      return got;
+    };
+    // the columns whose bit is missing
+    auto hide = [&](uint32_t v0, uint32_t v1) {
+      if (__all_sync(0xFFFFFFFFu, (v0 & v1) == 0xFFFFFFFFu)) return;
+#pragma unroll
+      for (int x = 0; x < 32; ++x) {
+        if (!(v0 >> x & 1)) s[x] = -INFINITY;
+        if (!(v1 >> x & 1)) s[32 + x] = -INFINITY;
+      }
     };
     if constexpr (PASS == kLse) {
-      const int t = sq.q0 + un.qt * kRows + tid;  // the query's stored row
-      const int t0 = sq.q0 + un.qt * kRows, t1 = min(t0 + kRows, sq.len);
+      const int t0 = sq.q0 + un.qt * kRows, t1 = min(t0 + kRows, sq.len), t = t0 + r;  // the query's stored row
       const bool mine = t < sq.len;
+      const bool idle = t0 + (warp & 3) * 32 >= sq.len;  // none of the warp's queries exists
       const bool is_cl = mine && (a.meta[sq.moff + t] & 1);
       float m = -INFINITY, l = 0.f;
       for (int kt = un.kt0; kt < un.kt1; ++kt) {
-        const int i0 = kt * kRows;
-        const bool spans = a.least[sq.moff / kRows + kt] < t1 - 1;  // a row of the tile is hidden from some of the queries
-        const bool test = spans || i0 + kRows - 1 > t0;
-        if (!(ok = s_wait())) break;
-#pragma unroll 1
-        for (int c = 0; c < kRows; c += 32) {
-          float s[32];
-          tmem_ld32(my + (step & 1) * kRows + c, s);
-          tmem_wait_ld();
-          if (test) {
-            const int last = t - i0 - c;  // columns past it are later rows
-            if (spans) {
-              const int4* hid = reinterpret_cast<const int4*>(a.meta + sq.moff + i0 + c);
-#pragma unroll
-              for (int x = 0; x < 8; ++x) {
-                const int4 v = __ldg(hid + x);
-                if (t > v.x >> 1) s[4 * x] = -INFINITY;
-                if (t > v.y >> 1) s[4 * x + 1] = -INFINITY;
-                if (t > v.z >> 1) s[4 * x + 2] = -INFINITY;
-                if (t > v.w >> 1) s[4 * x + 3] = -INFINITY;
-              }
-            }
-#pragma unroll
-            for (int x = 0; x < 32; ++x)
-              if (x > last) s[x] = -INFINITY;
+        const int i0 = kt * kRows + half * 64;  // the row of the thread's first column
+        uint32_t v0 = 0xFFFFFFFFu, v1 = v0;
+        if (a.least[sq.moff / kRows + kt] < t1 - 1) {  // a row of the tile is hidden from some of the queries
+          const int h0 = __ldg(a.meta + sq.moff + i0 + lane) >> 1, h1 = __ldg(a.meta + sq.moff + i0 + 32 + lane) >> 1;
+          v0 = ~__ballot_sync(0xFFFFFFFFu, h0 < t0);
+          v1 = ~__ballot_sync(0xFFFFFFFFu, h1 < t0);
+          // rows that some of the queries see and others do not: spans that end among the queries
+          for (uint32_t p = __ballot_sync(0xFFFFFFFFu, h0 >= t0 && h0 < t1 - 1); p; p &= p - 1) {
+            const int x = __ffs(p) - 1;
+            if (t > __shfl_sync(0xFFFFFFFFu, h0, x)) v0 &= ~(1u << x);
           }
-          float mx = fmaxf(s[0], s[1]);
-#pragma unroll
-          for (int x = 2; x < 32; x += 2) mx = fmaxf(mx, fmaxf(s[x], s[x + 1]));
-          const float mn = fmaxf(m, mx * c2), mu = mn == -INFINITY ? 0.f : mn;
-          float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
-          const float2 cc = make_float2(c2, c2), mm = make_float2(-mu, -mu);
-#pragma unroll
-          for (int x = 0; x < 32; x += 4) {
-            const float2 z0 = __ffma2_rn(make_float2(s[x], s[x + 1]), cc, mm);
-            const float2 z1 = __ffma2_rn(make_float2(s[x + 2], s[x + 3]), cc, mm);
-            sum0 = __fadd2_rn(sum0, make_float2(ex2(z0.x), ex2(z0.y)));
-            sum1 = __fadd2_rn(sum1, make_float2(ex2(z1.x), ex2(z1.y)));
+          for (uint32_t p = __ballot_sync(0xFFFFFFFFu, h1 >= t0 && h1 < t1 - 1); p; p &= p - 1) {
+            const int x = __ffs(p) - 1;
+            if (t > __shfl_sync(0xFFFFFFFFu, h1, x)) v1 &= ~(1u << x);
           }
-          l = l * ex2(m - mu) + ((sum0.x + sum0.y) + (sum1.x + sum1.y));
-          m = mn;
         }
-        s_done();
+        if (i0 + 63 > t0) {  // later rows
+          v0 &= low_bits(t - i0 + 1);
+          v1 &= low_bits(t - i0 - 31);
+        }
+        if (!(ok = take())) break;
+        if (idle || !__any_sync(0xFFFFFFFFu, v0 | v1)) continue;
+        hide(v0, v1);
+        float mx[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+        for (int x = 4; x < 64; x += 4)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) mx[e] = fmaxf(mx[e], s[x + e]);
+        const float mn = fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.c2), mu = mn == -INFINITY ? 0.f : mn;
+        float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
+        const float2 mm = make_float2(-mu, -mu);
+#pragma unroll
+        for (int x = 0; x < 64; x += 4) {
+          const float2 z0 = __ffma2_rn(make_float2(s[x], s[x + 1]), cc, mm);
+          const float2 z1 = __ffma2_rn(make_float2(s[x + 2], s[x + 3]), cc, mm);
+          sum0 = __fadd2_rn(sum0, make_float2(ex2(z0.x), ex2(z0.y)));
+          sum1 = __fadd2_rn(sum1, make_float2(ex2(z1.x), ex2(z1.y)));
+        }
+        l = l * ex2(m - mu) + ((sum0.x + sum0.y) + (sum1.x + sum1.y));
+        m = mn;
       }
-      if (ok && mine)
-        a.lse[((int64_t)un.split * a.H + h) * a.n_tok + sq.tok0 + un.qt * kRows + tid] =
-            is_cl ? make_float2(INFINITY, 1.f) : make_float2(m, l);
+      if (half) s_half[r] = make_float2(m, l);
+      bar_sync(1, kSThreads);
+      if (!half && ok && mine) {
+        const float2 o = s_half[r];
+        const float M = fmaxf(m, o.x), Mu = M == -INFINITY ? 0.f : M;
+        a.lse[((int64_t)un.split * a.H + h) * a.n_tok + sq.tok0 + un.qt * kRows + r] =
+            is_cl ? make_float2(INFINITY, 1.f) : make_float2(M, l * ex2(m - Mu) + o.y * ex2(o.x - Mu));
+      }
     } else {
-      // -L of query tile qt's tid-th query; a <CL> query's is -infinity
+      // -L of query tile qt's r-th query; -infinity for a <CL> query and for none
       auto neg_lse = [&](int qt) -> float {
-        const int x = qt * kRows + tid;
+        const int x = qt * kRows + r;
         if (sq.q0 + x >= sq.len) return -INFINITY;
         const float2* p = a.lse + (int64_t)h * a.n_tok + sq.tok0 + x;
         const int64_t step_s = (int64_t)a.H * a.n_tok;
         float M = -INFINITY, L = 0.f;
-        for (int s = 0; s < a.n_split; ++s) {
-          const float2 v = __ldcg(p + s * step_s);
+        for (int k = 0; k < a.n_split; ++k) {
+          const float2 v = __ldcg(p + k * step_s);
           if (v.x == INFINITY) return -INFINITY;  // a <CL> query, in every split
           const float Mn = fmaxf(M, v.x), Mu = Mn == -INFINITY ? 0.f : Mn;
           L = L * ex2(M - Mu) + v.y * ex2(v.x - Mu);
@@ -261,68 +287,55 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, LO, PASS>::CPS)
         return -(M + log2f(L));
       };
       pdl_wait();  // the queries' sums
-      float next = neg_lse(first_qt(un.kt0));
+      float next = half ? 0.f : neg_lse(first_qt(un.kt0));
       for (int kt = un.kt0; kt < un.kt1; ++kt) {
-        const int i = kt * kRows + tid;
+        const int i = kt * kRows + r;
         const bool row = i < sq.len;
         const int meta = row ? a.meta[sq.moff + i] : 0, hid = meta >> 1;
         float total = 0.f;
         const int qe = end_qt();
         for (int qt = first_qt(kt); qt < qe; ++qt) {
-          const int t0 = sq.q0 + qt * kRows, t1 = min(t0 + kRows, sq.len);
-          const float mine = next;
-          s_neg[step & 1][tid] = mine;
-          // also whether a query of the tile is a <CL> or none
-          uint32_t odd = mine == -INFINITY;
-          asm volatile(
-              "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %0, 0;\n\tbarrier.cta.red.or.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-              : "+r"(odd)
-              :
-              : "memory");
-          {  // the next step's
-            const bool more = qt + 1 < qe;
-            if (more || kt + 1 < un.kt1) {
-              const int nx = more ? qt + 1 : first_qt(kt + 1);
-              if (PASS == kSumMany) next = neg_lse(nx);
-            }
+          const int t0 = sq.q0 + qt * kRows, t1 = min(t0 + kRows, sq.len), buf = step & 1;
+          if (!half) {
+            s_neg[buf][r] = next;
+            const uint32_t none = __ballot_sync(0xFFFFFFFFu, next == -INFINITY);
+            if (lane == 0) s_none[buf][warp] = none;
           }
-          const int lo = max(i - t0, 0), hi = row ? min(hid, t1 - 1) - t0 : -1;  // the columns that see row i
-          const bool whole = __all_sync(0xFFFFFFFFu, lo == 0 && hi == kRows - 1) && !odd;
-          const float4* neg = reinterpret_cast<const float4*>(s_neg[step & 1]);
+          bar_sync(1, kSThreads);
+          if (!half && PASS == kSumMany) {  // the next step's
+            if (qt + 1 < qe)
+              next = neg_lse(qt + 1);
+            else if (kt + 1 < un.kt1)
+              next = neg_lse(first_qt(kt + 1));
+          }
+          // the columns that see row i
+          const int lo = max(i - t0, 0) - half * 64, hi = (row ? min(hid, t1 - 1) - t0 : -1) - half * 64;
+          const uint32_t v0 = low_bits(hi + 1) & ~low_bits(lo) & ~s_none[buf][2 * half];
+          const uint32_t v1 = low_bits(hi - 31) & ~low_bits(lo - 32) & ~s_none[buf][2 * half + 1];
           // after a wait that ran out the warp only keeps up with the others' barriers
-          if (!ok || !(ok = s_wait())) {
+          if (!ok) {
             ++step;
             continue;
           }
+          if (!(ok = take())) continue;
+          if (!__any_sync(0xFFFFFFFFu, v0 | v1)) continue;
+          hide(v0, v1);
+          const float4* neg = reinterpret_cast<const float4*>(s_neg[buf] + half * 64);
           float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
-          const float2 cc = make_float2(c2, c2);
-#pragma unroll 1
-          for (int c = 0; c < kRows; c += 32) {
-            float s[32];
-            tmem_ld32(my + (step & 1) * kRows + c, s);
-            tmem_wait_ld();
 #pragma unroll
-            for (int x = 0; x < 32; x += 4) {
-              const float4 n = neg[(c + x) / 4];
-              float2 z0 = __ffma2_rn(make_float2(s[x], s[x + 1]), cc, make_float2(n.x, n.y));
-              float2 z1 = __ffma2_rn(make_float2(s[x + 2], s[x + 3]), cc, make_float2(n.z, n.w));
-              if (!whole) {
-                const unsigned span = (unsigned)(hi - lo);
-                const int at = c + x - lo;
-                const bool any = hi >= lo;
-                if (!any || (unsigned)at > span || n.x == -INFINITY) z0.x = -INFINITY;
-                if (!any || (unsigned)(at + 1) > span || n.y == -INFINITY) z0.y = -INFINITY;
-                if (!any || (unsigned)(at + 2) > span || n.z == -INFINITY) z1.x = -INFINITY;
-                if (!any || (unsigned)(at + 3) > span || n.w == -INFINITY) z1.y = -INFINITY;
-              }
-              sum0 = __fadd2_rn(sum0, make_float2(ex2(z0.x), ex2(z0.y)));
-              sum1 = __fadd2_rn(sum1, make_float2(ex2(z1.x), ex2(z1.y)));
-            }
+          for (int x = 0; x < 64; x += 4) {
+            const float4 n = neg[x / 4];
+            const float2 z0 = __ffma2_rn(make_float2(s[x], s[x + 1]), cc, make_float2(n.x, n.y));
+            const float2 z1 = __ffma2_rn(make_float2(s[x + 2], s[x + 3]), cc, make_float2(n.z, n.w));
+            sum0 = __fadd2_rn(sum0, make_float2(ex2(z0.x), ex2(z0.y)));
+            sum1 = __fadd2_rn(sum1, make_float2(ex2(z1.x), ex2(z1.y)));
           }
           total += (sum0.x + sum0.y) + (sum1.x + sum1.y);
-          s_done();
         }
-        if (ok && row) {
+        if (half) s_half[r].x = total;
+        bar_sync(1, kSThreads);
+        if (!half && ok && row) {
+          total += s_half[r].x;
           if ((meta & 1) && i >= sq.q0) total += 1.f;  // a <CL> query's weight is its own row's
           float* sc = a.scores + ((int64_t)a.layer * a.H * a.C + sq.row0 + (int64_t)h * sq.cap + i);
           *sc += total;

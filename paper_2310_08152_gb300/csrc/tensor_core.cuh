@@ -169,6 +169,12 @@ struct Pack16<BF16T> {
   }
 };
 
+// Bits [0, n) of a 32-bit word, n clamped to [0, 32].
+__device__ __forceinline__ uint32_t low_bits(int n) {
+  uint32_t r;
+  asm("bmsk.clamp.b32 %0, 0, %1;" : "=r"(r) : "r"(max(n, 0)));
+  return r;
+}
 // A value that is the warp's, so that the compiler knows it to be.
 __device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xFFFFFFFFu, x, 0); }
 
