@@ -483,6 +483,8 @@ class KVCache:
         self.scores = None
         self.prefix = None
         self._score_scratch = None
+        self._budget = np.zeros((2, self.b), np.int64)
+        self._budget_at = self._budget.ctypes.data
 
     # views of the device layout (rows of d_head elements)
     def k_plane(self, layer: int):
@@ -623,7 +625,11 @@ class KVCache:
             import torch
 
             _dev(kept, "kept", torch.int32, self.M * self.H * self.C)
-        kvc_evict(self.handle, _per_seq(keep, self.b, "keep"), _per_seq(recent, self.b, "recent"), kept, stream)
+        # two rows of one array that is kept for it (making and handing over an array each took 6 us a call)
+        for row, x, name in ((0, keep, "keep"), (1, recent, "recent")):
+            self._budget[row] = x if isinstance(x, int) else _per_seq(x, self.b, name)
+        _check(lib().kvc_evict(self.handle, self._budget_at, self._budget_at + 8 * self.b, _ptr(kept),
+                               _stream_handle(stream)))
 
     # sequences that share a prefix
     def set_prefix(self, prefix: Optional["KVCache"], parent=None):

@@ -21,6 +21,7 @@
 #include <algorithm>
 #include <atomic>
 #include <cstdint>
+#include <type_traits>
 
 #include "device_common.cuh"
 #include "kernels.hpp"
@@ -29,7 +30,7 @@ namespace kvc {
 namespace {
 
 constexpr unsigned kFull = 0xFFFFFFFFu;
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
 constexpr int kWarps = kThreads / 32;
 constexpr int kScan = 4 * kThreads;  // candidates of one scan step
 constexpr int kBins = 2048;
@@ -87,11 +88,21 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, EvictShared& sh, uint
   return before + incl - v;
 }
 
-template <int D>
-__global__ void __launch_bounds__(kThreads) evict_kernel(Geometry g, Static st, Buffers buf, float* __restrict__ scores,
-                                                         const AffSeq* __restrict__ aff, int32_t* __restrict__ kept,
-                                                         int held, int chunk, int CN) {
+// IMG: the call's upload is a parameter (of img_bytes, its AffSeqs from aff_off on), which the first CTA stores at dyn.
+struct NoImage {};
+template <int D, bool IMG>
+__global__ void __launch_bounds__(kThreads, 7)
+    evict_kernel(Geometry g, Static st, Buffers buf, float* __restrict__ scores, const AffSeq* __restrict__ aff_,
+                 int32_t* __restrict__ kept, int held, int chunk, int CN,
+                 const __grid_constant__ std::conditional_t<IMG, AppendImage, NoImage> img, int img_bytes, int aff_off,
+                 uint4* __restrict__ dyn_out) {
   constexpr int VPR = D / 8;  // 16-byte vectors per row
+  const AffSeq* aff = aff_;
+  if constexpr (IMG) {
+    aff = reinterpret_cast<const AffSeq*>(reinterpret_cast<const unsigned char*>(&img) + aff_off);
+    if (blockIdx.x == 0)
+      for (int i = threadIdx.x; i < (img_bytes + 15) / 16; i += kThreads) dyn_out[i] = img.v[i];
+  }
   extern __shared__ __align__(128) unsigned char dyn[];
   // `chunk` recent rows of K and then of V (of one of them in a cluster), then the keys
   uint32_t* keys = reinterpret_cast<uint32_t*>(dyn + (size_t)chunk * (CN > 1 ? 1 : 2) * D * 2);
@@ -236,7 +247,7 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(Geometry g, Static st, 
       if (tid == 0) atomicOr(buf.status, STATUS_CHECK);
       break;
     }
-    constexpr int U = 4;
+    constexpr int U = 2;
     const int step = CN * kThreads, total = n_hole * VPR;
     for (int v0 = rank * kThreads + tid; v0 < total; v0 += U * step) {
       uint4 k[U], v[U];
@@ -333,9 +344,10 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(Geometry g, Static st, 
   }
 }
 
-template <int D>
+template <int D, bool IMG>
 cudaError_t launch_evict_t(const Geometry& g, const Static& st, const Buffers& buf, float* scores, const AffSeq* aff,
-                           int n_aff, int64_t max_cand, int64_t max_recent, int32_t* kept, int num_sms, cudaStream_t stream) {
+                           int n_aff, int64_t max_cand, int64_t max_recent, int32_t* kept, int num_sms,
+                           const EvictImage* image, cudaStream_t stream) {
   static std::atomic<bool> done[64];
   constexpr int kMost = 200 * 1024;  // of dynamic shared memory
   int dev = 0;
@@ -343,7 +355,7 @@ cudaError_t launch_evict_t(const Geometry& g, const Static& st, const Buffers& b
   if (e != cudaSuccess) return e;
   if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
   if (!done[dev].load(std::memory_order_acquire)) {
-    e = cudaFuncSetAttribute(evict_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+    e = cudaFuncSetAttribute(evict_kernel<D, IMG>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
     if (e != cudaSuccess) return e;
     done[dev].store(true, std::memory_order_release);
   }
@@ -353,8 +365,8 @@ cudaError_t launch_evict_t(const Geometry& g, const Static& st, const Buffers& b
   int cn = 1;
   if (max_cand <= kMaxHeldKeys)
     while (2 * cn <= kMaxCluster && 2 * cn * units <= 2 * num_sms) cn *= 2;
-  // recent rows of a chunk: 32 KB of K and V
-  const int chunk = (int)std::min<int64_t>(max_recent, (cn > 1 ? 32 : 16) * 1024 / (D * 2));
+  // recent rows of a chunk: 16 KB of K and V, which leaves room for seven CTAs per SM
+  const int chunk = (int)std::min<int64_t>(max_recent, (cn > 1 ? 16 : 8) * 1024 / (D * 2));
   const size_t smem = (size_t)chunk * (cn > 1 ? 1 : 2) * D * 2 + 4 * (size_t)held;
   static_assert(32 * 1024 + 4 * kMaxHeldKeys <= kMost, "shared memory");
   cudaLaunchConfig_t cfg = {};
@@ -369,23 +381,35 @@ cudaError_t launch_evict_t(const Geometry& g, const Static& st, const Buffers& b
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = cn > 1 ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, evict_kernel<D>, g, st, buf, scores, aff, kept, held, chunk, cn);
+  if constexpr (IMG)
+    return cudaLaunchKernelEx(&cfg, evict_kernel<D, IMG>, g, st, buf, scores, aff, kept, held, chunk, cn, *image->img,
+                              image->bytes, image->aff_off, static_cast<uint4*>(image->dyn));
+  else
+    return cudaLaunchKernelEx(&cfg, evict_kernel<D, IMG>, g, st, buf, scores, aff, kept, held, chunk, cn, NoImage{}, 0, 0,
+                              static_cast<uint4*>(nullptr));
 }
 
 }  // namespace
 
 cudaError_t launch_evict(const Geometry& g, const Static& st, const Buffers& buf, float* scores, const AffSeq* aff,
-                         int n_aff, int64_t max_cand, int64_t max_recent, int32_t* kept, int num_sms, cudaStream_t stream) {
+                         int n_aff, int64_t max_cand, int64_t max_recent, int32_t* kept, int num_sms,
+                         const EvictImage* image, cudaStream_t stream) {
   if (n_aff <= 0) return cudaSuccess;
+  auto go = [&](auto d) {
+    constexpr int D = decltype(d)::value;
+    return image != nullptr
+               ? launch_evict_t<D, true>(g, st, buf, scores, aff, n_aff, max_cand, max_recent, kept, num_sms, image, stream)
+               : launch_evict_t<D, false>(g, st, buf, scores, aff, n_aff, max_cand, max_recent, kept, num_sms, image, stream);
+  };
   switch (g.D) {
     case 64:
-      return launch_evict_t<64>(g, st, buf, scores, aff, n_aff, max_cand, max_recent, kept, num_sms, stream);
+      return go(std::integral_constant<int, 64>{});
     case 80:
-      return launch_evict_t<80>(g, st, buf, scores, aff, n_aff, max_cand, max_recent, kept, num_sms, stream);
+      return go(std::integral_constant<int, 80>{});
     case 96:
-      return launch_evict_t<96>(g, st, buf, scores, aff, n_aff, max_cand, max_recent, kept, num_sms, stream);
+      return go(std::integral_constant<int, 96>{});
     case 128:
-      return launch_evict_t<128>(g, st, buf, scores, aff, n_aff, max_cand, max_recent, kept, num_sms, stream);
+      return go(std::integral_constant<int, 128>{});
     default:
       return cudaErrorInvalidValue;
   }

@@ -166,7 +166,10 @@ struct OwnArgs {
   int b;
   float* out;               // [b][H][D] per layer
   int64_t out_stride;
-  int after_prefix;         // the kernel before this one is the prefix kernel
+  // The kernel before this one is the prefix kernel, of less than a wave: this one may start beside it and waits before it
+  // reads the parts.  Beside a larger one its waiting CTAs take room from it (8 samples of 8 prefixes of 800 rows, 32
+  // layers: 646 us, one after the other 588).
+  int early;
 };
 // Queries of one CTA where the largest group has `group` members; CTAs per SM of that kernel.
 int prefix_rows(int group);
@@ -182,8 +185,16 @@ cudaError_t launch_compact_scores(const Geometry& g, const Static& st, float* sc
 // Eviction (evict.cu): in every (layer, head) stream of the n_aff sequences, len_new of len_old rows stay, the last
 // `first_row` of them (the recent ones) and those with the largest scores.  max_cand, max_recent: the most candidates and
 // recent rows of a stream; kept: [M][H * C] or NULL, the earlier row number of each kept row.
+// image: the call's upload (state and AffSeqs) as a kernel parameter, where it fits one, stored at dyn by the kernel
+// (an eviction of two sequences in two layers: an upload and its event less, 23 us of host time before); else NULL.
+struct EvictImage {
+  const AppendImage* img;
+  int bytes, aff_off;
+  void* dyn;
+};
 cudaError_t launch_evict(const Geometry& g, const Static& st, const Buffers& buf, float* scores, const AffSeq* aff,
-                         int n_aff, int64_t max_cand, int64_t max_recent, int32_t* kept, int num_sms, cudaStream_t stream);
+                         int n_aff, int64_t max_cand, int64_t max_recent, int32_t* kept, int num_sms,
+                         const EvictImage* image, cudaStream_t stream);
 
 // ---------------------------------------------------------------------------------------------
 // Masked prefill attention (prefill.cu)

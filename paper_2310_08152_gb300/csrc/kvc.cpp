@@ -1493,7 +1493,7 @@ kvc_status kvc_decode_attention_shared(kvc_cache* c, int first, int n_layers, co
   oa.b = c->cfg.b;
   oa.out = out;
   oa.out_stride = out_layer_stride;
-  oa.after_prefix = c->px_units > 0;
+  oa.early = c->px_units > 0 && (int64_t)c->px_units * c->cfg.H * n_layers <= c->num_sms;
   e = kvc::launch_own(c->geom(), oa, c->max_segment, c->num_sms, stream);
   if (e != cudaSuccess) return cuda_fail(e, "own rows' kernel");
   c->launches += 1;
@@ -1519,7 +1519,9 @@ kvc_status kvc_evict(kvc_cache* c, const int64_t* keep, const int64_t* recent, i
   if (st != KVC_OK) return st;
   const size_t bytes = c->ws.dyn_payload + sizeof(kvc::AffSeq) * plan.size();
   cudaError_t e;
-  unsigned char* img = c->ring.reserve(bytes, &e);
+  kvc::AppendImage small;
+  const bool fits = bytes <= sizeof(small);
+  unsigned char* img = fits ? reinterpret_cast<unsigned char*>(&small) : c->ring.reserve(bytes, &e);
   if (!img) return cuda_fail(e, "staging");
   c->bk.book.apply_evict(plan);
   c->fill_state(img);
@@ -1534,11 +1536,14 @@ kvc_status kvc_evict(kvc_cache* c, const int64_t* keep, const int64_t* recent, i
     max_cand = std::max(max_cand, plan[i].len_old - plan[i].recent);
     max_recent = std::max(max_recent, plan[i].recent);
   }
-  e = c->ring.commit(c->wsp(c->ws.dyn), bytes, stream);
-  if (e != cudaSuccess) return cuda_fail(e, "upload eviction plan");
+  if (!fits) {
+    e = c->ring.commit(c->wsp(c->ws.dyn), bytes, stream);
+    if (e != cudaSuccess) return cuda_fail(e, "upload eviction plan");
+  }
+  const kvc::EvictImage image{&small, (int)bytes, (int)c->ws.dyn_payload, c->wsp(c->ws.dyn)};
   e = kvc::launch_evict(c->geom(), c->stat(), c->bufs(), c->scores,
                         reinterpret_cast<const kvc::AffSeq*>(c->wsp(c->ws.dyn + c->ws.dyn_payload)), (int)plan.size(),
-                        max_cand, max_recent, kept, c->num_sms, stream);
+                        max_cand, max_recent, kept, c->num_sms, fits ? &image : nullptr, stream);
   if (e != cudaSuccess) return cuda_fail(e, "eviction kernel");
   c->launches += 1;
   c->last_was_decode = false;

@@ -9,7 +9,7 @@
 //
 // The queries are the M rows of 16 x 8 x 16 matrix instructions: with the paper's 8 samples of a prompt the work is that
 // of one 16-row tile, an eighth of the smallest tile of the tcgen05 instructions, and P stays in registers between the
-// two products.  Four warps share a CTA's keys (and, past 32 queries, its queries); each keeps its own online softmax and
+// two products.  The warps share a CTA's keys (and, past 32 queries, its queries); each keeps its own online softmax and
 // the results are merged in shared memory at the end.  Tiles of 64 rows come through a ring of two or three stages with 16-byte
 // asynchronous copies into rows padded by 16 bytes, which keeps the matrix loads free of bank conflicts at every d_head.
 //
@@ -29,21 +29,24 @@ namespace kvc {
 namespace {
 
 constexpr unsigned kFull = 0xFFFFFFFFu;
-constexpr int kThreads = 128;
 constexpr int kKeys = 64;   // rows per tile
 
-// R = 16 MT queries per CTA: WM 16-row tiles per warp, RW warps over the queries, KW over the keys.
+// R = 16 MT queries per CTA of NW warps: WM 16-row tiles per warp, RW warps over the queries, KW over the keys.  At 64
+// queries eight warps of one tile each, since four of two hold 255 registers and leave the tensor cores waiting (two
+// layers of 32 heads of 128, 64 samples of 32,768 rows, bf16: 312 us).
 template <int D, int MT, bool ROT>
 struct PxCfg {
   static constexpr int R = 16 * MT;
-  static constexpr int WM = MT == 1 ? 1 : 2;
+  static constexpr int NW = MT == 4 ? 8 : 4;
+  static constexpr int THREADS = NW * 32;
+  static constexpr int WM = MT == 2 ? 2 : 1;
   static constexpr int RW = MT / WM;
-  static constexpr int KW = 4 / RW;
+  static constexpr int KW = NW / RW;
   static constexpr int KG = kKeys / KW / 16;  // 16-key groups per warp and tile
   static constexpr int RS = D * 2 + 16;       // bytes of a row in shared memory
   static constexpr int TILE = kKeys * RS;
   // three stages of K and V tiles, or two where a third would leave one CTA per SM
-  static constexpr int S = D == 128 && MT == 4 ? 2 : 3;
+  static constexpr int S = (D == 128 && MT == 4) || MT == 1 ? 2 : 3;
   static constexpr int OFF_Q = 2 * S * TILE;
   static constexpr int OFF_QLO = OFF_Q + R * RS;
   static constexpr int SMEM = OFF_QLO + (ROT ? R * RS : 0);
@@ -101,8 +104,10 @@ struct Mma<BF16T> {
 };
 
 template <typename T, int D, int MT, bool ROT>
-__global__ void __launch_bounds__(kThreads, MT == 4 || (D > 96 && MT > 1) ? 2 : 3) prefix_kernel(PrefixArgs p) {
+__global__ void __launch_bounds__(PxCfg<D, MT, ROT>::THREADS, MT == 4 || (D > 96 && MT > 1) ? 2 : MT == 1 && D < 96 ? 4 : 3)
+    prefix_kernel(PrefixArgs p) {
   using C = PxCfg<D, MT, ROT>;
+  constexpr int kThreads = C::THREADS;
   constexpr int WM = C::WM, KG = C::KG, CH = D / 8;
   extern __shared__ __align__(128) unsigned char smem[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -121,8 +126,8 @@ __global__ void __launch_bounds__(kThreads, MT == 4 || (D > 96 && MT > 1) ? 2 : 
     if (t < n_tiles) {
       const uint32_t dst = s0 + (t % C::S) * 2 * C::TILE;
 #pragma unroll
-      for (int i = 0; i < kKeys * CH / kThreads; ++i) {
-        const int x = tid + i * kThreads, r = x / CH, c = x % CH;
+      for (int x = tid; x < kKeys * CH; x += kThreads) {
+        const int r = x / CH, c = x % CH;
         const int key = t * kKeys + r;
         const bool in = key < n_keys;
         const int64_t e = in ? (int64_t)key * D + c * 8 : 0;
@@ -132,7 +137,6 @@ __global__ void __launch_bounds__(kThreads, MT == 4 || (D > 96 && MT > 1) ? 2 : 
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  static_assert(kKeys * CH % kThreads == 0, "a tile splits evenly");
   for (int t = 0; t < C::S - 1; ++t) load(t);
 
   // the queries, rotated where the cache's keys are
@@ -353,7 +357,7 @@ cudaError_t prefix_occ(int dev, int* occ) {
   int o = found[dev].load(std::memory_order_acquire);
   if (o == 0) {
     cudaError_t e = cudaFuncSetAttribute(prefix_kernel<T, D, MT, ROT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
-    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&o, prefix_kernel<T, D, MT, ROT>, kThreads, C::SMEM);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&o, prefix_kernel<T, D, MT, ROT>, C::THREADS, C::SMEM);
     if (e != cudaSuccess) return e;
     if (o < 1) o = 1;
     found[dev].store(o, std::memory_order_release);
@@ -389,7 +393,7 @@ __global__ void __launch_bounds__(kOwnWarps * 32, 2) own_kernel(OwnArgs a) {
   __shared__ float s_ml[kOwnWarps][2];
   const PrefixArgs& p = a.px;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (!a.after_prefix) pdl_wait();  // else whatever the prefix kernel waited for is complete, and it writes only the parts
+  if (!a.early) pdl_wait();  // else whatever the prefix kernel waited for is complete, and it writes only the parts
   pdl_launch_dependents();
   const int H = p.H;
   const int64_t seg = ((int64_t)blockIdx.x * kOwnWarps + warp) / WPS, per_layer = (int64_t)a.b * H;
@@ -538,7 +542,7 @@ __global__ void __launch_bounds__(kOwnWarps * 32, 2) own_kernel(OwnArgs a) {
       M = Mx;
     }
   }
-  if (a.after_prefix) pdl_wait();  // the parts; every thread of the grid waits, so that it never ends before the prefix's
+  if (a.early) pdl_wait();  // the parts; every thread of the grid waits, so that it never ends before the prefix's
   if (len == 0 || sub != 0) return;
   const float* part = p.parts + (((int64_t)layer * p.n_parts + p.split0[s]) * H + h) * PO;
   const int64_t step = (int64_t)H * PO;
@@ -569,7 +573,7 @@ cudaError_t launch_own_t(const OwnArgs& a, int64_t segs, cudaStream_t stream) {
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = a.early ? 1 : 0;
   return cudaLaunchKernelEx(&cfg, own_kernel<T, D, WPS>, a);
 }
 
@@ -617,7 +621,7 @@ cudaError_t launch_prefix(const Geometry& g, const PrefixArgs& a, int device, in
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((int64_t)a.n_units * g.H * a.n_layers));
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3(PxCfg<D, MT, ROT>::THREADS);
     cfg.dynamicSmemBytes = PxCfg<D, MT, ROT>::SMEM;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
