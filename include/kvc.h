@@ -298,8 +298,8 @@ kvc_status kvc_decode_attention_scored(kvc_cache* cache, int first, int n_layers
  *   score_j += softmax_j(scale * <q, k_j>)  over the stored rows j that the token sees,
  * q, n_q, scale, the mask and the rows that have to be stored as for kvc_prefill_attention (all of a prompt's
  * tokens, block by block, for the weights that its rows got in it; its last few for an observation window).
- *   scratch: device, 256-byte aligned, the bytes that kvc_score_scratch_bytes gives for these n_q at this
- *     time, the call's until it is complete on `stream`.
+ *   scratch: device, 256-byte aligned, the bytes that kvc_score_scratch_bytes gives for these n_q, the
+ *     call's until it is complete on `stream`.
  * Every sum is made in one order.  Errors as kvc_prefill_attention's, and KVC_ERR_STATE without scores. */
 kvc_status kvc_score_scratch_bytes(kvc_cache* cache, const int32_t* n_q, size_t* bytes);
 kvc_status kvc_score_prompt(kvc_cache* cache, int layer, const void* q, const int32_t* n_q, float scale, void* scratch,
@@ -330,12 +330,12 @@ kvc_status kvc_evict(kvc_cache* cache, const int64_t* keep, const int64_t* recen
  * rows are then stored, and read by a step, once for all of them.  The caches agree in M, H, d_head, dtype
  * and rotation and share a stream; capacities and batch differ as they like.
  *   parent: host [b], copied.
- *   scratch: device, 256-byte aligned, kvc_prefix_scratch_bytes(cache) bytes, the cache's until another
+ *   scratch: device, 256-byte aligned, kvc_prefix_scratch_bytes(cache, prefix) bytes, the cache's until another
  *     prefix is set or the cache is destroyed.
  * The prefix may grow, be compacted or evicted between calls, and outlives its use here; NULL for `prefix`
  * ends it (parent and scratch are then ignored).  Positions are the caller's: append the own tokens at the
  * positions that continue the prefix's. */
-size_t kvc_prefix_scratch_bytes(const kvc_cache* cache);
+size_t kvc_prefix_scratch_bytes(const kvc_cache* cache, const kvc_cache* prefix);
 kvc_status kvc_set_prefix(kvc_cache* cache, kvc_cache* prefix, const int32_t* parent, void* scratch,
                           size_t scratch_bytes);
 

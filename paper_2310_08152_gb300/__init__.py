@@ -359,8 +359,8 @@ def kvc_score_prompt(cache: int, layer: int, q, n_q, scale: float, scratch, stre
                                   scratch.numel() * scratch.element_size(), _stream_handle(stream)))
 
 
-def kvc_prefix_scratch_bytes(cache: int) -> int:
-    return lib().kvc_prefix_scratch_bytes(cache)
+def kvc_prefix_scratch_bytes(cache: int, prefix: int) -> int:
+    return lib().kvc_prefix_scratch_bytes(cache, prefix)
 
 
 def kvc_set_prefix(cache: int, prefix, parent, scratch):
@@ -482,7 +482,7 @@ class KVCache:
         self.book = Book(self.b, cap, policy, _handle=lib().kvc_get_book(self.handle))
         self.scores = None
         self.prefix = None
-        self._score_scratch = None
+        self._score_scratch = self._score_counts = None
         self._budget = np.zeros((2, self.b), np.int64)
         self._budget_at = self._budget.ctypes.data
 
@@ -610,11 +610,14 @@ class KVCache:
         if n_q.shape != (self.b,):
             raise ValueError(f"n_q must have {self.b} elements, got shape {n_q.shape}")
         _dev(q, "q", self.torch_dtype, int(np.add.reduce(n_q)) * self.H * self.d)
-        need = kvc_score_scratch_bytes(self.handle, n_q)
-        if self._score_scratch is None or self._score_scratch.numel() < need:
-            if self._score_scratch is not None and stream is not None:
-                torch.cuda.synchronize(self.k.device)  # the old one may be in use on that stream
-            self._score_scratch = torch.empty(max(need, 256), dtype=torch.uint8, device=self.k.device)
+        counts = n_q.tobytes()
+        if counts != self._score_counts:
+            need = kvc_score_scratch_bytes(self.handle, n_q)
+            if self._score_scratch is None or self._score_scratch.numel() < need:
+                if self._score_scratch is not None and stream is not None:
+                    torch.cuda.synchronize(self.k.device)  # the old one may be in use on that stream
+                self._score_scratch = torch.empty(max(need, 256), dtype=torch.uint8, device=self.k.device)
+            self._score_counts = counts
         kvc_score_prompt(self.handle, layer, q, n_q, scale, self._score_scratch, stream)
 
     def evict(self, keep, recent, kept=None, stream=None):
@@ -644,7 +647,7 @@ class KVCache:
         parent = np.asarray(parent, np.int32)
         if parent.shape != (self.b,):
             raise ValueError(f"parent must have {self.b} elements, got shape {parent.shape}")
-        scratch = torch.empty(kvc_prefix_scratch_bytes(self.handle), dtype=torch.uint8, device=self.k.device)
+        scratch = torch.empty(kvc_prefix_scratch_bytes(self.handle, prefix.handle), dtype=torch.uint8, device=self.k.device)
         kvc_set_prefix(self.handle, prefix.handle, parent, scratch)
         self.prefix, self._prefix_scratch = prefix, scratch
 

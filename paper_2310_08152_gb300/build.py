@@ -12,7 +12,7 @@ OUT = os.path.join(HERE, "_build")
 SO = os.path.join(OUT, "libkvc.so")
 INCLUDE = os.path.join(ROOT, "include")
 GENCODE = "arch=compute_103a,code=sm_103a"
-SOURCES = ["kvc.cpp", "book.cpp", "kernels.cu", "prefill.cu", "evict.cu", "prefix.cu", "score.cu"]
+SOURCES = ["kvc.cpp", "book.cpp", "kernels.cu", "prefill.cu", "evict.cu", "prefix.cu", "prefix_tc.cu", "score.cu"]
 HEADERS = [os.path.join(CSRC, h) for h in ("book.hpp", "kernels.hpp", "device_common.cuh", "tensor_core.cuh")] + [os.path.join(INCLUDE, "kvc.h")]
 
 

@@ -19,6 +19,10 @@ struct F16T {
   }
   static __device__ __forceinline__ float f1(uint16_t u) { return __half2float(__ushort_as_half(u)); }
   static __device__ __forceinline__ uint16_t r(float x) { return __half_as_ushort(__float2half_rn(x)); }
+  static __device__ __forceinline__ uint32_t r2(float x, float y) {
+    const __half2 h = __floats2half2_rn(x, y);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
 };
 struct BF16T {
   static __device__ __forceinline__ float2 f2(uint32_t u) {
@@ -26,6 +30,10 @@ struct BF16T {
   }
   static __device__ __forceinline__ float f1(uint16_t u) { return __bfloat162float(__ushort_as_bfloat16(u)); }
   static __device__ __forceinline__ uint16_t r(float x) { return __bfloat16_as_ushort(__float2bfloat16_rn(x)); }
+  static __device__ __forceinline__ uint32_t r2(float x, float y) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
 };
 
 // ---------------------------------------------------------------------------------------------
@@ -51,6 +59,58 @@ __device__ __forceinline__ void rope_sincos(int32_t pos, float2 g, float* s, flo
 // of 800 rows).
 __device__ __forceinline__ void rope_sincos_full(int32_t pos, float2 g, float* s, float* c) {
   sincospif(2.f * rope_turns(pos, g), s, c);
+}
+
+// Two 32-bit values as a sum of packed 16-bit parts: the first rounds them, each later one rounds what is left, which
+// binary32 holds exactly.  Two parts of f16 hold 22 bits of a value, three of bf16 all 24.
+template <typename T>
+constexpr int kFullParts = 2;
+template <>
+constexpr int kFullParts<BF16T> = 3;
+template <typename T, int N>
+__device__ __forceinline__ void split_parts(float x, float y, uint32_t* part) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    part[i] = T::r2(x, y);
+    if (i + 1 < N) {
+      const float2 back = T::f2(part[i]);
+      x -= back.x;
+      y -= back.y;
+    }
+  }
+}
+
+// Chunk c (eight columns) of a query as packed 16-bit parts, rotated at pos where NQ > 1 (the first `rot` columns; rot is a
+// multiple of 16).  q is 16-byte aligned.
+template <typename T, int NQ>
+__device__ __forceinline__ void query_chunk(const uint16_t* q, int c, int rot, int32_t pos, const float2* rope_g,
+                                            uint32_t (&part)[NQ][4]) {
+  const uint4 x = *reinterpret_cast<const uint4*>(q + c * 8);
+  const uint32_t a[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) part[0][e] = a[e];
+#pragma unroll
+  for (int i = 1; i < NQ; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) part[i][e] = 0;
+  if (NQ == 1 || c * 8 >= rot) return;
+  const int half = rot / 2;
+  const bool first = c * 8 < half;
+  const int i0 = first ? c * 8 : c * 8 - half;
+  const uint4 y = *reinterpret_cast<const uint4*>(q + (first ? c * 8 + half : i0));
+  const uint32_t b[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float2 u = T::f2(a[e]), v = T::f2(b[e]);
+    float sn0, cs0, sn1, cs1;
+    rope_sincos_full(pos, rope_g[i0 + 2 * e], &sn0, &cs0);
+    rope_sincos_full(pos, rope_g[i0 + 2 * e + 1], &sn1, &cs1);
+    uint32_t out[NQ];
+    split_parts<T, NQ>(first ? u.x * cs0 - v.x * sn0 : u.x * cs0 + v.x * sn0,
+                       first ? u.y * cs1 - v.y * sn1 : u.y * cs1 + v.y * sn1, out);
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) part[i][e] = out[i];
+  }
 }
 
 // ---------------------------------------------------------------------------------------------

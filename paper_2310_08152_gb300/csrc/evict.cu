@@ -36,6 +36,7 @@ constexpr int kScan = 4 * kThreads;  // candidates of one scan step
 constexpr int kBins = 2048;
 constexpr int kMaxHeldKeys = 40 * 1024;  // candidates whose keys stay in shared memory (160 KB); else they are read again
 constexpr int kMaxCluster = 8;
+constexpr int kFewDrops = 4;  // rows that go, at most, for which the least score is looked for row by row
 
 // A score's order as an unsigned number: a NaN below everything, -0 and +0 equal.
 __device__ __forceinline__ uint32_t order_key(float x) {
@@ -61,6 +62,8 @@ struct EvictShared {
     } l;
   };
   uint64_t full;
+  uint64_t least[2][kWarps];
+  int32_t dropped[kFewDrops];
   uint32_t wsum[kWarps];
   uint32_t bin, above, in_bin;
 };
@@ -136,117 +139,8 @@ __global__ void __launch_bounds__(kThreads, 7)
   }
   auto key = [&](int i) { return in_smem ? keys[i] : order_key(sc[i]); };
 
-  // ------------------------------ the A-th largest score ---------------------------------------
-  uint32_t T = 0;              // stays: key > T, and the first `need` (in row order) with key == T
-  int need = 0x7FFFFFFF;
-  bool ties = false;           // fewer of the equal ones stay than there are
-  if (A > 0) {
-    if (in_smem)
-      for (int i = tid; i < cand; i += kThreads) keys[i] = order_key(sc[i]);
-    uint32_t prefix = 0, want = (uint32_t)A;
-    int shift = 21;
-    for (int pass = 0; pass < 3; ++pass) {
-      const int width = pass == 2 ? 10 : 11;
-      const int hi = shift + width;  // the digits above are `prefix`
-#pragma unroll
-      for (int b = 0; b < kBins / kThreads; ++b) sh.hist[b * kThreads + tid] = 0;
-      __syncthreads();
-      const uint32_t mask = (1u << width) - 1u;
-      for (int i = tid; i < cand; i += kThreads) {
-        const uint32_t k = key(i);
-        if (pass == 0 || k >> hi == prefix) atomicAdd(&sh.hist[(k >> shift) & mask], 1u);
-      }
-      __syncthreads();
-      // thread t holds the eight bins from the (t + 1)-th eight from the top down
-      const int per = kBins / kThreads, top = kBins - 1 - tid * per;
-      uint32_t c[kBins / kThreads], mine = 0;
-#pragma unroll
-      for (int b = 0; b < per; ++b) {
-        c[b] = sh.hist[top - b];
-        mine += c[b];
-      }
-      uint32_t all;
-      uint32_t above = block_scan(mine, sh, &all);
-      if (above < want && want <= above + mine) {
-#pragma unroll
-        for (int b = 0; b < per; ++b) {
-          if (above < want && want <= above + c[b]) {
-            sh.bin = (uint32_t)(top - b);
-            sh.above = above;
-            sh.in_bin = c[b];
-          }
-          above += c[b];
-        }
-      }
-      __syncthreads();
-      prefix = prefix << width | sh.bin;
-      want -= sh.above;
-      T = prefix << shift;
-      if (want == sh.in_bin) break;  // the whole bin stays: every key from its lowest on
-      if (pass == 2) {
-        need = (int)want;
-        ties = true;
-      }
-      shift -= pass == 1 ? 10 : 11;
-      __syncthreads();
-    }
-    // no key of the bin's range lies at or below T but T itself, so "key >= T" is "key > T or the equal ones"
-  }
-
-  // ------------------------------ holes, and the rows that fill them ---------------------------
-  const uint32_t uneed = (uint32_t)need;
-  uint32_t eq_hole = 0, eq_src = 0;  // equal ones before each scan's next candidate
-  if (ties) {                        // those below row A
-    uint32_t c = 0;
-    for (int i = tid; i < A; i += kThreads) c += key(i) == T;
-    block_scan(c, sh, &eq_src);
-  }
-  __syncthreads();
-  if (CN > 1) cluster_sync();  // every CTA of the cluster has read the scores
-  // One step of a scan: the candidates [base, min(base + kScan, end)) that stay (or go) are appended to list at *count.
-  auto scan = [&](int base, int end, uint32_t& eq_before, bool stay, int32_t* list, int count) {
-    uint32_t gt = 0, eq = 0;
-    const int i0 = base + 4 * tid;
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      if (i0 + u < end) {
-        const uint32_t k = key(i0 + u);
-        gt |= (uint32_t)(k > T) << u;
-        eq |= (uint32_t)(k == T) << u;
-      }
-    }
-    uint32_t sum;
-    const uint32_t pre = block_scan(__popc(gt) | __popc(eq) << 16, sh, &sum);
-    uint32_t e = eq_before + (pre >> 16);
-    uint32_t stayed = (pre & 0xFFFFu) + (min(e, uneed) - min(eq_before, uneed));
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int i = i0 + u;
-      if (i < end) {
-        const bool s = (gt >> u & 1u) || ((eq >> u & 1u) && e < uneed);
-        e += eq >> u & 1u;
-        if (stay && s) list[count + stayed] = i;
-        if (!stay && !s) list[count + (uint32_t)(i - base) - stayed] = i;
-        if (!stay && s && kp != nullptr && rank == 0) kp[i] = i;
-        stayed += s;
-      }
-    }
-    const int total = (int)((sum & 0xFFFFu) + (min(eq_before + (sum >> 16), uneed) - min(eq_before, uneed)));
-    eq_before += sum >> 16;
-    __syncthreads();
-    return stay ? total : min(end - base, kScan) - total;
-  };
-  int at_src = A, n_src = 0;
-  for (int at_hole = 0; at_hole < A; at_hole += kScan) {
-    const int n_hole = scan(at_hole, A, eq_hole, false, sh.l.holes, 0);
-    while (n_src < n_hole && at_src < cand) {
-      n_src += scan(at_src, cand, eq_src, true, sh.l.srcs, n_src);
-      at_src += kScan;
-    }
-    if (n_hole > n_src) {  // cannot be: as many stay beyond row A as go below it
-      if (tid == 0) atomicOr(buf.status, STATUS_CHECK);
-      break;
-    }
+  // Moves the rows of the first n_hole entries of the lists.
+  auto move = [&](int n_hole) {
     constexpr int U = 2;
     const int step = CN * kThreads, total = n_hole * VPR;
     for (int v0 = rank * kThreads + tid; v0 < total; v0 += U * step) {
@@ -276,23 +170,180 @@ __global__ void __launch_bounds__(kThreads, 7)
         sc[to] = sc[from];
         if (kp != nullptr) kp[to] = from;
       }
-    __syncthreads();
-    // the rows not used yet go to the front of their list
-    const int left = n_src - n_hole;
-    int32_t keep_src[kScan / kThreads];
+  };
+  const int drop = cand - A;
+  if (A > 0 && drop <= kFewDrops && in_smem) {
+    // A few rows go (every step of a generation at its budget): the least score, of equal ones the highest row's, is found
+    // and taken out `drop` times, two barriers each, instead of the selection's and the scans' thirty (the step of 12,288
+    // streams that drop one of 1,025 rows: 223 us with those).
+    for (int i = tid; i < cand; i += kThreads) keys[i] = order_key(sc[i]);
+    for (int d = 0; d < drop; ++d) {
+      uint64_t best = ~0ull;
+      for (int i = tid; i < cand; i += kThreads) best = min(best, (uint64_t)keys[i] << 32 | (0xFFFFFFFFu - (uint32_t)i));
 #pragma unroll
-    for (int u = 0; u < kScan / kThreads; ++u) {
-      const int j = u * kThreads + tid;
-      if (j < left) keep_src[u] = sh.l.srcs[n_hole + j];
+      for (int off = 16; off >= 1; off >>= 1) best = min(best, __shfl_xor_sync(kFull, best, off));
+      if ((tid & 31) == 0) sh.least[d & 1][tid >> 5] = best;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) best = min(best, sh.least[d & 1][w]);
+      const int row = (int)(0xFFFFFFFFu - (uint32_t)best);
+      if (row % kThreads == tid) keys[row] = 0xFFFFFFFFu;  // above every score's key; the thread that reads it
+      if (tid == 0) sh.dropped[d] = row;
+    }
+    if (rank == 0 && kp != nullptr)
+      for (int i = tid; i < A; i += kThreads) kp[i] = i;
+    __syncthreads();
+    int n_hole = 0;
+    for (int d = 0; d < drop; ++d) n_hole += sh.dropped[d] < A;
+    if (tid < drop) {
+      const int row = sh.dropped[tid];
+      int below = 0;  // dropped rows below it
+      for (int d = 0; d < drop; ++d) below += sh.dropped[d] < row;
+      if (row < A) sh.l.holes[below] = row;
+      // rows A .. A + drop - 1 that stay: the tid-th of them, less the dropped ones below it
+      const int src = A + tid;
+      bool stays = true;
+      int rank_src = tid;
+      for (int d = 0; d < drop; ++d) {
+        stays = stays && sh.dropped[d] != src;
+        rank_src -= sh.dropped[d] >= A && sh.dropped[d] < src;
+      }
+      if (stays) sh.l.srcs[rank_src] = src;
     }
     __syncthreads();
+    if (CN > 1) cluster_sync();  // every CTA of the cluster has read the scores
+    move(n_hole);
+  } else {
+    // ------------------------------ the A-th largest score ---------------------------------------
+    uint32_t T = 0;              // stays: key > T, and the first `need` (in row order) with key == T
+    int need = 0x7FFFFFFF;
+    bool ties = false;           // fewer of the equal ones stay than there are
+    if (A > 0) {
+      if (in_smem)
+        for (int i = tid; i < cand; i += kThreads) keys[i] = order_key(sc[i]);
+      uint32_t prefix = 0, want = (uint32_t)A;
+      int shift = 21;
+      for (int pass = 0; pass < 3; ++pass) {
+        const int width = pass == 2 ? 10 : 11;
+        const int hi = shift + width;  // the digits above are `prefix`
 #pragma unroll
-    for (int u = 0; u < kScan / kThreads; ++u) {
-      const int j = u * kThreads + tid;
-      if (j < left) sh.l.srcs[j] = keep_src[u];
+        for (int b = 0; b < kBins / kThreads; ++b) sh.hist[b * kThreads + tid] = 0;
+        __syncthreads();
+        const uint32_t mask = (1u << width) - 1u;
+        for (int i = tid; i < cand; i += kThreads) {
+          const uint32_t k = key(i);
+          if (pass == 0 || k >> hi == prefix) atomicAdd(&sh.hist[(k >> shift) & mask], 1u);
+        }
+        __syncthreads();
+        // thread t holds the eight bins from the (t + 1)-th eight from the top down
+        const int per = kBins / kThreads, top = kBins - 1 - tid * per;
+        uint32_t c[kBins / kThreads], mine = 0;
+#pragma unroll
+        for (int b = 0; b < per; ++b) {
+          c[b] = sh.hist[top - b];
+          mine += c[b];
+        }
+        uint32_t all;
+        uint32_t above = block_scan(mine, sh, &all);
+        if (above < want && want <= above + mine) {
+#pragma unroll
+          for (int b = 0; b < per; ++b) {
+            if (above < want && want <= above + c[b]) {
+              sh.bin = (uint32_t)(top - b);
+              sh.above = above;
+              sh.in_bin = c[b];
+            }
+            above += c[b];
+          }
+        }
+        __syncthreads();
+        prefix = prefix << width | sh.bin;
+        want -= sh.above;
+        T = prefix << shift;
+        if (want == sh.in_bin) break;  // the whole bin stays: every key from its lowest on
+        if (pass == 2) {
+          need = (int)want;
+          ties = true;
+        }
+        shift -= pass == 1 ? 10 : 11;
+        __syncthreads();
+      }
+      // no key of the bin's range lies at or below T but T itself, so "key >= T" is "key > T or the equal ones"
     }
-    n_src = left;
+
+    // ------------------------------ holes, and the rows that fill them ---------------------------
+    const uint32_t uneed = (uint32_t)need;
+    uint32_t eq_hole = 0, eq_src = 0;  // equal ones before each scan's next candidate
+    if (ties) {                        // those below row A
+      uint32_t c = 0;
+      for (int i = tid; i < A; i += kThreads) c += key(i) == T;
+      block_scan(c, sh, &eq_src);
+    }
     __syncthreads();
+    if (CN > 1) cluster_sync();  // every CTA of the cluster has read the scores
+    // One step of a scan: the candidates [base, min(base + kScan, end)) that stay (or go) are appended to list at *count.
+    auto scan = [&](int base, int end, uint32_t& eq_before, bool stay, int32_t* list, int count) {
+      uint32_t gt = 0, eq = 0;
+      const int i0 = base + 4 * tid;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (i0 + u < end) {
+          const uint32_t k = key(i0 + u);
+          gt |= (uint32_t)(k > T) << u;
+          eq |= (uint32_t)(k == T) << u;
+        }
+      }
+      uint32_t sum;
+      const uint32_t pre = block_scan(__popc(gt) | __popc(eq) << 16, sh, &sum);
+      uint32_t e = eq_before + (pre >> 16);
+      uint32_t stayed = (pre & 0xFFFFu) + (min(e, uneed) - min(eq_before, uneed));
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int i = i0 + u;
+        if (i < end) {
+          const bool s = (gt >> u & 1u) || ((eq >> u & 1u) && e < uneed);
+          e += eq >> u & 1u;
+          if (stay && s) list[count + stayed] = i;
+          if (!stay && !s) list[count + (uint32_t)(i - base) - stayed] = i;
+          if (!stay && s && kp != nullptr && rank == 0) kp[i] = i;
+          stayed += s;
+        }
+      }
+      const int total = (int)((sum & 0xFFFFu) + (min(eq_before + (sum >> 16), uneed) - min(eq_before, uneed)));
+      eq_before += sum >> 16;
+      __syncthreads();
+      return stay ? total : min(end - base, kScan) - total;
+    };
+    int at_src = A, n_src = 0;
+    for (int at_hole = 0; at_hole < A; at_hole += kScan) {
+      const int n_hole = scan(at_hole, A, eq_hole, false, sh.l.holes, 0);
+      while (n_src < n_hole && at_src < cand) {
+        n_src += scan(at_src, cand, eq_src, true, sh.l.srcs, n_src);
+        at_src += kScan;
+      }
+      if (n_hole > n_src) {  // cannot be: as many stay beyond row A as go below it
+        if (tid == 0) atomicOr(buf.status, STATUS_CHECK);
+        break;
+      }
+      move(n_hole);
+      __syncthreads();
+      // the rows not used yet go to the front of their list
+      const int left = n_src - n_hole;
+      int32_t keep_src[kScan / kThreads];
+#pragma unroll
+      for (int u = 0; u < kScan / kThreads; ++u) {
+        const int j = u * kThreads + tid;
+        if (j < left) keep_src[u] = sh.l.srcs[n_hole + j];
+      }
+      __syncthreads();
+#pragma unroll
+      for (int u = 0; u < kScan / kThreads; ++u) {
+        const int j = u * kThreads + tid;
+        if (j < left) sh.l.srcs[j] = keep_src[u];
+      }
+      n_src = left;
+      __syncthreads();
+    }
   }
   if (CN > 1)
     cluster_sync();

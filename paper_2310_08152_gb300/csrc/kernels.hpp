@@ -159,6 +159,8 @@ struct PrefixArgs {
   const uint16_t* q;        // [b][H][D] per layer, 16-byte aligned
   int64_t q_stride;
   float c2;                 // scale * log2(e)
+  int* status;
+  unsigned long long wait_limit_ns;
 };
 // The own rows' part, joined with the prefix's.
 struct OwnArgs {
@@ -171,10 +173,18 @@ struct OwnArgs {
   // layers: 646 us, one after the other 588).
   int early;
 };
-// Queries of one CTA where the largest group has `group` members; CTAs per SM of that kernel.
+// Queries of one CTA where the largest group has `group` members (kPrefixTcRows: launch_prefix_tc, with maps of the
+// prefix's planes, else launch_prefix); CTAs per SM of that kernel.
+constexpr int kPrefixTcRows = 128;
+// Most rows of a run in launch_prefix.
+constexpr int64_t kPrefixRun = 8192;
 int prefix_rows(int group);
 cudaError_t prefix_ctas_per_sm(const Geometry& g, int device, int rows, int* occ);
 cudaError_t launch_prefix(const Geometry& g, const PrefixArgs& a, int device, int rows, cudaStream_t stream);
+struct alignas(64) PrefixMaps {
+  unsigned char k[128], v[128];
+};
+cudaError_t launch_prefix_tc(const Geometry& g, const PrefixMaps& maps, const PrefixArgs& a, cudaStream_t stream);
 cudaError_t launch_own(const Geometry& g, const OwnArgs& a, int64_t max_segment, int num_sms, cudaStream_t stream);
 
 // Scores follow their rows through a compaction (after launch_compact, from the same source map): in place, zero in
@@ -249,9 +259,9 @@ struct alignas(64) PrefillMaps {
 };
 
 cudaError_t encode_prefill_maps(const Geometry& g, const Buffers& buf, PrefillMaps* maps);
-// A 2-D map of the K planes as above in boxes of 128 rows; a 3-D map of queries [n_tok][H][D] in boxes of one column
+// A 2-D map of the K or the V planes (base) as above in boxes of 128 rows; a 3-D map of queries [n_tok][H][D] in boxes of one column
 // subtile x one head x 128 tokens.  out: 128 bytes.
-cudaError_t encode_key_map(const Geometry& g, const Buffers& buf, unsigned char* out);
+cudaError_t encode_rows_map(const Geometry& g, const void* base, unsigned char* out);
 cudaError_t encode_query_map(const Geometry& g, const void* q, int64_t n_tok, unsigned char* out);
 // Most CTAs of the persistent prefill grid.
 constexpr int kMaxPrefillCtas = 1024;
@@ -269,17 +279,17 @@ cudaError_t launch_prefill(const Geometry& g, const PrefillMaps& maps, const Pre
 // ---------------------------------------------------------------------------------------------
 // A sequence with queries: they are stored rows [q0, len), tokens tok0 .. of q; row0 = seq_row0[s]; its rows' mask bounds
 // (as the prefill's) start at meta[moff], a multiple of 128, the least `hid` of each 128 rows at least[moff / 128].
-struct ScoreSeq {
+struct alignas(16) ScoreSeq {
   int32_t tok0, q0, len, moff, row0, cap, s, pad;
 };
 // A unit of the first pass: key tiles [kt0, kt1) for query tile qt; of the second: key tiles [kt0, kt1).
-struct ScoreUnit {
-  int32_t seq, qt, kt0, kt1, split, pad0, pad1, pad2;
+struct alignas(16) ScoreUnit {
+  ScoreSeq q;
+  int32_t qt, kt0, kt1, split;
 };
 struct ScoreArgs {
   int layer, H, rot;
   int64_t C, n_tok;         // tokens of q
-  const ScoreSeq* seqs;
   const ScoreUnit* units;   // of the pass
   int n_units;              // each for H heads
   const int32_t* meta;
@@ -290,20 +300,22 @@ struct ScoreArgs {
   float c2;
   int* status;
   unsigned long long wait_limit_ns;
-  // rotated queries: their high and low parts
+  // rotated queries: their 16-bit parts, part_stride elements apart
   const uint16_t* q;
-  uint16_t* q_hi;
-  uint16_t* q_lo;
+  uint16_t* q_part;
+  int64_t part_stride;
   const int32_t* pos;
   const int64_t* off;
   const float2* rope_g;
 };
 struct alignas(64) ScoreMaps {
-  unsigned char k[128], q[128], q_lo[128];
+  unsigned char k[128], q[3][128];
 };
+// 16-bit parts that the queries go as: one, or of rotated ones two (f16) or three (bf16).
+int score_parts(const Geometry& g);
 // Resident CTAs per SM of the passes' kernels (sizes the units).
-int score_ctas_per_sm(int D, bool rot);
-// Rotates a.q into a.q_hi and a.q_lo (n_qt 128-query tiles: the first pass's units with split 0).
+int score_ctas_per_sm(const Geometry& g);
+// Rotates a.q into a.q_part (n_qt 128-query tiles: the first pass's units with split 0).
 cudaError_t launch_score_rotate(const Geometry& g, const ScoreArgs& a, cudaStream_t stream);
 // The first pass, and the second, where no sequence has more than 128 queries (few) or some do.
 cudaError_t launch_score_lse(const Geometry& g, const ScoreMaps& maps, const ScoreArgs& a, cudaStream_t stream);

@@ -65,16 +65,16 @@ struct WsLayout {
   size_t pre = 0;        // prefill plan: [PfTileRec tiles][PfItemRec items][int32 meta rows][int32 klist rows]
   int64_t pre_max_tiles = 0;
   size_t pre_bytes = 0;
-  size_t sp = 0;         // plan of a prompt's scores: [ScoreSeq][ScoreUnit first pass][second pass][int32 least][int32 meta]
+  size_t sp = 0;         // plan of a prompt's scores: [ScoreUnit first pass][second pass][int32 least][int32 meta]
   size_t sp_bytes = 0;
   size_t total = 0;
 };
 
 // Units that splitting the keys adds to the first pass of a prompt's scores, at most.
 constexpr int64_t kScoreUnits = 1280;
-size_t score_plan_bytes(int64_t n_seq, int64_t units0, int64_t units1, int64_t n_least, int64_t n_meta) {
-  return sizeof(kvc::ScoreSeq) * (size_t)n_seq + sizeof(kvc::ScoreUnit) * (size_t)(units0 + units1) +
-         align_up(4 * (size_t)n_least, 16) + 4 * (size_t)n_meta;
+size_t score_plan_bytes(int64_t units0, int64_t units1, int64_t n_least, int64_t n_meta) {
+  return sizeof(kvc::ScoreUnit) * (size_t)(units0 + units1) + align_up(4 * (size_t)n_least, 16) +
+         4 * (size_t)n_meta;
 }
 
 WsLayout ws_layout(int b, int H, int D, int rot, int64_t C) {
@@ -107,7 +107,7 @@ WsLayout ws_layout(int b, int H, int D, int rot, int64_t C) {
   L.pre_max_tiles = (C + 127) / 128 + b;
   L.pre_bytes = (sizeof(kvc::PfTileRec) + sizeof(kvc::PfItemRec) * (size_t)H) * (size_t)L.pre_max_tiles + 8 * (size_t)C;
   L.pre = take(L.pre_bytes);
-  L.sp_bytes = score_plan_bytes(b, L.pre_max_tiles, L.pre_max_tiles + kScoreUnits, L.pre_max_tiles, C + 128 * (int64_t)b);
+  L.sp_bytes = score_plan_bytes(L.pre_max_tiles, L.pre_max_tiles + kScoreUnits, L.pre_max_tiles, C + 128 * (int64_t)b);
   L.sp = take(L.sp_bytes);
   L.total = o;
   return L;
@@ -283,7 +283,7 @@ struct kvc_cache {
   std::vector<int32_t> sp_nq;
   int sp_units0 = 0, sp_units1 = 0;
   bool sp_few = true;
-  size_t sp_unit0 = 0, sp_unit1 = 0, sp_least = 0, sp_meta = 0;  // offsets inside the plan
+  size_t sp_unit1 = 0, sp_least = 0, sp_meta = 0;  // offsets inside the plan
   kvc::ScoreMaps sp_maps;
   bool sp_maps_ready = false;
   // kvc_set_prefix: the prefix's cache, each sequence's prefix in it (or -1) and the scratch; then the plan in the
@@ -295,6 +295,8 @@ struct kvc_cache {
   int px_layers = 0, px_rows = 0, px_units = 0;
   int64_t px_parts = 0;
   size_t px_members = 0, px_split0 = 0, px_nsplit = 0;  // offsets behind the units
+  kvc::PrefixMaps px_maps;
+  bool px_maps_ready = false;
   bool amaps_ok = false;  // the append kernel's TMA descriptors are in the workspace
   // compaction timing (kvc_set_compaction_timing): events before the scan, between the kernels, after
   bool time_compaction = false;
@@ -1102,16 +1104,17 @@ kvc_status kvc_decode_attention_scored(kvc_cache* c, int first, int n_layers, co
   return ok();
 }
 
-// Parts that the keys of each query tile are cut into in the first pass of a prompt's scores: enough for two waves.
-static int score_splits(const kvc_cache* c, const int32_t* n_q) {
-  int64_t tiles = 0, longest = 0;
+// Parts that the keys of each query tile are cut into in the first pass of a prompt's scores: enough for two waves, of two
+// key tiles at least (which the scratch's size, for any lengths, leaves out).
+static int score_splits(const kvc_cache* c, const int32_t* n_q, bool any_length) {
+  int64_t tiles = 0, longest = any_length ? INT32_MAX : 0;
   for (int s = 0; s < c->cfg.b; ++s) {
     if (n_q[s] <= 0) continue;
     tiles += (n_q[s] + 127) / 128;
-    longest = std::max(longest, (c->bk.book.stored(s) + 127) / 128);
+    if (!any_length) longest = std::max(longest, (c->bk.book.stored(s) + 127) / 128);
   }
   if (tiles == 0) return 1;
-  const int64_t slots = (int64_t)kvc::score_ctas_per_sm(c->cfg.d_head, c->cfg.rotary_dim > 0) * c->num_sms;
+  const int64_t slots = (int64_t)kvc::score_ctas_per_sm(c->geom()) * c->num_sms;
   const int64_t want = 2 * slots / std::max<int64_t>(1, tiles * c->cfg.H);
   return (int)std::max<int64_t>(1, std::min<int64_t>({want, longest / 2, kScoreUnits / tiles, 32}));
 }
@@ -1136,8 +1139,9 @@ kvc_status kvc_score_scratch_bytes(kvc_cache* c, const int32_t* n_q, size_t* byt
   if (!bytes) return fail(KVC_ERR_INVALID_ARG, "bytes is NULL");
   int64_t n = 0;
   for (int s = 0; s < c->cfg.b; ++s) n += n_q[s];
-  *bytes = align_up(8 * (size_t)score_splits(c, n_q) * c->cfg.H * (size_t)n, 256);
-  if (c->cfg.rotary_dim > 0) *bytes += 2 * align_up(2 * (size_t)n * c->cfg.H * c->cfg.d_head, 256);
+  *bytes = align_up(8 * (size_t)score_splits(c, n_q, true) * c->cfg.H * (size_t)n, 256);
+  if (c->cfg.rotary_dim > 0)
+    *bytes += kvc::score_parts(c->geom()) * align_up(2 * (size_t)n * c->cfg.H * c->cfg.d_head, 256);
   return ok();
 }
 
@@ -1168,37 +1172,34 @@ static kvc_status plan_score(kvc_cache* c, const int32_t* n_q, int n_split, cuda
     key_tiles += (len + 127) / 128;
   }
   // key tiles of a unit of the second pass where its query tile stays: two waves of units, sixteen tiles at most
-  const int64_t slots = (int64_t)kvc::score_ctas_per_sm(c->cfg.d_head, c->cfg.rotary_dim > 0) * c->num_sms;
+  const int64_t slots = (int64_t)kvc::score_ctas_per_sm(c->geom()) * c->num_sms;
   const int64_t per = few ? std::max<int64_t>(1, std::min<int64_t>(16, key_tiles * H / (2 * slots))) : 1;
-  for (size_t i = 0; i < seqs.size(); ++i) {
-    const kvc::ScoreSeq& q = seqs[i];
+  for (const kvc::ScoreSeq& q : seqs) {
     for (int32_t r = q.q0, qt = 0; r < q.len; r += 128, ++qt) {
       const int32_t nk = (std::min(r + 128, q.len) + 127) / 128;
       for (int32_t k = 0; k < n_split; ++k)
-        u0.push_back({(int32_t)i, qt, (int32_t)((int64_t)nk * k / n_split), (int32_t)((int64_t)nk * (k + 1) / n_split), k, 0, 0, 0});
+        u0.push_back({q, qt, (int32_t)((int64_t)nk * k / n_split), (int32_t)((int64_t)nk * (k + 1) / n_split), k});
     }
     const int32_t nkt = (q.len + 127) / 128;
     for (int32_t k = 0; k < nkt; k += (int32_t)per)
-      u1.push_back({(int32_t)i, 0, k, std::min(nkt, k + (int32_t)per), 0, 0, 0, 0});
+      u1.push_back({q, 0, k, std::min(nkt, k + (int32_t)per), 0});
   }
   // the second pass begins with the keys that the first read last, which are in L2; or the longest first: the first pass's
   // by their key tiles, the second's by the query tiles that see them
   if (few) std::reverse(u1.begin(), u1.end());
   if (!few) std::stable_sort(u0.begin(), u0.end(), [](const kvc::ScoreUnit& x, const kvc::ScoreUnit& y) { return x.kt1 - x.kt0 > y.kt1 - y.kt0; });
-  auto q_tiles = [&](const kvc::ScoreUnit& u) { return seqs[u.seq].len - std::max(seqs[u.seq].q0, u.kt0 * 128); };
-  if (!few) std::stable_sort(u1.begin(), u1.end(), [&](const kvc::ScoreUnit& x, const kvc::ScoreUnit& y) { return q_tiles(x) > q_tiles(y); });
-  const size_t bytes = score_plan_bytes((int64_t)seqs.size(), (int64_t)u0.size(), (int64_t)u1.size(), (int64_t)least.size(), (int64_t)meta.size());
+  auto q_tiles = [](const kvc::ScoreUnit& u) { return u.q.len - std::max(u.q.q0, u.kt0 * 128); };
+  if (!few) std::stable_sort(u1.begin(), u1.end(), [q_tiles](const kvc::ScoreUnit& x, const kvc::ScoreUnit& y) { return q_tiles(x) > q_tiles(y); });
+  const size_t bytes = score_plan_bytes((int64_t)u0.size(), (int64_t)u1.size(), (int64_t)least.size(), (int64_t)meta.size());
   if (bytes > c->ws.sp_bytes) return fail(KVC_ERR_STATE, "the plan of a prompt's scores exceeds the workspace");
   cudaError_t e;
   unsigned char* img = c->ring.reserve(bytes, &e);
   if (!img) return e != cudaSuccess ? cuda_fail(e, "staging") : fail(KVC_ERR_INVALID_ARG, "score plan exceeds ring");
-  c->sp_unit0 = sizeof(kvc::ScoreSeq) * seqs.size();
-  c->sp_unit1 = c->sp_unit0 + sizeof(kvc::ScoreUnit) * u0.size();
+  c->sp_unit1 = sizeof(kvc::ScoreUnit) * u0.size();
   c->sp_least = c->sp_unit1 + sizeof(kvc::ScoreUnit) * u1.size();
   c->sp_meta = c->sp_least + align_up(4 * least.size(), 16);
   if (!seqs.empty()) {
-    std::memcpy(img, seqs.data(), sizeof(kvc::ScoreSeq) * seqs.size());
-    std::memcpy(img + c->sp_unit0, u0.data(), sizeof(kvc::ScoreUnit) * u0.size());
+    std::memcpy(img, u0.data(), sizeof(kvc::ScoreUnit) * u0.size());
     std::memcpy(img + c->sp_unit1, u1.data(), sizeof(kvc::ScoreUnit) * u1.size());
     std::memcpy(img + c->sp_least, least.data(), 4 * least.size());
     std::memcpy(img + c->sp_meta, meta.data(), 4 * meta.size());
@@ -1233,7 +1234,7 @@ kvc_status kvc_score_prompt(kvc_cache* c, int layer, const void* q, const int32_
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
   st = c->ensure_cuda(stream);
   if (st != KVC_OK) return st;
-  const int n_split = score_splits(c, n_q);
+  const int n_split = score_splits(c, n_q, false);
   if (c->sp_version != c->version || !std::equal(c->sp_nq.begin(), c->sp_nq.end(), n_q)) {
     st = plan_score(c, n_q, n_split, stream);
     if (st != KVC_OK) return st;
@@ -1241,7 +1242,7 @@ kvc_status kvc_score_prompt(kvc_cache* c, int layer, const void* q, const int32_
   if (c->sp_units0 == 0) return ok();
   cudaError_t e = cudaSuccess;
   if (!c->sp_maps_ready) {
-    e = kvc::encode_key_map(c->geom(), c->bufs(), c->sp_maps.k);
+    e = kvc::encode_rows_map(c->geom(), c->cfg.k_base, c->sp_maps.k);
     if (e != cudaSuccess) return cuda_fail(e, "cuTensorMapEncodeTiled (K planes)");
     c->sp_maps_ready = true;
   }
@@ -1253,8 +1254,7 @@ kvc_status kvc_score_prompt(kvc_cache* c, int layer, const void* q, const int32_
   a.rot = c->cfg.rotary_dim;
   a.C = c->C;
   for (int s = 0; s < c->cfg.b; ++s) a.n_tok += n_q[s];
-  a.seqs = reinterpret_cast<const kvc::ScoreSeq*>(plan);
-  a.units = reinterpret_cast<const kvc::ScoreUnit*>(plan + c->sp_unit0);
+  a.units = reinterpret_cast<const kvc::ScoreUnit*>(plan);
   a.n_units = c->sp_units0;
   a.meta = reinterpret_cast<const int32_t*>(plan + c->sp_meta);
   a.least = reinterpret_cast<const int32_t*>(plan + c->sp_least);
@@ -1270,21 +1270,20 @@ kvc_status kvc_score_prompt(kvc_cache* c, int layer, const void* q, const int32_
   a.off = sta.off;
   a.rope_g = sta.rope_g;
   kvc::ScoreMaps maps = c->sp_maps;
-  const void* q_hi = q;
-  const void* q_lo = q;
+  const void* first = q;
   if (a.rot > 0) {
-    unsigned char* at = static_cast<unsigned char*>(scratch) + align_up(8 * (size_t)n_split * a.H * (size_t)a.n_tok, 256);
-    a.q_hi = reinterpret_cast<uint16_t*>(at);
-    a.q_lo = reinterpret_cast<uint16_t*>(at + align_up(2 * (size_t)a.n_tok * a.H * c->cfg.d_head, 256));
-    q_hi = a.q_hi;
-    q_lo = a.q_lo;
+    a.q_part = reinterpret_cast<uint16_t*>(static_cast<unsigned char*>(scratch) +
+                                           align_up(8 * (size_t)n_split * a.H * (size_t)a.n_tok, 256));
+    a.part_stride = (int64_t)align_up(2 * (size_t)a.n_tok * a.H * c->cfg.d_head, 256) / 2;
+    first = a.q_part;
     e = kvc::launch_score_rotate(c->geom(), a, stream);
     if (e != cudaSuccess) return cuda_fail(e, "query rotation kernel");
     c->launches += 1;
   }
-  e = kvc::encode_query_map(c->geom(), q_hi, a.n_tok, maps.q);
-  if (e == cudaSuccess) e = kvc::encode_query_map(c->geom(), q_lo, a.n_tok, maps.q_lo);
-  if (e != cudaSuccess) return cuda_fail(e, "cuTensorMapEncodeTiled (queries)");
+  for (int i = 0; i < kvc::score_parts(c->geom()); ++i) {
+    e = kvc::encode_query_map(c->geom(), static_cast<const uint16_t*>(first) + i * a.part_stride, a.n_tok, maps.q[i]);
+    if (e != cudaSuccess) return cuda_fail(e, "cuTensorMapEncodeTiled (queries)");
+  }
   e = kvc::launch_score_lse(c->geom(), maps, a, stream);
   if (e != cudaSuccess) return cuda_fail(e, "score kernel (first pass)");
   c->launches += 1;
@@ -1299,14 +1298,21 @@ kvc_status kvc_score_prompt(kvc_cache* c, int layer, const void* q, const int32_
 
 // The scratch of a shared-prefix decode: [units][members b][split0 b][n_split b], then the parts.  Units of one (layer,
 // head): at most one run per group of prefix_rows sequences, and kPrefixUnits more that splitting adds over all (layer,
-// head) pairs; parts: as many as sequences, layers and heads, and 64 for each run that splitting adds.
-static constexpr int64_t kPrefixUnits = 1280;
-static size_t prefix_tables(int b) { return align_up(sizeof(kvc::PrefixUnit) * (size_t)(kPrefixUnits + b), 16) + 3 * align_up(4 * (size_t)b, 16); }
+// head) pairs, or as many as keep runs at kPrefixRun rows; parts: as many as sequences, layers and heads, for each kPrefixRun
+// rows of the longest prefix, and 128 for each run that splitting adds.
+static constexpr int64_t kPrefixUnits = 640;
+static int64_t prefix_runs(const kvc_cache* prefix) {
+  return (*std::max_element(prefix->cap.begin(), prefix->cap.end()) + kvc::kPrefixRun - 1) / kvc::kPrefixRun;
+}
+static size_t prefix_tables(int b, int64_t runs) {
+  return align_up(sizeof(kvc::PrefixUnit) * (size_t)(kPrefixUnits + b * runs), 16) + 3 * align_up(4 * (size_t)b, 16);
+}
 
-size_t kvc_prefix_scratch_bytes(const kvc_cache* c) {
-  if (!c) return 0;
-  const int64_t rows = (int64_t)c->cfg.M * c->cfg.H * c->cfg.b + 64 * kPrefixUnits;
-  return align_up(prefix_tables(c->cfg.b), 256) + 4 * (size_t)rows * (size_t)(c->cfg.d_head + 4);
+size_t kvc_prefix_scratch_bytes(const kvc_cache* c, const kvc_cache* prefix) {
+  if (!c || !prefix) return 0;
+  const int64_t runs = prefix_runs(prefix);
+  const int64_t rows = (int64_t)c->cfg.M * c->cfg.H * c->cfg.b * runs + kvc::kPrefixTcRows * kPrefixUnits;
+  return align_up(prefix_tables(c->cfg.b, runs), 256) + 4 * (size_t)rows * (size_t)(c->cfg.d_head + 4);
 }
 
 kvc_status kvc_set_prefix(kvc_cache* c, kvc_cache* prefix, const int32_t* parent, void* scratch, size_t scratch_bytes) {
@@ -1327,13 +1333,16 @@ kvc_status kvc_set_prefix(kvc_cache* c, kvc_cache* prefix, const int32_t* parent
   for (int s = 0; s < a.b; ++s)
     if (parent[s] < -1 || parent[s] >= p.b)
       return fail(KVC_ERR_INVALID_ARG, "parent[%d] = %d outside [-1, %d)", s, parent[s], p.b);
+  if ((int64_t)p.M * p.H * prefix->C >= ((int64_t)1 << 31))
+    return fail(KVC_ERR_UNSUPPORTED, "M*H*sum(capacity) rows of the prefix exceed the 2^31 rows a tensor-map coordinate reaches");
   if (reinterpret_cast<uintptr_t>(scratch) & 255) return fail(KVC_ERR_INVALID_ARG, "scratch must be 256-byte aligned");
-  if (scratch_bytes < kvc_prefix_scratch_bytes(c))
-    return fail(KVC_ERR_INVALID_ARG, "%zu bytes of scratch, %zu needed", scratch_bytes, kvc_prefix_scratch_bytes(c));
+  if (scratch_bytes < kvc_prefix_scratch_bytes(c, prefix))
+    return fail(KVC_ERR_INVALID_ARG, "%zu bytes of scratch, %zu needed", scratch_bytes, kvc_prefix_scratch_bytes(c, prefix));
   c->prefix = prefix;
   c->parent.assign(parent, parent + a.b);
   c->px = static_cast<unsigned char*>(scratch);
   c->px_version = UINT64_MAX;
+  c->px_maps_ready = false;
   return ok();
 }
 
@@ -1353,13 +1362,14 @@ static kvc_status plan_prefix(kvc_cache* c, int n_layers, cudaStream_t stream) {
   int occ = 1;
   cudaError_t e = kvc::prefix_ctas_per_sm(c->geom(), c->device, rows, &occ);
   if (e != cudaSuccess) return cuda_fail(e, "prefix kernel");
+  const int64_t most_run = rows == kvc::kPrefixTcRows ? INT32_MAX : kvc::kPrefixRun, runs_max = prefix_runs(c->prefix);
   const int64_t pairs = (int64_t)n_layers * c->cfg.H, slots = (int64_t)occ * c->num_sms;
-  for (int g = 0; g < P; ++g) units1 += pairs * (int64_t)((group[g].size() + rows - 1) / rows);
-  // Rows of a run: at least 32 per member, so that a part's 8 (d_head + 4) bytes a member, written and read, stay small
-  // beside the run's rows, and 256.
+  auto chunks_of = [&](int g) { return (int64_t)((group[g].size() + rows - 1) / rows); };
+  for (int g = 0; g < P; ++g) units1 += pairs * chunks_of(g) * ((c->prefix->bk.book.stored(g) + most_run - 1) / most_run);
+  // Rows of a run: at least 256, and 16 per member, for a part's 8 (d_head + 4) bytes a member, written and read.
   auto run_of = [&](int g, int64_t run) {
-    const int64_t least = std::max<int64_t>(256, 32 * std::min<int64_t>((int64_t)group[g].size(), rows));
-    return std::max(run, least);
+    const int64_t least = std::max<int64_t>(256, 16 * std::min<int64_t>((int64_t)group[g].size(), rows));
+    return std::min(std::max(run, least), most_run);
   };
   auto runs_of = [&](int g, int64_t run) {
     const int64_t len = c->prefix->bk.book.stored(g), r = run_of(g, run);
@@ -1375,13 +1385,13 @@ static kvc_status plan_prefix(kvc_cache* c, int n_layers, cudaStream_t stream) {
     for (int g = 0; g < P; ++g) {
       if (group[g].empty()) continue;
       const int64_t n = runs_of(g, r);
-      units += pairs * n * (int64_t)((group[g].size() + rows - 1) / rows);
+      units += pairs * n * chunks_of(g);
       most = std::max(most, std::min(c->prefix->bk.book.stored(g), run_of(g, r)));
     }
     if (units > units1 + kPrefixUnits) break;
     double rows_all = 0;
     for (int g = 0; g < P; ++g)
-      rows_all += (double)pairs * (double)((group[g].size() + rows - 1) / rows) * (double)c->prefix->bk.book.stored(g);
+      rows_all += (double)pairs * (double)chunks_of(g) * (double)c->prefix->bk.book.stored(g);
     const double even = (rows_all + 160.0 * (double)units) / (double)slots;
     // balanced units finish in whole waves; ragged ones fill the gaps, but no earlier than an even share and a unit
     const double waves = (double)((units + slots - 1) / slots) * (double)(most + 160);
@@ -1413,7 +1423,8 @@ static kvc_status plan_prefix(kvc_cache* c, int n_layers, cudaStream_t stream) {
   }
   const size_t ub = align_up(sizeof(kvc::PrefixUnit) * units.size(), 16), ib = align_up(4 * (size_t)b, 16);
   const size_t part_bytes = 4 * (size_t)(parts * pairs) * (size_t)(c->cfg.d_head + 4);
-  if (ub + 3 * ib > prefix_tables(b) || align_up(prefix_tables(b), 256) + part_bytes > kvc_prefix_scratch_bytes(c))
+  if (ub + 3 * ib > prefix_tables(b, runs_max) ||
+      align_up(prefix_tables(b, runs_max), 256) + part_bytes > kvc_prefix_scratch_bytes(c, c->prefix))
     return fail(KVC_ERR_STATE, "the prefix plan exceeds its scratch");
   unsigned char* img = c->ring.reserve(ub + 3 * ib, &e);
   if (!img) return e != cudaSuccess ? cuda_fail(e, "staging") : fail(KVC_ERR_INVALID_ARG, "prefix plan exceeds ring");
@@ -1473,13 +1484,25 @@ kvc_status kvc_decode_attention_shared(kvc_cache* c, int first, int n_layers, co
   pa.split0 = reinterpret_cast<const int32_t*>(c->px + c->px_split0);
   pa.n_split = reinterpret_cast<const int32_t*>(c->px + c->px_nsplit);
   pa.n_parts = c->px_parts;
-  pa.parts = reinterpret_cast<float*>(c->px + align_up(prefix_tables(c->cfg.b), 256));
+  pa.parts = reinterpret_cast<float*>(c->px + align_up(prefix_tables(c->cfg.b, prefix_runs(p)), 256));
   pa.q = static_cast<const uint16_t*>(q);
   pa.q_stride = q_layer_stride;
   pa.c2 = scale * 1.4426950408889634f;
+  pa.status = c->bufs().status;
+  pa.wait_limit_ns = 2000000000ull;
   cudaError_t e;
   if (c->px_units > 0) {
-    e = kvc::launch_prefix(c->geom(), pa, c->device, c->px_rows, stream);
+    if (c->px_rows == kvc::kPrefixTcRows) {
+      if (!c->px_maps_ready) {
+        e = kvc::encode_rows_map(p->geom(), p->cfg.k_base, c->px_maps.k);
+        if (e == cudaSuccess) e = kvc::encode_rows_map(p->geom(), p->cfg.v_base, c->px_maps.v);
+        if (e != cudaSuccess) return cuda_fail(e, "cuTensorMapEncodeTiled (the prefix's planes)");
+        c->px_maps_ready = true;
+      }
+      e = kvc::launch_prefix_tc(c->geom(), c->px_maps, pa, stream);
+    } else {
+      e = kvc::launch_prefix(c->geom(), pa, c->device, c->px_rows, stream);
+    }
     if (e != cudaSuccess) return cuda_fail(e, "prefix kernel");
     c->launches += 1;
     c->last_was_decode = false;  // until the launch below

@@ -1155,9 +1155,9 @@ cudaError_t encode_prefill_maps(const Geometry& g, const Buffers& buf, PrefillMa
   return e;
 }
 
-cudaError_t encode_key_map(const Geometry& g, const Buffers& buf, unsigned char* out) {
+cudaError_t encode_rows_map(const Geometry& g, const void* base, unsigned char* out) {
   const cudaError_t e = load_encoder();
-  return e != cudaSuccess ? e : encode_plane(g, buf.k, 128, out);
+  return e != cudaSuccess ? e : encode_plane(g, const_cast<void*>(base), 128, out);
 }
 
 cudaError_t encode_query_map(const Geometry& g, const void* q, int64_t n_tok, unsigned char* out) {

@@ -2,21 +2,22 @@
 // which joins the two.
 //
 // prefix_kernel.  The samples of one prompt have the prompt's rows in common.  A decode of each on its own reads those rows once per
-// sample; here one CTA takes the queries of up to 64 samples of a (layer, head) against a run of the prefix's rows, so
+// sample; here one CTA takes the queries of up to 32 samples of a (layer, head) against a run of the prefix's rows, so
 // that the rows are read once for all of them, and leaves for each sample the part's maximum, sum and unscaled output
 //   m = max z_i,  l = sum 2^(z_i - m),  O = sum 2^(z_i - m) v_i,   z_i = scale log2(e) <q, k_i>,
 // which own_kernel joins with the sample's own rows.
 //
 // The queries are the M rows of 16 x 8 x 16 matrix instructions: with the paper's 8 samples of a prompt the work is that
 // of one 16-row tile, an eighth of the smallest tile of the tcgen05 instructions, and P stays in registers between the
-// two products.  The warps share a CTA's keys (and, past 32 queries, its queries); each keeps its own online softmax and
-// the results are merged in shared memory at the end.  Tiles of 64 rows come through a ring of two or three stages with 16-byte
+// two products.  The warps share a CTA's keys; each keeps its own online softmax and
+// the results are merged in shared memory at the end.  (More than 32 samples: prefix_tc.cu.)  Tiles of 64 rows come through a ring of two or three stages with 16-byte
 // asynchronous copies into rows padded by 16 bytes, which keeps the matrix loads free of bank conflicts at every d_head.
 //
-// Precision.  q.k is exact in its products and summed in 32 bits; a rotated query goes as a high and a low 16-bit part.
-// P goes as a high and a low part as well (22 bits in f16, 16 in bf16), so that the output keeps what a 32-bit P would
-// give to within 2^-18.  P's reference is 2^6 to 2^14 below the running maximum, which keeps f16's low part out of its
-// subnormal range and makes rescaling rare.
+// Precision.  q.k is exact in its products and summed in 32 bits; a rotated query, and P, go as two 16-bit parts in f16 (22
+// bits) and three in bf16 (24), for the output is in 32 bits.  (With two of bf16 its error was 2.3e-6 where 32-bit
+// arithmetic leaves 4e-7.)  P's reference is 2^6 to 2^14 below the running maximum, which keeps f16's low part out of its
+// subnormal range and makes rescaling rare.  The tensor cores cut what they add rather than round it, which over thousands
+// of rows adds up (16,384 rows into one sum: 1e-5): no sum here goes over more than a fourth of kPrefixRun rows.
 #include <cuda_runtime.h>
 
 #include <atomic>
@@ -29,27 +30,21 @@ namespace kvc {
 namespace {
 
 constexpr unsigned kFull = 0xFFFFFFFFu;
-constexpr int kKeys = 64;   // rows per tile
+constexpr int kThreads = 128;
+constexpr int kKeys = 64;  // rows per tile
 
-// R = 16 MT queries per CTA of NW warps: WM 16-row tiles per warp, RW warps over the queries, KW over the keys.  At 64
-// queries eight warps of one tile each, since four of two hold 255 registers and leave the tensor cores waiting (two
-// layers of 32 heads of 128, 64 samples of 32,768 rows, bf16: 312 us).
-template <int D, int MT, bool ROT>
+// R = 16 MT queries per CTA: MT 16-row tiles in each of four warps, which share the keys.
+// NQ 16-bit parts of a query.
+template <int D, int MT, int NQ>
 struct PxCfg {
   static constexpr int R = 16 * MT;
-  static constexpr int NW = MT == 4 ? 8 : 4;
-  static constexpr int THREADS = NW * 32;
-  static constexpr int WM = MT == 2 ? 2 : 1;
-  static constexpr int RW = MT / WM;
-  static constexpr int KW = NW / RW;
+  static constexpr int KW = kThreads / 32;
   static constexpr int KG = kKeys / KW / 16;  // 16-key groups per warp and tile
   static constexpr int RS = D * 2 + 16;       // bytes of a row in shared memory
   static constexpr int TILE = kKeys * RS;
-  // three stages of K and V tiles, or two where a third would leave one CTA per SM
-  static constexpr int S = (D == 128 && MT == 4) || MT == 1 ? 2 : 3;
+  static constexpr int S = MT == 1 ? 2 : 3;   // stages: two leave room for a fourth CTA per SM
   static constexpr int OFF_Q = 2 * S * TILE;
-  static constexpr int OFF_QLO = OFF_Q + R * RS;
-  static constexpr int SMEM = OFF_QLO + (ROT ? R * RS : 0);
+  static constexpr int SMEM = OFF_Q + NQ * R * RS;
   static constexpr int PO = D + 4;
   static_assert(KW * R * PO * 4 <= OFF_Q, "the warps' results fit in the stages");
 };
@@ -84,10 +79,6 @@ struct Mma<F16T> {
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
   }
-  static __device__ __forceinline__ uint32_t pack(float x, float y) {
-    const __half2 h = __floats2half2_rn(x, y);
-    return *reinterpret_cast<const uint32_t*>(&h);
-  }
 };
 template <>
 struct Mma<BF16T> {
@@ -97,21 +88,15 @@ struct Mma<BF16T> {
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
   }
-  static __device__ __forceinline__ uint32_t pack(float x, float y) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
-    return *reinterpret_cast<const uint32_t*>(&h);
-  }
 };
 
-template <typename T, int D, int MT, bool ROT>
-__global__ void __launch_bounds__(PxCfg<D, MT, ROT>::THREADS, MT == 4 || (D > 96 && MT > 1) ? 2 : MT == 1 && D < 96 ? 4 : 3)
-    prefix_kernel(PrefixArgs p) {
-  using C = PxCfg<D, MT, ROT>;
-  constexpr int kThreads = C::THREADS;
-  constexpr int WM = C::WM, KG = C::KG, CH = D / 8;
+template <typename T, int D, int MT, int NQ>
+__global__ void __launch_bounds__(kThreads, D > 96 && MT > 1 ? 2 : MT == 1 && D < 96 ? 4 : 3) prefix_kernel(PrefixArgs p) {
+  using C = PxCfg<D, MT, NQ>;
+  constexpr int WM = MT, KG = C::KG, CH = D / 8, NP = kFullParts<T>;
   extern __shared__ __align__(128) unsigned char smem[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int rw = warp % C::RW, kw = warp / C::RW;
+  const int kw = warp;
   const uint32_t s0 = smem_addr(smem);
   pdl_wait();               // q and the prefix's rows come from earlier kernels
   pdl_launch_dependents();  // the own rows' decode may start: what it reads before its wait is complete by now
@@ -142,45 +127,27 @@ __global__ void __launch_bounds__(PxCfg<D, MT, ROT>::THREADS, MT == 4 || (D > 96
   // the queries, rotated where the cache's keys are
   for (int x = tid; x < C::R * CH; x += kThreads) {
     const int r = x / CH, c = x % CH;
-    uint4 hi = make_uint4(0, 0, 0, 0), lo = hi;
+    uint32_t part[NQ][4];
+#pragma unroll
+    for (int i = 0; i < NQ; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) part[i][e] = 0;
     if (r < un.n_mem) {
       const int s = p.members[un.mem0 + r];
       const uint16_t* q = p.q + (int64_t)layer * p.q_stride + ((int64_t)s * p.H + h) * D;
-      hi = *reinterpret_cast<const uint4*>(q + c * 8);
-      if (ROT && c * 8 < p.rot) {
-        const int half = p.rot / 2;  // a multiple of eight
-        const bool first = c * 8 < half;
-        const uint4 other = *reinterpret_cast<const uint4*>(q + (first ? c * 8 + half : c * 8 - half));
-        const int32_t pos = p.ds[s].qpos;
-        const uint32_t* a = reinterpret_cast<const uint32_t*>(&hi);
-        const uint32_t* b = reinterpret_cast<const uint32_t*>(&other);
-        uint32_t oh[4], ol[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float2 x2 = T::f2(a[e]), y2 = T::f2(b[e]);
-          const int i = (first ? c * 8 : c * 8 - half) + 2 * e;
-          float sn0, cs0, sn1, cs1;
-          rope_sincos_full(pos, p.st.rope_g[i], &sn0, &cs0);
-          rope_sincos_full(pos, p.st.rope_g[i + 1], &sn1, &cs1);
-          const float z0 = first ? x2.x * cs0 - y2.x * sn0 : x2.x * cs0 + y2.x * sn0;
-          const float z1 = first ? x2.y * cs1 - y2.y * sn1 : x2.y * cs1 + y2.y * sn1;
-          oh[e] = Mma<T>::pack(z0, z1);
-          const float2 back = T::f2(oh[e]);
-          ol[e] = Mma<T>::pack(z0 - back.x, z1 - back.y);
-        }
-        hi = make_uint4(oh[0], oh[1], oh[2], oh[3]);
-        lo = make_uint4(ol[0], ol[1], ol[2], ol[3]);
-      }
+      query_chunk<T, NQ>(q, c, p.rot, NQ > 1 ? p.ds[s].qpos : 0, p.st.rope_g, part);
     }
-    *reinterpret_cast<uint4*>(smem + C::OFF_Q + r * C::RS + c * 16) = hi;
-    if constexpr (ROT) *reinterpret_cast<uint4*>(smem + C::OFF_QLO + r * C::RS + c * 16) = lo;
+#pragma unroll
+    for (int i = 0; i < NQ; ++i)
+      *reinterpret_cast<uint4*>(smem + C::OFF_Q + (i * C::R + r) * C::RS + c * 16) =
+          make_uint4(part[i][0], part[i][1], part[i][2], part[i][3]);
   }
 
   // matrix addresses of this lane: A and V^T tiles take rows lane % 16 and the column half lane / 16; K tiles the keys
   // lane % 8 + 8 (lane / 16) and the column half lane / 8 % 2
   const uint32_t a_off = (lane & 15) * C::RS + (lane >> 4) * 16;
   const uint32_t k_off = ((lane & 7) + (lane >> 4) * 8) * C::RS + (lane >> 3 & 1) * 16;
-  const uint32_t q_addr = s0 + C::OFF_Q + rw * WM * 16 * C::RS + a_off;
+  const uint32_t q_addr = s0 + C::OFF_Q + a_off;
   float o[WM][D / 8][4];
   float m[WM][2], l[WM][2];
 #pragma unroll
@@ -206,25 +173,22 @@ __global__ void __launch_bounds__(PxCfg<D, MT, ROT>::THREADS, MT == 4 || (D > 96
         for (int e = 0; e < 4; ++e) z[i][n][e] = 0.f;
 #pragma unroll
     for (int kk = 0; kk < D / 16; ++kk) {
-      uint32_t a[WM][4], al[WM][4];
+      uint32_t a[NQ][WM][4];
 #pragma unroll
-      for (int i = 0; i < WM; ++i) {
-        ldsm4(a[i], q_addr + i * 16 * C::RS + kk * 32);
-        if constexpr (ROT) ldsm4(al[i], q_addr + (C::OFF_QLO - C::OFF_Q) + i * 16 * C::RS + kk * 32);
-      }
+      for (int x = 0; x < NQ; ++x)
+#pragma unroll
+        for (int i = 0; i < WM; ++i) ldsm4(a[x][i], q_addr + (x * C::R + i * 16) * C::RS + kk * 32);
 #pragma unroll
       for (int g = 0; g < KG; ++g) {
         uint32_t b[4];
         ldsm4(b, kt + g * 16 * C::RS + k_off + kk * 32);
 #pragma unroll
-        for (int i = 0; i < WM; ++i) {
-          Mma<T>::go(z[i][2 * g], a[i], b[0], b[1]);
-          Mma<T>::go(z[i][2 * g + 1], a[i], b[2], b[3]);
-          if constexpr (ROT) {
-            Mma<T>::go(z[i][2 * g], al[i], b[0], b[1]);
-            Mma<T>::go(z[i][2 * g + 1], al[i], b[2], b[3]);
+        for (int x = 0; x < NQ; ++x)
+#pragma unroll
+          for (int i = 0; i < WM; ++i) {
+            Mma<T>::go(z[i][2 * g], a[x][i], b[0], b[1]);
+            Mma<T>::go(z[i][2 * g + 1], a[x][i], b[2], b[3]);
           }
-        }
       }
     }
     const int left = n_keys - t * kKeys - kw * KG * 16;  // the warp's keys of this tile that exist
@@ -272,7 +236,7 @@ __global__ void __launch_bounds__(PxCfg<D, MT, ROT>::THREADS, MT == 4 || (D > 96
     }
 #pragma unroll
     for (int g = 0; g < KG; ++g) {
-      uint32_t ph[WM][4], pl[WM][4];
+      uint32_t pp[NP][WM][4];
 #pragma unroll
       for (int i = 0; i < WM; ++i) {
 #pragma unroll
@@ -281,9 +245,10 @@ __global__ void __launch_bounds__(PxCfg<D, MT, ROT>::THREADS, MT == 4 || (D > 96
           const float mu = m[i][hh] == -INFINITY ? 0.f : m[i][hh];
           const float p0 = ex2(z[i][n][2 * hh] - mu), p1 = ex2(z[i][n][2 * hh + 1] - mu);
           l[i][hh] += p0 + p1;
-          ph[i][f] = Mma<T>::pack(p0, p1);
-          const float2 back = T::f2(ph[i][f]);
-          pl[i][f] = Mma<T>::pack(p0 - back.x, p1 - back.y);
+          uint32_t part[NP];
+          split_parts<T, NP>(p0, p1, part);
+#pragma unroll
+          for (int x = 0; x < NP; ++x) pp[x][i][f] = part[x];
         }
       }
 #pragma unroll
@@ -291,12 +256,12 @@ __global__ void __launch_bounds__(PxCfg<D, MT, ROT>::THREADS, MT == 4 || (D > 96
         uint32_t b[4];
         ldsm4t(b, vt + g * 16 * C::RS + a_off + n * 32);
 #pragma unroll
-        for (int i = 0; i < WM; ++i) {
-          Mma<T>::go(o[i][2 * n], ph[i], b[0], b[1]);
-          Mma<T>::go(o[i][2 * n + 1], ph[i], b[2], b[3]);
-          Mma<T>::go(o[i][2 * n], pl[i], b[0], b[1]);
-          Mma<T>::go(o[i][2 * n + 1], pl[i], b[2], b[3]);
-        }
+        for (int x = 0; x < NP; ++x)
+#pragma unroll
+          for (int i = 0; i < WM; ++i) {
+            Mma<T>::go(o[i][2 * n], pp[x][i], b[0], b[1]);
+            Mma<T>::go(o[i][2 * n + 1], pp[x][i], b[2], b[3]);
+          }
       }
     }
   }
@@ -310,7 +275,7 @@ __global__ void __launch_bounds__(PxCfg<D, MT, ROT>::THREADS, MT == 4 || (D > 96
       float s = l[i][hh];
       s += __shfl_xor_sync(kFull, s, 1);
       s += __shfl_xor_sync(kFull, s, 2);
-      float* to = res + ((int64_t)kw * C::R + (rw * WM + i) * 16 + hh * 8 + (lane >> 2)) * C::PO;
+      float* to = res + ((int64_t)kw * C::R + i * 16 + hh * 8 + (lane >> 2)) * C::PO;
       if ((lane & 3) == 0) {
         to[0] = m[i][hh];
         to[1] = s;
@@ -349,15 +314,15 @@ __global__ void __launch_bounds__(PxCfg<D, MT, ROT>::THREADS, MT == 4 || (D > 96
   }
 }
 
-template <typename T, int D, int MT, bool ROT>
+template <typename T, int D, int MT, int NQ>
 cudaError_t prefix_occ(int dev, int* occ) {
-  using C = PxCfg<D, MT, ROT>;
+  using C = PxCfg<D, MT, NQ>;
   static std::atomic<int> found[64];
   if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
   int o = found[dev].load(std::memory_order_acquire);
   if (o == 0) {
-    cudaError_t e = cudaFuncSetAttribute(prefix_kernel<T, D, MT, ROT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
-    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&o, prefix_kernel<T, D, MT, ROT>, C::THREADS, C::SMEM);
+    cudaError_t e = cudaFuncSetAttribute(prefix_kernel<T, D, MT, NQ>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&o, prefix_kernel<T, D, MT, NQ>, kThreads, C::SMEM);
     if (e != cudaSuccess) return e;
     if (o < 1) o = 1;
     found[dev].store(o, std::memory_order_release);
@@ -382,10 +347,10 @@ struct OwnLanes {
   static constexpr int U = D == 64 ? 4 : D == 80 ? 1 : 2;
   static constexpr int ROWS = U * RPI;
 };
-constexpr int kOwnWarps = 8;
+constexpr int kOwnWarps = 4;
 
 template <typename T, int D, int WPS>
-__global__ void __launch_bounds__(kOwnWarps * 32, 2) own_kernel(OwnArgs a) {
+__global__ void __launch_bounds__(kOwnWarps * 32, 4) own_kernel(OwnArgs a) {
   using L = OwnLanes<D>;
   constexpr int NV = L::NV, U = L::U, QPL = (D + 31) / 32, PO = D + 4;
   __shared__ __align__(16) float s_q[kOwnWarps][D];
@@ -406,6 +371,16 @@ __global__ void __launch_bounds__(kOwnWarps * 32, 2) own_kernel(OwnArgs a) {
   const int n_split = d.is_cl ? 0 : p.n_split[s];
   const int64_t row0 = (int64_t)(p.layer + layer) * H * p.C + p.st.seq_row0[s] + (int64_t)h * p.st.cap[s];
   float* qs = s_q[warp];
+  const float* part = p.parts + (((int64_t)layer * p.n_parts + p.split0[s]) * H + h) * PO;
+  // the first part is there already where this kernel did not start early: its loads are under way with the rows'
+  float M0 = -INFINITY, L0 = 0.f, O0[QPL];
+  auto load_part = [&]() {
+    M0 = __ldcg(part);
+    L0 = __ldcg(part + 1);
+#pragma unroll
+    for (int k = 0; k < QPL; ++k) O0[k] = lane + 32 * k < D ? __ldcg(part + 4 + lane + 32 * k) : 0.f;
+  };
+  if (!a.early && n_split > 0 && sub == 0) load_part();
   if (len > 0) {
     const uint16_t* q = p.q + (int64_t)layer * p.q_stride + (int64_t)w * D;
     const int half = p.rot / 2;
@@ -544,16 +519,18 @@ __global__ void __launch_bounds__(kOwnWarps * 32, 2) own_kernel(OwnArgs a) {
   }
   if (a.early) pdl_wait();  // the parts; every thread of the grid waits, so that it never ends before the prefix's
   if (len == 0 || sub != 0) return;
-  const float* part = p.parts + (((int64_t)layer * p.n_parts + p.split0[s]) * H + h) * PO;
+  if (a.early && n_split > 0) load_part();
   const int64_t step = (int64_t)H * PO;
-  for (int j = 0; j < n_split; ++j, part += step) {
-    const float Mj = __ldcg(part), Lj = __ldcg(part + 1);
-    const float Mn = fmaxf(M, Mj), Mu = Mn == -INFINITY ? 0.f : Mn;
-    const float eo = exp2f(M - Mu), ej = exp2f(Mj - Mu);
-    Ls = Ls * eo + Lj * ej;
+  for (int j = 0; j < n_split; ++j) {
+    if (j > 0) {
+      part += step;
+      load_part();
+    }
+    const float Mn = fmaxf(M, M0), Mu = Mn == -INFINITY ? 0.f : Mn;
+    const float eo = exp2f(M - Mu), ej = exp2f(M0 - Mu);
+    Ls = Ls * eo + L0 * ej;
 #pragma unroll
-    for (int k = 0; k < QPL; ++k)
-      if (lane + 32 * k < D) O[k] = O[k] * eo + __ldcg(part + 4 + lane + 32 * k) * ej;
+    for (int k = 0; k < QPL; ++k) O[k] = O[k] * eo + O0[k] * ej;
     M = Mn;
   }
   const float inv = 1.f / Ls;
@@ -581,8 +558,7 @@ template <typename F>
 cudaError_t by_shape(const Geometry& g, int rows, F&& f) {
   auto mt = [&](auto tc, auto dc, auto rc) {
     if (rows <= 16) return f(tc, dc, std::integral_constant<int, 1>{}, rc);
-    if (rows <= 32) return f(tc, dc, std::integral_constant<int, 2>{}, rc);
-    return f(tc, dc, std::integral_constant<int, 4>{}, rc);
+    return f(tc, dc, std::integral_constant<int, 2>{}, rc);
   };
   auto rot = [&](auto tc, auto dc) { return g.rot > 0 ? mt(tc, dc, std::true_type{}) : mt(tc, dc, std::false_type{}); };
   auto dt = [&](auto dc) { return g.dtype == 1 ? rot(BF16T{}, dc) : rot(F16T{}, dc); };
@@ -602,11 +578,16 @@ cudaError_t by_shape(const Geometry& g, int rows, F&& f) {
 
 }  // namespace
 
-int prefix_rows(int group) { return group <= 16 ? 16 : group <= 32 ? 32 : 64; }
+int prefix_rows(int group) { return group <= 16 ? 16 : group <= 32 ? 32 : kPrefixTcRows; }
 
 cudaError_t prefix_ctas_per_sm(const Geometry& g, int device, int rows, int* occ) {
+  if (rows == kPrefixTcRows) {
+    *occ = 1;
+    return cudaSuccess;
+  }
   return by_shape(g, rows, [&](auto t, auto d, auto m, auto r) {
-    return prefix_occ<decltype(t), decltype(d)::value, decltype(m)::value, decltype(r)::value>(device, occ);
+    using T = decltype(t);
+    return prefix_occ<T, decltype(d)::value, decltype(m)::value, (decltype(r)::value ? kFullParts<T> : 1)>(device, occ);
   });
 }
 
@@ -615,21 +596,21 @@ cudaError_t launch_prefix(const Geometry& g, const PrefixArgs& a, int device, in
   return by_shape(g, rows, [&](auto t, auto d, auto m, auto r) {
     using T = decltype(t);
     constexpr int D = decltype(d)::value, MT = decltype(m)::value;
-    constexpr bool ROT = decltype(r)::value;
+    constexpr int NQ = decltype(r)::value ? kFullParts<T> : 1;
     int occ = 0;
-    const cudaError_t e = prefix_occ<T, D, MT, ROT>(device, &occ);  // sets the kernel's shared memory
+    const cudaError_t e = prefix_occ<T, D, MT, NQ>(device, &occ);  // sets the kernel's shared memory
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((int64_t)a.n_units * g.H * a.n_layers));
-    cfg.blockDim = dim3(PxCfg<D, MT, ROT>::THREADS);
-    cfg.dynamicSmemBytes = PxCfg<D, MT, ROT>::SMEM;
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = PxCfg<D, MT, NQ>::SMEM;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, prefix_kernel<T, D, MT, ROT>, a);
+    return cudaLaunchKernelEx(&cfg, prefix_kernel<T, D, MT, NQ>, a);
   });
 }
 

@@ -16,10 +16,12 @@
 // Mask: row i is visible to the query at stored row t exactly when i <= t <= hid(i), except that a <CL> query sees only
 // itself.
 //
-// Eight warps take S from TMEM (two buffers of 128 columns), 64 columns each, so that four warps per scheduler hide each
-// other's latencies (four warps a CTA, two per scheduler: 325 us on OPT-1.3B-shaped prompts); one loads the tiles and one
+// Eight warps take S from TMEM (two buffers of 128 columns), so that four warps per scheduler hide each other's latencies
+// (four warps a CTA, two per scheduler: 325 us on OPT-1.3B-shaped prompts): in pass 0 64 columns each, in pass 1 four of
+// them each step by turns, which leaves no barrier between all of them but one per key tile (64 columns each there too:
+// 216 us, and 119 for the window of 64 queries); one loads the tiles and one
 // issues the products.  A mask is a bit per column, looked at where a bit is missing.
-// Rotated queries come from a kernel of their own as a high and a low 16-bit part, each a product of its own.
+// Rotated queries come from a kernel of their own as two (f16) or three (bf16) 16-bit parts, each a product of its own.
 // What bounds it: the exponentials, two a visible pair, and the instructions around them.
 #include <cuda.h>
 
@@ -41,21 +43,26 @@ __device__ __forceinline__ void bar_sync(int id, int n) { asm volatile("bar.sync
 
 enum Pass { kLse = 0, kSumFew = 1, kSumMany = 2 };
 
-template <int D, bool LO, int PASS>
+template <int D, int NQ, int PASS>
 struct ScCfg {
   static constexpr int SW = (2 * D) % 128 == 0 ? 128 : (2 * D) % 64 == 0 ? 64 : 32;
   static constexpr int SUB = SW / 2;
   static constexpr int NSUB = D / SUB;
   static constexpr uint32_t SUBB = kRows * SW;
   static constexpr uint32_t TILE = kRows * D * 2;
-  static constexpr uint32_t QT = TILE * (LO ? 2 : 1);
-  // Stages: what two CTAs per SM leave room for, up to three; with two parts of the queries at 128 columns one CTA.
-  static constexpr uint32_t ROOM = 110 * 1024;
-  static constexpr int fit(uint32_t fixed, uint32_t each) {
-    return fixed + 3 * each <= ROOM ? 3 : 2;
+  static constexpr uint32_t QT = TILE * NQ;  // a query tile's parts
+  // Stages: as many as two CTAs per SM leave room for, three at most, and where fewer than `least` would be left as many
+  // as one CTA has room for.
+  static constexpr uint32_t ROOM = 110 * 1024, ALL = 220 * 1024;
+  static constexpr int fit(uint32_t fixed, uint32_t each, int least) {
+    for (int n = 3; n >= least; --n)
+      if (fixed + n * each <= ROOM) return n;
+    for (int n = 3; n > 1; --n)
+      if (fixed + n * each <= ALL) return n;
+    return 1;
   }
-  static constexpr int KS = PASS == kSumMany ? 1 : fit(QT, TILE);
-  static constexpr int QS = PASS == kSumMany ? fit(TILE, QT) : 1;
+  static constexpr int KS = PASS == kSumMany ? 1 : fit(QT, TILE, 2);
+  static constexpr int QS = PASS == kSumMany ? fit(TILE, QT, 1) : 1;
   static constexpr uint32_t Q_OFF = KS * TILE;
   static constexpr uint32_t NEED = Q_OFF + QS * QT + 1024;  // + aligning the base
   // no third CTA on an SM, which would wait for columns of TMEM
@@ -64,11 +71,11 @@ struct ScCfg {
   static_assert(SMEM <= 227 * 1024, "shared memory");
 };
 
-template <typename T, int D, bool LO, int PASS>
-__global__ void __launch_bounds__(kScThreads, ScCfg<D, LO, PASS>::CPS)
+template <typename T, int D, int NQ, int PASS>
+__global__ void __launch_bounds__(kScThreads, ScCfg<D, NQ, PASS>::CPS)
     score_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mq,
-                 const __grid_constant__ CUtensorMap mql, const ScoreArgs a) {
-  using Cf = ScCfg<D, LO, PASS>;
+                 const __grid_constant__ CUtensorMap mq1, const __grid_constant__ CUtensorMap mq2, const ScoreArgs a) {
+  using Cf = ScCfg<D, NQ, PASS>;
   constexpr int KS = Cf::KS, QS = Cf::QS;
   extern __shared__ unsigned char raw[];
   __shared__ __align__(8) uint64_t k_full[KS], k_empty[KS], q_full[QS], q_empty[QS], s_full[2], s_empty[2];
@@ -95,7 +102,7 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, LO, PASS>::CPS)
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&s_full[i], 1);
-      mbar_init(&s_empty[i], kSThreads);
+      mbar_init(&s_empty[i], PASS == kLse ? kSThreads : kSThreads / 2);
     }
     fence_mbar_init();
   }
@@ -107,7 +114,7 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, LO, PASS>::CPS)
   const uint32_t tmem = tmem_slot;
   const int item = (int)(blockIdx.x / (unsigned)a.H), h = (int)(blockIdx.x - (unsigned)item * a.H);
   const ScoreUnit un = a.units[item];
-  const ScoreSeq sq = a.seqs[un.seq];
+  const ScoreSeq& sq = un.q;
   const int nqt = (sq.len - sq.q0 + kRows - 1) / kRows;
   // the query tiles of key tile kt: those that end at or after its first row
   auto first_qt = [&](int kt) { return PASS == kLse ? un.qt : kt * kRows <= sq.q0 ? 0 : (kt * kRows - sq.q0) / kRows; };
@@ -134,8 +141,10 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, LO, PASS>::CPS)
           const uint32_t dst = sm + Cf::Q_OFF + qs * Cf::QT;
 #pragma unroll
           for (int i = 0; i < Cf::NSUB; ++i) {
-            tma_load_3d(dst + i * Cf::SUBB, &mq, i * Cf::SUB, h, sq.tok0 + qt * kRows, &q_full[qs]);
-            if constexpr (LO) tma_load_3d(dst + Cf::TILE + i * Cf::SUBB, &mql, i * Cf::SUB, h, sq.tok0 + qt * kRows, &q_full[qs]);
+            const int x = i * Cf::SUB, z = sq.tok0 + qt * kRows;
+            tma_load_3d(dst + i * Cf::SUBB, &mq, x, h, z, &q_full[qs]);
+            if constexpr (NQ > 1) tma_load_3d(dst + Cf::TILE + i * Cf::SUBB, &mq1, x, h, z, &q_full[qs]);
+            if constexpr (NQ > 2) tma_load_3d(dst + 2 * Cf::TILE + i * Cf::SUBB, &mq2, x, h, z, &q_full[qs]);
           }
           ++nq;
         }
@@ -166,7 +175,7 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, LO, PASS>::CPS)
         const uint32_t q_d = desc_lo(sm + Cf::Q_OFF + qs * Cf::QT, 16);
         if (elect_one()) {
 #pragma unroll
-          for (int part = 0; part < (LO ? 2 : 1); ++part) {
+          for (int part = 0; part < NQ; ++part) {
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk) {
               const uint32_t off = ((kk * 16) / Cf::SUB * Cf::SUBB + (kk * 16) % Cf::SUB * 2) >> 4;
@@ -184,25 +193,25 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, LO, PASS>::CPS)
     }
   } else {
     // ---------------- S ----------------
-    const int half = warp >> 2;                      // columns [64 half, 64 half + 64)
-    const int r = (warp & 3) * 32 + lane;            // the thread's row of S (its TMEM lane)
-    const uint32_t my = tmem + ((uint32_t)((warp & 3) * 32) << 16) + half * 64;
+    const int half = warp >> 2;
+    const int r = (warp & 3) * 32 + lane;  // the thread's row of S (its TMEM lane)
+    const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
     const float2 cc = make_float2(a.c2, a.c2);
-    uint32_t step = 0;
     float s[64];
-    // S of the next step into registers, its columns of TMEM free again
-    auto take = [&]() -> bool {
+    auto s_wait = [&](uint32_t step) -> bool {
       const bool got = __all_sync(0xFFFFFFFFu, pf_wait(&s_full[step & 1], step / 2 & 1, limit_ns));
       tc_fence_after();
-      if (got) {
-        tmem_ld32(my + (step & 1) * kRows, s);
-        tmem_ld32(my + (step & 1) * kRows + 32, s + 32);
-        tmem_wait_ld();
-      }
+      return got;
+    };
+    // columns [c, c + 64) of the step's S into registers
+    auto take = [&](uint32_t step, int c) {
+      tmem_ld32(lanes + (step & 1) * kRows + c, s);
+      tmem_ld32(lanes + (step & 1) * kRows + c + 32, s + 32);
+      tmem_wait_ld();
+    };
+    auto s_done = [&](uint32_t step) {
       tc_fence_before();
       mbar_arrive(&s_empty[step & 1]);
-      ++step;
-      return got;
     };
     // the columns whose bit is missing
     auto hide = [&](uint32_t v0, uint32_t v1) {
@@ -240,7 +249,10 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, LO, PASS>::CPS)
           v0 &= low_bits(t - i0 + 1);
           v1 &= low_bits(t - i0 - 31);
         }
-        if (!(ok = take())) break;
+        const uint32_t step = kt - un.kt0;
+        if (!(ok = s_wait(step))) break;
+        take(step, half * 64);
+        s_done(step);
         if (idle || !__any_sync(0xFFFFFFFFu, v0 | v1)) continue;
         hide(v0, v1);
         float mx[4] = {s[0], s[1], s[2], s[3]};
@@ -287,59 +299,70 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, LO, PASS>::CPS)
         return -(M + log2f(L));
       };
       pdl_wait();  // the queries' sums
-      float next = half ? 0.f : neg_lse(first_qt(un.kt0));
+      // The steps go to the halves by turns (a half's steps all have the same buffer of S).
+      auto mine = [&](uint32_t step) { return (int)(step & 1) == half; };
+      auto load_neg = [&](float neg) {  // for the half's next step; its threads are done with the last one's
+        bar_sync(1 + half, kSThreads / 2);
+        s_neg[half][r] = neg;
+        const uint32_t none = __ballot_sync(0xFFFFFFFFu, neg == -INFINITY);
+        if (lane == 0) s_none[half][warp & 3] = none;
+        bar_sync(1 + half, kSThreads / 2);
+      };
+      if (PASS == kSumFew) load_neg(neg_lse(0));
+      uint32_t step = 0;
       for (int kt = un.kt0; kt < un.kt1; ++kt) {
         const int i = kt * kRows + r;
         const bool row = i < sq.len;
         const int meta = row ? a.meta[sq.moff + i] : 0, hid = meta >> 1;
         float total = 0.f;
+        bool any = false;  // the half had a step of this key tile
+        [[maybe_unused]] float next = 0.f;
         const int qe = end_qt();
-        for (int qt = first_qt(kt); qt < qe; ++qt) {
-          const int t0 = sq.q0 + qt * kRows, t1 = min(t0 + kRows, sq.len), buf = step & 1;
-          if (!half) {
-            s_neg[buf][r] = next;
-            const uint32_t none = __ballot_sync(0xFFFFFFFFu, next == -INFINITY);
-            if (lane == 0) s_none[buf][warp] = none;
+        for (int qt = first_qt(kt); qt < qe; ++qt, ++step) {
+          if (!mine(step)) continue;
+          if (PASS == kSumMany) {
+            load_neg(any ? next : neg_lse(qt));
+            if (qt + 2 < qe) next = neg_lse(qt + 2);
           }
-          bar_sync(1, kSThreads);
-          if (!half && PASS == kSumMany) {  // the next step's
-            if (qt + 1 < qe)
-              next = neg_lse(qt + 1);
-            else if (kt + 1 < un.kt1)
-              next = neg_lse(first_qt(kt + 1));
-          }
-          // the columns that see row i
-          const int lo = max(i - t0, 0) - half * 64, hi = (row ? min(hid, t1 - 1) - t0 : -1) - half * 64;
-          const uint32_t v0 = low_bits(hi + 1) & ~low_bits(lo) & ~s_none[buf][2 * half];
-          const uint32_t v1 = low_bits(hi - 31) & ~low_bits(lo - 32) & ~s_none[buf][2 * half + 1];
+          any = true;
+          const int t0 = sq.q0 + qt * kRows, t1 = min(t0 + kRows, sq.len);
           // after a wait that ran out the warp only keeps up with the others' barriers
-          if (!ok) {
-            ++step;
-            continue;
-          }
-          if (!(ok = take())) continue;
-          if (!__any_sync(0xFFFFFFFFu, v0 | v1)) continue;
-          hide(v0, v1);
-          const float4* neg = reinterpret_cast<const float4*>(s_neg[buf] + half * 64);
-          float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
+          if (!ok || !(ok = s_wait(step))) continue;
+          const int lo = max(i - t0, 0), hi = row ? min(hid, t1 - 1) - t0 : -1;  // the columns that see row i
+#pragma unroll 1
+          for (int c = 0; c < kRows; c += 64) {
+            const uint32_t v0 = low_bits(hi + 1 - c) & ~low_bits(lo - c) & ~s_none[half][c / 32];
+            const uint32_t v1 = low_bits(hi - 31 - c) & ~low_bits(lo - 32 - c) & ~s_none[half][c / 32 + 1];
+            const bool seen = __any_sync(0xFFFFFFFFu, v0 | v1);
+            if (seen) take(step, c);
+            if (c == 64) s_done(step);
+            if (!seen) continue;
+            hide(v0, v1);
+            const float4* neg = reinterpret_cast<const float4*>(s_neg[half] + c);
+            float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
 #pragma unroll
-          for (int x = 0; x < 64; x += 4) {
-            const float4 n = neg[x / 4];
-            const float2 z0 = __ffma2_rn(make_float2(s[x], s[x + 1]), cc, make_float2(n.x, n.y));
-            const float2 z1 = __ffma2_rn(make_float2(s[x + 2], s[x + 3]), cc, make_float2(n.z, n.w));
-            sum0 = __fadd2_rn(sum0, make_float2(ex2(z0.x), ex2(z0.y)));
-            sum1 = __fadd2_rn(sum1, make_float2(ex2(z1.x), ex2(z1.y)));
+            for (int x = 0; x < 64; x += 4) {
+              const float4 n = neg[x / 4];
+              const float2 z0 = __ffma2_rn(make_float2(s[x], s[x + 1]), cc, make_float2(n.x, n.y));
+              const float2 z1 = __ffma2_rn(make_float2(s[x + 2], s[x + 3]), cc, make_float2(n.z, n.w));
+              sum0 = __fadd2_rn(sum0, make_float2(ex2(z0.x), ex2(z0.y)));
+              sum1 = __fadd2_rn(sum1, make_float2(ex2(z1.x), ex2(z1.y)));
+            }
+            total += (sum0.x + sum0.y) + (sum1.x + sum1.y);
           }
-          total += (sum0.x + sum0.y) + (sum1.x + sum1.y);
         }
-        if (half) s_half[r].x = total;
-        bar_sync(1, kSThreads);
-        if (!half && ok && row) {
-          total += s_half[r].x;
+        if (PASS == kSumMany) {  // a key tile's steps are of both halves: the first adds them up
+          if (half) s_half[r].x = total;
+          bar_sync(3, kSThreads);
+          if (!half) total += s_half[r].x;
+          any = !half;
+        }
+        if (any && ok && row) {
           if ((meta & 1) && i >= sq.q0) total += 1.f;  // a <CL> query's weight is its own row's
           float* sc = a.scores + ((int64_t)a.layer * a.H * a.C + sq.row0 + (int64_t)h * sq.cap + i);
           *sc += total;
         }
+        if (PASS == kSumMany && kt + 1 < un.kt1) bar_sync(3, kSThreads);  // s_half is read
       }
     }
   }
@@ -352,63 +375,41 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, LO, PASS>::CPS)
   }
 }
 
-// The queries of a 128-query tile (blockIdx.x), rotated at their positions, as high and low parts.
+// The queries of a 128-query tile (blockIdx.x), rotated at their positions, in parts.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) score_rotate_kernel(const ScoreArgs a) {
-  constexpr int CH = D / 8;
+  constexpr int CH = D / 8, NQ = kFullParts<T>;
   const ScoreUnit un = a.units[blockIdx.x];
   if (un.split != 0) return;
-  const ScoreSeq sq = a.seqs[un.seq];
+  const ScoreSeq& sq = un.q;
   const int n = min(kRows, sq.len - sq.q0 - un.qt * kRows);
-  const int half = a.rot / 2;
   for (int x = blockIdx.y * 256 + threadIdx.x; x < n * a.H * CH; x += gridDim.y * 256) {
     const int r = x / (a.H * CH), w = x - r * (a.H * CH), c = w % CH;
-    const int64_t at = ((int64_t)(sq.tok0 + un.qt * kRows + r) * a.H * D) + w * 8;
-    uint4 hi = *reinterpret_cast<const uint4*>(a.q + at), lo = make_uint4(0, 0, 0, 0);
-    if (c * 8 < a.rot) {
-      const bool first = c * 8 < half;  // half is a multiple of eight
-      const uint4 other = *reinterpret_cast<const uint4*>(a.q + at + (first ? half : -half));
-      const int32_t pos = a.pos[a.off[sq.s] + sq.q0 + un.qt * kRows + r];
-      const uint32_t p[4] = {hi.x, hi.y, hi.z, hi.w}, o[4] = {other.x, other.y, other.z, other.w};
-      uint32_t vh[4], vl[4];
+    const int64_t row = ((int64_t)(sq.tok0 + un.qt * kRows + r) * a.H + w / CH) * D;
+    uint32_t part[NQ][4];
+    query_chunk<T, NQ>(a.q + row, c, a.rot, a.pos[a.off[sq.s] + sq.q0 + un.qt * kRows + r], a.rope_g, part);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float2 x2 = T::f2(p[e]), y2 = T::f2(o[e]);
-        const int i = (first ? c * 8 : c * 8 - half) + 2 * e;
-        float sn0, cs0, sn1, cs1;
-        rope_sincos_full(pos, a.rope_g[i], &sn0, &cs0);
-        rope_sincos_full(pos, a.rope_g[i + 1], &sn1, &cs1);
-        const float z0 = first ? x2.x * cs0 - y2.x * sn0 : x2.x * cs0 + y2.x * sn0;
-        const float z1 = first ? x2.y * cs1 - y2.y * sn1 : x2.y * cs1 + y2.y * sn1;
-        vh[e] = Pack16<T>::two(z0, z1);
-        const float2 back = T::f2(vh[e]);
-        vl[e] = Pack16<T>::two(z0 - back.x, z1 - back.y);
-      }
-      hi = make_uint4(vh[0], vh[1], vh[2], vh[3]);
-      lo = make_uint4(vl[0], vl[1], vl[2], vl[3]);
-    }
-    *reinterpret_cast<uint4*>(a.q_hi + at) = hi;
-    *reinterpret_cast<uint4*>(a.q_lo + at) = lo;
+    for (int i = 0; i < NQ; ++i)
+      *reinterpret_cast<uint4*>(a.q_part + i * a.part_stride + row + c * 8) = make_uint4(part[i][0], part[i][1], part[i][2], part[i][3]);
   }
 }
 
-template <typename T, int D, bool LO, int PASS>
+template <typename T, int D, int NQ, int PASS>
 cudaError_t launch_score_t(const ScoreMaps& maps, const ScoreArgs& a, cudaStream_t stream) {
-  using Cf = ScCfg<D, LO, PASS>;
+  using Cf = ScCfg<D, NQ, PASS>;
   static std::atomic<bool> done[64];
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
   if (!done[dev].load(std::memory_order_acquire)) {
-    e = cudaFuncSetAttribute(score_kernel<T, D, LO, PASS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cf::SMEM);
+    e = cudaFuncSetAttribute(score_kernel<T, D, NQ, PASS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cf::SMEM);
     if (e != cudaSuccess) return e;
     done[dev].store(true, std::memory_order_release);
   }
-  CUtensorMap mk, mq, ml;
+  CUtensorMap mk, mq[3];
   std::memcpy(&mk, maps.k, sizeof mk);
-  std::memcpy(&mq, maps.q, sizeof mq);
-  std::memcpy(&ml, maps.q_lo, sizeof ml);
+  for (int i = 0; i < 3; ++i) std::memcpy(&mq[i], maps.q[i < NQ ? i : 0], sizeof mq[i]);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)((int64_t)a.n_units * a.H));
   cfg.blockDim = dim3(kScThreads);
@@ -419,7 +420,7 @@ cudaError_t launch_score_t(const ScoreMaps& maps, const ScoreArgs& a, cudaStream
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = PASS == kLse ? 0 : 1;  // the first pass starts when all before it is complete
-  return cudaLaunchKernelEx(&cfg, score_kernel<T, D, LO, PASS>, mk, mq, ml, a);
+  return cudaLaunchKernelEx(&cfg, score_kernel<T, D, NQ, PASS>, mk, mq[0], mq[1], mq[2], a);
 }
 
 template <typename F>
@@ -445,13 +446,24 @@ cudaError_t launch_pass(const Geometry& g, const ScoreMaps& maps, const ScoreArg
   return by_type(g, [&](auto t, auto d) {
     using T = decltype(t);
     constexpr int D = decltype(d)::value;
-    return g.rot > 0 ? launch_score_t<T, D, true, PASS>(maps, a, stream) : launch_score_t<T, D, false, PASS>(maps, a, stream);
+    return g.rot > 0 ? launch_score_t<T, D, kFullParts<T>, PASS>(maps, a, stream) : launch_score_t<T, D, 1, PASS>(maps, a, stream);
   });
 }
 
 }  // namespace
 
-int score_ctas_per_sm(int D, bool rot) { return rot && D == 128 ? 1 : 2; }
+int score_parts(const Geometry& g) { return g.rot == 0 ? 1 : g.dtype == 1 ? kFullParts<BF16T> : kFullParts<F16T>; }
+
+int score_ctas_per_sm(const Geometry& g) {
+  int n = 1;
+  (void)by_type(g, [&](auto t, auto d) {
+    using T = decltype(t);
+    constexpr int D = decltype(d)::value;
+    n = g.rot > 0 ? ScCfg<D, kFullParts<T>, kLse>::CPS : ScCfg<D, 1, kLse>::CPS;
+    return cudaSuccess;
+  });
+  return n;
+}
 
 cudaError_t launch_score_rotate(const Geometry& g, const ScoreArgs& a, cudaStream_t stream) {
   if (a.n_units <= 0) return cudaSuccess;
