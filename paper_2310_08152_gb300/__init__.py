@@ -77,9 +77,9 @@ def _per_seq(a, b: int, name: str):
     a = np.asarray(a, dtype=np.int64)
     if a.ndim == 0:
         return np.full(b, a, np.int64)
-    if a.shape != (b,):
+    if a.size != b:
         raise ValueError(f"{name} must be a number or have {b} elements, got shape {a.shape}")
-    return np.ascontiguousarray(a)
+    return np.ascontiguousarray(a).reshape(b)
 
 
 def _dev(t, name, dtype=None, numel=None):
@@ -607,9 +607,9 @@ class KVCache:
         import torch
 
         n_q = _np(n_q, np.int32)
-        if n_q.shape != (self.b,):
+        if n_q.size != self.b:
             raise ValueError(f"n_q must have {self.b} elements, got shape {n_q.shape}")
-        _dev(q, "q", self.torch_dtype, int(np.add.reduce(n_q)) * self.H * self.d)
+        _dev(q, "q", self.torch_dtype, int(np.add.reduce(n_q, axis=None)) * self.H * self.d)
         counts = n_q.tobytes()
         if counts != self._score_counts:
             need = kvc_score_scratch_bytes(self.handle, n_q)
@@ -644,8 +644,8 @@ class KVCache:
             kvc_set_prefix(self.handle, None, None, None)
             self.prefix = self._prefix_scratch = None
             return
-        parent = np.asarray(parent, np.int32)
-        if parent.shape != (self.b,):
+        parent = _np(parent, np.int32)
+        if parent.size != self.b:
             raise ValueError(f"parent must have {self.b} elements, got shape {parent.shape}")
         scratch = torch.empty(kvc_prefix_scratch_bytes(self.handle, prefix.handle), dtype=torch.uint8, device=self.k.device)
         kvc_set_prefix(self.handle, prefix.handle, parent, scratch)
@@ -654,6 +654,8 @@ class KVCache:
     def decode_attention_shared(self, q, scale: float, out=None, stream=None, first: int = 0, n_layers=None):
         """Decode attention of layers [first, first + n_layers) over each sequence's prefix and its own rows: q and out
         [n_layers][b][H][d_head]; every layer from `first` on unless n_layers is given."""
+        if self.prefix is not None and not self.prefix.handle:
+            raise KvcError(5, "the prefix's cache is closed")
         n_layers, out = self._layers(q, out, first, n_layers)
         n = self.b * self.H * self.d
         kvc_decode_attention_shared(self.handle, first, n_layers, q, n, scale, out, n, stream)

@@ -30,9 +30,6 @@ namespace kvc {
 namespace {
 
 constexpr unsigned kFull = 0xFFFFFFFFu;
-constexpr int kThreads = 128;
-constexpr int kWarps = kThreads / 32;
-constexpr int kScan = 4 * kThreads;  // candidates of one scan step
 constexpr int kBins = 2048;
 constexpr int kMaxHeldKeys = 40 * 1024;  // candidates whose keys stay in shared memory (160 KB); else they are read again
 constexpr int kMaxCluster = 8;
@@ -54,7 +51,10 @@ __device__ __forceinline__ void bulk_s2g(void* dst, const void* src, uint32_t by
                : "memory");
 }
 
+template <int kThreads>
 struct EvictShared {
+  static constexpr int kWarps = kThreads / 32;
+  static constexpr int kScan = 4 * kThreads;  // candidates of one scan step
   union {
     uint32_t hist[kBins];
     struct {
@@ -69,7 +69,9 @@ struct EvictShared {
 };
 
 // Exclusive prefix of one value per thread over the block, and the block's sum (two barriers).
-__device__ __forceinline__ uint32_t block_scan(uint32_t v, EvictShared& sh, uint32_t* sum) {
+template <int kThreads>
+__device__ __forceinline__ uint32_t block_scan(uint32_t v, EvictShared<kThreads>& sh, uint32_t* sum) {
+  constexpr int kWarps = kThreads / 32;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   uint32_t incl = v;
 #pragma unroll
@@ -93,8 +95,8 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, EvictShared& sh, uint
 
 // IMG: the call's upload is a parameter (of img_bytes, its AffSeqs from aff_off on), which the first CTA stores at dyn.
 struct NoImage {};
-template <int D, bool IMG>
-__global__ void __launch_bounds__(kThreads, 7)
+template <int D, int kThreads, bool IMG>
+__global__ void __launch_bounds__(kThreads, kThreads == 128 ? 7 : 1024 / kThreads)
     evict_kernel(Geometry g, Static st, Buffers buf, float* __restrict__ scores, const AffSeq* __restrict__ aff_,
                  int32_t* __restrict__ kept, int held, int chunk, int CN,
                  const __grid_constant__ std::conditional_t<IMG, AppendImage, NoImage> img, int img_bytes, int aff_off,
@@ -109,7 +111,8 @@ __global__ void __launch_bounds__(kThreads, 7)
   extern __shared__ __align__(128) unsigned char dyn[];
   // `chunk` recent rows of K and then of V (of one of them in a cluster), then the keys
   uint32_t* keys = reinterpret_cast<uint32_t*>(dyn + (size_t)chunk * (CN > 1 ? 1 : 2) * D * 2);
-  __shared__ EvictShared sh;
+  __shared__ EvictShared<kThreads> sh;
+  constexpr int kWarps = EvictShared<kThreads>::kWarps, kScan = EvictShared<kThreads>::kScan;
   const int tid = threadIdx.x;
   const int rank = CN > 1 ? (int)(blockIdx.x % (unsigned)CN) : 0;
   const int unit = CN > 1 ? (int)(blockIdx.x / (unsigned)CN) : (int)blockIdx.x;
@@ -141,7 +144,7 @@ __global__ void __launch_bounds__(kThreads, 7)
 
   // Moves the rows of the first n_hole entries of the lists.
   auto move = [&](int n_hole) {
-    constexpr int U = 2;
+    constexpr int U = kThreads == 128 ? 2 : 4;
     const int step = CN * kThreads, total = n_hole * VPR;
     for (int v0 = rank * kThreads + tid; v0 < total; v0 += U * step) {
       uint4 k[U], v[U];
@@ -395,7 +398,7 @@ __global__ void __launch_bounds__(kThreads, 7)
   }
 }
 
-template <int D, bool IMG>
+template <int D, int NT, bool IMG>
 cudaError_t launch_evict_t(const Geometry& g, const Static& st, const Buffers& buf, float* scores, const AffSeq* aff,
                            int n_aff, int64_t max_cand, int64_t max_recent, int32_t* kept, int num_sms,
                            const EvictImage* image, cudaStream_t stream) {
@@ -406,7 +409,7 @@ cudaError_t launch_evict_t(const Geometry& g, const Static& st, const Buffers& b
   if (e != cudaSuccess) return e;
   if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
   if (!done[dev].load(std::memory_order_acquire)) {
-    e = cudaFuncSetAttribute(evict_kernel<D, IMG>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+    e = cudaFuncSetAttribute(evict_kernel<D, NT, IMG>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
     if (e != cudaSuccess) return e;
     done[dev].store(true, std::memory_order_release);
   }
@@ -416,13 +419,13 @@ cudaError_t launch_evict_t(const Geometry& g, const Static& st, const Buffers& b
   int cn = 1;
   if (max_cand <= kMaxHeldKeys)
     while (2 * cn <= kMaxCluster && 2 * cn * units <= 2 * num_sms) cn *= 2;
-  // recent rows of a chunk: 16 KB of K and V, which leaves room for seven CTAs per SM
-  const int chunk = (int)std::min<int64_t>(max_recent, (cn > 1 ? 16 : 8) * 1024 / (D * 2));
+  // recent rows of a chunk: 16 KB of K and V, which leaves room for seven CTAs of 128 threads per SM, or 24 KB
+  const int chunk = (int)std::min<int64_t>(max_recent, (cn > 1 ? 2 : 1) * (NT == 128 ? 8 : 12) * 1024 / (D * 2));
   const size_t smem = (size_t)chunk * (cn > 1 ? 1 : 2) * D * 2 + 4 * (size_t)held;
   static_assert(32 * 1024 + 4 * kMaxHeldKeys <= kMost, "shared memory");
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(units * cn));
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(NT);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
@@ -433,24 +436,33 @@ cudaError_t launch_evict_t(const Geometry& g, const Static& st, const Buffers& b
   cfg.attrs = attr;
   cfg.numAttrs = cn > 1 ? 1 : 0;
   if constexpr (IMG)
-    return cudaLaunchKernelEx(&cfg, evict_kernel<D, IMG>, g, st, buf, scores, aff, kept, held, chunk, cn, *image->img,
+    return cudaLaunchKernelEx(&cfg, evict_kernel<D, NT, IMG>, g, st, buf, scores, aff, kept, held, chunk, cn, *image->img,
                               image->bytes, image->aff_off, static_cast<uint4*>(image->dyn));
   else
-    return cudaLaunchKernelEx(&cfg, evict_kernel<D, IMG>, g, st, buf, scores, aff, kept, held, chunk, cn, NoImage{}, 0, 0,
+    return cudaLaunchKernelEx(&cfg, evict_kernel<D, NT, IMG>, g, st, buf, scores, aff, kept, held, chunk, cn, NoImage{}, 0, 0,
                               static_cast<uint4*>(nullptr));
 }
 
 }  // namespace
 
 cudaError_t launch_evict(const Geometry& g, const Static& st, const Buffers& buf, float* scores, const AffSeq* aff,
-                         int n_aff, int64_t max_cand, int64_t max_recent, int32_t* kept, int num_sms,
-                         const EvictImage* image, cudaStream_t stream) {
+                         int n_aff, int64_t max_cand, int64_t max_recent, int64_t max_drop, int32_t* kept,
+                         int num_sms, const EvictImage* image, cudaStream_t stream) {
   if (n_aff <= 0) return cudaSuccess;
   auto go = [&](auto d) {
     constexpr int D = decltype(d)::value;
-    return image != nullptr
-               ? launch_evict_t<D, true>(g, st, buf, scores, aff, n_aff, max_cand, max_recent, kept, num_sms, image, stream)
-               : launch_evict_t<D, false>(g, st, buf, scores, aff, n_aff, max_cand, max_recent, kept, num_sms, image, stream);
+    // Threads by the candidates, where more than a few go.  us with 128 / 256 / 512 threads: 12,288 streams of 960, 64 of
+    // them, 244 / 264 / -; 2,048 of 1,592, 256 of them, 129 / 119 / 141; 1,024 of 1,984, 1,536 of them, 77 / 55 / 62;
+    // 1,024 of 4,436, 500 of them, 149 / 127 / 115.  A few: 12,288 of 897, one of them, 147 / 174 / -.
+    auto by = [&](auto nt) {
+      constexpr int NT = decltype(nt)::value;
+      return image != nullptr ? launch_evict_t<D, NT, true>(g, st, buf, scores, aff, n_aff, max_cand, max_recent, kept,
+                                                            num_sms, image, stream)
+                              : launch_evict_t<D, NT, false>(g, st, buf, scores, aff, n_aff, max_cand, max_recent, kept,
+                                                             num_sms, image, stream);
+    };
+    if (max_drop <= kFewDrops || max_cand <= 1280) return by(std::integral_constant<int, 128>{});
+    return max_cand <= 3000 ? by(std::integral_constant<int, 256>{}) : by(std::integral_constant<int, 512>{});
   };
   switch (g.D) {
     case 64:

@@ -193,8 +193,8 @@ cudaError_t launch_compact_scores(const Geometry& g, const Static& st, float* sc
                                   const int32_t* src_map, cudaStream_t stream);
 
 // Eviction (evict.cu): in every (layer, head) stream of the n_aff sequences, len_new of len_old rows stay, the last
-// `first_row` of them (the recent ones) and those with the largest scores.  max_cand, max_recent: the most candidates and
-// recent rows of a stream; kept: [M][H * C] or NULL, the earlier row number of each kept row.
+// `first_row` of them (the recent ones) and those with the largest scores.  max_cand, max_recent, max_drop: the most
+// candidates, recent rows and rows that go of a stream; kept: [M][H * C] or NULL, the earlier row number of each kept row.
 // image: the call's upload (state and AffSeqs) as a kernel parameter, where it fits one, stored at dyn by the kernel
 // (an eviction of two sequences in two layers: an upload and its event less, 23 us of host time before); else NULL.
 struct EvictImage {
@@ -203,8 +203,8 @@ struct EvictImage {
   void* dyn;
 };
 cudaError_t launch_evict(const Geometry& g, const Static& st, const Buffers& buf, float* scores, const AffSeq* aff,
-                         int n_aff, int64_t max_cand, int64_t max_recent, int32_t* kept, int num_sms,
-                         const EvictImage* image, cudaStream_t stream);
+                         int n_aff, int64_t max_cand, int64_t max_recent, int64_t max_drop, int32_t* kept,
+                         int num_sms, const EvictImage* image, cudaStream_t stream);
 
 // ---------------------------------------------------------------------------------------------
 // Masked prefill attention (prefill.cu)

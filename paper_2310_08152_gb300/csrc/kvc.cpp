@@ -11,6 +11,7 @@
 #include <cstdio>
 #include <cstring>
 #include <deque>
+#include <exception>
 #include <new>
 #include <string>
 #include <vector>
@@ -39,6 +40,16 @@ kvc_status ok() {
 
 kvc_status cuda_fail(cudaError_t e, const char* what) {
   return fail(KVC_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
+}
+
+// Runs an entry point's body; an allocation that fails comes back as a status.
+template <typename F>
+kvc_status guarded(F&& body) {
+  try {
+    return body();
+  } catch (const std::exception&) {  // bad_alloc or length_error of a container
+    return KVC_ERR_NO_MEMORY;
+  }
 }
 
 constexpr double kPi = 3.14159265358979323846;
@@ -578,16 +589,18 @@ kvc_status kvc_book_compress(kvc_book* book, const int32_t* seq, const int64_t* 
 }
 
 kvc_status kvc_book_evict(kvc_book* book, const int64_t* keep, const int64_t* recent) {
-  if (!book) return fail(KVC_ERR_INVALID_ARG, "book is NULL");
-  if (!keep || !recent) return fail(KVC_ERR_INVALID_ARG, "keep/recent are NULL");
-  if (book->book.policy() == kvc::POLICY_LOCAL)
-    return fail(KVC_ERR_UNSUPPORTED, "the local-attention cache keeps a window; nothing is evicted from it");
-  std::vector<kvc::EvictSeq> plan;
-  std::string err;
-  int code = 0;
-  if (!book->book.plan_evict(keep, recent, plan, err, code)) return fail((kvc_status)code, "%s", err.c_str());
-  book->book.apply_evict(plan);
-  return ok();
+  return guarded([&]() -> kvc_status {
+    if (!book) return fail(KVC_ERR_INVALID_ARG, "book is NULL");
+    if (!keep || !recent) return fail(KVC_ERR_INVALID_ARG, "keep/recent are NULL");
+    if (book->book.policy() == kvc::POLICY_LOCAL)
+      return fail(KVC_ERR_UNSUPPORTED, "the local-attention cache keeps a window; nothing is evicted from it");
+    std::vector<kvc::EvictSeq> plan;
+    std::string err;
+    int code = 0;
+    if (!book->book.plan_evict(keep, recent, plan, err, code)) return fail((kvc_status)code, "%s", err.c_str());
+    book->book.apply_evict(plan);
+    return ok();
+  });
 }
 
 kvc_status kvc_book_pending_spans(const kvc_book* book, int seq, int64_t* cl, int64_t* cr, int64_t max, int64_t* n) {
@@ -1085,23 +1098,25 @@ static kvc_status layers_check(kvc_cache* c, int first, int n_layers, const void
 
 kvc_status kvc_decode_attention_scored(kvc_cache* c, int first, int n_layers, const void* q, int64_t q_layer_stride,
                                        float scale, float* out, int64_t out_layer_stride, void* stream_) {
-  kvc_status st = layers_check(c, first, n_layers, q, q_layer_stride, scale, out, out_layer_stride);
-  if (st != KVC_OK) return st;
-  if (!c->scores) return fail(KVC_ERR_STATE, "the cache has no scores (kvc_set_scores)");
-  cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-  st = c->ensure_cuda(stream);
-  if (st != KVC_OK) return st;
-  kvc::DecodeArgs a = decode_args(c, first, q, scale, out);
-  a.n_layers = n_layers;
-  a.q_layer_stride = q_layer_stride;
-  a.out_layer_stride = out_layer_stride;
-  int grid = 0;
-  const cudaError_t e =
-      kvc::launch_decode_scored(c->geom(), c->stat(), c->bufs(), a, c->scores, c->num_sms, stream, &grid, &c->last_plan);
-  if (e != cudaSuccess) return cuda_fail(e, "scored decode kernel");
-  c->launches += grid > 0 ? 1 : 0;
-  c->last_was_decode = true;
-  return ok();
+  return guarded([&]() -> kvc_status {
+    kvc_status st = layers_check(c, first, n_layers, q, q_layer_stride, scale, out, out_layer_stride);
+    if (st != KVC_OK) return st;
+    if (!c->scores) return fail(KVC_ERR_STATE, "the cache has no scores (kvc_set_scores)");
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    st = c->ensure_cuda(stream);
+    if (st != KVC_OK) return st;
+    kvc::DecodeArgs a = decode_args(c, first, q, scale, out);
+    a.n_layers = n_layers;
+    a.q_layer_stride = q_layer_stride;
+    a.out_layer_stride = out_layer_stride;
+    int grid = 0;
+    const cudaError_t e =
+        kvc::launch_decode_scored(c->geom(), c->stat(), c->bufs(), a, c->scores, c->num_sms, stream, &grid, &c->last_plan);
+    if (e != cudaSuccess) return cuda_fail(e, "scored decode kernel");
+    c->launches += grid > 0 ? 1 : 0;
+    c->last_was_decode = true;
+    return ok();
+  });
 }
 
 // Parts that the keys of each query tile are cut into in the first pass of a prompt's scores: enough for two waves, of two
@@ -1187,9 +1202,13 @@ static kvc_status plan_score(kvc_cache* c, const int32_t* n_q, int n_split, cuda
   // the second pass begins with the keys that the first read last, which are in L2; or the longest first: the first pass's
   // by their key tiles, the second's by the query tiles that see them
   if (few) std::reverse(u1.begin(), u1.end());
-  if (!few) std::stable_sort(u0.begin(), u0.end(), [](const kvc::ScoreUnit& x, const kvc::ScoreUnit& y) { return x.kt1 - x.kt0 > y.kt1 - y.kt0; });
+  if (!few)
+    std::stable_sort(u0.begin(), u0.end(),
+                     [](const kvc::ScoreUnit& x, const kvc::ScoreUnit& y) { return x.kt1 - x.kt0 > y.kt1 - y.kt0; });
   auto q_tiles = [](const kvc::ScoreUnit& u) { return u.q.len - std::max(u.q.q0, u.kt0 * 128); };
-  if (!few) std::stable_sort(u1.begin(), u1.end(), [q_tiles](const kvc::ScoreUnit& x, const kvc::ScoreUnit& y) { return q_tiles(x) > q_tiles(y); });
+  if (!few)
+    std::stable_sort(u1.begin(), u1.end(),
+                     [q_tiles](const kvc::ScoreUnit& x, const kvc::ScoreUnit& y) { return q_tiles(x) > q_tiles(y); });
   const size_t bytes = score_plan_bytes((int64_t)u0.size(), (int64_t)u1.size(), (int64_t)least.size(), (int64_t)meta.size());
   if (bytes > c->ws.sp_bytes) return fail(KVC_ERR_STATE, "the plan of a prompt's scores exceeds the workspace");
   cudaError_t e;
@@ -1217,83 +1236,85 @@ static kvc_status plan_score(kvc_cache* c, const int32_t* n_q, int n_split, cuda
 
 kvc_status kvc_score_prompt(kvc_cache* c, int layer, const void* q, const int32_t* n_q, float scale, void* scratch,
                             size_t scratch_bytes, void* stream_) {
-  kvc_status st = score_check(c, n_q);
-  if (st != KVC_OK) return st;
-  if (layer < 0 || layer >= c->cfg.M) return fail(KVC_ERR_INVALID_ARG, "layer %d out of range", layer);
-  if (std::all_of(n_q, n_q + c->cfg.b, [](int32_t n) { return n == 0; })) return ok();
-  if (!q || !scratch) return fail(KVC_ERR_INVALID_ARG, "q/scratch are NULL");
-  if (reinterpret_cast<uintptr_t>(q) & 15) return fail(KVC_ERR_INVALID_ARG, "q must be 16-byte aligned");
-  if (reinterpret_cast<uintptr_t>(scratch) & 255) return fail(KVC_ERR_INVALID_ARG, "scratch must be 256-byte aligned");
-  if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(KVC_ERR_INVALID_ARG, "scale must be positive and finite");
-  if (layer >= c->layers_done) return fail(KVC_ERR_STATE, "layer %d of the last tokens is not written yet", layer);
-  if (!c->scores) return fail(KVC_ERR_STATE, "the cache has no scores (kvc_set_scores)");
-  size_t need = 0;
-  st = kvc_score_scratch_bytes(c, n_q, &need);
-  if (st != KVC_OK) return st;
-  if (scratch_bytes < need) return fail(KVC_ERR_INVALID_ARG, "%zu bytes of scratch, %zu needed", scratch_bytes, need);
-  cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-  st = c->ensure_cuda(stream);
-  if (st != KVC_OK) return st;
-  const int n_split = score_splits(c, n_q, false);
-  if (c->sp_version != c->version || !std::equal(c->sp_nq.begin(), c->sp_nq.end(), n_q)) {
-    st = plan_score(c, n_q, n_split, stream);
+  return guarded([&]() -> kvc_status {
+    kvc_status st = score_check(c, n_q);
     if (st != KVC_OK) return st;
-  }
-  if (c->sp_units0 == 0) return ok();
-  cudaError_t e = cudaSuccess;
-  if (!c->sp_maps_ready) {
-    e = kvc::encode_rows_map(c->geom(), c->cfg.k_base, c->sp_maps.k);
-    if (e != cudaSuccess) return cuda_fail(e, "cuTensorMapEncodeTiled (K planes)");
-    c->sp_maps_ready = true;
-  }
-  const unsigned char* plan = c->wsp(c->ws.sp);
-  kvc::ScoreArgs a;
-  std::memset(&a, 0, sizeof a);
-  a.layer = layer;
-  a.H = c->cfg.H;
-  a.rot = c->cfg.rotary_dim;
-  a.C = c->C;
-  for (int s = 0; s < c->cfg.b; ++s) a.n_tok += n_q[s];
-  a.units = reinterpret_cast<const kvc::ScoreUnit*>(plan);
-  a.n_units = c->sp_units0;
-  a.meta = reinterpret_cast<const int32_t*>(plan + c->sp_meta);
-  a.least = reinterpret_cast<const int32_t*>(plan + c->sp_least);
-  a.lse = static_cast<float2*>(scratch);
-  a.n_split = n_split;
-  a.scores = c->scores;
-  a.c2 = (float)((double)scale * 1.4426950408889634);
-  a.status = c->bufs().status;
-  a.wait_limit_ns = 2000000000ull;
-  a.q = static_cast<const uint16_t*>(q);
-  a.pos = c->cfg.pos_base;
-  const kvc::Static sta = c->stat();
-  a.off = sta.off;
-  a.rope_g = sta.rope_g;
-  kvc::ScoreMaps maps = c->sp_maps;
-  const void* first = q;
-  if (a.rot > 0) {
-    a.q_part = reinterpret_cast<uint16_t*>(static_cast<unsigned char*>(scratch) +
-                                           align_up(8 * (size_t)n_split * a.H * (size_t)a.n_tok, 256));
-    a.part_stride = (int64_t)align_up(2 * (size_t)a.n_tok * a.H * c->cfg.d_head, 256) / 2;
-    first = a.q_part;
-    e = kvc::launch_score_rotate(c->geom(), a, stream);
-    if (e != cudaSuccess) return cuda_fail(e, "query rotation kernel");
+    if (layer < 0 || layer >= c->cfg.M) return fail(KVC_ERR_INVALID_ARG, "layer %d out of range", layer);
+    if (std::all_of(n_q, n_q + c->cfg.b, [](int32_t n) { return n == 0; })) return ok();
+    if (!q || !scratch) return fail(KVC_ERR_INVALID_ARG, "q/scratch are NULL");
+    if (reinterpret_cast<uintptr_t>(q) & 15) return fail(KVC_ERR_INVALID_ARG, "q must be 16-byte aligned");
+    if (reinterpret_cast<uintptr_t>(scratch) & 255) return fail(KVC_ERR_INVALID_ARG, "scratch must be 256-byte aligned");
+    if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(KVC_ERR_INVALID_ARG, "scale must be positive and finite");
+    if (layer >= c->layers_done) return fail(KVC_ERR_STATE, "layer %d of the last tokens is not written yet", layer);
+    if (!c->scores) return fail(KVC_ERR_STATE, "the cache has no scores (kvc_set_scores)");
+    size_t need = 0;
+    st = kvc_score_scratch_bytes(c, n_q, &need);
+    if (st != KVC_OK) return st;
+    if (scratch_bytes < need) return fail(KVC_ERR_INVALID_ARG, "%zu bytes of scratch, %zu needed", scratch_bytes, need);
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    st = c->ensure_cuda(stream);
+    if (st != KVC_OK) return st;
+    const int n_split = score_splits(c, n_q, false);
+    if (c->sp_version != c->version || !std::equal(c->sp_nq.begin(), c->sp_nq.end(), n_q)) {
+      st = plan_score(c, n_q, n_split, stream);
+      if (st != KVC_OK) return st;
+    }
+    if (c->sp_units0 == 0) return ok();
+    cudaError_t e = cudaSuccess;
+    if (!c->sp_maps_ready) {
+      e = kvc::encode_rows_map(c->geom(), c->cfg.k_base, c->sp_maps.k);
+      if (e != cudaSuccess) return cuda_fail(e, "cuTensorMapEncodeTiled (K planes)");
+      c->sp_maps_ready = true;
+    }
+    const unsigned char* plan = c->wsp(c->ws.sp);
+    kvc::ScoreArgs a;
+    std::memset(&a, 0, sizeof a);
+    a.layer = layer;
+    a.H = c->cfg.H;
+    a.rot = c->cfg.rotary_dim;
+    a.C = c->C;
+    for (int s = 0; s < c->cfg.b; ++s) a.n_tok += n_q[s];
+    a.units = reinterpret_cast<const kvc::ScoreUnit*>(plan);
+    a.n_units = c->sp_units0;
+    a.meta = reinterpret_cast<const int32_t*>(plan + c->sp_meta);
+    a.least = reinterpret_cast<const int32_t*>(plan + c->sp_least);
+    a.lse = static_cast<float2*>(scratch);
+    a.n_split = n_split;
+    a.scores = c->scores;
+    a.c2 = (float)((double)scale * 1.4426950408889634);
+    a.status = c->bufs().status;
+    a.wait_limit_ns = 2000000000ull;
+    a.q = static_cast<const uint16_t*>(q);
+    a.pos = c->cfg.pos_base;
+    const kvc::Static sta = c->stat();
+    a.off = sta.off;
+    a.rope_g = sta.rope_g;
+    kvc::ScoreMaps maps = c->sp_maps;
+    const void* first = q;
+    if (a.rot > 0) {
+      a.q_part = reinterpret_cast<uint16_t*>(static_cast<unsigned char*>(scratch) +
+                                             align_up(8 * (size_t)n_split * a.H * (size_t)a.n_tok, 256));
+      a.part_stride = (int64_t)align_up(2 * (size_t)a.n_tok * a.H * c->cfg.d_head, 256) / 2;
+      first = a.q_part;
+      e = kvc::launch_score_rotate(c->geom(), a, stream);
+      if (e != cudaSuccess) return cuda_fail(e, "query rotation kernel");
+      c->launches += 1;
+    }
+    for (int i = 0; i < kvc::score_parts(c->geom()); ++i) {
+      e = kvc::encode_query_map(c->geom(), static_cast<const uint16_t*>(first) + i * a.part_stride, a.n_tok, maps.q[i]);
+      if (e != cudaSuccess) return cuda_fail(e, "cuTensorMapEncodeTiled (queries)");
+    }
+    e = kvc::launch_score_lse(c->geom(), maps, a, stream);
+    if (e != cudaSuccess) return cuda_fail(e, "score kernel (first pass)");
     c->launches += 1;
-  }
-  for (int i = 0; i < kvc::score_parts(c->geom()); ++i) {
-    e = kvc::encode_query_map(c->geom(), static_cast<const uint16_t*>(first) + i * a.part_stride, a.n_tok, maps.q[i]);
-    if (e != cudaSuccess) return cuda_fail(e, "cuTensorMapEncodeTiled (queries)");
-  }
-  e = kvc::launch_score_lse(c->geom(), maps, a, stream);
-  if (e != cudaSuccess) return cuda_fail(e, "score kernel (first pass)");
-  c->launches += 1;
-  a.units = reinterpret_cast<const kvc::ScoreUnit*>(plan + c->sp_unit1);
-  a.n_units = c->sp_units1;
-  e = kvc::launch_score_sum(c->geom(), maps, a, c->sp_few, stream);
-  c->last_was_decode = false;
-  if (e != cudaSuccess) return cuda_fail(e, "score kernel (second pass)");
-  c->launches += 1;
-  return ok();
+    a.units = reinterpret_cast<const kvc::ScoreUnit*>(plan + c->sp_unit1);
+    a.n_units = c->sp_units1;
+    e = kvc::launch_score_sum(c->geom(), maps, a, c->sp_few, stream);
+    c->last_was_decode = false;
+    if (e != cudaSuccess) return cuda_fail(e, "score kernel (second pass)");
+    c->launches += 1;
+    return ok();
+  });
 }
 
 // The scratch of a shared-prefix decode: [units][members b][split0 b][n_split b], then the parts.  Units of one (layer,
@@ -1316,34 +1337,36 @@ size_t kvc_prefix_scratch_bytes(const kvc_cache* c, const kvc_cache* prefix) {
 }
 
 kvc_status kvc_set_prefix(kvc_cache* c, kvc_cache* prefix, const int32_t* parent, void* scratch, size_t scratch_bytes) {
-  if (!c) return fail(KVC_ERR_INVALID_ARG, "cache is NULL");
-  if (!prefix) {
-    c->prefix = nullptr;
-    c->px = nullptr;
+  return guarded([&]() -> kvc_status {
+    if (!c) return fail(KVC_ERR_INVALID_ARG, "cache is NULL");
+    if (!prefix) {
+      c->prefix = nullptr;
+      c->px = nullptr;
+      return ok();
+    }
+    if (prefix == c) return fail(KVC_ERR_INVALID_ARG, "a cache cannot be its own prefix");
+    if (!parent || !scratch) return fail(KVC_ERR_INVALID_ARG, "parent/scratch are NULL");
+    const kvc_config &a = c->cfg, &p = prefix->cfg;
+    if (a.policy == KVC_POLICY_LOCAL || p.policy == KVC_POLICY_LOCAL)
+      return fail(KVC_ERR_UNSUPPORTED, "the local-attention cache keeps a window and has no shared prefix");
+    if (a.M != p.M || a.H != p.H || a.d_head != p.d_head || a.dtype != p.dtype || a.rotary_dim != p.rotary_dim ||
+        (a.rotary_dim > 0 && a.rope_base != p.rope_base))
+      return fail(KVC_ERR_INVALID_ARG, "the caches differ in layers, heads, d_head, type or rotation");
+    for (int s = 0; s < a.b; ++s)
+      if (parent[s] < -1 || parent[s] >= p.b)
+        return fail(KVC_ERR_INVALID_ARG, "parent[%d] = %d outside [-1, %d)", s, parent[s], p.b);
+    if ((int64_t)p.M * p.H * prefix->C >= ((int64_t)1 << 31))
+      return fail(KVC_ERR_UNSUPPORTED, "M*H*sum(capacity) rows of the prefix exceed the 2^31 rows a coordinate reaches");
+    if (reinterpret_cast<uintptr_t>(scratch) & 255) return fail(KVC_ERR_INVALID_ARG, "scratch must be 256-byte aligned");
+    if (scratch_bytes < kvc_prefix_scratch_bytes(c, prefix))
+      return fail(KVC_ERR_INVALID_ARG, "%zu bytes of scratch, %zu needed", scratch_bytes, kvc_prefix_scratch_bytes(c, prefix));
+    c->prefix = prefix;
+    c->parent.assign(parent, parent + a.b);
+    c->px = static_cast<unsigned char*>(scratch);
+    c->px_version = UINT64_MAX;
+    c->px_maps_ready = false;
     return ok();
-  }
-  if (prefix == c) return fail(KVC_ERR_INVALID_ARG, "a cache cannot be its own prefix");
-  if (!parent || !scratch) return fail(KVC_ERR_INVALID_ARG, "parent/scratch are NULL");
-  const kvc_config &a = c->cfg, &p = prefix->cfg;
-  if (a.policy == KVC_POLICY_LOCAL || p.policy == KVC_POLICY_LOCAL)
-    return fail(KVC_ERR_UNSUPPORTED, "the local-attention cache keeps a window and has no shared prefix");
-  if (a.M != p.M || a.H != p.H || a.d_head != p.d_head || a.dtype != p.dtype || a.rotary_dim != p.rotary_dim ||
-      (a.rotary_dim > 0 && a.rope_base != p.rope_base))
-    return fail(KVC_ERR_INVALID_ARG, "the caches differ in layers, heads, d_head, type or rotation");
-  for (int s = 0; s < a.b; ++s)
-    if (parent[s] < -1 || parent[s] >= p.b)
-      return fail(KVC_ERR_INVALID_ARG, "parent[%d] = %d outside [-1, %d)", s, parent[s], p.b);
-  if ((int64_t)p.M * p.H * prefix->C >= ((int64_t)1 << 31))
-    return fail(KVC_ERR_UNSUPPORTED, "M*H*sum(capacity) rows of the prefix exceed the 2^31 rows a tensor-map coordinate reaches");
-  if (reinterpret_cast<uintptr_t>(scratch) & 255) return fail(KVC_ERR_INVALID_ARG, "scratch must be 256-byte aligned");
-  if (scratch_bytes < kvc_prefix_scratch_bytes(c, prefix))
-    return fail(KVC_ERR_INVALID_ARG, "%zu bytes of scratch, %zu needed", scratch_bytes, kvc_prefix_scratch_bytes(c, prefix));
-  c->prefix = prefix;
-  c->parent.assign(parent, parent + a.b);
-  c->px = static_cast<unsigned char*>(scratch);
-  c->px_version = UINT64_MAX;
-  c->px_maps_ready = false;
-  return ok();
+  });
 }
 
 // Cuts the prefixes' rows into runs and uploads the plan (units, members, each sequence's parts).
@@ -1449,128 +1472,133 @@ static kvc_status plan_prefix(kvc_cache* c, int n_layers, cudaStream_t stream) {
 
 kvc_status kvc_decode_attention_shared(kvc_cache* c, int first, int n_layers, const void* q, int64_t q_layer_stride,
                                        float scale, float* out, int64_t out_layer_stride, void* stream_) {
-  kvc_status st = layers_check(c, first, n_layers, q, q_layer_stride, scale, out, out_layer_stride);
-  if (st != KVC_OK) return st;
-  if (!c->prefix) return fail(KVC_ERR_STATE, "the cache has no prefix (kvc_set_prefix)");
-  if ((reinterpret_cast<uintptr_t>(q) & 15) || (n_layers > 1 && q_layer_stride % 8 != 0))
-    return fail(KVC_ERR_INVALID_ARG, "q must be 16-byte aligned, and so each layer's");
-  const kvc_cache* p = c->prefix;
-  if (first + n_layers > p->layers_done)
-    return fail(KVC_ERR_STATE, "layer %d of the prefix's last tokens is not written yet", std::max(first, p->layers_done));
-  for (int s = 0; s < c->cfg.b; ++s)
-    if (c->parent[s] >= 0 && !p->bk.book.all_visible(c->parent[s]))
-      return fail(KVC_ERR_STATE, "prefix %d has a span that is open or closed and not freed", c->parent[s]);
-  cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-  st = c->ensure_cuda(stream);
-  if (st != KVC_OK) return st;
-  if (p->cuda_ready && p->device != c->device) return fail(KVC_ERR_STATE, "the prefix is on another device");
-  if (c->px_version != p->version || c->px_layers != n_layers) {
-    st = plan_prefix(c, n_layers, stream);
+  return guarded([&]() -> kvc_status {
+    kvc_status st = layers_check(c, first, n_layers, q, q_layer_stride, scale, out, out_layer_stride);
     if (st != KVC_OK) return st;
-  }
-  kvc::PrefixArgs pa;
-  pa.layer = first;
-  pa.n_layers = n_layers;
-  pa.H = c->cfg.H;
-  pa.rot = c->cfg.rotary_dim;
-  pa.C = p->C;
-  pa.st = p->stat();
-  pa.k = p->bufs().k;
-  pa.v = p->bufs().v;
-  pa.units = reinterpret_cast<const kvc::PrefixUnit*>(c->px);
-  pa.n_units = c->px_units;
-  pa.members = reinterpret_cast<const int32_t*>(c->px + c->px_members);
-  pa.ds = reinterpret_cast<const kvc::DState*>(c->wsp(c->ws.dyn));
-  pa.split0 = reinterpret_cast<const int32_t*>(c->px + c->px_split0);
-  pa.n_split = reinterpret_cast<const int32_t*>(c->px + c->px_nsplit);
-  pa.n_parts = c->px_parts;
-  pa.parts = reinterpret_cast<float*>(c->px + align_up(prefix_tables(c->cfg.b, prefix_runs(p)), 256));
-  pa.q = static_cast<const uint16_t*>(q);
-  pa.q_stride = q_layer_stride;
-  pa.c2 = scale * 1.4426950408889634f;
-  pa.status = c->bufs().status;
-  pa.wait_limit_ns = 2000000000ull;
-  cudaError_t e;
-  if (c->px_units > 0) {
-    if (c->px_rows == kvc::kPrefixTcRows) {
-      if (!c->px_maps_ready) {
-        e = kvc::encode_rows_map(p->geom(), p->cfg.k_base, c->px_maps.k);
-        if (e == cudaSuccess) e = kvc::encode_rows_map(p->geom(), p->cfg.v_base, c->px_maps.v);
-        if (e != cudaSuccess) return cuda_fail(e, "cuTensorMapEncodeTiled (the prefix's planes)");
-        c->px_maps_ready = true;
-      }
-      e = kvc::launch_prefix_tc(c->geom(), c->px_maps, pa, stream);
-    } else {
-      e = kvc::launch_prefix(c->geom(), pa, c->device, c->px_rows, stream);
+    if (!c->prefix) return fail(KVC_ERR_STATE, "the cache has no prefix (kvc_set_prefix)");
+    if ((reinterpret_cast<uintptr_t>(q) & 15) || (n_layers > 1 && q_layer_stride % 8 != 0))
+      return fail(KVC_ERR_INVALID_ARG, "q must be 16-byte aligned, and so each layer's");
+    const kvc_cache* p = c->prefix;
+    if (first + n_layers > p->layers_done)
+      return fail(KVC_ERR_STATE, "layer %d of the prefix's last tokens is not written yet", std::max(first, p->layers_done));
+    for (int s = 0; s < c->cfg.b; ++s)
+      if (c->parent[s] >= 0 && !p->bk.book.all_visible(c->parent[s]))
+        return fail(KVC_ERR_STATE, "prefix %d has a span that is open or closed and not freed", c->parent[s]);
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    st = c->ensure_cuda(stream);
+    if (st != KVC_OK) return st;
+    if (p->cuda_ready && p->device != c->device) return fail(KVC_ERR_STATE, "the prefix is on another device");
+    if (c->px_version != p->version || c->px_layers != n_layers) {
+      st = plan_prefix(c, n_layers, stream);
+      if (st != KVC_OK) return st;
     }
-    if (e != cudaSuccess) return cuda_fail(e, "prefix kernel");
+    kvc::PrefixArgs pa;
+    pa.layer = first;
+    pa.n_layers = n_layers;
+    pa.H = c->cfg.H;
+    pa.rot = c->cfg.rotary_dim;
+    pa.C = p->C;
+    pa.st = p->stat();
+    pa.k = p->bufs().k;
+    pa.v = p->bufs().v;
+    pa.units = reinterpret_cast<const kvc::PrefixUnit*>(c->px);
+    pa.n_units = c->px_units;
+    pa.members = reinterpret_cast<const int32_t*>(c->px + c->px_members);
+    pa.ds = reinterpret_cast<const kvc::DState*>(c->wsp(c->ws.dyn));
+    pa.split0 = reinterpret_cast<const int32_t*>(c->px + c->px_split0);
+    pa.n_split = reinterpret_cast<const int32_t*>(c->px + c->px_nsplit);
+    pa.n_parts = c->px_parts;
+    pa.parts = reinterpret_cast<float*>(c->px + align_up(prefix_tables(c->cfg.b, prefix_runs(p)), 256));
+    pa.q = static_cast<const uint16_t*>(q);
+    pa.q_stride = q_layer_stride;
+    pa.c2 = scale * 1.4426950408889634f;
+    pa.status = c->bufs().status;
+    pa.wait_limit_ns = 2000000000ull;
+    cudaError_t e;
+    if (c->px_units > 0) {
+      if (c->px_rows == kvc::kPrefixTcRows) {
+        if (!c->px_maps_ready) {
+          e = kvc::encode_rows_map(p->geom(), p->cfg.k_base, c->px_maps.k);
+          if (e == cudaSuccess) e = kvc::encode_rows_map(p->geom(), p->cfg.v_base, c->px_maps.v);
+          if (e != cudaSuccess) return cuda_fail(e, "cuTensorMapEncodeTiled (the prefix's planes)");
+          c->px_maps_ready = true;
+        }
+        e = kvc::launch_prefix_tc(c->geom(), c->px_maps, pa, stream);
+      } else {
+        e = kvc::launch_prefix(c->geom(), pa, c->device, c->px_rows, stream);
+      }
+      if (e != cudaSuccess) return cuda_fail(e, "prefix kernel");
+      c->launches += 1;
+      c->last_was_decode = false;  // until the launch below
+    }
+    kvc::OwnArgs oa;
+    oa.px = pa;
+    oa.px.C = c->C;
+    oa.px.st = c->stat();
+    oa.px.k = c->bufs().k;
+    oa.px.v = c->bufs().v;
+    oa.b = c->cfg.b;
+    oa.out = out;
+    oa.out_stride = out_layer_stride;
+    oa.early = c->px_units > 0 && (int64_t)c->px_units * c->cfg.H * n_layers <= c->num_sms;
+    e = kvc::launch_own(c->geom(), oa, c->max_segment, c->num_sms, stream);
+    if (e != cudaSuccess) return cuda_fail(e, "own rows' kernel");
     c->launches += 1;
-    c->last_was_decode = false;  // until the launch below
-  }
-  kvc::OwnArgs oa;
-  oa.px = pa;
-  oa.px.C = c->C;
-  oa.px.st = c->stat();
-  oa.px.k = c->bufs().k;
-  oa.px.v = c->bufs().v;
-  oa.b = c->cfg.b;
-  oa.out = out;
-  oa.out_stride = out_layer_stride;
-  oa.early = c->px_units > 0 && (int64_t)c->px_units * c->cfg.H * n_layers <= c->num_sms;
-  e = kvc::launch_own(c->geom(), oa, c->max_segment, c->num_sms, stream);
-  if (e != cudaSuccess) return cuda_fail(e, "own rows' kernel");
-  c->launches += 1;
-  c->last_was_decode = true;
-  return ok();
+    c->last_was_decode = true;
+    return ok();
+  });
 }
 
 kvc_status kvc_evict(kvc_cache* c, const int64_t* keep, const int64_t* recent, int32_t* kept, void* stream_) {
-  if (!c) return fail(KVC_ERR_INVALID_ARG, "cache is NULL");
-  if (!keep || !recent) return fail(KVC_ERR_INVALID_ARG, "keep/recent are NULL");
-  if (c->cfg.policy == KVC_POLICY_LOCAL)
-    return fail(KVC_ERR_UNSUPPORTED, "the local-attention cache keeps a window; nothing is evicted from it");
-  if (c->layers_done != c->cfg.M)
-    return fail(KVC_ERR_STATE, "layers %d..%d of the last tokens are not written yet", c->layers_done, c->cfg.M - 1);
-  if (!c->scores) return fail(KVC_ERR_STATE, "the cache has no scores (kvc_set_scores)");
-  std::vector<kvc::EvictSeq> plan;
-  std::string err;
-  int code = 0;
-  if (!c->bk.book.plan_evict(keep, recent, plan, err, code)) return fail((kvc_status)code, "%s", err.c_str());
-  if (plan.empty()) return ok();
-  cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-  kvc_status st = c->ensure_cuda(stream);
-  if (st != KVC_OK) return st;
-  const size_t bytes = c->ws.dyn_payload + sizeof(kvc::AffSeq) * plan.size();
-  cudaError_t e;
-  kvc::AppendImage small;
-  const bool fits = bytes <= sizeof(small);
-  unsigned char* img = fits ? reinterpret_cast<unsigned char*>(&small) : c->ring.reserve(bytes, &e);
-  if (!img) return cuda_fail(e, "staging");
-  c->bk.book.apply_evict(plan);
-  c->fill_state(img);
-  kvc::AffSeq* aff = reinterpret_cast<kvc::AffSeq*>(img + c->ws.dyn_payload);
-  int64_t max_cand = 0, max_recent = 0;
-  for (size_t i = 0; i < plan.size(); ++i) {
-    std::memset(&aff[i], 0, sizeof(kvc::AffSeq));
-    aff[i].s = plan[i].s;
-    aff[i].len_old = (int32_t)plan[i].len_old;
-    aff[i].len_new = (int32_t)plan[i].keep;
-    aff[i].first_row = (int32_t)plan[i].recent;
-    max_cand = std::max(max_cand, plan[i].len_old - plan[i].recent);
-    max_recent = std::max(max_recent, plan[i].recent);
-  }
-  if (!fits) {
-    e = c->ring.commit(c->wsp(c->ws.dyn), bytes, stream);
-    if (e != cudaSuccess) return cuda_fail(e, "upload eviction plan");
-  }
-  const kvc::EvictImage image{&small, (int)bytes, (int)c->ws.dyn_payload, c->wsp(c->ws.dyn)};
-  e = kvc::launch_evict(c->geom(), c->stat(), c->bufs(), c->scores,
-                        reinterpret_cast<const kvc::AffSeq*>(c->wsp(c->ws.dyn + c->ws.dyn_payload)), (int)plan.size(),
-                        max_cand, max_recent, kept, c->num_sms, fits ? &image : nullptr, stream);
-  if (e != cudaSuccess) return cuda_fail(e, "eviction kernel");
-  c->launches += 1;
-  c->last_was_decode = false;
-  return ok();
+  return guarded([&]() -> kvc_status {
+    if (!c) return fail(KVC_ERR_INVALID_ARG, "cache is NULL");
+    if (!keep || !recent) return fail(KVC_ERR_INVALID_ARG, "keep/recent are NULL");
+    if (c->cfg.policy == KVC_POLICY_LOCAL)
+      return fail(KVC_ERR_UNSUPPORTED, "the local-attention cache keeps a window; nothing is evicted from it");
+    if (c->layers_done != c->cfg.M)
+      return fail(KVC_ERR_STATE, "layers %d..%d of the last tokens are not written yet", c->layers_done, c->cfg.M - 1);
+    if (!c->scores) return fail(KVC_ERR_STATE, "the cache has no scores (kvc_set_scores)");
+    std::vector<kvc::EvictSeq> plan;
+    std::string err;
+    int code = 0;
+    if (!c->bk.book.plan_evict(keep, recent, plan, err, code)) return fail((kvc_status)code, "%s", err.c_str());
+    if (plan.empty()) return ok();
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    kvc_status st = c->ensure_cuda(stream);
+    if (st != KVC_OK) return st;
+    const size_t bytes = c->ws.dyn_payload + sizeof(kvc::AffSeq) * plan.size();
+    cudaError_t e;
+    kvc::AppendImage small;
+    const bool fits = bytes <= sizeof(small);
+    unsigned char* img = fits ? reinterpret_cast<unsigned char*>(&small) : c->ring.reserve(bytes, &e);
+    if (!img) return cuda_fail(e, "staging");
+    c->bk.book.apply_evict(plan);
+    c->fill_state(img);
+    kvc::AffSeq* aff = reinterpret_cast<kvc::AffSeq*>(img + c->ws.dyn_payload);
+    int64_t max_cand = 0, max_recent = 0, max_drop = 0;
+    for (size_t i = 0; i < plan.size(); ++i) {
+      std::memset(&aff[i], 0, sizeof(kvc::AffSeq));
+      aff[i].s = plan[i].s;
+      aff[i].len_old = (int32_t)plan[i].len_old;
+      aff[i].len_new = (int32_t)plan[i].keep;
+      aff[i].first_row = (int32_t)plan[i].recent;
+      max_cand = std::max(max_cand, plan[i].len_old - plan[i].recent);
+      max_recent = std::max(max_recent, plan[i].recent);
+      max_drop = std::max(max_drop, plan[i].len_old - plan[i].keep);
+    }
+    if (!fits) {
+      e = c->ring.commit(c->wsp(c->ws.dyn), bytes, stream);
+      if (e != cudaSuccess) return cuda_fail(e, "upload eviction plan");
+    }
+    const kvc::EvictImage image{&small, (int)bytes, (int)c->ws.dyn_payload, c->wsp(c->ws.dyn)};
+    e = kvc::launch_evict(c->geom(), c->stat(), c->bufs(), c->scores,
+                          reinterpret_cast<const kvc::AffSeq*>(c->wsp(c->ws.dyn + c->ws.dyn_payload)), (int)plan.size(),
+                          max_cand, max_recent, max_drop, kept, c->num_sms, fits ? &image : nullptr, stream);
+    if (e != cudaSuccess) return cuda_fail(e, "eviction kernel");
+    c->launches += 1;
+    c->last_was_decode = false;
+    return ok();
+  });
 }
 
 kvc_status kvc_prefill_attention(kvc_cache* c, int layer, const void* q, const int32_t* n_q, float scale, float* out,
