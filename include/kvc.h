@@ -330,12 +330,12 @@ kvc_status kvc_evict(kvc_cache* cache, const int64_t* keep, const int64_t* recen
  * rows are then stored, and read by a step, once for all of them.  The caches agree in M, H, d_head, dtype
  * and rotation and share a stream; capacities and batch differ as they like.
  *   parent: host [b], copied.
- *   scratch: device, 256-byte aligned, kvc_prefix_scratch_bytes(cache, prefix) bytes, the cache's until another
+ *   scratch: device, 256-byte aligned, kvc_prefix_scratch_bytes(cache) bytes, the cache's until another
  *     prefix is set or the cache is destroyed.
  * The prefix may grow, be compacted or evicted between calls, and outlives its use here; NULL for `prefix`
  * ends it (parent and scratch are then ignored).  Positions are the caller's: append the own tokens at the
  * positions that continue the prefix's. */
-size_t kvc_prefix_scratch_bytes(const kvc_cache* cache, const kvc_cache* prefix);
+size_t kvc_prefix_scratch_bytes(const kvc_cache* cache);
 kvc_status kvc_set_prefix(kvc_cache* cache, kvc_cache* prefix, const int32_t* parent, void* scratch,
                           size_t scratch_bytes);
 

@@ -359,8 +359,8 @@ def kvc_score_prompt(cache: int, layer: int, q, n_q, scale: float, scratch, stre
                                   scratch.numel() * scratch.element_size(), _stream_handle(stream)))
 
 
-def kvc_prefix_scratch_bytes(cache: int, prefix: int) -> int:
-    return lib().kvc_prefix_scratch_bytes(cache, prefix)
+def kvc_prefix_scratch_bytes(cache: int) -> int:
+    return lib().kvc_prefix_scratch_bytes(cache)
 
 
 def kvc_set_prefix(cache: int, prefix, parent, scratch):
@@ -647,7 +647,7 @@ class KVCache:
         parent = _np(parent, np.int32)
         if parent.size != self.b:
             raise ValueError(f"parent must have {self.b} elements, got shape {parent.shape}")
-        scratch = torch.empty(kvc_prefix_scratch_bytes(self.handle, prefix.handle), dtype=torch.uint8, device=self.k.device)
+        scratch = torch.empty(kvc_prefix_scratch_bytes(self.handle), dtype=torch.uint8, device=self.k.device)
         kvc_set_prefix(self.handle, prefix.handle, parent, scratch)
         self.prefix, self._prefix_scratch = prefix, scratch
 

@@ -67,7 +67,7 @@ SIGNATURES = [
     ("kvc_decode_attention_scored", c_int, [P, c_int, c_int, P, c_int64, c_float, P, c_int64, P]),
     ("kvc_score_scratch_bytes", c_int, [P, P, P]),
     ("kvc_score_prompt", c_int, [P, c_int, P, P, c_float, P, c_size_t, P]),
-    ("kvc_prefix_scratch_bytes", c_size_t, [P, P]),
+    ("kvc_prefix_scratch_bytes", c_size_t, [P]),
     ("kvc_set_prefix", c_int, [P, P, P, P, c_size_t]),
     ("kvc_decode_attention_shared", c_int, [P, c_int, c_int, P, c_int64, c_float, P, c_int64, P]),
     ("kvc_evict", c_int, [P, P, P, P, P]),

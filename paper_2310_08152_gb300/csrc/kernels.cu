@@ -1855,15 +1855,21 @@ cudaError_t launch_append_t(const Geometry& g, const Static& st, const Buffers& 
   return cudaGetLastError();
 }
 
-// The shapes of the scored decode: two CTAs per SM of four consumer warps and two stages, and the small shape of two
-// consumer warps, three or four CTAs per SM; what two (four) CTAs leave of the shared memory holds logits.
+// The shapes of the scored decode: the main and the small shape of the plain one, whose shared memory beside the tiles holds
+// logits.  The main shape has three stages while two CTAs of an SM then hold the rows' logits, else two (24 layers of 512
+// segments of 1,024 rows: 481 us with two, 462 with three; 12 of 768 of up to 5,203, one CTA per SM with three, 941 and
+// 985).
 template <int D>
 struct ScoredShape {
+  static constexpr int S3 = CtaMainStages<D>::S;
   using Main = CtaCfg<D, 4, 2, 2>;
+  using Main3 = CtaCfg<D, 4, 2, S3>;
   using Small = CtaCfg<D, 2, 2, 2>;
-  static constexpr int kHeldMain = (113 * 1024 - Main::SMEM) / 4 / 32 * 32;
-  static constexpr int kHeldSmall = (56 * 1024 - Small::SMEM) / 4 / 32 * 32;
-  static_assert(kHeldMain >= 1024 && kHeldSmall >= 512, "room for logits");
+  static constexpr int kSmallCtas = 4;  // per SM
+  static constexpr int held(int room, int used) { return (room - used) / 4 / 32 * 32; }
+  static constexpr int kHeld = held(113 * 1024, Main::SMEM), kHeld3 = held(113 * 1024, Main3::SMEM);
+  static constexpr int kHeldSmall = held(56 * 1024, Small::SMEM);
+  static_assert(kHeld >= 1024 && kHeld3 >= 512 && kHeldSmall >= 512, "room for logits");
 };
 
 template <typename T, int D>
@@ -1872,11 +1878,12 @@ cudaError_t scored_setup(int dev) {
   if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
   if (done[dev].load(std::memory_order_acquire)) return cudaSuccess;
   using E = ScoredShape<D>;
-  cudaError_t e = cudaFuncSetAttribute(decode_cta_kernel<T, D, 4, 2, 2, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       E::Main::SMEM + 4 * E::kHeldMain);
-  if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(decode_cta_kernel<T, D, 2, 2, 2, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             E::Small::SMEM + 4 * E::kHeldSmall);
+  auto room = [](auto* kernel, int bytes) {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  };
+  cudaError_t e = room(decode_cta_kernel<T, D, 4, 2, 2, true>, E::Main::SMEM + 4 * E::kHeld);
+  if (e == cudaSuccess && E::S3 != 2) e = room(decode_cta_kernel<T, D, 4, 2, E::S3, true>, E::Main3::SMEM + 4 * E::kHeld3);
+  if (e == cudaSuccess) e = room(decode_cta_kernel<T, D, 2, 2, 2, true>, E::Small::SMEM + 4 * E::kHeldSmall);
   if (e == cudaSuccess) done[dev].store(true, std::memory_order_release);
   return e;
 }
@@ -1892,20 +1899,30 @@ cudaError_t launch_scored_t(const Geometry& g, const Static& st, const Buffers& 
   const int64_t mean = a.R / (a.n_segments < 1 ? 1 : a.n_segments);
   const bool balanced = decode_balanced(a);
   const int mode = balanced ? 1 : n_layers > 1 ? 4 : 0;
-  const int64_t slots = 2 * (int64_t)num_sms;
-  // Clusters as the plain decode takes them, and wherever a CTA's rows would pass the logits that it holds.
-  int cn = 1;
-  while (2 * cn <= kMaxClusterCtas && ((2 * cn * nseg <= slots && a.max_segment >= 2 * cn * 192) ||
-                                       a.max_segment > (int64_t)cn * E::kHeldMain))
-    cn *= 2;
-  if (cn == 1 && mean < 384 && a.max_segment <= 6 * mean + 256 && nseg > slots) {
-    const int64_t k = balanced ? std::max<int64_t>(1, std::min<int64_t>(8, nseg / (8 * slots))) : 1;
-    const int held = (int)std::min<int64_t>(E::kHeldSmall, (a.max_segment + 31) / 32 * 32);
-    return launch_decode_cta<T, D, 2, 2, 2, true>(g, st, buf, a, 1, k, mode, stream, grid, plan, scores, held);
+  const int64_t slots = 2 * (int64_t)num_sms, slots_s = E::kSmallCtas * (int64_t)num_sms;
+  // The plain decode's plan where it takes CTAs (one layer of 512 segments of 1,024 rows, the small shape: 26.9 us with a
+  // CTA of the main shape for each).  Where it takes warps, or rows split over them, or layers one by one: a CTA of the
+  // main shape for each segment, or short ones several to a CTA of the small shape.
+  CtaPlan c = decode_cta_plan<D>(a, nseg, balanced, slots, slots_s, slots);
+  if (!c.use) {
+    c = {true, false, 1, 1};
+    if (mean < 384 && a.max_segment <= 6 * mean + 256 && nseg > slots)
+      c = {true, true, 1, balanced ? std::max<int64_t>(1, std::min<int64_t>(8, nseg / (8 * slots))) : 1};
+    while (!balanced && 2 * c.cluster <= kMaxClusterCtas && 2 * c.cluster * nseg <= slots && a.max_segment >= 2 * c.cluster * 192)
+      c.cluster *= 2;
   }
-  const int64_t rows = (a.max_segment + cn - 1) / cn;
-  const int held = (int)std::min<int64_t>(E::kHeldMain, (rows + 31) / 32 * 32);
-  return launch_decode_cta<T, D, 4, 2, 2, true>(g, st, buf, a, cn, 1, mode, stream, grid, plan, scores, held);
+  if (c.small && a.max_segment > E::kHeldSmall) c = {true, false, 1, 1};
+  const int64_t want = (a.max_segment + 31) / 32 * 32;  // logits of a whole segment
+  if (c.small)
+    return launch_decode_cta<T, D, 2, 2, 2, true>(g, st, buf, a, 1, c.k, mode, stream, grid, plan, scores, (int)want);
+  // clusters also where a CTA's rows would pass the logits that it holds
+  if (a.max_segment > (int64_t)c.cluster * E::kHeld) c.k = 1;
+  while (2 * c.cluster <= kMaxClusterCtas && a.max_segment > (int64_t)c.cluster * E::kHeld) c.cluster *= 2;
+  const int64_t rows = ((a.max_segment + c.cluster - 1) / c.cluster + 31) / 32 * 32;
+  if (E::S3 != 2 && rows <= E::kHeld3)
+    return launch_decode_cta<T, D, 4, 2, E::S3, true>(g, st, buf, a, c.cluster, c.k, mode, stream, grid, plan, scores, (int)rows);
+  return launch_decode_cta<T, D, 4, 2, 2, true>(g, st, buf, a, c.cluster, c.k, mode, stream, grid, plan, scores,
+                                                (int)std::min<int64_t>(E::kHeld, rows));
 }
 
 template <typename F>

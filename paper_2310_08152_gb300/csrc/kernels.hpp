@@ -176,8 +176,6 @@ struct OwnArgs {
 // Queries of one CTA where the largest group has `group` members (kPrefixTcRows: launch_prefix_tc, with maps of the
 // prefix's planes, else launch_prefix); CTAs per SM of that kernel.
 constexpr int kPrefixTcRows = 128;
-// Most rows of a run in launch_prefix.
-constexpr int64_t kPrefixRun = 8192;
 int prefix_rows(int group);
 cudaError_t prefix_ctas_per_sm(const Geometry& g, int device, int rows, int* occ);
 cudaError_t launch_prefix(const Geometry& g, const PrefixArgs& a, int device, int rows, cudaStream_t stream);

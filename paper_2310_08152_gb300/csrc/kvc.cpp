@@ -1319,21 +1319,16 @@ kvc_status kvc_score_prompt(kvc_cache* c, int layer, const void* q, const int32_
 
 // The scratch of a shared-prefix decode: [units][members b][split0 b][n_split b], then the parts.  Units of one (layer,
 // head): at most one run per group of prefix_rows sequences, and kPrefixUnits more that splitting adds over all (layer,
-// head) pairs, or as many as keep runs at kPrefixRun rows; parts: as many as sequences, layers and heads, for each kPrefixRun
-// rows of the longest prefix, and 128 for each run that splitting adds.
+// head) pairs; parts: as many as sequences, layers and heads, and 128 for each run that splitting adds.
 static constexpr int64_t kPrefixUnits = 640;
-static int64_t prefix_runs(const kvc_cache* prefix) {
-  return (*std::max_element(prefix->cap.begin(), prefix->cap.end()) + kvc::kPrefixRun - 1) / kvc::kPrefixRun;
-}
-static size_t prefix_tables(int b, int64_t runs) {
-  return align_up(sizeof(kvc::PrefixUnit) * (size_t)(kPrefixUnits + b * runs), 16) + 3 * align_up(4 * (size_t)b, 16);
+static size_t prefix_tables(int b) {
+  return align_up(sizeof(kvc::PrefixUnit) * (size_t)(kPrefixUnits + b), 16) + 3 * align_up(4 * (size_t)b, 16);
 }
 
-size_t kvc_prefix_scratch_bytes(const kvc_cache* c, const kvc_cache* prefix) {
-  if (!c || !prefix) return 0;
-  const int64_t runs = prefix_runs(prefix);
-  const int64_t rows = (int64_t)c->cfg.M * c->cfg.H * c->cfg.b * runs + kvc::kPrefixTcRows * kPrefixUnits;
-  return align_up(prefix_tables(c->cfg.b, runs), 256) + 4 * (size_t)rows * (size_t)(c->cfg.d_head + 4);
+size_t kvc_prefix_scratch_bytes(const kvc_cache* c) {
+  if (!c) return 0;
+  const int64_t rows = (int64_t)c->cfg.M * c->cfg.H * c->cfg.b + kvc::kPrefixTcRows * kPrefixUnits;
+  return align_up(prefix_tables(c->cfg.b), 256) + 4 * (size_t)rows * (size_t)(c->cfg.d_head + 4);
 }
 
 kvc_status kvc_set_prefix(kvc_cache* c, kvc_cache* prefix, const int32_t* parent, void* scratch, size_t scratch_bytes) {
@@ -1358,8 +1353,8 @@ kvc_status kvc_set_prefix(kvc_cache* c, kvc_cache* prefix, const int32_t* parent
     if ((int64_t)p.M * p.H * prefix->C >= ((int64_t)1 << 31))
       return fail(KVC_ERR_UNSUPPORTED, "M*H*sum(capacity) rows of the prefix exceed the 2^31 rows a coordinate reaches");
     if (reinterpret_cast<uintptr_t>(scratch) & 255) return fail(KVC_ERR_INVALID_ARG, "scratch must be 256-byte aligned");
-    if (scratch_bytes < kvc_prefix_scratch_bytes(c, prefix))
-      return fail(KVC_ERR_INVALID_ARG, "%zu bytes of scratch, %zu needed", scratch_bytes, kvc_prefix_scratch_bytes(c, prefix));
+    if (scratch_bytes < kvc_prefix_scratch_bytes(c))
+      return fail(KVC_ERR_INVALID_ARG, "%zu bytes of scratch, %zu needed", scratch_bytes, kvc_prefix_scratch_bytes(c));
     c->prefix = prefix;
     c->parent.assign(parent, parent + a.b);
     c->px = static_cast<unsigned char*>(scratch);
@@ -1385,14 +1380,13 @@ static kvc_status plan_prefix(kvc_cache* c, int n_layers, cudaStream_t stream) {
   int occ = 1;
   cudaError_t e = kvc::prefix_ctas_per_sm(c->geom(), c->device, rows, &occ);
   if (e != cudaSuccess) return cuda_fail(e, "prefix kernel");
-  const int64_t most_run = rows == kvc::kPrefixTcRows ? INT32_MAX : kvc::kPrefixRun, runs_max = prefix_runs(c->prefix);
   const int64_t pairs = (int64_t)n_layers * c->cfg.H, slots = (int64_t)occ * c->num_sms;
   auto chunks_of = [&](int g) { return (int64_t)((group[g].size() + rows - 1) / rows); };
-  for (int g = 0; g < P; ++g) units1 += pairs * chunks_of(g) * ((c->prefix->bk.book.stored(g) + most_run - 1) / most_run);
+  for (int g = 0; g < P; ++g) units1 += pairs * chunks_of(g);
   // Rows of a run: at least 256, and 16 per member, for a part's 8 (d_head + 4) bytes a member, written and read.
   auto run_of = [&](int g, int64_t run) {
     const int64_t least = std::max<int64_t>(256, 16 * std::min<int64_t>((int64_t)group[g].size(), rows));
-    return std::min(std::max(run, least), most_run);
+    return std::max(run, least);
   };
   auto runs_of = [&](int g, int64_t run) {
     const int64_t len = c->prefix->bk.book.stored(g), r = run_of(g, run);
@@ -1446,8 +1440,8 @@ static kvc_status plan_prefix(kvc_cache* c, int n_layers, cudaStream_t stream) {
   }
   const size_t ub = align_up(sizeof(kvc::PrefixUnit) * units.size(), 16), ib = align_up(4 * (size_t)b, 16);
   const size_t part_bytes = 4 * (size_t)(parts * pairs) * (size_t)(c->cfg.d_head + 4);
-  if (ub + 3 * ib > prefix_tables(b, runs_max) ||
-      align_up(prefix_tables(b, runs_max), 256) + part_bytes > kvc_prefix_scratch_bytes(c, c->prefix))
+  if (ub + 3 * ib > prefix_tables(b) ||
+      align_up(prefix_tables(b), 256) + part_bytes > kvc_prefix_scratch_bytes(c))
     return fail(KVC_ERR_STATE, "the prefix plan exceeds its scratch");
   unsigned char* img = c->ring.reserve(ub + 3 * ib, &e);
   if (!img) return e != cudaSuccess ? cuda_fail(e, "staging") : fail(KVC_ERR_INVALID_ARG, "prefix plan exceeds ring");
@@ -1508,7 +1502,7 @@ kvc_status kvc_decode_attention_shared(kvc_cache* c, int first, int n_layers, co
     pa.split0 = reinterpret_cast<const int32_t*>(c->px + c->px_split0);
     pa.n_split = reinterpret_cast<const int32_t*>(c->px + c->px_nsplit);
     pa.n_parts = c->px_parts;
-    pa.parts = reinterpret_cast<float*>(c->px + align_up(prefix_tables(c->cfg.b, prefix_runs(p)), 256));
+    pa.parts = reinterpret_cast<float*>(c->px + align_up(prefix_tables(c->cfg.b), 256));
     pa.q = static_cast<const uint16_t*>(q);
     pa.q_stride = q_layer_stride;
     pa.c2 = scale * 1.4426950408889634f;
