@@ -258,9 +258,9 @@ struct alignas(64) PrefillMaps {
 
 cudaError_t encode_prefill_maps(const Geometry& g, const Buffers& buf, PrefillMaps* maps);
 // A 2-D map of the K or the V planes (base) as above in boxes of 128 rows; a 3-D map of queries [n_tok][H][D] in boxes of one column
-// subtile x one head x 128 tokens.  out: 128 bytes.
+// subtile x one head x `rows` tokens.  out: 128 bytes.
 cudaError_t encode_rows_map(const Geometry& g, const void* base, unsigned char* out);
-cudaError_t encode_query_map(const Geometry& g, const void* q, int64_t n_tok, unsigned char* out);
+cudaError_t encode_query_map(const Geometry& g, const void* q, int64_t n_tok, int rows, unsigned char* out);
 // Most CTAs of the persistent prefill grid.
 constexpr int kMaxPrefillCtas = 1024;
 // Keys of one key tile for head dimension D and the cache type, and where a tile's own rows start among
@@ -315,9 +315,10 @@ int score_parts(const Geometry& g);
 int score_ctas_per_sm(const Geometry& g);
 // Rotates a.q into a.q_part (n_qt 128-query tiles: the first pass's units with split 0).
 cudaError_t launch_score_rotate(const Geometry& g, const ScoreArgs& a, cudaStream_t stream);
-// The first pass, and the second, where no sequence has more than 128 queries (few) or some do.
-cudaError_t launch_score_lse(const Geometry& g, const ScoreMaps& maps, const ScoreArgs& a, cudaStream_t stream);
-cudaError_t launch_score_sum(const Geometry& g, const ScoreMaps& maps, const ScoreArgs& a, bool few, cudaStream_t stream);
+// The passes; most: the most queries of a sequence.  The boxes of the query maps hold score_query_rows(most) tokens.
+inline int score_query_rows(int most) { return most <= 16 ? 16 : 128; }
+cudaError_t launch_score_lse(const Geometry& g, const ScoreMaps& maps, const ScoreArgs& a, int most, cudaStream_t stream);
+cudaError_t launch_score_sum(const Geometry& g, const ScoreMaps& maps, const ScoreArgs& a, int most, cudaStream_t stream);
 
 // One warp waits on an mbarrier phase that never completes, with the limit given; the bounded wait
 // gives up and sets STATUS_TIMEOUT in *status.  Exercises the kernels' timeout reporting.

@@ -293,7 +293,7 @@ struct kvc_cache {
   uint64_t sp_version = UINT64_MAX;
   std::vector<int32_t> sp_nq;
   int sp_units0 = 0, sp_units1 = 0;
-  bool sp_few = true;
+  int sp_most = 0;  // queries of a sequence, at most
   size_t sp_unit1 = 0, sp_least = 0, sp_meta = 0;  // offsets inside the plan
   kvc::ScoreMaps sp_maps;
   bool sp_maps_ready = false;
@@ -1167,7 +1167,8 @@ static kvc_status plan_score(kvc_cache* c, const int32_t* n_q, int n_split, cuda
   std::vector<kvc::ScoreUnit> u0, u1;
   std::vector<int32_t> meta, least, rows;
   int32_t tok = 0;
-  bool few = true;
+  const int most = *std::max_element(n_q, n_q + b);
+  const bool few = most <= 128;
   int64_t key_tiles = 0;
   for (int s = 0; s < b; ++s) {
     if (n_q[s] == 0) continue;
@@ -1183,7 +1184,6 @@ static kvc_status plan_score(kvc_cache* c, const int32_t* n_q, int n_split, cuda
     }
     meta.insert(meta.end(), rows.begin(), rows.end());
     tok += n_q[s];
-    few = few && n_q[s] <= 128;
     key_tiles += (len + 127) / 128;
   }
   // key tiles of a unit of the second pass where its query tile stays: two waves of units, sixteen tiles at most
@@ -1230,7 +1230,7 @@ static kvc_status plan_score(kvc_cache* c, const int32_t* n_q, int n_split, cuda
   c->sp_nq.assign(n_q, n_q + b);
   c->sp_units0 = (int)u0.size();
   c->sp_units1 = (int)u1.size();
-  c->sp_few = few;
+  c->sp_most = most;
   return KVC_OK;
 }
 
@@ -1301,15 +1301,16 @@ kvc_status kvc_score_prompt(kvc_cache* c, int layer, const void* q, const int32_
       c->launches += 1;
     }
     for (int i = 0; i < kvc::score_parts(c->geom()); ++i) {
-      e = kvc::encode_query_map(c->geom(), static_cast<const uint16_t*>(first) + i * a.part_stride, a.n_tok, maps.q[i]);
+      e = kvc::encode_query_map(c->geom(), static_cast<const uint16_t*>(first) + i * a.part_stride, a.n_tok,
+                              kvc::score_query_rows(c->sp_most), maps.q[i]);
       if (e != cudaSuccess) return cuda_fail(e, "cuTensorMapEncodeTiled (queries)");
     }
-    e = kvc::launch_score_lse(c->geom(), maps, a, stream);
+    e = kvc::launch_score_lse(c->geom(), maps, a, c->sp_most, stream);
     if (e != cudaSuccess) return cuda_fail(e, "score kernel (first pass)");
     c->launches += 1;
     a.units = reinterpret_cast<const kvc::ScoreUnit*>(plan + c->sp_unit1);
     a.n_units = c->sp_units1;
-    e = kvc::launch_score_sum(c->geom(), maps, a, c->sp_few, stream);
+    e = kvc::launch_score_sum(c->geom(), maps, a, c->sp_most, stream);
     c->last_was_decode = false;
     if (e != cudaSuccess) return cuda_fail(e, "score kernel (second pass)");
     c->launches += 1;

@@ -1160,13 +1160,13 @@ cudaError_t encode_rows_map(const Geometry& g, const void* base, unsigned char* 
   return e != cudaSuccess ? e : encode_plane(g, const_cast<void*>(base), 128, out);
 }
 
-cudaError_t encode_query_map(const Geometry& g, const void* q, int64_t n_tok, unsigned char* out) {
+cudaError_t encode_query_map(const Geometry& g, const void* q, int64_t n_tok, int rows, unsigned char* out) {
   const cudaError_t e = load_encoder();
   if (e != cudaSuccess) return e;
   const int sw = (2 * g.D) % 128 == 0 ? 128 : (2 * g.D) % 64 == 0 ? 64 : 32;
   cuuint64_t dims[3] = {(cuuint64_t)g.D, (cuuint64_t)g.H, (cuuint64_t)n_tok};
   cuuint64_t strides[2] = {(cuuint64_t)g.D * 2, (cuuint64_t)g.H * g.D * 2};
-  cuuint32_t box[3] = {(cuuint32_t)(sw / 2), 1, 128};
+  cuuint32_t box[3] = {(cuuint32_t)(sw / 2), 1, (cuuint32_t)rows};
   cuuint32_t elem[3] = {1, 1, 1};
   const CUtensorMapSwizzle swz =
       sw == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : sw == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B;

@@ -41,16 +41,21 @@ constexpr int kScThreads = kSThreads + 64;
 constexpr int kRows = 128;  // queries, and keys, of a tile
 __device__ __forceinline__ void bar_sync(int id, int n) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n) : "memory"); }
 
-enum Pass { kLse = 0, kSumFew = 1, kSumMany = 2 };
+// kLse16 is the first pass of windows of up to 16 queries, which are the columns there too; kSumFew takes them and windows
+// of up to 128.
+enum Pass { kLse = 0, kSumFew = 1, kSumMany = 2, kLse16 = 3 };
 
-template <int D, int NQ, int PASS>
+// NQ 16-bit parts of a query, QN queries of a tile.
+template <int D, int NQ, int PASS, int QN>
 struct ScCfg {
   static constexpr int SW = (2 * D) % 128 == 0 ? 128 : (2 * D) % 64 == 0 ? 64 : 32;
   static constexpr int SUB = SW / 2;
   static constexpr int NSUB = D / SUB;
   static constexpr uint32_t SUBB = kRows * SW;
   static constexpr uint32_t TILE = kRows * D * 2;
-  static constexpr uint32_t QT = TILE * NQ;  // a query tile's parts
+  static constexpr uint32_t QSUBB = QN * SW;
+  static constexpr uint32_t QTILE = QN * D * 2;
+  static constexpr uint32_t QT = QTILE * NQ;  // a query tile's parts
   // Stages: as many as two CTAs per SM leave room for, three at most, and where fewer than `least` would be left as many
   // as one CTA has room for.
   static constexpr uint32_t ROOM = 110 * 1024, ALL = 220 * 1024;
@@ -71,18 +76,18 @@ struct ScCfg {
   static_assert(SMEM <= 227 * 1024, "shared memory");
 };
 
-template <typename T, int D, int NQ, int PASS>
-__global__ void __launch_bounds__(kScThreads, ScCfg<D, NQ, PASS>::CPS)
+template <typename T, int D, int NQ, int PASS, int QN>
+__global__ void __launch_bounds__(kScThreads, ScCfg<D, NQ, PASS, QN>::CPS)
     score_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mq,
                  const __grid_constant__ CUtensorMap mq1, const __grid_constant__ CUtensorMap mq2, const ScoreArgs a) {
-  using Cf = ScCfg<D, NQ, PASS>;
+  using Cf = ScCfg<D, NQ, PASS, QN>;
   constexpr int KS = Cf::KS, QS = Cf::QS;
   extern __shared__ unsigned char raw[];
   __shared__ __align__(8) uint64_t k_full[KS], k_empty[KS], q_full[QS], q_empty[QS], s_full[2], s_empty[2];
   __shared__ uint32_t tmem_slot;
   __shared__ __align__(16) float s_neg[2][kRows];  // pass 1: -L of a tile's queries
   __shared__ uint32_t s_none[2][4];                // and which of them are <CL> or none
-  __shared__ float2 s_half[kRows];                 // results of the upper columns
+  __shared__ float2 s_half[kRows];                 // results of the upper columns (kLse16: of 16 queries by eight warps)
   const uint32_t sm = (smem_addr(raw) + 1023u) & ~1023u;
   const int warp = uniform((int)(threadIdx.x >> 5)), lane = threadIdx.x & 31, tid = threadIdx.x;
   const uint32_t limit_ns = (uint32_t)a.wait_limit_ns;
@@ -142,9 +147,9 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, NQ, PASS>::CPS)
 #pragma unroll
           for (int i = 0; i < Cf::NSUB; ++i) {
             const int x = i * Cf::SUB, z = sq.tok0 + qt * kRows;
-            tma_load_3d(dst + i * Cf::SUBB, &mq, x, h, z, &q_full[qs]);
-            if constexpr (NQ > 1) tma_load_3d(dst + Cf::TILE + i * Cf::SUBB, &mq1, x, h, z, &q_full[qs]);
-            if constexpr (NQ > 2) tma_load_3d(dst + 2 * Cf::TILE + i * Cf::SUBB, &mq2, x, h, z, &q_full[qs]);
+            tma_load_3d(dst + i * Cf::QSUBB, &mq, x, h, z, &q_full[qs]);
+            if constexpr (NQ > 1) tma_load_3d(dst + Cf::QTILE + i * Cf::QSUBB, &mq1, x, h, z, &q_full[qs]);
+            if constexpr (NQ > 2) tma_load_3d(dst + 2 * Cf::QTILE + i * Cf::QSUBB, &mq2, x, h, z, &q_full[qs]);
           }
           ++nq;
         }
@@ -158,7 +163,10 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, NQ, PASS>::CPS)
     __syncwarp();
   } else if (warp == kSWarps + 1) {
     // ---------------- products ----------------
-    constexpr uint32_t id = mma_idesc(Pack16<T>::kType, 0, kRows, kRows);
+    // columns: the keys, or the queries, where there is one tile of them no more than there are (64 of 128: the second pass
+    // of the window of 64 has half the work)
+    const int n_col = PASS == kLse || PASS == kSumMany ? kRows : (sq.len - sq.q0 + 15) & ~15;
+    const uint32_t id = mma_idesc(Pack16<T>::kType, 0, kRows, n_col);
     constexpr uint32_t SBO = 8 * Cf::SW;
     auto uni_wait = [&](uint64_t* bar, uint32_t parity) -> bool { return __all_sync(0xFFFFFFFFu, pf_wait(bar, parity, limit_ns)); };
     uint32_t nk = 0, nq = 0, step = 0;
@@ -179,7 +187,8 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, NQ, PASS>::CPS)
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk) {
               const uint32_t off = ((kk * 16) / Cf::SUB * Cf::SUBB + (kk * 16) % Cf::SUB * 2) >> 4;
-              const uint64_t dk = desc(k_d + off, SBO, Cf::SW), dq = desc(q_d + part * (Cf::TILE >> 4) + off, SBO, Cf::SW);
+              const uint32_t qoff = ((kk * 16) / Cf::SUB * Cf::QSUBB + (kk * 16) % Cf::SUB * 2) >> 4;
+              const uint64_t dk = desc(k_d + off, SBO, Cf::SW), dq = desc(q_d + part * (Cf::QTILE >> 4) + qoff, SBO, Cf::SW);
               tc_mma(tmem + sb * kRows, PASS == kLse ? dq : dk, PASS == kLse ? dk : dq, id, part + kk > 0);
             }
           }
@@ -197,16 +206,21 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, NQ, PASS>::CPS)
     const int r = (warp & 3) * 32 + lane;  // the thread's row of S (its TMEM lane)
     const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
     const float2 cc = make_float2(a.c2, a.c2);
-    float s[64];
+    constexpr int NC = QN < 64 ? QN : 64;  // columns taken at a time
+    float s[NC];
     auto s_wait = [&](uint32_t step) -> bool {
       const bool got = __all_sync(0xFFFFFFFFu, pf_wait(&s_full[step & 1], step / 2 & 1, limit_ns));
       tc_fence_after();
       return got;
     };
-    // columns [c, c + 64) of the step's S into registers
+    // columns [c, c + NC) of the step's S into registers
     auto take = [&](uint32_t step, int c) {
-      tmem_ld32(lanes + (step & 1) * kRows + c, s);
-      tmem_ld32(lanes + (step & 1) * kRows + c + 32, s + 32);
+      if constexpr (NC == 64) {
+        tmem_ld32(lanes + (step & 1) * kRows + c, s);
+        tmem_ld32(lanes + (step & 1) * kRows + c + 32, s + 32);
+      } else {
+        tmem_ld16(lanes + (step & 1) * kRows + c, s);
+      }
       tmem_wait_ld();
     };
     auto s_done = [&](uint32_t step) {
@@ -217,16 +231,16 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, NQ, PASS>::CPS)
     auto hide = [&](uint32_t v0, uint32_t v1) {
       if (__all_sync(0xFFFFFFFFu, (v0 & v1) == 0xFFFFFFFFu)) return;
 #pragma unroll
-      for (int x = 0; x < 32; ++x) {
-        if (!(v0 >> x & 1)) s[x] = -INFINITY;
-        if (!(v1 >> x & 1)) s[32 + x] = -INFINITY;
-      }
+      for (int x = 0; x < NC; ++x)
+        if (!((x < 32 ? v0 : v1) >> (x & 31) & 1)) s[x] = -INFINITY;
     };
+    // The steps of the passes over key tiles go to the halves by turns (a half's steps all have the same buffer of S).
+    [[maybe_unused]] auto mine = [&](uint32_t step) { return (int)(step & 1) == half; };
     if constexpr (PASS == kLse) {
       const int t0 = sq.q0 + un.qt * kRows, t1 = min(t0 + kRows, sq.len), t = t0 + r;  // the query's stored row
-      const bool mine = t < sq.len;
+      const bool live = t < sq.len;
       const bool idle = t0 + (warp & 3) * 32 >= sq.len;  // none of the warp's queries exists
-      const bool is_cl = mine && (a.meta[sq.moff + t] & 1);
+      const bool is_cl = live && (a.meta[sq.moff + t] & 1);
       float m = -INFINITY, l = 0.f;
       for (int kt = un.kt0; kt < un.kt1; ++kt) {
         const int i0 = kt * kRows + half * 64;  // the row of the thread's first column
@@ -275,11 +289,57 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, NQ, PASS>::CPS)
       }
       if (half) s_half[r] = make_float2(m, l);
       bar_sync(1, kSThreads);
-      if (!half && ok && mine) {
+      if (!half && ok && live) {
         const float2 o = s_half[r];
         const float M = fmaxf(m, o.x), Mu = M == -INFINITY ? 0.f : M;
         a.lse[((int64_t)un.split * a.H + h) * a.n_tok + sq.tok0 + un.qt * kRows + r] =
             is_cl ? make_float2(INFINITY, 1.f) : make_float2(M, l * ex2(m - Mu) + o.y * ex2(o.x - Mu));
+      }
+    } else if constexpr (PASS == kLse16) {
+      // A key per thread: each keeps the maximum and sum of every query over its own keys, joined at the end.
+      float m[QN], l[QN];
+#pragma unroll
+      for (int x = 0; x < QN; ++x) {
+        m[x] = -INFINITY;
+        l[x] = 0.f;
+      }
+      for (int kt = un.kt0; kt < un.kt1; ++kt) {
+        const uint32_t step = kt - un.kt0;
+        if (!mine(step)) continue;
+        const int i = kt * kRows + r, hid = i < sq.len ? a.meta[sq.moff + i] >> 1 : -1;
+        const int lo = max(i - sq.q0, 0), hi = min(hid, sq.len - 1) - sq.q0;
+        if (!(ok = s_wait(step))) break;
+        take(step, 0);
+        s_done(step);
+        hide((low_bits(hi + 1) & ~low_bits(lo)) | ~low_bits(QN), 0xFFFFFFFFu);
+#pragma unroll
+        for (int x = 0; x < QN; ++x) {
+          const float z = s[x] * a.c2, mn = fmaxf(m[x], z), mu = mn == -INFINITY ? 0.f : mn;
+          l[x] = l[x] * ex2(m[x] - mu) + ex2(z - mu);
+          m[x] = mn;
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < QN; ++x) {
+        float M = m[x];
+#pragma unroll
+        for (int off = 16; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, off));
+        float L = l[x] * ex2(m[x] - (M == -INFINITY ? 0.f : M));
+#pragma unroll
+        for (int off = 16; off >= 1; off >>= 1) L += __shfl_xor_sync(0xFFFFFFFFu, L, off);
+        if (lane == x) s_half[warp * QN + x] = make_float2(M, L);
+      }
+      bar_sync(1, kSThreads);
+      if (tid < sq.len - sq.q0 && ok) {
+        float M = -INFINITY, L = 0.f;
+        for (int w = 0; w < kSWarps; ++w) {
+          const float2 v = s_half[w * QN + tid];
+          const float Mn = fmaxf(M, v.x), Mu = Mn == -INFINITY ? 0.f : Mn;
+          L = L * ex2(M - Mu) + v.y * ex2(v.x - Mu);
+          M = Mn;
+        }
+        const bool is_cl = a.meta[sq.moff + sq.q0 + tid] & 1;
+        a.lse[((int64_t)un.split * a.H + h) * a.n_tok + sq.tok0 + tid] = is_cl ? make_float2(INFINITY, 1.f) : make_float2(M, L);
       }
     } else {
       // -L of query tile qt's r-th query; -infinity for a <CL> query and for none
@@ -299,8 +359,6 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, NQ, PASS>::CPS)
         return -(M + log2f(L));
       };
       pdl_wait();  // the queries' sums
-      // The steps go to the halves by turns (a half's steps all have the same buffer of S).
-      auto mine = [&](uint32_t step) { return (int)(step & 1) == half; };
       auto load_neg = [&](float neg) {  // for the half's next step; its threads are done with the last one's
         bar_sync(1 + half, kSThreads / 2);
         s_neg[half][r] = neg;
@@ -330,18 +388,18 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, NQ, PASS>::CPS)
           if (!ok || !(ok = s_wait(step))) continue;
           const int lo = max(i - t0, 0), hi = row ? min(hid, t1 - 1) - t0 : -1;  // the columns that see row i
 #pragma unroll 1
-          for (int c = 0; c < kRows; c += 64) {
+          for (int c = 0; c < QN; c += NC) {
             const uint32_t v0 = low_bits(hi + 1 - c) & ~low_bits(lo - c) & ~s_none[half][c / 32];
-            const uint32_t v1 = low_bits(hi - 31 - c) & ~low_bits(lo - 32 - c) & ~s_none[half][c / 32 + 1];
+            const uint32_t v1 = low_bits(hi - 31 - c) & ~low_bits(lo - 32 - c) & ~s_none[half][(c / 32 + 1) & 3];
             const bool seen = __any_sync(0xFFFFFFFFu, v0 | v1);
             if (seen) take(step, c);
-            if (c == 64) s_done(step);
+            if (c + NC == QN) s_done(step);
             if (!seen) continue;
-            hide(v0, v1);
+            hide(NC == 64 ? v0 : v0 | ~low_bits(NC), NC == 64 ? v1 : 0xFFFFFFFFu);
             const float4* neg = reinterpret_cast<const float4*>(s_neg[half] + c);
             float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
 #pragma unroll
-            for (int x = 0; x < 64; x += 4) {
+            for (int x = 0; x < NC; x += 4) {
               const float4 n = neg[x / 4];
               const float2 z0 = __ffma2_rn(make_float2(s[x], s[x + 1]), cc, make_float2(n.x, n.y));
               const float2 z1 = __ffma2_rn(make_float2(s[x + 2], s[x + 3]), cc, make_float2(n.z, n.w));
@@ -394,16 +452,16 @@ __global__ void __launch_bounds__(256) score_rotate_kernel(const ScoreArgs a) {
   }
 }
 
-template <typename T, int D, int NQ, int PASS>
+template <typename T, int D, int NQ, int PASS, int QN>
 cudaError_t launch_score_t(const ScoreMaps& maps, const ScoreArgs& a, cudaStream_t stream) {
-  using Cf = ScCfg<D, NQ, PASS>;
+  using Cf = ScCfg<D, NQ, PASS, QN>;
   static std::atomic<bool> done[64];
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
   if (!done[dev].load(std::memory_order_acquire)) {
-    e = cudaFuncSetAttribute(score_kernel<T, D, NQ, PASS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cf::SMEM);
+    e = cudaFuncSetAttribute(score_kernel<T, D, NQ, PASS, QN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cf::SMEM);
     if (e != cudaSuccess) return e;
     done[dev].store(true, std::memory_order_release);
   }
@@ -419,8 +477,8 @@ cudaError_t launch_score_t(const ScoreMaps& maps, const ScoreArgs& a, cudaStream
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = PASS == kLse ? 0 : 1;  // the first pass starts when all before it is complete
-  return cudaLaunchKernelEx(&cfg, score_kernel<T, D, NQ, PASS>, mk, mq[0], mq[1], mq[2], a);
+  cfg.numAttrs = PASS == kLse || PASS == kLse16 ? 0 : 1;  // the first pass starts when all before it is complete
+  return cudaLaunchKernelEx(&cfg, score_kernel<T, D, NQ, PASS, QN>, mk, mq[0], mq[1], mq[2], a);
 }
 
 template <typename F>
@@ -440,13 +498,14 @@ cudaError_t by_type(const Geometry& g, F&& f) {
   }
 }
 
-template <int PASS>
+template <int PASS, int QN>
 cudaError_t launch_pass(const Geometry& g, const ScoreMaps& maps, const ScoreArgs& a, cudaStream_t stream) {
   if (a.n_units <= 0) return cudaSuccess;
   return by_type(g, [&](auto t, auto d) {
     using T = decltype(t);
     constexpr int D = decltype(d)::value;
-    return g.rot > 0 ? launch_score_t<T, D, kFullParts<T>, PASS>(maps, a, stream) : launch_score_t<T, D, 1, PASS>(maps, a, stream);
+    return g.rot > 0 ? launch_score_t<T, D, kFullParts<T>, PASS, QN>(maps, a, stream)
+                     : launch_score_t<T, D, 1, PASS, QN>(maps, a, stream);
   });
 }
 
@@ -459,7 +518,7 @@ int score_ctas_per_sm(const Geometry& g) {
   (void)by_type(g, [&](auto t, auto d) {
     using T = decltype(t);
     constexpr int D = decltype(d)::value;
-    n = g.rot > 0 ? ScCfg<D, kFullParts<T>, kLse>::CPS : ScCfg<D, 1, kLse>::CPS;
+    n = g.rot > 0 ? ScCfg<D, kFullParts<T>, kLse, kRows>::CPS : ScCfg<D, 1, kLse, kRows>::CPS;
     return cudaSuccess;
   });
   return n;
@@ -475,12 +534,14 @@ cudaError_t launch_score_rotate(const Geometry& g, const ScoreArgs& a, cudaStrea
   });
 }
 
-cudaError_t launch_score_lse(const Geometry& g, const ScoreMaps& maps, const ScoreArgs& a, cudaStream_t stream) {
-  return launch_pass<kLse>(g, maps, a, stream);
+cudaError_t launch_score_lse(const Geometry& g, const ScoreMaps& maps, const ScoreArgs& a, int most, cudaStream_t stream) {
+  return most <= 16 ? launch_pass<kLse16, 16>(g, maps, a, stream) : launch_pass<kLse, kRows>(g, maps, a, stream);
 }
 
-cudaError_t launch_score_sum(const Geometry& g, const ScoreMaps& maps, const ScoreArgs& a, bool few, cudaStream_t stream) {
-  return few ? launch_pass<kSumFew>(g, maps, a, stream) : launch_pass<kSumMany>(g, maps, a, stream);
+cudaError_t launch_score_sum(const Geometry& g, const ScoreMaps& maps, const ScoreArgs& a, int most, cudaStream_t stream) {
+  return most <= 16      ? launch_pass<kSumFew, 16>(g, maps, a, stream)
+         : most <= kRows ? launch_pass<kSumFew, kRows>(g, maps, a, stream)
+                         : launch_pass<kSumMany, kRows>(g, maps, a, stream);
 }
 
 }  // namespace kvc

@@ -122,6 +122,21 @@ def test_many_streams():
     evict_and_check(cache, [300, 520, 90], 80, 16)
 
 
+@pytest.mark.parametrize("drop", [1, 40])
+def test_large_batch(drop):
+    """A plan too large for a kernel parameter."""
+    lens = [60 + s % 7 + drop for s in range(130)]
+    cache, _ = make(1, 2, 64, lens)
+    cache.attach_scores()
+    fill(cache, lens, lambda s, n: spread(s, n, 1, 2))
+    evict_and_check(cache, lens, 60, 11)
+    q = query(cache, torch.Generator(device="cuda"))
+    out = cache.decode_attention_layers(q, 0.125)  # the state that later calls read went up with the plan
+    for s in (0, 77, 129):
+        k, v = rows_of(cache, s, 60)
+        close(out[0, s], attend(q[0, s].double(), k[0], v[0], list(range(60)), 0.125)[0])
+
+
 def test_candidates_that_do_not_fit_shared_memory():
     n = 50001
     cache, _ = make(1, 2, 64, [n])

@@ -61,7 +61,7 @@ def check(cache, n_q, g, layer=0, scale=None, sd=2.0):
 
 
 CASES = [([1], [1]), ([2], [1]), ([5], [5]), ([127], [127]), ([128], [128]), ([129], [129]), ([130], [1]), ([257], [128]),
-         ([300], [300]), ([1000], [17]), ([1000], [641]), ([40, 700, 128, 3], [40, 100, 0, 3]), ([600, 90, 1], [500, 0, 1])]
+         ([300], [300]), ([1000], [17]), ([1000], [16]), ([777, 30, 4], [9, 16, 1]), ([500], [80]), ([1000], [641]), ([40, 700, 128, 3], [40, 100, 0, 3]), ([600, 90, 1], [500, 0, 1])]
 
 
 @pytest.mark.parametrize("lens,n_q", CASES, ids=lambda x: str(x))
@@ -79,6 +79,7 @@ def test_long_prompt(d, dtype, rot):
     check(cache, [33], g)
     cache, g = make(1, 8, d, [20011, 40], dtype, rot, seed=2)
     check(cache, [64, 40], g)
+    check(cache, [11, 16], g)
 
 
 @pytest.mark.parametrize("H,lens,n_q", [(32, [2048, 1500], [2048, 700]), (40, [900] * 12, [900] * 12), (32, [3000] * 8, [100] * 8)])
@@ -103,6 +104,8 @@ def test_masks(policy, rot):
     cache, g = make(1, 2, 64, lens, rot=rot, kinds=kinds, policy=policy)
     check(cache, lens, g)
     check(cache, [200, 128, 1, 129, 300], g)
+    check(cache, [100, 128, 1, 77, 30], g)
+    check(cache, [16, 3, 1, 16, 12], g)
 
 
 def test_bounds_agree_with_the_oracle():
@@ -120,6 +123,8 @@ def test_bounds_agree_with_the_oracle():
 def test_only_sentinels():
     cache, g = make(1, 2, 64, [260], kinds=[np.array([CL, CR] * 130, np.uint8)])
     check(cache, [260], g)
+    check(cache, [100], g)
+    check(cache, [16], g)
     check(cache, [1], g)
 
 

@@ -75,6 +75,25 @@ def test_long_prefixes_are_split(n, members, d, dtype):
     check(prefix, cache, [0] * members, [1 + i % 3 for i in range(members)], q, d ** -0.5, out)
 
 
+@pytest.mark.parametrize("dtype,rising", [("f16", False), ("bf16", True), ("f16", True)])
+def test_runs_of_several_sums(dtype, rising):
+    """Enough heads and layers that a long prefix is not split: its sums go to memory now and then, with a maximum that stays
+    or that keeps growing between them."""
+    parent, own = [0] * 40, [1 + i % 2 for i in range(40)]
+    prefix, cache, g = pair(19, 32, 64, [5000], parent, own, dtype)
+    if rising:
+        prefix.k.view(19, 32, 5000, 64).mul_(torch.linspace(0.2, 4.0, 5000, device="cuda")[:, None].to(prefix.k.dtype))
+    q = query(cache, g)
+    out = cache.decode_attention_shared(q, 0.25 if rising else 0.125)
+    kp, vp = rows_of(prefix, 0, 5000)
+    for m, h, s in ((0, 0, 0), (3, 31, 39), (18, 5, 17), (9, 16, 2)):
+        ko, vo = rows_of(cache, s, own[s])
+        k, v = torch.cat([kp[m, h:h + 1], ko[m, h:h + 1]], 1), torch.cat([vp[m, h:h + 1], vo[m, h:h + 1]], 1)
+        ref, _ = attend(q[m, s, h:h + 1].double(), k, v, list(range(k.shape[1])), 0.25 if rising else 0.125)
+        close(out[m, s, h:h + 1], ref, f"layer {m}, head {h}, sequence {s}")
+    assert cache.device_status() == 0
+
+
 def test_many_layers_and_part_of_them():
     parent, own = [0, 0, 1, 1, 1], [3, 4, 5, 6, 70]
     prefix, cache, g = pair(12, 16, 64, [500, 130], parent, own)
