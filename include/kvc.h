@@ -17,6 +17,9 @@
  *   kvc_compress_spans    free the rows of closed spans by in-place compaction (Sec. 3.1, freeing the KV)
  *   kvc_decode_attention  one query per (sequence, head) over the kept rows    (Sec. 1 / 3.1 mask; Sec. 4.3)
  *   kvc_prefill_attention every query of a prompt block under the mask, on tensor cores (Sec. 3.1)
+ *   kvc_decode_attention_scored, kvc_score_prompt, kvc_evict   attention weights summed for each row, and rows that
+ *                         leave the cache by them
+ *   kvc_set_prefix, kvc_decode_attention_shared   sequences (samples of a prompt) over rows that they share (Sec. 4.2)
  *   kvc_masked_reference_layout   the full history, the mask and the stored rows, for verification
  * plus a host-only span book (kvc_book_*) holding the span bookkeeping that
  * decides what each call does.
@@ -406,8 +409,8 @@ kvc_status kvc_last_compaction_ms(kvc_cache* cache, float* scan_ms, float* move_
  * plan[0] = mode (0: unbalanced segments of one layer: a CTA or a cluster of CTAs per (sequence, head)
  * segment, up to two segments per CTA, or the kept rows split evenly over a full wave of warps, split
  * segments merged by a log-sum-exp combine; 1: balanced segments, a CTA or a cluster of CTAs for each,
- * or up to eight consecutive ones per CTA; 2: one warp per segment; 3: several consecutive whole
- * segments per warp; 4: unbalanced segments over several layers, one or two per CTA, or runs of
+ * or up to eight consecutive ones per CTA; 2: one warp per segment (the scored decode's too; the shared
+ * decode's own rows: one or four); 3: several consecutive whole segments per warp; 4: unbalanced segments over several layers, one or two per CTA, or runs of
  * consecutive whole segments per warp cut by rows; -1: nothing launched yet), plan[1] = warps that
  * attend, plan[2] = rows per tile, plan[3] = pipeline stages per warp (per CTA where CTAs take
  * segments). */

@@ -1902,12 +1902,11 @@ cudaError_t launch_scored_t(const Geometry& g, const Static& st, const Buffers& 
   const int64_t slots = 2 * (int64_t)num_sms, slots_s = E::kSmallCtas * (int64_t)num_sms;
   // The plain decode's plan where it takes CTAs (one layer of 512 segments of 1,024 rows, the small shape: 26.9 us with a
   // CTA of the main shape for each).  Where it takes warps, or rows split over them, or layers one by one: a CTA of the
-  // main shape for each segment, or short ones several to a CTA of the small shape.
+  // main shape for each segment, or of the small shape for short ones.
   CtaPlan c = decode_cta_plan<D>(a, nseg, balanced, slots, slots_s, slots);
   if (!c.use) {
     c = {true, false, 1, 1};
-    if (mean < 384 && a.max_segment <= 6 * mean + 256 && nseg > slots)
-      c = {true, true, 1, balanced ? std::max<int64_t>(1, std::min<int64_t>(8, nseg / (8 * slots))) : 1};
+    if (mean < 384 && a.max_segment <= 6 * mean + 256 && nseg > slots) c.small = true;
     while (!balanced && 2 * c.cluster <= kMaxClusterCtas && 2 * c.cluster * nseg <= slots && a.max_segment >= 2 * c.cluster * 192)
       c.cluster *= 2;
   }

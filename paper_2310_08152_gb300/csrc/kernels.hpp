@@ -172,7 +172,12 @@ struct OwnArgs {
   // reads the parts.  Beside a larger one its waiting CTAs take room from it (8 samples of 8 prefixes of 800 rows, 32
   // layers: 646 us, one after the other 588).
   int early;
+  float* scores = nullptr;  // launch_own_scored: as launch_decode_scored's
 };
+// The scored decode of many short segments (n_segments of all layers, `rows` rows in all) by the same kernel, without a
+// prefix; whether it is the one for them.
+bool own_scored_takes(int64_t n_segments, int64_t rows, int64_t max_segment, int num_sms);
+cudaError_t launch_own_scored(const Geometry& g, const OwnArgs& a, cudaStream_t stream, DecodePlan* plan);
 // Queries of one CTA where the largest group has `group` members (kPrefixTcRows: launch_prefix_tc, with maps of the
 // prefix's planes, else launch_prefix); CTAs per SM of that kernel.
 constexpr int kPrefixTcRows = 128;
@@ -183,7 +188,9 @@ struct alignas(64) PrefixMaps {
   unsigned char k[128], v[128];
 };
 cudaError_t launch_prefix_tc(const Geometry& g, const PrefixMaps& maps, const PrefixArgs& a, cudaStream_t stream);
-cudaError_t launch_own(const Geometry& g, const OwnArgs& a, int64_t max_segment, int num_sms, cudaStream_t stream);
+
+cudaError_t launch_own(const Geometry& g, const OwnArgs& a, int64_t max_segment, int num_sms, cudaStream_t stream,
+                       DecodePlan* plan);
 
 // Scores follow their rows through a compaction (after launch_compact, from the same source map): in place, zero in
 // the slots that lost their row.

@@ -1109,9 +1109,30 @@ kvc_status kvc_decode_attention_scored(kvc_cache* c, int first, int n_layers, co
     a.n_layers = n_layers;
     a.q_layer_stride = q_layer_stride;
     a.out_layer_stride = out_layer_stride;
-    int grid = 0;
-    const cudaError_t e =
-        kvc::launch_decode_scored(c->geom(), c->stat(), c->bufs(), a, c->scores, c->num_sms, stream, &grid, &c->last_plan);
+    int grid = 1;
+    cudaError_t e;
+    if (kvc::own_scored_takes(n_layers * c->n_segments, n_layers * c->R, c->max_segment, c->num_sms)) {
+      kvc::OwnArgs o{};
+      o.px.layer = first;
+      o.px.n_layers = n_layers;
+      o.px.H = c->cfg.H;
+      o.px.rot = c->cfg.rotary_dim;
+      o.px.C = c->C;
+      o.px.st = c->stat();
+      o.px.k = c->bufs().k;
+      o.px.v = c->bufs().v;
+      o.px.ds = a.dstate;
+      o.px.q = static_cast<const uint16_t*>(q);
+      o.px.q_stride = q_layer_stride;
+      o.px.c2 = a.scale * 1.4426950408889634f;
+      o.b = c->cfg.b;
+      o.out = out;
+      o.out_stride = out_layer_stride;
+      o.scores = c->scores;
+      e = kvc::launch_own_scored(c->geom(), o, stream, &c->last_plan);
+    } else {
+      e = kvc::launch_decode_scored(c->geom(), c->stat(), c->bufs(), a, c->scores, c->num_sms, stream, &grid, &c->last_plan);
+    }
     if (e != cudaSuccess) return cuda_fail(e, "scored decode kernel");
     c->launches += grid > 0 ? 1 : 0;
     c->last_was_decode = true;
@@ -1536,7 +1557,7 @@ kvc_status kvc_decode_attention_shared(kvc_cache* c, int first, int n_layers, co
     oa.out = out;
     oa.out_stride = out_layer_stride;
     oa.early = c->px_units > 0 && (int64_t)c->px_units * c->cfg.H * n_layers <= c->num_sms;
-    e = kvc::launch_own(c->geom(), oa, c->max_segment, c->num_sms, stream);
+    e = kvc::launch_own(c->geom(), oa, c->max_segment, c->num_sms, stream, &c->last_plan);
     if (e != cudaSuccess) return cuda_fail(e, "own rows' kernel");
     c->launches += 1;
     c->last_was_decode = true;

@@ -359,14 +359,20 @@ struct OwnLanes {
   static constexpr int ROWS = U * RPI;
 };
 constexpr int kOwnWarps = 4;
+// SCORED: the decode of many short segments that adds each row's weight to its score, no prefix.  The logits (of up to
+// kOwnHeld rows) stay in shared memory until the segment's maximum and sum are known, so K and V are read once; each score
+// takes one addition of this call.  Bound by the bytes of K, V and the scores.
+constexpr int kOwnHeld = 1024;
 
-template <typename T, int D, int WPS>
+template <typename T, int D, int WPS, bool SCORED>
 __global__ void __launch_bounds__(kOwnWarps * 32, 4) own_kernel(OwnArgs a) {
   using L = OwnLanes<D>;
   constexpr int NV = L::NV, U = L::U, QPL = (D + 31) / 32, PO = D + 4;
   __shared__ __align__(16) float s_q[kOwnWarps][D];
   __shared__ __align__(16) float s_o[kOwnWarps][L::RPI][D];  // the row groups' columns; the first row of a warp's: its result
   __shared__ float s_ml[kOwnWarps][2];
+  __shared__ float s_z[SCORED ? kOwnWarps : 1][SCORED ? kOwnHeld : 1];
+  static_assert(!SCORED || WPS == 1, "a warp has its segment's logits");
   const PrefixArgs& p = a.px;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (!a.early) pdl_wait();  // else whatever the prefix kernel waited for is complete, and it writes only the parts
@@ -379,10 +385,10 @@ __global__ void __launch_bounds__(kOwnWarps * 32, 4) own_kernel(OwnArgs a) {
   const int w = live ? (int)(seg - layer * per_layer) : 0, s = w / H, h = w - s * H;
   const DState d = p.ds[s];
   const int len = live ? d.len : 0;  // 0: the sequence has no token
-  const int n_split = d.is_cl ? 0 : p.n_split[s];
+  const int n_split = SCORED || d.is_cl ? 0 : p.n_split[s];
   const int64_t row0 = (int64_t)(p.layer + layer) * H * p.C + p.st.seq_row0[s] + (int64_t)h * p.st.cap[s];
   float* qs = s_q[warp];
-  const float* part = p.parts + (((int64_t)layer * p.n_parts + p.split0[s]) * H + h) * PO;
+  const float* part = SCORED ? nullptr : p.parts + (((int64_t)layer * p.n_parts + p.split0[s]) * H + h) * PO;
   // the first part is there already where this kernel did not start early: its loads are under way with the rows'
   float M0 = -INFINITY, L0 = 0.f, O0[QPL];
   auto load_part = [&]() {
@@ -452,6 +458,10 @@ __global__ void __launch_bounds__(kOwnWarps * 32, 4) own_kernel(OwnArgs a) {
 #pragma unroll
       for (int off = L::LPR / 2; off >= 1; off >>= 1) z[u] += __shfl_xor_sync(kFull, z[u], off);
       if (!ok[u]) z[u] = -INFINITY;
+      if constexpr (SCORED) {
+        const int x = r0 + u * L::RPI + grp - d.begin;
+        if (tl == 0 && x < kOwnHeld) s_z[warp][x] = z[u];
+      }
       mn = fmaxf(mn, z[u]);
     }
     const float mu = mn == -INFINITY ? 0.f : mn;
@@ -528,6 +538,16 @@ __global__ void __launch_bounds__(kOwnWarps * 32, 4) own_kernel(OwnArgs a) {
       M = Mx;
     }
   }
+  if constexpr (SCORED) {
+    if (len > 0) {
+      const float Mu = M == -INFINITY ? 0.f : M, inv = 1.f / Ls;
+      float* sc = a.scores + (int64_t)(p.layer + layer) * H * p.C + p.st.seq_row0[s] + (int64_t)h * p.st.cap[s] + d.begin;
+      for (int x = lane; x < len - d.begin; x += 32) {  // written by this warp, before the barriers above
+        const float w = exp2f(s_z[warp][x] - Mu) * inv;
+        if (w != 0.f) atomicAdd(sc + x, w);
+      }
+    }
+  }
   if (a.early) pdl_wait();  // the parts; every thread of the grid waits, so that it never ends before the prefix's
   if (len == 0 || sub != 0) return;
   if (a.early && n_split > 0) load_part();
@@ -551,8 +571,9 @@ __global__ void __launch_bounds__(kOwnWarps * 32, 4) own_kernel(OwnArgs a) {
     if (lane + 32 * k < D) out[lane + 32 * k] = O[k] * inv;
 }
 
-template <typename T, int D, int WPS>
-cudaError_t launch_own_t(const OwnArgs& a, int64_t segs, cudaStream_t stream) {
+template <typename T, int D, int WPS, bool SCORED>
+cudaError_t launch_own_t(const OwnArgs& a, int64_t segs, cudaStream_t stream, DecodePlan* plan) {
+  *plan = {2, (int)(segs * WPS), OwnLanes<D>::ROWS, 1};
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)((segs * WPS + kOwnWarps - 1) / kOwnWarps));
   cfg.blockDim = dim3(kOwnWarps * 32);
@@ -561,8 +582,8 @@ cudaError_t launch_own_t(const OwnArgs& a, int64_t segs, cudaStream_t stream) {
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = a.early ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, own_kernel<T, D, WPS>, a);
+  cfg.numAttrs = SCORED || a.early ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, own_kernel<T, D, WPS, SCORED>, a);
 }
 
 template <typename F>
@@ -625,13 +646,29 @@ cudaError_t launch_prefix(const Geometry& g, const PrefixArgs& a, int device, in
   });
 }
 
-cudaError_t launch_own(const Geometry& g, const OwnArgs& a, int64_t max_segment, int num_sms, cudaStream_t stream) {
+cudaError_t launch_own(const Geometry& g, const OwnArgs& a, int64_t max_segment, int num_sms, cudaStream_t stream,
+                       DecodePlan* plan) {
   const int64_t segs = (int64_t)a.px.n_layers * a.b * g.H;
   const bool share = segs <= 16 * (int64_t)num_sms || max_segment > 1024;
   return by_shape(g, 16, [&](auto t, auto d, auto, auto) {
     using T = decltype(t);
     constexpr int D = decltype(d)::value;
-    return share ? launch_own_t<T, D, 4>(a, segs, stream) : launch_own_t<T, D, 1>(a, segs, stream);
+    return share ? launch_own_t<T, D, 4, false>(a, segs, stream, plan) : launch_own_t<T, D, 1, false>(a, segs, stream, plan);
+  });
+}
+
+// A warp for each segment where there are many short ones, else the CTAs of the scored decode.  us with CTAs -> with warps,
+// f16, d_head 64: 12,288 segments of 95 rows 73.8 -> 50.1 (what they read and write would take 45.5), of 200 rows 123 ->
+// 98.6, of 400 rows 224 -> 185, of 700 rows 335 -> 326, of 1,024 rows 463 -> 485; d_head 128, bf16: of 120 rows 138 -> 126,
+// 6,144 of 700 rows 318 -> 343.  Fewer segments leave warps without work: 1,280 of 300 rows 20.6 -> 21.2 (d_head 128: 35.4
+// -> 44.3), 512 of 100 rows 4.7 -> 6.9.
+bool own_scored_takes(int64_t n_segments, int64_t rows, int64_t max_segment, int num_sms) {
+  return max_segment <= kOwnHeld && rows <= 400 * n_segments && n_segments >= 16 * (int64_t)num_sms;
+}
+
+cudaError_t launch_own_scored(const Geometry& g, const OwnArgs& a, cudaStream_t stream, DecodePlan* plan) {
+  return by_shape(g, 16, [&](auto t, auto d, auto, auto) {
+    return launch_own_t<decltype(t), decltype(d)::value, 1, true>(a, (int64_t)a.px.n_layers * a.b * g.H, stream, plan);
   });
 }
 

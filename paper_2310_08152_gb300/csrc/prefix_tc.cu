@@ -1,7 +1,7 @@
 // The prefix part of a shared-prefix decode for large groups, on the fifth-generation tensor cores: up to 128 members'
 // queries of one (layer, head) against a run of the prefix's rows.  What it computes and leaves is prefix_kernel's
 // (prefix.cu); past 32 members the 16 x 8 x 16 instructions bound that kernel (64 samples of 32,768 rows, two layers of 32
-// heads of 128, bf16: 312 us, its tensor pipe at 54 %, where the rows' bytes take 158), and these do four times as much.
+// heads of 128, bf16: 312 us, its tensor pipe at 54 %, where the rows' bytes take 158; here 187), and these do four times as much.
 //
 // One CTA per SM.  Per tile of 128 rows: S = Q K^T into one of two TMEM buffers; eight warps take it, a query per thread
 // pair and 64 columns each, agree on the row's maximum through shared memory, and leave P as two 16-bit parts
@@ -29,7 +29,7 @@ constexpr int kTcThreads = kPThreads + 64;
 // Tiles that go into one sum in TMEM.  The tensor core cuts what it adds rather than round it: 16,384 rows of both parts in
 // one sum left an error of 1.2e-5.  So the parts have a sum each, the small one's error being small, and after 2,048 rows
 // the sums are added to the part in memory.  (A third part of a bf16 P, which would take the output's error from 2e-6 to
-// 1e-6, made the longest case 389 us.)
+// 1e-6, made the case above 389 us.)
 constexpr int kSumTiles = 16;
 
 template <int D, int NQ>
@@ -210,7 +210,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     float m = -INFINITY, l = 0.f;
     float m_sum = -INFINITY;  // the reference of the sum at `to`
     // O, whose reference is `ref`, joined with the sum at `to`: stored, added without waiting for what is there, or, where
-    // the reference has moved, scaled and added.  (Read and written back each time: the longest case 268 us.)
+    // the reference has moved, scaled and added.  (Read and written back each time:
+    // the case above 268 us, 257 so.)
     auto add_o = [&](float ref, bool first) {
       const float e = first ? 1.f : ex2(m_sum - ref);
       const bool same = __all_sync(0xFFFFFFFFu, e == 1.f || !live);

@@ -103,6 +103,41 @@ def test_hidden_rows_get_nothing(policy):
     check(cache, q, 0.125, seen, [0] * 5, before, out)
 
 
+@pytest.mark.parametrize("d,dtype,rot", [(64, "f16", 0), (64, "bf16", 64), (80, "f16", 48), (80, "bf16", 0), (96, "bf16", 96),
+                                         (96, "f16", 0), (128, "f16", 128), (128, "bf16", 0)])
+def test_thousands_of_short_segments(d, dtype, rot):
+    """A warp for each segment, of one row up to as many as a warp holds the logits of; hidden runs, <CL> queries, a
+    sequence without tokens; twice, so that the second call adds to the first's."""
+    N, CL, CR = kvc.NORMAL, kvc.CL, kvc.CR
+    kinds = [np.array([N] * n, np.uint8) for n in (1, 2, 0, 31, 32, 33, 127, 129, 1023)] + [
+        np.array([N] * 70 + [CL] + [N] * 9, np.uint8),
+        np.array([N] * 40 + [CL], np.uint8),
+        np.array([N] * 5 + [CL] + [N] * 150 + [CR], np.uint8),
+        np.array([N] * 5 + [CL] + [N] * 150 + [CR, N, N], np.uint8),
+        np.array([CL], np.uint8)]
+    seen = [list(range(k.size)) for k in kinds[:9]] + [
+        [i for i in range(80) if i != 70], [40], [i for i in range(157) if i != 5], [i for i in range(159) if not 5 <= i < 156], [0]]
+    lens = [k.size for k in kinds]
+    cache, g = make(12, 16, d, lens, dtype, rot, kinds=kinds, seed=d + rot, spare=3)
+    cache.attach_scores()
+    q = query(cache, g)
+    plain = cache.decode_attention_layers(q, d ** -0.5)
+    qpos = [cache.masked_reference_layout(s)["pos"][-1] if n else 0 for s, n in enumerate(lens)]
+    for _ in range(2):
+        before = cache.scores.clone()
+        out = cache.decode_attention_scored(q, d ** -0.5)
+        check(cache, q, d ** -0.5, seen, qpos, before, out)
+        assert cache.last_decode_plan["mode"] == 2
+    for s, n in enumerate(lens):
+        if n:
+            close(out[:, s], plain[:, s])
+    again = [cache.scores.clone(), out]
+    cache.attach_scores()
+    cache.decode_attention_scored(q, d ** -0.5)
+    out = cache.decode_attention_scored(q, d ** -0.5)
+    assert torch.equal(again[0], cache.scores) and torch.equal(again[1][:, lens.index(1)], out[:, lens.index(1)])
+
+
 def test_scores_add_up_over_steps_and_layers_by_turns():
     cache, g = make(3, 4, 64, [100, 37], spare=8)
     cache.attach_scores()
