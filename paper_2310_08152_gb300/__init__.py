@@ -92,6 +92,43 @@ def _dev(t, name, dtype=None, numel=None):
     return t
 
 
+class _Memory:
+    """Device memory of a cache's calls, which run on any stream, while torch's pool gives what is dropped to the next
+    tensor of the stream that it was made on.  Before its first use on another stream, that stream waits for the work
+    that was queued ahead of the making, which the pool may have had the memory from; and the pool is told of the
+    stream, so that dropped memory is not given out before what is queued there by then is complete."""
+
+    def __init__(self, make):
+        import torch
+
+        self.tensor = make()
+        self.streams = {_stream_handle(None)}  # those it may be used on
+        self.made = None  # an event; not in a capture, whose graph has memory of its own
+        if not torch.cuda.is_current_stream_capturing():
+            self.made = torch.cuda.Event()
+            self.made.record()
+
+    def used_on(self, handle: int):
+        if handle in self.streams:
+            return
+        import torch
+
+        stream = torch.cuda.ExternalStream(handle, device=self.tensor.device)
+        if self.made is not None:
+            with torch.cuda.stream(stream):
+                capturing = torch.cuda.is_current_stream_capturing()
+            if capturing:  # work outside of the capture is not the graph's to wait for
+                mode = lib().kvc_thread_capture_mode(2)
+                try:
+                    self.made.synchronize()
+                finally:
+                    lib().kvc_thread_capture_mode(mode)
+            else:
+                stream.wait_event(self.made)
+        self.tensor.record_stream(stream)
+        self.streams.add(handle)
+
+
 # ------------------------------------------------------------------------------------------
 # span book (host only)
 # ------------------------------------------------------------------------------------------
@@ -480,8 +517,8 @@ class KVCache:
                 lib().kvc_thread_capture_mode(mode)
             kvc_set_staging(self.handle, self.staging)
         self.book = Book(self.b, cap, policy, _handle=lib().kvc_get_book(self.handle))
-        self.scores = None
-        self.prefix = None
+        self.scores = self._scores = None  # the tensor, and its _Memory
+        self.prefix = self._prefix_scratch = None
         self._score_scratch = self._score_counts = None
         self._budget = np.zeros((2, self.b), np.int64)
         self._budget_at = self._budget.ctypes.data
@@ -520,8 +557,16 @@ class KVCache:
         (kvc_append_free_closed if free_closed else kvc_append)(self.handle, layer, k, v, n_new, pos, kinds, stream)
         return pos
 
+    def _stream(self, stream, *memory) -> int:
+        """The handle of a call's stream, which the given memory of the cache's is about to be used on."""
+        handle = _stream_handle(stream)
+        for m in memory:
+            if m is not None:
+                m.used_on(handle)
+        return handle
+
     def compress_spans(self, seq, cl, cr, stream=None):
-        kvc_compress_spans(self.handle, seq, cl, cr, stream)
+        kvc_compress_spans(self.handle, seq, cl, cr, self._stream(stream, self._scores))
 
     def decode_attention(self, layer: int, q, scale: float, out=None, stream=None):
         import torch
@@ -578,16 +623,17 @@ class KVCache:
         layout of the rows ([M, H * C]), or a new zeroed tensor.  The cache keeps and returns it."""
         import torch
 
-        if scores is None:
-            scores = torch.zeros(self.M, self.H * self.C, dtype=torch.float32, device=self.k.device)
-        _dev(scores, "scores", torch.float32, self.M * self.H * self.C)
-        kvc_set_scores(self.handle, scores)
-        self.scores = scores
-        return scores
+        if scores is not None:
+            _dev(scores, "scores", torch.float32, self.M * self.H * self.C)
+        memory = _Memory(lambda: torch.zeros(self.M, self.H * self.C, dtype=torch.float32, device=self.k.device)
+                         if scores is None else scores)
+        kvc_set_scores(self.handle, memory.tensor)
+        self.scores, self._scores = memory.tensor, memory
+        return memory.tensor
 
     def detach_scores(self):
         kvc_set_scores(self.handle, None)
-        self.scores = None
+        self.scores = self._scores = None
 
     def score_rows(self, layer: int, s: int, h: int, n: int):
         """The scores of rows [0, n) of sequence s, head h in a layer."""
@@ -598,7 +644,7 @@ class KVCache:
         [n_layers][b][H][d_head]; every layer from `first` on unless n_layers is given."""
         n_layers, out = self._layers(q, out, first, n_layers)
         n = self.b * self.H * self.d
-        kvc_decode_attention_scored(self.handle, first, n_layers, q, n, scale, out, n, stream)
+        kvc_decode_attention_scored(self.handle, first, n_layers, q, n, scale, out, n, self._stream(stream, self._scores))
         return out
 
     def score_prompt(self, layer: int, q, n_q, scale: float, stream=None):
@@ -613,12 +659,11 @@ class KVCache:
         counts = n_q.tobytes()
         if counts != self._score_counts:
             need = kvc_score_scratch_bytes(self.handle, n_q)
-            if self._score_scratch is None or self._score_scratch.numel() < need:
-                if self._score_scratch is not None and stream is not None:
-                    torch.cuda.synchronize(self.k.device)  # the old one may be in use on that stream
-                self._score_scratch = torch.empty(max(need, 256), dtype=torch.uint8, device=self.k.device)
+            if self._score_scratch is None or self._score_scratch.tensor.numel() < need:
+                self._score_scratch = _Memory(lambda: torch.empty(max(need, 256), dtype=torch.uint8, device=self.k.device))
             self._score_counts = counts
-        kvc_score_prompt(self.handle, layer, q, n_q, scale, self._score_scratch, stream)
+        kvc_score_prompt(self.handle, layer, q, n_q, scale, self._score_scratch.tensor,
+                         self._stream(stream, self._score_scratch, self._scores))
 
     def evict(self, keep, recent, kept=None, stream=None):
         """Brings every (layer, head) stream of the sequences with keep >= 0 down to `keep` rows: its last `recent` ones
@@ -632,7 +677,7 @@ class KVCache:
         for row, x, name in ((0, keep, "keep"), (1, recent, "recent")):
             self._budget[row] = x if isinstance(x, int) else _per_seq(x, self.b, name)
         _check(lib().kvc_evict(self.handle, self._budget_at, self._budget_at + 8 * self.b, _ptr(kept),
-                               _stream_handle(stream)))
+                               self._stream(stream, self._scores)))
 
     # sequences that share a prefix
     def set_prefix(self, prefix: Optional["KVCache"], parent=None):
@@ -647,8 +692,8 @@ class KVCache:
         parent = _np(parent, np.int32)
         if parent.size != self.b:
             raise ValueError(f"parent must have {self.b} elements, got shape {parent.shape}")
-        scratch = torch.empty(kvc_prefix_scratch_bytes(self.handle), dtype=torch.uint8, device=self.k.device)
-        kvc_set_prefix(self.handle, prefix.handle, parent, scratch)
+        scratch = _Memory(lambda: torch.empty(kvc_prefix_scratch_bytes(self.handle), dtype=torch.uint8, device=self.k.device))
+        kvc_set_prefix(self.handle, prefix.handle, parent, scratch.tensor)
         self.prefix, self._prefix_scratch = prefix, scratch
 
     def decode_attention_shared(self, q, scale: float, out=None, stream=None, first: int = 0, n_layers=None):
@@ -658,7 +703,8 @@ class KVCache:
             raise KvcError(5, "the prefix's cache is closed")
         n_layers, out = self._layers(q, out, first, n_layers)
         n = self.b * self.H * self.d
-        kvc_decode_attention_shared(self.handle, first, n_layers, q, n, scale, out, n, stream)
+        kvc_decode_attention_shared(self.handle, first, n_layers, q, n, scale, out, n,
+                                    self._stream(stream, self._prefix_scratch))
         return out
 
     def masked_reference_layout(self, seq: int, stream=None):
