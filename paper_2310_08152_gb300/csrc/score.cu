@@ -240,7 +240,6 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, NQ, PASS, QN>::CPS)
       const int t0 = sq.q0 + un.qt * kRows, t1 = min(t0 + kRows, sq.len), t = t0 + r;  // the query's stored row
       const bool live = t < sq.len;
       const bool idle = t0 + (warp & 3) * 32 >= sq.len;  // none of the warp's queries exists
-      const bool is_cl = live && (a.meta[sq.moff + t] & 1);
       float m = -INFINITY, l = 0.f;
       for (int kt = un.kt0; kt < un.kt1; ++kt) {
         const int i0 = kt * kRows + half * 64;  // the row of the thread's first column
@@ -293,7 +292,7 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, NQ, PASS, QN>::CPS)
         const float2 o = s_half[r];
         const float M = fmaxf(m, o.x), Mu = M == -INFINITY ? 0.f : M;
         a.lse[((int64_t)un.split * a.H + h) * a.n_tok + sq.tok0 + un.qt * kRows + r] =
-            is_cl ? make_float2(INFINITY, 1.f) : make_float2(M, l * ex2(m - Mu) + o.y * ex2(o.x - Mu));
+            make_float2(M, l * ex2(m - Mu) + o.y * ex2(o.x - Mu));
       }
     } else if constexpr (PASS == kLse16) {
       // A key per thread: each keeps the maximum and sum of every query over its own keys, joined at the end.
@@ -338,20 +337,18 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, NQ, PASS, QN>::CPS)
           L = L * ex2(M - Mu) + v.y * ex2(v.x - Mu);
           M = Mn;
         }
-        const bool is_cl = a.meta[sq.moff + sq.q0 + tid] & 1;
-        a.lse[((int64_t)un.split * a.H + h) * a.n_tok + sq.tok0 + tid] = is_cl ? make_float2(INFINITY, 1.f) : make_float2(M, L);
+        a.lse[((int64_t)un.split * a.H + h) * a.n_tok + sq.tok0 + tid] = make_float2(M, L);
       }
     } else {
       // -L of query tile qt's r-th query; -infinity for a <CL> query and for none
       auto neg_lse = [&](int qt) -> float {
         const int x = qt * kRows + r;
-        if (sq.q0 + x >= sq.len) return -INFINITY;
+        if (sq.q0 + x >= sq.len || (a.meta[sq.moff + sq.q0 + x] & 1)) return -INFINITY;
         const float2* p = a.lse + (int64_t)h * a.n_tok + sq.tok0 + x;
         const int64_t step_s = (int64_t)a.H * a.n_tok;
         float M = -INFINITY, L = 0.f;
         for (int k = 0; k < a.n_split; ++k) {
           const float2 v = __ldcg(p + k * step_s);
-          if (v.x == INFINITY) return -INFINITY;  // a <CL> query, in every split
           const float Mn = fmaxf(M, v.x), Mu = Mn == -INFINITY ? 0.f : Mn;
           L = L * ex2(M - Mu) + v.y * ex2(v.x - Mu);
           M = Mn;

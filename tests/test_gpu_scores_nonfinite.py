@@ -1,0 +1,64 @@
+"""Infinities and NaN in queries and keys: what the scores of the rows get from them, against softmaxes in 64 bits.  A
+query one of whose visible logits is not a number, or +infinity, has weights that are NaN at every row it sees, and adds
+nothing to the rows it does not see."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2310_08152_gb300 as kvc
+
+from _serving import collected  # noqa: F401
+from _serving import RTOL, make, per_row, query, rotate, rows_of
+
+pytestmark = pytest.mark.gpu
+
+N, CL, CR = kvc.NORMAL, kvc.CL, kvc.CR
+INF, NAN = float("inf"), float("nan")
+
+
+def weights(cache, s, q, n_q, scale):
+    """(seen [n_q, n], weights [H, n_q, n]) of the last n_q tokens of sequence s in layer 0; q: [n_q, H, d].  Rows that a
+    query does not see are left out of its softmax and get 0."""
+    meta = cache.prefill_keys(s, n_q)
+    n = meta.size
+    i = torch.arange(n, device="cuda")
+    t = i[n - n_q:, None]
+    is_cl = torch.tensor((meta & 1).astype(bool), device="cuda")[n - n_q:, None]
+    seen = torch.where(is_cl, i == t, (i <= t) & (t <= torch.tensor(meta >> 1, device="cuda")))
+    pos = cache.masked_reference_layout(s)["stored_pos"]
+    qq = torch.stack([rotate(q[j], pos[n - n_q + j], cache.rotary_dim) for j in range(n_q)], 1)
+    z = torch.einsum("hqd,hnd->hqn", qq, rows_of(cache, s, n)[0][0].double()) * scale
+    w = torch.zeros_like(z)
+    for j in range(n_q):
+        w[:, j, seen[j]] = torch.softmax(z[:, j, seen[j]], -1)
+    return seen, w
+
+
+def agree(got, ref, what=""):
+    """NaN where the reference is, its values elsewhere (RTOL of themselves, as every weight summed here is)."""
+    got, ref = got.double().cpu(), ref.double().cpu()
+    bad = torch.isnan(ref)
+    assert bad.any() and not bad.all(), what
+    assert torch.equal(torch.isnan(got), bad), what
+    assert float(((got - ref).abs() - RTOL * ref.abs())[~bad].max()) <= 1e-9, what
+
+
+# windows of up to 16 queries, of up to 128, whole prompts
+WINDOWS = [12, 90, 700]
+
+
+@pytest.mark.parametrize("n_q", WINDOWS)
+@pytest.mark.parametrize("d,dtype,rot", [(64, "f16", 0), (80, "bf16", 80), (128, "bf16", 0)])
+def test_infinite_logit_of_a_prompt_query(n_q, d, dtype, rot):
+    """One infinite component: the query's logits are infinities of both signs.  The last query, which sees every row, in
+    head 0, and one in the middle in head 1; head 2 is untouched."""
+    cache, g = make(1, 3, d, [700], dtype, rot, seed=n_q)
+    cache.attach_scores()
+    q = torch.empty(n_q, 3, d, dtype=cache.torch_dtype, device="cuda").normal_(0.0, 2.0, generator=g)
+    q[-1, 0, d - 1] = INF
+    cache.score_prompt(0, q, [n_q], d ** -0.5)
+    got = per_row(cache, cache.scores, 0, 700)[0]
+    ref = weights(cache, 0, q, n_q, d ** -0.5)[1].sum(1)
+    assert torch.isnan(ref[0]).all() and torch.isfinite(ref[1:]).all()
+    agree(got, ref)
+    assert cache.device_status() == 0
