@@ -86,7 +86,8 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, NQ, PASS, QN>::CPS)
   __shared__ __align__(8) uint64_t k_full[KS], k_empty[KS], q_full[QS], q_empty[QS], s_full[2], s_empty[2];
   __shared__ uint32_t tmem_slot;
   __shared__ __align__(16) float s_neg[2][kRows];  // pass 1: -L of a tile's queries
-  __shared__ uint32_t s_none[2][4];                // and which of them are <CL> or none
+  __shared__ __align__(16) uint32_t s_none[2][4];  // which of them have no part in the sums: <CL>, none and s_bad
+  __shared__ __align__(16) uint32_t s_bad[2][4];   // whose weights are not numbers
   __shared__ float2 s_half[kRows];                 // results of the upper columns (kLse16: of 16 queries by eight warps)
   const uint32_t sm = (smem_addr(raw) + 1023u) & ~1023u;
   const int warp = uniform((int)(threadIdx.x >> 5)), lane = threadIdx.x & 31, tid = threadIdx.x;
@@ -340,7 +341,8 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, NQ, PASS, QN>::CPS)
         a.lse[((int64_t)un.split * a.H + h) * a.n_tok + sq.tok0 + tid] = make_float2(M, L);
       }
     } else {
-      // -L of query tile qt's r-th query; -infinity for a <CL> query and for none
+      // -L of query tile qt's r-th query; -infinity for a <CL> query and for none, NaN where its weights are not numbers:
+      // a logit is NaN or +infinity, or all are -infinity
       auto neg_lse = [&](int qt) -> float {
         const int x = qt * kRows + r;
         if (sq.q0 + x >= sq.len || (a.meta[sq.moff + sq.q0 + x] & 1)) return -INFINITY;
@@ -353,14 +355,19 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, NQ, PASS, QN>::CPS)
           L = L * ex2(M - Mu) + v.y * ex2(v.x - Mu);
           M = Mn;
         }
-        return -(M + log2f(L));
+        const float lse = M + log2f(L);
+        return fabsf(lse) < INFINITY ? -lse : NAN;
       };
       pdl_wait();  // the queries' sums
       auto load_neg = [&](float neg) {  // for the half's next step; its threads are done with the last one's
         bar_sync(1 + half, kSThreads / 2);
-        s_neg[half][r] = neg;
-        const uint32_t none = __ballot_sync(0xFFFFFFFFu, neg == -INFINITY);
-        if (lane == 0) s_none[half][warp & 3] = none;
+        // such a query's weight is NaN at the rows that it sees, and must not reach the others of its columns
+        s_neg[half][r] = neg == neg ? neg : -INFINITY;
+        const uint32_t bad = __ballot_sync(0xFFFFFFFFu, neg != neg), none = __ballot_sync(0xFFFFFFFFu, neg == -INFINITY) | bad;
+        if (lane == 0) {
+          s_none[half][warp & 3] = none;
+          s_bad[half][warp & 3] = bad;
+        }
         bar_sync(1 + half, kSThreads / 2);
       };
       if (PASS == kSumFew) load_neg(neg_lse(0));
@@ -384,6 +391,13 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, NQ, PASS, QN>::CPS)
           // after a wait that ran out the warp only keeps up with the others' barriers
           if (!ok || !(ok = s_wait(step))) continue;
           const int lo = max(i - t0, 0), hi = row ? min(hid, t1 - 1) - t0 : -1;  // the columns that see row i
+          const uint4 bad = *reinterpret_cast<const uint4*>(s_bad[half]);
+          if (bad.x | bad.y | bad.z | bad.w) {
+            const uint32_t b[4] = {bad.x, bad.y, bad.z, bad.w};
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+              if (b[c] & low_bits(hi + 1 - 32 * c) & ~low_bits(lo - 32 * c)) total = NAN;
+          }
 #pragma unroll 1
           for (int c = 0; c < QN; c += NC) {
             const uint32_t v0 = low_bits(hi + 1 - c) & ~low_bits(lo - c) & ~s_none[half][c / 32];

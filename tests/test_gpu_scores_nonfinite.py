@@ -18,7 +18,8 @@ INF, NAN = float("inf"), float("nan")
 
 def weights(cache, s, q, n_q, scale):
     """(seen [n_q, n], weights [H, n_q, n]) of the last n_q tokens of sequence s in layer 0; q: [n_q, H, d].  Rows that a
-    query does not see are left out of its softmax and get 0."""
+    query does not see are left out of its softmax and get 0.  A rotated query goes into the products in parts, of either
+    sign or 0, so that at an infinite key its logit is NaN where it would be -infinity."""
     meta = cache.prefill_keys(s, n_q)
     n = meta.size
     i = torch.arange(n, device="cuda")
@@ -27,7 +28,10 @@ def weights(cache, s, q, n_q, scale):
     seen = torch.where(is_cl, i == t, (i <= t) & (t <= torch.tensor(meta >> 1, device="cuda")))
     pos = cache.masked_reference_layout(s)["stored_pos"]
     qq = torch.stack([rotate(q[j], pos[n - n_q + j], cache.rotary_dim) for j in range(n_q)], 1)
-    z = torch.einsum("hqd,hnd->hqn", qq, rows_of(cache, s, n)[0][0].double()) * scale
+    k = rows_of(cache, s, n)[0][0].double()
+    z = torch.einsum("hqd,hnd->hqn", qq, k) * scale
+    if cache.rotary_dim:
+        z.masked_fill_(torch.isinf(k).any(-1)[:, None], NAN)
     w = torch.zeros_like(z)
     for j in range(n_q):
         w[:, j, seen[j]] = torch.softmax(z[:, j, seen[j]], -1)
@@ -62,3 +66,58 @@ def test_infinite_logit_of_a_prompt_query(n_q, d, dtype, rot):
     assert torch.isnan(ref[0]).all() and torch.isfinite(ref[1:]).all()
     agree(got, ref)
     assert cache.device_status() == 0
+
+
+def spanned(n, spans):
+    """Token kinds with spans [cl, cr]."""
+    kinds = np.zeros(n, np.uint8)
+    for cl, cr in spans:
+        kinds[cl], kinds[cr] = CL, CR
+    return kinds
+
+
+@pytest.mark.parametrize("n_q", WINDOWS)
+@pytest.mark.parametrize("d,dtype,rot", [(64, "f16", 64), (80, "bf16", 80), (96, "bf16", 0), (128, "f16", 0)])
+def test_prompt_queries_that_are_not_finite(n_q, d, dtype, rot):
+    """NaN and infinities in queries and keys: later rows, freed spans' interiors and <CL> rows' own weights stay numbers.
+    Heads: a NaN query; a NaN key that the last queries see; an infinite key in a span's interior, hidden from the
+    queries past its <CR>; logits that are all -infinity."""
+    kinds = spanned(700, [(100, 130), (300, 350), (650, 692)])
+    cache, g = make(1, 5, d, [700], dtype, rot, kinds=[kinds], seed=n_q + d)
+    cache.attach_scores()
+    q = torch.empty(n_q, 5, d, dtype=cache.torch_dtype, device="cuda").normal_(0.0, 2.0, generator=g)
+    k = rows_of(cache, 0, 700)[0][0]
+    q[n_q // 2, 0, d - 1] = NAN
+    q[-1, 0, 2] = NAN
+    k[1, 694, 5] = NAN
+    k[2, 660, 1] = INF
+    k[3] = k[3].abs()
+    q[n_q - 3, 3] = -INF
+    cache.score_prompt(0, q, [n_q], d ** -0.5)
+    seen, w = weights(cache, 0, q, n_q, d ** -0.5)
+    ref = w.sum(1)
+    got = per_row(cache, cache.scores, 0, 700)[0]
+    assert torch.isnan(ref[:4]).any(1).all() and torch.isfinite(ref[:3]).any(1).all() and torch.isfinite(ref[4]).all()
+    agree(got, ref)
+    assert cache.device_status() == 0
+
+
+@pytest.mark.parametrize("n_q", WINDOWS)
+def test_several_sequences_one_of_them_not_finite(n_q):
+    cache, g = make(1, 2, 64, [700, 90, 130], "f16", seed=4)
+    cache.attach_scores()
+    n = [n_q, min(n_q, 90), min(n_q, 130)]
+    q = torch.empty(sum(n), 2, 64, dtype=torch.float16, device="cuda").normal_(0.0, 2.0, generator=g)
+    q[n[0] + n[1] - 2, 1] = NAN  # of the second sequence
+    cache.score_prompt(0, q, n, 0.125)
+    at = 0
+    for s, m in enumerate(n):
+        rows = (700, 90, 130)[s]
+        ref = weights(cache, s, q[at:at + m], m, 0.125)[1].sum(1)
+        got = per_row(cache, cache.scores, s, rows)[0]
+        if s == 1:
+            agree(got, ref)
+        else:
+            assert torch.isfinite(got).all()
+            assert float(((got.double() - ref).abs() - RTOL * ref.abs()).max()) <= 1e-9
+        at += m
