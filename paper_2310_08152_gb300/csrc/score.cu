@@ -88,6 +88,7 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, NQ, PASS, QN>::CPS)
   __shared__ __align__(16) float s_neg[2][kRows];  // pass 1: -L of a tile's queries
   __shared__ __align__(16) uint32_t s_none[2][4];  // which of them have no part in the sums: <CL>, none and s_bad
   __shared__ __align__(16) uint32_t s_bad[2][4];   // whose weights are not numbers
+  __shared__ __align__(16) uint32_t s_cl[2][4];    // <CL>
   __shared__ float2 s_half[kRows];                 // results of the upper columns (kLse16: of 16 queries by eight warps)
   const uint32_t sm = (smem_addr(raw) + 1023u) & ~1023u;
   const int warp = uniform((int)(threadIdx.x >> 5)), lane = threadIdx.x & 31, tid = threadIdx.x;
@@ -241,6 +242,9 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, NQ, PASS, QN>::CPS)
       const int t0 = sq.q0 + un.qt * kRows, t1 = min(t0 + kRows, sq.len), t = t0 + r;  // the query's stored row
       const bool live = t < sq.len;
       const bool idle = t0 + (warp & 3) * 32 >= sq.len;  // none of the warp's queries exists
+      const bool is_cl = live && (a.meta[sq.moff + t] & 1);
+      // a <CL> query's sum is its own row's: the half that has this row begins anew there, the last that it sees
+      const bool mine_cl = is_cl && (t >> 6 & 1) == half && t / kRows >= un.kt0 && t / kRows < un.kt1;
       float m = -INFINITY, l = 0.f;
       for (int kt = un.kt0; kt < un.kt1; ++kt) {
         const int i0 = kt * kRows + half * 64;  // the row of the thread's first column
@@ -262,6 +266,12 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, NQ, PASS, QN>::CPS)
         if (i0 + 63 > t0) {  // later rows
           v0 &= low_bits(t - i0 + 1);
           v1 &= low_bits(t - i0 - 31);
+          if (mine_cl && (uint32_t)(t - i0) < 64u) {
+            v0 = low_bits(t - i0 + 1) & ~low_bits(t - i0);
+            v1 = low_bits(t - i0 - 31) & ~low_bits(t - i0 - 32);
+            m = -INFINITY;
+            l = 0.f;
+          }
         }
         const uint32_t step = kt - un.kt0;
         if (!(ok = s_wait(step))) break;
@@ -287,6 +297,10 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, NQ, PASS, QN>::CPS)
         l = l * ex2(m - mu) + ((sum0.x + sum0.y) + (sum1.x + sum1.y));
         m = mn;
       }
+      if (is_cl && !mine_cl) {
+        m = -INFINITY;
+        l = 0.f;
+      }
       if (half) s_half[r] = make_float2(m, l);
       bar_sync(1, kSThreads);
       if (!half && ok && live) {
@@ -303,15 +317,18 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, NQ, PASS, QN>::CPS)
         m[x] = -INFINITY;
         l[x] = 0.f;
       }
+      // the <CL> queries, which see their own rows alone
+      const uint32_t cl = __ballot_sync(0xFFFFFFFFu, lane < sq.len - sq.q0 && (a.meta[sq.moff + min(sq.q0 + lane, sq.len - 1)] & 1));
       for (int kt = un.kt0; kt < un.kt1; ++kt) {
         const uint32_t step = kt - un.kt0;
         if (!mine(step)) continue;
         const int i = kt * kRows + r, hid = i < sq.len ? a.meta[sq.moff + i] >> 1 : -1;
         const int lo = max(i - sq.q0, 0), hi = min(hid, sq.len - 1) - sq.q0;
+        const uint32_t others = cl & ~(low_bits(i - sq.q0 + 1) & ~low_bits(i - sq.q0));
         if (!(ok = s_wait(step))) break;
         take(step, 0);
         s_done(step);
-        hide((low_bits(hi + 1) & ~low_bits(lo)) | ~low_bits(QN), 0xFFFFFFFFu);
+        hide((low_bits(hi + 1) & ~low_bits(lo) & ~others) | ~low_bits(QN), 0xFFFFFFFFu);
 #pragma unroll
         for (int x = 0; x < QN; ++x) {
           const float z = s[x] * a.c2, mn = fmaxf(m[x], z), mu = mn == -INFINITY ? 0.f : mn;
@@ -341,11 +358,11 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, NQ, PASS, QN>::CPS)
         a.lse[((int64_t)un.split * a.H + h) * a.n_tok + sq.tok0 + tid] = make_float2(M, L);
       }
     } else {
-      // -L of query tile qt's r-th query; -infinity for a <CL> query and for none, NaN where its weights are not numbers:
-      // a logit is NaN or +infinity, or all are -infinity
+      // -L of query tile qt's r-th query; -infinity for none, NaN where its weights are not numbers: a logit is NaN or
+      // +infinity, or all are -infinity
       auto neg_lse = [&](int qt) -> float {
         const int x = qt * kRows + r;
-        if (sq.q0 + x >= sq.len || (a.meta[sq.moff + sq.q0 + x] & 1)) return -INFINITY;
+        if (sq.q0 + x >= sq.len) return -INFINITY;
         const float2* p = a.lse + (int64_t)h * a.n_tok + sq.tok0 + x;
         const int64_t step_s = (int64_t)a.H * a.n_tok;
         float M = -INFINITY, L = 0.f;
@@ -359,18 +376,24 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, NQ, PASS, QN>::CPS)
         return fabsf(lse) < INFINITY ? -lse : NAN;
       };
       pdl_wait();  // the queries' sums
-      auto load_neg = [&](float neg) {  // for the half's next step; its threads are done with the last one's
+      auto cl_query = [&](int qt) -> bool {  // and whether it is a <CL>
+        const int t = sq.q0 + qt * kRows + r;
+        return t < sq.len && (a.meta[sq.moff + t] & 1);
+      };
+      auto load_neg = [&](float neg, bool is_cl) {  // for the half's next step; its threads are done with the last one's
         bar_sync(1 + half, kSThreads / 2);
         // such a query's weight is NaN at the rows that it sees, and must not reach the others of its columns
         s_neg[half][r] = neg == neg ? neg : -INFINITY;
-        const uint32_t bad = __ballot_sync(0xFFFFFFFFu, neg != neg), none = __ballot_sync(0xFFFFFFFFu, neg == -INFINITY) | bad;
+        const uint32_t bad = __ballot_sync(0xFFFFFFFFu, neg != neg), none = __ballot_sync(0xFFFFFFFFu, neg == -INFINITY);
+        const uint32_t cl = __ballot_sync(0xFFFFFFFFu, is_cl);
         if (lane == 0) {
-          s_none[half][warp & 3] = none;
+          s_none[half][warp & 3] = none | bad | cl;
           s_bad[half][warp & 3] = bad;
+          s_cl[half][warp & 3] = cl;
         }
         bar_sync(1 + half, kSThreads / 2);
       };
-      if (PASS == kSumFew) load_neg(neg_lse(0));
+      if (PASS == kSumFew) load_neg(neg_lse(0), cl_query(0));
       uint32_t step = 0;
       for (int kt = un.kt0; kt < un.kt1; ++kt) {
         const int i = kt * kRows + r;
@@ -379,12 +402,16 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, NQ, PASS, QN>::CPS)
         float total = 0.f;
         bool any = false;  // the half had a step of this key tile
         [[maybe_unused]] float next = 0.f;
+        [[maybe_unused]] bool next_cl = false;
         const int qe = end_qt();
         for (int qt = first_qt(kt); qt < qe; ++qt, ++step) {
           if (!mine(step)) continue;
           if (PASS == kSumMany) {
-            load_neg(any ? next : neg_lse(qt));
-            if (qt + 2 < qe) next = neg_lse(qt + 2);
+            load_neg(any ? next : neg_lse(qt), any ? next_cl : cl_query(qt));
+            if (qt + 2 < qe) {
+              next = neg_lse(qt + 2);
+              next_cl = cl_query(qt + 2);
+            }
           }
           any = true;
           const int t0 = sq.q0 + qt * kRows, t1 = min(t0 + kRows, sq.len);
@@ -396,8 +423,10 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, NQ, PASS, QN>::CPS)
             const uint32_t b[4] = {bad.x, bad.y, bad.z, bad.w};
 #pragma unroll
             for (int c = 0; c < 4; ++c)
-              if (b[c] & low_bits(hi + 1 - 32 * c) & ~low_bits(lo - 32 * c)) total = NAN;
+              if (b[c] & low_bits(hi + 1 - 32 * c) & ~low_bits(lo - 32 * c) & ~s_cl[half][c]) total = NAN;
           }
+          if ((meta & 1) && i >= t0 && i < t1)  // a <CL> query's weight is its own row's: 1, whatever its logit, if that is finite
+            total += s_bad[half][(i - t0) >> 5] >> ((i - t0) & 31) & 1 ? NAN : 1.f;
 #pragma unroll 1
           for (int c = 0; c < QN; c += NC) {
             const uint32_t v0 = low_bits(hi + 1 - c) & ~low_bits(lo - c) & ~s_none[half][c / 32];
@@ -427,7 +456,6 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, NQ, PASS, QN>::CPS)
           any = !half;
         }
         if (any && ok && row) {
-          if ((meta & 1) && i >= sq.q0) total += 1.f;  // a <CL> query's weight is its own row's
           float* sc = a.scores + ((int64_t)a.layer * a.H * a.C + sq.row0 + (int64_t)h * sq.cap + i);
           *sc += total;
         }

@@ -121,3 +121,33 @@ def test_several_sequences_one_of_them_not_finite(n_q):
             assert torch.isfinite(got).all()
             assert float(((got.double() - ref).abs() - RTOL * ref.abs()).max()) <= 1e-9
         at += m
+
+
+@pytest.mark.parametrize("n_q", WINDOWS + [128])
+@pytest.mark.parametrize("d,dtype,rot", [(64, "f16", 0), (96, "bf16", 96), (128, "bf16", 0)])
+def test_cl_queries_that_are_not_finite(n_q, d, dtype, rot):
+    """A <CL> query's weight at its own row, the only one it sees, is 1 where its logit is finite, whatever the rows before
+    it hold, and NaN where it is not.  Heads: the query; its key; a NaN key before it, in a span's interior; nothing."""
+    spans = [(40, 70), (100, 127), (191, 250), (300, 350), (639, 660), (689, 690), (694, 697)]
+    kinds = spanned(700, spans)
+    cache, g = make(1, 4, d, [700], dtype, rot, kinds=[kinds], seed=n_q + d)
+    cache.attach_scores()
+    q = torch.empty(n_q, 4, d, dtype=cache.torch_dtype, device="cuda").normal_(0.0, 2.0, generator=g)
+    k = rows_of(cache, 0, 700)[0][0]
+    for cl, _ in spans[::2]:
+        if cl >= 700 - n_q:
+            q[cl - (700 - n_q), 0] = INF
+    q[694 - (700 - n_q), 0, 1] = NAN
+    k[1, 694, 3] = INF
+    k[2, 110, 0] = NAN
+    cache.score_prompt(0, q, [n_q], d ** -0.5)
+    ref = weights(cache, 0, q, n_q, d ** -0.5)[1].sum(1)
+    got = per_row(cache, cache.scores, 0, 700)[0]
+    assert torch.isnan(ref[0]).sum() == sum(c >= 700 - n_q for c in {694} | {c for c, _ in spans[::2]})
+    for h in range(4):
+        if torch.isnan(ref[h]).any():
+            agree(got[h], ref[h], f"head {h}")
+        else:
+            assert torch.isfinite(got[h]).all()
+            assert float(((got[h].double() - ref[h]).abs() - RTOL * ref[h].abs()).max()) <= 1e-9
+    assert cache.device_status() == 0
