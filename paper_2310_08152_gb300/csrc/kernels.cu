@@ -1044,7 +1044,8 @@ struct CtaCfg {
   static constexpr int OFF_Z = 2 * S * TILE;              // a row of zeros
   static constexpr int OFF_Q = OFF_Z + L::RB;             // [W][D] floats
   static constexpr int OFF_O = OFF_Q + W * D * 4;         // [2][W][PO] floats: the warps' results, by piece parity
-  static constexpr int OFF_C = OFF_O + 2 * W * PO * 4;    // [8][PO] floats: the cluster's results, in rank 0
+  // [8][PO] floats: the cluster's results, in rank 0 (the scored decode: their M, L and dead in every rank)
+  static constexpr int OFF_C = OFF_O + 2 * W * PO * 4;
   static constexpr int OFF_B = OFF_C + 8 * PO * 4;
   static constexpr int SMEM = OFF_B + 2 * S * 8;
   // resident CTAs per SM that the registers are cut for, as the shared memory (1 KB of it reserved
@@ -1487,7 +1488,8 @@ __global__ void __launch_bounds__((W + 1) * 32, SCORED && W == 4 ? 2 : CtaCfg<D,
       for (int e = lane;; e += 32) {
         const int x = e / C::WR * C::TR + jw + e % C::WR;
         if (e / C::WR * C::TR >= in_smem) break;
-        if (x >= in_smem) continue;
+        const int row = pc_r0 + x;
+        if (x >= in_smem || (row >= mlo && row < mhi)) continue;  // a hidden row gets nothing, not even a NaN
         const float w = exp2f(logits[x] - Mxu) * inv;
         if (w != 0.f) atomicAdd(sc + x, w);
       }

@@ -543,6 +543,8 @@ __global__ void __launch_bounds__(kOwnWarps * 32, 4) own_kernel(OwnArgs a) {
       const float Mu = M == -INFINITY ? 0.f : M, inv = 1.f / Ls;
       float* sc = a.scores + (int64_t)(p.layer + layer) * H * p.C + p.st.seq_row0[s] + (int64_t)h * p.st.cap[s] + d.begin;
       for (int x = lane; x < len - d.begin; x += 32) {  // written by this warp, before the barriers above
+        const int row = d.begin + x;
+        if (row >= d.mask_lo && row < d.mask_hi) continue;  // a hidden row gets nothing, not even a NaN
         const float w = exp2f(s_z[warp][x] - Mu) * inv;
         if (w != 0.f) atomicAdd(sc + x, w);
       }

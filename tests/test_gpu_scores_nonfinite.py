@@ -151,3 +151,48 @@ def test_cl_queries_that_are_not_finite(n_q, d, dtype, rot):
             assert torch.isfinite(got[h]).all()
             assert float(((got[h].double() - ref[h]).abs() - RTOL * ref[h].abs()).max()) <= 1e-9
     assert cache.device_status() == 0
+
+
+# few segments (a CTA or a cluster each), and thousands (a warp each)
+@pytest.mark.parametrize("M,H", [(1, 4), (30, 90)])
+@pytest.mark.parametrize("d,dtype", [(64, "f16"), (80, "bf16"), (128, "f16")])
+def test_decode_queries_that_are_not_finite(M, H, d, dtype):
+    """A step's weights: NaN at the rows that such a query sees, nothing at the hidden ones (a closed span that is not
+    freed), other heads and sequences untouched."""
+    kinds = [np.array([N] * 5 + [CL] + [N] * 150 + [CR, N, N], np.uint8), np.zeros(90, np.uint8)]
+    cache, g = make(M, H, d, [159, 90], dtype, kinds=kinds, seed=H)
+    sc = cache.attach_scores()
+    q = query(cache, g)
+    k = rows_of(cache, 0, 159)[0][0]
+    q[0, 0, 0, 0] = NAN
+    q[0, 0, 1, d - 1] = INF
+    k[2, 157, 5] = NAN
+    k[3, 30] = INF  # hidden
+    cache.decode_attention_scored(q, d ** -0.5)
+    assert (cache.last_decode_plan["mode"] == 2) == (M > 1)
+    seen = torch.tensor([i for i in range(159) if not 5 <= i < 156], device="cuda")
+    hidden = torch.arange(5, 156, device="cuda")
+    got = per_row(cache, sc, 0, 159)
+    assert torch.isnan(got[0, :3][:, seen]).all()
+    assert torch.all(got[:, :, hidden] == 0)
+    assert torch.isfinite(got[0, 3:]).all() and torch.isfinite(got[1:]).all()
+    for x in (got[0, 3:][:, seen], got[1:][:, :, seen], per_row(cache, sc, 1, 90)):
+        assert float((x.double().sum(-1) - 1).abs().max() if x.numel() else 0) <= 1e-5
+    w = torch.softmax(torch.einsum("d,nd->n", q[0, 0, 3].double(), k[3][seen].double()) * d ** -0.5, -1)
+    assert float(((got[0, 3][seen].double() - w).abs() - RTOL * w).max()) <= 1e-9
+
+
+def test_long_segment_of_a_query_that_is_not_finite():
+    """A cluster of CTAs, and rows past the logits that they hold."""
+    n = 90000
+    kinds = [np.array([N] * 40000 + [CL] + [N] * 45000 + [CR] + [N] * (n - 85002), np.uint8)]
+    cache, g = make(1, 2, 64, [n], kinds=kinds, seed=9)
+    sc = cache.attach_scores()
+    q = query(cache, g)
+    q[0, 0, 0, 7] = NAN
+    cache.decode_attention_scored(q, 0.125)
+    got = per_row(cache, sc, 0, n)[0]
+    assert torch.all(got[:, 40000:85001] == 0)
+    assert torch.isnan(got[0, :40000]).all() and torch.isnan(got[0, 85001:]).all()
+    assert abs(float(got[1].double().sum()) - 1) <= 1e-5
+    assert cache.device_status() == 0
