@@ -305,7 +305,7 @@ kvc_status kvc_decode_attention_scored(kvc_cache* cache, int first, int n_layers
  *     call's until it is complete on `stream`.
  * Every sum is made in one order.  A token whose logits hold a NaN or +infinity, or are all -infinity, makes
  * the scores of the rows that it sees NaN (a <CL> query its own), and of no others.  (Where the cache rotates, the query goes into the
- * products in parts, so that an infinite component of a stored key makes the logit NaN whatever its sign.)
+ * products in parts, so that an infinite component of a stored key may make a logit of -infinity NaN.)
  * Errors as kvc_prefill_attention's, and KVC_ERR_STATE without scores. */
 kvc_status kvc_score_scratch_bytes(kvc_cache* cache, const int32_t* n_q, size_t* bytes);
 kvc_status kvc_score_prompt(kvc_cache* cache, int layer, const void* q, const int32_t* n_q, float scale, void* scratch,

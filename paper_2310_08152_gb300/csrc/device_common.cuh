@@ -7,6 +7,7 @@
 #include <cuda_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 namespace kvc {
 
@@ -67,11 +68,16 @@ template <typename T>
 constexpr int kFullParts = 2;
 template <>
 constexpr int kFullParts<BF16T> = 3;
-template <typename T, int N>
+// With LARGE the first part ends at f16's largest value, so that the sum reaches twice that: two turned columns may be
+// sqrt(2) times the larger of them.  (What is past 65,504 has 11 bits, in steps of 16, where the query's own are of 32.)
+template <typename T, int N, bool LARGE = false>
 __device__ __forceinline__ void split_parts(float x, float y, uint32_t* part) {
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    part[i] = T::r2(x, y);
+    if constexpr (LARGE && std::is_same_v<T, F16T>)
+      part[i] = i == 0 ? T::r2(fminf(fmaxf(x, -65504.f), 65504.f), fminf(fmaxf(y, -65504.f), 65504.f)) : T::r2(x, y);
+    else
+      part[i] = T::r2(x, y);
     if (i + 1 < N) {
       const float2 back = T::f2(part[i]);
       x -= back.x;
@@ -106,8 +112,8 @@ __device__ __forceinline__ void query_chunk(const uint16_t* q, int c, int rot, i
     rope_sincos_full(pos, rope_g[i0 + 2 * e], &sn0, &cs0);
     rope_sincos_full(pos, rope_g[i0 + 2 * e + 1], &sn1, &cs1);
     uint32_t out[NQ];
-    split_parts<T, NQ>(first ? u.x * cs0 - v.x * sn0 : u.x * cs0 + v.x * sn0,
-                       first ? u.y * cs1 - v.y * sn1 : u.y * cs1 + v.y * sn1, out);
+    split_parts<T, NQ, true>(first ? u.x * cs0 - v.x * sn0 : u.x * cs0 + v.x * sn0,
+                             first ? u.y * cs1 - v.y * sn1 : u.y * cs1 + v.y * sn1, out);
 #pragma unroll
     for (int i = 0; i < NQ; ++i) part[i][e] = out[i];
   }
