@@ -22,6 +22,7 @@
 
 #include <atomic>
 #include <cstdint>
+#include <type_traits>
 
 #include "device_common.cuh"
 #include "kernels.hpp"
@@ -171,26 +172,32 @@ __global__ void __launch_bounds__(kThreads, D > 96 && MT > 1 ? 2 : MT == 1 && D 
       for (int n = 0; n < KG * 2; ++n)
 #pragma unroll
         for (int e = 0; e < 4; ++e) z[i][n][e] = 0.f;
+    // z += the product of parts [x0, x1); the small ones first, which the tensor cores would cut at the whole sum's last bit
+    auto add_parts = [&](auto x0c, auto x1c) {
+      constexpr int X0 = decltype(x0c)::value, NX = decltype(x1c)::value - X0;
 #pragma unroll
-    for (int kk = 0; kk < D / 16; ++kk) {
-      uint32_t a[NQ][WM][4];
+      for (int kk = 0; kk < D / 16; ++kk) {
+        uint32_t a[NX][WM][4];
 #pragma unroll
-      for (int x = 0; x < NQ; ++x)
+        for (int x = 0; x < NX; ++x)
 #pragma unroll
-        for (int i = 0; i < WM; ++i) ldsm4(a[x][i], q_addr + (x * C::R + i * 16) * C::RS + kk * 32);
+          for (int i = 0; i < WM; ++i) ldsm4(a[x][i], q_addr + ((X0 + x) * C::R + i * 16) * C::RS + kk * 32);
 #pragma unroll
-      for (int g = 0; g < KG; ++g) {
-        uint32_t b[4];
-        ldsm4(b, kt + g * 16 * C::RS + k_off + kk * 32);
+        for (int g = 0; g < KG; ++g) {
+          uint32_t b[4];
+          ldsm4(b, kt + g * 16 * C::RS + k_off + kk * 32);
 #pragma unroll
-        for (int x = 0; x < NQ; ++x)
+          for (int x = NX - 1; x >= 0; --x)
 #pragma unroll
-          for (int i = 0; i < WM; ++i) {
-            Mma<T>::go(z[i][2 * g], a[x][i], b[0], b[1]);
-            Mma<T>::go(z[i][2 * g + 1], a[x][i], b[2], b[3]);
-          }
+            for (int i = 0; i < WM; ++i) {
+              Mma<T>::go(z[i][2 * g], a[x][i], b[0], b[1]);
+              Mma<T>::go(z[i][2 * g + 1], a[x][i], b[2], b[3]);
+            }
+        }
       }
-    }
+    };
+    if constexpr (NQ > 1) add_parts(std::integral_constant<int, 1>{}, std::integral_constant<int, NQ>{});
+    add_parts(std::integral_constant<int, 0>{}, std::integral_constant<int, 1>{});
     const int left = n_keys - t * kKeys - kw * KG * 16;  // the warp's keys of this tile that exist
     const bool ragged = left < KG * 16;
     bool moved = false;

@@ -139,11 +139,11 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       const uint32_t k_d = desc_lo(sm + Cf::K_OFF + st * Cf::TILE, 16);
       if (elect_one()) {
 #pragma unroll
-        for (int part = 0; part < NQ; ++part) {
+        for (int part = NQ - 1; part >= 0; --part) {  // the small parts first: what is added to a sum is cut
 #pragma unroll
           for (int kk = 0; kk < D / 16; ++kk) {
             const uint32_t off = ((kk * 16) / SUB * Cf::SUBB + (kk * 16) % SUB * 2) >> 4;
-            tc_mma(tmem + sb * kRows, desc(q_d + part * (Cf::TILE >> 4) + off, SBO, SW), desc(k_d + off, SBO, SW), idS, part + kk > 0);
+            tc_mma(tmem + sb * kRows, desc(q_d + part * (Cf::TILE >> 4) + off, SBO, SW), desc(k_d + off, SBO, SW), idS, part < NQ - 1 || kk > 0);
           }
         }
         tc_commit(&s_full[sb]);

@@ -185,13 +185,13 @@ __global__ void __launch_bounds__(kScThreads, ScCfg<D, NQ, PASS, QN>::CPS)
         const uint32_t q_d = desc_lo(sm + Cf::Q_OFF + qs * Cf::QT, 16);
         if (elect_one()) {
 #pragma unroll
-          for (int part = 0; part < NQ; ++part) {
+          for (int part = NQ - 1; part >= 0; --part) {  // the small parts first: the tensor core cuts what it adds to a sum
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk) {
               const uint32_t off = ((kk * 16) / Cf::SUB * Cf::SUBB + (kk * 16) % Cf::SUB * 2) >> 4;
               const uint32_t qoff = ((kk * 16) / Cf::SUB * Cf::QSUBB + (kk * 16) % Cf::SUB * 2) >> 4;
               const uint64_t dk = desc(k_d + off, SBO, Cf::SW), dq = desc(q_d + part * (Cf::QTILE >> 4) + qoff, SBO, Cf::SW);
-              tc_mma(tmem + sb * kRows, PASS == kLse ? dq : dk, PASS == kLse ? dk : dq, id, part + kk > 0);
+              tc_mma(tmem + sb * kRows, PASS == kLse ? dq : dk, PASS == kLse ? dk : dq, id, part < NQ - 1 || kk > 0);
             }
           }
           tc_commit(&s_full[sb]);
