@@ -4,12 +4,18 @@
 // heads of 128, bf16: 312 us, its tensor pipe at 54 %, where the rows' bytes take 158; here 187), and these do four times as much.
 //
 // One CTA per SM.  Per tile of 128 rows: S = Q K^T into one of two TMEM buffers; eight warps take it, a query per thread
-// pair and 64 columns each, agree on the row's maximum through shared memory, and leave P as two 16-bit parts
-// in TMEM, over S; each part has a sum O += P V of its own.  The product of the next tile goes ahead of P V of this one.  P's reference is kept as in
-// prefix_kernel, so that O is rarely scaled.  K and V come by TMA through rings of two tiles; the queries, whose rows are
-// anywhere in the batch, are gathered (and rotated) by the warps.  Rows of V past the run's end are zeroed in shared
-// memory, for whatever they hold would meet P = 0.
-// What bounds it: HBM from 64 members up at 128 columns; the exponentials' warps below.
+// pair and 64 columns each, agree on the row's maximum through shared memory, and leave P in TMEM, as two 16-bit parts in
+// f16 (22 bits) and three in bf16 (24): the first two over S, the third beside it.  The product of the next tile goes ahead
+// of P V of this one.  P's reference is kept as in prefix_kernel, so that O is rarely scaled.  K and V come by TMA through
+// rings of two tiles; the queries, whose rows are anywhere in the batch, are gathered (and rotated) by the warps.  Rows of
+// V past the run's end are zeroed in shared memory, for whatever they hold would meet P = 0.
+//
+// The tensor core cuts what it adds rather than round it (16,384 rows in one sum: an error of 1.2e-5 of the output's
+// norm), so each tile's P V is a sum of its own, the small parts first, which the warps add to their columns of O in
+// registers: errors of 4e-7 to 9e-7, where two parts and sums of 2,048 rows in TMEM left 1.3e-6 to 4.6e-6 in bf16.  The
+// call of the case above, with two own rows a sample, takes 218 us (206 with two parts and long sums), in f16 192 (207); 4
+// layers of 32 heads of 64 in bf16 385 (325).  P written 32 columns at a time instead of 16 spills registers: 243.
+// What bounds it: HBM from 64 members up at 128 columns; the exponentials' warps below, and the third part's packing.
 #include <cuda.h>
 
 #include <atomic>
@@ -26,13 +32,7 @@ constexpr int kRows = 128;  // queries of a CTA, rows of a tile
 constexpr int kPWarps = 8;
 constexpr int kPThreads = kPWarps * 32;
 constexpr int kTcThreads = kPThreads + 64;
-// Tiles that go into one sum in TMEM.  The tensor core cuts what it adds rather than round it: 16,384 rows of both parts in
-// one sum left an error of 1.2e-5.  So the parts have a sum each, the small one's error being small, and after 2,048 rows
-// the sums are added to the part in memory.  (A third part of a bf16 P, which would take the output's error from 2e-6 to
-// 1e-6, made the case above 389 us.)
-constexpr int kSumTiles = 16;
-
-template <int D, int NQ>
+template <int D, int NQ, int NP>
 struct TcCfg {
   static constexpr int SW = (2 * D) % 128 == 0 ? 128 : (2 * D) % 64 == 0 ? 64 : 32;
   static constexpr int SUB = SW / 2;
@@ -45,9 +45,10 @@ struct TcCfg {
   static constexpr uint32_t K_OFF = TILE * NQ;
   static constexpr uint32_t V_OFF = K_OFF + KST * TILE;
   static constexpr uint32_t SMEM = V_OFF + VST * TILE + 1024;  // + aligning the base
-  // TMEM columns: two S tiles, each taken over by the two parts of its P, then O's sums, one for each part
-  static constexpr uint32_t O_COL = 256;
-  static_assert(SMEM <= 227 * 1024 - 3584 && O_COL + 2 * D <= 512, "shared memory, TMEM");
+  // TMEM columns: two S tiles, each taken over by the first two parts of its P, the third parts, then O of a tile
+  static constexpr uint32_t P2_COL = 256;
+  static constexpr uint32_t O_COL = P2_COL + (NP > 2 ? 2 * 64 : 0);
+  static_assert(SMEM <= 227 * 1024 - 3584 && O_COL + D <= 512, "shared memory, TMEM");
 };
 
 __device__ __forceinline__ void bar_sync(int id, int n) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n) : "memory"); }
@@ -55,7 +56,8 @@ __device__ __forceinline__ void bar_sync(int id, int n) { asm volatile("bar.sync
 template <typename T, int D, int NQ>
 __global__ void __launch_bounds__(kTcThreads, 1)
     prefix_tc_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, const PrefixArgs p) {
-  using Cf = TcCfg<D, NQ>;
+  constexpr int NP = kFullParts<T>;  // of P
+  using Cf = TcCfg<D, NQ, NP>;
   constexpr int SW = Cf::SW, SUB = Cf::SUB, KST = Cf::KST, VST = Cf::VST, CH = D / 8;
   extern __shared__ unsigned char raw[];
   __shared__ __align__(8) uint64_t k_full[KST], k_empty[KST], v_full[VST], v_empty[VST], s_full[2], q_full, p_full, pv_done;
@@ -164,11 +166,11 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       const uint32_t v_d = desc_lo(sm + Cf::V_OFF + st * Cf::TILE, Cf::SUBB);
       if (elect_one()) {
 #pragma unroll
-        for (int part = 0; part < 2; ++part) {
+        for (int part = NP - 1; part >= 0; --part) {
+          const uint32_t p_col = part < 2 ? (t & 1) * kRows + part * 64 : Cf::P2_COL + (t & 1) * 64;
 #pragma unroll
           for (int kk = 0; kk < kRows / 16; ++kk)
-            tc_mma_ts(tmem + Cf::O_COL + part * D, tmem + (t & 1) * kRows + part * 64 + 8 * kk, desc(v_d + kk * SW, SBO, SW), idO,
-                      t % kSumTiles + kk > 0);
+            tc_mma_ts(tmem + Cf::O_COL, tmem + p_col + 8 * kk, desc(v_d + kk * SW, SBO, SW), idO, part < NP - 1 || kk > 0);
         }
         tc_commit(&pv_done);
         tc_commit(&v_empty[st]);
@@ -208,37 +210,27 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     const int member = live ? p.members[un.mem0 + r] : 0;
     float* to = p.parts + (((int64_t)layer * p.n_parts + p.split0[member] + un.split) * p.H + h) * (D + 4);
     float m = -INFINITY, l = 0.f;
-    float m_sum = -INFINITY;  // the reference of the sum at `to`
-    // O, whose reference is `ref`, joined with the sum at `to`: stored, added without waiting for what is there, or, where
-    // the reference has moved, scaled and added.  (Read and written back each time:
-    // the case above 268 us, 257 so.)
-    auto add_o = [&](float ref, bool first) {
-      const float e = first ? 1.f : ex2(m_sum - ref);
-      const bool same = __all_sync(0xFFFFFFFFu, e == 1.f || !live);
-#pragma unroll 1
-      for (int c = half; c < D / 16; c += 2) {
-        float o[16], o1[16];
-        tmem_ld16(tmem + lanes + Cf::O_COL + c * 16, o);
-        tmem_ld16(tmem + lanes + Cf::O_COL + D + c * 16, o1);
-        tmem_wait_ld();
-        float4* at = reinterpret_cast<float4*>(to + 4 + c * 16);
+    // the thread's columns of O, 16 at a time: chunks half, half + 2, ..
+    constexpr int OC = (D / 16 + 1) / 2;
+    float o[OC][16];
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const float4 v = make_float4(o[4 * x] + o1[4 * x], o[4 * x + 1] + o1[4 * x + 1], o[4 * x + 2] + o1[4 * x + 2],
-                                       o[4 * x + 3] + o1[4 * x + 3]);
-          if (!live) continue;
-          if (first) {
-            at[x] = v;
-          } else if (same) {
-            asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(at + x), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w)
-                         : "memory");
-          } else {
-            const float4 old = __ldcg(at + x);
-            __stcg(at + x, make_float4(v.x + old.x * e, v.y + old.y * e, v.z + old.z * e, v.w + old.w * e));
-          }
+    for (int c = 0; c < OC; ++c)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) o[c][x] = 0.f;
+    auto add_o = [&]() {
+#pragma unroll
+      for (int c = 0; c < OC; ++c) {
+        if (half + 2 * c >= D / 16) break;
+        float v[16];
+        tmem_ld16(tmem + lanes + Cf::O_COL + (half + 2 * c) * 16, v);
+        tmem_wait_ld();
+#pragma unroll
+        for (int x = 0; x < 16; x += 2) {
+          const float2 sum = __fadd2_rn(make_float2(o[c][x], o[c][x + 1]), make_float2(v[x], v[x + 1]));
+          o[c][x] = sum.x;
+          o[c][x + 1] = sum.y;
         }
       }
-      m_sum = ref;
     };
     for (int t = 0; t < n_tiles; ++t) {
       float s[64];
@@ -276,7 +268,6 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       bar_sync(1, kPThreads);
       top = fmaxf(top, s_max[sb][half ^ 1][r]);
       float scale = 1.f;
-      const float m_old = m;
       const bool moved = top > m + 14.f;
       if (moved) {
         const float to = top - 6.f;
@@ -287,44 +278,39 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       if (ok) {
         float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
         tc_fence_after();
-        // the two parts over S, which both halves have read by now
+        // the first two parts over S, which both halves have read by now
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          uint32_t p0[16], p1[16];
+        for (int c = 0; c < 4; ++c) {
+          uint32_t pp[NP][8];
 #pragma unroll
-          for (int x = 0; x < 16; ++x) {
-            const int e = 32 * c + 2 * x;
+          for (int x = 0; x < 8; ++x) {
+            const int e = 16 * c + 2 * x;
             const float2 w = make_float2(ex2(s[e] - mu), ex2(s[e + 1] - mu));
             if (x & 1)
               sum1 = __fadd2_rn(sum1, w);
             else
               sum0 = __fadd2_rn(sum0, w);
-            uint32_t part[2];
-            split_parts<T, 2>(w.x, w.y, part);
-            p0[x] = part[0];
-            p1[x] = part[1];
+            uint32_t part[NP];
+            split_parts<T, NP>(w.x, w.y, part);
+#pragma unroll
+            for (int i = 0; i < NP; ++i) pp[i][x] = part[i];
           }
-          tmem_st16u(tmem + lanes + sb * kRows + half * 32 + 16 * c, p0);
-          tmem_st16u(tmem + lanes + sb * kRows + 64 + half * 32 + 16 * c, p1);
+#pragma unroll
+          for (int i = 0; i < NP; ++i)
+            tmem_st8u(tmem + lanes + (i < 2 ? sb * kRows + i * 64 : Cf::P2_COL + sb * 64) + half * 32 + 8 * c, pp[i]);
         }
         l = l * scale + ((sum0.x + sum0.y) + (sum1.x + sum1.y));
-        // O is free once the tile before is added
+        // O is free once that of the tile before is taken
         if (t > 0) ok = __all_sync(0xFFFFFFFFu, pf_wait(&pv_done, (t - 1) & 1, limit_ns));
       }
       if (ok) {
         tc_fence_after();
-        if (t > 0 && t % kSumTiles == 0) {  // the product of this tile begins a new sum
-          add_o(m_old, t == kSumTiles);
-        } else if (t > 0 && __any_sync(0xFFFFFFFFu, moved)) {
-#pragma unroll 1
-          for (int c = half; c < D / 8; c += 2) {
-            float o[16];
-            tmem_ld16(tmem + lanes + Cf::O_COL + c * 16, o);
-            tmem_wait_ld();
+        if (t > 0) add_o();
+        if (__any_sync(0xFFFFFFFFu, moved)) {
 #pragma unroll
-            for (int x = 0; x < 16; ++x) o[x] *= scale;
-            tmem_st16(tmem + lanes + Cf::O_COL + c * 16, o);
-          }
+          for (int c = 0; c < OC; ++c)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) o[c][x] *= scale;
         }
         if (t + 1 == n_tiles && n_keys % kRows != 0) {  // rows of V past the end
           const int st = t % VST, from = n_keys % kRows;
@@ -348,8 +334,17 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     bar_sync(1, kPThreads);
     tc_fence_after();
     if (ok) {
-      if (!half && live) *reinterpret_cast<float4*>(to) = make_float4(m, l + s_sum[r], 0.f, 0.f);
-      add_o(m, n_tiles <= kSumTiles);
+      add_o();
+      if (live) {
+        if (!half) *reinterpret_cast<float4*>(to) = make_float4(m, l + s_sum[r], 0.f, 0.f);
+#pragma unroll
+        for (int c = 0; c < OC; ++c) {
+          if (half + 2 * c >= D / 16) break;
+          float4* at = reinterpret_cast<float4*>(to + 4 + (half + 2 * c) * 16);
+#pragma unroll
+          for (int x = 0; x < 4; ++x) at[x] = make_float4(o[c][4 * x], o[c][4 * x + 1], o[c][4 * x + 2], o[c][4 * x + 3]);
+        }
+      }
     }
   }
   if (!ok) atomicOr(p.status, STATUS_TIMEOUT);
@@ -369,7 +364,7 @@ cudaError_t launch_tc_t(const PrefixMaps& maps, const PrefixArgs& a, cudaStream_
   if (e != cudaSuccess) return e;
   if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
   if (!done[dev].load(std::memory_order_acquire)) {
-    e = cudaFuncSetAttribute(prefix_tc_kernel<T, D, NQ>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TcCfg<D, NQ>::SMEM);
+    e = cudaFuncSetAttribute(prefix_tc_kernel<T, D, NQ>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TcCfg<D, NQ, kFullParts<T>>::SMEM);
     if (e != cudaSuccess) return e;
     done[dev].store(true, std::memory_order_release);
   }
@@ -379,7 +374,7 @@ cudaError_t launch_tc_t(const PrefixMaps& maps, const PrefixArgs& a, cudaStream_
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)((int64_t)a.n_units * a.H * a.n_layers));
   cfg.blockDim = dim3(kTcThreads);
-  cfg.dynamicSmemBytes = TcCfg<D, NQ>::SMEM;
+  cfg.dynamicSmemBytes = TcCfg<D, NQ, kFullParts<T>>::SMEM;
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -40,15 +40,16 @@ def shared_error(d, dtype, rot, n, members, M=1, H=2, own=2):
 
 
 @pytest.mark.parametrize("d,dtype,rot", TYPES)
-@pytest.mark.parametrize("members", [8, 24])
+@pytest.mark.parametrize("members", [8, 24, 40, 130])
 def test_shared_decode(members, d, dtype, rot):
     assert shared_error(d, dtype, rot, 5000, members) <= NORM
 
 
-@pytest.mark.parametrize("d,dtype,rot", [(64, "f16", 64), (128, "bf16", 128)])
-def test_shared_decode_of_whole_prefixes(d, dtype, rot):
+@pytest.mark.parametrize("d,dtype,rot", [(64, "f16", 64), (80, "bf16", 0), (128, "bf16", 128)])
+@pytest.mark.parametrize("members", [24, 40])
+def test_shared_decode_of_whole_prefixes(members, d, dtype, rot):
     """Heads and layers enough that a prefix is one run."""
-    assert shared_error(d, dtype, rot, 5000, 24, 10, 32) <= NORM
+    assert shared_error(d, dtype, rot, 5000, members, 10, 32) <= NORM
 
 
 @pytest.mark.parametrize("d,dtype,rot", TYPES)
