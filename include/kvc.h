@@ -340,7 +340,10 @@ kvc_status kvc_evict(kvc_cache* cache, const int64_t* keep, const int64_t* recen
  *     prefix is set or the cache is destroyed.
  * The prefix may grow, be compacted or evicted between calls, and outlives its use here; NULL for `prefix`
  * ends it (parent and scratch are then ignored).  Positions are the caller's: append the own tokens at the
- * positions that continue the prefix's. */
+ * positions that continue the prefix's.
+ * Prefixes do not nest: KVC_ERR_UNSUPPORTED for a cache that has a prefix itself, here and, where it got one
+ * later, in kvc_decode_attention_shared.  That call alone reads the prefix: every other one (the plain and the
+ * scored decodes, kvc_prefill_attention, kvc_score_prompt, kvc_evict) works on the cache's own rows. */
 size_t kvc_prefix_scratch_bytes(const kvc_cache* cache);
 kvc_status kvc_set_prefix(kvc_cache* cache, kvc_cache* prefix, const int32_t* parent, void* scratch,
                           size_t scratch_bytes);

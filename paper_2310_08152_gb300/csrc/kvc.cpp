@@ -1362,6 +1362,7 @@ kvc_status kvc_set_prefix(kvc_cache* c, kvc_cache* prefix, const int32_t* parent
       return ok();
     }
     if (prefix == c) return fail(KVC_ERR_INVALID_ARG, "a cache cannot be its own prefix");
+    if (prefix->prefix) return fail(KVC_ERR_UNSUPPORTED, "the prefix's cache has a prefix itself (kvc_set_prefix)");
     if (!parent || !scratch) return fail(KVC_ERR_INVALID_ARG, "parent/scratch are NULL");
     const kvc_config &a = c->cfg, &p = prefix->cfg;
     if (a.policy == KVC_POLICY_LOCAL || p.policy == KVC_POLICY_LOCAL)
@@ -1495,6 +1496,7 @@ kvc_status kvc_decode_attention_shared(kvc_cache* c, int first, int n_layers, co
     if ((reinterpret_cast<uintptr_t>(q) & 15) || (n_layers > 1 && q_layer_stride % 8 != 0))
       return fail(KVC_ERR_INVALID_ARG, "q must be 16-byte aligned, and so each layer's");
     const kvc_cache* p = c->prefix;
+    if (p->prefix) return fail(KVC_ERR_UNSUPPORTED, "the prefix's cache has a prefix itself (kvc_set_prefix)");
     if (first + n_layers > p->layers_done)
       return fail(KVC_ERR_STATE, "layer %d of the prefix's last tokens is not written yet", std::max(first, p->layers_done));
     for (int s = 0; s < c->cfg.b; ++s)

@@ -1,0 +1,61 @@
+"""Shared prefixes and scores, as far as the library checks them before any device work."""
+import numpy as np
+import pytest
+
+import paper_2310_08152_gb300 as kvc
+
+
+def cache(b=2, M=1, H=8, d=64):
+    """A cache's handle with buffers that nothing touches."""
+    cfg, _ = kvc.make_config(M, H, d, [16] * b, "f16", 0, 10000.0, kvc.POLICY_PAPER, 0.0)
+    cfg.k_base = cfg.v_base = cfg.pos_base = cfg.orig_base = cfg.workspace = 1 << 40
+    cfg.workspace_bytes = 1 << 40
+    return kvc.kvc_create(cfg)
+
+
+class Scratch:
+    """So much memory at an address."""
+
+    def __init__(self, n):
+        self.n = n
+
+    def numel(self):
+        return self.n
+
+    def element_size(self):
+        return 1
+
+    def data_ptr(self):
+        return 1 << 41
+
+
+def set_prefix(c, prefix):
+    kvc.kvc_set_prefix(c, prefix, [0, 1], Scratch(kvc.kvc_prefix_scratch_bytes(c)))
+
+
+def test_prefixes_do_not_nest():
+    a, b, c = cache(), cache(), cache()
+    set_prefix(b, c)
+    with pytest.raises(kvc.KvcError) as e:
+        set_prefix(a, b)
+    assert e.value.status == 2
+    kvc.kvc_set_prefix(b, None, None, None)
+    set_prefix(a, b)
+    for h in (a, b, c):
+        kvc.kvc_destroy(h)
+
+
+@pytest.mark.gpu
+def test_a_prefix_that_gets_one_later():
+    from _serving import make, query
+
+    (a, g), (b, _), (c, _) = (make(1, 2, 64, [5, 5], seed=i) for i in range(3))
+    q = query(a, g)
+    a.set_prefix(b, [0, 1])
+    ref = a.decode_attention_shared(q, 0.125)
+    b.set_prefix(c, [0, 1])
+    with pytest.raises(kvc.KvcError) as e:
+        a.decode_attention_shared(q, 0.125)
+    assert e.value.status == 2
+    b.set_prefix(None)
+    assert np.array_equal(a.decode_attention_shared(q, 0.125).cpu(), ref.cpu())
