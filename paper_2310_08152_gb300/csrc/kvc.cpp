@@ -1085,10 +1085,14 @@ kvc_status kvc_set_scores(kvc_cache* c, float* scores) {
   return ok();
 }
 
-// Checks the arguments of the decodes over several layers.
+// Checks the arguments of the decodes over several layers; *none: there is nothing to do.
 static kvc_status layers_check(kvc_cache* c, int first, int n_layers, const void* q, int64_t q_layer_stride, float scale,
-                               float* out, int64_t out_layer_stride) {
+                               float* out, int64_t out_layer_stride, bool* none) {
   if (!c) return fail(KVC_ERR_INVALID_ARG, "cache is NULL");
+  if (n_layers < 0 || first < 0 || first + n_layers > c->cfg.M)
+    return fail(KVC_ERR_INVALID_ARG, "layers [%d, %d) out of range [0, %d)", first, first + n_layers, c->cfg.M);
+  *none = n_layers == 0;
+  if (*none) return ok();
   const int64_t need = (int64_t)c->cfg.b * c->cfg.H * c->cfg.d_head;
   if (n_layers > 1 && (q_layer_stride < need || out_layer_stride < need))
     return fail(KVC_ERR_INVALID_ARG, "layer strides (%lld, %lld) below one layer's %lld elements",
@@ -1099,8 +1103,9 @@ static kvc_status layers_check(kvc_cache* c, int first, int n_layers, const void
 kvc_status kvc_decode_attention_scored(kvc_cache* c, int first, int n_layers, const void* q, int64_t q_layer_stride,
                                        float scale, float* out, int64_t out_layer_stride, void* stream_) {
   return guarded([&]() -> kvc_status {
-    kvc_status st = layers_check(c, first, n_layers, q, q_layer_stride, scale, out, out_layer_stride);
-    if (st != KVC_OK) return st;
+    bool none = false;
+    kvc_status st = layers_check(c, first, n_layers, q, q_layer_stride, scale, out, out_layer_stride, &none);
+    if (st != KVC_OK || none) return st;
     if (!c->scores) return fail(KVC_ERR_STATE, "the cache has no scores (kvc_set_scores)");
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     st = c->ensure_cuda(stream);
@@ -1490,8 +1495,9 @@ static kvc_status plan_prefix(kvc_cache* c, int n_layers, cudaStream_t stream) {
 kvc_status kvc_decode_attention_shared(kvc_cache* c, int first, int n_layers, const void* q, int64_t q_layer_stride,
                                        float scale, float* out, int64_t out_layer_stride, void* stream_) {
   return guarded([&]() -> kvc_status {
-    kvc_status st = layers_check(c, first, n_layers, q, q_layer_stride, scale, out, out_layer_stride);
-    if (st != KVC_OK) return st;
+    bool none = false;
+    kvc_status st = layers_check(c, first, n_layers, q, q_layer_stride, scale, out, out_layer_stride, &none);
+    if (st != KVC_OK || none) return st;
     if (!c->prefix) return fail(KVC_ERR_STATE, "the cache has no prefix (kvc_set_prefix)");
     if ((reinterpret_cast<uintptr_t>(q) & 15) || (n_layers > 1 && q_layer_stride % 8 != 0))
       return fail(KVC_ERR_INVALID_ARG, "q must be 16-byte aligned, and so each layer's");

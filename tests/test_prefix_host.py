@@ -59,3 +59,15 @@ def test_a_prefix_that_gets_one_later():
     assert e.value.status == 2
     b.set_prefix(None)
     assert np.array_equal(a.decode_attention_shared(q, 0.125).cpu(), ref.cpu())
+
+
+def test_decodes_of_no_layers_do_nothing():
+    """As the plain decode's, before anything else is looked at."""
+    h = cache(M=2)
+    lib, scale = kvc.lib(), 0.125
+    for call in (lib.kvc_decode_attention_layers, lib.kvc_decode_attention_scored, lib.kvc_decode_attention_shared):
+        for first in (0, 1, 2):
+            assert call(h, first, 0, None, 0, scale, None, 0, None) == 0
+        for first, n in ((0, -1), (-1, 0), (-1, 1), (3, 0), (1, 2)):
+            assert call(h, first, n, None, 0, scale, None, 0, None) == 1
+    kvc.kvc_destroy(h)
