@@ -1346,7 +1346,8 @@ kvc_status kvc_score_prompt(kvc_cache* c, int layer, const void* q, const int32_
 
 // The scratch of a shared-prefix decode: [units][members b][split0 b][n_split b], then the parts.  Units of one (layer,
 // head): at most one run per group of prefix_rows sequences, and kPrefixUnits more that splitting adds over all (layer,
-// head) pairs; parts: as many as sequences, layers and heads, and 128 for each run that splitting adds.
+// head) pairs; parts: as many as sequences, layers and heads, and for each run that splitting adds one for each of its
+// queries, of which a run has no more than the batch has sequences.
 static constexpr int64_t kPrefixUnits = 640;
 static size_t prefix_tables(int b) {
   return align_up(sizeof(kvc::PrefixUnit) * (size_t)(kPrefixUnits + b), 16) + 3 * align_up(4 * (size_t)b, 16);
@@ -1354,7 +1355,7 @@ static size_t prefix_tables(int b) {
 
 size_t kvc_prefix_scratch_bytes(const kvc_cache* c) {
   if (!c) return 0;
-  const int64_t rows = (int64_t)c->cfg.M * c->cfg.H * c->cfg.b + kvc::kPrefixTcRows * kPrefixUnits;
+  const int64_t rows = (int64_t)c->cfg.M * c->cfg.H * c->cfg.b + std::min(kvc::kPrefixTcRows, c->cfg.b) * kPrefixUnits;
   return align_up(prefix_tables(c->cfg.b), 256) + 4 * (size_t)rows * (size_t)(c->cfg.d_head + 4);
 }
 

@@ -71,3 +71,35 @@ def test_decodes_of_no_layers_do_nothing():
         for first, n in ((0, -1), (-1, 0), (-1, 1), (3, 0), (1, 2)):
             assert call(h, first, n, None, 0, scale, None, 0, None) == 1
     kvc.kvc_destroy(h)
+
+
+@pytest.mark.parametrize("b,M,H,d,most", [(2, 1, 8, 64, 1 << 19), (8, 1, 32, 128, 4 << 20), (64, 2, 32, 128, 27 << 20)])
+def test_scratch_is_of_the_batch_s_size(b, M, H, d, most):
+    """640 runs that splitting adds, of min(b, 128) queries each with d + 4 floats, besides M H b parts and the plan."""
+    h = cache(b, M, H, d)
+    n = kvc.kvc_prefix_scratch_bytes(h)
+    kvc.kvc_destroy(h)
+    parts = M * H * b + 640 * min(b, 128)
+    assert parts * 4 * (d + 4) <= n <= min(most, parts * 4 * (d + 4) + 32 * (640 + b) + 12 * b + 1024)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("members,n", [(1, 200000), (2, 150000), (17, 60000), (33, 60000), (129, 30000)])
+@pytest.mark.parametrize("M,H", [(1, 1), (1, 7)])
+def test_plans_fit_the_scratch(members, n, M, H):
+    """Few heads and a long prefix: as many runs as there may be; what lies behind the scratch is left alone."""
+    import torch
+
+    from _serving import query
+    from test_gpu_shared_prefix import check, pair
+
+    parent, own = [0] * members, [1] * members
+    prefix, c, g = pair(M, H, 64, [n], parent, own, seed=members)
+    need = kvc.kvc_prefix_scratch_bytes(c.handle)
+    memory = torch.full((need + 65536,), 77, dtype=torch.uint8, device="cuda")
+    kvc.kvc_set_prefix(c.handle, prefix.handle, parent, memory[:need])
+    q = query(c, g)
+    out = c.decode_attention_shared(q, 0.125)
+    check(prefix, c, parent, own, q, 0.125, out)
+    assert bool((memory[need:] == 77).all())
+    kvc.kvc_set_prefix(c.handle, None, None, None)
