@@ -136,7 +136,7 @@ cudaError_t launch_decode_scored(const Geometry& g, const Static& st, const Buff
 struct PrefixUnit {
   int32_t s;           // sequence of the prefix's cache
   int32_t key0, key1;  // its stored rows
-  int32_t mem0, n_mem; // members[mem0 ..], at most prefix_rows' answer of them
+  int32_t mem0, n_mem; // members[mem0 ..], as many as a CTA takes at most
   int32_t split;       // the run's number among the prefix's
   int32_t pad0, pad1;
 };
@@ -178,10 +178,16 @@ struct OwnArgs {
 // prefix; whether it is the one for them.
 bool own_scored_takes(int64_t n_segments, int64_t rows, int64_t max_segment, int num_sms);
 cudaError_t launch_own_scored(const Geometry& g, const OwnArgs& a, cudaStream_t stream, DecodePlan* plan);
-// Queries of one CTA where the largest group has `group` members (kPrefixTcRows: launch_prefix_tc, with maps of the
-// prefix's planes, else launch_prefix); CTAs per SM of that kernel.
+// Queries of one CTA (16 or 32: launch_prefix; kPrefixTcRows: launch_prefix_tc, with maps of the prefix's planes): as many
+// as the largest group of `group` members may need, or fewer in several CTAs, where most groups are small.  What a row
+// costs a CTA of so many queries, in twentieths of a row of 16 queries: all prefixes of one length, us with 16 / 32 / 128
+// queries: 16 groups of 8 and one of 33, d_head 80, f16, 548 / 828 / 833, d_head 128, bf16, 387 / 583 / 461; 8 of 8 and 8 of
+// 64 1321 / 1464 / 1214 and 707 / 835 / 466; 16 of 33 1437 / 1712 / 1178 and 842 / 1033 / 457; 4 of 8 and 4 of 40 501 / 641 /
+// 515 and 330 / 447 / 246.
 constexpr int kPrefixTcRows = 128;
 int prefix_rows(int group);
+inline int prefix_row_cost(int rows, int d_head) { return rows == 16 ? 20 : rows == 32 ? 31 : d_head == 128 ? 27 : 36; }
+// CTAs per SM of that kernel.
 cudaError_t prefix_ctas_per_sm(const Geometry& g, int device, int rows, int* occ);
 cudaError_t launch_prefix(const Geometry& g, const PrefixArgs& a, int device, int rows, cudaStream_t stream);
 struct alignas(64) PrefixMaps {

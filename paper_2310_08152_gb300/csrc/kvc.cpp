@@ -1345,7 +1345,7 @@ kvc_status kvc_score_prompt(kvc_cache* c, int layer, const void* q, const int32_
 }
 
 // The scratch of a shared-prefix decode: [units][members b][split0 b][n_split b], then the parts.  Units of one (layer,
-// head): at most one run per group of prefix_rows sequences, and kPrefixUnits more that splitting adds over all (layer,
+// head): at most one run for each CTA of a group, and kPrefixUnits more that splitting adds over all (layer,
 // head) pairs; parts: as many as sequences, layers and heads, and for each run that splitting adds one for each of its
 // queries, of which a run has no more than the batch has sequences.
 static constexpr int64_t kPrefixUnits = 640;
@@ -1405,7 +1405,19 @@ static kvc_status plan_prefix(kvc_cache* c, int n_layers, cudaStream_t stream) {
     largest = std::max(largest, (int)group[g].size());
     if (!group[g].empty()) longest = std::max(longest, c->prefix->bk.book.stored(g));
   }
-  const int rows = kvc::prefix_rows(largest);
+  // Queries of a CTA: those whose kernel takes the prefixes' rows, once per chunk of each group, in the least time
+  int rows = 0;
+  int64_t least = INT64_MAX;
+  for (int r : {16, 32, kvc::kPrefixTcRows}) {
+    int64_t cost = 0;
+    for (int g = 0; g < P; ++g)
+      if (!group[g].empty())
+        cost += c->prefix->bk.book.stored(g) * (int64_t)((group[g].size() + r - 1) / r) * kvc::prefix_row_cost(r, c->cfg.d_head);
+    if (cost < least && r <= kvc::prefix_rows(largest)) {
+      least = cost;
+      rows = r;
+    }
+  }
   int occ = 1;
   cudaError_t e = kvc::prefix_ctas_per_sm(c->geom(), c->device, rows, &occ);
   if (e != cudaSuccess) return cuda_fail(e, "prefix kernel");

@@ -279,3 +279,19 @@ def test_refusals():
     grown.append(new, new, [1], [0], layer=1)
     cache.decode_attention_shared(q, 0.125)
     assert cache.device_status() == 0
+
+
+@pytest.mark.parametrize("sizes,queries", [([33] + [8] * 16, 16), ([64] + [1] * 16, 16), ([33] + [32] * 16, 32), ([64] * 4, 64),
+                                           ([64] * 8 + [8] * 8, 64), ([20] + [3] * 9, 16), ([32] * 3, 32)])
+def test_groups_of_different_sizes(sizes, queries):
+    """One large group does not make the others' CTAs as wide as its own; the first unit of the plan is of the first group."""
+    parent = [g for g, n in enumerate(sizes) for _ in range(n)]
+    own = [1 + i % 3 for i in range(len(parent))]
+    lens = [130 + 7 * g for g in range(len(sizes))]
+    lens[0] = 200
+    prefix, cache, g = pair(1, 2, 64, lens, parent, own)
+    q = query(cache, g)
+    out = cache.decode_attention_shared(q, 0.125)
+    check(prefix, cache, parent, own, q, 0.125, out)
+    unit = cache._prefix_scratch.tensor[:32].view(torch.int32).tolist()  # prefix, rows, members' first and number, ..
+    assert unit[0] == 0 and unit[4] == queries
