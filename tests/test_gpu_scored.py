@@ -256,3 +256,21 @@ def test_refusals():
         local.attach_scores()
     assert e.value.status == 2
     assert torch.all(cache.scores == 0)
+
+
+@pytest.mark.parametrize("M,H,lens,mode", [(12, 16, [1, 2, 31, 33, 129, 1023, 400, 90, 700, 64, 5, 300, 12], 2), (2, 8, [3000, 50, 700], 4),
+                                           (1, 4, [5000], 1), (24, 16, [200, 200], 1)])
+def test_outputs_and_scores_repeat_bit_for_bit(M, H, lens, mode):
+    """Every sequence's, in a warp, a CTA or a cluster per segment; also where the scores are added to what is there."""
+    cache, g = make(M, H, 80, lens, "bf16", 80, seed=M)
+    q = query(cache, g)
+    runs = []
+    for _ in range(3):
+        cache.attach_scores()
+        a = cache.decode_attention_scored(q, 0.1)
+        assert cache.last_decode_plan["mode"] == mode
+        b = cache.decode_attention_scored(q, 0.1)
+        runs.append((a, b, cache.scores.clone()))
+    for run in runs[1:]:
+        assert all(torch.equal(x, y) for x, y in zip(run, runs[0]))
+    assert torch.equal(runs[0][0], runs[0][1])

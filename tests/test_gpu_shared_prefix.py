@@ -295,3 +295,35 @@ def test_groups_of_different_sizes(sizes, queries):
     check(prefix, cache, parent, own, q, 0.125, out)
     unit = cache._prefix_scratch.tensor[:32].view(torch.int32).tolist()  # prefix, rows, members' first and number, ..
     assert unit[0] == 0 and unit[4] == queries
+
+
+@pytest.mark.parametrize("members", [6, 20, 40, 130])
+@pytest.mark.parametrize("d,dtype,rot", [(64, "f16", 0), (64, "bf16", 64), (80, "bf16", 0), (96, "f16", 96), (128, "bf16", 128), (128, "f16", 0)])
+def test_what_lies_behind_the_rows_is_not_read(members, d, dtype, rot):
+    """Spare rows of K and V that hold NaN or infinities, behind prefixes whose ends lie in every part of a tile, and queries
+    that are not finite: each spoils its own output only.  For every kernel and swizzle."""
+    lens = [300, 129, 255, 64] if members < 130 else [300]
+    parent = [g for g in range(len(lens)) for _ in range(members)]
+    own = [1 + i % 3 for i in range(len(parent))]
+    prefix, cache, g = pair(1, 2, d, lens, parent, own, dtype, rot, spare=70, seed=members + d)
+    for c, stored in ((prefix, lens), (cache, own)):
+        for plane, what in ((c.k, float("nan")), (c.v, float("inf"))):
+            for s, n in enumerate(stored):
+                base, cap = c.H * int(c.offsets[s]), int(c.capacity[s])
+                rows = plane.view(-1, d)[base:base + 2 * cap].view(2, cap, d)
+                rows[0, n:], rows[1, n:] = what, float("nan")
+    q = query(cache, g)
+    clean = cache.decode_attention_shared(q, d ** -0.5)
+    check(prefix, cache, parent, own, q, d ** -0.5, clean)
+    bad = q.clone()
+    spoilt = [(2, 0), (members // 2, 1), (members - 1, 1)]
+    for (s, h), what in zip(spoilt, (float("nan"), float("inf"), float("-inf"))):
+        bad[0, s, h, 5] = what
+    out = cache.decode_attention_shared(bad, d ** -0.5)
+    for s in range(len(parent)):
+        for h in range(2):
+            if (s, h) in spoilt:
+                assert torch.isnan(out[0, s, h]).all()
+            else:
+                assert torch.equal(out[0, s, h], clean[0, s, h])
+    assert cache.device_status() == 0
