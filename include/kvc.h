@@ -306,7 +306,8 @@ kvc_status kvc_decode_attention_scored(kvc_cache* cache, int first, int n_layers
  * Every sum is made in one order.  A token whose logits hold a NaN or +infinity, or are all -infinity, makes
  * the scores of the rows that it sees NaN (a <CL> query its own), and of no others.  (Where the cache rotates, the query goes into the
  * products in parts, so that an infinite component of a stored key may make a logit of -infinity NaN.)
- * Errors as kvc_prefill_attention's, and KVC_ERR_STATE without scores. */
+ * Errors as kvc_prefill_attention's, and KVC_ERR_STATE without scores, or on a stream that is being captured
+ * unless the same call (rows and n_q) was made before the capture. */
 kvc_status kvc_score_scratch_bytes(kvc_cache* cache, const int32_t* n_q, size_t* bytes);
 kvc_status kvc_score_prompt(kvc_cache* cache, int layer, const void* q, const int32_t* n_q, float scale, void* scratch,
                             size_t scratch_bytes, void* stream);
@@ -353,7 +354,8 @@ kvc_status kvc_set_prefix(kvc_cache* cache, kvc_cache* prefix, const int32_t* pa
  * rows those that the decode shows it.  Sequences without own tokens are skipped.  q and each layer's part of
  * it are 16-byte aligned.
  * Errors, besides the decode's: KVC_ERR_STATE without a prefix, where a prefix has a span that is open or
- * closed and not freed, or where its layers are not written. */
+ * closed and not freed, where its layers are not written, or on a stream that is being captured unless a call
+ * over these rows of the prefix and as many layers was made before the capture. */
 kvc_status kvc_decode_attention_shared(kvc_cache* cache, int first, int n_layers, const void* q, int64_t q_layer_stride,
                                        float scale, float* out, int64_t out_layer_stride, void* stream);
 

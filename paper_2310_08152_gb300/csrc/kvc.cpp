@@ -1186,8 +1186,17 @@ kvc_status kvc_score_scratch_bytes(kvc_cache* c, const int32_t* n_q, size_t* byt
   return ok();
 }
 
+// A plan's upload in a capture would read the staging ring at each replay, after other uploads have gone through it.
+static kvc_status outside_capture(cudaStream_t stream) {
+  cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+  if (cudaStreamIsCapturing(stream, &status) != cudaSuccess) (void)cudaGetLastError();  // the upload itself will tell
+  if (status == cudaStreamCaptureStatusNone) return KVC_OK;
+  return fail(KVC_ERR_STATE, "the stream is being captured and this call's plan is not on the device: make the call once before");
+}
+
 // Builds and uploads the plan of a prompt's scores.
 static kvc_status plan_score(kvc_cache* c, const int32_t* n_q, int n_split, cudaStream_t stream) {
+  if (const kvc_status st = outside_capture(stream); st != KVC_OK) return st;
   const int b = c->cfg.b, H = c->cfg.H;
   std::vector<kvc::ScoreSeq> seqs;
   std::vector<kvc::ScoreUnit> u0, u1;
@@ -1395,6 +1404,7 @@ kvc_status kvc_set_prefix(kvc_cache* c, kvc_cache* prefix, const int32_t* parent
 
 // Cuts the prefixes' rows into runs and uploads the plan (units, members, each sequence's parts).
 static kvc_status plan_prefix(kvc_cache* c, int n_layers, cudaStream_t stream) {
+  if (const kvc_status st = outside_capture(stream); st != KVC_OK) return st;
   const int b = c->cfg.b, P = c->prefix->cfg.b;
   std::vector<std::vector<int32_t>> group(P);
   for (int s = 0; s < b; ++s)

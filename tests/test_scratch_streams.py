@@ -267,3 +267,35 @@ def test_shared_decode_in_a_graph():
         torch.cuda.synchronize()
         assert torch.equal(out, ref)
     assert own.device_status() == 0
+
+
+@pytest.mark.gpu
+def test_a_plan_is_not_uploaded_in_a_capture():
+    """The shared decode and the prompt scores refuse a capture whose plan is not on the device yet; the capture goes on."""
+    prefix, own, q = _samples()
+    own.set_prefix(prefix, [0] * 8)
+    ref = own.decode_attention_shared(q, 0.125)
+    one = own.decode_attention_shared(q[:1].contiguous(), 0.125, n_layers=1)
+    torch.cuda.synchronize()
+    graph, out = torch.cuda.CUDAGraph(), torch.zeros_like(one)
+    part, all_out = q[:1].contiguous(), torch.zeros_like(ref)
+    prefix.attach_scores()
+    window = torch.zeros(9, 8, 64, dtype=torch.float16, device="cuda")
+    prefix.score_prompt(0, window, [9], 0.125)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        own.decode_attention_shared(part, 0.125, out=out, n_layers=1)
+        with pytest.raises(kvc.KvcError) as e:  # a plan for another number of layers
+            own.decode_attention_shared(q, 0.125, out=all_out)
+        assert e.value.status == 5
+        with pytest.raises(kvc.KvcError) as e:  # other queries
+            prefix.score_prompt(0, window[:8], [8], 0.125)
+        assert e.value.status == 5
+        prefix.score_prompt(0, window, [9], 0.125)
+    before = prefix.scores.clone()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, one) and torch.all(all_out == 0)
+    assert abs(float((prefix.scores - before).double().sum()) - 9 * 8) <= 1e-3
+    assert torch.equal(own.decode_attention_shared(q, 0.125), ref)
+    assert own.device_status() == 0 and prefix.device_status() == 0
