@@ -323,6 +323,9 @@ kvc_status kvc_score_prompt(kvc_cache* cache, int layer, const void* q, const in
  * stay beyond it; the recent rows follow in their order.  pos and orig of the rows below the recent ones
  * become -1.  Attention, appends, spans among the recent and later tokens, compaction and prefills of later
  * tokens work on as before.
+ * "Last" is by place: rows below the recent ones of an earlier call are no longer in the order of their tokens,
+ * so where `recent` reaches past those that were recent then and those appended since, it keeps the rows that
+ * happen to lie there.
  * Errors: KVC_ERR_STATE without scores, with layers of the last tokens not written, or where an open span
  * or one that is closed and not freed reaches before the recent rows; KVC_ERR_UNSUPPORTED under
  * KVC_POLICY_LOCAL. */

@@ -668,7 +668,8 @@ class KVCache:
     def evict(self, keep, recent, kept=None, stream=None):
         """Brings every (layer, head) stream of the sequences with keep >= 0 down to `keep` rows: its last `recent` ones
         and those with the largest scores.  keep, recent: a number, or one per sequence; kept: int32 [M, H * C] for the
-        earlier number of each row that is left."""
+        earlier number of each row that is left.  "Last" is by place: a larger `recent` than an earlier call's reaches
+        into rows that are no longer in the order of their tokens."""
         if kept is not None:
             import torch
 
