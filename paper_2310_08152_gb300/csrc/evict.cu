@@ -238,7 +238,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 128 ? 7 : 1024 / kThread
           if (pass == 0 || k >> hi == prefix) atomicAdd(&sh.hist[(k >> shift) & mask], 1u);
         }
         __syncthreads();
-        // thread t holds the eight bins from the (t + 1)-th eight from the top down
+        // thread t holds the t-th `per` bins from the top down
         const int per = kBins / kThreads, top = kBins - 1 - tid * per;
         uint32_t c[kBins / kThreads], mine = 0;
 #pragma unroll

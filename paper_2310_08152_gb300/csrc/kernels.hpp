@@ -326,7 +326,7 @@ struct alignas(64) ScoreMaps {
 int score_parts(const Geometry& g);
 // Resident CTAs per SM of the passes' kernels (sizes the units).
 int score_ctas_per_sm(const Geometry& g);
-// Rotates a.q into a.q_part (n_qt 128-query tiles: the first pass's units with split 0).
+// Rotates a.q into a.q_part, the query tile of each of the first pass's units with split 0 (the others' blocks end at once).
 cudaError_t launch_score_rotate(const Geometry& g, const ScoreArgs& a, cudaStream_t stream);
 // The passes; most: the most queries of a sequence.  The boxes of the query maps hold score_query_rows(most) tokens.
 inline int score_query_rows(int most) { return most <= 16 ? 16 : 128; }

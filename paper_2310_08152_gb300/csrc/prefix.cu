@@ -26,6 +26,7 @@
 
 #include "device_common.cuh"
 #include "kernels.hpp"
+#include "tensor_core.cuh"
 
 namespace kvc {
 namespace {
@@ -64,11 +65,6 @@ __device__ __forceinline__ void ldsm4t(uint32_t* r, uint32_t addr) {
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
                : "r"(addr)
                : "memory");
-}
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
 }
 
 template <typename T>

@@ -51,8 +51,6 @@ struct TcCfg {
   static_assert(SMEM <= 227 * 1024 - 3584 && O_COL + D <= 512, "shared memory, TMEM");
 };
 
-__device__ __forceinline__ void bar_sync(int id, int n) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n) : "memory"); }
-
 template <typename T, int D, int NQ>
 __global__ void __launch_bounds__(kTcThreads, 1)
     prefix_tc_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, const PrefixArgs p) {
