@@ -17,7 +17,8 @@
 // bits) and three in bf16 (24), for the output is in 32 bits.  (With two of bf16 its error was 2.3e-6 where 32-bit
 // arithmetic leaves 4e-7.)  P's reference is 2^6 to 2^14 below the running maximum, which keeps f16's low part out of its
 // subnormal range and makes rescaling rare.  The tensor cores cut what they add rather than round it, which over thousands
-// of rows adds up (29,706 rows, 2,048 into a sum: 5.5e-6): here they sum 16 rows at a time, and the sums are added outside.
+// of rows adds up (29,706 rows, 2,048 into a sum: 5.5e-6): here they sum 16 rows at a time, and the sums are added outside;
+// and a logit's small parts come before its large one (after it: 2.1e-6 at d_head 128 in bf16, 7e-7 so).
 #include <cuda_runtime.h>
 
 #include <atomic>
@@ -663,8 +664,8 @@ cudaError_t launch_own(const Geometry& g, const OwnArgs& a, int64_t max_segment,
 }
 
 // A warp for each segment where there are many short ones, else the CTAs of the scored decode.  us with CTAs -> with warps,
-// f16, d_head 64: 12,288 segments of 95 rows 73.8 -> 50.1 (what they read and write would take 45.5), of 200 rows 123 ->
-// 98.6, of 400 rows 224 -> 185, of 700 rows 335 -> 326, of 1,024 rows 463 -> 485; d_head 128, bf16: of 120 rows 138 -> 126,
+// f16, d_head 64: 12,288 segments of 95 rows 80 -> 51 (what they read and write would take 45.5), of 200 rows 129 -> 100,
+// of 400 rows 224 -> 187, of 700 rows 335 -> 326, of 1,024 rows 463 -> 485; d_head 128, bf16: of 120 rows 139 -> 127,
 // 6,144 of 700 rows 318 -> 343.  Fewer segments leave warps without work: 1,280 of 300 rows 20.6 -> 21.2 (d_head 128: 35.4
 // -> 44.3), 512 of 100 rows 4.7 -> 6.9.
 bool own_scored_takes(int64_t n_segments, int64_t rows, int64_t max_segment, int num_sms) {

@@ -1,7 +1,7 @@
 // The prefix part of a shared-prefix decode for large groups, on the fifth-generation tensor cores: up to 128 members'
 // queries of one (layer, head) against a run of the prefix's rows.  What it computes and leaves is prefix_kernel's
 // (prefix.cu); past 32 members the 16 x 8 x 16 instructions bound that kernel (64 samples of 32,768 rows, two layers of 32
-// heads of 128, bf16: 312 us, its tensor pipe at 54 %, where the rows' bytes take 158; here 187), and these do four times as much.
+// heads of 128, bf16: 312 us, its tensor pipe at 54 %, where the rows' bytes take 158; here 206), and these do four times as much.
 //
 // One CTA per SM.  Per tile of 128 rows: S = Q K^T into one of two TMEM buffers; eight warps take it, a query per thread
 // pair and 64 columns each, agree on the row's maximum through shared memory, and leave P in TMEM, as two 16-bit parts in
@@ -15,7 +15,8 @@
 // registers: errors of 4e-7 to 9e-7, where two parts and sums of 2,048 rows in TMEM left 1.3e-6 to 4.6e-6 in bf16.  The
 // call of the case above, with two own rows a sample, takes 218 us (206 with two parts and long sums), in f16 192 (207); 4
 // layers of 32 heads of 64 in bf16 385 (325).  P written 32 columns at a time instead of 16 spills registers: 243.
-// What bounds it: HBM from 64 members up at 128 columns; the exponentials' warps below, and the third part's packing.
+// What bounds it: the products (the tensor pipe is at 56 % in that case) and the warps that make P, a third part of it in
+// bf16, by turns; HBM is at 5.2 TB/s.
 #include <cuda.h>
 
 #include <atomic>
