@@ -113,7 +113,8 @@ class _Memory:
             return
         import torch
 
-        stream = torch.cuda.ExternalStream(handle, device=self.tensor.device)
+        device = self.tensor.device  # ExternalStream(0) would be a new stream
+        stream = torch.cuda.ExternalStream(handle, device=device) if handle else torch.cuda.default_stream(device)
         if self.made is not None:
             with torch.cuda.stream(stream):
                 capturing = torch.cuda.is_current_stream_capturing()

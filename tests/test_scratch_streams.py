@@ -8,7 +8,7 @@ import torch
 
 import paper_2310_08152_gb300 as kvc
 
-HERE, SIDE = 1, 2  # the current stream's handle and another's
+HERE, SIDE, DEFAULT = 1, 2, 0  # the current stream's handle, another's and the default stream's
 
 
 class Pool:
@@ -49,7 +49,7 @@ class Pool:
 
         class Stream:
             def __init__(self, handle, device=None):
-                self.cuda_stream = handle
+                self.cuda_stream = handle or 1000  # as torch does: a new stream where the handle is 0
 
             def wait_event(self, event):
                 pool.log.append(("waits", self.cuda_stream))
@@ -67,7 +67,10 @@ class Pool:
                 current.at = self.old
 
         self.current = current
+        default = Stream(1)
+        default.cuda_stream = DEFAULT
         cuda = types.SimpleNamespace(Event=Event, ExternalStream=Stream, stream=current, synchronize=lambda d=None: None,
+                                     default_stream=lambda device=None: default,
                                      current_device=lambda: 0, is_current_stream_capturing=lambda: current.at in pool.capturing)
         monkeypatch.setattr(torch, "cuda", cuda)
         monkeypatch.setattr(torch, "empty", lambda n, **kw: Tensor(n))
@@ -154,6 +157,14 @@ def test_scores_that_are_replaced(pool, call):
     pool.before(("waits", SIDE), ("told", 0, SIDE))
 
 
+def test_the_default_stream_is_one_too(pool, prefix):
+    c = pool.cache()
+    c.set_prefix(prefix, [0, 0])
+    c.decode_attention_shared(None, 1.0, out=object(), stream=DEFAULT)
+    c.set_prefix(None)
+    pool.before(("waits", DEFAULT), ("told", 0, DEFAULT), ("dropped", 0))
+
+
 def test_stream_is_ordered_once(pool, prefix):
     c = pool.cache()
     c.set_prefix(prefix, [0, 0])
@@ -199,6 +210,27 @@ def test_prefix_dropped_behind_a_decode_on_another_stream(again):
     own.set_prefix(prefix if again else None, [0] * 8)
     # what the pool gives out now is written on the current stream at once
     taken = [torch.full((kvc.kvc_prefix_scratch_bytes(own.handle),), 255, dtype=torch.uint8, device="cuda") for _ in range(3)]
+    torch.cuda.synchronize()
+    assert torch.equal(out, ref) and all(bool((t == 255).all()) for t in taken)
+    assert own.device_status() == 0
+
+
+@pytest.mark.gpu
+def test_prefix_made_and_dropped_on_another_stream_than_the_decode_s():
+    """Made on a side stream, used on the default one, dropped and its memory given out again on the side stream."""
+    prefix, own, q = _samples()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        own.set_prefix(prefix, [0] * 8)
+    ref = own.decode_attention_shared(q, 0.125)
+    out = torch.empty_like(ref)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(20_000_000)
+    own.decode_attention_shared(q, 0.125, out=out)
+    own.set_prefix(None)
+    n = kvc.kvc_prefix_scratch_bytes(own.handle)
+    with torch.cuda.stream(side):
+        taken = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for _ in range(3)]
     torch.cuda.synchronize()
     assert torch.equal(out, ref) and all(bool((t == 255).all()) for t in taken)
     assert own.device_status() == 0
