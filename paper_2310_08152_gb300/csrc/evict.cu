@@ -369,7 +369,10 @@ __global__ void __launch_bounds__(kThreads, kThreads == 128 ? 7 : 1024 / kThread
       if (do_v) bulk_s2g(V + (int64_t)(A + r) * VPR, dyn + (CN > 1 ? 0 : (size_t)chunk * D * 2), bytes);
       asm volatile("cp.async.bulk.commit_group;" ::: "memory");
     }
-    if (!ok) atomicOr(buf.status, STATUS_TIMEOUT);
+    if (!ok) {
+      atomicOr(buf.status, STATUS_TIMEOUT);
+      (void)mbar_wait_bounded(&sh.full, phase, 2000000000ull);  // never leave with a copy in flight
+    }
     asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   }
   if (rank == 0) {

@@ -35,3 +35,12 @@ def test_decode_lanes_agree_on_a_wait_and_a_dead_part_is_not_merged():
     assert "st_cluster_f32(dst + 2, 0, bad);" in cta
     stores = re.findall(r"if \(([^;{}]*)\) orow\[", cta)
     assert stores and all("bad == 0.f" in s for s in stores), stores
+
+
+def test_eviction_waits_again_for_its_copy_before_it_ends():
+    src = _source("evict.cu")
+    waits = [m.start() for m in re.finditer(r"mbar_wait_bounded\(&sh\.full, phase, ", src)]
+    assert len(waits) == 2, waits
+    assert src[:waits[0]].endswith("if (!(ok = ")  # its verdict ends the loop that stores what was loaded
+    end = src[waits[0]:waits[1]]
+    assert "break;" in end and "if (!ok) {" in end and "STATUS_TIMEOUT" in end  # reported, and waited for once more
