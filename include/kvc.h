@@ -20,6 +20,8 @@
  *   kvc_decode_attention_scored, kvc_score_prompt, kvc_evict   attention weights summed for each row, and rows that
  *                         leave the cache by them
  *   kvc_set_prefix, kvc_decode_attention_shared   sequences (samples of a prompt) over rows that they share (Sec. 4.2)
+ *   kvc_copy, kvc_truncate  sequences forked, moved to another cache, cut back and freed; with kvc_config.bits = 4 a cache
+ *                         holds, appends to and decodes over rows of 4 bits
  *   kvc_masked_reference_layout   the full history, the mask and the stored rows, for verification
  * plus a host-only span book (kvc_book_*) holding the span bookkeeping that
  * decides what each call does.
@@ -122,6 +124,10 @@ kvc_status kvc_book_compress(kvc_book* book, const int32_t* seq, const int64_t* 
 /* The bookkeeping of kvc_evict (same arguments, checks and errors). */
 kvc_status kvc_book_evict(kvc_book* book, const int64_t* keep, const int64_t* recent);
 
+/* The bookkeeping of kvc_truncate and kvc_copy (same arguments, checks and errors). */
+kvc_status kvc_book_truncate(kvc_book* book, const int64_t* tokens);
+kvc_status kvc_book_copy(kvc_book* book, const kvc_book* from, int n, const int32_t* dst, const int32_t* src);
+
 /* Closed spans of `seq` that are not yet freed: up to `max` (cl, cr) pairs; *n gets the count. */
 kvc_status kvc_book_pending_spans(const kvc_book* book, int seq, int64_t* cl, int64_t* cr, int64_t max,
                                   int64_t* n);
@@ -177,6 +183,19 @@ typedef struct {
   void* workspace;              /* device scratch owned by the cache while it lives */
   size_t workspace_bytes;
   float local_ratio;            /* KVC_POLICY_LOCAL only: r in [0, 1); the window is ~(1 - r) of the history */
+  /* Bits of a stored element: 16 (or 0), or 4.  In 4 bits a K or V row (K rotated and rounded to `dtype` first) is held in
+   * groups of 32 columns, the last one of 16 where d_head is 80.  A group has its least value lo and a step, both of `dtype`:
+   *   step = (greatest - lo) / 15 rounded up to that type, or 0 where that quotient is below 2^-126,
+   *   code = (x - lo) (1 / step) to the nearest whole number, ties to even (0 where step is 0),
+   * with difference, quotients and product rounded to binary32; a column stands for lo + step code, which is within step / 2
+   * (1 + 2^-20) of x (where step is 0, within 15 x 2^-126).  A group that holds a NaN or an infinity, or whose range overflows, reads as NaN.
+   * Layout: the codes [M][H * C] rows of d_head / 2 bytes, column c in bits 4 (c % 2) of byte c / 2; 256-byte aligned behind
+   * them the groups' pairs, [M][H * C] rows of (step, lo) pairs of `dtype`.  C and off are those of capacities rounded up to
+   * multiples of 4 rows (so are pos and orig).
+   * Such a cache has kvc_append and its variants, kvc_compress_spans, kvc_decode_attention and kvc_decode_attention_layers,
+   * kvc_copy and kvc_truncate; what else reads or moves rows, and kvc_set_scores, is KVC_ERR_UNSUPPORTED: copy the sequences
+   * into a cache of 16 bits.  Not with KVC_POLICY_LOCAL. */
+  int bits;
 } kvc_config;
 
 /* Byte sizes of the caller-owned buffers for `cfg` (k_base etc. may be NULL).  Any out pointer may
@@ -362,6 +381,35 @@ kvc_status kvc_set_prefix(kvc_cache* cache, kvc_cache* prefix, const int32_t* pa
 kvc_status kvc_decode_attention_shared(kvc_cache* cache, int first, int n_layers, const void* q, int64_t q_layer_stride,
                                        float scale, float* out, int64_t out_layer_stride, void* stream);
 
+/* ------------------------------------------------------------------------ */
+/* Sequences copied, cut back and freed.                                      */
+/* ------------------------------------------------------------------------ */
+
+/* Sequence dst[i] of `cache` becomes a copy of sequence src[i] of `from` (i < n), which may be the same cache: its stored
+ * rows of every layer, their positions and history indices, its history, spans and lengths.  What dst[i] held is gone; a
+ * copy of an empty sequence frees it.  So the samples of a prompt or beams go on by themselves, and sequences move between
+ * caches.  Each source's rows are read once for all its targets.
+ *   dst, src: host [n]; a target occurs once and, within one cache, is no source of the same call.
+ * The caches agree in M, H, d_head, dtype, rotation and policy; capacities, batch and bits differ as they like.  From 16 to
+ * 4 bits the rows are quantised as an append does it (kvc_config.bits), from 4 to 16 they become the values that they stand
+ * for, rounded to dtype; between equal bits they are copied as they are.  Where `cache` has scores, the rows get those of
+ * `from`, or 0 where it has none.  Prefixes (kvc_set_prefix) stay as they are set for dst; src's own rows alone are copied.
+ * The call is ordered behind earlier work on both caches by the caller, as later work on `from` behind it.
+ * Errors: KVC_ERR_CAPACITY where a target cannot hold its source's rows; KVC_ERR_STATE with layers of the last tokens of
+ * either cache not written; KVC_ERR_UNSUPPORTED under KVC_POLICY_LOCAL. */
+kvc_status kvc_copy(kvc_cache* cache, const kvc_cache* from, int n, const int32_t* dst, const int32_t* src, void* stream);
+
+/* Cuts sequence s back to the first tokens[s] tokens of its history (host [b]; below 0: the sequence stays as it is), as
+ * where drafted tokens are not accepted; 0 frees the sequence, which begins anew with its next append.  The next query is
+ * the last token that is left; a span whose <CR> goes is open again.  Scores of rows that go become 0.
+ * Errors: KVC_ERR_INVALID_ARG for more tokens than there are; KVC_ERR_STATE with layers of the last tokens not written, for
+ * a cut inside a span that was freed (its tokens' rows are gone), or before the tokens that an eviction left rows of their
+ * own; KVC_ERR_UNSUPPORTED for a cut above 0 under KVC_POLICY_LOCAL.
+ * kvc_copy and kvc_truncate on a stream that is captured: a replay repeats the device's part, not the bookkeeping; they are
+ * KVC_ERR_STATE there where the state of the cache's sequences (about 40 bytes each, 16 to 32 more for each that changes)
+ * exceeds the 3,584 bytes of a kernel parameter. */
+kvc_status kvc_truncate(kvc_cache* cache, const int64_t* tokens, void* stream);
+
 /* Masked prefill attention of layer `layer` on the tensor cores (Sec. 3.1: the modified causal
  * mask holds for every token of a prompt; Manipulating Key-Value Memory: a long prefix may be run
  * block by block).  For every sequence s with n_q[s] > 0 the queries are its last n_q[s] tokens;
@@ -422,7 +470,8 @@ kvc_status kvc_last_compaction_ms(kvc_cache* cache, float* scan_ms, float* move_
  * segments merged by a log-sum-exp combine; 1: balanced segments, a CTA or a cluster of CTAs for each,
  * or up to eight consecutive ones per CTA; 2: one warp per segment (the scored decode's too; the shared
  * decode's own rows: one or four); 3: several consecutive whole segments per warp; 4: unbalanced segments over several layers, one or two per CTA, or runs of
- * consecutive whole segments per warp cut by rows; -1: nothing launched yet), plan[1] = warps that
+ * consecutive whole segments per warp cut by rows; 5: a cache of 4 bits, equal shares of all tiles per warp; -1: nothing
+ * launched yet), plan[1] = warps that
  * attend, plan[2] = rows per tile, plan[3] = pipeline stages per warp (per CTA where CTAs take
  * segments). */
 kvc_status kvc_last_decode_plan(const kvc_cache* cache, int32_t* plan);

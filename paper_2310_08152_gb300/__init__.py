@@ -176,6 +176,23 @@ def kvc_book_evict(book: int, keep, recent):
     _check(lib().kvc_book_evict(book, keep.ctypes.data, recent.ctypes.data))
 
 
+def kvc_book_truncate(book: int, tokens):
+    tokens = _np(tokens, np.int64)
+    _check(lib().kvc_book_truncate(book, tokens.ctypes.data))
+
+
+def _copies(dst, src):
+    dst, src = _np(dst, np.int32).reshape(-1), _np(src, np.int32).reshape(-1)
+    if dst.size != src.size:
+        raise ValueError(f"{dst.size} targets for {src.size} sources")
+    return dst, src
+
+
+def kvc_book_copy(book: int, other: int, dst, src):
+    dst, src = _copies(dst, src)
+    _check(lib().kvc_book_copy(book, other, dst.size, dst.ctypes.data, src.ctypes.data))
+
+
 def kvc_book_pending_spans(book: int, seq: int):
     n = ctypes.c_int64(64)  # room for most; more take a second call
     spans = None
@@ -263,6 +280,16 @@ class Book:
             raise KvcError(5, "a cache's book is read-only; evict through the cache")
         kvc_book_evict(self.handle, _per_seq(keep, self.b, "keep"), _per_seq(recent, self.b, "recent"))
 
+    def truncate(self, tokens):
+        if self.readonly:
+            raise KvcError(5, "a cache's book is read-only; truncate through the cache")
+        kvc_book_truncate(self.handle, _per_seq(tokens, self.b, "tokens"))
+
+    def copy_from(self, other: "Book", dst, src):
+        if self.readonly:
+            raise KvcError(5, "a cache's book is read-only; copy through the cache")
+        kvc_book_copy(self.handle, other.handle, dst, src)
+
     def pending_spans(self, seq: int):
         return kvc_book_pending_spans(self.handle, seq)
 
@@ -289,7 +316,7 @@ class Book:
 # ------------------------------------------------------------------------------------------
 
 def make_config(M, H, d_head, capacity, dtype="f16", rotary_dim=0, rope_base=10000.0, policy=POLICY_PAPER,
-                local_ratio=0.0):
+                local_ratio=0.0, bits=16):
     cap = _np(capacity, np.int64)
     cfg = _lib.KvcConfig()
     cfg.M, cfg.H, cfg.d_head, cfg.b = M, H, d_head, cap.size
@@ -298,6 +325,7 @@ def make_config(M, H, d_head, capacity, dtype="f16", rotary_dim=0, rope_base=100
     cfg.rope_base = rope_base
     cfg.policy = policy
     cfg.local_ratio = local_ratio
+    cfg.bits = bits
     cfg.seq_capacity = cap.ctypes.data
     return cfg, cap
 
@@ -419,6 +447,16 @@ def kvc_evict(cache: int, keep, recent, kept=None, stream=None):
     _check(lib().kvc_evict(cache, keep.ctypes.data, recent.ctypes.data, _ptr(kept), _stream_handle(stream)))
 
 
+def kvc_copy(cache: int, other: int, dst, src, stream=None):
+    dst, src = _copies(dst, src)
+    _check(lib().kvc_copy(cache, other, dst.size, dst.ctypes.data, src.ctypes.data, _stream_handle(stream)))
+
+
+def kvc_truncate(cache: int, tokens, stream=None):
+    tokens = _np(tokens, np.int64)
+    _check(lib().kvc_truncate(cache, tokens.ctypes.data, _stream_handle(stream)))
+
+
 def kvc_prefill_attention(cache: int, layer: int, q, n_q, scale: float, out, stream=None):
     n_q = _np(n_q, np.int32)
     _check(lib().kvc_prefill_attention(cache, layer, _ptr(q), n_q.ctypes.data, float(scale), _ptr(out),
@@ -475,23 +513,33 @@ class KVCache:
     """A sentinel-compressed KV cache: owns its device buffers (torch) and the library handle."""
 
     def __init__(self, M: int, H: int, d_head: int, capacity, dtype: str = "f16", rotary_dim: int = 0,
-                 rope_base: float = 10000.0, policy: int = POLICY_PAPER, device=None, local_ratio: float = 0.0):
+                 rope_base: float = 10000.0, policy: int = POLICY_PAPER, device=None, local_ratio: float = 0.0,
+                 bits: int = 16):
+        """bits: 16, or 4 for rows held as 4-bit codes with a step and a least value for each group of 32 columns
+        (kvc_config.bits): such a cache appends, compresses spans, decodes, copies and truncates; for the rest its sequences
+        are copied into one of 16 bits."""
         import torch
 
         self.M, self.H, self.d, self.dtype = M, H, d_head, dtype
         self.rotary_dim, self.rope_base, self.policy = rotary_dim, rope_base, policy
         self.local_ratio = local_ratio
-        cfg, cap = make_config(M, H, d_head, capacity, dtype, rotary_dim, rope_base, policy, local_ratio)
+        cfg, cap = make_config(M, H, d_head, capacity, dtype, rotary_dim, rope_base, policy, local_ratio, bits)
         self.capacity = cap
+        self.bits = bits
         self.b = cap.size
-        self.C = int(cap.sum())
-        self.offsets = np.concatenate([[0], np.cumsum(cap)[:-1]]).astype(np.int64)
+        rows = (cap + 3) // 4 * 4 if bits == 4 else cap  # of each sequence in the layout
+        self.C = int(rows.sum())
+        self.offsets = np.concatenate([[0], np.cumsum(rows)[:-1]]).astype(np.int64)
         sizes = kvc_required_bytes(cfg)
         device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
         tdt = torch.float16 if dtype == "f16" else torch.bfloat16
         self.torch_dtype = tdt
-        self.k = torch.empty(sizes["k"] // 2, dtype=tdt, device=device)
-        self.v = torch.empty(sizes["v"] // 2, dtype=tdt, device=device)
+        if bits == 4:  # codes and pairs
+            self.k = torch.empty(sizes["k"], dtype=torch.uint8, device=device)
+            self.v = torch.empty(sizes["v"], dtype=torch.uint8, device=device)
+        else:
+            self.k = torch.empty(sizes["k"] // 2, dtype=tdt, device=device)
+            self.v = torch.empty(sizes["v"] // 2, dtype=tdt, device=device)
         self.pos = torch.empty(sizes["meta"] // 4, dtype=torch.int32, device=device)
         self.orig = torch.empty(sizes["meta"] // 4, dtype=torch.int32, device=device)
         self.workspace = torch.empty(sizes["workspace"], dtype=torch.uint8, device=device)
@@ -526,10 +574,16 @@ class KVCache:
 
     # views of the device layout (rows of d_head elements)
     def k_plane(self, layer: int):
+        self._rows16()
         return self.k.view(self.M, self.H * self.C, self.d)[layer]
 
     def v_plane(self, layer: int):
+        self._rows16()
         return self.v.view(self.M, self.H * self.C, self.d)[layer]
+
+    def _rows16(self):
+        if self.bits == 4:
+            raise KvcError(2, "the rows are held in 4 bits; copy_from brings them into a cache of 16")
 
     def stream_rows(self, plane, s: int, h: int, n: int):
         """Rows [0, n) of sequence s, head h in a (layer, K/V) plane."""
@@ -680,6 +734,22 @@ class KVCache:
             self._budget[row] = x if isinstance(x, int) else _per_seq(x, self.b, name)
         _check(lib().kvc_evict(self.handle, self._budget_at, self._budget_at + 8 * self.b, _ptr(kept),
                                self._stream(stream, self._scores)))
+
+    # sequences copied, cut back and freed
+    def copy_from(self, other: "KVCache", dst, src, stream=None):
+        """Sequence dst[i] becomes a copy of sequence src[i] of `other`, this cache or another: rows (quantised or turned into
+        the values that they stand for where the caches' bits differ), history, spans and scores.  The samples of a prompt:
+        cache.copy_from(cache, [1, 2, 3], [0, 0, 0])."""
+        if not other.handle:
+            raise KvcError(5, "the other cache is closed")
+        memory = (self._scores, other._scores) if self._scores is not None else ()
+        kvc_copy(self.handle, other.handle, dst, src, self._stream(stream, *memory))
+
+    def truncate(self, tokens, stream=None):
+        """Cuts every sequence s back to the first tokens[s] of its history (a number for all; -1 leaves a sequence as it is):
+        drafted tokens go, and 0 frees the sequence for another."""
+        tokens = _per_seq(tokens, self.b, "tokens")
+        kvc_truncate(self.handle, tokens, self._stream(stream, self._scores))
 
     # sequences that share a prefix
     def set_prefix(self, prefix: Optional["KVCache"], parent=None):

@@ -30,6 +30,7 @@ class KvcConfig(ctypes.Structure):
         ("workspace", P),
         ("workspace_bytes", c_size_t),
         ("local_ratio", c_float),
+        ("bits", c_int),
     ]
 
 
@@ -45,6 +46,8 @@ SIGNATURES = [
     ("kvc_book_append_free_closed", c_int, [P, P, P, P]),
     ("kvc_book_compress", c_int, [P, P, P, P, c_int]),
     ("kvc_book_evict", c_int, [P, P, P]),
+    ("kvc_book_truncate", c_int, [P, P]),
+    ("kvc_book_copy", c_int, [P, P, c_int, P, P]),
     ("kvc_book_pending_spans", c_int, [P, c_int, P, P, c_int64, P]),
     ("kvc_book_lengths", c_int, [P, P, P]),
     ("kvc_book_prefill_keys", c_int, [P, c_int, c_int64, P, c_int64, P]),
@@ -70,6 +73,8 @@ SIGNATURES = [
     ("kvc_prefix_scratch_bytes", c_size_t, [P]),
     ("kvc_set_prefix", c_int, [P, P, P, P, c_size_t]),
     ("kvc_decode_attention_shared", c_int, [P, c_int, c_int, P, c_int64, c_float, P, c_int64, P]),
+    ("kvc_copy", c_int, [P, P, c_int, P, P, P]),
+    ("kvc_truncate", c_int, [P, P, P]),
     ("kvc_evict", c_int, [P, P, P, P, P]),
     ("kvc_prefill_attention", c_int, [P, c_int, P, P, c_float, P, P]),
     ("kvc_masked_reference_layout", c_int, [P, c_int, c_int64, P, P, P, P, P, P, P, P]),

@@ -292,6 +292,127 @@ void Book::apply_evict(const std::vector<EvictSeq>& plan) {
   }
 }
 
+bool Book::plan_truncate(const int64_t* tokens, std::vector<DropSeq>& plan, std::string& err, int& code) const {
+  char buf[256];
+  plan.clear();
+  for (int s = 0; s < b_; ++s) {
+    const Seq& q = seqs_[s];
+    const int64_t n = tokens[s], T = (int64_t)q.kind.size();
+    if (n < 0 || n == T) continue;
+    if (n > T) {
+      std::snprintf(buf, sizeof buf, "sequence %d: %lld tokens to keep of %lld", s, (long long)n, (long long)T);
+      err = buf;
+      code = 1;
+      return false;
+    }
+    DropSeq d;
+    d.s = s;
+    d.tokens = n;
+    d.len_old = q.stored;
+    if (n > 0) {
+      if (policy_ == POLICY_LOCAL) {
+        err = "the local-attention cache has overwritten the rows before its window: its sequences can only be dropped whole";
+        code = 2;
+        return false;
+      }
+      if (n < q.first_named) {
+        std::snprintf(buf, sizeof buf, "sequence %d: an eviction has left the tokens before %lld without rows of their own", s,
+                      (long long)q.first_named);
+        err = buf;
+        code = 5;
+        return false;
+      }
+      for (const Span& sp : q.spans) {
+        if (!sp.freed || n <= sp.cl || n > sp.cr) continue;
+        std::snprintf(buf, sizeof buf, "sequence %d: token %lld lies in the freed span (%lld, %lld)", s, (long long)n,
+                      (long long)sp.cl, (long long)sp.cr);
+        err = buf;
+        code = 5;
+        return false;
+      }
+      auto it = std::lower_bound(q.freed.begin(), q.freed.end(), std::make_pair(n, (int64_t)0));
+      d.len_new = q.unnamed + (n - q.first_named) - q.freed_before[(size_t)(it - q.freed.begin())];
+    }
+    plan.push_back(d);
+  }
+  return true;
+}
+
+void Book::apply_truncate(const std::vector<DropSeq>& plan) {
+  for (const DropSeq& d : plan) {
+    Seq& q = seqs_[d.s];
+    if (d.tokens == 0) {
+      Seq fresh;
+      fresh.cap = q.cap;
+      fresh.freed_before.push_back(0);
+      q = std::move(fresh);
+      continue;
+    }
+    const int64_t n = d.tokens;
+    for (int64_t j = n; j < (int64_t)q.kind.size(); ++j) q.normals -= q.kind[j] == NORMAL;
+    q.kind.resize((size_t)n);
+    q.pos.resize((size_t)n);
+    while (!q.spans.empty() && q.spans.back().cl >= n) q.spans.pop_back();
+    if (!q.spans.empty() && q.spans.back().cr >= n) q.spans.back().cr = -1;  // closed by a token that goes: open again
+    q.open = !q.spans.empty() && q.spans.back().cr < 0;
+    q.freed.erase(std::lower_bound(q.freed.begin(), q.freed.end(), std::make_pair(n, (int64_t)0)), q.freed.end());
+    rebuild_prefix(q);
+    q.stored = d.len_new;
+  }
+}
+
+bool Book::check_copy(const Book& from, int n, const int32_t* dst, const int32_t* src, std::string& err, int& code) const {
+  char buf[256];
+  code = 1;
+  if (policy_ == POLICY_LOCAL || from.policy_ == POLICY_LOCAL) {
+    err = "a sequence of the local-attention cache is a ring and is not copied";
+    code = 2;
+    return false;
+  }
+  if (policy_ != from.policy_) {
+    err = "the policies differ";
+    return false;
+  }
+  std::vector<uint8_t> target((size_t)b_, 0);
+  for (int i = 0; i < n; ++i) {
+    if (dst[i] < 0 || dst[i] >= b_ || src[i] < 0 || src[i] >= from.b_) {
+      std::snprintf(buf, sizeof buf, "copy %d: sequence %d of %d to sequence %d of %d", i, src[i], from.b_, dst[i], b_);
+      err = buf;
+      return false;
+    }
+    if (target[(size_t)dst[i]]++) {
+      std::snprintf(buf, sizeof buf, "copy %d: sequence %d is a target twice", i, dst[i]);
+      err = buf;
+      return false;
+    }
+    if (from.seqs_[src[i]].stored > seqs_[dst[i]].cap) {
+      std::snprintf(buf, sizeof buf, "copy %d: %lld rows exceed capacity %lld of sequence %d", i,
+                    (long long)from.seqs_[src[i]].stored, (long long)seqs_[dst[i]].cap, dst[i]);
+      err = buf;
+      code = 3;
+      return false;
+    }
+  }
+  if (&from == this)
+    for (int i = 0; i < n; ++i)
+      if (target[(size_t)src[i]]) {
+        std::snprintf(buf, sizeof buf, "copy %d: sequence %d is a target and a source", i, src[i]);
+        err = buf;
+        return false;
+      }
+  return true;
+}
+
+void Book::apply_copy(const Book& from, int n, const int32_t* dst, const int32_t* src) {
+  std::vector<Seq> copies;  // before anything changes: an allocation may fail
+  copies.reserve((size_t)n);
+  for (int i = 0; i < n; ++i) copies.push_back(from.seqs_[src[i]]);
+  for (int i = 0; i < n; ++i) {
+    copies[(size_t)i].cap = seqs_[dst[i]].cap;
+    seqs_[dst[i]] = std::move(copies[(size_t)i]);
+  }
+}
+
 bool Book::all_visible(int s) const {
   for (const Span& sp : seqs_[s].spans)
     if (!sp.freed) return false;

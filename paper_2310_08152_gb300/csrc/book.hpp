@@ -55,6 +55,14 @@ struct CompactSeq {
   std::vector<std::pair<int64_t, int64_t>> drops;
 };
 
+// One sequence whose last tokens are dropped: rows [len_new, len_old) go, the first `tokens` of its history stay.
+struct DropSeq {
+  int s = 0;
+  int64_t tokens = 0;
+  int64_t len_old = 0;
+  int64_t len_new = 0;
+};
+
 class Book {
  public:
   Book(int b, Policy policy, const int64_t* capacity, double local_ratio = 0.0);
@@ -92,6 +100,16 @@ class Book {
   void apply_evict(const std::vector<EvictSeq>& plan);
   // Rows of sequence s that evictions have left unnamed (its first ones).
   int64_t unnamed(int s) const { return seqs_[s].unnamed; }
+
+  // Dropping the last tokens: sequence s goes on with the first tokens[s] of its history (below 0: all of it).  Rows that
+  // were freed or evicted do not come back, so the cut lies neither inside a freed span nor before the first named row;
+  // no token at all (a sequence that begins anew) is always allowed.
+  bool plan_truncate(const int64_t* tokens, std::vector<DropSeq>& plan, std::string& err, int& code) const;
+  void apply_truncate(const std::vector<DropSeq>& plan);
+
+  // Sequence dst[i] becomes a copy of sequence src[i] of `from` (this book or another of the same policy).
+  bool check_copy(const Book& from, int n, const int32_t* dst, const int32_t* src, std::string& err, int& code) const;
+  void apply_copy(const Book& from, int n, const int32_t* dst, const int32_t* src);
 
   // The decode query of sequence s (its last token).  False (with `err`) if the rows hidden from it
   // are not one contiguous run of stored rows.

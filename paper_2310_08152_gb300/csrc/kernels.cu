@@ -1974,7 +1974,7 @@ cudaError_t launch_append_image(const Geometry& g, const Static& st, const Buffe
 
 cudaError_t launch_compact(const Geometry& g, const Static& st, const Buffers& buf, const AffSeq* aff, int n_aff,
                            const int32_t* ranges, int32_t* src_map, cudaStream_t stream, int* launched,
-                           cudaEvent_t between) {
+                           cudaEvent_t between, const PackedBuffers* packed) {
   *launched = 0;
   if (n_aff <= 0) return cudaSuccess;
   compact_scan_kernel<<<n_aff, kScanThreads, 0, stream>>>(st, buf, aff, reinterpret_cast<const int2*>(ranges),
@@ -1985,6 +1985,11 @@ cudaError_t launch_compact(const Geometry& g, const Static& st, const Buffers& b
   if (between != nullptr) {
     e = cudaEventRecord(between, stream);
     if (e != cudaSuccess) return e;
+  }
+  if (packed) {
+    e = launch_packed_move(g, st, *packed, aff, n_aff, src_map, stream);
+    if (e == cudaSuccess) *launched = 2;
+    return e;
   }
   const int64_t blocks = (int64_t)n_aff * g.M * 2 * g.H;
   e = by_dhead(g.D, [&](auto dc) {

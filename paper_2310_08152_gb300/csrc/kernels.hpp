@@ -59,6 +59,22 @@ constexpr int kMaxDecodeWorkers = 8192;
 
 bool dhead_supported(int D);
 
+// The planes of a cache of 4 bits (packed.cuh): [M][H * C] rows of D / 2 bytes of codes and of packed_groups(D) words of
+// (step, lo) pairs, for K and for V.  Its sequences' capacities in the layout are multiples of kPackedRows, so that a run
+// of rows that starts at a multiple of it starts at 16 bytes in every plane.
+struct PackedBuffers {
+  unsigned char* kc;
+  unsigned char* vc;
+  uint32_t* kp;
+  uint32_t* vp;
+};
+constexpr int kPackedRows = 4;
+inline int packed_groups(int D) { return (D + 31) / 32; }
+// The decode's work is counted in tiles of kPackedTile rows: P then holds prefix sums of tiles, from row
+// begin / kPackedRows * kPackedRows on.  Each worker (warp) has a counter and two parts of D + 4 floats.
+constexpr int kPackedTile = 64;
+constexpr int kMaxPackedWorkers = 4096;
+
 // Writes the n_plan stored tokens of a call whose inputs hold n_in tokens per layer (k_in, v_in
 // 16-byte aligned).  maps: the device copy of encode_append_maps' output, or NULL; with it, calls of
 // at least num_sms (layer, token) units go through the TMA kernel, whose bounded waits give up
@@ -74,6 +90,12 @@ struct alignas(16) AppendImage {
 cudaError_t launch_append_image(const Geometry& g, const Static& st, const Buffers& buf, const AppendImage& img,
                                 size_t img_bytes, size_t plan_off, void* dyn, int64_t n_plan, int64_t n_in,
                                 int n_layers, const void* k_in, const void* v_in, cudaStream_t stream);
+// The same of a cache of 4 bits: K is rotated and rounded as above, then packed.  img: the upload as a kernel parameter
+// (img_bytes, the plan from plan_off on, stored at dyn), or NULL and the plan on the device.
+cudaError_t launch_packed_append(const Geometry& g, const Static& st, const Buffers& buf, const PackedBuffers& pb,
+                                 const TokPlan* plan, const AppendImage* img, size_t img_bytes, size_t plan_off, void* dyn,
+                                 int64_t n_plan, int64_t n_in, int m0, int n_layers, bool write_meta, const void* k_in,
+                                 const void* v_in, cudaStream_t stream);
 // Bytes of encode_append_maps' output: a 128-byte TMA descriptor per (K/V, sequence).
 inline size_t append_maps_bytes(int b) { return 2 * 128 * (size_t)b; }
 // Encodes, per sequence s, 4-D TMA descriptors over the K and then the V planes: dims {D, cap[s],
@@ -83,10 +105,13 @@ inline size_t append_maps_bytes(int b) { return 2 * 128 * (size_t)b; }
 cudaError_t encode_append_maps(const Geometry& g, const Buffers& buf, const int64_t* seq_row0, const int32_t* cap,
                                unsigned char* out);
 
-// Scan, then row moves.  between: an event recorded on the stream between the two kernels, or NULL.
+// Scan, then row moves.  between: an event recorded on the stream between the two kernels, or NULL.  packed: the planes of
+// a cache of 4 bits, whose rows are moved instead of buf's.
 cudaError_t launch_compact(const Geometry& g, const Static& st, const Buffers& buf, const AffSeq* aff, int n_aff,
                            const int32_t* ranges, int32_t* src_map, cudaStream_t stream, int* launched,
-                           cudaEvent_t between = nullptr);
+                           cudaEvent_t between = nullptr, const PackedBuffers* packed = nullptr);
+cudaError_t launch_packed_move(const Geometry& g, const Static& st, const PackedBuffers& pb, const AffSeq* aff, int n_aff,
+                               const int32_t* src_map, cudaStream_t stream);
 
 struct DecodeArgs {
   int device;            // the current device
@@ -126,6 +151,11 @@ struct DecodePlan {
 // cudaErrorNotSupported, and the caller goes layer by layer.
 cudaError_t launch_decode(const Geometry& g, const Static& st, const Buffers& buf, const DecodeArgs& a,
                           int num_sms, cudaStream_t stream, int* grid, DecodePlan* plan);
+
+// The decode of a cache of 4 bits, all the launch's layers together (a.P and a.R in tiles; a.counters:
+// [kMaxPackedWorkers], zero between launches).
+cudaError_t launch_packed_decode(const Geometry& g, const Static& st, const PackedBuffers& pb, const DecodeArgs& a,
+                                 int* status, int num_sms, cudaStream_t stream, int* grid, DecodePlan* plan);
 
 // The decode with each row's attention weight added to its score (scores: [M][H * C], in the rows' layout): a CTA or a
 // cluster per segment, or several segments per CTA, whatever the segments.
@@ -332,6 +362,45 @@ cudaError_t launch_score_rotate(const Geometry& g, const ScoreArgs& a, cudaStrea
 inline int score_query_rows(int most) { return most <= 16 ? 16 : 128; }
 cudaError_t launch_score_lse(const Geometry& g, const ScoreMaps& maps, const ScoreArgs& a, int most, cudaStream_t stream);
 cudaError_t launch_score_sum(const Geometry& g, const ScoreMaps& maps, const ScoreArgs& a, int most, cudaStream_t stream);
+
+// ---------------------------------------------------------------------------------------------
+// Copies of sequences (copy.cu)
+// ---------------------------------------------------------------------------------------------
+// A source sequence and its targets: targets[first .. first + n).
+struct alignas(16) CopySource {
+  int32_t s, len, first, n;
+};
+// A target sequence, the rows that it held before, the rows that it holds now, and the source sequence.
+struct alignas(16) CopyTarget {
+  int32_t s, len_old, len, src;
+};
+// One side of a copy: planes of 16 bits (bits 16: k, v) or of 4.
+struct CopySide {
+  int bits;
+  int64_t C;
+  Static st;
+  uint16_t* k;
+  uint16_t* v;
+  PackedBuffers pb;
+  int32_t* pos;
+  int32_t* orig;
+  float* scores;  // or NULL
+};
+// img: the targets' upload (decode state, sources, targets) as a kernel parameter, stored at dyn, or NULL.  sources and
+// targets: offsets in that upload.  n_rows: the longest source.
+struct CopyArgs {
+  CopySide src, dst;
+  int n_sources, n_targets;
+  int64_t n_rows;
+  size_t sources, targets;
+  const AppendImage* img;
+  size_t img_bytes;
+  void* dyn;
+};
+// Rows and metadata; then, where the targets' cache has scores, theirs (the source's or zero, and zero behind them).
+cudaError_t launch_copy(const Geometry& g, const CopyArgs& a, cudaStream_t stream, int* launched);
+// Stores an upload that comes as a kernel parameter, and zeroes the scores of rows [len, len_old) of the targets in it.
+cudaError_t launch_drop(const Geometry& g, const CopyArgs& a, cudaStream_t stream, int* launched);
 
 // One warp waits on an mbarrier phase that never completes, with the limit given; the bounded wait
 // gives up and sets STATUS_TIMEOUT in *status.  Exercises the kernels' timeout reporting.

@@ -78,6 +78,7 @@ struct WsLayout {
   size_t pre_bytes = 0;
   size_t sp = 0;         // plan of a prompt's scores: [ScoreUnit first pass][second pass][int32 least][int32 meta]
   size_t sp_bytes = 0;
+  size_t packed_counters = 0;  // int32 [kMaxPackedWorkers], of a cache of 4 bits
   size_t total = 0;
 };
 
@@ -88,7 +89,20 @@ size_t score_plan_bytes(int64_t units0, int64_t units1, int64_t n_least, int64_t
          4 * (size_t)n_meta;
 }
 
-WsLayout ws_layout(int b, int H, int D, int rot, int64_t C) {
+bool is_packed(const kvc_config& c) { return c.bits == 4; }
+// Rows that a sequence's capacity takes in the layout.
+int64_t layout_rows(const kvc_config& c, int64_t capacity) {
+  return is_packed(c) ? (int64_t)align_up((size_t)capacity, kvc::kPackedRows) : capacity;
+}
+// Bytes of a cache's K or V, and of the codes ahead of the pairs in one of 4 bits.
+size_t code_bytes(const kvc_config& c, int64_t C) { return align_up((size_t)c.M * c.H * (size_t)C * (c.d_head / 2), 256); }
+size_t plane_bytes(const kvc_config& c, int64_t C) {
+  if (!is_packed(c)) return (size_t)c.M * c.H * (size_t)C * c.d_head * 2;
+  return code_bytes(c, C) + (size_t)c.M * c.H * (size_t)C * 4 * (size_t)kvc::packed_groups(c.d_head);
+}
+
+WsLayout ws_layout(const kvc_config& c, int64_t C) {
+  const int b = c.b, H = c.H, D = c.d_head, rot = c.rotary_dim;
   WsLayout L;
   size_t o = 0;
   auto take = [&](size_t n) {
@@ -120,6 +134,7 @@ WsLayout ws_layout(int b, int H, int D, int rot, int64_t C) {
   L.pre = take(L.pre_bytes);
   L.sp_bytes = score_plan_bytes(L.pre_max_tiles, L.pre_max_tiles + kScoreUnits, L.pre_max_tiles, C + 128 * (int64_t)b);
   L.sp = take(L.sp_bytes);
+  if (is_packed(c)) L.packed_counters = take(4 * (size_t)kvc::kMaxPackedWorkers);
   L.total = o;
   return L;
 }
@@ -139,12 +154,15 @@ kvc_status check_config(const kvc_config* c, int64_t* C_out) {
     return fail(KVC_ERR_INVALID_ARG, "policy %d", (int)c->policy);
   if (c->policy == KVC_POLICY_LOCAL && !(c->local_ratio >= 0.0f && c->local_ratio < 1.0f))
     return fail(KVC_ERR_INVALID_ARG, "local_ratio=%g must be in [0, 1)", (double)c->local_ratio);
+  if (c->bits != 0 && c->bits != 16 && c->bits != 4) return fail(KVC_ERR_UNSUPPORTED, "rows of %d bits (16 or 4)", c->bits);
+  if (is_packed(*c) && c->policy == KVC_POLICY_LOCAL)
+    return fail(KVC_ERR_UNSUPPORTED, "the local-attention cache holds 16-bit rows");
   if (!c->seq_capacity) return fail(KVC_ERR_INVALID_ARG, "seq_capacity is NULL");
   int64_t C = 0;
   for (int s = 0; s < c->b; ++s) {
     if (c->seq_capacity[s] < 1 || c->seq_capacity[s] >= INT32_MAX)
       return fail(KVC_ERR_INVALID_ARG, "seq_capacity[%d]=%lld out of range", s, (long long)c->seq_capacity[s]);
-    C += c->seq_capacity[s];
+    C += layout_rows(*c, c->seq_capacity[s]);
   }
   if ((int64_t)c->H * C >= ((int64_t)1 << 40)) return fail(KVC_ERR_INVALID_ARG, "cache too large");
   if (C >= INT32_MAX) return fail(KVC_ERR_INVALID_ARG, "sum of capacities must stay below 2^31");
@@ -316,14 +334,14 @@ struct kvc_cache {
 
   kvc_cache(const kvc_config& c, int64_t C_)
       : cfg(c), C(C_), bk(c.b, (kvc::Policy)c.policy, c.seq_capacity, (double)c.local_ratio) {
-    cap.assign(c.seq_capacity, c.seq_capacity + c.b);
+    for (int s = 0; s < c.b; ++s) cap.push_back(layout_rows(c, c.seq_capacity[s]));
     off.resize(c.b);
     int64_t o = 0;
     for (int s = 0; s < c.b; ++s) {
       off[s] = o;
       o += cap[s];
     }
-    ws = ws_layout(c.b, c.H, c.d_head, c.rotary_dim, C);
+    ws = ws_layout(c, C);
     layers_done = c.M;
   }
 
@@ -361,6 +379,17 @@ struct kvc_cache {
     b.orig = cfg.orig_base;
     b.status = reinterpret_cast<int*>(wsp(ws.hdr));
     return b;
+  }
+
+  bool packed() const { return is_packed(cfg); }
+  kvc::PackedBuffers packed_bufs() const {
+    unsigned char *k = static_cast<unsigned char*>(cfg.k_base), *v = static_cast<unsigned char*>(cfg.v_base);
+    const size_t n = code_bytes(cfg, C);
+    return {k, v, reinterpret_cast<uint32_t*>(k + n), reinterpret_cast<uint32_t*>(v + n)};
+  }
+  kvc::CopySide copy_side() const {
+    const kvc::Buffers b = bufs();
+    return {packed() ? 4 : 16, C, stat(), b.k, b.v, packed() ? packed_bufs() : kvc::PackedBuffers{}, b.pos, b.orig, scores};
   }
 
   size_t staging_bytes() const {
@@ -407,7 +436,7 @@ struct kvc_cache {
     // the append kernel's TMA descriptors (64-byte aligned in the workspace); without them (a box
     // cannot hold H heads) appends take the kernel that copies through registers
     amaps_ok = false;
-    if ((reinterpret_cast<uintptr_t>(wsp(ws.amaps)) & 63) == 0) {
+    if (!packed() && (reinterpret_cast<uintptr_t>(wsp(ws.amaps)) & 63) == 0) {
       std::vector<int32_t> cap32(cap.begin(), cap.end());
       std::vector<int64_t> row0h(b);
       for (int s = 0; s < b; ++s) row0h[s] = (int64_t)cfg.H * off[s];
@@ -422,6 +451,7 @@ struct kvc_cache {
     }
     e = cudaMemsetAsync(wsp(ws.hdr), 0, 256, stream);
     if (e == cudaSuccess) e = cudaMemsetAsync(wsp(ws.counters), 0, ws.counters_bytes, stream);
+    if (e == cudaSuccess && packed()) e = cudaMemsetAsync(wsp(ws.packed_counters), 0, 4 * (size_t)kvc::kMaxPackedWorkers, stream);
     if (e != cudaSuccess) return cuda_fail(e, "cudaMemsetAsync");
     device = dev;
     cuda_ready = true;
@@ -454,6 +484,8 @@ struct kvc_cache {
         ds[s].wrap = (int32_t)std::min<int64_t>(v.wrap, INT32_MAX);
         ds[s].is_cl = v.is_cl;
         Lc = v.len - v.begin;
+        if (packed())  // tiles, from a row on that starts at 16 bytes
+          Lc = (v.len - v.begin / kvc::kPackedRows * kvc::kPackedRows + kvc::kPackedTile - 1) / kvc::kPackedTile;
       } else {
         if (decode_ok) decode_err = err;
         decode_ok = false;
@@ -603,6 +635,30 @@ kvc_status kvc_book_evict(kvc_book* book, const int64_t* keep, const int64_t* re
   });
 }
 
+kvc_status kvc_book_truncate(kvc_book* book, const int64_t* tokens) {
+  return guarded([&]() -> kvc_status {
+    if (!book || !tokens) return fail(KVC_ERR_INVALID_ARG, "book/tokens are NULL");
+    std::vector<kvc::DropSeq> plan;
+    std::string err;
+    int code = 0;
+    if (!book->book.plan_truncate(tokens, plan, err, code)) return fail((kvc_status)code, "%s", err.c_str());
+    book->book.apply_truncate(plan);
+    return ok();
+  });
+}
+
+kvc_status kvc_book_copy(kvc_book* book, const kvc_book* from, int n, const int32_t* dst, const int32_t* src) {
+  return guarded([&]() -> kvc_status {
+    if (!book || !from) return fail(KVC_ERR_INVALID_ARG, "book/from are NULL");
+    if (n < 0 || (n > 0 && (!dst || !src))) return fail(KVC_ERR_INVALID_ARG, "sequence arrays");
+    std::string err;
+    int code = 0;
+    if (!book->book.check_copy(from->book, n, dst, src, err, code)) return fail((kvc_status)code, "%s", err.c_str());
+    book->book.apply_copy(from->book, n, dst, src);
+    return ok();
+  });
+}
+
 kvc_status kvc_book_pending_spans(const kvc_book* book, int seq, int64_t* cl, int64_t* cr, int64_t max, int64_t* n) {
   if (!book || !n) return fail(KVC_ERR_INVALID_ARG, "NULL argument");
   if (seq < 0 || seq >= book->book.b()) return fail(KVC_ERR_INVALID_ARG, "seq %d out of range", seq);
@@ -676,11 +732,11 @@ kvc_status kvc_required_bytes(const kvc_config* cfg, size_t* k_bytes, size_t* v_
   int64_t C = 0;
   kvc_status st = check_config(cfg, &C);
   if (st != KVC_OK) return st;
-  const size_t kv = (size_t)cfg->M * cfg->H * (size_t)C * cfg->d_head * 2;
+  const size_t kv = plane_bytes(*cfg, C);
   if (k_bytes) *k_bytes = kv;
   if (v_bytes) *v_bytes = kv;
   if (meta_bytes_each) *meta_bytes_each = 4 * (size_t)C;
-  if (workspace_bytes) *workspace_bytes = ws_layout(cfg->b, cfg->H, cfg->d_head, cfg->rotary_dim, C).total;
+  if (workspace_bytes) *workspace_bytes = ws_layout(*cfg, C).total;
   return ok();
 }
 
@@ -694,12 +750,12 @@ kvc_status kvc_create(const kvc_config* cfg, kvc_cache** out) {
   auto al = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 255u) == 0; };
   if (!al(cfg->k_base) || !al(cfg->v_base) || !al(cfg->pos_base) || !al(cfg->orig_base) || !al(cfg->workspace))
     return fail(KVC_ERR_INVALID_ARG, "device buffers must be 256-byte aligned");
-  const size_t need = ws_layout(cfg->b, cfg->H, cfg->d_head, cfg->rotary_dim, C).total;
+  const size_t need = ws_layout(*cfg, C).total;
   if (cfg->workspace_bytes < need)
     return fail(KVC_ERR_INVALID_ARG, "workspace_bytes=%zu < required %zu", cfg->workspace_bytes, need);
   kvc_cache* c = new (std::nothrow) kvc_cache(*cfg, C);
   if (!c) return fail(KVC_ERR_NO_MEMORY, "cache");
-  c->cfg.seq_capacity = c->cap.data();
+  c->cfg.seq_capacity = nullptr;  // the caller's array; the book and `cap` have what it held
   *out = c;
   return ok();
 }
@@ -811,7 +867,13 @@ static kvc_status append_impl(kvc_cache* c, int layer, const void* k, const void
         ++w;
       }
     }
-    if (fits) {
+    if (fits && c->packed()) {
+      e = kvc::launch_packed_append(g, c->stat(), c->bufs(), c->packed_bufs(), nullptr, &small, bytes, c->ws.dyn_payload,
+                                    c->wsp(c->ws.dyn), n_plan, N, 0, nl, true, k, v, stream);
+      if (e != cudaSuccess) return cuda_fail(e, "append kernel");
+      c->launches += 1;
+      c->last_was_decode = false;
+    } else if (fits) {
       e = kvc::launch_append_image(g, c->stat(), c->bufs(), small, bytes, c->ws.dyn_payload, c->wsp(c->ws.dyn), n_plan, N,
                                    nl, k, v, stream);
       if (e != cudaSuccess) return cuda_fail(e, "append kernel");
@@ -831,9 +893,11 @@ static kvc_status append_impl(kvc_cache* c, int layer, const void* k, const void
   }
   if (c->batch_ntok > 0) {
     const kvc::TokPlan* plan = reinterpret_cast<const kvc::TokPlan*>(c->wsp(c->ws.dyn + c->ws.dyn_payload));
-    cudaError_t e = kvc::launch_append(g, c->stat(), c->bufs(), plan, c->batch_ntok, c->batch_nin, m0, nl, m0 == 0, k,
-                                       v, c->amaps_ok ? c->wsp(c->ws.amaps) : nullptr, c->num_sms, 2000000000ull,
-                                       stream);
+    cudaError_t e =
+        c->packed() ? kvc::launch_packed_append(g, c->stat(), c->bufs(), c->packed_bufs(), plan, nullptr, 0, 0, nullptr,
+                                                c->batch_ntok, c->batch_nin, m0, nl, m0 == 0, k, v, stream)
+                    : kvc::launch_append(g, c->stat(), c->bufs(), plan, c->batch_ntok, c->batch_nin, m0, nl, m0 == 0, k, v,
+                                         c->amaps_ok ? c->wsp(c->ws.amaps) : nullptr, c->num_sms, 2000000000ull, stream);
     if (e != cudaSuccess) return cuda_fail(e, "append kernel");
     c->launches += 1;
     c->last_was_decode = false;
@@ -918,11 +982,12 @@ kvc_status kvc_compress_spans(kvc_cache* c, const int32_t* seq, const int64_t* c
       if (!ev && (e = cudaEventCreate(&ev)) != cudaSuccess) return cuda_fail(e, "cudaEventCreate");
     if ((e = cudaEventRecord(c->cev[0], stream)) != cudaSuccess) return cuda_fail(e, "cudaEventRecord");
   }
+  const kvc::PackedBuffers pb = c->packed() ? c->packed_bufs() : kvc::PackedBuffers{};
   e = kvc::launch_compact(c->geom(), c->stat(), c->bufs(),
                           reinterpret_cast<const kvc::AffSeq*>(c->wsp(c->ws.dyn + c->ws.dyn_payload)), n_aff,
                           reinterpret_cast<const int32_t*>(c->wsp(c->ws.dyn + c->ws.dyn_payload + aff_bytes)),
                           reinterpret_cast<int32_t*>(c->wsp(c->ws.src_map)), stream, &launched,
-                          timed ? c->cev[1] : nullptr);
+                          timed ? c->cev[1] : nullptr, c->packed() ? &pb : nullptr);
   c->launches += launched;
   c->last_was_decode = false;
   if (e != cudaSuccess) return cuda_fail(e, "compaction kernels");
@@ -938,6 +1003,11 @@ kvc_status kvc_compress_spans(kvc_cache* c, const int32_t* seq, const int64_t* c
     c->timed_compaction = true;
   }
   return ok();
+}
+
+// What works on 16-bit rows alone.
+static kvc_status refuse_packed(const char* what) {
+  return fail(KVC_ERR_UNSUPPORTED, "%s needs rows of 16 bits; copy the sequences into such a cache (kvc_copy)", what);
 }
 
 // Checks shared by the decode entry points, for layers [layer, layer + n_layers).
@@ -974,12 +1044,30 @@ static kvc::DecodeArgs decode_args(kvc_cache* c, int layer, const void* q, float
   return a;
 }
 
+// The decode of a cache of 4 bits, all layers in one launch.
+static kvc_status decode_packed(kvc_cache* c, int first, int n_layers, const void* q, int64_t q_layer_stride, float scale,
+                                float* out, int64_t out_layer_stride, cudaStream_t stream) {
+  kvc::DecodeArgs a = decode_args(c, first, q, scale, out);
+  a.n_layers = n_layers;
+  a.q_layer_stride = q_layer_stride;
+  a.out_layer_stride = out_layer_stride;
+  a.counters = reinterpret_cast<int*>(c->wsp(c->ws.packed_counters));
+  int grid = 0;
+  const cudaError_t e = kvc::launch_packed_decode(c->geom(), c->stat(), c->packed_bufs(), a, c->bufs().status, c->num_sms,
+                                                  stream, &grid, &c->last_plan);
+  if (e != cudaSuccess) return cuda_fail(e, "decode kernel (4 bits)");
+  c->launches += grid > 0 ? 1 : 0;
+  c->last_was_decode = true;
+  return ok();
+}
+
 kvc_status kvc_decode_attention(kvc_cache* c, int layer, const void* q, float scale, float* out, void* stream_) {
   kvc_status st = decode_check(c, layer, 1, q, scale, out);
   if (st != KVC_OK) return st;
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
   st = c->ensure_cuda(stream);
   if (st != KVC_OK) return st;
+  if (c->packed()) return decode_packed(c, layer, 1, q, 0, scale, out, 0, stream);
   const kvc::DecodeArgs a = decode_args(c, layer, q, scale, out);
   int grid = 0;
   cudaError_t e = kvc::launch_decode(c->geom(), c->stat(), c->bufs(), a, c->num_sms, stream, &grid, &c->last_plan);
@@ -1004,6 +1092,7 @@ kvc_status kvc_decode_attention_layers(kvc_cache* c, int first, int n_layers, co
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
   st = c->ensure_cuda(stream);
   if (st != KVC_OK) return st;
+  if (c->packed()) return decode_packed(c, first, n_layers, q, q_layer_stride, scale, out, out_layer_stride, stream);
   if (n_layers > 1) {
     // whole segments: every layer's in one launch (no per-launch prologue and drain per layer)
     kvc::DecodeArgs a = decode_args(c, first, q, scale, out);
@@ -1034,6 +1123,7 @@ kvc_status kvc_decode_attention_static_scratch(kvc_cache* c, int layer, const vo
                                                void* stream_) {
   kvc_status st0 = decode_check(c, layer, 1, q, scale, out);
   if (st0 != KVC_OK) return st0;
+  if (c->packed()) return refuse_packed("this decode");
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
   // split-K partials for every possible worker and segment, then one arrival counter per segment
   const size_t segs = (size_t)c->cfg.b * c->cfg.H;
@@ -1081,6 +1171,7 @@ kvc_status kvc_set_scores(kvc_cache* c, float* scores) {
   if (reinterpret_cast<uintptr_t>(scores) & 15) return fail(KVC_ERR_INVALID_ARG, "scores must be 16-byte aligned");
   if (scores && c->cfg.policy == KVC_POLICY_LOCAL)
     return fail(KVC_ERR_UNSUPPORTED, "the local-attention cache keeps a window and has no scores");
+  if (scores && c->packed()) return refuse_packed("a cache with scores");
   c->scores = scores;
   return ok();
 }
@@ -1165,6 +1256,7 @@ static kvc_status score_check(kvc_cache* c, const int32_t* n_q) {
   if (!n_q) return fail(KVC_ERR_INVALID_ARG, "n_q is NULL");
   if (c->cfg.policy == KVC_POLICY_LOCAL)
     return fail(KVC_ERR_UNSUPPORTED, "the local-attention cache keeps a window and has no scores");
+  if (c->packed()) return refuse_packed("the scores of a prompt");
   if ((int64_t)c->cfg.M * c->cfg.H * c->C >= ((int64_t)1 << 31))
     return fail(KVC_ERR_UNSUPPORTED, "M*H*sum(capacity) rows exceed the 2^31 rows a tensor-map coordinate reaches");
   for (int s = 0; s < c->cfg.b; ++s)
@@ -1382,6 +1474,7 @@ kvc_status kvc_set_prefix(kvc_cache* c, kvc_cache* prefix, const int32_t* parent
     const kvc_config &a = c->cfg, &p = prefix->cfg;
     if (a.policy == KVC_POLICY_LOCAL || p.policy == KVC_POLICY_LOCAL)
       return fail(KVC_ERR_UNSUPPORTED, "the local-attention cache keeps a window and has no shared prefix");
+    if (c->packed() || prefix->packed()) return refuse_packed("a shared prefix");
     if (a.M != p.M || a.H != p.H || a.d_head != p.d_head || a.dtype != p.dtype || a.rotary_dim != p.rotary_dim ||
         (a.rotary_dim > 0 && a.rope_base != p.rope_base))
       return fail(KVC_ERR_INVALID_ARG, "the caches differ in layers, heads, d_head, type or rotation");
@@ -1602,6 +1695,7 @@ kvc_status kvc_evict(kvc_cache* c, const int64_t* keep, const int64_t* recent, i
     if (!keep || !recent) return fail(KVC_ERR_INVALID_ARG, "keep/recent are NULL");
     if (c->cfg.policy == KVC_POLICY_LOCAL)
       return fail(KVC_ERR_UNSUPPORTED, "the local-attention cache keeps a window; nothing is evicted from it");
+    if (c->packed()) return refuse_packed("an eviction");
     if (c->layers_done != c->cfg.M)
       return fail(KVC_ERR_STATE, "layers %d..%d of the last tokens are not written yet", c->layers_done, c->cfg.M - 1);
     if (!c->scores) return fail(KVC_ERR_STATE, "the cache has no scores (kvc_set_scores)");
@@ -1648,6 +1742,137 @@ kvc_status kvc_evict(kvc_cache* c, const int64_t* keep, const int64_t* recent, i
   });
 }
 
+// An upload of a call that is captured comes as a kernel parameter: a captured copy from the staging ring would read, at each
+// replay, what later uploads have left there.
+static kvc_status capturable(bool fits, cudaStream_t stream) {
+  if (fits) return KVC_OK;
+  cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+  if (cudaStreamIsCapturing(stream, &status) != cudaSuccess) (void)cudaGetLastError();
+  if (status == cudaStreamCaptureStatusNone) return KVC_OK;
+  return fail(KVC_ERR_STATE, "the state of so many sequences is uploaded, which a capture would not keep");
+}
+
+kvc_status kvc_truncate(kvc_cache* c, const int64_t* tokens, void* stream_) {
+  return guarded([&]() -> kvc_status {
+    if (!c) return fail(KVC_ERR_INVALID_ARG, "cache is NULL");
+    if (!tokens) return fail(KVC_ERR_INVALID_ARG, "tokens is NULL");
+    if (c->layers_done != c->cfg.M)
+      return fail(KVC_ERR_STATE, "layers %d..%d of the last tokens are not written yet", c->layers_done, c->cfg.M - 1);
+    std::vector<kvc::DropSeq> plan;
+    std::string err;
+    int code = 0;
+    if (!c->bk.book.plan_truncate(tokens, plan, err, code)) return fail((kvc_status)code, "%s", err.c_str());
+    if (plan.empty()) return ok();
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    kvc_status st = c->ensure_cuda(stream);
+    if (st != KVC_OK) return st;
+    kvc::CopyArgs a{};
+    a.dst = c->copy_side();
+    a.n_targets = (int)plan.size();
+    a.targets = c->ws.dyn_payload;
+    a.img_bytes = a.targets + sizeof(kvc::CopyTarget) * plan.size();
+    a.dyn = c->wsp(c->ws.dyn);
+    cudaError_t e;
+    kvc::AppendImage small;
+    const bool fits = a.img_bytes <= sizeof(small);
+    if ((st = capturable(fits, stream)) != KVC_OK) return st;
+    unsigned char* img = fits ? reinterpret_cast<unsigned char*>(&small) : c->ring.reserve(a.img_bytes, &e);
+    if (!img) return cuda_fail(e, "staging");
+    c->bk.book.apply_truncate(plan);
+    c->fill_state(img);
+    kvc::CopyTarget* t = reinterpret_cast<kvc::CopyTarget*>(img + a.targets);
+    for (size_t i = 0; i < plan.size(); ++i) t[i] = {plan[i].s, (int32_t)plan[i].len_old, (int32_t)plan[i].len_new, 0};
+    c->last_was_decode = false;
+    if (fits) {
+      a.img = &small;
+    } else {
+      e = c->ring.commit(a.dyn, a.img_bytes, stream);
+      if (e != cudaSuccess) return cuda_fail(e, "upload of the sequences' state");
+    }
+    int launched = 0;
+    e = kvc::launch_drop(c->geom(), a, stream, &launched);
+    c->launches += launched;
+    if (e != cudaSuccess) return cuda_fail(e, "truncation kernel");
+    return ok();
+  });
+}
+
+kvc_status kvc_copy(kvc_cache* c, const kvc_cache* from, int n, const int32_t* dst, const int32_t* src, void* stream_) {
+  return guarded([&]() -> kvc_status {
+    if (!c || !from) return fail(KVC_ERR_INVALID_ARG, "cache/from are NULL");
+    if (n < 0 || (n > 0 && (!dst || !src))) return fail(KVC_ERR_INVALID_ARG, "sequence arrays");
+    const kvc_config &x = c->cfg, &y = from->cfg;
+    if (x.M != y.M || x.H != y.H || x.d_head != y.d_head || x.dtype != y.dtype || x.rotary_dim != y.rotary_dim ||
+        (x.rotary_dim > 0 && x.rope_base != y.rope_base))
+      return fail(KVC_ERR_INVALID_ARG, "the caches differ in layers, heads, d_head, type or rotation");
+    for (const kvc_cache* k : {static_cast<const kvc_cache*>(c), from})
+      if (k->layers_done != k->cfg.M)
+        return fail(KVC_ERR_STATE, "layers %d..%d of the last tokens are not written yet", k->layers_done, k->cfg.M - 1);
+    std::string err;
+    int code = 0;
+    if (!c->bk.book.check_copy(from->bk.book, n, dst, src, err, code)) return fail((kvc_status)code, "%s", err.c_str());
+    if (n == 0) return ok();
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    kvc_status st = c->ensure_cuda(stream);
+    if (st != KVC_OK) return st;
+    if (from->cuda_ready && from->device != c->device) return fail(KVC_ERR_STATE, "the caches are on different devices");
+    // targets by source, the sources in the order of their first target
+    std::vector<int32_t> slot((size_t)from->cfg.b, -1);
+    std::vector<kvc::CopySource> sources;
+    for (int i = 0; i < n; ++i) {
+      int32_t& k = slot[(size_t)src[i]];
+      if (k < 0) {
+        k = (int32_t)sources.size();
+        sources.push_back({src[i], (int32_t)from->bk.book.stored(src[i]), 0, 0});
+      }
+      ++sources[(size_t)k].n;
+    }
+    int64_t n_rows = 0;
+    for (size_t k = 0; k < sources.size(); ++k) {
+      if (k > 0) sources[k].first = sources[k - 1].first + sources[k - 1].n;
+      n_rows = std::max<int64_t>(n_rows, sources[k].len);
+    }
+    std::vector<kvc::CopyTarget> targets((size_t)n);
+    std::vector<int32_t> next(sources.size());
+    for (int i = 0; i < n; ++i) {
+      const size_t k = (size_t)slot[(size_t)src[i]];
+      targets[(size_t)(sources[k].first + next[k]++)] = {dst[i], (int32_t)c->bk.book.stored(dst[i]), sources[k].len, src[i]};
+    }
+    kvc::CopyArgs a{};
+    a.src = from->copy_side();
+    a.dst = c->copy_side();
+    a.n_sources = (int)sources.size();
+    a.n_targets = n;
+    a.n_rows = n_rows;
+    a.sources = c->ws.dyn_payload;
+    a.targets = a.sources + sizeof(kvc::CopySource) * sources.size();
+    a.img_bytes = a.targets + sizeof(kvc::CopyTarget) * targets.size();
+    a.dyn = c->wsp(c->ws.dyn);
+    cudaError_t e;
+    kvc::AppendImage small;
+    const bool fits = a.img_bytes <= sizeof(small);
+    if ((st = capturable(fits, stream)) != KVC_OK) return st;
+    unsigned char* img = fits ? reinterpret_cast<unsigned char*>(&small) : c->ring.reserve(a.img_bytes, &e);
+    if (!img) return cuda_fail(e, "staging");
+    c->bk.book.apply_copy(from->bk.book, n, dst, src);
+    c->fill_state(img);
+    std::memcpy(img + a.sources, sources.data(), sizeof(kvc::CopySource) * sources.size());
+    std::memcpy(img + a.targets, targets.data(), sizeof(kvc::CopyTarget) * targets.size());
+    c->last_was_decode = false;
+    if (fits) {
+      a.img = &small;
+    } else {
+      e = c->ring.commit(a.dyn, a.img_bytes, stream);
+      if (e != cudaSuccess) return cuda_fail(e, "upload of the copies' plan");
+    }
+    int launched = 0;
+    e = kvc::launch_copy(c->geom(), a, stream, &launched);
+    c->launches += launched;
+    if (e != cudaSuccess) return cuda_fail(e, "copy kernel");
+    return ok();
+  });
+}
+
 kvc_status kvc_prefill_attention(kvc_cache* c, int layer, const void* q, const int32_t* n_q, float scale, float* out,
                                  void* stream_) {
   if (!c) return fail(KVC_ERR_INVALID_ARG, "cache is NULL");
@@ -1660,6 +1885,7 @@ kvc_status kvc_prefill_attention(kvc_cache* c, int layer, const void* q, const i
   if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(KVC_ERR_INVALID_ARG, "scale must be positive and finite");
   if (c->cfg.policy == KVC_POLICY_LOCAL)
     return fail(KVC_ERR_UNSUPPORTED, "masked prefill is not defined for the local-attention cache");
+  if (c->packed()) return refuse_packed("the masked prefill");
   if ((int64_t)c->cfg.M * H * c->C >= ((int64_t)1 << 31))
     return fail(KVC_ERR_UNSUPPORTED, "M*H*sum(capacity) rows exceed the 2^31 rows a tensor-map coordinate reaches");
   if (layer >= c->layers_done) return fail(KVC_ERR_STATE, "layer %d of the last tokens is not written yet", layer);
@@ -1859,7 +2085,8 @@ kvc_status kvc_device_status(kvc_cache* c, void* stream_, int32_t* word) {
   e = cudaMemsetAsync(c->wsp(c->ws.hdr), 0, 4, stream);
   // a timed-out decode may leave split-K arrival counters behind: start them from zero again
   if (e == cudaSuccess && (w & kvc::STATUS_TIMEOUT))
-    e = cudaMemsetAsync(c->wsp(c->ws.counters), 0, 4 * (size_t)c->cfg.b * c->cfg.H, stream);
+    e = c->packed() ? cudaMemsetAsync(c->wsp(c->ws.packed_counters), 0, 4 * (size_t)kvc::kMaxPackedWorkers, stream)
+                    : cudaMemsetAsync(c->wsp(c->ws.counters), 0, 4 * (size_t)c->cfg.b * c->cfg.H, stream);
   if (e != cudaSuccess) return cuda_fail(e, "clear status");
   if (w & kvc::STATUS_TIMEOUT) return fail(KVC_ERR_TIMEOUT, "a kernel's bounded wait ran out (status 0x%x)", w);
   return fail(KVC_ERR_DEVICE_CHECK, "a kernel's consistency check failed (status 0x%x)", w);
