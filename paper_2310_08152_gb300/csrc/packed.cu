@@ -2,7 +2,6 @@
 //
 //   packed_append_kernel  new tokens' K/V rows, K rotated and rounded as the 16-bit append does it, into codes and pairs
 //   packed_move_kernel    the row moves of a compaction
-//   packed_decode_kernel  the decode over the codes
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -13,8 +12,6 @@
 
 namespace kvc {
 namespace {
-
-constexpr unsigned kFull = 0xFFFFFFFFu;
 
 // ---------------------------------------------------------------------------------------------
 // Append
@@ -177,92 +174,6 @@ __global__ void __launch_bounds__(kMoveThreads)
   }
 }
 
-// ---------------------------------------------------------------------------------------------
-// Decode: out = sum_j softmax_j(scale <q, k_j>) v_j over the rows that the query sees, with k_j = lo + step c_j a group of
-// columns:  <q, k_j> = sum over the groups of step <q, c_j> + lo sum(q).  A block a (layer, sequence, head); a row a thread
-// for the logits, a column a thread for the sum over the rows; running maximum and sum.
-// ---------------------------------------------------------------------------------------------
-struct PackedDev {
-  const DState* ds;
-  const uint16_t* q;
-  float* out;
-  int64_t q_stride, out_stride;
-  int layer;
-  float qscale;  // scale * log2(e)
-};
-
-template <typename T, int D>
-__global__ void __launch_bounds__(128) packed_decode_kernel(Geometry g, Static st, PackedBuffers pb, PackedDev p) {
-  using R = PackedRow<D>;
-  __shared__ float qs[D], raw[D], ps[128], red[4], gsum[R::G];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int h = blockIdx.x % g.H, s = (blockIdx.x / g.H) % g.b, li = blockIdx.x / (g.H * g.b);
-  const DState ds = p.ds[s];
-  if (ds.len <= ds.begin) return;
-  const uint16_t* q = p.q + li * p.q_stride + ((int64_t)s * g.H + h) * D;
-  if (tid < D) raw[tid] = T::f1(q[tid]);
-  __syncthreads();
-  if (tid < D) {
-    float x = raw[tid];
-    if (tid < g.rot) {
-      const int half = g.rot / 2;
-      float sn, cs;
-      rope_sincos_full(ds.qpos, st.rope_g[tid < half ? tid : tid - half], &sn, &cs);
-      x = tid < half ? x * cs - raw[tid + half] * sn : x * cs + raw[tid - half] * sn;
-    }
-    qs[tid] = x;
-  }
-  __syncthreads();
-  if (tid < R::G) {
-    float x = 0.f;
-    for (int c = 32 * tid; c < min(D, 32 * tid + 32); ++c) x += qs[c];
-    gsum[tid] = x;
-  }
-  const int64_t row0 = (int64_t)(p.layer + li) * g.H * g.C + st.seq_row0[s] + (int64_t)h * st.cap[s];
-  float m = -INFINITY, l = 0.f, o = 0.f;
-  for (int r0 = ds.begin; r0 < ds.len; r0 += 128) {
-    const int r = r0 + tid, n = min(128, ds.len - r0);
-    const bool seen = r < ds.len && !(r >= ds.mask_lo && r < ds.mask_hi);
-    __syncthreads();
-    float z = -INFINITY;
-    if (seen) {
-      z = 0.f;
-      for (int gg = 0; gg < R::G; ++gg) {
-        float x = 0.f;
-        for (int w = 4 * gg; w < min(R::W, 4 * gg + 4); ++w) {
-          const uint32_t word = reinterpret_cast<const uint32_t*>(pb.kc)[(row0 + r) * R::W + w];
-          for (int e = 0; e < 8; ++e) x = fmaf(qs[8 * w + e], (float)(word >> (4 * e) & 15u), x);
-        }
-        const uint32_t pair = pb.kp[(row0 + r) * R::G + gg];
-        z += T::f1((uint16_t)pair) * x + T::f1((uint16_t)(pair >> 16)) * gsum[gg];
-      }
-      z *= p.qscale;
-    }
-    float mx = z;
-    for (int i = 16; i > 0; i >>= 1) mx = fmaxf(mx, __shfl_xor_sync(kFull, mx, i));
-    if (lane == 0) red[warp] = mx;
-    __syncthreads();
-    mx = fmaxf(m, fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
-    const float ref = mx == -INFINITY ? 0.f : mx;
-    ps[tid] = seen ? exp2f(z - ref) : 0.f;
-    const float f = exp2f(m - ref);
-    __syncthreads();
-    m = mx;
-    l *= f;
-    o *= f;
-    for (int i = 0; i < n; ++i) {
-      if (r0 + i >= ds.mask_lo && r0 + i < ds.mask_hi) continue;
-      l += ps[i];
-      if (tid < D) {
-        const uint32_t word = reinterpret_cast<const uint32_t*>(pb.vc)[(row0 + r0 + i) * R::W + tid / 8];
-        const uint32_t pair = pb.vp[(row0 + r0 + i) * R::G + tid / 32];
-        o += ps[i] * fmaf(T::f1((uint16_t)pair), (float)(word >> (4 * (tid % 8)) & 15u), T::f1((uint16_t)(pair >> 16)));
-      }
-    }
-  }
-  if (tid < D) p.out[li * p.out_stride + ((int64_t)s * g.H + h) * D + tid] = o / l;
-}
-
 template <typename F>
 cudaError_t by_type(const Geometry& g, F&& f) {
   auto dtype = [&](auto dc) { return g.dtype == 1 ? f(BF16T{}, dc) : f(F16T{}, dc); };
@@ -309,27 +220,6 @@ cudaError_t launch_packed_move(const Geometry& g, const Static& st, const Packed
   return by_type(g, [&](auto, auto dc) {
     packed_move_kernel<decltype(dc)::value>
         <<<(unsigned)((int64_t)n_aff * g.M * 2 * g.H), kMoveThreads, 0, stream>>>(g, st, pb, aff, src_map);
-    return cudaGetLastError();
-  });
-}
-
-cudaError_t launch_packed_decode(const Geometry& g, const Static& st, const PackedBuffers& pb, const DecodeArgs& a,
-                                 int* status, int num_sms, cudaStream_t stream, int* grid, DecodePlan* plan) {
-  (void)status;
-  (void)num_sms;
-  PackedDev p;
-  p.ds = a.dstate;
-  p.q = static_cast<const uint16_t*>(a.q);
-  p.out = a.out;
-  p.q_stride = a.q_layer_stride;
-  p.out_stride = a.out_layer_stride;
-  p.layer = a.layer;
-  p.qscale = a.scale * 1.4426950408889634f;
-  const int64_t blocks = (int64_t)a.n_layers * g.b * g.H;
-  *grid = (int)blocks;
-  *plan = {5, (int)blocks * 4, 128, 1};
-  return by_type(g, [&](auto t, auto dc) {
-    packed_decode_kernel<decltype(t), decltype(dc)::value><<<(unsigned)blocks, 128, 0, stream>>>(g, st, pb, p);
     return cudaGetLastError();
   });
 }
