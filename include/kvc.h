@@ -190,7 +190,7 @@ typedef struct {
    * with difference, quotients and product rounded to binary32; a column stands for lo + step code, which is within step / 2
    * (1 + 2^-20) of x (where step is 0, within 15 x 2^-126).  A group that holds a NaN or an infinity, or whose range overflows, reads as NaN.
    * Layout: the codes [M][H * C] rows of d_head / 2 bytes, column c in bits 4 (c % 2) of byte c / 2; 256-byte aligned behind
-   * them the groups' pairs, [M][H * C] rows of (step, lo) pairs of `dtype`.  C and off are those of capacities rounded up to
+   * them the groups' pairs, [M][H * C] rows of (lo, step) pairs of `dtype`.  C and off are those of capacities rounded up to
    * multiples of 4 rows (so are pos and orig).
    * Such a cache has kvc_append and its variants, kvc_compress_spans, kvc_decode_attention and kvc_decode_attention_layers,
    * kvc_copy and kvc_truncate; what else reads or moves rows, and kvc_set_scores, is KVC_ERR_UNSUPPORTED: copy the sequences

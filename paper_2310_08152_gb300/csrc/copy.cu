@@ -143,7 +143,8 @@ __device__ __forceinline__ void copy_block(const CopyDev& p, const CopyPlan& pla
       for (int u = 0; u < U; ++u) {
         const int i = tid + u * kCopyThreads, r = i / R::CP, c = i % R::CP;
         if (r >= n || c >= R::W) continue;
-        const float step = T::f1((uint16_t)y[u]), lo = T::f1((uint16_t)(y[u] >> 16));
+        const float2 pv = pair_values(y[u], T{});
+        const float lo = pv.x, step = pv.y;
         uint32_t o[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e)

@@ -60,7 +60,7 @@ constexpr int kMaxDecodeWorkers = 8192;
 bool dhead_supported(int D);
 
 // The planes of a cache of 4 bits (packed.cuh): [M][H * C] rows of D / 2 bytes of codes and of packed_groups(D) words of
-// (step, lo) pairs, for K and for V.  Its sequences' capacities in the layout are multiples of kPackedRows, so that a run
+// (lo, step) pairs, for K and for V.  Its sequences' capacities in the layout are multiples of kPackedRows, so that a run
 // of rows that starts at a multiple of it starts at 16 bytes in every plane.
 struct PackedBuffers {
   unsigned char* kc;

@@ -6,13 +6,19 @@
 // by 1 / step in binary32, and stands for lo + step * code.  Rounding the step up keeps the group's largest value within
 // half a step of code 15; a group that holds a NaN or an infinity has a step of NaN and reads as NaN.
 //
-// A row's codes are D / 8 words, word w the columns 8 w .. 8 w + 7 from its low bits up; its (step, lo) pairs are a word a
-// group, the step in the low half.  Codes and pairs are planes of their own, in the layout of the rows.
+// A row's codes are D / 8 words, word w the columns 8 w .. 8 w + 7 from its low bits up; its (lo, step) pairs are a word a
+// group, the step in the high half.  Codes and pairs are planes of their own, in the layout of the rows.
 #pragma once
 
 #include "device_common.cuh"
 
 namespace kvc {
+
+// (lo, step) of a pair.
+__device__ __forceinline__ float2 pair_values(uint32_t pair, F16T) { return F16T::f2(pair); }
+__device__ __forceinline__ float2 pair_values(uint32_t pair, BF16T) {
+  return make_float2(__uint_as_float(pair << 16), __uint_as_float(pair & 0xFFFF0000u));
+}
 
 template <int D>
 struct PackedRow {
@@ -26,7 +32,7 @@ struct PackedRow {
 __device__ __forceinline__ uint16_t round_up16(float x, F16T) { return __half_as_ushort(__float2half_ru(x)); }
 __device__ __forceinline__ uint16_t round_up16(float x, BF16T) { return __bfloat16_as_ushort(__float2bfloat16_ru(x)); }
 
-// The code word of a lane's eight columns (values of the 16-bit type T), and the (step, lo) pair of its group, whose four
+// The code word of a lane's eight columns (values of the 16-bit type T), and the (lo, step) pair of its group, whose four
 // lanes are consecutive and call this together.  A lane without columns is not `active`.
 template <typename T>
 __device__ __forceinline__ uint32_t pack8(const float (&x)[8], bool active, uint32_t* pair) {
@@ -60,7 +66,7 @@ __device__ __forceinline__ uint32_t pack8(const float (&x)[8], bool active, uint
     const float t = fminf(__fmul_rn(__fsub_rn(x[e], lo), inv), 15.f);
     word |= (__float_as_uint(__fadd_rn(t, 8388608.f)) & 15u) << (4 * e);
   }
-  *pair = (uint32_t)s16 | (uint32_t)T::r(lo) << 16;
+  *pair = (uint32_t)T::r(lo) | (uint32_t)s16 << 16;
   return word;
 }
 

@@ -40,9 +40,12 @@ struct Shape {
   static constexpr int S = S_;
   static constexpr int KC = kTile * R::RB, KP = kTile * R::PB;
   static constexpr int STAGE = 2 * (KC + KP);  // K codes, K pairs, V codes, V pairs
-  static constexpr int PS = 2 * 8 * 32 * 2;    // weights times steps: [32-row block][column][row] f16; the query between pieces
+  // weights times steps: [column of the operand][row of both halves of a tile] as pairs of f16, the columns 16 bytes more
+  // than 128 apart, so that eight lanes' 16-byte loads meet no bank twice; the query between pieces
+  static constexpr int PW = 36;
+  static constexpr int PS = 4 * 8 * PW;
   static constexpr int SMEM = S * STAGE + PS + 8 * S;
-  static_assert(4 * D <= PS);
+  static_assert(4 * D <= PS && PS % 16 == 0);
 };
 
 struct PackedDev {
@@ -62,25 +65,21 @@ struct PackedDev {
   int kv_before_wait;
 };
 
-// A tile among all: x-th of the launch, r-th of its segment's Lc.
-struct Cursor {
-  int64_t x, Lc, r;
+// A segment among all.
+struct Segment {
   int s, h, layer;
-  // to the next tile, which exists if x + 1 < hi
-  __device__ __forceinline__ void advance(int64_t hi, const int64_t* P, int H, int b) {
-    ++x;
-    if (++r < Lc || x >= hi) return;
-    r = 0;
-    if (++h == H) {
-      h = 0;
-      do {
-        if (++s == b) {
-          s = 0;
-          ++layer;
-        }
-      } while (P[s + 1] == P[s]);
-      Lc = P[s + 1] - P[s];
-    }
+  int tiles;
+  // to the next one with tiles, which exists
+  __device__ __forceinline__ void advance(const int64_t* P, int H, int b) {
+    if (++h < H) return;
+    h = 0;
+    do {
+      if (++s == b) {
+        s = 0;
+        ++layer;
+      }
+      tiles = (int)(P[s + 1] - P[s]);
+    } while (tiles == 0);
   }
 };
 
@@ -120,7 +119,16 @@ __device__ __forceinline__ uint32_t high_codes(uint32_t w) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-__device__ __forceinline__ float half_bits(uint32_t h) { return __half2float(__ushort_as_half((uint16_t)h)); }
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float warp_max(float x) {  // of the numbers among them
+  float y;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+  return y;
+}
 __device__ __forceinline__ uint32_t pack_halves(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
@@ -134,9 +142,40 @@ __device__ __forceinline__ void key_word(float (&c)[4], uint32_t a, uint32_t b, 
   mma(c, low_codes(a), low_codes(b), high_codes(a), high_codes(b), q[2], q[3]);
 }
 
-// 16 rows of the values' product for four columns: two of rows 0, 4 (x01) and 8, 12 (x23), and the two eight bits up.
+// 16 rows of the values' product for four columns: two of the rows in x01 (a tile's halves side by side) and x23, and the two
+// eight bits up.
 __device__ __forceinline__ void value_pair(float (&c)[4], uint32_t x01, uint32_t x23, uint32_t b0, uint32_t b1) {
   mma(c, low_codes(x01), high_codes(x01), low_codes(x23), high_codes(x23), b0, b1);
+}
+
+// A row's weight goes into the running maximum times a power of two that is not below half its largest step, so that weight
+// times step stays in f16's range whatever the steps are: the exponent of that power, as a number.  With bf16 also not below
+// 2^-20 of its least values, whose product with a weight f32 would not hold otherwise, and at least 2^-88: a weight is at most
+// 2^102, and the sum of 2^25 of them in f32's range (smaller steps' products end earlier than 2^15; below 2^-110 they lose
+// bits).  Steps that are not finite do not count.
+template <int G>
+__device__ __forceinline__ float row_exponent(const uint32_t (&pair)[G], F16T) {
+  uint32_t big = pair[0];
+#pragma unroll
+  for (int i = 1; i < G; ++i) big = max(big, pair[i]);
+  if (big >= 0x7C000000u) {
+    big = 0;
+#pragma unroll
+    for (int i = 0; i < G; ++i)
+      if (pair[i] < 0x7C000000u) big = max(big, pair[i]);
+  }
+  return __uint_as_float(0x4B000000u | big >> 26) - 8388623.f;  // 2^23 + field, less 2^23 + 15
+}
+template <int G>
+__device__ __forceinline__ float row_exponent(const uint32_t (&pair)[G], BF16T) {
+  int big = 39 << 23;
+#pragma unroll
+  for (int i = 0; i < G; ++i) {
+    const int step = (int)pair[i], least = (int)(pair[i] << 16 & 0x7FFFFFFFu) - (20 << 23);
+    if (step < 0x7F800000) big = max(big, step);
+    if (least < 0x7F800000 - (20 << 23)) big = max(big, least);
+  }
+  return __uint_as_float(0x4B000000u | (uint32_t)big >> 23) - 8388735.f;
 }
 
 template <typename T, int D, int S>
@@ -150,13 +189,14 @@ __global__ void __launch_bounds__(32, D == 128 ? 10 : D == 96 ? 13 : 16)
   constexpr int QF = 2 * (D / 16);                  // registers of the query
   extern __shared__ __align__(128) unsigned char smem[];
   pdl_launch_dependents();
-  const int lane = threadIdx.x, gr = lane >> 2, t = lane & 3;
+  const int lane = threadIdx.x, gr = lane >> 2, t = lane & 3, tg = t < G ? t : G - 1;
   const int wid = blockIdx.x, H = g.H;
   const int64_t Rt = (int64_t)p.n_layers * p.R;
   const int64_t lo = (int64_t)wid * Rt / p.NW, hi = (int64_t)(wid + 1) * Rt / p.NW;
 
   unsigned char* ps = smem + S * C::STAGE;
   float* qs = reinterpret_cast<float*>(ps);
+  uint32_t* pw = reinterpret_cast<uint32_t*>(ps);
   uint64_t* full = reinterpret_cast<uint64_t*>(ps + C::PS);
   if (lane == 0) {
 #pragma unroll
@@ -167,50 +207,58 @@ __global__ void __launch_bounds__(32, D == 128 ? 10 : D == 96 ? 13 : 16)
   __syncwarp();
   if (!p.kv_before_wait) pdl_wait();
 
-  Cursor ci;  // consumed tiles
-  ci.x = lo;
-  ci.layer = (int)(lo / p.R);
+  Segment cs;      // of the consumed tiles
+  int r;           // the next one in it
+  int64_t x = lo;  // and among all
   {
-    const int64_t o = lo - (int64_t)ci.layer * p.R;
-    ci.s = seq_of(p.P, g.b, H, o, lane);
-    const int64_t P0 = p.P[ci.s];
-    ci.Lc = p.P[ci.s + 1] - P0;
-    ci.h = (int)((o - (int64_t)H * P0) / ci.Lc);
-    ci.r = o - (int64_t)H * P0 - (int64_t)ci.h * ci.Lc;
+    cs.layer = (int)(lo / p.R);
+    const int64_t o = lo - (int64_t)cs.layer * p.R;
+    cs.s = seq_of(p.P, g.b, H, o, lane);
+    const int64_t P0 = p.P[cs.s];
+    cs.tiles = (int)(p.P[cs.s + 1] - P0);
+    cs.h = (int)((o - (int64_t)H * P0) / cs.tiles);
+    r = (int)(o - (int64_t)H * P0 - (int64_t)cs.h * cs.tiles);
   }
-  Cursor ii = ci;  // issued tiles (lane 0)
-  int is = -1, i_begin = 0, i_len = 0, i_cap = 0;
-  int64_t i_row0 = 0;
+  // lane 0 issues copies: the segment, its rows from the next tile on, that tile's place in the planes, and how many are left
+  Segment is = cs;
+  int i_rows = 0;
+  int64_t i_code = 0, i_pair = 0, i_left = hi - lo;
+  auto i_segment = [&](int first) {
+    const DState d = p.ds[is.s];
+    const int r0 = d.begin / kPackedRows * kPackedRows + first * kTile;
+    const int64_t row = (int64_t)(p.layer + is.layer) * H * g.C + st.seq_row0[is.s] + (int64_t)is.h * st.cap[is.s] + r0;
+    i_rows = d.len - r0;
+    i_code = row * R::RB;
+    i_pair = row * R::PB;
+  };
   auto issue = [&](int stage) {
-    if (ii.s != is) {
-      is = ii.s;
-      const DState d = p.ds[is];
-      i_begin = d.begin / kPackedRows * kPackedRows;
-      i_len = d.len;
-      i_row0 = st.seq_row0[is];
-      i_cap = st.cap[is];
-    }
-    const int r0 = i_begin + (int)ii.r * kTile;
-    const uint32_t n = (uint32_t)((min(kTile, i_len - r0) + kPackedRows - 1) / kPackedRows * kPackedRows);
-    const int64_t row = (int64_t)(p.layer + ii.layer) * H * g.C + i_row0 + (int64_t)ii.h * i_cap + r0;
+    const uint32_t n = (uint32_t)min(kTile, (i_rows + kPackedRows - 1) & -kPackedRows);
     unsigned char* to = smem + stage * C::STAGE;
     mbar_arrive_expect_tx(&full[stage], 2 * n * (R::RB + R::PB));
-    bulk_g2s(to, pb.kc + row * R::RB, n * R::RB, &full[stage]);
-    bulk_g2s(to + C::KC, pb.kp + row * R::G, n * R::PB, &full[stage]);
-    bulk_g2s(to + C::KC + C::KP, pb.vc + row * R::RB, n * R::RB, &full[stage]);
-    bulk_g2s(to + 2 * C::KC + C::KP, pb.vp + row * R::G, n * R::PB, &full[stage]);
-    ii.advance(hi, p.P, H, g.b);
+    bulk_g2s(to, pb.kc + i_code, n * R::RB, &full[stage]);
+    bulk_g2s(to + C::KC, reinterpret_cast<const unsigned char*>(pb.kp) + i_pair, n * R::PB, &full[stage]);
+    bulk_g2s(to + C::KC + C::KP, pb.vc + i_code, n * R::RB, &full[stage]);
+    bulk_g2s(to + 2 * C::KC + C::KP, reinterpret_cast<const unsigned char*>(pb.vp) + i_pair, n * R::PB, &full[stage]);
+    i_rows -= kTile;
+    i_code += C::KC;
+    i_pair += C::KP;
+    if (--i_left > 0 && i_rows <= 0) {
+      is.advance(p.P, H, g.b);
+      i_segment(0);
+    }
   };
   // a decode before this one writes neither rows nor state: they may come before it is complete, while the query, the outputs
   // and the parts may be shared with it
-  if (lane == 0)
-    for (int i = 0; i < S && ii.x < hi; ++i) issue(i);
+  if (lane == 0) {
+    i_segment(r);
+    for (int i = 0; i < S && i_left > 0; ++i) issue(i);
+  }
   if (p.kv_before_wait) pdl_wait();
 
   // the query of a segment, fetched a piece ahead: columns lane + 32 j, and those they are rotated with
   constexpr int QL = (D + 31) / 32;
   float qa[QL], qb[QL];
-  auto fetch_q = [&](const Cursor& c) {
+  auto fetch_q = [&](const Segment& c) {
     const uint16_t* row = p.q + (int64_t)c.layer * p.q_stride + ((int64_t)c.s * H + c.h) * D;
     const int half = g.rot / 2;
 #pragma unroll
@@ -223,36 +271,35 @@ __global__ void __launch_bounds__(32, D == 128 ? 10 : D == 96 ? 13 : 16)
       }
     }
   };
-  fetch_q(ci);
-
-  uint32_t qf[QF];      // the query as the keys' other operand
-  float qsum = 0.f;     // its sum over group t's columns, times qscale
-  float kscale = 0.f;   // of a product of codes and the query's parts
-  float o[2 * NT], l = 0.f, los[G], m = -INFINITY;
-  DState ds = p.ds[ci.s];
+  fetch_q(cs);
+  DState ds = p.ds[cs.s];
   int stage = 0;
   uint32_t phase = 0;
-  bool fresh = true;
 
-  while (ci.x < hi) {
-    if (fresh) {  // a new piece
-      fresh = false;
+  while (x < hi) {
+    // ---- a piece: tiles [r, r1) of a segment
+    const int r1 = (int)min((int64_t)cs.tiles, r + (hi - x));
+    const int64_t seg0 = x - r, seg1 = seg0 + cs.tiles;  // the segment's tiles among all
+    uint32_t qf[QF];  // the query as the keys' other operand
+    float qsum;       // its sum over group t's columns, times qscale
+    float kscale;     // of a product of codes and the query's parts
+    {
       float sum[QL], big = 0.f;
 #pragma unroll
       for (int j = 0; j < QL; ++j) {
         const int k = lane + 32 * j;
         if (k < g.rot) {
           const int half = g.rot / 2;
-          float sn, cs;
-          rope_sincos_full(ds.qpos, st.rope_g[k < half ? k : k - half], &sn, &cs);
-          qa[j] = k < half ? qa[j] * cs - qb[j] * sn : qa[j] * cs + qb[j] * sn;
+          float sn, c;
+          rope_sincos_full(ds.qpos, st.rope_g[k < half ? k : k - half], &sn, &c);
+          qa[j] = k < half ? qa[j] * c - qb[j] * sn : qa[j] * c + qb[j] * sn;
         }
         sum[j] = qa[j];
         big = fmaxf(big, fabsf(qa[j]));
       }
+      big = warp_max(big);
 #pragma unroll
       for (int i = 16; i > 0; i >>= 1) {
-        big = fmaxf(big, __shfl_xor_sync(kFull, big, i));
 #pragma unroll
         for (int j = 0; j < QL; ++j) sum[j] += __shfl_xor_sync(kFull, sum[j], i);
       }
@@ -260,7 +307,10 @@ __global__ void __launch_bounds__(32, D == 128 ? 10 : D == 96 ? 13 : 16)
       const int e = big > 0.f && big < INFINITY ? max(-115, min(115, 13 - (int)(__float_as_uint(big) >> 23) + 127)) : 0;
       const float up = __uint_as_float((uint32_t)(127 + e) << 23);
       kscale = p.qscale * __uint_as_float((uint32_t)(127 - e) << 23);
-      qsum = (t == 0 ? sum[0] : t == 1 ? sum[1] : t == 2 && QL > 2 ? sum[QL > 2 ? 2 : 0] : QL > 3 ? sum[QL > 3 ? 3 : 0] : 0.f) * p.qscale;
+      qsum = 0.f;
+#pragma unroll
+      for (int j = 0; j < QL; ++j)
+        if (t == j) qsum = sum[j] * p.qscale;
       __syncwarp();  // the weights of the piece before are read
 #pragma unroll
       for (int j = 0; j < QL; ++j)
@@ -268,9 +318,9 @@ __global__ void __launch_bounds__(32, D == 128 ? 10 : D == 96 ? 13 : 16)
       __syncwarp();
       // column gr of the operand: group gr / 2, part gr % 2
       auto part = [&](int k) {
-        const float x = (k >> 5) == (gr >> 1) ? qs[k] : 0.f;
-        const float h = __half2float(__float2half_rn(x));
-        return gr & 1 ? x - h : h;
+        const float y = (k >> 5) == (gr >> 1) ? qs[k] : 0.f;
+        const float h = __half2float(__float2half_rn(y));
+        return gr & 1 ? y - h : h;
       };
       auto word = [&](int k, uint32_t* f) {
         f[0] = pack_halves(part(k), part(k + 4));
@@ -286,74 +336,70 @@ __global__ void __launch_bounds__(32, D == 128 ? 10 : D == 96 ? 13 : 16)
         qf[9] = pack_halves(part(64 + 4 * t + 1), part(64 + 4 * t + 3));
       }
       __syncwarp();
-#pragma unroll
-      for (int i = 0; i < 2 * NT; ++i) o[i] = 0.f;
-#pragma unroll
-      for (int i = 0; i < G; ++i) los[i] = 0.f;
-      l = 0.f;
-      m = -INFINITY;
     }
+    float o[2 * NT], l = 0.f, los[G], m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 2 * NT; ++i) o[i] = 0.f;
+#pragma unroll
+    for (int i = 0; i < G; ++i) los[i] = 0.f;
 
-    // ---- a tile
-    if (!__all_sync(kFull, mbar_wait_bounded(&full[stage], phase, p.limit_ns))) {
-      if (lane == 0) {
-        atomicOr(p.status, STATUS_TIMEOUT);
-        // the copies that are still in flight end before their memory does
-        for (int64_t i = ci.x; i < ii.x; ++i) {
-          mbar_wait_bounded(&full[stage], phase, p.limit_ns);
-          if (++stage == S) {
-            stage = 0;
-            phase ^= 1;
+    int r0 = ds.begin / kPackedRows * kPackedRows + r * kTile;
+    x += r1 - r;
+    for (; r < r1; ++r, r0 += kTile) {
+      // ---- a tile
+      if (!__all_sync(kFull, mbar_wait_bounded(&full[stage], phase, p.limit_ns))) {
+        if (lane == 0) {
+          atomicOr(p.status, STATUS_TIMEOUT);
+          // the copies that are still in flight end before their memory does
+          const int64_t taken = x - lo - (r1 - r);
+          for (int64_t i = taken; i < hi - lo - i_left; ++i) {
+            mbar_wait_bounded(&full[stage], phase, p.limit_ns);
+            if (++stage == S) {
+              stage = 0;
+              phase ^= 1;
+            }
           }
         }
+        __syncwarp();
+        return;  // the segment is not joined
       }
-      __syncwarp();
-      return;  // the segment is not joined
-    }
-    const unsigned char* kc = smem + stage * C::STAGE;
-    const uint32_t* kp = reinterpret_cast<const uint32_t*>(kc + C::KC);
-    const unsigned char* vc = kc + C::KC + C::KP;
-    const uint32_t* vp = reinterpret_cast<const uint32_t*>(vc + C::KC);
-    const int r0 = ds.begin / kPackedRows * kPackedRows + (int)ci.r * kTile;
-    const int nb = ds.len - r0 > 32 ? 2 : 1;  // blocks of 32 rows with rows
+      const unsigned char* kc = smem + stage * C::STAGE;
+      const uint32_t* kp = reinterpret_cast<const uint32_t*>(kc + C::KC);
+      const unsigned char* vc = kc + C::KC + C::KP;
+      const uint32_t* vp = reinterpret_cast<const uint32_t*>(vc + C::KC);
 
-    float z[2];
+      float z[2];  // logits of rows gr + 8 t of the tile's halves
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      z[b] = 0.f;
-      if (b < nb) {
+      for (int b = 0; b < 2; ++b) {
         float v[4];  // lane t's group's part of the logits of rows gr + 8 i
 #pragma unroll
         for (int a = 0; a < 2; ++a) {
           const int row = 32 * b + 16 * a + gr;
-          const unsigned char *x = kc + row * R::RB, *y = x + 8 * R::RB;
+          const unsigned char *u0 = kc + row * R::RB, *w0 = u0 + 8 * R::RB;
           float c[4] = {0.f, 0.f, 0.f, 0.f};
           if constexpr (D == 128) {
-            const uint4 u = *reinterpret_cast<const uint4*>(x + 16 * t), w = *reinterpret_cast<const uint4*>(y + 16 * t);
+            const uint4 u = *reinterpret_cast<const uint4*>(u0 + 16 * t), w = *reinterpret_cast<const uint4*>(w0 + 16 * t);
             key_word(c, u.x, w.x, reinterpret_cast<const uint32_t(&)[4]>(qf[0]));
             key_word(c, u.y, w.y, reinterpret_cast<const uint32_t(&)[4]>(qf[4]));
             key_word(c, u.z, w.z, reinterpret_cast<const uint32_t(&)[4]>(qf[8]));
             key_word(c, u.w, w.w, reinterpret_cast<const uint32_t(&)[4]>(qf[12]));
           } else {
-            const uint2 u = *reinterpret_cast<const uint2*>(x + 8 * t), w = *reinterpret_cast<const uint2*>(y + 8 * t);
+            const uint2 u = *reinterpret_cast<const uint2*>(u0 + 8 * t), w = *reinterpret_cast<const uint2*>(w0 + 8 * t);
             key_word(c, u.x, w.x, reinterpret_cast<const uint32_t(&)[4]>(qf[0]));
             key_word(c, u.y, w.y, reinterpret_cast<const uint32_t(&)[4]>(qf[4]));
           }
           if constexpr (D == 96)
-            key_word(c, *reinterpret_cast<const uint32_t*>(x + 32 + 4 * t), *reinterpret_cast<const uint32_t*>(y + 32 + 4 * t),
+            key_word(c, *reinterpret_cast<const uint32_t*>(u0 + 32 + 4 * t), *reinterpret_cast<const uint32_t*>(w0 + 32 + 4 * t),
                      reinterpret_cast<const uint32_t(&)[4]>(qf[8]));
           if constexpr (D == 80) {  // four columns: the second byte's go to the upper half
-            const uint32_t u = __byte_perm(*reinterpret_cast<const uint16_t*>(x + 32 + 2 * t), 0, 0x4140);
-            const uint32_t w = __byte_perm(*reinterpret_cast<const uint16_t*>(y + 32 + 2 * t), 0, 0x4140);
+            const uint32_t u = __byte_perm(*reinterpret_cast<const uint16_t*>(u0 + 32 + 2 * t), 0, 0x4140);
+            const uint32_t w = __byte_perm(*reinterpret_cast<const uint16_t*>(w0 + 32 + 2 * t), 0, 0x4140);
             mma(c, low_codes(u), low_codes(w), high_codes(u), high_codes(w), qf[8], qf[9]);
           }
-          v[2 * a] = v[2 * a + 1] = 0.f;
-          if (t < G) {
-            const uint32_t p0 = kp[row * G + t], p1 = kp[(row + 8) * G + t];
-            const float s0 = T::f1((uint16_t)p0), s1 = T::f1((uint16_t)p1);
-            v[2 * a] = fmaf(s0, (c[0] + c[1]) * kscale, fmaf(8.f, s0, T::f1((uint16_t)(p0 >> 16))) * qsum);
-            v[2 * a + 1] = fmaf(s1, (c[2] + c[3]) * kscale, fmaf(8.f, s1, T::f1((uint16_t)(p1 >> 16))) * qsum);
-          }
+          // a lane past the groups has a product and a sum of 0
+          const float2 p0 = pair_values(kp[row * G + tg], T{}), p1 = pair_values(kp[(row + 8) * G + tg], T{});
+          v[2 * a] = fmaf(p0.y, fmaf(c[0] + c[1], kscale, 8.f * qsum), p0.x * qsum);
+          v[2 * a + 1] = fmaf(p1.y, fmaf(c[2] + c[3], kscale, 8.f * qsum), p1.x * qsum);
         }
         // the sum over the groups; lane t is left with row gr + 8 t
         const bool odd = t & 1, two = t & 2;
@@ -361,124 +407,105 @@ __global__ void __launch_bounds__(32, D == 128 ? 10 : D == 96 ? 13 : 16)
         const float s1 = (odd ? v[3] : v[2]) + __shfl_xor_sync(kFull, odd ? v[2] : v[3], 1);
         z[b] = (two ? s1 : s0) + __shfl_xor_sync(kFull, two ? s0 : s1, 2);
       }
-    }
 
-    // the lane's rows (gr + 8 t of each block): the values' pairs, and the exponent of the row's largest step, which goes
-    // into the running maximum, so that weight times step stays in f16's range whatever the steps are
-    bool seen[2];
-    uint32_t vpair[2][G];
-    float zs[2];
+      uint32_t vpair[2][G];
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const int row = 32 * b + 8 * t + gr, at = r0 + row;
-      seen[b] = at >= ds.begin && at < ds.len && !(at >= ds.mask_lo && at < ds.mask_hi);
-      uint32_t big = 0;
+      for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int i = 0; i < G; ++i) {
-        vpair[b][i] = vp[row * G + i];
-        const uint32_t s = vpair[b][i] & 0xFFFFu;
-        if (s < (std::is_same_v<T, F16T> ? 0x7C00u : 0x7F80u)) big = max(big, s);
-        if constexpr (std::is_same_v<T, BF16T>) {  // and of 2^-20 of its least values, which f32 would not hold times a weight
-          const uint32_t x = vpair[b][i] >> 16 & 0x7FFFu;
-          if (x < 0x7F80u) big = max(big, x > (20u << 7) ? x - (20u << 7) : 0u);
+        for (int i = 0; i < G; ++i) vpair[b][i] = vp[(32 * b + 8 * t + gr) * G + i];
+      if (r0 < ds.begin || r0 + kTile > ds.len || (ds.mask_lo < r0 + kTile && ds.mask_hi > r0)) {  // not all of it is seen
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const int at = r0 + 32 * b + 8 * t + gr;
+          if (at >= ds.begin && at < ds.len && !(at >= ds.mask_lo && at < ds.mask_hi)) continue;
+          z[b] = -INFINITY;
+#pragma unroll
+          for (int i = 0; i < G; ++i) vpair[b][i] = 0;
         }
       }
-      // from 2^-88 on: a weight is at most 2^102, and the sum of 2^25 of them in f32's range (with smaller steps the weights times
-      // them end earlier than 2^15, and below 2^-110 they lose bits)
-      const int e = max((int)(__float_as_uint(T::f1((uint16_t)big)) >> 23) - 127, -88);
-      zs[b] = seen[b] ? z[b] + (float)e : -INFINITY;
-    }
-    float mx = fmaxf(zs[0], zs[1]);
+      const float mx = warp_max(fmaxf(z[0] + row_exponent(vpair[0], T{}), z[1] + row_exponent(vpair[1], T{})));
+      if (mx > m + 4.f) {  // the reference moves where weights times steps would pass 2^15
+        const float f = exp2_fast(m - mx);
 #pragma unroll
-    for (int i = 16; i > 0; i >>= 1) mx = fmaxf(mx, __shfl_xor_sync(kFull, mx, i));
-    if (mx > m + 4.f) {  // of the warp: the reference moves where weights times steps would pass 2^15
-      const float f = exp2f(m - mx);
+        for (int i = 0; i < 2 * NT; ++i) o[i] *= f;
 #pragma unroll
-      for (int i = 0; i < 2 * NT; ++i) o[i] *= f;
-#pragma unroll
-      for (int i = 0; i < G; ++i) los[i] *= f;
-      l *= f;
-      m = mx;
-    }
-    const float ref = m == -INFINITY ? 10.f : 10.f - m;
-    uint16_t* pw = reinterpret_cast<uint16_t*>(ps);
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const float w = seen[b] ? exp2f(z[b] + ref) : 0.f;
-      l += w;
-      const int at = 256 * b + 8 * (gr & 3) + 2 * t + (gr >> 2);  // of row r = gr + 8 t: 8 (r % 4) + r / 4
+        for (int i = 0; i < G; ++i) los[i] *= f;
+        l *= f;
+        m = mx;
+      }
+      const float ref = m == -INFINITY ? 10.f : 10.f - m;
+      const float e0 = exp2_fast(z[0] + ref), e1 = exp2_fast(z[1] + ref);
+      l += e0 + e1;
+      const int at = 8 * (gr & 3) + 2 * t + (gr >> 2);  // of row i = gr + 8 t of the halves: 8 (i % 4) + i / 4
 #pragma unroll
       for (int i = 0; i < G; ++i) {
-        const float step = T::f1((uint16_t)vpair[b][i]), least = T::f1((uint16_t)(vpair[b][i] >> 16));
-        const float x = seen[b] ? w * step : 0.f;
-        if (seen[b]) los[i] = fmaf(w, fmaf(8.f, step, least), los[i]);
-        const __half h = __float2half_rn(x);
-        pw[at + 64 * i] = __half_as_ushort(h);
-        pw[at + 64 * i + 32] = __half_as_ushort(__float2half_rn(x - __half2float(h)));
+        const float2 p0 = pair_values(vpair[0][i], T{}), p1 = pair_values(vpair[1][i], T{});
+        const float x0 = e0 * p0.y, x1 = e1 * p1.y;
+        los[i] = fmaf(8.f, x0 + x1, fmaf(e0, p0.x, fmaf(e1, p1.x, los[i])));
+        const uint32_t h = pack_halves(x0, x1);
+        const float2 back = F16T::f2(h);
+        pw[2 * i * C::PW + at] = h;
+        pw[(2 * i + 1) * C::PW + at] = pack_halves(x0 - back.x, x1 - back.y);
       }
-    }
-    __syncwarp();
+      __syncwarp();
 
-    float acc[NT][4];
+      float acc[NT][4];
 #pragma unroll
-    for (int i = 0; i < NT; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
+      for (int i = 0; i < NT; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      if (b < nb) {
-        const uint4 wb = *reinterpret_cast<const uint4*>(pw + 256 * b + 32 * gr + 8 * t);
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {  // 16 rows: t + 4 i of the block's half
-          const uint32_t b0 = k ? wb.z : wb.x, b1 = k ? wb.w : wb.y;
-          const unsigned char* x = vc + (32 * b + 16 * k + t) * R::RB;
-          auto word = [&](int i, uint32_t w0, uint32_t w1, uint32_t w2, uint32_t w3) {
-            uint32_t u = __byte_perm(w0, w1, 0x5410), v = __byte_perm(w2, w3, 0x5410);
-            value_pair(acc[i], u, v, b0, b1);
-            value_pair(acc[i + 1], u >> 8, v >> 8, b0, b1);
-            u = __byte_perm(w0, w1, 0x7632), v = __byte_perm(w2, w3, 0x7632);
-            value_pair(acc[i + 2], u, v, b0, b1);
-            value_pair(acc[i + 3], u >> 8, v >> 8, b0, b1);
-          };
-          if constexpr (D == 128) {
-            const uint2 w0 = *reinterpret_cast<const uint2*>(x + 8 * gr);
-            const uint2 w1 = *reinterpret_cast<const uint2*>(x + 4 * R::RB + 8 * gr);
-            const uint2 w2 = *reinterpret_cast<const uint2*>(x + 8 * R::RB + 8 * gr);
-            const uint2 w3 = *reinterpret_cast<const uint2*>(x + 12 * R::RB + 8 * gr);
-            word(0, w0.x, w1.x, w2.x, w3.x);
-            word(4, w0.y, w1.y, w2.y, w3.y);
-          } else {
-            auto at = [&](int i) { return *reinterpret_cast<const uint32_t*>(x + 4 * i * R::RB + 4 * gr); };
-            word(0, at(0), at(1), at(2), at(3));
-          }
-          if constexpr (D == 96) {  // the last four words, half a word a lane
-            auto at = [&](int i) { return (uint32_t)*reinterpret_cast<const uint16_t*>(x + 4 * i * R::RB + 32 + 2 * gr); };
-            const uint32_t u = __byte_perm(at(0), at(1), 0x5410), v = __byte_perm(at(2), at(3), 0x5410);
-            value_pair(acc[4], u, v, b0, b1);
-            value_pair(acc[5], u >> 8, v >> 8, b0, b1);
-          }
-          if constexpr (D == 80) {  // the last two, a byte a lane
-            auto at = [&](int i) { return (uint32_t)x[4 * i * R::RB + 32 + gr]; };
-            value_pair(acc[4], at(0) | at(1) << 16, at(2) | at(3) << 16, b0, b1);
-          }
+      for (int k = 0; k < 4; ++k) {  // rows t + 8 k and t + 8 k + 4 of both halves
+        const uint2 w = *reinterpret_cast<const uint2*>(pw + gr * C::PW + 8 * t + 2 * k);
+        const unsigned char* u = vc + (8 * k + t) * R::RB;
+        auto word = [&](int i, uint32_t w0, uint32_t w1, uint32_t w2, uint32_t w3) {
+          uint32_t y = __byte_perm(w0, w1, 0x5410), v = __byte_perm(w2, w3, 0x5410);
+          value_pair(acc[i], y, v, w.x, w.y);
+          value_pair(acc[i + 1], y >> 8, v >> 8, w.x, w.y);
+          y = __byte_perm(w0, w1, 0x7632), v = __byte_perm(w2, w3, 0x7632);
+          value_pair(acc[i + 2], y, v, w.x, w.y);
+          value_pair(acc[i + 3], y >> 8, v >> 8, w.x, w.y);
+        };
+        constexpr int HALF = 32 * R::RB, NEXT = 4 * R::RB;
+        if constexpr (D == 128) {
+          auto at2 = [&](int j) { return *reinterpret_cast<const uint2*>(u + j + 8 * gr); };
+          const uint2 w0 = at2(0), w1 = at2(HALF), w2 = at2(NEXT), w3 = at2(HALF + NEXT);
+          word(0, w0.x, w1.x, w2.x, w3.x);
+          word(4, w0.y, w1.y, w2.y, w3.y);
+        } else {
+          auto at1 = [&](int j) { return *reinterpret_cast<const uint32_t*>(u + j + 4 * gr); };
+          word(0, at1(0), at1(HALF), at1(NEXT), at1(HALF + NEXT));
+        }
+        if constexpr (D == 96) {  // the last four words, half a word a lane
+          auto at1 = [&](int j) { return (uint32_t)*reinterpret_cast<const uint16_t*>(u + j + 32 + 2 * gr); };
+          const uint32_t y = __byte_perm(at1(0), at1(HALF), 0x5410), v = __byte_perm(at1(NEXT), at1(HALF + NEXT), 0x5410);
+          value_pair(acc[4], y, v, w.x, w.y);
+          value_pair(acc[5], y >> 8, v >> 8, w.x, w.y);
+        }
+        if constexpr (D == 80) {  // the last two, a byte a lane
+          auto at1 = [&](int j) { return (uint32_t)u[j + 32 + gr]; };
+          value_pair(acc[4], at1(0) | at1(HALF) << 16, at1(NEXT) | at1(HALF + NEXT) << 16, w.x, w.y);
         }
       }
-    }
 #pragma unroll
-    for (int i = 0; i < NT; ++i) {
-      o[2 * i] += acc[i][0] + acc[i][1];
-      o[2 * i + 1] += acc[i][2] + acc[i][3];
-    }
-    __syncwarp();  // the stage and the weights are read
-    if (lane == 0 && ii.x < hi) issue(stage);
-    if (++stage == S) {
-      stage = 0;
-      phase ^= 1;
+      for (int i = 0; i < NT; ++i) {
+        o[2 * i] += acc[i][0] + acc[i][1];
+        o[2 * i + 1] += acc[i][2] + acc[i][3];
+      }
+      __syncwarp();  // the stage and the weights are read
+      if (lane == 0 && i_left > 0) issue(stage);
+      if (++stage == S) {
+        stage = 0;
+        phase ^= 1;
+      }
     }
 
     // ---- the end of a piece
-    const Cursor was = ci;
-    ci.advance(hi, p.P, H, g.b);
-    if (ci.x < hi && was.r + 1 < was.Lc) continue;
-    if (ci.x < hi) fetch_q(ci);
+    const Segment was = cs;
+    if (x < hi) {
+      cs.advance(p.P, H, g.b);
+      fetch_q(cs);
+      if (cs.s != was.s) ds = p.ds[cs.s];
+    }
+    r = 0;
 #pragma unroll
     for (int i = 16; i > 0; i >>= 1) {
       l += __shfl_xor_sync(kFull, l, i);
@@ -495,11 +522,7 @@ __global__ void __launch_bounds__(32, D == 128 ? 10 : D == 96 ? 13 : 16)
     for (int k = 1; k < G; ++k)
       if (t == k) mine = los[k];
 #pragma unroll
-    for (int i = 0; i < NT; ++i) {
-      o[2 * i] += mine;
-      o[2 * i + 1] += mine;
-    }
-    const int64_t seg0 = ci.x - (was.r + 1), seg1 = seg0 + was.Lc;  // the segment's tiles among all
+    for (int i = 0; i < 2 * NT; ++i) o[i] += mine;
     float* orow = p.out + (int64_t)was.layer * p.out_stride + ((int64_t)was.s * H + was.h) * D;
     if (seg0 >= lo && seg1 <= hi) {
 #pragma unroll
@@ -508,51 +531,47 @@ __global__ void __launch_bounds__(32, D == 128 ? 10 : D == 96 ? 13 : 16)
           orow[col(i)] = o[2 * i] / l;
           orow[col(i) + 1] = o[2 * i + 1] / l;
         }
-    } else {
-      // a worker has at most two parts: of a segment that began before it, and of one that goes on behind it
-      float* part = p.parts + ((int64_t)wid * 2 + (seg0 < lo ? 0 : 1)) * (D + 4);
-#pragma unroll
-      for (int i = 0; i < NT; ++i)
-        if (t == col(i) / 32) {
-          __stcg(part + 4 + col(i), o[2 * i]);
-          __stcg(part + 5 + col(i), o[2 * i + 1]);
-        }
-      if (lane == 0) {
-        __stcg(part, m);
-        __stcg(part + 1, l);
-      }
-      const int first = worker_of(seg0, Rt, p.NW), last = worker_of(seg1 - 1, Rt, p.NW);
-      __threadfence();
-      __syncwarp();
-      int done = 0;
-      if (lane == 0) done = atomicAdd(p.counters + first, 1) == last - first;
-      if (__shfl_sync(kFull, done, 0)) {
-        __threadfence();
-        auto at = [&](int w) { return p.parts + ((int64_t)w * 2 + (w == first ? 1 : 0)) * (D + 4); };
-        float big = -INFINITY;
-        for (int w = first + lane; w <= last; w += 32) big = fmaxf(big, __ldcg(at(w)));
-#pragma unroll
-        for (int i = 16; i > 0; i >>= 1) big = fmaxf(big, __shfl_xor_sync(kFull, big, i));
-        float sum = 0.f, x[QL];
-#pragma unroll
-        for (int j = 0; j < QL; ++j) x[j] = 0.f;
-        for (int w = first; w <= last; ++w) {
-          const float* a = at(w);
-          const float mw = __ldcg(a);
-          const float f = mw == -INFINITY ? 0.f : exp2f(mw - big);
-          sum = fmaf(f, __ldcg(a + 1), sum);
-#pragma unroll
-          for (int j = 0; j < QL; ++j)
-            if (lane + 32 * j < D) x[j] = fmaf(f, __ldcg(a + 4 + lane + 32 * j), x[j]);
-        }
-#pragma unroll
-        for (int j = 0; j < QL; ++j)
-          if (lane + 32 * j < D) orow[lane + 32 * j] = x[j] / sum;
-        if (lane == 0) p.counters[first] = 0;
-      }
+      continue;
     }
-    fresh = true;
-    if (ci.x < hi && ci.s != was.s) ds = p.ds[ci.s];
+    // a worker has at most two parts: of a segment that began before it, and of one that goes on behind it
+    float* part = p.parts + ((int64_t)wid * 2 + (seg0 < lo ? 0 : 1)) * (D + 4);
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+      if (t == col(i) / 32) {
+        __stcg(part + 4 + col(i), o[2 * i]);
+        __stcg(part + 5 + col(i), o[2 * i + 1]);
+      }
+    if (lane == 0) {
+      __stcg(part, m);
+      __stcg(part + 1, l);
+    }
+    const int first = worker_of(seg0, Rt, p.NW), last = worker_of(seg1 - 1, Rt, p.NW);
+    __threadfence();
+    __syncwarp();
+    int done = 0;
+    if (lane == 0) done = atomicAdd(p.counters + first, 1) == last - first;
+    if (!__shfl_sync(kFull, done, 0)) continue;
+    __threadfence();
+    auto from = [&](int w) { return p.parts + ((int64_t)w * 2 + (w == first ? 1 : 0)) * (D + 4); };
+    float big = -INFINITY;
+    for (int w = first + lane; w <= last; w += 32) big = fmaxf(big, __ldcg(from(w)));
+    big = warp_max(big);
+    float sum = 0.f, y[QL];
+#pragma unroll
+    for (int j = 0; j < QL; ++j) y[j] = 0.f;
+    for (int w = first; w <= last; ++w) {
+      const float* a = from(w);
+      const float mw = __ldcg(a);
+      const float f = mw == -INFINITY ? 0.f : exp2_fast(mw - big);
+      sum = fmaf(f, __ldcg(a + 1), sum);
+#pragma unroll
+      for (int j = 0; j < QL; ++j)
+        if (lane + 32 * j < D) y[j] = fmaf(f, __ldcg(a + 4 + lane + 32 * j), y[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < QL; ++j)
+      if (lane + 32 * j < D) orow[lane + 32 * j] = y[j] / sum;
+    if (lane == 0) p.counters[first] = 0;
   }
 }
 

@@ -63,7 +63,7 @@ def stored(cache, s, n, which="k"):
     at = torch.tensor([[[m * H * cache.C + H * int(cache.offsets[s]) + h * cap + i for i in range(n)] for h in range(H)] for m in range(M)],
                       dtype=torch.long).view(M, H, n)
     c, p = code[at], pair[at]
-    return torch.stack([c & 15, c >> 4], -1).flatten(-2), p[..., 0].double(), p[..., 1].double()
+    return torch.stack([c & 15, c >> 4], -1).flatten(-2), p[..., 1].double(), p[..., 0].double()
 
 
 def fill(M, H, d, lens, dtype="f16", rot=0, spare=0, kinds=None, policy=kvc.POLICY_PAPER, seed=0, bits=4, pos=None):
