@@ -35,7 +35,7 @@ __device__ __forceinline__ int64_t stream_row0(const Geometry& g, const CopySide
 
 // Rows a block takes: 16 KB of 16-bit rows of 64 columns.
 template <int SB, int DB>
-constexpr int kCopyRows = SB == 4 && DB == 4 ? 256 : 128;
+constexpr int kCopyRows = DB == 4 ? 256 : 128;
 
 template <typename T, int D, int SB, int DB>
 __device__ __forceinline__ void copy_block(const CopyDev& p, const CopyPlan& plan) {
@@ -92,68 +92,73 @@ __device__ __forceinline__ void copy_block(const CopyDev& p, const CopyPlan& pla
       for (int u = 0; u < UP; ++u)
         if (tid + u * kCopyThreads < n * R::G) dp[tid + u * kCopyThreads] = y[u];
     }
+  } else if constexpr (SB == 16) {
+    // a lane has a group: the range, the step and its reciprocal once, and four words of codes side by side
+    constexpr int U = CR * R::G / kCopyThreads;
+    static_assert(CR * R::G % kCopyThreads == 0);
+    const uint16_t* src = (kv ? p.src.v : p.src.k) + row * D;
+    const int64_t row_first = target_row(0);
+#pragma unroll 1
+    for (int u = 0; u < U; ++u) {
+      const int i = tid + u * kCopyThreads, r = i / R::G, gi = i % R::G;
+      if (r >= n) break;
+      const uint4* from = reinterpret_cast<const uint4*>(src + r * D + 32 * gi);
+      const bool whole = D % 32 == 0 || gi + 1 < R::G;  // else a group of 16 columns
+      uint32_t x[16];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint4 v = e < 2 || whole ? __ldg(from + e) : make_uint4(0, 0, 0, 0);
+        x[4 * e] = v.x, x[4 * e + 1] = v.y, x[4 * e + 2] = v.z, x[4 * e + 3] = v.w;
+      }
+      if (!whole) {
+#pragma unroll
+        for (int e = 8; e < 16; ++e) x[e] = x[e - 8];
+      }
+      float lo, inv;
+      const uint32_t pair = group_pair<T>(range_of<T>(x, 16), &lo, &inv);
+      uint32_t y[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = code_word<T>(x + 4 * e, lo, inv);
+      for (int j = 0; j < cs.n; ++j) {
+        const int64_t to = (j == 0 ? row_first : target_row(j)) + r;
+        uint32_t* codes = reinterpret_cast<uint32_t*>(kv ? p.dst.pb.vc : p.dst.pb.kc) + to * R::W + 4 * gi;
+        if constexpr (D % 32 == 0) {
+          *reinterpret_cast<uint4*>(codes) = make_uint4(y[0], y[1], y[2], y[3]);
+        } else {  // rows of 40 bytes
+          *reinterpret_cast<uint2*>(codes) = make_uint2(y[0], y[1]);
+          if (whole) *reinterpret_cast<uint2*>(codes + 2) = make_uint2(y[2], y[3]);
+        }
+        (kv ? p.dst.pb.vp : p.dst.pb.kp)[to * R::G + gi] = pair;
+      }
+    }
   } else {
-    // between the two: a lane has eight columns, the four lanes of a group side by side
-    constexpr int U = CR * R::CP / kCopyThreads;
-    static_assert(CR * R::CP % kCopyThreads == 0);
-    if constexpr (SB == 16) {
-      const uint16_t* src = (kv ? p.src.v : p.src.k) + row * D;
-      uint4 x[U];
+    // a lane has eight columns
+    constexpr int U = CR * R::W / kCopyThreads;
+    static_assert(CR * R::W % kCopyThreads == 0);
+    const uint32_t* src = reinterpret_cast<const uint32_t*>(kv ? p.src.pb.vc : p.src.pb.kc) + row * R::W;
+    const uint32_t* sp = (kv ? p.src.pb.vp : p.src.pb.kp) + row * R::G;
+    uint32_t x[U], y[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int i = tid + u * kCopyThreads, r = i / R::CP, c = i % R::CP;
-        x[u] = make_uint4(0, 0, 0, 0);
-        if (r < n && c < R::W) x[u] = __ldcs(reinterpret_cast<const uint4*>(src + r * D) + c);
+    for (int u = 0; u < U; ++u) {
+      const int i = tid + u * kCopyThreads;
+      x[u] = y[u] = 0;
+      if (i < n * R::W) {
+        x[u] = __ldcs(src + i);
+        y[u] = __ldg(sp + i / R::W * R::G + i % R::W / 4);
       }
+    }
+    uint4 o[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int i = tid + u * kCopyThreads, r = i / R::CP, c = i % R::CP;
-        const uint32_t a[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
-        float f[8];
+    for (int u = 0; u < U; ++u) {
+      const float2 pv = pair_values(y[u], T{});
+      const float2 a = code_values(x[u], 0, pv), b = code_values(x[u], 1, pv), c = code_values(x[u], 2, pv), d = code_values(x[u], 3, pv);
+      o[u] = make_uint4(T::r2(a.x, b.x), T::r2(c.x, d.x), T::r2(a.y, b.y), T::r2(c.y, d.y));
+    }
+    for (int j = 0; j < cs.n; ++j) {
+      uint4* dst = reinterpret_cast<uint4*>((kv ? p.dst.v : p.dst.k) + target_row(j) * D);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float2 v = T::f2(a[e]);
-          f[2 * e] = v.x;
-          f[2 * e + 1] = v.y;
-        }
-        const bool active = r < n && c < R::W;
-        uint32_t pair;
-        const uint32_t word = pack8<T>(f, active, &pair);
-        if (!active) continue;
-        for (int j = 0; j < cs.n; ++j) {
-          const int64_t to = target_row(j) + r;
-          reinterpret_cast<uint32_t*>(kv ? p.dst.pb.vc : p.dst.pb.kc)[to * R::W + c] = word;
-          if (c % 4 == 0) (kv ? p.dst.pb.vp : p.dst.pb.kp)[to * R::G + c / 4] = pair;
-        }
-      }
-    } else {
-      const uint32_t* src = reinterpret_cast<const uint32_t*>(kv ? p.src.pb.vc : p.src.pb.kc) + row * R::W;
-      const uint32_t* sp = (kv ? p.src.pb.vp : p.src.pb.kp) + row * R::G;
-      uint32_t x[U], y[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int i = tid + u * kCopyThreads, r = i / R::CP, c = i % R::CP;
-        x[u] = y[u] = 0;
-        if (r < n && c < R::W) {
-          x[u] = __ldcs(src + r * R::W + c);
-          y[u] = __ldcs(sp + r * R::G + c / 4);
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int i = tid + u * kCopyThreads, r = i / R::CP, c = i % R::CP;
-        if (r >= n || c >= R::W) continue;
-        const float2 pv = pair_values(y[u], T{});
-        const float lo = pv.x, step = pv.y;
-        uint32_t o[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          o[e] = T::r2(fmaf(step, (float)(x[u] >> (8 * e) & 15u), lo), fmaf(step, (float)(x[u] >> (8 * e + 4) & 15u), lo));
-        for (int j = 0; j < cs.n; ++j) {
-          uint16_t* dst = (kv ? p.dst.v : p.dst.k) + (target_row(j) + r) * D;
-          __stcs(reinterpret_cast<uint4*>(dst) + c, make_uint4(o[0], o[1], o[2], o[3]));
-        }
-      }
+      for (int u = 0; u < U; ++u)
+        if (tid + u * kCopyThreads < n * R::W) __stcs(dst + tid + u * kCopyThreads, o[u]);
     }
   }
   if (sidx == 0) {

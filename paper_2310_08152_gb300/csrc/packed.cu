@@ -53,17 +53,11 @@ __device__ __forceinline__ void pack_units(const Geometry& g, const Static& st, 
       const int h = is_v ? hk - H : hk;
       const bool active = hk < 2 * H && t < nt && c < R::W;
       const TokPlan tp = plan[t0 + min(t, nt - 1)];
-      float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      uint32_t x[4] = {0, 0, 0, 0};
       if (active) {
         const uint16_t* src = (is_v ? v_in : k_in) + (((int64_t)l * n_in + tp.in_tok) * H + h) * D;
         const uint4 a = __ldg(reinterpret_cast<const uint4*>(src + 8 * c));
-        const uint32_t av[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float2 f = T::f2(av[e]);
-          x[2 * e] = f.x;
-          x[2 * e + 1] = f.y;
-        }
+        x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w;
         if (!is_v && 8 * c < g.rot) {
           const bool first = 8 * c < half;
           const int p0 = first ? 8 * c : 8 * c - half;
@@ -71,12 +65,10 @@ __device__ __forceinline__ void pack_units(const Geometry& g, const Static& st, 
           const uint32_t bv[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float2 f = T::f2(bv[e]);
+            const float2 f = T::f2(x[e]), o = T::f2(bv[e]);
             const float2 r0 = rope_cs[t][p0 + 2 * e], r1 = rope_cs[t][p0 + 2 * e + 1];
-            const float y0 = first ? x[2 * e] * r0.x - f.x * r0.y : x[2 * e] * r0.x + f.x * r0.y;
-            const float y1 = first ? x[2 * e + 1] * r1.x - f.y * r1.y : x[2 * e + 1] * r1.x + f.y * r1.y;
-            x[2 * e] = T::f1(T::r(y0));
-            x[2 * e + 1] = T::f1(T::r(y1));
+            x[e] = T::r2(first ? f.x * r0.x - o.x * r0.y : f.x * r0.x + o.x * r0.y,
+                         first ? f.y * r1.x - o.y * r1.y : f.y * r1.x + o.y * r1.y);
           }
         }
       }
