@@ -34,26 +34,31 @@ namespace {
 constexpr unsigned kFull = 0xFFFFFFFFu;
 constexpr int kTile = kPackedTile;
 
-template <int D, int S_>
+template <int D>
 struct Shape {
   using R = PackedRow<D>;
-  static constexpr int S = S_;
+  // Workers of an SM.  Each of its four schedulers has the same number, or those with more end last: 15, 13 and 10 at 80, 96
+  // and 128 columns, which two stages of both leave room for, were 20 to 25 % slower.
+  static constexpr int WARPS = D == 128 ? 12 : 16;
+  // Stages of keys and of values (of 128 columns three of both leave room for 8)
+  static constexpr int SK = 2, SV = D == 64 ? 2 : 1;
   static constexpr int KC = kTile * R::RB, KP = kTile * R::PB;
-  static constexpr int STAGE = 2 * (KC + KP);  // K codes, K pairs, V codes, V pairs
+  static constexpr int STAGE = KC + KP;  // codes, pairs
   // weights times steps: [column of the operand][row of both halves of a tile] as pairs of f16, the columns 16 bytes more
   // than 128 apart, so that eight lanes' 16-byte loads meet no bank twice; the query between pieces
   static constexpr int PW = 36;
   static constexpr int PS = 4 * 8 * PW;
-  static constexpr int SMEM = S * STAGE + PS + 8 * S;
+  static constexpr int SMEM = (SK + SV) * STAGE + PS + 8 * (SK + SV);
   static_assert(4 * D <= PS && PS % 16 == 0);
+  static_assert(WARPS * (SMEM + 1024) <= 228 * 1024);
 };
 
 struct PackedDev {
   const DState* ds;
   const int64_t* P;  // prefix sums of the sequences' tiles
-  int64_t R;         // tiles of a layer
-  int n_layers, layer;
-  int NW;
+  int R;             // tiles of a layer
+  int layer;         // the first one
+  int NW, share, extra;  // workers; tiles of each, and how many have one more, the first ones
   const uint16_t* q;
   float* out;
   int64_t q_stride, out_stride;
@@ -83,15 +88,18 @@ struct Segment {
   }
 };
 
-// The worker whose share [w Rt / NW, (w + 1) Rt / NW) holds tile x.
-__device__ __forceinline__ int worker_of(int64_t x, int64_t Rt, int NW) { return (int)(((x + 1) * NW - 1) / Rt); }
+// The worker that has tile x.
+__device__ __forceinline__ int worker_of(int x, const PackedDev& p) {
+  const int most = p.extra * (p.share + 1);
+  return x < most ? x / (p.share + 1) : p.extra + (x - most) / p.share;
+}
 
 // The sequence that holds tile o of a layer: the last s with H P[s] <= o, a search of the whole warp.
-__device__ __forceinline__ int seq_of(const int64_t* P, int b, int H, int64_t o, int lane) {
+__device__ __forceinline__ int seq_of(const int64_t* P, int b, int H, int o, int lane) {
   int a = 0, z = b;
   while (z - a > 1) {
     const int step = (z - a + 31) / 32, k = a + lane * step;
-    const unsigned bal = __ballot_sync(kFull, k < z && (int64_t)H * P[k] <= o);
+    const unsigned bal = __ballot_sync(kFull, k < z && H * (int)P[k] <= o);
     a += (31 - __clz(bal)) * step;
     z = min(z, a + step);
   }
@@ -178,80 +186,101 @@ __device__ __forceinline__ float row_exponent(const uint32_t (&pair)[G], BF16T) 
   return __uint_as_float(0x4B000000u | (uint32_t)big >> 23) - 8388735.f;
 }
 
-template <typename T, int D, int S>
-__global__ void __launch_bounds__(32, D == 128 ? 10 : D == 96 ? 13 : 16)
+template <typename T, int D>
+__global__ void __launch_bounds__(32, Shape<D>::WARPS)
     packed_decode_kernel(Geometry g, Static st, PackedBuffers pb, PackedDev p) {
-  using C = Shape<D, S>;
+  using C = Shape<D>;
   using R = PackedRow<D>;
   constexpr int G = R::G;
   constexpr int KW = D == 128 ? 4 : 2;              // code words of a row a lane has of the keys
   constexpr int NT = D / 16;                        // tiles of 16 columns of the values
   constexpr int QF = 2 * (D / 16);                  // registers of the query
+  constexpr bool kJoint = C::SK == C::SV;           // keys and values come together
   extern __shared__ __align__(128) unsigned char smem[];
   pdl_launch_dependents();
   const int lane = threadIdx.x, gr = lane >> 2, t = lane & 3, tg = t < G ? t : G - 1;
   const int wid = blockIdx.x, H = g.H;
-  const int64_t Rt = (int64_t)p.n_layers * p.R;
-  const int64_t lo = (int64_t)wid * Rt / p.NW, hi = (int64_t)(wid + 1) * Rt / p.NW;
+  const int lo = wid * p.share + min(wid, p.extra), hi = lo + p.share + (wid < p.extra ? 1 : 0);
 
-  unsigned char* ps = smem + S * C::STAGE;
-  float* qs = reinterpret_cast<float*>(ps);
+  unsigned char* ks = smem;
+  unsigned char* vs = smem + C::SK * C::STAGE;
+  unsigned char* ps = vs + C::SV * C::STAGE;
   uint32_t* pw = reinterpret_cast<uint32_t*>(ps);
-  uint64_t* full = reinterpret_cast<uint64_t*>(ps + C::PS);
+  uint64_t* kfull = reinterpret_cast<uint64_t*>(ps + C::PS);
+  uint64_t* vfull = kfull + C::SK;
   if (lane == 0) {
 #pragma unroll
-    for (int i = 0; i < S; ++i) mbar_init(&full[i], 1);
+    for (int i = 0; i < C::SK + C::SV; ++i) mbar_init(&kfull[i], 1);
     fence_mbar_init();
   }
   fence_proxy_async_smem();
   __syncwarp();
   if (!p.kv_before_wait) pdl_wait();
 
-  Segment cs;      // of the consumed tiles
-  int r;           // the next one in it
-  int64_t x = lo;  // and among all
+  Segment cs;  // of the consumed tiles
+  int r;       // the next one in it
+  int x = lo;  // and among all
   {
-    cs.layer = (int)(lo / p.R);
-    const int64_t o = lo - (int64_t)cs.layer * p.R;
+    cs.layer = lo / p.R;
+    const int o = lo - cs.layer * p.R;
     cs.s = seq_of(p.P, g.b, H, o, lane);
-    const int64_t P0 = p.P[cs.s];
-    cs.tiles = (int)(p.P[cs.s + 1] - P0);
-    cs.h = (int)((o - (int64_t)H * P0) / cs.tiles);
-    r = (int)(o - (int64_t)H * P0 - (int64_t)cs.h * cs.tiles);
+    const int P0 = (int)p.P[cs.s];
+    cs.tiles = (int)p.P[cs.s + 1] - P0;
+    cs.h = (o - H * P0) / cs.tiles;
+    r = o - H * P0 - cs.h * cs.tiles;
   }
-  // lane 0 issues copies: the segment, its rows from the next tile on, that tile's place in the planes, and how many are left
-  Segment is = cs;
-  int i_rows = 0;
-  int64_t i_code = 0, i_pair = 0, i_left = hi - lo;
-  auto i_segment = [&](int first) {
-    const DState d = p.ds[is.s];
-    const int r0 = d.begin / kPackedRows * kPackedRows + first * kTile;
-    const int64_t row = (int64_t)(p.layer + is.layer) * H * g.C + st.seq_row0[is.s] + (int64_t)is.h * st.cap[is.s] + r0;
-    i_rows = d.len - r0;
-    i_code = row * R::RB;
-    i_pair = row * R::PB;
+  // What lane 0 issues copies from: the segment, its rows from the next tile on, the first of them in the planes, and how many
+  // tiles are left.
+  struct Feed {
+    Segment seg;
+    int rows, left;
+    int64_t row;
   };
-  auto issue = [&](int stage) {
-    const uint32_t n = (uint32_t)min(kTile, (i_rows + kPackedRows - 1) & -kPackedRows);
-    unsigned char* to = smem + stage * C::STAGE;
-    mbar_arrive_expect_tx(&full[stage], 2 * n * (R::RB + R::PB));
-    bulk_g2s(to, pb.kc + i_code, n * R::RB, &full[stage]);
-    bulk_g2s(to + C::KC, reinterpret_cast<const unsigned char*>(pb.kp) + i_pair, n * R::PB, &full[stage]);
-    bulk_g2s(to + C::KC + C::KP, pb.vc + i_code, n * R::RB, &full[stage]);
-    bulk_g2s(to + 2 * C::KC + C::KP, reinterpret_cast<const unsigned char*>(pb.vp) + i_pair, n * R::PB, &full[stage]);
-    i_rows -= kTile;
-    i_code += C::KC;
-    i_pair += C::KP;
-    if (--i_left > 0 && i_rows <= 0) {
-      is.advance(p.P, H, g.b);
-      i_segment(0);
+  auto enter = [&](Feed& f, int first) {
+    const DState d = p.ds[f.seg.s];
+    const int r0 = d.begin / kPackedRows * kPackedRows + first * kTile;
+    f.row = (int64_t)(p.layer + f.seg.layer) * H * g.C + st.seq_row0[f.seg.s] + (int64_t)f.seg.h * st.cap[f.seg.s] + r0;
+    f.rows = d.len - r0;
+  };
+  auto step = [&](Feed& f) {
+    f.rows -= kTile;
+    f.row += kTile;
+    if (--f.left > 0 && f.rows <= 0) {
+      f.seg.advance(p.P, H, g.b);
+      enter(f, 0);
     }
+  };
+  auto copy = [&](const Feed& f, unsigned char* to, const unsigned char* codes, const uint32_t* pairs, uint64_t* bar, uint32_t n) {
+    bulk_g2s(to, codes + f.row * R::RB, n * R::RB, bar);
+    bulk_g2s(to + C::KC, pairs + f.row * R::G, n * R::PB, bar);
+  };
+  auto rows_of = [&](const Feed& f) { return (uint32_t)min(kTile, (f.rows + kPackedRows - 1) & -kPackedRows); };
+  Feed kf{cs, 0, hi - lo, 0}, vf{cs, 0, hi - lo, 0};
+  auto issue_k = [&](int stage) {
+    const uint32_t n = rows_of(kf);
+    mbar_arrive_expect_tx(&kfull[stage], n * (R::RB + R::PB) * (kJoint ? 2 : 1));
+    copy(kf, ks + stage * C::STAGE, pb.kc, pb.kp, &kfull[stage], n);
+    if (kJoint) copy(kf, vs + stage * C::STAGE, pb.vc, pb.vp, &kfull[stage], n);
+    step(kf);
+  };
+  auto issue_v = [&](int stage) {
+    const uint32_t n = rows_of(vf);
+    mbar_arrive_expect_tx(&vfull[stage], n * (R::RB + R::PB));
+    copy(vf, vs + stage * C::STAGE, pb.vc, pb.vp, &vfull[stage], n);
+    step(vf);
   };
   // a decode before this one writes neither rows nor state: they may come before it is complete, while the query, the outputs
   // and the parts may be shared with it
   if (lane == 0) {
-    i_segment(r);
-    for (int i = 0; i < S && i_left > 0; ++i) issue(i);
+    enter(kf, r);
+    if (!kJoint) {
+      vf.row = kf.row;
+      vf.rows = kf.rows;
+    }
+    issue_k(0);
+    if (!kJoint)
+      for (int i = 0; i < C::SV && vf.left > 0; ++i) issue_v(i);
+    for (int i = 1; i < C::SK && kf.left > 0; ++i) issue_k(i);
   }
   if (p.kv_before_wait) pdl_wait();
 
@@ -273,13 +302,30 @@ __global__ void __launch_bounds__(32, D == 128 ? 10 : D == 96 ? 13 : 16)
   };
   fetch_q(cs);
   DState ds = p.ds[cs.s];
-  int stage = 0;
-  uint32_t phase = 0;
+  int kst = 0, vst = 0;
+  uint32_t kph = 0, vph = 0;
+  auto next = [](int& stage, uint32_t& phase, int n) {
+    if (++stage == n) {
+      stage = 0;
+      phase ^= 1;
+    }
+  };
+  // After a wait that ran out: the copies that are still in flight end before their memory does.  `waits`: how many of the
+  // keys' tiles, and of the values', were waited for.
+  auto give_up = [&](int k_taken, int v_taken) {
+    if (lane == 0) {
+      atomicOr(p.status, STATUS_TIMEOUT);
+      for (int i = k_taken; i < hi - lo - kf.left; ++i, next(kst, kph, C::SK)) mbar_wait_bounded(&kfull[kst], kph, p.limit_ns);
+      if (!kJoint)
+        for (int i = v_taken; i < hi - lo - vf.left; ++i, next(vst, vph, C::SV)) mbar_wait_bounded(&vfull[vst], vph, p.limit_ns);
+    }
+    __syncwarp();
+  };
 
   while (x < hi) {
     // ---- a piece: tiles [r, r1) of a segment
-    const int r1 = (int)min((int64_t)cs.tiles, r + (hi - x));
-    const int64_t seg0 = x - r, seg1 = seg0 + cs.tiles;  // the segment's tiles among all
+    const int r1 = min(cs.tiles, r + hi - x);
+    const int seg0 = x - r, seg1 = seg0 + cs.tiles;  // the segment's tiles among all
     uint32_t qf[QF];  // the query as the keys' other operand
     float qsum;       // its sum over group t's columns, times qscale
     float kscale;     // of a product of codes and the query's parts
@@ -313,27 +359,29 @@ __global__ void __launch_bounds__(32, D == 128 ? 10 : D == 96 ? 13 : 16)
         if (t == j) qsum = sum[j] * p.qscale;
       __syncwarp();  // the weights of the piece before are read
 #pragma unroll
-      for (int j = 0; j < QL; ++j)
-        if (lane + 32 * j < D) qs[lane + 32 * j] = qa[j] * up;
+      for (int j = 0; j < QL; ++j) {  // both parts of a column side by side
+        const float y = qa[j] * up, h = __half2float(__float2half_rn(y));
+        if (lane + 32 * j < D) pw[lane + 32 * j] = pack_halves(h, y - h);
+      }
       __syncwarp();
       // column gr of the operand: group gr / 2, part gr % 2
-      auto part = [&](int k) {
-        const float y = (k >> 5) == (gr >> 1) ? qs[k] : 0.f;
-        const float h = __half2float(__float2half_rn(y));
-        return gr & 1 ? y - h : h;
-      };
+      const uint32_t which = gr & 1 ? 0x7632u : 0x5410u;
       auto word = [&](int k, uint32_t* f) {
-        f[0] = pack_halves(part(k), part(k + 4));
-        f[1] = pack_halves(part(k + 1), part(k + 5));
-        f[2] = pack_halves(part(k + 2), part(k + 6));
-        f[3] = pack_halves(part(k + 3), part(k + 7));
+        const uint4 a = *reinterpret_cast<const uint4*>(pw + k), b = *reinterpret_cast<const uint4*>(pw + k + 4);
+        const uint32_t mask = (k >> 5) == (gr >> 1) ? 0xFFFFFFFFu : 0u;
+        f[0] = __byte_perm(a.x, b.x, which) & mask;
+        f[1] = __byte_perm(a.y, b.y, which) & mask;
+        f[2] = __byte_perm(a.z, b.z, which) & mask;
+        f[3] = __byte_perm(a.w, b.w, which) & mask;
       };
 #pragma unroll
       for (int i = 0; i < KW; ++i) word(8 * (KW * t + i), qf + 4 * i);
       if constexpr (D == 96) word(64 + 8 * t, qf + 8);
       if constexpr (D == 80) {
-        qf[8] = pack_halves(part(64 + 4 * t), part(64 + 4 * t + 2));
-        qf[9] = pack_halves(part(64 + 4 * t + 1), part(64 + 4 * t + 3));
+        const uint4 a = *reinterpret_cast<const uint4*>(pw + 64 + 4 * t);
+        const uint32_t mask = gr >> 1 == 2 ? 0xFFFFFFFFu : 0u;
+        qf[8] = __byte_perm(a.x, a.z, which) & mask;
+        qf[9] = __byte_perm(a.y, a.w, which) & mask;
       }
       __syncwarp();
     }
@@ -347,25 +395,14 @@ __global__ void __launch_bounds__(32, D == 128 ? 10 : D == 96 ? 13 : 16)
     x += r1 - r;
     for (; r < r1; ++r, r0 += kTile) {
       // ---- a tile
-      if (!__all_sync(kFull, mbar_wait_bounded(&full[stage], phase, p.limit_ns))) {
-        if (lane == 0) {
-          atomicOr(p.status, STATUS_TIMEOUT);
-          // the copies that are still in flight end before their memory does
-          const int64_t taken = x - lo - (r1 - r);
-          for (int64_t i = taken; i < hi - lo - i_left; ++i) {
-            mbar_wait_bounded(&full[stage], phase, p.limit_ns);
-            if (++stage == S) {
-              stage = 0;
-              phase ^= 1;
-            }
-          }
-        }
-        __syncwarp();
+      if (!__all_sync(kFull, mbar_wait_bounded(&kfull[kst], kph, p.limit_ns))) {
+        const int taken = x - lo - (r1 - r);
+        give_up(taken, taken);
         return;  // the segment is not joined
       }
-      const unsigned char* kc = smem + stage * C::STAGE;
+      const unsigned char* kc = ks + kst * C::STAGE;
       const uint32_t* kp = reinterpret_cast<const uint32_t*>(kc + C::KC);
-      const unsigned char* vc = kc + C::KC + C::KP;
+      const unsigned char* vc = vs + (kJoint ? kst : vst) * C::STAGE;
       const uint32_t* vp = reinterpret_cast<const uint32_t*>(vc + C::KC);
 
       float z[2];  // logits of rows gr + 8 t of the tile's halves
@@ -408,6 +445,12 @@ __global__ void __launch_bounds__(32, D == 128 ? 10 : D == 96 ? 13 : 16)
         z[b] = (two ? s1 : s0) + __shfl_xor_sync(kFull, two ? s0 : s1, 2);
       }
 
+      if (!kJoint && !__all_sync(kFull, mbar_wait_bounded(&vfull[vst], vph, p.limit_ns))) {
+        const int taken = x - lo - (r1 - r);
+        next(kst, kph, C::SK);
+        give_up(taken + 1, taken);
+        return;
+      }
       uint32_t vpair[2][G];
 #pragma unroll
       for (int b = 0; b < 2; ++b)
@@ -448,6 +491,10 @@ __global__ void __launch_bounds__(32, D == 128 ? 10 : D == 96 ? 13 : 16)
         pw[(2 * i + 1) * C::PW + at] = pack_halves(x0 - back.x, x1 - back.y);
       }
       __syncwarp();
+      if (!kJoint) {  // the keys are read
+        if (lane == 0 && kf.left > 0) issue_k(kst);
+        next(kst, kph, C::SK);
+      }
 
       float acc[NT][4];
 #pragma unroll
@@ -491,10 +538,12 @@ __global__ void __launch_bounds__(32, D == 128 ? 10 : D == 96 ? 13 : 16)
         o[2 * i + 1] += acc[i][2] + acc[i][3];
       }
       __syncwarp();  // the stage and the weights are read
-      if (lane == 0 && i_left > 0) issue(stage);
-      if (++stage == S) {
-        stage = 0;
-        phase ^= 1;
+      if (kJoint) {
+        if (lane == 0 && kf.left > 0) issue_k(kst);
+        next(kst, kph, C::SK);
+      } else {
+        if (lane == 0 && vf.left > 0) issue_v(vst);
+        next(vst, vph, C::SV);
       }
     }
 
@@ -525,11 +574,12 @@ __global__ void __launch_bounds__(32, D == 128 ? 10 : D == 96 ? 13 : 16)
     for (int i = 0; i < 2 * NT; ++i) o[i] += mine;
     float* orow = p.out + (int64_t)was.layer * p.out_stride + ((int64_t)was.s * H + was.h) * D;
     if (seg0 >= lo && seg1 <= hi) {
+      const float inv = 1.f / l;
 #pragma unroll
       for (int i = 0; i < NT; ++i)
         if (t == col(i) / 32) {
-          orow[col(i)] = o[2 * i] / l;
-          orow[col(i) + 1] = o[2 * i + 1] / l;
+          orow[col(i)] = o[2 * i] * inv;
+          orow[col(i) + 1] = o[2 * i + 1] * inv;
         }
       continue;
     }
@@ -545,7 +595,7 @@ __global__ void __launch_bounds__(32, D == 128 ? 10 : D == 96 ? 13 : 16)
       __stcg(part, m);
       __stcg(part + 1, l);
     }
-    const int first = worker_of(seg0, Rt, p.NW), last = worker_of(seg1 - 1, Rt, p.NW);
+    const int first = worker_of(seg0, p), last = worker_of(seg1 - 1, p);
     __threadfence();
     __syncwarp();
     int done = 0;
@@ -568,31 +618,32 @@ __global__ void __launch_bounds__(32, D == 128 ? 10 : D == 96 ? 13 : 16)
       for (int j = 0; j < QL; ++j)
         if (lane + 32 * j < D) y[j] = fmaf(f, __ldcg(a + 4 + lane + 32 * j), y[j]);
     }
+    const float inv = 1.f / sum;
 #pragma unroll
     for (int j = 0; j < QL; ++j)
-      if (lane + 32 * j < D) orow[lane + 32 * j] = y[j] / sum;
+      if (lane + 32 * j < D) orow[lane + 32 * j] = y[j] * inv;
     if (lane == 0) p.counters[first] = 0;
   }
 }
 
-template <int D>
-constexpr int kStages = 2;
-
-template <typename T, int D, int S>
-cudaError_t launch_t(const Geometry& g, const Static& st, const PackedBuffers& pb, PackedDev p, int device, int num_sms,
-                     cudaStream_t stream, int* grid, DecodePlan* plan) {
-  using C = Shape<D, S>;
-  auto* kernel = packed_decode_kernel<T, D, S>;
-  static std::atomic<int> occupancy[64];  // CTAs per SM, by device
+template <typename T, int D>
+cudaError_t launch_t(const Geometry& g, const Static& st, const PackedBuffers& pb, PackedDev p, int64_t tiles, int device,
+                     int num_sms, cudaStream_t stream, int* grid, DecodePlan* plan) {
+  using C = Shape<D>;
+  auto* kernel = packed_decode_kernel<T, D>;
+  static std::atomic<int> occupancy[64];  // workers of an SM, by device
   int occ = device >= 0 && device < 64 ? occupancy[device].load(std::memory_order_relaxed) : 0;
   if (occ == 0) {
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
     if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&occ, kernel, 32, C::SMEM);
     if (e != cudaSuccess) return e;
     if (occ < 1) return cudaErrorInvalidConfiguration;
+    occ = std::min(occ, C::WARPS);
     if (device >= 0 && device < 64) occupancy[device].store(occ, std::memory_order_relaxed);
   }
-  p.NW = (int)std::min<int64_t>({(int64_t)occ * num_sms, kMaxPackedWorkers, p.R * p.n_layers});
+  p.NW = (int)std::min<int64_t>({(int64_t)occ * num_sms, kMaxPackedWorkers, tiles});
+  p.share = (int)(tiles / p.NW);
+  p.extra = (int)(tiles % p.NW);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)p.NW);
   cfg.blockDim = dim3(32);
@@ -604,7 +655,7 @@ cudaError_t launch_t(const Geometry& g, const Static& st, const PackedBuffers& p
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   *grid = p.NW;
-  *plan = {5, p.NW, kTile, S};
+  *plan = {5, p.NW, kTile, C::SK};
   return cudaLaunchKernelEx(&cfg, kernel, g, st, pb, p);
 }
 
@@ -615,10 +666,11 @@ cudaError_t launch_packed_decode(const Geometry& g, const Static& st, const Pack
   PackedDev p;
   p.ds = a.dstate;
   p.P = a.P;
-  p.R = a.R;
-  p.n_layers = a.n_layers;
+  const int64_t tiles = a.R * a.n_layers;
+  if (tiles > INT32_MAX) return cudaErrorInvalidValue;  // 10 TB of rows
+  p.R = (int)a.R;
   p.layer = a.layer;
-  p.NW = 0;
+  p.NW = p.share = p.extra = 0;
   p.q = static_cast<const uint16_t*>(a.q);
   p.out = a.out;
   p.q_stride = a.q_layer_stride;
@@ -631,8 +683,8 @@ cudaError_t launch_packed_decode(const Geometry& g, const Static& st, const Pack
   p.kv_before_wait = a.kv_before_wait;
   auto by_dtype = [&](auto dc) {
     constexpr int D = decltype(dc)::value;
-    return g.dtype == 1 ? launch_t<BF16T, D, kStages<D>>(g, st, pb, p, a.device, num_sms, stream, grid, plan)
-                        : launch_t<F16T, D, kStages<D>>(g, st, pb, p, a.device, num_sms, stream, grid, plan);
+    return g.dtype == 1 ? launch_t<BF16T, D>(g, st, pb, p, tiles, a.device, num_sms, stream, grid, plan)
+                        : launch_t<F16T, D>(g, st, pb, p, tiles, a.device, num_sms, stream, grid, plan);
   };
   switch (g.D) {
     case 64:

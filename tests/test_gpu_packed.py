@@ -287,7 +287,8 @@ def test_offsets_past_32_bits():
     cache.append(x, x, [5, 70], np.zeros(75, np.uint8))
     q = torch.randn(1, 2, H, d, device="cuda").half().expand(M, -1, -1, -1).contiguous()
     out = cache.decode_attention_layers(q, 0.1)
-    assert torch.equal(out[-1], out[0])
+    for m in range(M):  # not bit for bit: the workers' shares end elsewhere in each layer's segments
+        close4(out[m], out[0], f"layer {m}")
     small = kvc.KVCache(1, H, d, [8, 80], "f16", bits=4)
     small.append(x[:1].contiguous(), x[:1].contiguous(), [5, 70], np.zeros(75, np.uint8))
     close4(out[:1], small.decode_attention_layers(q[:1].contiguous(), 0.1), "small")
