@@ -70,9 +70,10 @@ struct PackedBuffers {
 };
 constexpr int kPackedRows = 4;
 inline int packed_groups(int D) { return (D + 31) / 32; }
-// The decode's work is counted in tiles of kPackedTile rows: P then holds prefix sums of tiles, from row
-// begin / kPackedRows * kPackedRows on.  Each worker (warp) has a counter and two parts of D + 4 floats.
-constexpr int kPackedTile = 64;
+// The decode's work is counted in tiles of kPackedTile rows, from row begin / kPackedRows * kPackedRows of a segment on, and
+// kPackedPiece more for each segment: P then holds the prefix sums of that.  Each worker (warp) has a counter and two parts of
+// D + 4 floats.
+constexpr int kPackedTile = 64, kPackedPiece = 1;
 constexpr int kMaxPackedWorkers = 4096;
 
 // Writes the n_plan stored tokens of a call whose inputs hold n_in tokens per layer (k_in, v_in
@@ -152,7 +153,7 @@ struct DecodePlan {
 cudaError_t launch_decode(const Geometry& g, const Static& st, const Buffers& buf, const DecodeArgs& a,
                           int num_sms, cudaStream_t stream, int* grid, DecodePlan* plan);
 
-// The decode of a cache of 4 bits, all the launch's layers together (a.P and a.R in tiles; a.counters:
+// The decode of a cache of 4 bits, all the launch's layers together (a.P and a.R as above; a.counters:
 // [kMaxPackedWorkers], zero between launches).
 cudaError_t launch_packed_decode(const Geometry& g, const Static& st, const PackedBuffers& pb, const DecodeArgs& a,
                                  int* status, int num_sms, cudaStream_t stream, int* grid, DecodePlan* plan);

@@ -484,8 +484,8 @@ struct kvc_cache {
         ds[s].wrap = (int32_t)std::min<int64_t>(v.wrap, INT32_MAX);
         ds[s].is_cl = v.is_cl;
         Lc = v.len - v.begin;
-        if (packed())  // tiles, from a row on that starts at 16 bytes
-          Lc = (v.len - v.begin / kvc::kPackedRows * kvc::kPackedRows + kvc::kPackedTile - 1) / kvc::kPackedTile;
+        if (packed() && Lc > 0)  // tiles, from a row on that starts at 16 bytes, and the segment's beginning
+          Lc = (v.len - v.begin / kvc::kPackedRows * kvc::kPackedRows + kvc::kPackedTile - 1) / kvc::kPackedTile + kvc::kPackedPiece;
       } else {
         if (decode_ok) decode_err = err;
         decode_ok = false;

@@ -16,7 +16,8 @@
 // one, but the matrix unit aligns its products by the exponents, as if their leading bits were set: 1.1e-5 of the norm off.)
 //
 // The work: the tiles of 64 rows of all (layer, sequence, head) segments in a row, an equal share for each warp that fits the
-// GPU.  A warp is a worker of its own, with a ring of stages in shared memory that 1-D bulk copies fill (codes and pairs of
+// GPU, where the beginning of a segment counts as one tile (its query, its end and its output: two thirds of one; uneven
+// sequences of 64 to 4,096 rows, whose workers on short ones were the last, 187 -> 164 us).  A warp is a worker of its own, with a ring of stages in shared memory that 1-D bulk copies fill (codes and pairs of
 // K and V, four copies a tile).  A segment that spans several workers is joined by the last of them to finish, from parts in
 // the workspace, in the workers' order.
 #include <cuda_runtime.h>
@@ -48,17 +49,18 @@ struct Shape {
   // than 128 apart, so that eight lanes' 16-byte loads meet no bank twice; the query between pieces
   static constexpr int PW = 36;
   static constexpr int PS = 4 * 8 * PW;
-  static constexpr int SMEM = (SK + SV) * STAGE + PS + 8 * (SK + SV);
+  static constexpr int RS = 8 * (D / 2);       // the rotation's cosines and sines at a sequence's position
+  static constexpr int SMEM = (SK + SV) * STAGE + PS + RS + 8 * (SK + SV);
   static_assert(4 * D <= PS && PS % 16 == 0);
   static_assert(WARPS * (SMEM + 1024) <= 228 * 1024);
 };
 
 struct PackedDev {
   const DState* ds;
-  const int64_t* P;  // prefix sums of the sequences' tiles
-  int R;             // tiles of a layer
+  const int64_t* P;  // prefix sums of the sequences' places: kPackedPiece, then a tile each
+  int R;             // places of a layer
   int layer;         // the first one
-  int NW, share, extra;  // workers; tiles of each, and how many have one more, the first ones
+  int NW, share, extra;  // workers; places of each, and how many have one more, the first ones
   const uint16_t* q;
   float* out;
   int64_t q_stride, out_stride;
@@ -83,18 +85,18 @@ struct Segment {
         s = 0;
         ++layer;
       }
-      tiles = (int)(P[s + 1] - P[s]);
-    } while (tiles == 0);
+      tiles = (int)(P[s + 1] - P[s]) - kPackedPiece;
+    } while (tiles <= 0);
   }
 };
 
-// The worker that has tile x.
+// The worker that has the tile at place x.
 __device__ __forceinline__ int worker_of(int x, const PackedDev& p) {
   const int most = p.extra * (p.share + 1);
   return x < most ? x / (p.share + 1) : p.extra + (x - most) / p.share;
 }
 
-// The sequence that holds tile o of a layer: the last s with H P[s] <= o, a search of the whole warp.
+// The sequence that holds place o of a layer: the last s with H P[s] <= o, a search of the whole warp.
 __device__ __forceinline__ int seq_of(const int64_t* P, int b, int H, int o, int lane) {
   int a = 0, z = b;
   while (z - a > 1) {
@@ -186,6 +188,44 @@ __device__ __forceinline__ float row_exponent(const uint32_t (&pair)[G], BF16T) 
   return __uint_as_float(0x4B000000u | (uint32_t)big >> 23) - 8388735.f;
 }
 
+// The output row of a segment from the parts of workers first to last, in their order.  Eight parts' columns are on their way
+// together (28 parts one by one: 2 us of 162).
+template <int D>
+__device__ __forceinline__ void join(const float* parts, int first, int last, float* out, int lane) {
+  constexpr int QL = (D + 31) / 32;
+  auto from = [&](int w) { return parts + ((int64_t)w * 2 + (w == first ? 1 : 0)) * (D + 4); };
+  float big = -INFINITY;
+  for (int w = first + lane; w <= last; w += 32) big = fmaxf(big, __ldcg(from(w)));
+  big = warp_max(big);
+  float sum = 0.f, y[QL];
+#pragma unroll
+  for (int j = 0; j < QL; ++j) y[j] = 0.f;
+  for (int w0 = first; w0 <= last; w0 += 8) {
+    float f = 0.f, c[8][QL];
+    const float* mine = from(min(w0 + (lane & 7), last));
+    const float m = __ldcg(mine), l = __ldcg(mine + 1);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float* a = from(min(w0 + i, last)) + 4;
+#pragma unroll
+      for (int j = 0; j < QL; ++j) c[i][j] = lane + 32 * j < D ? __ldcg(a + lane + 32 * j) : 0.f;
+    }
+    if (m != -INFINITY) f = exp2_fast(m - big);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float fi = __shfl_sync(kFull, f, i), li = __shfl_sync(kFull, l, i);
+      if (w0 + i > last) continue;
+      sum = fmaf(fi, li, sum);
+#pragma unroll
+      for (int j = 0; j < QL; ++j) y[j] = fmaf(fi, c[i][j], y[j]);
+    }
+  }
+  const float inv = 1.f / sum;
+#pragma unroll
+  for (int j = 0; j < QL; ++j)
+    if (lane + 32 * j < D) out[lane + 32 * j] = y[j] * inv;
+}
+
 template <typename T, int D>
 __global__ void __launch_bounds__(32, Shape<D>::WARPS)
     packed_decode_kernel(Geometry g, Static st, PackedBuffers pb, PackedDev p) {
@@ -206,7 +246,8 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
   unsigned char* vs = smem + C::SK * C::STAGE;
   unsigned char* ps = vs + C::SV * C::STAGE;
   uint32_t* pw = reinterpret_cast<uint32_t*>(ps);
-  uint64_t* kfull = reinterpret_cast<uint64_t*>(ps + C::PS);
+  float2* rope = reinterpret_cast<float2*>(ps + C::PS);
+  uint64_t* kfull = reinterpret_cast<uint64_t*>(ps + C::PS + C::RS);
   uint64_t* vfull = kfull + C::SK;
   if (lane == 0) {
 #pragma unroll
@@ -219,21 +260,27 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
 
   Segment cs;  // of the consumed tiles
   int r;       // the next one in it
-  int x = lo;  // and among all
+  int x = lo;  // and its place among all
   {
     cs.layer = lo / p.R;
-    const int o = lo - cs.layer * p.R;
+    int o = lo - cs.layer * p.R;
     cs.s = seq_of(p.P, g.b, H, o, lane);
-    const int P0 = (int)p.P[cs.s];
-    cs.tiles = (int)p.P[cs.s + 1] - P0;
-    cs.h = (o - H * P0) / cs.tiles;
-    r = o - H * P0 - cs.h * cs.tiles;
+    const int P0 = (int)p.P[cs.s], n = (int)p.P[cs.s + 1] - P0;
+    o -= H * P0;
+    cs.tiles = n - kPackedPiece;
+    cs.h = o / n;
+    r = o - cs.h * n - kPackedPiece;
+    if (r < 0) {
+      x -= r;
+      r = 0;
+    }
   }
-  // What lane 0 issues copies from: the segment, its rows from the next tile on, the first of them in the planes, and how many
-  // tiles are left.
+  if (x >= hi) return;  // a share of one that is a segment's beginning
+  // What lane 0 issues copies from: the segment, the next tile's place, its rows from that tile on, and the first of them in
+  // the planes.
   struct Feed {
     Segment seg;
-    int rows, left;
+    int rows, x;
     int64_t row;
   };
   auto enter = [&](Feed& f, int first) {
@@ -245,7 +292,10 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
   auto step = [&](Feed& f) {
     f.rows -= kTile;
     f.row += kTile;
-    if (--f.left > 0 && f.rows <= 0) {
+    ++f.x;
+    if (f.rows > 0) return;
+    f.x += kPackedPiece;
+    if (f.x < hi) {
       f.seg.advance(p.P, H, g.b);
       enter(f, 0);
     }
@@ -255,7 +305,7 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
     bulk_g2s(to + C::KC, pairs + f.row * R::G, n * R::PB, bar);
   };
   auto rows_of = [&](const Feed& f) { return (uint32_t)min(kTile, (f.rows + kPackedRows - 1) & -kPackedRows); };
-  Feed kf{cs, 0, hi - lo, 0}, vf{cs, 0, hi - lo, 0};
+  Feed kf{cs, 0, x, 0}, vf{cs, 0, x, 0};
   auto issue_k = [&](int stage) {
     const uint32_t n = rows_of(kf);
     mbar_arrive_expect_tx(&kfull[stage], n * (R::RB + R::PB) * (kJoint ? 2 : 1));
@@ -279,8 +329,8 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
     }
     issue_k(0);
     if (!kJoint)
-      for (int i = 0; i < C::SV && vf.left > 0; ++i) issue_v(i);
-    for (int i = 1; i < C::SK && kf.left > 0; ++i) issue_k(i);
+      for (int i = 0; i < C::SV && vf.x < hi; ++i) issue_v(i);
+    for (int i = 1; i < C::SK && kf.x < hi; ++i) issue_k(i);
   }
   if (p.kv_before_wait) pdl_wait();
 
@@ -302,6 +352,7 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
   };
   fetch_q(cs);
   DState ds = p.ds[cs.s];
+  int turned = -1;  // the sequence whose rotation is in shared memory
   int kst = 0, vst = 0;
   uint32_t kph = 0, vph = 0;
   auto next = [](int& stage, uint32_t& phase, int n) {
@@ -310,14 +361,13 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
       phase ^= 1;
     }
   };
-  // After a wait that ran out: the copies that are still in flight end before their memory does.  `waits`: how many of the
-  // keys' tiles, and of the values', were waited for.
-  auto give_up = [&](int k_taken, int v_taken) {
+  // After a wait that ran out: copies that are still in flight end before their memory does.
+  auto give_up = [&]() {
     if (lane == 0) {
       atomicOr(p.status, STATUS_TIMEOUT);
-      for (int i = k_taken; i < hi - lo - kf.left; ++i, next(kst, kph, C::SK)) mbar_wait_bounded(&kfull[kst], kph, p.limit_ns);
+      for (int i = 0; i < C::SK; ++i, next(kst, kph, C::SK)) mbar_wait_bounded(&kfull[kst], kph, p.limit_ns);
       if (!kJoint)
-        for (int i = v_taken; i < hi - lo - vf.left; ++i, next(vst, vph, C::SV)) mbar_wait_bounded(&vfull[vst], vph, p.limit_ns);
+        for (int i = 0; i < C::SV; ++i, next(vst, vph, C::SV)) mbar_wait_bounded(&vfull[vst], vph, p.limit_ns);
     }
     __syncwarp();
   };
@@ -325,20 +375,28 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
   while (x < hi) {
     // ---- a piece: tiles [r, r1) of a segment
     const int r1 = min(cs.tiles, r + hi - x);
-    const int seg0 = x - r, seg1 = seg0 + cs.tiles;  // the segment's tiles among all
+    const int seg0 = x - r, seg1 = seg0 + cs.tiles;  // the places of the segment's tiles
     uint32_t qf[QF];  // the query as the keys' other operand
     float qsum;       // its sum over group t's columns, times qscale
     float kscale;     // of a product of codes and the query's parts
     {
+      const int half = g.rot / 2;
+      if (half > 0 && turned != cs.s) {  // of the sequence's heads, which come one after the other
+        turned = cs.s;
+        for (int k = lane; k < half; k += 32) {
+          float sn, c;
+          rope_sincos_full(ds.qpos, st.rope_g[k], &sn, &c);
+          rope[k] = make_float2(c, sn);
+        }
+        __syncwarp();
+      }
       float sum[QL], big = 0.f;
 #pragma unroll
       for (int j = 0; j < QL; ++j) {
         const int k = lane + 32 * j;
         if (k < g.rot) {
-          const int half = g.rot / 2;
-          float sn, c;
-          rope_sincos_full(ds.qpos, st.rope_g[k < half ? k : k - half], &sn, &c);
-          qa[j] = k < half ? qa[j] * c - qb[j] * sn : qa[j] * c + qb[j] * sn;
+          const float2 cs2 = rope[k < half ? k : k - half];
+          qa[j] = k < half ? qa[j] * cs2.x - qb[j] * cs2.y : qa[j] * cs2.x + qb[j] * cs2.y;
         }
         sum[j] = qa[j];
         big = fmaxf(big, fabsf(qa[j]));
@@ -396,8 +454,7 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
     for (; r < r1; ++r, r0 += kTile) {
       // ---- a tile
       if (!__all_sync(kFull, mbar_wait_bounded(&kfull[kst], kph, p.limit_ns))) {
-        const int taken = x - lo - (r1 - r);
-        give_up(taken, taken);
+        give_up();
         return;  // the segment is not joined
       }
       const unsigned char* kc = ks + kst * C::STAGE;
@@ -446,9 +503,8 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
       }
 
       if (!kJoint && !__all_sync(kFull, mbar_wait_bounded(&vfull[vst], vph, p.limit_ns))) {
-        const int taken = x - lo - (r1 - r);
         next(kst, kph, C::SK);
-        give_up(taken + 1, taken);
+        give_up();
         return;
       }
       uint32_t vpair[2][G];
@@ -492,7 +548,7 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
       }
       __syncwarp();
       if (!kJoint) {  // the keys are read
-        if (lane == 0 && kf.left > 0) issue_k(kst);
+        if (lane == 0 && kf.x < hi) issue_k(kst);
         next(kst, kph, C::SK);
       }
 
@@ -539,16 +595,17 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
       }
       __syncwarp();  // the stage and the weights are read
       if (kJoint) {
-        if (lane == 0 && kf.left > 0) issue_k(kst);
+        if (lane == 0 && kf.x < hi) issue_k(kst);
         next(kst, kph, C::SK);
       } else {
-        if (lane == 0 && vf.left > 0) issue_v(vst);
+        if (lane == 0 && vf.x < hi) issue_v(vst);
         next(vst, vph, C::SV);
       }
     }
 
     // ---- the end of a piece
     const Segment was = cs;
+    x += kPackedPiece;
     if (x < hi) {
       cs.advance(p.P, H, g.b);
       fetch_q(cs);
@@ -596,38 +653,21 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
       __stcg(part + 1, l);
     }
     const int first = worker_of(seg0, p), last = worker_of(seg1 - 1, p);
-    __threadfence();
     __syncwarp();
     int done = 0;
-    if (lane == 0) done = atomicAdd(p.counters + first, 1) == last - first;
-    if (!__shfl_sync(kFull, done, 0)) continue;
-    __threadfence();
-    auto from = [&](int w) { return p.parts + ((int64_t)w * 2 + (w == first ? 1 : 0)) * (D + 4); };
-    float big = -INFINITY;
-    for (int w = first + lane; w <= last; w += 32) big = fmaxf(big, __ldcg(from(w)));
-    big = warp_max(big);
-    float sum = 0.f, y[QL];
-#pragma unroll
-    for (int j = 0; j < QL; ++j) y[j] = 0.f;
-    for (int w = first; w <= last; ++w) {
-      const float* a = from(w);
-      const float mw = __ldcg(a);
-      const float f = mw == -INFINITY ? 0.f : exp2_fast(mw - big);
-      sum = fmaf(f, __ldcg(a + 1), sum);
-#pragma unroll
-      for (int j = 0; j < QL; ++j)
-        if (lane + 32 * j < D) y[j] = fmaf(f, __ldcg(a + 4 + lane + 32 * j), y[j]);
+    if (lane == 0) {  // the warp's part is visible before the count, the others' after it
+      __threadfence();
+      done = atomicAdd(p.counters + first, 1) == last - first;
+      if (done) __threadfence();
     }
-    const float inv = 1.f / sum;
-#pragma unroll
-    for (int j = 0; j < QL; ++j)
-      if (lane + 32 * j < D) orow[lane + 32 * j] = y[j] * inv;
+    if (!__shfl_sync(kFull, done, 0)) continue;
+    join<D>(p.parts, first, last, orow, lane);
     if (lane == 0) p.counters[first] = 0;
   }
 }
 
 template <typename T, int D>
-cudaError_t launch_t(const Geometry& g, const Static& st, const PackedBuffers& pb, PackedDev p, int64_t tiles, int device,
+cudaError_t launch_t(const Geometry& g, const Static& st, const PackedBuffers& pb, PackedDev p, int64_t places, int device,
                      int num_sms, cudaStream_t stream, int* grid, DecodePlan* plan) {
   using C = Shape<D>;
   auto* kernel = packed_decode_kernel<T, D>;
@@ -641,9 +681,9 @@ cudaError_t launch_t(const Geometry& g, const Static& st, const PackedBuffers& p
     occ = std::min(occ, C::WARPS);
     if (device >= 0 && device < 64) occupancy[device].store(occ, std::memory_order_relaxed);
   }
-  p.NW = (int)std::min<int64_t>({(int64_t)occ * num_sms, kMaxPackedWorkers, tiles});
-  p.share = (int)(tiles / p.NW);
-  p.extra = (int)(tiles % p.NW);
+  p.NW = (int)std::min<int64_t>({(int64_t)occ * num_sms, kMaxPackedWorkers, places});
+  p.share = (int)(places / p.NW);
+  p.extra = (int)(places % p.NW);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)p.NW);
   cfg.blockDim = dim3(32);
@@ -666,8 +706,8 @@ cudaError_t launch_packed_decode(const Geometry& g, const Static& st, const Pack
   PackedDev p;
   p.ds = a.dstate;
   p.P = a.P;
-  const int64_t tiles = a.R * a.n_layers;
-  if (tiles > INT32_MAX) return cudaErrorInvalidValue;  // 10 TB of rows
+  const int64_t places = a.R * a.n_layers;
+  if (places > INT32_MAX) return cudaErrorInvalidValue;  // 10 TB of rows
   p.R = (int)a.R;
   p.layer = a.layer;
   p.NW = p.share = p.extra = 0;
@@ -683,8 +723,8 @@ cudaError_t launch_packed_decode(const Geometry& g, const Static& st, const Pack
   p.kv_before_wait = a.kv_before_wait;
   auto by_dtype = [&](auto dc) {
     constexpr int D = decltype(dc)::value;
-    return g.dtype == 1 ? launch_t<BF16T, D>(g, st, pb, p, tiles, a.device, num_sms, stream, grid, plan)
-                        : launch_t<F16T, D>(g, st, pb, p, tiles, a.device, num_sms, stream, grid, plan);
+    return g.dtype == 1 ? launch_t<BF16T, D>(g, st, pb, p, places, a.device, num_sms, stream, grid, plan)
+                        : launch_t<F16T, D>(g, st, pb, p, places, a.device, num_sms, stream, grid, plan);
   };
   switch (g.D) {
     case 64:
