@@ -847,7 +847,7 @@ static kvc_status append_impl(kvc_cache* c, int layer, const void* k, const void
     cudaError_t e;
     // a few tokens (fewer units than SMs) bring their upload as a kernel parameter
     kvc::AppendImage small;
-    const bool fits = n_plan > 0 && bytes <= sizeof(small) && n_plan * nl < c->num_sms;
+    const bool fits = n_plan > 0 && bytes <= sizeof(small) && (c->packed() || n_plan * nl < c->num_sms);
     unsigned char* img = fits ? reinterpret_cast<unsigned char*>(&small) : c->ring.reserve(bytes, &e);
     if (!img) return cuda_fail(e, "staging");
     c->bk.book.apply_append(n_new, kinds, pos, (free_in_block && !local) ? kept.data() : nullptr);

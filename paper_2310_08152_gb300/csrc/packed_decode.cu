@@ -41,16 +41,20 @@ struct Shape {
   // Workers of an SM.  Each of its four schedulers has the same number, or those with more end last: 15, 13 and 10 at 80, 96
   // and 128 columns, which two stages of both leave room for, were 20 to 25 % slower.
   static constexpr int WARPS = D == 128 ? 12 : 16;
-  // Stages of keys and of values (of 128 columns three of both leave room for 8)
-  static constexpr int SK = 2, SV = D == 64 ? 2 : 1;
+  // Stages of a worker: of 64 columns two for a tile's keys and values together, else, where those have no room, three for
+  // keys and values in turn.  What is read makes room for what comes S behind it.  (Of 64 columns in turn, in four: 176 -> 182
+  // us, by twice the waits; of 128, two stages of keys and one of values: 155 -> 159, as values then come late.)
+  static constexpr bool JOINT = D == 64;
+  static constexpr int S = JOINT ? 2 : 3;
   static constexpr int KC = kTile * R::RB, KP = kTile * R::PB;
-  static constexpr int STAGE = KC + KP;  // codes, pairs
+  static constexpr int HALF = KC + KP, STAGE = JOINT ? 2 * HALF : HALF;  // codes and pairs, of the keys and then of the values
   // weights times steps: [column of the operand][row of both halves of a tile] as pairs of f16, the columns 16 bytes more
   // than 128 apart, so that eight lanes' 16-byte loads meet no bank twice; the query between pieces
+  static_assert(JOINT || S % 2 == 1);
   static constexpr int PW = 36;
   static constexpr int PS = 4 * 8 * PW;
   static constexpr int RS = 8 * (D / 2);       // the rotation's cosines and sines at a sequence's position
-  static constexpr int SMEM = (SK + SV) * STAGE + PS + RS + 8 * (SK + SV);
+  static constexpr int SMEM = S * STAGE + PS + RS + 8 * S;
   static_assert(4 * D <= PS && PS % 16 == 0);
   static_assert(WARPS * (SMEM + 1024) <= 228 * 1024);
 };
@@ -235,23 +239,19 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
   constexpr int KW = D == 128 ? 4 : 2;              // code words of a row a lane has of the keys
   constexpr int NT = D / 16;                        // tiles of 16 columns of the values
   constexpr int QF = 2 * (D / 16);                  // registers of the query
-  constexpr bool kJoint = C::SK == C::SV;           // keys and values come together
   extern __shared__ __align__(128) unsigned char smem[];
   pdl_launch_dependents();
   const int lane = threadIdx.x, gr = lane >> 2, t = lane & 3, tg = t < G ? t : G - 1;
   const int wid = blockIdx.x, H = g.H;
   const int lo = wid * p.share + min(wid, p.extra), hi = lo + p.share + (wid < p.extra ? 1 : 0);
 
-  unsigned char* ks = smem;
-  unsigned char* vs = smem + C::SK * C::STAGE;
-  unsigned char* ps = vs + C::SV * C::STAGE;
+  unsigned char* ps = smem + C::S * C::STAGE;
   uint32_t* pw = reinterpret_cast<uint32_t*>(ps);
   float2* rope = reinterpret_cast<float2*>(ps + C::PS);
-  uint64_t* kfull = reinterpret_cast<uint64_t*>(ps + C::PS + C::RS);
-  uint64_t* vfull = kfull + C::SK;
+  uint64_t* full = reinterpret_cast<uint64_t*>(ps + C::PS + C::RS);
   if (lane == 0) {
 #pragma unroll
-    for (int i = 0; i < C::SK + C::SV; ++i) mbar_init(&kfull[i], 1);
+    for (int i = 0; i < C::S; ++i) mbar_init(&full[i], 1);
     fence_mbar_init();
   }
   fence_proxy_async_smem();
@@ -278,59 +278,45 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
   if (x >= hi) return;  // a share of one that is a segment's beginning
   // What lane 0 issues copies from: the segment, the next tile's place, its rows from that tile on, and the first of them in
   // the planes.
-  struct Feed {
+  struct {
     Segment seg;
     int rows, x;
     int64_t row;
-  };
-  auto enter = [&](Feed& f, int first) {
-    const DState d = p.ds[f.seg.s];
+  } feed{cs, 0, x, 0};
+  auto enter = [&](int first) {
+    const DState d = p.ds[feed.seg.s];
     const int r0 = d.begin / kPackedRows * kPackedRows + first * kTile;
-    f.row = (int64_t)(p.layer + f.seg.layer) * H * g.C + st.seq_row0[f.seg.s] + (int64_t)f.seg.h * st.cap[f.seg.s] + r0;
-    f.rows = d.len - r0;
+    feed.row = (int64_t)(p.layer + feed.seg.layer) * H * g.C + st.seq_row0[feed.seg.s] + (int64_t)feed.seg.h * st.cap[feed.seg.s] + r0;
+    feed.rows = d.len - r0;
   };
-  auto step = [&](Feed& f) {
-    f.rows -= kTile;
-    f.row += kTile;
-    ++f.x;
-    if (f.rows > 0) return;
-    f.x += kPackedPiece;
-    if (f.x < hi) {
-      f.seg.advance(p.P, H, g.b);
-      enter(f, 0);
+  // the tile's keys, its values or both, after which the next tile comes
+  auto issue = [&](int stage, bool keys) {
+    const uint32_t n = (uint32_t)min(kTile, (feed.rows + kPackedRows - 1) & -kPackedRows);
+    unsigned char* to = smem + stage * C::STAGE;
+    mbar_arrive_expect_tx(&full[stage], n * (R::RB + R::PB) * (C::JOINT ? 2 : 1));
+    bulk_g2s(to, (keys ? pb.kc : pb.vc) + feed.row * R::RB, n * R::RB, &full[stage]);
+    bulk_g2s(to + C::KC, (keys ? pb.kp : pb.vp) + feed.row * R::G, n * R::PB, &full[stage]);
+    if (C::JOINT) {
+      bulk_g2s(to + C::HALF, pb.vc + feed.row * R::RB, n * R::RB, &full[stage]);
+      bulk_g2s(to + C::HALF + C::KC, pb.vp + feed.row * R::G, n * R::PB, &full[stage]);
+    } else if (keys) {
+      return;
     }
-  };
-  auto copy = [&](const Feed& f, unsigned char* to, const unsigned char* codes, const uint32_t* pairs, uint64_t* bar, uint32_t n) {
-    bulk_g2s(to, codes + f.row * R::RB, n * R::RB, bar);
-    bulk_g2s(to + C::KC, pairs + f.row * R::G, n * R::PB, bar);
-  };
-  auto rows_of = [&](const Feed& f) { return (uint32_t)min(kTile, (f.rows + kPackedRows - 1) & -kPackedRows); };
-  Feed kf{cs, 0, x, 0}, vf{cs, 0, x, 0};
-  auto issue_k = [&](int stage) {
-    const uint32_t n = rows_of(kf);
-    mbar_arrive_expect_tx(&kfull[stage], n * (R::RB + R::PB) * (kJoint ? 2 : 1));
-    copy(kf, ks + stage * C::STAGE, pb.kc, pb.kp, &kfull[stage], n);
-    if (kJoint) copy(kf, vs + stage * C::STAGE, pb.vc, pb.vp, &kfull[stage], n);
-    step(kf);
-  };
-  auto issue_v = [&](int stage) {
-    const uint32_t n = rows_of(vf);
-    mbar_arrive_expect_tx(&vfull[stage], n * (R::RB + R::PB));
-    copy(vf, vs + stage * C::STAGE, pb.vc, pb.vp, &vfull[stage], n);
-    step(vf);
+    feed.rows -= kTile;
+    feed.row += kTile;
+    ++feed.x;
+    if (feed.rows > 0) return;
+    feed.x += kPackedPiece;
+    if (feed.x < hi) {
+      feed.seg.advance(p.P, H, g.b);
+      enter(0);
+    }
   };
   // a decode before this one writes neither rows nor state: they may come before it is complete, while the query, the outputs
   // and the parts may be shared with it
   if (lane == 0) {
-    enter(kf, r);
-    if (!kJoint) {
-      vf.row = kf.row;
-      vf.rows = kf.rows;
-    }
-    issue_k(0);
-    if (!kJoint)
-      for (int i = 0; i < C::SV && vf.x < hi; ++i) issue_v(i);
-    for (int i = 1; i < C::SK && kf.x < hi; ++i) issue_k(i);
+    enter(r);
+    for (int i = 0; i < C::S && feed.x < hi; ++i) issue(i, C::JOINT || i % 2 == 0);
   }
   if (p.kv_before_wait) pdl_wait();
 
@@ -353,21 +339,20 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
   fetch_q(cs);
   DState ds = p.ds[cs.s];
   int turned = -1;  // the sequence whose rotation is in shared memory
-  int kst = 0, vst = 0;
-  uint32_t kph = 0, vph = 0;
-  auto next = [](int& stage, uint32_t& phase, int n) {
-    if (++stage == n) {
+  int stage = 0;
+  uint32_t phase = 0;
+  auto next = [&]() {
+    if (++stage == C::S) {
       stage = 0;
       phase ^= 1;
     }
   };
+  auto arrived = [&]() { return __all_sync(kFull, mbar_wait_bounded(&full[stage], phase, p.limit_ns)); };
   // After a wait that ran out: copies that are still in flight end before their memory does.
   auto give_up = [&]() {
     if (lane == 0) {
       atomicOr(p.status, STATUS_TIMEOUT);
-      for (int i = 0; i < C::SK; ++i, next(kst, kph, C::SK)) mbar_wait_bounded(&kfull[kst], kph, p.limit_ns);
-      if (!kJoint)
-        for (int i = 0; i < C::SV; ++i, next(vst, vph, C::SV)) mbar_wait_bounded(&vfull[vst], vph, p.limit_ns);
+      for (int i = 0; i < C::S; ++i, next()) mbar_wait_bounded(&full[stage], phase, p.limit_ns);
     }
     __syncwarp();
   };
@@ -453,14 +438,14 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
     x += r1 - r;
     for (; r < r1; ++r, r0 += kTile) {
       // ---- a tile
-      if (!__all_sync(kFull, mbar_wait_bounded(&kfull[kst], kph, p.limit_ns))) {
+      if (!arrived()) {
         give_up();
         return;  // the segment is not joined
       }
-      const unsigned char* kc = ks + kst * C::STAGE;
+      const int k_stage = stage;
+      const unsigned char* kc = smem + k_stage * C::STAGE;
       const uint32_t* kp = reinterpret_cast<const uint32_t*>(kc + C::KC);
-      const unsigned char* vc = vs + (kJoint ? kst : vst) * C::STAGE;
-      const uint32_t* vp = reinterpret_cast<const uint32_t*>(vc + C::KC);
+      next();
 
       float z[2];  // logits of rows gr + 8 t of the tile's halves
 #pragma unroll
@@ -502,11 +487,14 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
         z[b] = (two ? s1 : s0) + __shfl_xor_sync(kFull, two ? s0 : s1, 2);
       }
 
-      if (!kJoint && !__all_sync(kFull, mbar_wait_bounded(&vfull[vst], vph, p.limit_ns))) {
-        next(kst, kph, C::SK);
+      if (!C::JOINT && !arrived()) {
         give_up();
         return;
       }
+      const int v_stage = C::JOINT ? k_stage : stage;
+      const unsigned char* vc = smem + v_stage * C::STAGE + (C::JOINT ? C::HALF : 0);
+      const uint32_t* vp = reinterpret_cast<const uint32_t*>(vc + C::KC);
+      if (!C::JOINT) next();
       uint32_t vpair[2][G];
 #pragma unroll
       for (int b = 0; b < 2; ++b)
@@ -547,10 +535,7 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
         pw[(2 * i + 1) * C::PW + at] = pack_halves(x0 - back.x, x1 - back.y);
       }
       __syncwarp();
-      if (!kJoint) {  // the keys are read
-        if (lane == 0 && kf.x < hi) issue_k(kst);
-        next(kst, kph, C::SK);
-      }
+      if (!C::JOINT && lane == 0 && feed.x < hi) issue(k_stage, false);  // the keys are read: S is odd
 
       float acc[NT][4];
 #pragma unroll
@@ -593,14 +578,8 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
         o[2 * i] += acc[i][0] + acc[i][1];
         o[2 * i + 1] += acc[i][2] + acc[i][3];
       }
-      __syncwarp();  // the stage and the weights are read
-      if (kJoint) {
-        if (lane == 0 && kf.x < hi) issue_k(kst);
-        next(kst, kph, C::SK);
-      } else {
-        if (lane == 0 && vf.x < hi) issue_v(vst);
-        next(vst, vph, C::SV);
-      }
+      __syncwarp();  // the values and the weights are read
+      if (lane == 0 && feed.x < hi) issue(v_stage, true);
     }
 
     // ---- the end of a piece
@@ -695,7 +674,7 @@ cudaError_t launch_t(const Geometry& g, const Static& st, const PackedBuffers& p
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   *grid = p.NW;
-  *plan = {5, p.NW, kTile, C::SK};
+  *plan = {5, p.NW, kTile, C::S};
   return cudaLaunchKernelEx(&cfg, kernel, g, st, pb, p);
 }
 
