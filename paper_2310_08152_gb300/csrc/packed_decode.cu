@@ -40,11 +40,11 @@ struct Shape {
   using R = PackedRow<D>;
   // Workers of an SM.  Each of its four schedulers has the same number, or those with more end last: 15, 13 and 10 at 80, 96
   // and 128 columns, which two stages of both leave room for, were 20 to 25 % slower.
-  static constexpr int WARPS = D == 128 ? 12 : 16;
+  static constexpr int WARPS = D == 64 ? 16 : 12;
   // Stages of a worker: of 64 columns two for a tile's keys and values together, else, where those have no room, three for
   // keys and values in turn.  What is read makes room for what comes S behind it.  (Of 64 columns in turn, in four: 176 -> 182
   // us, by twice the waits; of 128, two stages of keys and one of values: 155 -> 159, as values then come late.)
-  static constexpr bool JOINT = D == 64;
+  static constexpr bool JOINT = D != 128;
   static constexpr int S = JOINT ? 2 : 3;
   static constexpr int KC = kTile * R::RB, KP = kTile * R::PB;
   static constexpr int HALF = KC + KP, STAGE = JOINT ? 2 * HALF : HALF;  // codes and pairs, of the keys and then of the values
@@ -276,34 +276,42 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
     }
   }
   if (x >= hi) return;  // a share of one that is a segment's beginning
-  // What lane 0 issues copies from: the segment, the next tile's place, its rows from that tile on, and the first of them in
-  // the planes.
+  // The first lanes issue copies: together K codes, K pairs, V codes and V pairs one each (a lane by itself: 170 -> 175 us of
+  // 64 columns), in turn the first lane codes and pairs (two lanes: 155 -> 156 of 128).  What they issue them from: the
+  // segment, the next tile's place, the segment's rows from that tile on, and the first of them in the planes.
+  constexpr int kFeeders = C::JOINT ? 4 : 1;
   struct {
     Segment seg;
     int rows, x;
     int64_t row;
-  } feed{cs, 0, x, 0};
+    const unsigned char* from;  // of the lane's plane
+  } feed{cs, 0, x, 0, nullptr};
+  const uint32_t row_bytes = lane & 1 ? R::PB : R::RB;
   auto enter = [&](int first) {
     const DState d = p.ds[feed.seg.s];
     const int r0 = d.begin / kPackedRows * kPackedRows + first * kTile;
     feed.row = (int64_t)(p.layer + feed.seg.layer) * H * g.C + st.seq_row0[feed.seg.s] + (int64_t)feed.seg.h * st.cap[feed.seg.s] + r0;
     feed.rows = d.len - r0;
+    if (C::JOINT) {
+      const void *codes = lane & 2 ? pb.vc : pb.kc, *pairs = lane & 2 ? pb.vp : pb.kp;
+      feed.from = static_cast<const unsigned char*>(lane & 1 ? pairs : codes) + feed.row * row_bytes;
+    }
   };
   // the tile's keys, its values or both, after which the next tile comes
   auto issue = [&](int stage, bool keys) {
     const uint32_t n = (uint32_t)min(kTile, (feed.rows + kPackedRows - 1) & -kPackedRows);
     unsigned char* to = smem + stage * C::STAGE;
-    mbar_arrive_expect_tx(&full[stage], n * (R::RB + R::PB) * (C::JOINT ? 2 : 1));
-    bulk_g2s(to, (keys ? pb.kc : pb.vc) + feed.row * R::RB, n * R::RB, &full[stage]);
-    bulk_g2s(to + C::KC, (keys ? pb.kp : pb.vp) + feed.row * R::G, n * R::PB, &full[stage]);
+    if (lane == 0) mbar_arrive_expect_tx(&full[stage], n * (R::RB + R::PB) * (C::JOINT ? 2 : 1));
     if (C::JOINT) {
-      bulk_g2s(to + C::HALF, pb.vc + feed.row * R::RB, n * R::RB, &full[stage]);
-      bulk_g2s(to + C::HALF + C::KC, pb.vp + feed.row * R::G, n * R::PB, &full[stage]);
-    } else if (keys) {
-      return;
+      bulk_g2s(to + (lane & 1 ? C::KC : 0) + (lane & 2 ? C::HALF : 0), feed.from, n * row_bytes, &full[stage]);
+      feed.from += kTile * row_bytes;
+    } else {
+      bulk_g2s(to, (keys ? pb.kc : pb.vc) + feed.row * R::RB, n * R::RB, &full[stage]);
+      bulk_g2s(to + C::KC, (keys ? pb.kp : pb.vp) + feed.row * R::G, n * R::PB, &full[stage]);
+      if (keys) return;
+      feed.row += kTile;
     }
     feed.rows -= kTile;
-    feed.row += kTile;
     ++feed.x;
     if (feed.rows > 0) return;
     feed.x += kPackedPiece;
@@ -314,7 +322,7 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
   };
   // a decode before this one writes neither rows nor state: they may come before it is complete, while the query, the outputs
   // and the parts may be shared with it
-  if (lane == 0) {
+  if (lane < kFeeders) {
     enter(r);
     for (int i = 0; i < C::S && feed.x < hi; ++i) issue(i, C::JOINT || i % 2 == 0);
   }
@@ -535,7 +543,7 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
         pw[(2 * i + 1) * C::PW + at] = pack_halves(x0 - back.x, x1 - back.y);
       }
       __syncwarp();
-      if (!C::JOINT && lane == 0 && feed.x < hi) issue(k_stage, false);  // the keys are read: S is odd
+      if (!C::JOINT && lane < kFeeders && feed.x < hi) issue(k_stage, false);  // the keys are read: S is odd
 
       float acc[NT][4];
 #pragma unroll
@@ -579,7 +587,7 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
         o[2 * i + 1] += acc[i][2] + acc[i][3];
       }
       __syncwarp();  // the values and the weights are read
-      if (lane == 0 && feed.x < hi) issue(v_stage, true);
+      if (lane < kFeeders && feed.x < hi) issue(v_stage, true);
     }
 
     // ---- the end of a piece
