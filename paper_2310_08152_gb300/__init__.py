@@ -571,6 +571,8 @@ class KVCache:
         self._score_scratch = self._score_counts = None
         self._budget = np.zeros((2, self.b), np.int64)
         self._budget_at = self._budget.ctypes.data
+        self._pairs = np.zeros((2, self.b), np.int32)  # copy_from's
+        self._pairs_at = self._pairs.ctypes.data
 
     # views of the device layout (rows of d_head elements)
     def k_plane(self, layer: int):
@@ -743,13 +745,20 @@ class KVCache:
         if not other.handle:
             raise KvcError(5, "the other cache is closed")
         memory = (self._scores, other._scores) if self._scores is not None else ()
-        kvc_copy(self.handle, other.handle, dst, src, self._stream(stream, *memory))
+        handle = self._stream(stream, *memory)
+        n = len(dst)
+        if n != len(src) or n > self.b:
+            kvc_copy(self.handle, other.handle, dst, src, handle)  # whose errors they are
+            return
+        # as for evict: two rows of one array that is kept (two arrays and their addresses each took 2 us a call)
+        self._pairs[0, :n], self._pairs[1, :n] = dst, src
+        _check(lib().kvc_copy(self.handle, other.handle, n, self._pairs_at, self._pairs_at + 4 * self.b, handle))
 
     def truncate(self, tokens, stream=None):
         """Cuts every sequence s back to the first tokens[s] of its history (a number for all; -1 leaves a sequence as it is):
         drafted tokens go, and 0 frees the sequence for another."""
-        tokens = _per_seq(tokens, self.b, "tokens")
-        kvc_truncate(self.handle, tokens, self._stream(stream, self._scores))
+        self._budget[0] = tokens if isinstance(tokens, int) else _per_seq(tokens, self.b, "tokens")
+        _check(lib().kvc_truncate(self.handle, self._budget_at, self._stream(stream, self._scores)))
 
     # sequences that share a prefix
     def set_prefix(self, prefix: Optional["KVCache"], parent=None):

@@ -174,6 +174,12 @@ __device__ __forceinline__ void copy_block(const CopyDev& p, const CopyPlan& pla
   }
 }
 
+// The state that the next kernels read; a decode may do so as soon as this kernel's blocks have ended.
+__device__ __forceinline__ void store_upload(const AppendImage& img, int bytes, uint4* dyn) {
+  for (int i = threadIdx.x; i < bytes / 16; i += kCopyThreads) dyn[i] = img.v[i];
+  __threadfence();
+}
+
 template <typename T, int D, int SB, int DB>
 __global__ void __launch_bounds__(kCopyThreads) copy_kernel(CopyDev p, CopyPlan plan) {
   copy_block<T, D, SB, DB>(p, plan);
@@ -183,8 +189,7 @@ __global__ void __launch_bounds__(kCopyThreads) copy_kernel(CopyDev p, CopyPlan 
 template <typename T, int D, int SB, int DB>
 __global__ void __launch_bounds__(kCopyThreads)
     copy_image_kernel(CopyDev p, const __grid_constant__ AppendImage img, int img_bytes, int sources, int targets, uint4* dyn) {
-  if (blockIdx.x == 0)
-    for (int i = threadIdx.x; i < img_bytes / 16; i += kCopyThreads) dyn[i] = img.v[i];
+  if (blockIdx.x == 0) store_upload(img, img_bytes, dyn);
   const char* at = reinterpret_cast<const char*>(&img);
   copy_block<T, D, SB, DB>(p, {reinterpret_cast<const CopySource*>(at + sources), reinterpret_cast<const CopyTarget*>(at + targets)});
 }
@@ -207,8 +212,8 @@ __global__ void __launch_bounds__(kCopyThreads) copy_scores_kernel(CopyDev p, co
 
 __global__ void __launch_bounds__(kCopyThreads)
     drop_image_kernel(CopyDev p, const __grid_constant__ AppendImage img, int img_bytes, int targets, uint4* dyn) {
-  if (blockIdx.x == 0)
-    for (int i = threadIdx.x; i < img_bytes / 16; i += kCopyThreads) dyn[i] = img.v[i];
+  pdl_wait();  // a decode before it lets it start and still reads the state
+  if (blockIdx.x == 0) store_upload(img, img_bytes, dyn);
   if (p.dst.scores == nullptr) return;
   const CopyTarget* t = reinterpret_cast<const CopyTarget*>(reinterpret_cast<const char*>(&img) + targets);
   score_block(p, t[blockIdx.x / (p.g.M * p.g.H)], false);
@@ -274,14 +279,25 @@ cudaError_t launch_drop(const Geometry& g, const CopyArgs& a, cudaStream_t strea
   *launched = 0;
   const CopyDev p{g, a.src, a.dst, 0};
   const unsigned blocks = a.dst.scores ? (unsigned)((int64_t)a.n_targets * g.M * g.H) : 1;
-  if (a.img)
-    drop_image_kernel<<<blocks, kCopyThreads, 0, stream>>>(p, *a.img, (int)a.img_bytes, (int)a.targets,
-                                                           static_cast<uint4*>(a.dyn));
-  else if (a.dst.scores)
+  if (a.img) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(blocks);
+    cfg.blockDim = dim3(kCopyThreads);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, drop_image_kernel, p, *a.img, (int)a.img_bytes, (int)a.targets,
+                                             static_cast<uint4*>(a.dyn));
+    if (e != cudaSuccess) return e;
+  } else if (a.dst.scores) {
     copy_scores_kernel<<<blocks, kCopyThreads, 0, stream>>>(
         p, reinterpret_cast<const CopyTarget*>(static_cast<const char*>(a.dyn) + a.targets), 0);
-  else
+  } else {
     return cudaSuccess;
+  }
   const cudaError_t e = cudaGetLastError();
   if (e == cudaSuccess) *launched = 1;
   return e;
