@@ -239,6 +239,9 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
   constexpr int KW = D == 128 ? 4 : 2;              // code words of a row a lane has of the keys
   constexpr int NT = D / 16;                        // tiles of 16 columns of the values
   constexpr int QF = 2 * (D / 16);                  // registers of the query
+  // Columns of the keys' other operand, of which lane t gets 2 t and 2 t + 1: with two groups, part t % 2 of each (twice, so
+  // that a lane and its neighbour have all of a row's sums); with more, both parts of group t.
+  constexpr bool kTwice = G == 2;
   extern __shared__ __align__(128) unsigned char smem[];
   pdl_launch_dependents();
   const int lane = threadIdx.x, gr = lane >> 2, t = lane & 3, tg = t < G ? t : G - 1;
@@ -370,7 +373,7 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
     const int r1 = min(cs.tiles, r + hi - x);
     const int seg0 = x - r, seg1 = seg0 + cs.tiles;  // the places of the segment's tiles
     uint32_t qf[QF];  // the query as the keys' other operand
-    float qsum;       // its sum over group t's columns, times qscale
+    float qsum[2];    // its sum over group t's columns, or over the first's and the second's, times qscale
     float kscale;     // of a product of codes and the query's parts
     {
       const int half = g.rot / 2;
@@ -404,10 +407,14 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
       const int e = big > 0.f && big < INFINITY ? max(-115, min(115, 13 - (int)(__float_as_uint(big) >> 23) + 127)) : 0;
       const float up = __uint_as_float((uint32_t)(127 + e) << 23);
       kscale = p.qscale * __uint_as_float((uint32_t)(127 - e) << 23);
-      qsum = 0.f;
+      qsum[0] = qsum[1] = 0.f;
 #pragma unroll
-      for (int j = 0; j < QL; ++j)
-        if (t == j) qsum = sum[j] * p.qscale;
+      for (int j = 0; j < QL; ++j) {
+        if (kTwice)
+          qsum[j & 1] = sum[j] * p.qscale;
+        else if (t == j)
+          qsum[0] = sum[j] * p.qscale;
+      }
       __syncwarp();  // the weights of the piece before are read
 #pragma unroll
       for (int j = 0; j < QL; ++j) {  // both parts of a column side by side
@@ -415,11 +422,11 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
         if (lane + 32 * j < D) pw[lane + 32 * j] = pack_halves(h, y - h);
       }
       __syncwarp();
-      // column gr of the operand: group gr / 2, part gr % 2
-      const uint32_t which = gr & 1 ? 0x7632u : 0x5410u;
+      const int col_group = kTwice ? gr & 1 : gr >> 1;
+      const uint32_t which = (kTwice ? gr & 2 : gr & 1) ? 0x7632u : 0x5410u;  // the part
       auto word = [&](int k, uint32_t* f) {
         const uint4 a = *reinterpret_cast<const uint4*>(pw + k), b = *reinterpret_cast<const uint4*>(pw + k + 4);
-        const uint32_t mask = (k >> 5) == (gr >> 1) ? 0xFFFFFFFFu : 0u;
+        const uint32_t mask = (k >> 5) == col_group ? 0xFFFFFFFFu : 0u;
         f[0] = __byte_perm(a.x, b.x, which) & mask;
         f[1] = __byte_perm(a.y, b.y, which) & mask;
         f[2] = __byte_perm(a.z, b.z, which) & mask;
@@ -430,7 +437,7 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
       if constexpr (D == 96) word(64 + 8 * t, qf + 8);
       if constexpr (D == 80) {
         const uint4 a = *reinterpret_cast<const uint4*>(pw + 64 + 4 * t);
-        const uint32_t mask = gr >> 1 == 2 ? 0xFFFFFFFFu : 0u;
+        const uint32_t mask = col_group == 2 ? 0xFFFFFFFFu : 0u;
         qf[8] = __byte_perm(a.x, a.z, which) & mask;
         qf[9] = __byte_perm(a.y, a.w, which) & mask;
       }
@@ -459,11 +466,12 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         float v[4];  // lane t's group's part of the logits of rows gr + 8 i
+        float cc[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
         for (int a = 0; a < 2; ++a) {
           const int row = 32 * b + 16 * a + gr;
           const unsigned char *u0 = kc + row * R::RB, *w0 = u0 + 8 * R::RB;
-          float c[4] = {0.f, 0.f, 0.f, 0.f};
+          float(&c)[4] = cc[a];
           if constexpr (D == 128) {
             const uint4 u = *reinterpret_cast<const uint4*>(u0 + 16 * t), w = *reinterpret_cast<const uint4*>(w0 + 16 * t);
             key_word(c, u.x, w.x, reinterpret_cast<const uint32_t(&)[4]>(qf[0]));
@@ -483,16 +491,31 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
             const uint32_t w = __byte_perm(*reinterpret_cast<const uint16_t*>(w0 + 32 + 2 * t), 0, 0x4140);
             mma(c, low_codes(u), low_codes(w), high_codes(u), high_codes(w), qf[8], qf[9]);
           }
+          if (kTwice) continue;
           // a lane past the groups has a product and a sum of 0
           const float2 p0 = pair_values(kp[row * G + tg], T{}), p1 = pair_values(kp[(row + 8) * G + tg], T{});
-          v[2 * a] = fmaf(p0.y, fmaf(c[0] + c[1], kscale, 8.f * qsum), p0.x * qsum);
-          v[2 * a + 1] = fmaf(p1.y, fmaf(c[2] + c[3], kscale, 8.f * qsum), p1.x * qsum);
+          v[2 * a] = fmaf(p0.y, fmaf(c[0] + c[1], kscale, 8.f * qsum[0]), p0.x * qsum[0]);
+          v[2 * a + 1] = fmaf(p1.y, fmaf(c[2] + c[3], kscale, 8.f * qsum[0]), p1.x * qsum[0]);
         }
-        // the sum over the groups; lane t is left with row gr + 8 t
         const bool odd = t & 1, two = t & 2;
-        const float s0 = (odd ? v[1] : v[0]) + __shfl_xor_sync(kFull, odd ? v[0] : v[1], 1);
-        const float s1 = (odd ? v[3] : v[2]) + __shfl_xor_sync(kFull, odd ? v[2] : v[3], 1);
-        z[b] = (two ? s1 : s0) + __shfl_xor_sync(kFull, two ? s0 : s1, 2);
+        if constexpr (kTwice) {
+          // lane t's row is gr + 8 t: one part of its two products is here, the other at the neighbour, whose row's part goes
+          // there
+          float d[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) d[i] = two ? cc[1][i] : cc[0][i];
+          const float s0 = (odd ? d[2] : d[0]) + __shfl_xor_sync(kFull, odd ? d[0] : d[2], 1);
+          const float s1 = (odd ? d[3] : d[1]) + __shfl_xor_sync(kFull, odd ? d[1] : d[3], 1);
+          const uint2 kpair = *reinterpret_cast<const uint2*>(kp + 2 * (32 * b + 8 * t + gr));
+          const float2 p0 = pair_values(kpair.x, T{}), p1 = pair_values(kpair.y, T{});
+          z[b] = fmaf(p0.y, fmaf(s0, kscale, 8.f * qsum[0]), p0.x * qsum[0]) +
+                 fmaf(p1.y, fmaf(s1, kscale, 8.f * qsum[1]), p1.x * qsum[1]);
+        } else {
+          // the sum over the groups; lane t is left with row gr + 8 t
+          const float s0 = (odd ? v[1] : v[0]) + __shfl_xor_sync(kFull, odd ? v[0] : v[1], 1);
+          const float s1 = (odd ? v[3] : v[2]) + __shfl_xor_sync(kFull, odd ? v[2] : v[3], 1);
+          z[b] = (two ? s1 : s0) + __shfl_xor_sync(kFull, two ? s0 : s1, 2);
+        }
       }
 
       if (!C::JOINT && !arrived()) {
