@@ -102,34 +102,10 @@ __device__ __forceinline__ void copy_block(const CopyDev& p, const CopyPlan& pla
     for (int u = 0; u < U; ++u) {
       const int i = tid + u * kCopyThreads, r = i / R::G, gi = i % R::G;
       if (r >= n) break;
-      const uint4* from = reinterpret_cast<const uint4*>(src + r * D + 32 * gi);
-      const bool whole = D % 32 == 0 || gi + 1 < R::G;  // else a group of 16 columns
-      uint32_t x[16];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint4 v = e < 2 || whole ? __ldg(from + e) : make_uint4(0, 0, 0, 0);
-        x[4 * e] = v.x, x[4 * e + 1] = v.y, x[4 * e + 2] = v.z, x[4 * e + 3] = v.w;
-      }
-      if (!whole) {
-#pragma unroll
-        for (int e = 8; e < 16; ++e) x[e] = x[e - 8];
-      }
-      float lo, inv;
-      const uint32_t pair = group_pair<T>(range_of<T>(x, 16), &lo, &inv);
-      uint32_t y[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] = code_word<T>(x + 4 * e, lo, inv);
-      for (int j = 0; j < cs.n; ++j) {
-        const int64_t to = (j == 0 ? row_first : target_row(j)) + r;
-        uint32_t* codes = reinterpret_cast<uint32_t*>(kv ? p.dst.pb.vc : p.dst.pb.kc) + to * R::W + 4 * gi;
-        if constexpr (D % 32 == 0) {
-          *reinterpret_cast<uint4*>(codes) = make_uint4(y[0], y[1], y[2], y[3]);
-        } else {  // rows of 40 bytes
-          *reinterpret_cast<uint2*>(codes) = make_uint2(y[0], y[1]);
-          if (whole) *reinterpret_cast<uint2*>(codes + 2) = make_uint2(y[2], y[3]);
-        }
-        (kv ? p.dst.pb.vp : p.dst.pb.kp)[to * R::G + gi] = pair;
-      }
+      uint32_t code[4];
+      const uint32_t pair = pack_group<T, D>(src + r * D, gi, code);
+      for (int j = 0; j < cs.n; ++j)
+        store_group<D>(kv ? p.dst.pb.vc : p.dst.pb.kc, kv ? p.dst.pb.vp : p.dst.pb.kp, (j == 0 ? row_first : target_row(j)) + r, gi, code, pair);
     }
   } else {
     // a lane has eight columns

@@ -16,11 +16,12 @@ namespace {
 // ---------------------------------------------------------------------------------------------
 // Append
 // ---------------------------------------------------------------------------------------------
-// A block takes (layer, group of TG tokens) units; a lane takes eight columns of a row, the four lanes of a group of
-// columns side by side.  The tokens of a unit come before the heads, so that a warp writes the rows of TG tokens, which are
-// neighbours in a stream, together.
+// A block takes (layer, group of TG tokens) units.  A lane takes a group of columns of a row (the step and its reciprocal once
+// for 32 columns), except of keys that are rotated: there eight columns, whose group's four lanes are side by side.  The
+// tokens of a unit come before the heads, so that a warp writes the rows of neighbouring tokens, which are neighbours in a
+// stream, together.
 constexpr int kPackThreads = 256;
-constexpr int kPackTokens = 4;
+constexpr int kPackTokens = 8;
 
 template <typename T, int D>
 __device__ __forceinline__ void pack_units(const Geometry& g, const Static& st, const Buffers& buf, const PackedBuffers& pb,
@@ -32,7 +33,10 @@ __device__ __forceinline__ void pack_units(const Geometry& g, const Static& st, 
   __shared__ float2 rope_cs[kPackTokens][D / 2];  // (cos, sin) of the tokens' rotated pairs
   const int H = g.H, half = g.rot / 2;
   const int64_t groups = (ntok + tg - 1) / tg, n_units = groups * n_layers;
-  const int n_items = 2 * H * tg * R::CP;
+  const int tsh = tg == 1 ? 0 : 3;
+  static_assert(kPackTokens == 8);
+  // rows of a lane a group: the values, and the keys that are not rotated
+  const int n_groups = (half > 0 ? H : 2 * H) * tg * R::G, n_items = half > 0 ? H * tg * R::CP : 0;
   for (int64_t u = blockIdx.x; u < n_units; u += gridDim.x) {
     const int l = (int)(u / groups);
     const int64_t t0 = (u - (int64_t)l * groups) * tg;
@@ -47,19 +51,31 @@ __device__ __forceinline__ void pack_units(const Geometry& g, const Static& st, 
       }
       __syncthreads();
     }
+    auto source = [&](const uint16_t* in, const TokPlan& tp, int h) { return in + (((int64_t)l * n_in + tp.in_tok) * H + h) * D; };
+    auto target = [&](const TokPlan& tp, int h) {
+      return (int64_t)(m0 + l) * H * g.C + st.seq_row0[tp.s] + (int64_t)h * st.cap[tp.s] + tp.row;
+    };
+    for (int i = threadIdx.x; i < n_groups; i += blockDim.x) {
+      const int gi = i % R::G, j = i / R::G, t = j & (tg - 1), hv = j >> tsh;
+      if (t >= nt) continue;
+      const bool is_v = hv < H;
+      const int h = is_v ? hv : hv - H;
+      const TokPlan tp = plan[t0 + t];
+      uint32_t code[4];
+      const uint32_t pair = pack_group<T, D>(source(is_v ? v_in : k_in, tp, h), gi, code);
+      store_group<D>(is_v ? pb.vc : pb.kc, is_v ? pb.vp : pb.kp, target(tp, h), gi, code, pair);
+    }
     // a multiple of 32 for every warp: the lanes of a group reduce together
     for (int i = threadIdx.x; i < (n_items + 31) / 32 * 32; i += blockDim.x) {
-      const int c = i % R::CP, j = i / R::CP, t = j % tg, hk = j / tg;
-      const bool is_v = hk >= H;
-      const int h = is_v ? hk - H : hk;
-      const bool active = hk < 2 * H && t < nt && c < R::W;
+      const int c = i % R::CP, j = i / R::CP, t = j & (tg - 1), h = j >> tsh;
+      const bool active = h < H && t < nt && c < R::W;
       const TokPlan tp = plan[t0 + min(t, nt - 1)];
       uint32_t x[4] = {0, 0, 0, 0};
       if (active) {
-        const uint16_t* src = (is_v ? v_in : k_in) + (((int64_t)l * n_in + tp.in_tok) * H + h) * D;
+        const uint16_t* src = source(k_in, tp, h);
         const uint4 a = __ldg(reinterpret_cast<const uint4*>(src + 8 * c));
         x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w;
-        if (!is_v && 8 * c < g.rot) {
+        if (8 * c < g.rot) {
           const bool first = 8 * c < half;
           const int p0 = first ? 8 * c : 8 * c - half;
           const uint4 b = __ldg(reinterpret_cast<const uint4*>(src + (first ? 8 * c + half : p0)));
@@ -76,9 +92,9 @@ __device__ __forceinline__ void pack_units(const Geometry& g, const Static& st, 
       uint32_t pair;
       const uint32_t word = pack8<T>(x, active, &pair);
       if (!active) continue;
-      const int64_t row = (int64_t)(m0 + l) * H * g.C + st.seq_row0[tp.s] + (int64_t)h * st.cap[tp.s] + tp.row;
-      reinterpret_cast<uint32_t*>(is_v ? pb.vc : pb.kc)[row * R::W + c] = word;
-      if (c % 4 == 0) (is_v ? pb.vp : pb.kp)[row * R::G + c / 4] = pair;
+      const int64_t row = target(tp, h);
+      reinterpret_cast<uint32_t*>(pb.kc)[row * R::W + c] = word;
+      if (c % 4 == 0) pb.kp[row * R::G + c / 4] = pair;
     }
     if (write_meta && l == 0 && threadIdx.x < nt) {
       const TokPlan tp = plan[t0 + threadIdx.x];

@@ -106,6 +106,43 @@ __device__ __forceinline__ uint32_t code_word(const uint32_t* w, float lo, float
   return y - (0x4B000000u + 0xB0000000u);
 }
 
+// A lane's group gi of a row of 16-bit values (16-byte aligned): its pair and its code words, of which a group of 16 columns
+// has two.
+template <typename T, int D>
+__device__ __forceinline__ uint32_t pack_group(const uint16_t* row, int gi, uint32_t (&code)[4]) {
+  const uint4* from = reinterpret_cast<const uint4*>(row + 32 * gi);
+  const bool whole = D % 32 == 0 || gi + 1 < PackedRow<D>::G;
+  uint32_t x[16];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint4 v = e < 2 || whole ? __ldg(from + e) : make_uint4(0, 0, 0, 0);
+    x[4 * e] = v.x, x[4 * e + 1] = v.y, x[4 * e + 2] = v.z, x[4 * e + 3] = v.w;
+  }
+  if (!whole) {
+#pragma unroll
+    for (int e = 8; e < 16; ++e) x[e] = x[e - 8];
+  }
+  float lo, inv;
+  const uint32_t pair = group_pair<T>(range_of<T>(x, 16), &lo, &inv);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) code[e] = code_word<T>(x + 4 * e, lo, inv);
+  return pair;
+}
+
+// Stores it as group gi of row `row` of the planes.
+template <int D>
+__device__ __forceinline__ void store_group(unsigned char* codes, uint32_t* pairs, int64_t row, int gi, const uint32_t (&code)[4], uint32_t pair) {
+  using R = PackedRow<D>;
+  uint32_t* to = reinterpret_cast<uint32_t*>(codes) + row * R::W + 4 * gi;
+  if constexpr (D % 32 == 0) {
+    *reinterpret_cast<uint4*>(to) = make_uint4(code[0], code[1], code[2], code[3]);
+  } else {  // rows of 40 bytes
+    *reinterpret_cast<uint2*>(to) = make_uint2(code[0], code[1]);
+    if (gi + 1 < R::G) *reinterpret_cast<uint2*>(to + 2) = make_uint2(code[2], code[3]);
+  }
+  pairs[row * R::G + gi] = pair;
+}
+
 // Of a lane's eight columns: the code word, and the pair of the group, whose four lanes are consecutive and call this
 // together.  A lane without columns is not `active`.
 template <typename T>
