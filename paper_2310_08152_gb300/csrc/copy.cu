@@ -16,6 +16,8 @@ namespace kvc {
 namespace {
 
 constexpr int kCopyThreads = 256;
+template <int DB>
+constexpr int kCopyRows = copy_rows(DB);
 
 // The device's view of a call's upload: in a kernel parameter or in the workspace.
 struct CopyPlan {
@@ -26,28 +28,29 @@ struct CopyPlan {
 struct CopyDev {
   Geometry g;
   CopySide src, dst;
-  int n_chunks;
+  int n_chunks, n_sources;
 };
 
 __device__ __forceinline__ int64_t stream_row0(const Geometry& g, const CopySide& c, int m, int h, int s) {
   return (int64_t)m * g.H * c.C + c.st.seq_row0[s] + (int64_t)h * c.st.cap[s];
 }
 
-// Rows a block takes: 16 KB of 16-bit rows of 64 columns.
-template <int SB, int DB>
-constexpr int kCopyRows = DB == 4 ? 256 : 128;
 
 template <typename T, int D, int SB, int DB>
 __device__ __forceinline__ void copy_block(const CopyDev& p, const CopyPlan& plan) {
   using R = PackedRow<D>;
-  constexpr int CR = kCopyRows<SB, DB>;
-  const int streams = p.g.M * 2 * p.g.H;
-  const int chunk = blockIdx.x % p.n_chunks;
-  const int rest = blockIdx.x / p.n_chunks;
-  const int sidx = rest % streams, si = rest / streams;
+  constexpr int CR = kCopyRows<DB>;
+  const int chunk = blockIdx.x % p.n_chunks, sidx = blockIdx.x / p.n_chunks;
+  int si = 0;  // the last source that begins at the chunk or before it; one without rows has none
+  for (int z = p.n_sources; z - si > 1;) {
+    const int mid = (si + z) / 2;
+    if (plan.sources[mid].chunk0 <= chunk)
+      si = mid;
+    else
+      z = mid;
+  }
   const CopySource cs = plan.sources[si];
-  const int r0 = chunk * CR;
-  if (r0 >= cs.len) return;
+  const int r0 = (chunk - cs.chunk0) * CR;
   const int n = min(CR, cs.len - r0);
   const int h = sidx % p.g.H, kv = (sidx / p.g.H) & 1, m = sidx / (2 * p.g.H);
   const int tid = threadIdx.x;
@@ -196,11 +199,8 @@ __global__ void __launch_bounds__(kCopyThreads)
 }
 
 template <typename T, int D, int SB, int DB>
-cudaError_t launch_t(const CopyDev& p0, const CopyArgs& a, cudaStream_t stream) {
-  CopyDev p = p0;
-  p.n_chunks = (int)((a.n_rows + kCopyRows<SB, DB> - 1) / kCopyRows<SB, DB>);
-  const int64_t blocks = (int64_t)a.n_sources * p.g.M * 2 * p.g.H * p.n_chunks;
-  if (blocks > INT32_MAX) return cudaErrorInvalidValue;
+cudaError_t launch_t(const CopyDev& p, const CopyArgs& a, cudaStream_t stream) {
+  const int64_t blocks = a.n_chunks * p.g.M * 2 * p.g.H;
   const char* dyn = static_cast<const char*>(a.dyn);
   if (a.img)
     copy_image_kernel<T, D, SB, DB><<<(unsigned)blocks, kCopyThreads, 0, stream>>>(
@@ -224,8 +224,8 @@ cudaError_t launch_bits(const CopyDev& p, const CopyArgs& a, cudaStream_t stream
 
 cudaError_t launch_copy(const Geometry& g, const CopyArgs& a, cudaStream_t stream, int* launched) {
   *launched = 0;
-  if (a.n_rows <= 0) return launch_drop(g, a, stream, launched);
-  const CopyDev p{g, a.src, a.dst, 0};
+  if (a.n_chunks <= 0) return launch_drop(g, a, stream, launched);
+  const CopyDev p{g, a.src, a.dst, (int)a.n_chunks, a.n_sources};
   cudaError_t e = cudaErrorInvalidValue;
   switch (g.D) {
     case 64:
@@ -253,7 +253,7 @@ cudaError_t launch_copy(const Geometry& g, const CopyArgs& a, cudaStream_t strea
 
 cudaError_t launch_drop(const Geometry& g, const CopyArgs& a, cudaStream_t stream, int* launched) {
   *launched = 0;
-  const CopyDev p{g, a.src, a.dst, 0};
+  const CopyDev p{g, a.src, a.dst, 0, 0};
   const unsigned blocks = a.dst.scores ? (unsigned)((int64_t)a.n_targets * g.M * g.H) : 1;
   if (a.img) {
     cudaLaunchConfig_t cfg = {};

@@ -3,6 +3,7 @@
 
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 
 namespace kvc {
@@ -367,10 +368,12 @@ cudaError_t launch_score_sum(const Geometry& g, const ScoreMaps& maps, const Sco
 // ---------------------------------------------------------------------------------------------
 // Copies of sequences (copy.cu)
 // ---------------------------------------------------------------------------------------------
-// A source sequence and its targets: targets[first .. first + n).
+// A source sequence and its targets: targets[first .. first + n); its rows are chunks chunk0 .. of the call's.
 struct alignas(16) CopySource {
-  int32_t s, len, first, n;
+  int32_t s, len, first, n, chunk0, pad0, pad1, pad2;
 };
+// Rows of a chunk, which a block copies: 16 KB of 16-bit rows of 64 columns, and twice as many that become 4-bit ones.
+constexpr int copy_rows(int dst_bits) { return dst_bits == 4 ? 256 : 128; }
 // A target sequence, the rows that it held before, the rows that it holds now, and the source sequence.
 struct alignas(16) CopyTarget {
   int32_t s, len_old, len, src;
@@ -388,16 +391,20 @@ struct CopySide {
   float* scores;  // or NULL
 };
 // img: the targets' upload (decode state, sources, targets) as a kernel parameter, stored at dyn, or NULL.  sources and
-// targets: offsets in that upload.  n_rows: the longest source.
+// targets: offsets in that upload.  n_chunks: of all sources.
 struct CopyArgs {
   CopySide src, dst;
   int n_sources, n_targets;
-  int64_t n_rows;
+  int64_t n_chunks;
   size_t sources, targets;
   const AppendImage* img;
   size_t img_bytes;
   void* dyn;
 };
+// The blocks that the kernels take, which have to be at most INT32_MAX.
+inline int64_t copy_blocks(const Geometry& g, const CopyArgs& a) {
+  return std::max(a.n_chunks * g.M * 2 * g.H, a.dst.scores ? (int64_t)a.n_targets * g.M * g.H : 1);
+}
 // Rows and metadata; then, where the targets' cache has scores, theirs (the source's or zero, and zero behind them).
 cudaError_t launch_copy(const Geometry& g, const CopyArgs& a, cudaStream_t stream, int* launched);
 // Stores an upload that comes as a kernel parameter, and zeroes the scores of rows [len, len_old) of the targets in it.

@@ -120,7 +120,8 @@ WsLayout ws_layout(const kvc_config& c, int64_t C) {
   L.dyn_payload = align_up(L.dyn_P + 8 * (size_t)(b + 1), 16);
   const size_t tok = sizeof(kvc::TokPlan) * (size_t)C;
   const size_t cmp = sizeof(kvc::AffSeq) * (size_t)b + 8 * (size_t)(C / 2 + 1);
-  L.dyn_bytes = L.dyn_payload + std::max(tok, cmp);
+  const size_t cpy = (sizeof(kvc::CopySource) + sizeof(kvc::CopyTarget)) * (size_t)b;
+  L.dyn_bytes = L.dyn_payload + std::max({tok, cmp, cpy});
   L.dyn = take(L.dyn_bytes);
   L.src_map = take(4 * (size_t)C);
   L.pre_counter = align_up(4 * (size_t)b * H, 16);
@@ -1749,7 +1750,7 @@ static kvc_status capturable(bool fits, cudaStream_t stream) {
   cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
   if (cudaStreamIsCapturing(stream, &status) != cudaSuccess) (void)cudaGetLastError();
   if (status == cudaStreamCaptureStatusNone) return KVC_OK;
-  return fail(KVC_ERR_STATE, "the state of so many sequences is uploaded, which a capture would not keep");
+  return fail(KVC_ERR_STATE, "the state of so many sequences goes through the staging ring, whose copy a capture would not keep");
 }
 
 kvc_status kvc_truncate(kvc_cache* c, const int64_t* tokens, void* stream_) {
@@ -1823,14 +1824,19 @@ kvc_status kvc_copy(kvc_cache* c, const kvc_cache* from, int n, const int32_t* d
       int32_t& k = slot[(size_t)src[i]];
       if (k < 0) {
         k = (int32_t)sources.size();
-        sources.push_back({src[i], (int32_t)from->bk.book.stored(src[i]), 0, 0});
+        sources.push_back({src[i], (int32_t)from->bk.book.stored(src[i]), 0, 0, 0, 0, 0, 0});
       }
       ++sources[(size_t)k].n;
     }
-    int64_t n_rows = 0;
+    // those without rows last, so that a chunk's source is the last one that begins at it or before it
+    std::stable_partition(sources.begin(), sources.end(), [](const kvc::CopySource& x) { return x.len > 0; });
+    const int chunk = kvc::copy_rows(c->packed() ? 4 : 16);
+    int64_t n_chunks = 0;
     for (size_t k = 0; k < sources.size(); ++k) {
+      slot[(size_t)sources[k].s] = (int32_t)k;
       if (k > 0) sources[k].first = sources[k - 1].first + sources[k - 1].n;
-      n_rows = std::max<int64_t>(n_rows, sources[k].len);
+      sources[k].chunk0 = (int32_t)n_chunks;
+      n_chunks += (sources[k].len + chunk - 1) / chunk;
     }
     std::vector<kvc::CopyTarget> targets((size_t)n);
     std::vector<int32_t> next(sources.size());
@@ -1843,7 +1849,8 @@ kvc_status kvc_copy(kvc_cache* c, const kvc_cache* from, int n, const int32_t* d
     a.dst = c->copy_side();
     a.n_sources = (int)sources.size();
     a.n_targets = n;
-    a.n_rows = n_rows;
+    a.n_chunks = n_chunks;
+    if (kvc::copy_blocks(c->geom(), a) > INT32_MAX) return fail(KVC_ERR_UNSUPPORTED, "a copy of so many rows takes several calls");
     a.sources = c->ws.dyn_payload;
     a.targets = a.sources + sizeof(kvc::CopySource) * sources.size();
     a.img_bytes = a.targets + sizeof(kvc::CopyTarget) * targets.size();

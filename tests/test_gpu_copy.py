@@ -71,6 +71,33 @@ def test_between_16_and_4_bits(d, dtype):
         assert float((out[:, 3] - back.decode_attention_layers(q, 0.1)[:, 3]).norm() / out[:, 3].norm()) < 2e-3
 
 
+@pytest.mark.parametrize("bits", [(16, 16), (16, 4), (4, 4), (4, 16)])
+def test_uneven_sources_and_empty_ones(bits):
+    """Runs of rows that end with a source's last row, at a block's edge and one to either side of it; sources without rows
+    among the others free their targets."""
+    lens = [0, 1500, 0, 1, 127, 128, 129, 255, 256, 257, 0, 513]
+    b = len(lens)
+    a, g, k, v = fill(2, 2, 80, lens, "bf16", bits=bits[0])
+    c, _, _, _ = fill(2, 2, 80, [3] * (2 * b), "bf16", spare=1600, bits=bits[1], seed=5)
+    order = [int(x) for x in np.random.default_rng(3).permutation(2 * b)]
+    src = [i % b for i in range(2 * b)]
+    c.copy_from(a, order, src)
+    assert [c.lengths()[0][d] for d in order] == [lens[s] for s in src]
+    for d, s in zip(order, src):
+        if lens[s] == 0:
+            continue
+        for w, x in zip("kv", (k, v)):
+            rows = tokens(x, lens, s)
+            if bits[1] == 4:
+                for got, want in zip(stored(c, d, lens[s], w), quantise(rows)):
+                    assert torch.equal(got, want), (d, s, w)
+            else:
+                want = rows if bits[0] == 16 else held(rows).float().to(rows.dtype)
+                assert torch.equal(rows_of(c, d, lens[s])["kv".index(w)], want), (d, s, w)
+        assert c.masked_reference_layout(d)["stored_pos"].tolist() == list(range(lens[s]))
+    assert c.device_status() == 0
+
+
 def test_rows_behind_the_last_stay():
     narrow, g, _, _ = fill(1, 2, 80, [40, 13, 0], "f16", spare=30)
     for t in (narrow.k, narrow.v):
