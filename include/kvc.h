@@ -188,7 +188,8 @@ typedef struct {
    *   step = (greatest - lo) / 15 rounded up to that type, or 0 where that quotient is below 2^-126,
    *   code = (x - lo) (1 / step) to the nearest whole number, ties to even (0 where step is 0),
    * with difference, quotients and product rounded to binary32; a column stands for lo + step code, which is within step / 2
-   * (1 + 2^-20) of x (where step is 0, within 15 x 2^-126).  A group that holds a NaN or an infinity, or whose range overflows, reads as NaN.
+   * (1 + 2^-20) of x (where step is 0, within 15 x 2^-126).  A group that holds a NaN or an infinity, or whose range
+   * overflows, reads as NaN.
    * Layout: the codes [M][H * C] rows of d_head / 2 bytes, column c in bits 4 (c % 2) of byte c / 2; 256-byte aligned behind
    * them the groups' pairs, [M][H * C] rows of (lo, step) pairs of `dtype`.  C and off are those of capacities rounded up to
    * multiples of 4 rows (so are pos and orig).

@@ -17,9 +17,16 @@
 //
 // The work: the tiles of 64 rows of all (layer, sequence, head) segments in a row, an equal share for each warp that fits the
 // GPU, where the beginning of a segment counts as one tile (its query, its end and its output: two thirds of one; uneven
-// sequences of 64 to 4,096 rows, whose workers on short ones were the last, 187 -> 164 us).  A warp is a worker of its own, with a ring of stages in shared memory that 1-D bulk copies fill (codes and pairs of
-// K and V, four copies a tile).  A segment that spans several workers is joined by the last of them to finish, from parts in
-// the workspace, in the workers' order.
+// sequences of 64 to 4,096 rows, where the workers on short ones were the last: 187 -> 164 us).  A warp is a worker of its
+// own, with a ring of stages in shared memory that 1-D bulk copies fill (codes and pairs of K and V).  A segment that spans
+// several workers is joined by the last of them to finish, from parts in the workspace, in the workers' order.
+//
+// What bounds it: memory at 96 and 128 columns (100,003 rows of 128, two layers of 32 heads: 155 us, 6.6 TB/s); at 64 columns
+// the instructions beside it (24 layers of 16 x 1,024 rows, 32 heads: 170 us, 5.9 TB/s; the copies alone 150, the arithmetic
+// alone about as long).  A tile of 64 columns takes some 640 instructions of a warp, 300 of them for the codes; the pipe of
+// masks and shifts is busy 55 % of the time, the tensor cores 24 %.  Tried and dropped at 64 columns: the next tile's logits
+// beside this tile's values (170 -> 175, for room for twelve workers only), 20 workers with 96 registers (185), codes by a
+// conversion from 8-bit floats (its rate is that of the masks that it would save).
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -38,19 +45,19 @@ constexpr int kTile = kPackedTile;
 template <int D>
 struct Shape {
   using R = PackedRow<D>;
-  // Workers of an SM.  Each of its four schedulers has the same number, or those with more end last: 15, 13 and 10 at 80, 96
-  // and 128 columns, which two stages of both leave room for, were 20 to 25 % slower.
+  // Workers of an SM: the same number for each of its four schedulers, or those with more end last (10 and 13, as room for two
+  // stages allowed at 128 and 96 columns, were 12 and 20 % slower).  Twelve have registers for what the compiler would like
+  // (80 columns, with 16 workers and less room each: 161 us, with 12: 155); of 64 columns 16 were faster, 172 and 178.
   static constexpr int WARPS = D == 64 ? 16 : 12;
-  // Stages of a worker: of 64 columns two for a tile's keys and values together, else, where those have no room, three for
-  // keys and values in turn.  What is read makes room for what comes S behind it.  (Of 64 columns in turn, in four: 176 -> 182
-  // us, by twice the waits; of 128, two stages of keys and one of values: 155 -> 159, as values then come late.)
+  // Stages of a worker: two for a tile's keys and values together, or, of 128 columns, where those leave room for 8 workers
+  // only (157 us, 155 so), three for keys and values in turn.  What is read makes room for what comes S behind it.
   static constexpr bool JOINT = D != 128;
   static constexpr int S = JOINT ? 2 : 3;
+  static_assert(JOINT || S % 2 == 1);
   static constexpr int KC = kTile * R::RB, KP = kTile * R::PB;
   static constexpr int HALF = KC + KP, STAGE = JOINT ? 2 * HALF : HALF;  // codes and pairs, of the keys and then of the values
   // weights times steps: [column of the operand][row of both halves of a tile] as pairs of f16, the columns 16 bytes more
   // than 128 apart, so that eight lanes' 16-byte loads meet no bank twice; the query between pieces
-  static_assert(JOINT || S % 2 == 1);
   static constexpr int PW = 36;
   static constexpr int PS = 4 * 8 * PW;
   static constexpr int RS = 8 * (D / 2);       // the rotation's cosines and sines at a sequence's position
@@ -279,9 +286,9 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
     }
   }
   if (x >= hi) return;  // a share of one that is a segment's beginning
-  // The first lanes issue copies: together K codes, K pairs, V codes and V pairs one each (a lane by itself: 170 -> 175 us of
-  // 64 columns), in turn the first lane codes and pairs (two lanes: 155 -> 156 of 128).  What they issue them from: the
-  // segment, the next tile's place, the segment's rows from that tile on, and the first of them in the planes.
+  // The first lanes issue copies: together K codes, K pairs, V codes and V pairs one each (all by one lane: 175 us instead of
+  // 171, 64 columns), in turn the first lane codes and pairs (by two: 156 instead of 155, 128 columns).  What they issue them
+  // from: the segment, the next tile's place, the segment's rows from that tile on, and the first of them in the planes.
   constexpr int kFeeders = C::JOINT ? 4 : 1;
   struct {
     Segment seg;
@@ -293,7 +300,8 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
   auto enter = [&](int first) {
     const DState d = p.ds[feed.seg.s];
     const int r0 = d.begin / kPackedRows * kPackedRows + first * kTile;
-    feed.row = (int64_t)(p.layer + feed.seg.layer) * H * g.C + st.seq_row0[feed.seg.s] + (int64_t)feed.seg.h * st.cap[feed.seg.s] + r0;
+    feed.row = (int64_t)(p.layer + feed.seg.layer) * H * g.C + st.seq_row0[feed.seg.s] +
+               (int64_t)feed.seg.h * st.cap[feed.seg.s] + r0;
     feed.rows = d.len - r0;
     if (C::JOINT) {
       const void *codes = lane & 2 ? pb.vc : pb.kc, *pairs = lane & 2 ? pb.vp : pb.kp;
