@@ -169,37 +169,13 @@ __device__ __forceinline__ void value_pair(float (&c)[4], uint32_t x01, uint32_t
   mma(c, low_codes(x01), high_codes(x01), low_codes(x23), high_codes(x23), b0, b1);
 }
 
-// A row's weight goes into the running maximum times a power of two that is not below half its largest step, so that weight
-// times step stays in f16's range whatever the steps are: the exponent of that power, as a number.  With bf16 also not below
-// 2^-20 of its least values, whose product with a weight f32 would not hold otherwise, and at least 2^-88: a weight is at most
-// 2^102, and the sum of 2^25 of them in f32's range (smaller steps' products end earlier than 2^15; below 2^-110 they lose
-// bits).  Steps that are not finite do not count.
-template <int G>
-__device__ __forceinline__ float row_exponent(const uint32_t (&pair)[G], F16T) {
-  uint32_t big = pair[0];
-#pragma unroll
-  for (int i = 1; i < G; ++i) big = max(big, pair[i]);
-  if (big >= 0x7C000000u) {
-    big = 0;
-#pragma unroll
-    for (int i = 0; i < G; ++i)
-      if (pair[i] < 0x7C000000u) big = max(big, pair[i]);
-  }
-  return __uint_as_float(0x4B000000u | big >> 26) - 8388623.f;  // 2^23 + field, less 2^23 + 15
-}
-template <int G>
-__device__ __forceinline__ float row_exponent(const uint32_t (&pair)[G], BF16T) {
-  int big = 39 << 23;
-#pragma unroll
-  for (int i = 0; i < G; ++i) {
-    const int step = (int)pair[i], least = (int)(pair[i] << 16 & 0x7FFFFFFFu) - (20 << 23);
-    if (step < 0x7F800000) big = max(big, step);
-    if (least < 0x7F800000 - (20 << 23)) big = max(big, least);
-  }
-  return __uint_as_float(0x4B000000u | (uint32_t)big >> 23) - 8388735.f;
-}
+// What a (lo, step) pair asks of f16 and f32: weights times steps have to be in the one's range, and, where lo may be far
+// larger than the step, weights times lo in the other's.
+__device__ __forceinline__ float pair_size(float2 pair, F16T) { return pair.y; }
+__device__ __forceinline__ float pair_size(float2 pair, BF16T) { return fmaxf(pair.y, fabsf(pair.x) * 9.5367431640625e-7f); }  // 2^-20
 
-// The output row of a segment from the parts of workers first to last, in their order.  Eight parts' columns are on their way
+// The output row of a segment from the parts of workers first to last, in their order: each the mean of its rows' values, by
+// their weights, and the sum of those.  Eight parts' columns are on their way
 // together (28 parts one by one: 2 us of 162).
 template <int D>
 __device__ __forceinline__ void join(const float* parts, int first, int last, float* out, int lane) {
@@ -221,12 +197,13 @@ __device__ __forceinline__ void join(const float* parts, int first, int last, fl
 #pragma unroll
       for (int j = 0; j < QL; ++j) c[i][j] = lane + 32 * j < D ? __ldcg(a + lane + 32 * j) : 0.f;
     }
-    if (m != -INFINITY) f = exp2_fast(m - big);
+    if (m != -INFINITY) f = exp2_fast(m - big) * l;
+    if (l != l) f = l;  // a logit that is NaN
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float fi = __shfl_sync(kFull, f, i), li = __shfl_sync(kFull, l, i);
-      if (w0 + i > last) continue;
-      sum = fmaf(fi, li, sum);
+      const float fi = __shfl_sync(kFull, f, i);
+      if (w0 + i > last || fi == 0.f) continue;  // a part without a weight has no mean
+      sum += fi;
 #pragma unroll
       for (int j = 0; j < QL; ++j) y[j] = fmaf(fi, c[i][j], y[j]);
     }
@@ -451,11 +428,14 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
       }
       __syncwarp();
     }
-    float o[2 * NT], l = 0.f, los[G], m = -INFINITY;
+    float o[2 * NT], l = 0.f, los[G], m = -INFINITY, unit[G];
 #pragma unroll
     for (int i = 0; i < 2 * NT; ++i) o[i] = 0.f;
 #pragma unroll
-    for (int i = 0; i < G; ++i) los[i] = 0.f;
+    for (int i = 0; i < G; ++i) {
+      los[i] = 0.f;
+      unit[i] = 1.f;
+    }
 
     int r0 = ds.begin / kPackedRows * kPackedRows + r * kTile;
     x += r1 - r;
@@ -549,7 +529,31 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
           for (int i = 0; i < G; ++i) vpair[b][i] = 0;
         }
       }
-      const float mx = warp_max(fmaxf(z[0] + row_exponent(vpair[0], T{}), z[1] + row_exponent(vpair[1], T{})));
+      // A group's pairs go by a power of two of their own, that of the largest among a piece's first rows, so that groups of
+      // different sizes have their weights times steps near 1 alike.  A row's weight then goes into the running maximum times
+      // the power of two of its largest pair (2^-60 at least: a weight is at most 2^74), so that those products stay within
+      // 2^15 whatever the later rows are.  Pairs that are NaN do not count.
+      if (m == -INFINITY) {
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+          const float big = warp_max(fmaxf(pair_size(pair_values(vpair[0][i], T{}), T{}), pair_size(pair_values(vpair[1][i], T{}), T{})));
+          const int e = big > 0.f ? max(-100, min(100, (int)(__float_as_uint(big) >> 23) - 127)) : 0;
+          unit[i] = __uint_as_float((uint32_t)(127 - e) << 23);
+        }
+      }
+      float zs[2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        float big = 8.6736174e-19f;  // 2^-60
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+          const float2 pv = pair_values(vpair[b][i], T{});
+          big = fmaxf(big, pair_size(make_float2(pv.x * unit[i], pv.y * unit[i]), T{}));
+        }
+        // its exponent, as a number: 2^23 and the field, less 2^23 and 127
+        zs[b] = z[b] + (__uint_as_float(0x4B000000u | __float_as_uint(big) >> 23) - 8388735.f);
+      }
+      const float mx = warp_max(fmaxf(zs[0], zs[1]));
       if (mx > m + 4.f) {  // the reference moves where weights times steps would pass 2^15
         const float f = exp2_fast(m - mx);
 #pragma unroll
@@ -566,8 +570,8 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
 #pragma unroll
       for (int i = 0; i < G; ++i) {
         const float2 p0 = pair_values(vpair[0][i], T{}), p1 = pair_values(vpair[1][i], T{});
-        const float x0 = e0 * p0.y, x1 = e1 * p1.y;
-        los[i] = fmaf(8.f, x0 + x1, fmaf(e0, p0.x, fmaf(e1, p1.x, los[i])));
+        const float x0 = e0 * (p0.y * unit[i]), x1 = e1 * (p1.y * unit[i]);
+        los[i] = fmaf(8.f, x0 + x1, fmaf(e0, p0.x * unit[i], fmaf(e1, p1.x * unit[i], los[i])));
         const uint32_t h = pack_halves(x0, x1);
         const float2 back = F16T::f2(h);
         pw[2 * i * C::PW + at] = h;
@@ -641,20 +645,24 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
       if (D == 128) return 16 * gr + 8 * (i / 4) + 2 * (i % 4);
       return i < 4 ? 8 * gr + 2 * i : D == 96 ? 64 + 4 * gr + 2 * (i - 4) : 64 + 2 * gr;
     };
-    float mine = los[0];  // group t's
+    float mine = los[0], scale = unit[0];  // group t's
 #pragma unroll
     for (int k = 1; k < G; ++k)
-      if (t == k) mine = los[k];
+      if (t == k) {
+        mine = los[k];
+        scale = unit[k];
+      }
+    scale = __uint_as_float((254u << 23) - __float_as_uint(scale));  // 1 / scale, a power of two
+    const float inv = 1.f / l;
 #pragma unroll
-    for (int i = 0; i < 2 * NT; ++i) o[i] += mine;
+    for (int i = 0; i < 2 * NT; ++i) o[i] = (o[i] + mine) * inv * scale;
     float* orow = p.out + (int64_t)was.layer * p.out_stride + ((int64_t)was.s * H + was.h) * D;
     if (seg0 >= lo && seg1 <= hi) {
-      const float inv = 1.f / l;
 #pragma unroll
       for (int i = 0; i < NT; ++i)
         if (t == col(i) / 32) {
-          orow[col(i)] = o[2 * i] * inv;
-          orow[col(i) + 1] = o[2 * i + 1] * inv;
+          orow[col(i)] = o[2 * i];
+          orow[col(i) + 1] = o[2 * i + 1];
         }
       continue;
     }

@@ -352,3 +352,101 @@ def test_refusals_of_a_live_cache():
         cache.decode_attention_scored(q, 0.1)
     assert e.value.status == 5  # no scores
     cache.decode_attention_layers(q, 0.1)
+
+
+@pytest.mark.parametrize("d,dtype", [(64, "f16"), (80, "bf16"), (128, "f16")])
+def test_hidden_runs_over_whole_tiles_and_workers(d, dtype):
+    """Parts without a visible row: a span that is closed and not freed covers whole tiles, and the shares of whole workers."""
+    lens = [300, 20011, 130]
+    kinds = [np.zeros(n, np.uint8) for n in lens]
+    kinds[0][1], kinds[0][290] = CL, CR
+    kinds[1][0], kinds[1][20009] = CL, CR
+    kinds[2][3], kinds[2][128] = CL, CR
+    cache, g, _, _ = fill(1, 2, d, lens, dtype, kinds=kinds)
+    q = query(cache, g)
+    got = cache.decode_attention_layers(q, 0.1)
+    for s, (n, a, z) in enumerate(zip(lens, (1, 0, 3), (290, 20009, 128))):
+        rows = [i for i in range(n) if not a <= i < z]
+        close4(got[:, s], reference(cache, s, q, n, rows, 0.1, 0), f"sequence {s}")
+    cache.compress_spans([0, 1, 2], [1, 0, 3], [290, 20009, 128])
+    again = cache.decode_attention_layers(q, 0.1)
+    close4(again, got, "freed")
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("d", [64, 96])
+def test_queries_scales_and_rows_at_the_edge(d, dtype):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(11)
+    k, v = (torch.empty(1, 200, 2, d, device="cuda").normal_(generator=g) for _ in range(2))
+    big = 6e4 if dtype == "f16" else 1e30
+    v[:, :, 1, :32] = big               # a column group that is constant and large, beside others of the usual size
+    k[:, 100:, 0, 32:] = 0.25           # constant, within a group that varies before
+    cache = kvc.KVCache(1, 2, d, [200], dtype, bits=4)
+    cache.append(k.to(TDT[dtype]), v.to(TDT[dtype]), [200], np.zeros(200, np.uint8))
+    q = torch.empty(1, 1, 2, d, dtype=TDT[dtype], device="cuda").normal_(generator=g)
+    for scale in (0.1, -0.1, 0.0, 1e-30):
+        got = cache.decode_attention_layers(q, scale)
+        ref = reference(cache, 0, q, 200, range(200), scale, 0)
+        for h in range(2):
+            for a in range(0, d, 32):
+                close4(got[:, 0, h, a:a + 32], ref[:, h, a:a + 32], f"scale {scale} head {h} columns {a}")
+    close4(cache.decode_attention_layers(torch.zeros_like(q), 0.1)[:, 0], reference(cache, 0, q * 0, 200, range(200), 0.1, 0), "zero query")
+    # logits of thousands: one row has all the weight (its neighbours in the order are far below it)
+    z = torch.einsum("hd,hnd->hn", q[0, 0].double().cpu(), values(*stored(cache, 0, 200))[0])
+    top = z.topk(2).values
+    scale = 2000.0 / float((top[:, 0] - top[:, 1]).min())
+    got = cache.decode_attention_layers(q, scale)[0, 0]
+    rows = values(*stored(cache, 0, 200, "v"))[0]
+    for h in range(2):
+        close4(got[h], rows[h, int(z[h].argmax())], f"head {h}")
+
+
+@pytest.mark.parametrize("d", [64, 80, 128])
+def test_steps_back_to_back(d):
+    """Steps whose calls follow each other at once give what they give one by one: append, decode, a drafted token taken back,
+    another's decode, sequences replaced."""
+    def run(wait):
+        cache, g, _, _ = fill(3, 4, d, [200, 64, 333, 1], "f16", spare=200, rot=16, seed=4)
+        outs = []
+        for i in range(60):
+            x, y = (torch.empty(3, 4, 4, d, dtype=torch.float16, device="cuda").normal_(generator=g) for _ in range(2))
+            q = query(cache, g)
+            calls = [lambda: cache.append(x, y, [1] * 4, np.zeros(4, np.uint8)), lambda: outs.append(cache.decode_attention_layers(q, 0.1)),
+                     lambda: outs.append(cache.decode_attention_layers(q, 0.2))]
+            if i % 3 == 0:
+                back = cache.lengths()[0].copy()
+                calls.append(lambda: cache.truncate(back))
+                calls.append(lambda: outs.append(cache.decode_attention_layers(q, 0.1)))
+            if i % 7 == 0:
+                calls.append(lambda: cache.copy_from(cache, [3], [1]))
+                calls.append(lambda: outs.append(cache.decode_attention_layers(q, 0.1)))
+            for call in calls:
+                call()
+                if wait:
+                    torch.cuda.synchronize()
+        assert cache.device_status() == 0
+        return outs
+
+    for a, b in zip(run(False), run(True)):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype,sizes", [("f16", [1e4, 1e-3, 1.0, 30.0]), ("bf16", [1e20, 1e-20, 1.0, 1e-3])])
+@pytest.mark.parametrize("d", [64, 80, 128])
+def test_groups_of_different_sizes(d, dtype, sizes):
+    """Each group of the output's columns to its own size, though the values' groups differ by many powers of two, and so in one
+    part of a long sequence as in another."""
+    n = 5003
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    k, v = (torch.empty(1, n, 2, d, device="cuda").normal_(generator=g) for _ in range(2))
+    for i, a in enumerate(range(0, d, 32)):
+        v[..., a:a + 32] *= sizes[i]
+    cache = kvc.KVCache(1, 2, d, [n], dtype, bits=4)
+    cache.append(k.to(TDT[dtype]), v.to(TDT[dtype]), [n], np.zeros(n, np.uint8))
+    q = torch.empty(1, 1, 2, d, dtype=TDT[dtype], device="cuda").normal_(0, 2, generator=g)
+    got = cache.decode_attention_layers(q, 0.125)
+    ref = reference(cache, 0, q, n, range(n), 0.125, 0)
+    for a in range(0, d, 32):
+        close4(got[:, 0, :, a:a + 32], ref[:, :, a:a + 32], f"columns {a}")
