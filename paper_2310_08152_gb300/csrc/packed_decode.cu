@@ -22,11 +22,12 @@
 // several workers is joined by the last of them to finish, from parts in the workspace, in the workers' order.
 //
 // What bounds it: memory at 96 and 128 columns (100,003 rows of 128, two layers of 32 heads: 155 us, 6.6 TB/s); at 64 columns
-// the instructions beside it (24 layers of 16 x 1,024 rows, 32 heads: 170 us, 5.9 TB/s; the copies alone 150, the arithmetic
+// the instructions beside it (24 layers of 16 x 1,024 rows, 32 heads: 166 us, 6.1 TB/s; the copies alone 150, the arithmetic
 // alone about as long).  A tile of 64 columns takes some 640 instructions of a warp, 300 of them for the codes; the pipe of
-// masks and shifts is busy 55 % of the time, the tensor cores 24 %.  Tried and dropped at 64 columns: the next tile's logits
-// beside this tile's values (170 -> 175, for room for twelve workers only), 20 workers with 96 registers (185), codes by a
-// conversion from 8-bit floats (its rate is that of the masks that it would save).
+// masks and shifts is busy 55 % of the time, the tensor cores 24 %.  Tried and dropped, at 64 columns: the next tile's logits
+// beside this tile's values (170 -> 175, as that leaves room for twelve workers only), 20 workers with 96 registers (185),
+// codes by a conversion from 8-bit floats (its rate is that of the masks that it would save), all that a worker's first tile
+// depends on in one round of loads (no change).
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -47,7 +48,7 @@ struct Shape {
   using R = PackedRow<D>;
   // Workers of an SM: the same number for each of its four schedulers, or those with more end last (10 and 13, as room for two
   // stages allowed at 128 and 96 columns, were 12 and 20 % slower).  Twelve have registers for what the compiler would like
-  // (80 columns, with 16 workers and less room each: 161 us, with 12: 155); of 64 columns 16 were faster, 172 and 178.
+  // (80 columns, with 16 workers and less room each: 161 us, with 12: 155 then); of 64 columns 16 were faster, 172 and 178.
   static constexpr int WARPS = D == 64 ? 16 : 12;
   // Stages of a worker: two for a tile's keys and values together, or, of 128 columns, where those leave room for 8 workers
   // only (157 us, 155 so), three for keys and values in turn.  What is read makes room for what comes S behind it.
