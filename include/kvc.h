@@ -397,7 +397,8 @@ kvc_status kvc_decode_attention_shared(kvc_cache* cache, int first, int n_layers
  * `from`, or 0 where it has none.  Prefixes (kvc_set_prefix) stay as they are set for dst; src's own rows alone are copied.
  * The call is ordered behind earlier work on both caches by the caller, as later work on `from` behind it.
  * Errors: KVC_ERR_CAPACITY where a target cannot hold its source's rows; KVC_ERR_STATE with layers of the last tokens of
- * either cache not written; KVC_ERR_UNSUPPORTED under KVC_POLICY_LOCAL. */
+ * either cache not written, or with the caches on different devices; KVC_ERR_UNSUPPORTED under KVC_POLICY_LOCAL, or for more
+ * than 2^31 runs of 128 rows (256 to 4 bits) of a layer and head. */
 kvc_status kvc_copy(kvc_cache* cache, const kvc_cache* from, int n, const int32_t* dst, const int32_t* src, void* stream);
 
 /* Cuts sequence s back to the first tokens[s] tokens of its history (host [b]; below 0: the sequence stays as it is), as
@@ -407,7 +408,7 @@ kvc_status kvc_copy(kvc_cache* cache, const kvc_cache* from, int n, const int32_
  * a cut inside a span that was freed (its tokens' rows are gone), or before the tokens that an eviction left rows of their
  * own; KVC_ERR_UNSUPPORTED for a cut above 0 under KVC_POLICY_LOCAL.
  * kvc_copy and kvc_truncate on a stream that is captured: a replay repeats the device's part, not the bookkeeping; they are
- * KVC_ERR_STATE there where the state of the cache's sequences (about 40 bytes each, 16 to 32 more for each that changes)
+ * KVC_ERR_STATE there where the state of the cache's sequences (about 40 bytes each, 16 to 48 more for each that changes)
  * exceeds the 3,584 bytes of a kernel parameter. */
 kvc_status kvc_truncate(kvc_cache* cache, const int64_t* tokens, void* stream);
 

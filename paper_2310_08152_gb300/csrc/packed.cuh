@@ -4,7 +4,7 @@
 // both in the cache's 16-bit type: the step is a fifteenth of the group's range, rounded up to that type (0 below 2^-126,
 // where its reciprocal would not be finite).  Column x has the code rint((x - lo) / step), from 0 to 15, with the product
 // by 1 / step in binary32, and stands for lo + step * code.  Rounding the step up keeps the group's largest value within
-// half a step of code 15; a group that holds a NaN or an infinity has a step of NaN and reads as NaN.
+// half a step of code 15; a group that holds a NaN or an infinity has a step and a least value of NaN.
 //
 // A row's codes are D / 8 words, word w the columns 8 w .. 8 w + 7 from its low bits up; its (lo, step) pairs are a word a
 // group, the step in the high half.  Codes and pairs are planes of their own, in the layout of the rows.
@@ -67,10 +67,11 @@ __device__ __forceinline__ uint32_t range_of(const uint32_t* w, int n) {
 // A group's (lo, step) pair from its range, lo, and 1 / step (0 where the step is 0).
 template <typename T>
 __device__ __forceinline__ uint32_t group_pair(uint32_t range, float* lo, float* inv) {
-  const uint32_t lo16 = range & 0xFFFFu;
+  uint32_t lo16 = range & 0xFFFFu;
   *lo = T::f1((uint16_t)lo16);
   float s = __fdiv_rn(__fsub_rn(T::f1((uint16_t)(range >> 16 ^ 0x8000u)), *lo), 15.f);
   s = fmaf(s, 0.f, s);  // NaN where it is not finite
+  if (s != s) lo16 = 0x7FFFu;
   if (s < 1.17549435e-38f) s = 0.f;
   const uint32_t s16 = round_up16(s, T{});
   const float step = T::f1((uint16_t)s16);

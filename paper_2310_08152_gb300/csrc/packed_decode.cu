@@ -531,14 +531,15 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
         }
       }
       // A group's pairs go by a power of two of their own, that of the largest among a piece's first rows, so that groups of
-      // different sizes have their weights times steps near 1 alike.  A row's weight then goes into the running maximum times
+      // different sizes have their weights times steps near 1 alike (2^-60 to 2^100: later values of 2^67 are still finite in
+      // it).  A row's weight then goes into the running maximum times
       // the power of two of its largest pair (2^-60 at least: a weight is at most 2^74), so that those products stay within
       // 2^15 whatever the later rows are.  Pairs that are NaN do not count.
       if (m == -INFINITY) {
 #pragma unroll
         for (int i = 0; i < G; ++i) {
           const float big = warp_max(fmaxf(pair_size(pair_values(vpair[0][i], T{}), T{}), pair_size(pair_values(vpair[1][i], T{}), T{})));
-          const int e = big > 0.f ? max(-100, min(100, (int)(__float_as_uint(big) >> 23) - 127)) : 0;
+          const int e = big > 0.f ? max(-60, min(100, (int)(__float_as_uint(big) >> 23) - 127)) : 0;
           unit[i] = __uint_as_float((uint32_t)(127 - e) << 23);
         }
       }
@@ -688,6 +689,7 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
       if (done) __threadfence();
     }
     if (!__shfl_sync(kFull, done, 0)) continue;
+    __syncwarp();
     join<D>(p.parts, first, last, orow, lane);
     if (lane == 0) p.counters[first] = 0;
   }

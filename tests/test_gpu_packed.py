@@ -255,19 +255,20 @@ def test_values_of_every_size(d, dtype):
 
 
 @pytest.mark.parametrize("d", [64, 80, 128])
-def test_values_that_are_not_finite(d):
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_values_that_are_not_finite(d, dtype):
     """A query that is not finite gets NaN; a NaN among the keys' groups makes its logit NaN; among the values its columns;
     none reaches a query that does not see the row."""
     lens = [100, 100, 100, 100, 100]
     kinds = [np.zeros(n, np.uint8) for n in lens]
     kinds[4][60] = CL
-    cache = kvc.KVCache(1, 2, d, [100] * 5, "f16", bits=4)
-    k, v = (torch.randn(1, 500, 2, d, device="cuda").half() for _ in range(2))
+    cache = kvc.KVCache(1, 2, d, [100] * 5, dtype, bits=4)
+    k, v = (torch.randn(1, 500, 2, d, device="cuda").to(TDT[dtype]) for _ in range(2))
     k[:, 150, 0, 3] = math.nan
-    v[:, 250, 1, 40] = math.inf
+    v[:, 250, 1, 40] = -math.inf
     k[:, 460], v[:, 460] = math.nan, math.inf  # the hidden <CL> row
     cache.append(k, v, lens, np.concatenate(kinds))
-    q = torch.randn(1, 5, 2, d, device="cuda").half()
+    q = torch.randn(1, 5, 2, d, device="cuda").to(TDT[dtype])
     q[0, 3, 0, 7] = math.inf
     out = cache.decode_attention_layers(q, 0.125)[0]
     nan = torch.isnan(out).cpu()
@@ -275,6 +276,9 @@ def test_values_that_are_not_finite(d):
     want[1, 0] = want[3, 0] = True
     want[2, 1, 32:64] = True
     assert torch.equal(nan, want)
+    k2, v2 = (values(*stored(cache, 2, 100, w))[0, 1:] for w in "kv")  # the other columns beside those that are NaN
+    rest = [c for c in range(d) if not 32 <= c < 64]
+    close4(out[2, 1:, rest], attend(q[0, 2, 1:].double().cpu(), k2, v2, range(100), 0.125)[0][:, rest], "beside")
     rows = [i for i in range(100) if i != 60]
     close4(out[4], reference(cache, 4, q, 100, rows, 0.125, 0)[0], "hidden row")
     close4(out[0], reference(cache, 0, q, 100, range(100), 0.125, 0)[0], "plain")
