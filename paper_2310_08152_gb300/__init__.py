@@ -509,8 +509,13 @@ def kvc_last_decode_plan(cache: int) -> dict:
     return {"mode": int(a[0]), "workers": int(a[1]), "tile_rows": int(a[2]), "stages": int(a[3])}
 
 
+_FEW = 256  # tokens whose counts, kinds and positions go through a cache's own arrays
+
+
 class KVCache:
     """A sentinel-compressed KV cache: owns its device buffers (torch) and the library handle."""
+
+    _few = None
 
     def __init__(self, M: int, H: int, d_head: int, capacity, dtype: str = "f16", rotary_dim: int = 0,
                  rope_base: float = 10000.0, policy: int = POLICY_PAPER, device=None, local_ratio: float = 0.0,
@@ -573,6 +578,8 @@ class KVCache:
         self._budget_at = self._budget.ctypes.data
         self._pairs = np.zeros((2, self.b), np.int32)  # copy_from's
         self._pairs_at = self._pairs.ctypes.data
+        few = np.zeros(self.b, np.int32), np.zeros(_FEW, np.uint8), np.zeros(_FEW, np.int32)  # append's: counts, kinds, positions
+        self._few = (*few, [a.ctypes.data for a in few])
 
     # views of the device layout (rows of d_head elements)
     def k_plane(self, layer: int):
@@ -598,7 +605,7 @@ class KVCache:
         n_new = _np(n_new, np.int32)
         kinds = _np(kinds, np.uint8)
         tied = layer <= 0 and pos is None
-        N = int(np.add.reduce(n_new, axis=None))
+        N = sum(n_new.tolist()) if n_new.ndim == 1 and n_new.size <= 64 else int(np.add.reduce(n_new, axis=None))
         n = (self.M if layer < 0 else 1) * N * self.H * self.d
         try:
             _dev(k, "k", self.torch_dtype, n)
@@ -607,6 +614,14 @@ class KVCache:
             if tied:
                 self.book.next_positions(n_new, kinds)  # its errors come first
             raise
+        if tied and N <= _FEW and self._few is not None and n_new.shape == (self.b,) and kinds.shape == (N,):
+            # a few tokens: through arrays that are kept (with three new ones an append and a cut of a token of each
+            # of two sequences took 22 us of the host, so 13 to 15)
+            new, kept, out, at = self._few
+            new[:], kept[:N] = n_new, kinds
+            _check(lib().kvc_append_tied(self.handle, layer, k.data_ptr(), v.data_ptr(), at[0], at[1], at[2],
+                                         1 if free_closed else 0, _stream_handle(stream)))
+            return out[:N].copy()
         if tied:
             pos = np.empty(max(N, 1), np.int32)
             kvc_append_tied(self.handle, layer, k, v, n_new, kinds, pos, free_closed, stream)

@@ -36,7 +36,6 @@ __device__ __forceinline__ int64_t stream_row0(const Geometry& g, const CopySide
   return (int64_t)m * g.H * c.C + c.st.seq_row0[s] + (int64_t)h * c.st.cap[s];
 }
 
-
 template <typename T, int D, int SB, int DB>
 __device__ __forceinline__ void copy_block(const CopyDev& p, const CopyPlan& plan) {
   using R = PackedRow<D>;
