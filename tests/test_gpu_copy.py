@@ -5,7 +5,7 @@ import torch
 
 import paper_2310_08152_gb300 as kvc
 from _packed import CL, CR, close4, fill, held, quantise, stored, tokens, unpack16
-from _serving import TDT, collected, make, per_row, query, rows_of  # noqa: F401
+from _serving import TDT, attend, close, collected, make, per_row, query, rows_of  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -274,6 +274,85 @@ def test_streams_and_graphs():
             assert e.value.status == 5
     assert many.lengths()[0].tolist() == [2] * 200
     many.truncate(1)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_prefixes_copied_and_cut(d):
+    """Copies and cuts of a shared prefix and of the sequences over it: each decode is over the rows that are there then."""
+    prefix, _ = make(2, 3, d, [300, 40], spare=300)
+    parent, own = [0, 0, 1, -1], [3, 1, 2, 5]
+    pos = np.concatenate([(0 if p < 0 else 40) + np.arange(n) for p, n in zip(parent, own)]).astype(np.int32)
+    cache, g = make(2, 3, d, own, seed=1, spare=9, pos=pos)
+    cache.set_prefix(prefix, parent)
+
+    def check(plen, own):
+        q = query(cache, g)
+        out = cache.decode_attention_shared(q, 0.1)
+        assert prefix.lengths()[0].tolist() == plen and cache.lengths()[0].tolist() == own
+        for s, (p, n) in enumerate(zip(parent, own)):
+            k, v = rows_of(cache, s, n)
+            if p >= 0:
+                k, v = (torch.cat(x, 2) for x in zip(rows_of(prefix, p, plen[p]), (k, v)))
+            for m in range(2):
+                close(out[m, s], attend(q[m, s].double(), k[m], v[m], list(range(k.shape[2])), 0.1)[0], f"sequence {s}")
+
+    check([300, 40], own)
+    prefix.truncate([130, -1])
+    check([130, 40], own)
+    prefix.copy_from(prefix, [1], [0])
+    check([130, 130], own)
+    other, _ = make(2, 3, d, [257, 3], seed=2)
+    prefix.copy_from(other, [0, 1], [1, 0])
+    check([3, 257], own)
+    cache.copy_from(cache, [2, 3], [0, 1])  # own rows alone: sequence 2 stays over prefix 1, sequence 3 over none
+    check([3, 257], [3, 1, 3, 1])
+    cache.truncate([1, -1, 2, -1])
+    check([3, 257], [1, 1, 2, 1])
+    prefix.truncate([0, -1])
+    check([0, 257], [1, 1, 2, 1])
+    for c in (prefix, cache):
+        assert c.device_status() == 0
+
+
+def test_prompts_after_copies_and_cuts():
+    """A block's attention and scores are over the rows that are there, though an earlier call had as many queries."""
+    lens, n_q = [200, 90, 30], [20, 7, 11]
+    a, g = make(2, 4, 64, lens, spare=200)
+    k, v = (torch.empty(2, 38, 4, 64, device="cuda", dtype=torch.float16).normal_(generator=g) for _ in range(2))
+    q = torch.empty(38, 4, 64, device="cuda", dtype=torch.float16).normal_(0.0, 2.0, generator=g)
+    scores = a.attach_scores()
+
+    def block():
+        a.append(k, v, n_q, np.zeros(38, np.uint8))
+        out = a.prefill_attention(0, q, n_q, 0.1)
+        scores.zero_()
+        a.score_prompt(0, q, n_q, 0.1)
+        return out
+
+    def check(out, before):
+        t = 0
+        for s, (n, m) in enumerate(zip(before, n_q)):
+            rows = [x[0] for x in rows_of(a, s, n + m)]
+            total = torch.zeros(4, n + m, dtype=torch.float64, device="cuda")
+            for i in range(m):
+                ref, w = attend(q[t + i].double(), *rows, list(range(n + i + 1)), 0.1)
+                # a weight that the tensor cores take is rounded to 16 bits: by 2^-11 = 4.9e-4 of itself at most, and so at
+                # most are the outputs and their sums; the logits in 32 bits add 1.2e-4
+                assert float((out[t + i].double() - ref).norm() / ref.norm()) < 2e-3
+                total[:, :n + i + 1] += w
+            got = per_row(a, scores, s, n + m)[0].double()
+            assert float((got - total).norm() / total.norm()) < 2e-3
+            t += m
+
+    check(block(), lens)
+    a.truncate([150, 90, 0])
+    check(block(), [150, 90, 0])
+    a.copy_from(a, [0], [1])
+    check(block(), [97, 97, 11])
+    a.copy_from(a, [2], [0])
+    a.truncate([3, -1, 60])
+    check(block(), [3, 104, 60])
+    assert a.device_status() == 0
 
 
 def test_refusals_leave_the_cache():
