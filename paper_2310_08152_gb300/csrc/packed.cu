@@ -30,7 +30,8 @@ __device__ __forceinline__ void pack_units(const Geometry& g, const Static& st, 
                                            int write_meta, const uint16_t* __restrict__ k_in,
                                            const uint16_t* __restrict__ v_in) {
   using R = PackedRow<D>;
-  pdl_launch_dependents();  // a decode's workers may start, and wait for this kernel before they read anything
+  // A decode's workers may start: they wait for this kernel before they read anything or let what follows them start.
+  pdl_launch_dependents();
   __shared__ float2 rope_cs[kPackTokens][D / 2];  // (cos, sin) of the tokens' rotated pairs
   const int H = g.H, half = g.rot / 2;
   const int64_t groups = (ntok + tg - 1) / tg, n_units = groups * n_layers;

@@ -228,7 +228,9 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
   // that a lane and its neighbour have all of a row's sums); with more, both parts of group t.
   constexpr bool kTwice = G == 2;
   extern __shared__ __align__(128) unsigned char smem[];
-  pdl_launch_dependents();
+  // What comes next may be a decode that reads rows and state ahead of its own wait, which covers this kernel but not the ones
+  // before it: it may start once those are complete, as they are behind a decode (kv_before_wait), or have been waited for.
+  if (p.kv_before_wait) pdl_launch_dependents();
   const int lane = threadIdx.x, gr = lane >> 2, t = lane & 3, tg = t < G ? t : G - 1;
   const int wid = blockIdx.x, H = g.H;
   const int lo = wid * p.share + min(wid, p.extra), hi = lo + p.share + (wid < p.extra ? 1 : 0);
@@ -244,7 +246,10 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
   }
   fence_proxy_async_smem();
   __syncwarp();
-  if (!p.kv_before_wait) pdl_wait();
+  if (!p.kv_before_wait) {
+    pdl_wait();
+    pdl_launch_dependents();
+  }
 
   Segment cs;  // of the consumed tiles
   int r;       // the next one in it
@@ -309,8 +314,8 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
       enter(0);
     }
   };
-  // a decode before this one writes neither rows nor state: they may come before it is complete, while the query, the outputs
-  // and the parts may be shared with it
+  // a decode before this one writes neither rows nor state, and did not let this one start before what wrote them was complete:
+  // they may come before it is complete, while the query, the outputs and the parts may be shared with it
   if (lane < kFeeders) {
     enter(r);
     for (int i = 0; i < C::S && feed.x < hi; ++i) issue(i, C::JOINT || i % 2 == 0);
