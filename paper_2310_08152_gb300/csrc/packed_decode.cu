@@ -146,6 +146,11 @@ __device__ __forceinline__ float exp2_fast(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+__device__ __forceinline__ float log2_fast(float x) {
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 __device__ __forceinline__ float warp_max(float x) {  // of the numbers among them
   float y;
   asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
@@ -170,10 +175,17 @@ __device__ __forceinline__ void value_pair(float (&c)[4], uint32_t x01, uint32_t
   mma(c, low_codes(x01), high_codes(x01), low_codes(x23), high_codes(x23), b0, b1);
 }
 
-// What a (lo, step) pair asks of f16 and f32: weights times steps have to be in the one's range, and, where lo may be far
-// larger than the step, weights times lo in the other's.
+// The size of a (lo, step) pair: weights times steps have to be in f16's range, and, where lo may be far larger than the step,
+// weights times lo in f32's.  And the greatest power of two that a group's sizes are taken times, 2^kMostUnit: with weights of
+// 2^14 at most, products by any lo then stay finite.
 __device__ __forceinline__ float pair_size(float2 pair, F16T) { return pair.y; }
 __device__ __forceinline__ float pair_size(float2 pair, BF16T) { return fmaxf(pair.y, fabsf(pair.x) * 9.5367431640625e-7f); }  // 2^-20
+template <typename T>
+constexpr float kMostUnit = std::is_same_v<T, F16T> ? 60.f : 110.f;
+
+// The exponent of a number that is not negative; -127 of one below 2^-126.
+__device__ __forceinline__ float exponent_of(float x) { return (float)((int)(__float_as_uint(x) >> 23) - 127); }
+__device__ __forceinline__ float power_of_two(float e) { return __uint_as_float((uint32_t)(127 + (int)e) << 23); }  // -126 <= e
 
 // The output row of a segment from the parts of workers first to last, in their order: each the mean of its rows' values, by
 // their weights, and the sum of those.  Eight parts' columns are on their way
@@ -440,7 +452,7 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
 #pragma unroll
     for (int i = 0; i < G; ++i) {
       los[i] = 0.f;
-      unit[i] = 1.f;
+      unit[i] = power_of_two(kMostUnit<T>);
     }
 
     int r0 = ds.begin / kPackedRows * kPackedRows + r * kTile;
@@ -535,40 +547,38 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
           for (int i = 0; i < G; ++i) vpair[b][i] = 0;
         }
       }
-      // A group's pairs go by a power of two of their own, that of the largest among a piece's first rows, so that groups of
-      // different sizes have their weights times steps near 1 alike (2^-60 to 2^100: later values of 2^67 are still finite in
-      // it).  A row's weight then goes into the running maximum times
-      // the power of two of its largest pair (2^-60 at least: a weight is at most 2^74), so that those products stay within
-      // 2^15 whatever the later rows are.  Pairs that are NaN do not count.
-      if (m == -INFINITY) {
-#pragma unroll
-        for (int i = 0; i < G; ++i) {
-          const float big = warp_max(fmaxf(pair_size(pair_values(vpair[0][i], T{}), T{}), pair_size(pair_values(vpair[1][i], T{}), T{})));
-          const int e = big > 0.f ? max(-60, min(100, (int)(__float_as_uint(big) >> 23) - 127)) : 0;
-          unit[i] = __uint_as_float((uint32_t)(127 - e) << 23);
-        }
-      }
+      // A row's weight is 2^(10 - m) times what it would be without a reference, m a whole number that the logits do not pass by
+      // more than 4.  Each group's sums go by a power of two of their own besides, unit[i], so that the largest product of a
+      // weight and a pair's size among the rows so far is some 2^10 whatever the groups' sizes are and however they change along
+      // the rows: unit[i] falls where a row's product would pass 2^14, and rises as m does, which makes the weights of the rows
+      // before smaller.  (Taken from a piece's first rows alone, it left weights of 2^-40 beside pairs that became 2^40 times
+      // as large: no bits of the other groups.)  A group without a size yet has the greatest one.  Pairs that are NaN do not
+      // count.
       float zs[2];
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        float big = 8.6736174e-19f;  // 2^-60
+        float big = 1.f;
+#pragma unroll
+        for (int i = 0; i < G; ++i) big = fmaxf(big, pair_size(pair_values(vpair[b][i], T{}), T{}) * unit[i]);
+        zs[b] = z[b] + log2_fast(big);
+      }
+      if (warp_max(fmaxf(zs[0], zs[1])) > m + 4.f) {
+        const float m_new = fmaxf(m, ceilf(warp_max(fmaxf(z[0], z[1])))), up = m_new - m;
+        float f = 1.f;  // group t's
 #pragma unroll
         for (int i = 0; i < G; ++i) {
-          const float2 pv = pair_values(vpair[b][i], T{});
-          big = fmaxf(big, pair_size(make_float2(pv.x * unit[i], pv.y * unit[i]), T{}));
+          const float s0 = pair_size(pair_values(vpair[0][i], T{}), T{}), s1 = pair_size(pair_values(vpair[1][i], T{}), T{});
+          const float most = ceilf(warp_max(fmaxf(z[0] + exponent_of(s0), z[1] + exponent_of(s1))));
+          const float was = exponent_of(unit[i]), now = fmaxf(fminf(fminf(was + up, kMostUnit<T>), m_new - most), -126.f);
+          const float fi = exp2_fast(now - was - up);
+          unit[i] = power_of_two(now);
+          los[i] *= fi;
+          if (t == i) f = fi;
         }
-        // its exponent, as a number: 2^23 and the field, less 2^23 and 127
-        zs[b] = z[b] + (__uint_as_float(0x4B000000u | __float_as_uint(big) >> 23) - 8388735.f);
-      }
-      const float mx = warp_max(fmaxf(zs[0], zs[1]));
-      if (mx > m + 4.f) {  // the reference moves where weights times steps would pass 2^15
-        const float f = exp2_fast(m - mx);
 #pragma unroll
         for (int i = 0; i < 2 * NT; ++i) o[i] *= f;
-#pragma unroll
-        for (int i = 0; i < G; ++i) los[i] *= f;
-        l *= f;
-        m = mx;
+        l *= exp2_fast(-up);
+        m = m_new;
       }
       const float ref = m == -INFINITY ? 10.f : 10.f - m;
       const float e0 = exp2_fast(z[0] + ref), e1 = exp2_fast(z[1] + ref);
@@ -577,8 +587,8 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
 #pragma unroll
       for (int i = 0; i < G; ++i) {
         const float2 p0 = pair_values(vpair[0][i], T{}), p1 = pair_values(vpair[1][i], T{});
-        const float x0 = e0 * (p0.y * unit[i]), x1 = e1 * (p1.y * unit[i]);
-        los[i] = fmaf(8.f, x0 + x1, fmaf(e0, p0.x * unit[i], fmaf(e1, p1.x * unit[i], los[i])));
+        const float w0 = e0 * unit[i], w1 = e1 * unit[i], x0 = w0 * p0.y, x1 = w1 * p1.y;
+        los[i] = fmaf(8.f, x0 + x1, fmaf(w0, p0.x, fmaf(w1, p1.x, los[i])));
         const uint32_t h = pack_halves(x0, x1);
         const float2 back = F16T::f2(h);
         pw[2 * i * C::PW + at] = h;
