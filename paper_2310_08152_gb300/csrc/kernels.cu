@@ -103,8 +103,8 @@ __device__ __forceinline__ void append_units(const Geometry& g, const Static& st
       for (int e = 0; e < 8; ++e) {
         const float2 r = rope_cs[vec * 8 + e];
         const float x1 = T::f1(xa[e]), x2 = T::f1(xb[e]);
-        pa[e] = T::r(x1 * r.x - x2 * r.y);
-        pb[e] = T::r(x2 * r.x + x1 * r.y);
+        pa[e] = T::r(turned_first(x1, x2, r));
+        pb[e] = T::r(turned_second(x1, x2, r));
       }
       *reinterpret_cast<uint4*>(dst + vec * 8) = ya;
       *reinterpret_cast<uint4*>(dst + (vec + hv) * 8) = yb;
@@ -249,8 +249,8 @@ __global__ void __launch_bounds__(32, 1) append_tma_kernel(Geometry g, Static st
         for (int e = 0; e < 8; ++e) {
           const float2 r = cs[vec * 8 + e];
           const float x1 = T::f1(xa[e]), x2 = T::f1(xb[e]);
-          pa[e] = T::r(x1 * r.x - x2 * r.y);
-          pb[e] = T::r(x2 * r.x + x1 * r.y);
+          pa[e] = T::r(turned_first(x1, x2, r));
+          pb[e] = T::r(turned_second(x1, x2, r));
         }
         *qa = ya;
         *qb = yb;

@@ -88,8 +88,8 @@ __device__ __forceinline__ void pack_units(const Geometry& g, const Static& st, 
           for (int e = 0; e < 4; ++e) {
             const float2 f = T::f2(x[e]), o = T::f2(bv[e]);
             const float2 r0 = rope_cs[t][p0 + 2 * e], r1 = rope_cs[t][p0 + 2 * e + 1];
-            x[e] = T::r2(first ? f.x * r0.x - o.x * r0.y : f.x * r0.x + o.x * r0.y,
-                         first ? f.y * r1.x - o.y * r1.y : f.y * r1.x + o.y * r1.y);
+            x[e] = first ? T::r2(turned_first(f.x, o.x, r0), turned_first(f.y, o.y, r1))
+                         : T::r2(turned_second(o.x, f.x, r0), turned_second(o.y, f.y, r1));
           }
         }
       }
