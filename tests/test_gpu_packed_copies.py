@@ -41,3 +41,31 @@ def test_rotated_keys_are_those_of_the_16_bit_cache(d, rot, dtype):
         for which in "kv":
             for a, b, name in zip(stored(narrow, s, int(n), which), stored(copy, s, int(n), which), ("codes", "steps", "least values")):
                 assert torch.equal(a, b), (s, which, name, int((a != b).sum()))
+
+
+@pytest.mark.parametrize("bits", [(16, 4), (4, 16), (16, 16)])
+def test_a_source_that_ends_while_its_copy_is_queued(bits):
+    """On another stream: the source is dropped as soon as the call has returned, and what is made next may get its memory."""
+    M, H, d, n = 8, 16, 64, 3000
+    side = torch.cuda.Stream()
+
+    def copied(drop):
+        g = torch.Generator(device="cuda")
+        g.manual_seed(1)
+        x = [torch.empty(M, n, H, d, dtype=torch.float16, device="cuda").normal_(generator=g) for _ in range(2)]
+        source = kvc.KVCache(M, H, d, [n], bits=bits[0])
+        target = kvc.KVCache(M, H, d, [n], bits=bits[1])
+        source.append(*x, [n], np.zeros(n, np.uint8))
+        torch.cuda.synchronize()
+        sizes = [t.numel() * t.element_size() for t in (source.k, source.v, source.pos, source.orig)]
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(20_000_000)  # some 10 ms
+        target.copy_from(source, [0], [0], stream=side)
+        if drop:
+            del source
+            over = [torch.zeros(m, dtype=torch.uint8, device="cuda") for m in sizes]
+        torch.cuda.synchronize()
+        return target.k.view(torch.uint8).clone(), target.v.view(torch.uint8).clone(), target.pos.clone(), target.orig.clone()
+
+    for a, b in zip(copied(True), copied(False)):
+        assert torch.equal(a, b)
