@@ -393,8 +393,8 @@ kvc_status kvc_decode_attention_shared(kvc_cache* cache, int first, int n_layers
  *   dst, src: host [n]; a target occurs once and, within one cache, is no source of the same call.
  * The caches agree in M, H, d_head, dtype, rotation and policy; capacities, batch and bits differ as they like.  From 16 to
  * 4 bits the rows are quantised as an append does it (kvc_config.bits), from 4 to 16 they become the values that they stand
- * for, rounded to dtype; between equal bits they are copied as they are.  Where `cache` has scores, the rows get those of
- * `from`, or 0 where it has none.  Prefixes (kvc_set_prefix) stay as they are set for dst; src's own rows alone are copied.
+ * for, rounded to dtype, to its largest finite value where they are past it; between equal bits they are copied as they are.
+ * Where `cache` has scores, the rows get those of `from`, or 0 where it has none.  Prefixes (kvc_set_prefix) stay as they are set for dst; src's own rows alone are copied.
  * The call is ordered behind earlier work on both caches by the caller, as later work on `from` behind it.
  * Errors: KVC_ERR_CAPACITY where a target cannot hold its source's rows; KVC_ERR_STATE with layers of the last tokens of
  * either cache not written, or with the caches on different devices; KVC_ERR_UNSUPPORTED under KVC_POLICY_LOCAL, or for more

@@ -36,6 +36,19 @@ __device__ __forceinline__ int64_t stream_row0(const Geometry& g, const CopySide
   return (int64_t)m * g.H * c.C + c.st.seq_row0[s] + (int64_t)h * c.st.cap[s];
 }
 
+// Two values rounded to 16 bits, to the type's largest one where they are past it: a step that was rounded up may take a group's
+// greatest value there.  A NaN stays one.
+__device__ __forceinline__ uint32_t finite2(float lo, float hi, F16T) {
+  uint32_t y;
+  asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(y) : "f"(hi), "f"(lo));
+  return y;
+}
+__device__ __forceinline__ uint32_t finite2(float lo, float hi, BF16T) {
+  uint32_t y;
+  asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(y) : "f"(hi), "f"(lo));
+  return y;
+}
+
 template <typename T, int D, int SB, int DB>
 __device__ __forceinline__ void copy_block(const CopyDev& p, const CopyPlan& plan) {
   using R = PackedRow<D>;
@@ -133,7 +146,7 @@ __device__ __forceinline__ void copy_block(const CopyDev& p, const CopyPlan& pla
       const float2 pv = pair_values(y[u], T{});
       const float2 a = code_values(x[u], 0, pv), b = code_values(x[u], 1, pv);
       const float2 c = code_values(x[u], 2, pv), d = code_values(x[u], 3, pv);
-      o[u] = make_uint4(T::r2(a.x, b.x), T::r2(c.x, d.x), T::r2(a.y, b.y), T::r2(c.y, d.y));
+      o[u] = make_uint4(finite2(a.x, b.x, T{}), finite2(c.x, d.x, T{}), finite2(a.y, b.y, T{}), finite2(c.y, d.y, T{}));
     }
     for (int j = 0; j < cs.n; ++j) {
       uint4* dst = reinterpret_cast<uint4*>((kv ? p.dst.v : p.dst.k) + target_row(j) * D);

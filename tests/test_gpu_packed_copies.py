@@ -1,13 +1,51 @@
-"""What copies between caches of 16 and 4 bits make of rotated keys, and of a source that ends."""
+"""What copies between caches of 16 and 4 bits make of rows at the types' ends, of rotated keys, and of a source that ends."""
 import numpy as np
 import pytest
 import torch
 
 import paper_2310_08152_gb300 as kvc
-from _packed import stored
-from _serving import TDT, collected  # noqa: F401
+from _packed import stored, unpack16, values
+from _serving import TDT, collected, rows_of  # noqa: F401
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("d", [64, 80, 96, 128])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_finite_rows_come_back_finite(d, dtype):
+    """A step that is rounded up puts a group's greatest value past the type's largest, by half a step at most."""
+    t = TDT[dtype]
+    top = torch.finfo(t).max
+    n, H = 300, 2
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    x = torch.empty(1, n, H, d, device="cuda").normal_(generator=g).to(t)
+    low = -1.0 if dtype == "f16" else -0.5  # in bf16 a range of 1.5 x 3.39e38, which binary32 does not hold: NaN by definition
+    x[0, 0:40, :, 3], x[0, 0:40, :, 7] = top, 0.0
+    x[0, 40:80, :, 33:64:2], x[0, 40:80, :, 34:64:2] = top, low * top
+    x[0, 80:120] = top
+    x[0, 120:160, :, ::3] = torch.linspace(0.3, 1.0, 40, device="cuda")[:, None, None].to(t) * top
+    x[0, 160:200, :, 5] = -top
+    x[0, 210:250, :, :32] = torch.linspace(0.0, 0.9, 40, device="cuda")[:, None, None].to(t) * top  # steps of all kinds
+    x[0, 210:250, :, 3] = top
+    x[0, 200, 0, 3] = float("nan")
+    x[0, 201, 1, 40] = float("inf")
+    cache = kvc.KVCache(1, H, d, [n], dtype, bits=4)
+    cache.append(x, x, [n], np.zeros(n, np.uint8))
+    held = values(*stored(cache, 0, n))[0]
+    assert (held[torch.isfinite(held)].abs() > top).any()  # the case is there
+    back = [y[0].cpu() for y in rows_of(unpack16(cache), 0, n)]
+    want = held.clamp(max=top).to(t)  # a NaN stays one
+    nans = 64 + (0 if dtype == "f16" else 40 * H * 32)  # two groups that are not finite, and 40 rows' of too large a range
+    for y in back:
+        nan = torch.isnan(want)
+        assert torch.equal(torch.isnan(y), nan) and nan.sum() == nans
+        assert torch.equal(y[~nan], want[~nan])
+    # and a row that has been there and back stays within a step's rounding of itself
+    again = kvc.KVCache(1, H, d, [n], dtype, bits=4)
+    again.copy_from(unpack16(cache), [0], [0])
+    rows = [i for i in range(n) if i not in (200, 201) and (dtype == "f16" or not 40 <= i < 80)]
+    assert torch.isfinite(values(*stored(again, 0, n))[0][:, rows]).all()
 
 
 @pytest.mark.parametrize("d,rot", [(64, 64), (64, 16), (80, 80), (80, 48), (96, 96), (128, 128), (128, 32)])
