@@ -405,8 +405,8 @@ kvc_status kvc_copy(kvc_cache* cache, const kvc_cache* from, int n, const int32_
  * where drafted tokens are not accepted; 0 frees the sequence, which begins anew with its next append.  The next query is
  * the last token that is left; a span whose <CR> goes is open again.  Scores of rows that go become 0.
  * Errors: KVC_ERR_INVALID_ARG for more tokens than there are; KVC_ERR_STATE with layers of the last tokens not written, for
- * a cut inside a span that was freed (its tokens' rows are gone), or before the tokens that an eviction left rows of their
- * own; KVC_ERR_UNSUPPORTED for a cut above 0 under KVC_POLICY_LOCAL.
+ * a cut inside a span that was freed (its tokens' rows are gone), from right behind its <CL>, which KVC_POLICY_KEEP_CL keeps,
+ * to its <CR>, or before the tokens that an eviction left rows of their own; KVC_ERR_UNSUPPORTED for a cut above 0 under KVC_POLICY_LOCAL.
  * kvc_copy and kvc_truncate on a stream that is captured: a replay repeats the device's part, not the bookkeeping; they are
  * KVC_ERR_STATE there where the state of the cache's sequences (about 40 bytes each, 16 to 48 more for each that changes)
  * exceeds the 3,584 bytes of a kernel parameter. */
