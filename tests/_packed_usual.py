@@ -8,8 +8,8 @@ With q and k of deviation 1 and scale 1 / sqrt(d), in the base-2 exponent of a w
 A weight's exponential is off by 2^-22 at most (1e-7 root mean square), a weight times a step, in two 16-bit parts, by 2^-23, and a
 sum of a thousand of those loses about as much again as its two halves, of lo + 8 step and of c - 8, are some five times what is
 left of them: 5 x 2^-24 = 3e-7.  All of these are independent from row to row, as what they are multiplied by is, so an output is
-off by their root mean square, 5e-7 of its norm.  USUAL is eight times that, for norms of a few dozen columns, and grows with the
-logits where those are larger."""
+off by their root mean square, 5e-7 of its norm.  USUAL is eight times that, for norms of a few dozen columns; it grows with the
+logits where those are larger, and past a thousand rows with their root, as what is left of the two halves falls by it."""
 from __future__ import annotations
 
 import torch
@@ -28,7 +28,7 @@ def expected(cache, s, q, n, scale, rows=None, pos=0):
 
 
 def close_usual(got, ref, what="", deviation=1.0):
-    """deviation: of the logits."""
+    """deviation: what the bound grows by, of the logits or the root of thousands of rows."""
     got, ref = got.double().cpu(), ref.double().cpu()
     assert got.shape == ref.shape, (what, got.shape, ref.shape)
     assert torch.isfinite(got).all(), f"{what}: not finite"
