@@ -14,7 +14,7 @@ INCLUDE = os.path.join(ROOT, "include")
 GENCODE = "arch=compute_103a,code=sm_103a"
 SOURCES = ["kvc.cpp", "book.cpp", "kernels.cu", "prefill.cu", "evict.cu", "prefix.cu", "prefix_tc.cu", "score.cu",
            "packed.cu", "packed_decode.cu", "copy.cu"]
-HEADERS = [os.path.join(CSRC, h) for h in ("book.hpp", "kernels.hpp", "device_common.cuh", "tensor_core.cuh", "packed.cuh")] + [os.path.join(INCLUDE, "kvc.h")]
+HEADERS = [os.path.join(CSRC, h) for h in ("book.hpp", "kernels.hpp", "device_common.cuh", "tensor_core.cuh", "packed.cuh", "turned_keys.cuh")] + [os.path.join(INCLUDE, "kvc.h")]
 
 
 def _flags(verbose_ptx: bool = False):

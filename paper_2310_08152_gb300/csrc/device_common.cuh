@@ -62,12 +62,6 @@ __device__ __forceinline__ void rope_sincos_full(int32_t pos, float2 g, float* s
   sincospif(2.f * rope_turns(pos, g), s, c);
 }
 
-// A key's columns x1 and x2, half a rotation apart, turned by (cos, sin) of their angle.  Each product and sum is spelled out,
-// as a compiler that fuses either product with the sum would round the keys of one kernel unlike another's: the same tokens have
-// to give the same rows in every append, and the same codes from an append to 4 bits as from a copy of the 16-bit rows.
-__device__ __forceinline__ float turned_first(float x1, float x2, float2 cs) { return __fmaf_rn(x1, cs.x, -__fmul_rn(x2, cs.y)); }
-__device__ __forceinline__ float turned_second(float x1, float x2, float2 cs) { return __fmaf_rn(x1, cs.y, __fmul_rn(x2, cs.x)); }
-
 // Two 32-bit values as a sum of packed 16-bit parts: the first rounds them, each later one rounds what is left, which
 // binary32 holds exactly.  Two parts of f16 hold 22 bits of a value, three of bf16 all 24.
 template <typename T>

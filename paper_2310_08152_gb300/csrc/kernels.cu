@@ -29,6 +29,7 @@
 
 #include "device_common.cuh"
 #include "kernels.hpp"
+#include "turned_keys.cuh"
 
 namespace kvc {
 namespace {

@@ -9,6 +9,7 @@
 
 #include "kernels.hpp"
 #include "packed.cuh"
+#include "turned_keys.cuh"
 
 namespace kvc {
 namespace {
