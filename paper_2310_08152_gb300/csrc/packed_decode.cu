@@ -36,6 +36,7 @@
 
 #include "kernels.hpp"
 #include "packed.cuh"
+#include "tensor_core.cuh"
 
 namespace kvc {
 namespace {
@@ -141,12 +142,7 @@ __device__ __forceinline__ uint32_t high_codes(uint32_t w) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ float log2_fast(float x) {
+__device__ __forceinline__ float lg2(float x) {
   float y;
   asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
@@ -210,7 +206,7 @@ __device__ __forceinline__ void join(const float* parts, int first, int last, fl
 #pragma unroll
       for (int j = 0; j < QL; ++j) c[i][j] = lane + 32 * j < D ? __ldcg(a + lane + 32 * j) : 0.f;
     }
-    if (m != -INFINITY) f = exp2_fast(m - big) * l;
+    if (m != -INFINITY) f = ex2(m - big) * l;
     if (l != l) f = l;  // a logit that is NaN
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -560,7 +556,7 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
         float big = 1.f;
 #pragma unroll
         for (int i = 0; i < G; ++i) big = fmaxf(big, pair_size(pair_values(vpair[b][i], T{}), T{}) * unit[i]);
-        zs[b] = z[b] + log2_fast(big);
+        zs[b] = z[b] + lg2(big);
       }
       if (warp_max(fmaxf(zs[0], zs[1])) > m + 4.f) {
         const float m_new = fmaxf(m, ceilf(warp_max(fmaxf(z[0], z[1])))), up = m_new - m;
@@ -570,18 +566,18 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
           const float s0 = pair_size(pair_values(vpair[0][i], T{}), T{}), s1 = pair_size(pair_values(vpair[1][i], T{}), T{});
           const float most = ceilf(warp_max(fmaxf(z[0] + exponent_of(s0), z[1] + exponent_of(s1))));
           const float was = exponent_of(unit[i]), now = fmaxf(fminf(fminf(was + up, kMostUnit<T>), m_new - most), -126.f);
-          const float fi = exp2_fast(now - was - up);
+          const float fi = ex2(now - was - up);
           unit[i] = power_of_two(now);
           los[i] *= fi;
           if (t == i) f = fi;
         }
 #pragma unroll
         for (int i = 0; i < 2 * NT; ++i) o[i] *= f;
-        l *= exp2_fast(-up);
+        l *= ex2(-up);
         m = m_new;
       }
       const float ref = m == -INFINITY ? 10.f : 10.f - m;
-      const float e0 = exp2_fast(z[0] + ref), e1 = exp2_fast(z[1] + ref);
+      const float e0 = ex2(z[0] + ref), e1 = ex2(z[1] + ref);
       l += e0 + e1;
       const int at = 8 * (gr & 3) + 2 * t + (gr >> 2);  // of row i = gr + 8 t of the halves: 8 (i % 4) + i / 4
 #pragma unroll
