@@ -184,43 +184,56 @@ __device__ __forceinline__ float exponent_of(float x) { return (float)((int)(__f
 __device__ __forceinline__ float power_of_two(float e) { return __uint_as_float((uint32_t)(127 + (int)e) << 23); }  // -126 <= e
 
 // The output row of a segment from the parts of workers first to last, in their order: each the mean of its rows' values, by
-// their weights, and the sum of those.  Eight parts' columns are on their way
-// together (28 parts one by one: 2 us of 162).
+// their weights, and the sum of those.  The means come times their share of all weights, which keeps the sum in range wherever
+// the output is (weights and their sums go up to 2^34).  Eight parts' columns are on their way together (28 parts one by one:
+// 2 us of 162).
 template <int D>
 __device__ __forceinline__ void join(const float* parts, int first, int last, float* out, int lane) {
   constexpr int QL = (D + 31) / 32;
   auto from = [&](int w) { return parts + ((int64_t)w * 2 + (w == first ? 1 : 0)) * (D + 4); };
-  float big = -INFINITY;
-  for (int w = first + lane; w <= last; w += 32) big = fmaxf(big, __ldcg(from(w)));
-  big = warp_max(big);
-  float sum = 0.f, y[QL];
+  float big = -INFINITY, sum = 0.f;  // of the lane's parts, then of all
+  for (int w = first + lane; w <= last; w += 32) {
+    const float2 ml = __ldcg(reinterpret_cast<const float2*>(from(w)));
+    const float to = fmaxf(big, ml.x);
+    if (to != -INFINITY) {
+      sum = sum * ex2(big - to) + ml.y * ex2(ml.x - to);
+      big = to;
+    } else {
+      sum += ml.y;  // 0, or a logit that is NaN
+    }
+  }
+  {
+    const float to = warp_max(big);
+    if (big != -INFINITY) sum *= ex2(big - to);
+    big = to;
+  }
 #pragma unroll
-  for (int j = 0; j < QL; ++j) y[j] = 0.f;
+  for (int i = 16; i > 0; i >>= 1) sum += __shfl_xor_sync(kFull, sum, i);
+  const float inv = 1.f / sum;
+  float y[QL];
+#pragma unroll
+  for (int j = 0; j < QL; ++j) y[j] = sum > 0.f ? 0.f : NAN;
   for (int w0 = first; w0 <= last; w0 += 8) {
     float f = 0.f, c[8][QL];
-    const float* mine = from(min(w0 + (lane & 7), last));
-    const float m = __ldcg(mine), l = __ldcg(mine + 1);
+    const float2 ml = __ldcg(reinterpret_cast<const float2*>(from(min(w0 + (lane & 7), last))));
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float* a = from(min(w0 + i, last)) + 4;
 #pragma unroll
       for (int j = 0; j < QL; ++j) c[i][j] = lane + 32 * j < D ? __ldcg(a + lane + 32 * j) : 0.f;
     }
-    if (m != -INFINITY) f = ex2(m - big) * l;
-    if (l != l) f = l;  // a logit that is NaN
+    if (ml.x != -INFINITY) f = ex2(ml.x - big) * ml.y * inv;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float fi = __shfl_sync(kFull, f, i);
       if (w0 + i > last || fi == 0.f) continue;  // a part without a weight has no mean
-      sum += fi;
 #pragma unroll
       for (int j = 0; j < QL; ++j) y[j] = fmaf(fi, c[i][j], y[j]);
     }
   }
-  const float inv = 1.f / sum;
 #pragma unroll
   for (int j = 0; j < QL; ++j)
-    if (lane + 32 * j < D) out[lane + 32 * j] = y[j] * inv;
+    if (lane + 32 * j < D) out[lane + 32 * j] = y[j];
 }
 
 template <typename T, int D>

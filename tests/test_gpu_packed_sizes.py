@@ -113,3 +113,13 @@ def test_a_row_with_nearly_all_the_weight_has_none_of_a_group(d, dtype, at, H):
     # the one row's logit is 40, with magnitudes that are added of some eight times that
     close_groups(got[:, 0], expected(cache, 0, q, n, scale), deviation=40.0)
     assert cache.device_status() == 0
+
+
+@pytest.mark.parametrize("d", [64, 80, 96, 128])
+@pytest.mark.parametrize("size", [1e33, 4e36, 3e37])
+@pytest.mark.parametrize("n,segments", [(1024, ONE), (1024, MANY), (20011, ONE)])
+def test_values_near_the_largest(d, size, n, segments):
+    """Outputs far below the largest 32-bit number, times weights that are not."""
+    if n > 2000 and d in (80, 96):
+        pytest.skip("the longer sequence at the least and the greatest width")
+    decode(torch.full((n, groups(d)), size), d, "bf16", segments, deviation=max(1.0, math.sqrt(n / 1000)))
