@@ -173,7 +173,8 @@ __device__ __forceinline__ void value_pair(float (&c)[4], uint32_t x01, uint32_t
 
 // The size of a (lo, step) pair: weights times steps have to be in f16's range, and, where lo may be far larger than the step,
 // weights times lo in f32's.  And the greatest power of two that a group's sizes are taken times, 2^kMostUnit: with weights of
-// 2^14 at most, products by any lo then stay finite.
+// 2^14 at most, products by any lo then stay finite.  (A group whose weights times sizes are all below some 2^-72, in bf16
+// 2^-122, where the largest weight is 1, has fewer bits than others.)
 __device__ __forceinline__ float pair_size(float2 pair, F16T) { return pair.y; }
 __device__ __forceinline__ float pair_size(float2 pair, BF16T) { return fmaxf(pair.y, fabsf(pair.x) * 9.5367431640625e-7f); }  // 2^-20
 template <typename T>
@@ -406,32 +407,33 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
           const float2 cs2 = rope[k < half ? k : k - half];
           qa[j] = k < half ? qa[j] * cs2.x - qb[j] * cs2.y : qa[j] * cs2.x + qb[j] * cs2.y;
         }
-        sum[j] = qa[j];
         big = fmaxf(big, fabsf(qa[j]));
       }
       big = warp_max(big);
+      // the largest column goes to [2^13, 2^14): it and a second part are then far from f16's ends, and sums from f32's
+      const int e = big > 0.f && big < INFINITY ? max(-115, min(115, 13 - (int)(__float_as_uint(big) >> 23) + 127)) : 0;
+      const float up = __uint_as_float((uint32_t)(127 + e) << 23);
+      kscale = p.qscale * __uint_as_float((uint32_t)(127 - e) << 23);
+#pragma unroll
+      for (int j = 0; j < QL; ++j) sum[j] = qa[j] *= up;
 #pragma unroll
       for (int i = 16; i > 0; i >>= 1) {
 #pragma unroll
         for (int j = 0; j < QL; ++j) sum[j] += __shfl_xor_sync(kFull, sum[j], i);
       }
-      // the largest column goes to [2^13, 2^14): it and a second part are then far from f16's ends
-      const int e = big > 0.f && big < INFINITY ? max(-115, min(115, 13 - (int)(__float_as_uint(big) >> 23) + 127)) : 0;
-      const float up = __uint_as_float((uint32_t)(127 + e) << 23);
-      kscale = p.qscale * __uint_as_float((uint32_t)(127 - e) << 23);
       qsum[0] = qsum[1] = 0.f;
 #pragma unroll
       for (int j = 0; j < QL; ++j) {
         if (kTwice)
-          qsum[j & 1] = sum[j] * p.qscale;
+          qsum[j & 1] = sum[j] * kscale;
         else if (t == j)
-          qsum[0] = sum[j] * p.qscale;
+          qsum[0] = sum[j] * kscale;
       }
       __syncwarp();  // the weights of the piece before are read
 #pragma unroll
       for (int j = 0; j < QL; ++j) {  // both parts of a column side by side
-        const float y = qa[j] * up, h = __half2float(__float2half_rn(y));
-        if (lane + 32 * j < D) pw[lane + 32 * j] = pack_halves(h, y - h);
+        const float h = __half2float(__float2half_rn(qa[j]));
+        if (lane + 32 * j < D) pw[lane + 32 * j] = pack_halves(h, qa[j] - h);
       }
       __syncwarp();
       const int col_group = kTwice ? gr & 1 : gr >> 1;

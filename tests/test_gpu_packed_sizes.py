@@ -123,3 +123,21 @@ def test_values_near_the_largest(d, size, n, segments):
     if n > 2000 and d in (80, 96):
         pytest.skip("the longer sequence at the least and the greatest width")
     decode(torch.full((n, groups(d)), size), d, "bf16", segments, deviation=max(1.0, math.sqrt(n / 1000)))
+
+
+@pytest.mark.parametrize("d", [64, 80, 96, 128])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_queries_near_the_largest(d, sign):
+    """Columns whose sum is past the largest 32-bit number; the logits are not."""
+    n, H = 500, 2
+    g = torch.Generator(device="cuda")
+    g.manual_seed(13)
+    k, v = (torch.empty(1, n, H, d, device="cuda").normal_(generator=g).bfloat16() for _ in range(2))
+    cache = kvc.KVCache(1, H, d, [n], "bf16", bits=4)
+    cache.append(k, v, [n], np.zeros(n, np.uint8))
+    q = torch.full((1, 1, H, d), sign * 2e37, dtype=torch.bfloat16, device="cuda")
+    scale = float(np.float32(1.6e-37 / d))
+    got = cache.decode_attention_layers(q, scale)
+    # a group's sum of the query is 32 columns of 3.2 / d each, where usual ones leave sqrt(32 / d)
+    close_groups(got[:, 0], expected(cache, 0, q, n, scale), deviation=32 * 3.2 / d / math.sqrt(32 / d))
+    assert cache.device_status() == 0
