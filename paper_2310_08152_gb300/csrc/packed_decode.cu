@@ -411,7 +411,9 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
       }
       big = warp_max(big);
       // the largest column goes to [2^13, 2^14): it and a second part are then far from f16's ends, and sums from f32's
-      const int e = big > 0.f && big < INFINITY ? max(-115, min(115, 13 - (int)(__float_as_uint(big) >> 23) + 127)) : 0;
+      // (less where the scale is so small that the products' would lose bits below 2^-126)
+      const int most = min(115, (int)(__float_as_uint(p.qscale) >> 23 & 255) - 2);
+      const int e = big > 0.f && big < INFINITY ? max(-115, min(most, 13 - (int)(__float_as_uint(big) >> 23) + 127)) : 0;
       const float up = __uint_as_float((uint32_t)(127 + e) << 23);
       kscale = p.qscale * __uint_as_float((uint32_t)(127 - e) << 23);
 #pragma unroll

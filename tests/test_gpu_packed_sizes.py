@@ -141,3 +141,19 @@ def test_queries_near_the_largest(d, sign):
     # a group's sum of the query is 32 columns of 3.2 / d each, where usual ones leave sqrt(32 / d)
     close_groups(got[:, 0], expected(cache, 0, q, n, scale), deviation=32 * 3.2 / d / math.sqrt(32 / d))
     assert cache.device_status() == 0
+
+
+@pytest.mark.parametrize("d", [64, 80, 96, 128])
+@pytest.mark.parametrize("size,q_size", [(3e36, 1.0), (1e37, 1e-2), (1e30, 1e-5)])
+def test_large_keys_and_a_small_scale(d, size, q_size):
+    n, H = 500, 2
+    g = torch.Generator(device="cuda")
+    g.manual_seed(14)
+    k, v = (torch.empty(1, n, H, d, device="cuda").normal_(generator=g) for _ in range(2))
+    cache = kvc.KVCache(1, H, d, [n], "bf16", bits=4)
+    cache.append((k * size).bfloat16(), v.bfloat16(), [n], np.zeros(n, np.uint8))
+    q = (torch.empty(1, 1, H, d, device="cuda").normal_(generator=g) * q_size).bfloat16()
+    scale = float(np.float32(1 / math.sqrt(d) / size / q_size))
+    got = cache.decode_attention_layers(q, scale)
+    close_groups(got[:, 0], expected(cache, 0, q, n, scale))
+    assert cache.device_status() == 0
