@@ -142,11 +142,6 @@ __device__ __forceinline__ uint32_t high_codes(uint32_t w) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-__device__ __forceinline__ float lg2(float x) {
-  float y;
-  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 __device__ __forceinline__ float warp_max(float x) {  // of the numbers among them
   float y;
   asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
@@ -180,40 +175,31 @@ __device__ __forceinline__ float pair_size(float2 pair, BF16T) { return fmaxf(pa
 template <typename T>
 constexpr float kMostUnit = std::is_same_v<T, F16T> ? 60.f : 110.f;
 
+// What a query's columns are added up times: 32 of bf16's largest are past f32's.
+template <typename T>
+constexpr float kQueryShare = std::is_same_v<T, F16T> ? 1.f : 0.015625f;
+
 // The exponent of a number that is not negative; -127 of one below 2^-126.
 __device__ __forceinline__ float exponent_of(float x) { return (float)((int)(__float_as_uint(x) >> 23) - 127); }
 __device__ __forceinline__ float power_of_two(float e) { return __uint_as_float((uint32_t)(127 + (int)e) << 23); }  // -126 <= e
 
 // The output row of a segment from the parts of workers first to last, in their order: each the mean of its rows' values, by
-// their weights, and the sum of those.  The means come times their share of all weights, which keeps the sum in range wherever
-// the output is (weights and their sums go up to 2^34).  Eight parts' columns are on their way together (28 parts one by one:
-// 2 us of 162).
+// their weights, and the sum of those.  The means come times 2^-12 of the largest sum at most, so that what is added up stays in
+// range wherever the output is.  Eight parts' columns are on their way together (28 parts one by one: 2 us of 162).
 template <int D>
 __device__ __forceinline__ void join(const float* parts, int first, int last, float* out, int lane) {
   constexpr int QL = (D + 31) / 32;
+  static_assert(kMaxPackedWorkers <= 1 << 12);
   auto from = [&](int w) { return parts + ((int64_t)w * 2 + (w == first ? 1 : 0)) * (D + 4); };
-  float big = -INFINITY, sum = 0.f;  // of the lane's parts, then of all
+  float big = -INFINITY;
   for (int w = first + lane; w <= last; w += 32) {
     const float2 ml = __ldcg(reinterpret_cast<const float2*>(from(w)));
-    const float to = fmaxf(big, ml.x);
-    if (to != -INFINITY) {
-      sum = sum * ex2(big - to) + ml.y * ex2(ml.x - to);
-      big = to;
-    } else {
-      sum += ml.y;  // 0, or a logit that is NaN
-    }
+    big = fmaxf(big, ml.x + exponent_of(ml.y));
   }
-  {
-    const float to = warp_max(big);
-    if (big != -INFINITY) sum *= ex2(big - to);
-    big = to;
-  }
+  big = warp_max(big) + 13.f;
+  float sum = 0.f, y[QL];
 #pragma unroll
-  for (int i = 16; i > 0; i >>= 1) sum += __shfl_xor_sync(kFull, sum, i);
-  const float inv = 1.f / sum;
-  float y[QL];
-#pragma unroll
-  for (int j = 0; j < QL; ++j) y[j] = sum > 0.f ? 0.f : NAN;
+  for (int j = 0; j < QL; ++j) y[j] = 0.f;
   for (int w0 = first; w0 <= last; w0 += 8) {
     float f = 0.f, c[8][QL];
     const float2 ml = __ldcg(reinterpret_cast<const float2*>(from(min(w0 + (lane & 7), last))));
@@ -223,18 +209,21 @@ __device__ __forceinline__ void join(const float* parts, int first, int last, fl
 #pragma unroll
       for (int j = 0; j < QL; ++j) c[i][j] = lane + 32 * j < D ? __ldcg(a + lane + 32 * j) : 0.f;
     }
-    if (ml.x != -INFINITY) f = ex2(ml.x - big) * ml.y * inv;
+    if (ml.x != -INFINITY) f = ex2(ml.x - big) * ml.y;
+    if (ml.y != ml.y) f = ml.y;  // a logit that is NaN
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float fi = __shfl_sync(kFull, f, i);
       if (w0 + i > last || fi == 0.f) continue;  // a part without a weight has no mean
+      sum += fi;
 #pragma unroll
       for (int j = 0; j < QL; ++j) y[j] = fmaf(fi, c[i][j], y[j]);
     }
   }
+  const float inv = 1.f / sum;
 #pragma unroll
   for (int j = 0; j < QL; ++j)
-    if (lane + 32 * j < D) out[lane + 32 * j] = y[j];
+    if (lane + 32 * j < D) out[lane + 32 * j] = y[j] * inv;
 }
 
 template <typename T, int D>
@@ -407,35 +396,35 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
           const float2 cs2 = rope[k < half ? k : k - half];
           qa[j] = k < half ? qa[j] * cs2.x - qb[j] * cs2.y : qa[j] * cs2.x + qb[j] * cs2.y;
         }
+        sum[j] = qa[j] * kQueryShare<T>;
         big = fmaxf(big, fabsf(qa[j]));
       }
       big = warp_max(big);
-      // the largest column goes to [2^13, 2^14): it and a second part are then far from f16's ends, and sums from f32's
-      // (less where the scale is so small that the products' would lose bits below 2^-126)
-      const int most = min(115, (int)(__float_as_uint(p.qscale) >> 23 & 255) - 2);
-      const int e = big > 0.f && big < INFINITY ? max(-115, min(most, 13 - (int)(__float_as_uint(big) >> 23) + 127)) : 0;
-      const float up = __uint_as_float((uint32_t)(127 + e) << 23);
-      kscale = p.qscale * __uint_as_float((uint32_t)(127 - e) << 23);
-#pragma unroll
-      for (int j = 0; j < QL; ++j) sum[j] = qa[j] *= up;
 #pragma unroll
       for (int i = 16; i > 0; i >>= 1) {
 #pragma unroll
         for (int j = 0; j < QL; ++j) sum[j] += __shfl_xor_sync(kFull, sum[j], i);
       }
+      // the largest column goes to [2^13, 2^14): it and a second part are then far from f16's ends
+      // (less where the scale is so small that the products' would lose bits below 2^-126)
+      const int most = min(115, (int)(__float_as_uint(p.qscale) >> 23 & 255) - 2);
+      const int e = big > 0.f && big < INFINITY ? max(-115, min(most, 13 - (int)(__float_as_uint(big) >> 23) + 127)) : 0;
+      const float up = __uint_as_float((uint32_t)(127 + e) << 23);
+      kscale = p.qscale * __uint_as_float((uint32_t)(127 - e) << 23);
+      const float sum_scale = p.qscale * (1.f / kQueryShare<T>);
       qsum[0] = qsum[1] = 0.f;
 #pragma unroll
       for (int j = 0; j < QL; ++j) {
         if (kTwice)
-          qsum[j & 1] = sum[j] * kscale;
+          qsum[j & 1] = sum[j] * sum_scale;
         else if (t == j)
-          qsum[0] = sum[j] * kscale;
+          qsum[0] = sum[j] * sum_scale;
       }
       __syncwarp();  // the weights of the piece before are read
 #pragma unroll
       for (int j = 0; j < QL; ++j) {  // both parts of a column side by side
-        const float h = __half2float(__float2half_rn(qa[j]));
-        if (lane + 32 * j < D) pw[lane + 32 * j] = pack_halves(h, qa[j] - h);
+        const float y = qa[j] * up, h = __half2float(__float2half_rn(y));
+        if (lane + 32 * j < D) pw[lane + 32 * j] = pack_halves(h, y - h);
       }
       __syncwarp();
       const int col_group = kTwice ? gr & 1 : gr >> 1;
@@ -567,22 +556,34 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
       // before smaller.  (Taken from a piece's first rows alone, it left weights of 2^-40 beside pairs that became 2^40 times
       // as large: no bits of the other groups.)  A group without a size yet has the greatest one.  Pairs that are NaN do not
       // count.
-      float zs[2];
+      float e[2], w[2][G], x01[2][G];  // weights; times the groups' powers of two; times steps
+      auto weigh = [&]() -> float {  // the largest of what has to stay in range
+        const float ref = m == -INFINITY ? 10.f : 10.f - m;
+        float most = 0.f;
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        float big = 1.f;
+        for (int b = 0; b < 2; ++b) {
+          e[b] = ex2(z[b] + ref);
+          most = fmaxf(most, e[b]);
 #pragma unroll
-        for (int i = 0; i < G; ++i) big = fmaxf(big, pair_size(pair_values(vpair[b][i], T{}), T{}) * unit[i]);
-        zs[b] = z[b] + lg2(big);
-      }
-      if (warp_max(fmaxf(zs[0], zs[1])) > m + 4.f) {
-        const float m_new = fmaxf(m, ceilf(warp_max(fmaxf(z[0], z[1])))), up = m_new - m;
+          for (int i = 0; i < G; ++i) {
+            const float2 pv = pair_values(vpair[b][i], T{});
+            w[b][i] = e[b] * unit[i];
+            x01[b][i] = w[b][i] * pv.y;
+            most = fmaxf(most, w[b][i] * pair_size(pv, T{}));
+          }
+        }
+        return most;
+      };
+      const bool begins = m == -INFINITY;  // nothing but 0 or NaN is summed yet
+      const float most = warp_max(weigh());
+      if (begins || most > 16384.f) {
+        const float m_new = fmaxf(m, ceilf(warp_max(fmaxf(z[0], z[1])))), up = begins ? INFINITY : m_new - m;
         float f = 1.f;  // group t's
 #pragma unroll
         for (int i = 0; i < G; ++i) {
           const float s0 = pair_size(pair_values(vpair[0][i], T{}), T{}), s1 = pair_size(pair_values(vpair[1][i], T{}), T{});
-          const float most = ceilf(warp_max(fmaxf(z[0] + exponent_of(s0), z[1] + exponent_of(s1))));
-          const float was = exponent_of(unit[i]), now = fmaxf(fminf(fminf(was + up, kMostUnit<T>), m_new - most), -126.f);
+          const float top = ceilf(warp_max(fmaxf(z[0] + exponent_of(s0), z[1] + exponent_of(s1))));
+          const float was = exponent_of(unit[i]), now = fmaxf(fminf(fminf(was + up, kMostUnit<T>), m_new - top), -126.f);
           const float fi = ex2(now - was - up);
           unit[i] = power_of_two(now);
           los[i] *= fi;
@@ -592,16 +593,14 @@ __global__ void __launch_bounds__(32, Shape<D>::WARPS)
         for (int i = 0; i < 2 * NT; ++i) o[i] *= f;
         l *= ex2(-up);
         m = m_new;
+        weigh();
       }
-      const float ref = m == -INFINITY ? 10.f : 10.f - m;
-      const float e0 = ex2(z[0] + ref), e1 = ex2(z[1] + ref);
-      l += e0 + e1;
+      l += e[0] + e[1];
       const int at = 8 * (gr & 3) + 2 * t + (gr >> 2);  // of row i = gr + 8 t of the halves: 8 (i % 4) + i / 4
 #pragma unroll
       for (int i = 0; i < G; ++i) {
-        const float2 p0 = pair_values(vpair[0][i], T{}), p1 = pair_values(vpair[1][i], T{});
-        const float w0 = e0 * unit[i], w1 = e1 * unit[i], x0 = w0 * p0.y, x1 = w1 * p1.y;
-        los[i] = fmaf(8.f, x0 + x1, fmaf(w0, p0.x, fmaf(w1, p1.x, los[i])));
+        const float x0 = x01[0][i], x1 = x01[1][i];
+        los[i] = fmaf(8.f, x0 + x1, fmaf(w[0][i], pair_values(vpair[0][i], T{}).x, fmaf(w[1][i], pair_values(vpair[1][i], T{}).x, los[i])));
         const uint32_t h = pack_halves(x0, x1);
         const float2 back = F16T::f2(h);
         pw[2 * i * C::PW + at] = h;
