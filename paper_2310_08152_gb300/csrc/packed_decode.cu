@@ -22,9 +22,9 @@
 // several workers is joined by the last of them to finish, from parts in the workspace, in the workers' order.
 //
 // What bounds it: memory at 96 and 128 columns (100,003 rows of 128, two layers of 32 heads: 155 us, 6.6 TB/s); at 64 columns
-// the instructions beside it (24 layers of 16 x 1,024 rows, 32 heads: 166 us, 6.1 TB/s; the copies alone 150, the arithmetic
+// the instructions beside it (24 layers of 16 x 1,024 rows, 32 heads: 165 us, 6.1 TB/s; the copies alone 150, the arithmetic
 // alone about as long).  A tile of 64 columns takes some 640 instructions of a warp, 300 of them for the codes; the pipe of
-// masks and shifts is busy 55 % of the time, the tensor cores 24 %.  Tried and dropped, at 64 columns: the next tile's logits
+// masks and shifts is busy 54 % of the time, the tensor cores 25 %.  Tried and dropped, at 64 columns: the next tile's logits
 // beside this tile's values (170 -> 175, as that leaves room for twelve workers only), 20 workers with 96 registers (185),
 // codes by a conversion from 8-bit floats (its rate is that of the masks that it would save), all that a worker's first tile
 // depends on in one round of loads (no change).
